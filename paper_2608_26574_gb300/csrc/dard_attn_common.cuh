@@ -12,6 +12,7 @@
 #include <cmath>
 #include <mutex>
 
+#include "dard_host.cuh"
 #include "dard_internal.h"
 #include "dard_ptx.cuh"
 #include "dard_rope.cuh"
@@ -336,20 +337,6 @@ __device__ __forceinline__ void pair_bar_sync(int quarter) {
 
 // ---------------------------------------------------------------- host side
 
-PFN_cuTensorMapEncodeTiled_v12000 encode_fn() {
-  static PFN_cuTensorMapEncodeTiled_v12000 fn = nullptr;
-  static std::once_flag once;
-  std::call_once(once, [] {
-    void* f = nullptr;
-    cudaDriverEntryPointQueryResult q;
-    if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &f, 12000, cudaEnableDefault,
-                                         &q) == cudaSuccess &&
-        q == cudaDriverEntryPointSuccess)
-      fn = reinterpret_cast<PFN_cuTensorMapEncodeTiled_v12000>(f);
-  });
-  return fn;
-}
-
 bool make_map(CUtensorMap* m, const void* ptr, int heads, int d, int rows, int box_rows) {
   auto fn = encode_fn();
   if (!fn) return false;
@@ -362,21 +349,6 @@ bool make_map(CUtensorMap* m, const void* ptr, int heads, int d, int rows, int b
             CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-// cudaFuncSetAttribute once per (kernel, device).
-template <class F>
-cudaError_t ensure_smem_attr(F* kernel, size_t bytes, std::atomic<uint64_t>& done) {
-  int dev = 0;
-  cudaError_t e = cudaGetDevice(&dev);
-  if (e != cudaSuccess) return e;
-  const uint64_t bit = 1ull << (dev & 63);
-  if (done.load(std::memory_order_acquire) & bit) return cudaSuccess;
-  e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                           static_cast<int>(bytes));
-  if (e == cudaSuccess)
-    e = cudaFuncSetAttribute(kernel, cudaFuncAttributePreferredSharedMemoryCarveout, 100);
-  if (e == cudaSuccess) done.fetch_or(bit, std::memory_order_acq_rel);
-  return e;
-}
 // Launch configuration of an attention kernel: an optional cluster of `cluster` CTAs along
 // x, and programmatic dependent launch (pdl: the kernel may start while the RoPE key pass
 // launched before it is still running; its producer waits for that pass before any key
@@ -409,19 +381,6 @@ struct AttnLaunch {
   AttnLaunch(const AttnLaunch&) = delete;
   AttnLaunch& operator=(const AttnLaunch&) = delete;
 };
-
-int sm_count() {
-  static std::atomic<int> cache[64];
-  int dev = 0;
-  if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return 148;
-  int n = cache[dev].load(std::memory_order_relaxed);
-  if (n <= 0) {
-    if (cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess || n <= 0)
-      n = 148;
-    cache[dev].store(n, std::memory_order_relaxed);
-  }
-  return n;
-}
 
 }  // namespace
 }  // namespace dard
