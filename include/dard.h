@@ -313,6 +313,187 @@ dard_status dard_score_and_transition(const dard_score_args* args, void* stream)
 #define DARD_SCORE_NOALLOC_MAX_ROWS 8192
 dard_status dard_score_and_transition_noalloc(const dard_score_args* args, void* stream);
 
+/* ------------------------------------------------------------------------------------- *
+ * The MLP half of a layer with experts, in microscaled 8-bit floating point (MXFP8). The
+ * paper has no counterpart: these are interface additions, for models whose MLP is a mixture
+ * of experts (a dense MLP is the case of one expert). In a layer's order:
+ *
+ *   dard_residual_norm   residual addition, root-mean-square norm, optional MXFP8 output
+ *   dard_mx_quantize     the MXFP8 rounding alone (weights, other activations)
+ *   dard_route           router scores -> experts and weights of each token, and the plan
+ *   dard_experts         the experts' products and the weighted sum over a token's experts
+ *
+ * MXFP8: e4m3 codes, one byte each, with one scale byte for each 32 consecutive elements of
+ * a row. The scale byte b stands for 2^(b - 127) (e8m0). Rounding: b is the smallest for which
+ * max|v| 2^(127 - b) <= 448 (the largest e4m3 value) over the 32 values, at least 0; a code
+ * is v 2^(127 - b) rounded to the nearest e4m3 value, ties to even. A block that holds a NaN
+ * or an infinity gets the scale byte 255 and NaN codes, so that what is computed from it is
+ * NaN. Row lengths are multiples of 32.
+ *
+ * Scale layouts of a [rows, cols] matrix:
+ *   DARD_MX_SCALE_ROWS   row-major bytes [rows, pitch], pitch a multiple of 16, at least
+ *                        cols / 32; the bytes after cols / 32 are not written or used.
+ *   DARD_MX_SCALE_TILES  tiles of 128 rows x 4 scales, 512 bytes each, in the layout that the
+ *                        tensor core's scale copies take: tile (r / 128, c / 4) of
+ *                        [ceil(rows / 128), ceil(cols / 128)] tiles, and in it row r, scale c
+ *                        at byte (r % 32) * 16 + (r % 128) / 32 * 4 + c % 4. Bytes without an
+ *                        element are 0. A batch of matrices stores each matrix's tiles in turn.
+ * ------------------------------------------------------------------------------------- */
+typedef enum { DARD_MX_SCALE_ROWS = 0, DARD_MX_SCALE_TILES = 1 } dard_mx_scale_layout;
+
+/* Residual addition and root-mean-square norm of `rows` rows of `dim` elements:
+ *     r = round(x + delta)                  (round: to dtype; r = x without delta)
+ *     n = r / sqrt(mean(r^2) + eps) * weight
+ *     residual = r,  y = round(n),  (y8, y8_scale) = MXFP8(n)
+ * Sums and n are fp32; n enters the MXFP8 rounding unrounded. A row with a NaN is NaN
+ * throughout; a row with an infinity is NaN there and 0 elsewhere. Strides are in elements.
+ * Rows whose pointers, strides and dim are multiples of 16 bytes (y8: 8 bytes) take 16-byte
+ * accesses, others element accesses. */
+typedef struct {
+  const void* x;             /* device [rows, dim], row stride x_stride                    */
+  const void* delta;         /* optional device [rows, dim]                                */
+  const void* weight;        /* optional device [dim], dtype; NULL means 1                 */
+  void* residual;            /* optional device [rows, dim] out: r; may be x or delta      */
+  void* y;                   /* optional device [rows, dim] out; may be x or delta         */
+  uint8_t* y8;               /* optional device [rows, dim] out: e4m3 codes                */
+  uint8_t* y8_scale;         /* device [rows, y8_scale_stride] out, required with y8       */
+  int32_t dtype;             /* dard_dtype of x, delta, weight, residual and y             */
+  int32_t dim;               /* 1 .. DARD_NORM_MAX_DIM; a multiple of 32 with y8           */
+  int64_t rows;              /* >= 0                                                       */
+  int64_t x_stride, delta_stride, residual_stride, y_stride, y8_stride, y8_scale_stride;
+  float eps;                 /* >= 0, finite                                               */
+} dard_norm_args;
+#define DARD_NORM_MAX_DIM 32768
+
+/* residual and y must be different buffers. One launch. Errors: DARD_ERR_NULL (x, every output
+ * NULL, or y8 without y8_scale), _SHAPE (rows < 0, dim, a stride below dim), _VALUE (dtype,
+ * eps), _ALIGN (x, delta, weight, residual or y not a multiple of the element size;
+ * y8_scale_stride no multiple of 16, y8_scale not 16-byte aligned), _CUDA. */
+dard_status dard_residual_norm(const dard_norm_args* args, void* stream);
+
+/* The MXFP8 rounding of a batch of matrices. One launch (two where the tile layout has bytes
+ * without an element). */
+typedef struct {
+  const void* x;             /* device [batch, rows, cols]                                 */
+  uint8_t* codes;            /* device [batch, rows, cols] out, contiguous                 */
+  uint8_t* scales;           /* device out: layout ROWS [batch * rows, scale_stride],
+                                layout TILES [batch, ceil(rows/128), ceil(cols/128), 512]  */
+  int32_t dtype;             /* dard_dtype of x                                            */
+  int32_t layout;            /* dard_mx_scale_layout                                       */
+  int32_t batch, cols;       /* batch >= 0; cols a positive multiple of 32                 */
+  int64_t rows;              /* of each matrix, >= 0                                       */
+  int64_t x_row_stride, x_batch_stride;  /* elements                                       */
+  int64_t scale_stride;      /* layout ROWS only: a multiple of 16, >= cols / 32           */
+} dard_mx_args;
+
+/* Errors: DARD_ERR_NULL, _SHAPE, _VALUE (dtype, layout), _ALIGN (x no multiple of the element
+ * size; codes or scales not 16-byte aligned; scale_stride no multiple of 16), _CUDA. */
+dard_status dard_mx_quantize(const dard_mx_args* args, void* stream);
+
+/* Routing of tokens to experts. Per token, from its E logits l:
+ *     score     SOFTMAX: softmax(l);  SIGMOID: 1 / (1 + exp(-l))
+ *     choice    score + bias (bias: balances the experts' load; it enters the choice only)
+ *     groups    E experts in `groups` runs of E / groups; with top_groups < groups a group's
+ *               rank is the sum of its two largest choices (its only one if it has one
+ *               expert), and only the top_groups best groups stay
+ *     ids       the top_k largest choices left, in falling order
+ *     weights   their scores; with renormalise divided by their sum (0 if the sum is 0);
+ *               times `scale`
+ * Ties go to the lowest group or expert. A logit of -inf switches its expert off for the token:
+ * it is never chosen (and counts as -inf in its group's rank). Slots for which no expert is
+ * left get id -1 and weight 0. A token with a NaN or +inf logit is invalid: every id -1,
+ * every weight 0, and DARD_STATUS_INVALID_ROW in the status word. Arithmetic is fp32.
+ *
+ * The plan (optional): the (token, slot) pairs token * top_k + slot sorted by expert, pairs of
+ * one expert in rising order. offsets[e] .. offsets[e + 1] are expert e's entries of `rows`;
+ * entries from offsets[experts] on (slots without an expert) are -1. It stays on the device:
+ * dard_experts reads it there, with no host round trip. */
+typedef enum { DARD_ROUTE_SOFTMAX = 0, DARD_ROUTE_SIGMOID = 1 } dard_route_scoring;
+#define DARD_MAX_EXPERTS 512
+#define DARD_MAX_TOP_K 32
+#define DARD_MAX_GROUPS 32
+typedef struct {
+  const void* logits;        /* device [tokens, experts], row stride logits_stride         */
+  int64_t logits_stride;     /* elements, >= experts                                       */
+  const float* bias;         /* optional device [experts]                                  */
+  int32_t dtype;             /* dard_dtype of logits                                       */
+  int32_t scoring;           /* dard_route_scoring                                         */
+  int32_t tokens;            /* >= 0; tokens * top_k at most 2^31 - 1                      */
+  int32_t experts;           /* 1 .. DARD_MAX_EXPERTS                                      */
+  int32_t top_k;             /* 1 .. min(experts, DARD_MAX_TOP_K)                          */
+  int32_t groups;            /* 1 .. DARD_MAX_GROUPS, divides experts                      */
+  int32_t top_groups;        /* 1 .. groups                                                */
+  int32_t renormalise;       /* 0 or 1                                                     */
+  float scale;               /* finite                                                     */
+  int32_t* ids;              /* device [tokens, top_k] out                                 */
+  float* weights;            /* device [tokens, top_k] out                                 */
+  int32_t* offsets;          /* optional device [experts + 1] out                          */
+  int32_t* rows;             /* device [tokens * top_k] out, required with offsets         */
+  uint32_t* status;          /* optional device word, DARD_STATUS_* bits OR-ed in          */
+  void* workspace;           /* device scratch of dard_route_workspace_size() bytes (with
+                                offsets); needs no preparation. Calls that overlap on the
+                                GPU need separate workspaces.                              */
+  size_t workspace_bytes;
+} dard_route_args;
+
+/* Bytes of workspace a call with these sizes needs (0 where it needs none, or on invalid
+ * sizes). */
+size_t dard_route_workspace_size(int32_t tokens, int32_t experts, int32_t top_k);
+
+/* One launch for few tokens or without the plan, else two. Errors: DARD_ERR_NULL, _SHAPE,
+ * _VALUE, _ALIGN (logits no multiple of the element size), _WORKSPACE, _CUDA. */
+dard_status dard_route(const dard_route_args* args, void* stream);
+
+/* The experts' products. For token t and slot s with expert e = ids[t, s] >= 0:
+ *     h = silu(w1[e] x_t) * (w3[e] x_t)       silu(g) = g / (1 + exp(-g))
+ *     o = w2[e] MXFP8(h)                      (dtype BF16: w2[e] round(h))
+ *     y_t = sum_s weights[t, s] o             (slots with id -1 add nothing)
+ * x and the weights are MXFP8 (dtype DARD_MXFP8: e4m3 codes, x_scale by rows, weight scales
+ * in tiles) or bf16 (dtype DARD_BF16, the scales unused). Products and sums are fp32 on the
+ * tcgen05 tensor cores; the block scales are applied by the matrix instruction. The products of
+ * one token's experts are added in slot order, so that equal calls give equal bits.
+ * ids, weights, offsets and rows are what dard_route writes. */
+#define DARD_MXFP8 2         /* a dtype of dard_experts_args only                          */
+typedef struct {
+  const void* x;             /* device [tokens, dim], row stride x_stride                  */
+  const uint8_t* x_scale;    /* device [tokens, x_scale_stride]                            */
+  const void* w1;            /* device [experts, hidden, dim]: the gate                    */
+  const void* w3;            /* device [experts, hidden, dim]: the value the gate scales   */
+  const void* w2;            /* device [experts, dim, hidden]                              */
+  const uint8_t* w1_scale;   /* device, layout TILES of [experts] matrices                 */
+  const uint8_t* w3_scale;
+  const uint8_t* w2_scale;
+  const int32_t* ids;        /* device [tokens, top_k]                                     */
+  const float* weights;      /* device [tokens, top_k]                                     */
+  const int32_t* offsets;    /* device [experts + 1]                                       */
+  const int32_t* rows;       /* device [tokens * top_k]                                    */
+  void* y;                   /* device [tokens, dim] out, row stride y_stride              */
+  int64_t x_stride, x_scale_stride, y_stride;   /* elements                                */
+  int32_t dtype;             /* DARD_MXFP8 or DARD_BF16                                    */
+  int32_t y_dtype;           /* dard_dtype of y                                            */
+  int32_t tokens;            /* >= 0; tokens * top_k at most 2^24                          */
+  int32_t experts;           /* 1 .. DARD_MAX_EXPERTS                                      */
+  int32_t top_k;             /* 1 .. min(experts, DARD_MAX_TOP_K)                          */
+  int32_t dim, hidden;       /* multiples of 32, at most DARD_EXPERTS_MAX_DIM              */
+  void* workspace;           /* device scratch of dard_experts_workspace_size() bytes, 256-byte
+                                aligned; needs no preparation. Calls that overlap on the GPU
+                                need separate workspaces.                                  */
+  size_t workspace_bytes;
+  uint32_t* status;          /* optional device word: DARD_STATUS_TIMEOUT                  */
+} dard_experts_args;
+#define DARD_EXPERTS_MAX_DIM 65536
+
+/* Bytes of workspace for these sizes and either dtype (0 on invalid sizes): the product in
+ * between, and the products of each (token, slot) pair before their sum. */
+size_t dard_experts_workspace_size(int32_t tokens, int32_t experts, int32_t top_k, int32_t dim,
+                                   int32_t hidden);
+
+/* Three launches, chained by programmatic dependent launch. x, the weights and their scales
+ * must be 16-byte aligned, with x_stride and x_scale_stride multiples of 16 bytes; y and
+ * y_stride multiples of 16 bytes. Entries of rows outside [0, tokens * top_k) are skipped.
+ * Errors: DARD_ERR_NULL, _SHAPE, _VALUE (dtype), _ALIGN, _WORKSPACE, _CUDA. */
+dard_status dard_experts(const dard_experts_args* args, void* stream);
+
 /* Human-readable name of a status code; never NULL. */
 const char* dard_status_string(dard_status s);
 

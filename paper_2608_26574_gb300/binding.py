@@ -21,6 +21,11 @@ ORDER_CONFIDENCE, ORDER_BIDIR, ORDER_L2R, ORDER_ENTROPY, ORDER_MARGIN = 0, 1, 2,
 STATUS_BAD_STATE, STATUS_BAD_SHADOW, STATUS_INVALID_ROW, STATUS_TIMEOUT = 0x1, 0x2, 0x4, 0x8
 MAX_SEQS, MAX_BLOCK = 256, 128
 SCORE_NOALLOC_MAX_ROWS = 8192
+DARD_MXFP8 = 2  # dard_experts only
+MX_SCALE_ROWS, MX_SCALE_TILES = 0, 1
+ROUTE_SOFTMAX, ROUTE_SIGMOID = 0, 1
+MX_BLOCK = 32
+NORM_MAX_DIM, MAX_EXPERTS, MAX_TOP_K, MAX_GROUPS = 32768, 512, 32, 32
 
 _I32P = ctypes.POINTER(ctypes.c_int32)
 
@@ -56,6 +61,45 @@ class ScoreArgs(ctypes.Structure):
                 ("order_key", ctypes.c_void_p), ("order_mode", ctypes.c_int32)]
 
 
+class NormArgs(ctypes.Structure):
+    _fields_ = ([(n, ctypes.c_void_p) for n in ("x", "delta", "weight", "residual", "y", "y8",
+                                                "y8_scale")] +
+                [("dtype", ctypes.c_int32), ("dim", ctypes.c_int32), ("rows", ctypes.c_int64)] +
+                [(n, ctypes.c_int64) for n in ("x_stride", "delta_stride", "residual_stride",
+                                               "y_stride", "y8_stride", "y8_scale_stride")] +
+                [("eps", ctypes.c_float)])
+
+
+class MxArgs(ctypes.Structure):
+    _fields_ = [("x", ctypes.c_void_p), ("codes", ctypes.c_void_p), ("scales", ctypes.c_void_p),
+                ("dtype", ctypes.c_int32), ("layout", ctypes.c_int32),
+                ("batch", ctypes.c_int32), ("cols", ctypes.c_int32), ("rows", ctypes.c_int64),
+                ("x_row_stride", ctypes.c_int64), ("x_batch_stride", ctypes.c_int64),
+                ("scale_stride", ctypes.c_int64)]
+
+
+class RouteArgs(ctypes.Structure):
+    _fields_ = ([("logits", ctypes.c_void_p), ("logits_stride", ctypes.c_int64),
+                 ("bias", ctypes.c_void_p)] +
+                [(n, ctypes.c_int32) for n in ("dtype", "scoring", "tokens", "experts", "top_k",
+                                               "groups", "top_groups", "renormalise")] +
+                [("scale", ctypes.c_float)] +
+                [(n, ctypes.c_void_p) for n in ("ids", "weights", "offsets", "rows", "status",
+                                                "workspace")] +
+                [("workspace_bytes", ctypes.c_size_t)])
+
+
+class ExpertsArgs(ctypes.Structure):
+    _fields_ = ([(n, ctypes.c_void_p) for n in ("x", "x_scale", "w1", "w3", "w2", "w1_scale",
+                                                "w3_scale", "w2_scale", "ids", "weights",
+                                                "offsets", "rows", "y")] +
+                [(n, ctypes.c_int64) for n in ("x_stride", "x_scale_stride", "y_stride")] +
+                [(n, ctypes.c_int32) for n in ("dtype", "y_dtype", "tokens", "experts", "top_k",
+                                               "dim", "hidden")] +
+                [("workspace", ctypes.c_void_p), ("workspace_bytes", ctypes.c_size_t),
+                 ("status", ctypes.c_void_p)])
+
+
 class DardError(RuntimeError):
     def __init__(self, code: int, fn: str, message: str):
         super().__init__(f"{fn} failed: {status_string(code)}: {message}")
@@ -79,6 +123,12 @@ EXPORTS = {
     "dard_score_and_transition_noalloc": (ctypes.c_int, [ctypes.POINTER(ScoreArgs),
                                                          ctypes.c_void_p]),
     "dard_score_workspace_size": (ctypes.c_size_t, [ctypes.c_int32, ctypes.c_int32, ctypes.c_int32]),
+    "dard_residual_norm": (ctypes.c_int, [ctypes.POINTER(NormArgs), ctypes.c_void_p]),
+    "dard_mx_quantize": (ctypes.c_int, [ctypes.POINTER(MxArgs), ctypes.c_void_p]),
+    "dard_route_workspace_size": (ctypes.c_size_t, [ctypes.c_int32] * 3),
+    "dard_route": (ctypes.c_int, [ctypes.POINTER(RouteArgs), ctypes.c_void_p]),
+    "dard_experts_workspace_size": (ctypes.c_size_t, [ctypes.c_int32] * 5),
+    "dard_experts": (ctypes.c_int, [ctypes.POINTER(ExpertsArgs), ctypes.c_void_p]),
     "dard_status_string": (ctypes.c_char_p, [ctypes.c_int]),
     "dard_last_error": (ctypes.c_char_p, []),
     "dard_version": (ctypes.c_int32, []),
@@ -403,3 +453,292 @@ def dard_score_and_transition_noalloc(logits_x, logits_s, block_len, state_in, t
     (at most ``SCORE_NOALLOC_MAX_ROWS`` block rows; calls that overlap on one device race)."""
     ScoreCall(block_len, state_in, tau_c, tau_u, lam, p0, conf, token, state_out, None,
               w_out=w_out, counts=counts, status=status)(logits_x, logits_s, stream)
+
+
+# ------------------------------------------------------------------ experts' MLP (MXFP8)
+def mx_scale_shape(shape, layout: int = MX_SCALE_ROWS) -> tuple:
+    """Shape of the uint8 scale tensor of a [rows, cols] matrix or a [batch, rows, cols] batch:
+    layout ROWS [..., rows, cols / 32 rounded up to 16], layout TILES [..., row tiles, column
+    tiles, 512]."""
+    *lead, rows, cols = shape
+    if cols % MX_BLOCK:
+        raise ValueError(f"rows of {cols} elements are no multiple of {MX_BLOCK}")
+    if layout == MX_SCALE_ROWS:
+        return (*lead, rows, -(-cols // (16 * MX_BLOCK)) * 16)
+    return (*lead, -(-rows // 128), -(-cols // 128), 512)
+
+
+def _is_dtype(t, name: str, *dtypes):
+    if t.dtype not in dtypes:
+        raise ValueError(f"{name}: {' or '.join(str(d) for d in dtypes)} expected, got {t.dtype}")
+
+
+def _codes_dtypes():
+    torch = _torch()
+    return torch.float8_e4m3fn, torch.uint8
+
+
+def _scale_dtypes():
+    torch = _torch()
+    return torch.uint8, torch.float8_e8m0fnu
+
+
+def _matrix(t, name: str, rows: int, cols: int, device: int) -> tuple[int, int]:
+    """(pointer, row stride) of a 2-D device tensor [rows, at least cols] with contiguous rows."""
+    if not t.is_cuda:
+        raise ValueError(f"{name}: device tensor expected")
+    if t.get_device() != device:
+        raise ValueError(f"{name}: on device {t.get_device()}, expected {device}")
+    shp = t.shape
+    if len(shp) != 2 or shp[0] != rows or shp[1] < cols:
+        raise ValueError(f"{name}: [{rows}, {cols}] expected, got {tuple(shp)}")
+    stride = t.stride(0)
+    if shp[0] <= 1 or shp[1] == 0:
+        stride = max(stride, shp[1])  # no second row to step to
+    elif stride < shp[1]:
+        raise ValueError(f"{name}: rows overlap (row stride {stride})")
+    if shp[1] > 1 and t.stride(1) != 1:
+        raise ValueError(f"{name}: contiguous rows expected")
+    return t.data_ptr(), stride
+
+
+class NormCall:
+    """``dard_residual_norm`` with the weight and epsilon of one norm marshalled once.
+
+    Call it with ``x`` [rows, dim] and any of the outputs: ``residual`` receives x + ``delta``
+    (x itself without delta) and may be x or delta; ``y`` the norm in x's dtype; ``y8`` (e4m3 or
+    uint8) and ``y8_scale`` (layout ROWS, see ``mx_scale_shape``) the norm in MXFP8."""
+
+    def __init__(self, dim: int, dtype, weight=None, eps: float = 1e-6):
+        torch = _torch()
+        if dtype not in (torch.bfloat16, torch.float32):
+            raise ValueError(f"unsupported dtype {dtype}")
+        self.dim, self.dtype = dim, dtype
+        a = NormArgs()
+        a.dim, a.eps = dim, eps
+        a.dtype = DARD_BF16 if dtype == torch.bfloat16 else DARD_F32
+        self.device = None if weight is None else weight.get_device()
+        if weight is not None and weight.numel() != dim:
+            raise ValueError(f"weight: {dim} elements expected, got {weight.numel()}")
+        a.weight = _dev(weight, "weight", dim, dtype)
+        self._weight = weight
+        self._codes, self._scales = _codes_dtypes(), _scale_dtypes()
+        self._args, self._ref = a, ctypes.byref(a)
+        self._fn = lib().dard_residual_norm
+
+    def __call__(self, x, delta=None, residual=None, y=None, y8=None, y8_scale=None, stream=None):
+        a, dim, dt = self._args, self.dim, self.dtype
+        rows, dev = x.shape[0], x.get_device()
+        if x.shape[-1] != dim:
+            raise ValueError(f"x: rows of {dim} elements expected, got {tuple(x.shape)}")
+        if self.device is not None and dev != self.device:
+            raise ValueError(f"x: on device {dev}, the weight on {self.device}")
+        a.rows = rows
+        a.x, a.x_stride = _matrix(x, "x", rows, dim, dev)
+        if x.dtype != dt:
+            raise ValueError(f"x: {dt} expected, got {x.dtype}")
+        for name, t in (("delta", delta), ("residual", residual), ("y", y)):
+            if t is None:
+                setattr(a, name, None)
+                continue
+            if t.dtype != dt or t.shape[-1] != dim:
+                raise ValueError(f"{name}: {dt} [{rows}, {dim}] expected, got {t.dtype} "
+                                 f"{tuple(t.shape)}")
+            ptr, stride = _matrix(t, name, rows, dim, dev)
+            setattr(a, name, ptr)
+            setattr(a, name + "_stride", stride)
+        a.y8 = a.y8_scale = None
+        if y8 is not None:
+            if y8_scale is None:
+                raise ValueError("y8 needs y8_scale")
+            _is_dtype(y8, "y8", *self._codes)
+            _is_dtype(y8_scale, "y8_scale", *self._scales)
+            if y8.shape[-1] != dim:
+                raise ValueError(f"y8: [{rows}, {dim}] expected, got {tuple(y8.shape)}")
+            a.y8, a.y8_stride = _matrix(y8, "y8", rows, dim, dev)
+            a.y8_scale, a.y8_scale_stride = _matrix(y8_scale, "y8_scale", rows, dim // MX_BLOCK, dev)
+        _check(self._fn(self._ref, _stream_handle(stream, dev)), "dard_residual_norm")
+
+
+def dard_residual_norm(x, delta=None, weight=None, eps: float = 1e-6, residual=None, y=None,
+                       y8=None, y8_scale=None, stream=None):
+    """Residual addition and root-mean-square norm of the rows of x, see ``NormCall``."""
+    NormCall(x.shape[-1], x.dtype, weight, eps)(x, delta, residual, y, y8, y8_scale, stream)
+
+
+def dard_mx_quantize(x, codes, scales, layout: int = MX_SCALE_ROWS, stream=None):
+    """MXFP8 rounding of x [rows, cols] or [batch, rows, cols] (contiguous rows, any row and batch
+    stride) into contiguous ``codes`` of x's shape and ``scales`` of ``mx_scale_shape``."""
+    if not x.is_cuda:
+        raise ValueError("x: device tensor expected")
+    dev, shp = x.get_device(), x.shape
+    if len(shp) not in (2, 3) or (shp[-1] > 1 and x.stride(-1) != 1):
+        raise ValueError("x: [rows, cols] or [batch, rows, cols] with contiguous rows expected")
+    if codes.shape != shp:
+        raise ValueError(f"codes: {tuple(shp)} expected, got {tuple(codes.shape)}")
+    if layout not in (MX_SCALE_ROWS, MX_SCALE_TILES):
+        raise ValueError(f"layout {layout} is neither MX_SCALE_ROWS nor MX_SCALE_TILES")
+    want = mx_scale_shape(shp, layout)
+    if layout == MX_SCALE_TILES and tuple(scales.shape) != want:
+        raise ValueError(f"scales: {want} expected, got {tuple(scales.shape)}")
+    if layout == MX_SCALE_ROWS and (scales.shape[:-1] != shp[:-1] or
+                                    scales.shape[-1] < shp[-1] // MX_BLOCK):
+        raise ValueError(f"scales: {want} expected, got {tuple(scales.shape)}")
+    _is_dtype(codes, "codes", *_codes_dtypes())
+    _is_dtype(scales, "scales", *_scale_dtypes())
+    a = MxArgs()
+    a.x, a.dtype, a.layout = x.data_ptr(), _dtype_code(x), layout
+    a.codes = _dev(codes, "codes", 0, codes.dtype, dev)
+    a.scales = _dev(scales, "scales", 0, scales.dtype, dev)
+    a.batch = shp[0] if len(shp) == 3 else 1
+    a.rows, a.cols = shp[-2], shp[-1]
+    # a stride that no step uses may be anything
+    a.x_row_stride = x.stride(-2) if shp[-2] > 1 else shp[-1]
+    a.x_batch_stride = x.stride(0) if a.batch > 1 and len(shp) == 3 else 0
+    a.scale_stride = scales.shape[-1] if layout == MX_SCALE_ROWS else 0
+    _check(lib().dard_mx_quantize(ctypes.byref(a), _stream_handle(stream, dev)),
+           "dard_mx_quantize")
+
+
+def dard_route_workspace_size(tokens: int, experts: int, top_k: int) -> int:
+    return int(lib().dard_route_workspace_size(tokens, experts, top_k))
+
+
+class RouteCall:
+    """``dard_route`` with a router's settings and its bias marshalled once.
+
+    Call it with logits [tokens, experts] (bf16 or fp32, contiguous rows), ``ids`` and
+    ``weights`` [tokens, top_k], and, for the plan that ``ExpertsCall`` reads, ``offsets``
+    [experts + 1] and ``rows`` [tokens * top_k]. The workspace holds
+    ``dard_route_workspace_size`` bytes for the most tokens of a call with a plan."""
+
+    def __init__(self, experts: int, top_k: int, scoring: int = ROUTE_SOFTMAX, bias=None,
+                 groups: int = 1, top_groups: int = 1, renormalise: bool = True,
+                 scale: float = 1.0, workspace=None, status=None):
+        torch = _torch()
+        self.experts, self.top_k = experts, top_k
+        self._i32, self._f32 = torch.int32, torch.float32
+        a = RouteArgs()
+        self.device = next((t.get_device() for t in (bias, workspace, status) if t is not None), None)
+        a.bias = _dev(bias, "bias", experts, torch.float32, self.device)
+        a.status = _dev(status, "status", 1, torch.int32, self.device)
+        a.scoring, a.experts, a.top_k, a.groups = scoring, experts, top_k, groups
+        a.top_groups, a.renormalise, a.scale = top_groups, 1 if renormalise else 0, scale
+        if workspace is not None:
+            a.workspace = _dev(workspace, "workspace", 0, workspace.dtype, self.device)
+            a.workspace_bytes = workspace.numel() * workspace.element_size()
+        self._keep = (bias, workspace, status)
+        self._args, self._ref = a, ctypes.byref(a)
+        self._fn = lib().dard_route
+
+    def __call__(self, logits, ids, weights, offsets=None, rows=None, stream=None):
+        a, k = self._args, self.top_k
+        tokens, dev = logits.shape[0], logits.get_device()
+        if logits.dim() != 2 or logits.shape[1] != self.experts:
+            raise ValueError(f"logits: [tokens, {self.experts}] expected, got {tuple(logits.shape)}")
+        if self.device is not None and dev != self.device:
+            raise ValueError(f"logits: on device {dev}, expected {self.device}")
+        a.logits, a.logits_stride = _matrix(logits, "logits", tokens, self.experts, dev)
+        a.dtype, a.tokens = _dtype_code(logits), tokens
+        if ids.shape != (tokens, k) or weights.shape != (tokens, k):
+            raise ValueError(f"ids and weights: [{tokens}, {k}] expected, got {tuple(ids.shape)}, "
+                             f"{tuple(weights.shape)}")
+        a.ids = _dev(ids, "ids", tokens * k, self._i32, dev)
+        a.weights = _dev(weights, "weights", tokens * k, self._f32, dev)
+        if (offsets is None) != (rows is None):
+            raise ValueError("offsets and rows come together")
+        a.offsets = _dev(offsets, "offsets", self.experts + 1, self._i32, dev)
+        a.rows = _dev(rows, "rows", tokens * k, self._i32, dev)
+        _check(self._fn(self._ref, _stream_handle(stream, dev)), "dard_route")
+
+
+def dard_route(logits, ids, weights, top_k: int, scoring: int = ROUTE_SOFTMAX, bias=None,
+               groups: int = 1, top_groups: int = 1, renormalise: bool = True, scale: float = 1.0,
+               offsets=None, rows=None, workspace=None, status=None, stream=None):
+    """Experts and weights of each row of logits, and the plan, see ``RouteCall``."""
+    RouteCall(logits.shape[-1], top_k, scoring, bias, groups, top_groups, renormalise, scale,
+              workspace, status)(logits, ids, weights, offsets, rows, stream)
+
+
+def dard_experts_workspace_size(tokens: int, experts: int, top_k: int, dim: int,
+                                hidden: int) -> int:
+    return int(lib().dard_experts_workspace_size(tokens, experts, top_k, dim, hidden))
+
+
+class ExpertsCall:
+    """``dard_experts`` with one layer's weights and the workspace marshalled once.
+
+    w1 and w3 are [experts, hidden, dim], w2 [experts, dim, hidden], contiguous: bf16 (scales
+    None), or e4m3 / uint8 codes with uint8 / e8m0 scales in layout TILES (``dard_mx_quantize``).
+    Call it with x [tokens, dim] (x_scale in layout ROWS for MXFP8), the outputs of a
+    ``RouteCall`` and y [tokens, dim] in bf16 or fp32. The workspace holds
+    ``dard_experts_workspace_size`` bytes for every token count that calls use."""
+
+    def __init__(self, w1, w1_scale, w3, w3_scale, w2, w2_scale, workspace, status=None):
+        torch = _torch()
+        if w1.dim() != 3 or w3.shape != w1.shape or tuple(w2.shape) != (
+                w1.shape[0], w1.shape[2], w1.shape[1]):
+            raise ValueError("w1 and w3 [experts, hidden, dim] and w2 [experts, dim, hidden] expected, "
+                             f"got {tuple(w1.shape)}, {tuple(w3.shape)}, {tuple(w2.shape)}")
+        self.experts, self.hidden, self.dim = w1.shape
+        self.mx = w1.dtype != torch.bfloat16
+        self._codes, self._scales = _codes_dtypes(), _scale_dtypes()
+        self._i32, self._f32, self._bf16 = torch.int32, torch.float32, torch.bfloat16
+        self.device = dev = w1.get_device()
+        a = ExpertsArgs()
+        for name, w, s in (("w1", w1, w1_scale), ("w3", w3, w3_scale), ("w2", w2, w2_scale)):
+            _is_dtype(w, name, *(self._codes if self.mx else (self._bf16,)))
+            setattr(a, name, _dev(w, name, w.numel(), w.dtype, dev))
+            if not self.mx:
+                if s is not None:
+                    raise ValueError(f"{name}_scale: bf16 weights have no scales")
+                continue
+            if s is None:
+                raise ValueError(f"{name}_scale: needed with 8-bit weights")
+            want = mx_scale_shape(w.shape, MX_SCALE_TILES)
+            _is_dtype(s, name + "_scale", *self._scales)
+            if tuple(s.shape) != want:
+                raise ValueError(f"{name}_scale: {want} expected, got {tuple(s.shape)}")
+            setattr(a, name + "_scale", _dev(s, name + "_scale", s.numel(), s.dtype, dev))
+        a.experts, a.hidden, a.dim = self.experts, self.hidden, self.dim
+        a.dtype = DARD_MXFP8 if self.mx else DARD_BF16
+        if workspace is None:
+            raise ValueError("workspace is required (see dard_experts_workspace_size)")
+        a.workspace = _dev(workspace, "workspace", 0, workspace.dtype, dev)
+        a.workspace_bytes = workspace.numel() * workspace.element_size()
+        a.status = _dev(status, "status", 1, torch.int32, dev)
+        self._keep = (w1, w1_scale, w3, w3_scale, w2, w2_scale, workspace, status)
+        self._args, self._ref = a, ctypes.byref(a)
+        self._fn = lib().dard_experts
+
+    def __call__(self, x, x_scale, ids, weights, offsets, rows, y, stream=None):
+        a, dev, dim = self._args, self.device, self.dim
+        tokens, k = ids.shape
+        if x.shape[-1] != dim or y.shape[-1] != dim:
+            raise ValueError(f"x and y: rows of {dim} elements expected, got {tuple(x.shape)}, "
+                             f"{tuple(y.shape)}")
+        _is_dtype(x, "x", *(self._codes if self.mx else (self._bf16,)))
+        a.x, a.x_stride = _matrix(x, "x", tokens, dim, dev)
+        if self.mx:
+            if x_scale is None:
+                raise ValueError("x_scale: needed with 8-bit weights")
+            _is_dtype(x_scale, "x_scale", *self._scales)
+            a.x_scale, a.x_scale_stride = _matrix(x_scale, "x_scale", tokens, dim // MX_BLOCK, dev)
+        _is_dtype(y, "y", self._bf16, self._f32)
+        a.y, a.y_stride = _matrix(y, "y", tokens, dim, dev)
+        a.y_dtype = DARD_BF16 if y.dtype == self._bf16 else DARD_F32
+        if weights.shape != ids.shape:
+            raise ValueError(f"weights: {tuple(ids.shape)} expected, got {tuple(weights.shape)}")
+        a.tokens, a.top_k = tokens, k
+        a.ids = _dev(ids, "ids", tokens * k, self._i32, dev)
+        a.weights = _dev(weights, "weights", tokens * k, self._f32, dev)
+        a.offsets = _dev(offsets, "offsets", self.experts + 1, self._i32, dev)
+        a.rows = _dev(rows, "rows", tokens * k, self._i32, dev)
+        _check(self._fn(self._ref, _stream_handle(stream, dev)), "dard_experts")
+
+
+def dard_experts(x, x_scale, w1, w1_scale, w3, w3_scale, w2, w2_scale, ids, weights, offsets,
+                 rows, y, workspace, status=None, stream=None):
+    """The experts' products of every token, weighted and added, see ``ExpertsCall``."""
+    ExpertsCall(w1, w1_scale, w3, w3_scale, w2, w2_scale, workspace, status)(
+        x, x_scale, ids, weights, offsets, rows, y, stream)
