@@ -8,7 +8,9 @@ This drives the library's two entry points the way a diffusion LLM would, step a
   MLP are plain library GEMMs (torch / cuBLAS); every attention layer is
   ``dard_step_attention`` over the augmented sequence x~_t = (x_t; s_t) of Sec. 3.1. The
   shadow rows hold the mask token (s_t is fully masked) and take the positions of the
-  block positions they copy (shared positional embedding).
+  block positions they copy (shared positional embedding). With ``experts`` > 0 the MLP is a
+  mixture of experts in MXFP8 (``experts.ExpertMLP``): the residual additions, norms, routing and
+  experts' products then run in the library's kernels too.
 * ``decode`` runs Algorithm 1 block by block (semi-autoregressive blocks of ``block_len``
   positions): each step builds the augmented input, runs the model, and calls
   ``dard_score_and_transition`` with the end-of-step outputs in place (states, the block's
@@ -32,6 +34,7 @@ import numpy as np
 import torch
 
 from . import binding as B
+from .experts import ExpertMLP
 
 
 @dataclass
@@ -46,6 +49,10 @@ class ModelConfig:
     dtype: str = "bf16"           # "bf16" (tensor-core attention) or "f32" (CUDA-core)
     logit_scale: float = 4.0      # sharpens the random LM head so that some predictions
     rope_base: float = 10000.0    # are confident enough to cross the thresholds
+    experts: int = 0              # 0: the dense MLP; else a mixture of this many experts with
+    top_k: int = 2                # `mlp` hidden elements each, top_k of them per row
+    expert_mx: bool = True        # the experts' products in MXFP8 (else bf16)
+    expert_scoring: int = B.ROUTE_SOFTMAX
 
     @property
     def mask_token(self) -> int:
@@ -67,12 +74,24 @@ class DLLM:
         d, hd = cfg.d_model, cfg.head_dim
         self.emb = w(cfg.vocab, d, fan_in=1)
         self.layers = []
+        # experts only: the layers' shared buffers and their status word
+        workspaces: dict = {}
+        self.status = torch.zeros(1, dtype=torch.int32, device=self.device)
+        self.norm = B.NormCall(d, self.dt) if cfg.experts > 0 else None
         for _ in range(cfg.n_layers):
             self.layers.append(dict(
                 wq=w(d, cfg.hq * hd, fan_in=d), wk=w(d, cfg.hkv * hd, fan_in=d),
-                wv=w(d, cfg.hkv * hd, fan_in=d), wo=w(cfg.hq * hd, d, fan_in=cfg.hq * hd),
-                w1=w(d, cfg.mlp, fan_in=d), w3=w(d, cfg.mlp, fan_in=d),
-                w2=w(cfg.mlp, d, fan_in=cfg.mlp)))
+                wv=w(d, cfg.hkv * hd, fan_in=d), wo=w(cfg.hq * hd, d, fan_in=cfg.hq * hd)))
+            if cfg.experts > 0:
+                e, f = cfg.experts, cfg.mlp
+                self.layers[-1]["mlp"] = ExpertMLP(
+                    w(e, f, d, fan_in=d), w(e, f, d, fan_in=d), w(e, d, f, fan_in=f),
+                    w(d, e, fan_in=d), cfg.top_k, mx=cfg.expert_mx,
+                    route=dict(scoring=cfg.expert_scoring), status=self.status,
+                    workspaces=workspaces)
+            else:
+                self.layers[-1].update(w1=w(d, cfg.mlp, fan_in=d), w3=w(d, cfg.mlp, fan_in=d),
+                                       w2=w(cfg.mlp, d, fan_in=cfg.mlp))
         self.head = w(d, cfg.vocab, fan_in=d)
 
     @staticmethod
@@ -94,8 +113,13 @@ class DLLM:
                                     batch.shadow_src, status=batch.status,
                                     rope_theta=cfg.rope_base,
                                     rope_style=B.DARD_ROPE_INTERLEAVED)
+        delta = None  # experts only: the last MLP's output, not yet added to h
         for L in self.layers:
-            a = self.rmsnorm(h)
+            if cfg.experts > 0:
+                a = torch.empty_like(h)
+                self.norm(h, delta, residual=h if delta is not None else None, y=a)
+            else:
+                a = self.rmsnorm(h)
             q = (a @ L["wq"]).view(rows, cfg.hq, cfg.head_dim).contiguous()
             k = (a @ L["wk"]).view(rows, cfg.hkv, cfg.head_dim).contiguous()
             v = (a @ L["wv"]).view(rows, cfg.hkv, cfg.head_dim).contiguous()
@@ -104,10 +128,16 @@ class DLLM:
             attention(q, k, v, o, k_rope=k_rope)
             if need_attn_out:
                 attn_outs.append((q, k, v, o))
+            if cfg.experts > 0:
+                delta = L["mlp"](h, o.view(rows, cfg.hq * cfg.head_dim) @ L["wo"])
+                continue
             h = h + o.view(rows, cfg.hq * cfg.head_dim) @ L["wo"]
             m = self.rmsnorm(h)
             h = h + (torch.nn.functional.silu(m @ L["w1"]) * (m @ L["w3"])) @ L["w2"]
-        h = self.rmsnorm(h)
+        if cfg.experts > 0:
+            self.norm(h, delta, y=h)
+        else:
+            h = self.rmsnorm(h)
         hx = h[batch.x_rows]
         hs = h[batch.s_rows]
         lx = (hx @ self.head) * cfg.logit_scale
@@ -281,6 +311,11 @@ def main():
     ap.add_argument("--heads", type=int, default=32)
     ap.add_argument("--vocab", type=int, default=126464)
     ap.add_argument("--mlp", type=int, default=12288)
+    ap.add_argument("--experts", type=int, default=0,
+                    help="experts of each layer's MLP, --mlp hidden elements each (0: dense)")
+    ap.add_argument("--top-k", type=int, default=2, help="experts per row")
+    ap.add_argument("--expert-bf16", action="store_true",
+                    help="the experts' products in bf16 instead of MXFP8")
     ap.add_argument("--logit-scale", type=float, default=24.0)
     ap.add_argument("--order", type=int, default=B.ORDER_CONFIDENCE)
     ap.add_argument("--min-progress", action="store_true")
@@ -292,7 +327,8 @@ def main():
     Bu.build()
     cfg = ModelConfig(vocab=args.vocab, d_model=args.d_model, n_layers=args.layers,
                       hq=args.heads, hkv=args.heads, head_dim=128, mlp=args.mlp,
-                      logit_scale=args.logit_scale)
+                      logit_scale=args.logit_scale, experts=args.experts, top_k=args.top_k,
+                      expert_mx=not args.expert_bf16)
     model = DLLM(cfg, seed=args.seed)
     rng = np.random.default_rng(args.seed)
     prompts = [rng.integers(0, cfg.vocab - 1, size=args.prompt).astype(np.int32)
