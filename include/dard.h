@@ -415,7 +415,7 @@ typedef enum { DARD_ROUTE_SOFTMAX = 0, DARD_ROUTE_SIGMOID = 1 } dard_route_scori
 typedef struct {
   const void* logits;        /* device [tokens, experts], row stride logits_stride         */
   int64_t logits_stride;     /* elements, >= experts                                       */
-  const float* bias;         /* optional device [experts]                                  */
+  const float* bias;         /* optional device [experts], finite                          */
   int32_t dtype;             /* dard_dtype of logits                                       */
   int32_t scoring;           /* dard_route_scoring                                         */
   int32_t tokens;            /* >= 0; tokens * top_k at most 2^31 - 1                      */
@@ -430,9 +430,9 @@ typedef struct {
   int32_t* offsets;          /* optional device [experts + 1] out                          */
   int32_t* rows;             /* device [tokens * top_k] out, required with offsets         */
   uint32_t* status;          /* optional device word, DARD_STATUS_* bits OR-ed in          */
-  void* workspace;           /* device scratch of dard_route_workspace_size() bytes (with
-                                offsets); needs no preparation. Calls that overlap on the
-                                GPU need separate workspaces.                              */
+  void* workspace;           /* device scratch of dard_route_workspace_size() bytes, 16-byte
+                                aligned (with offsets); needs no preparation. Calls that
+                                overlap on the GPU need separate workspaces.               */
   size_t workspace_bytes;
 } dard_route_args;
 
@@ -483,12 +483,12 @@ typedef struct {
 } dard_experts_args;
 #define DARD_EXPERTS_MAX_DIM 65536
 
-/* Bytes of workspace for these sizes and either dtype (0 on invalid sizes): the product in
- * between, and the products of each (token, slot) pair before their sum. */
+/* Bytes of workspace for these sizes and either dtype (0 on invalid sizes): x in the plan's
+ * order, the product in between, and the products of each (token, slot) pair before their sum. */
 size_t dard_experts_workspace_size(int32_t tokens, int32_t experts, int32_t top_k, int32_t dim,
                                    int32_t hidden);
 
-/* Three launches, chained by programmatic dependent launch. x, the weights and their scales
+/* Two to four launches, chained by programmatic dependent launch. x, the weights and their scales
  * must be 16-byte aligned, with x_stride and x_scale_stride multiples of 16 bytes; y and
  * y_stride multiples of 16 bytes. Entries of rows outside [0, tokens * top_k) are skipped.
  * Errors: DARD_ERR_NULL, _SHAPE, _VALUE (dtype), _ALIGN, _WORKSPACE, _CUDA. */

@@ -10,6 +10,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+import struct
 
 import numpy as np
 
@@ -468,38 +469,57 @@ def mx_scale_shape(shape, layout: int = MX_SCALE_ROWS) -> tuple:
     return (*lead, -(-rows // 128), -(-cols // 128), 512)
 
 
-def _is_dtype(t, name: str, *dtypes):
+def _is_dtype(t, name: str, dtypes):
     if t.dtype not in dtypes:
         raise ValueError(f"{name}: {' or '.join(str(d) for d in dtypes)} expected, got {t.dtype}")
 
 
-def _codes_dtypes():
+def _types() -> dict:
+    """The accepted dtypes of codes, scales and the other tensors."""
     torch = _torch()
-    return torch.float8_e4m3fn, torch.uint8
+    return {"codes": (torch.float8_e4m3fn, torch.uint8),
+            "scales": (torch.uint8, torch.float8_e8m0fnu), "bf16": (torch.bfloat16,),
+            "f32": (torch.float32,), "i32": (torch.int32,),
+            "float": (torch.bfloat16, torch.float32)}
 
 
-def _scale_dtypes():
-    torch = _torch()
-    return torch.uint8, torch.float8_e8m0fnu
+_TYPES: dict = {}
 
 
-def _matrix(t, name: str, rows: int, cols: int, device: int) -> tuple[int, int]:
-    """(pointer, row stride) of a 2-D device tensor [rows, at least cols] with contiguous rows."""
+def _dtypes(kind: str) -> tuple:
+    if not _TYPES:
+        _TYPES.update(_types())
+    return _TYPES[kind]
+
+
+def _rows2(t, name: str, shape: tuple, dtypes: tuple, device: int) -> tuple[int, int]:
+    """(pointer, row stride) of a device tensor of this 2-D shape with contiguous rows. (One
+    pass of cheap comparisons; what is wrong is looked for only when one fails.)"""
+    if t.dtype in dtypes and t.get_device() == device and t.shape == shape:
+        s0, s1 = t.stride()
+        if s1 == 1 and s0 >= shape[1]:
+            return t.data_ptr(), s0
     if not t.is_cuda:
         raise ValueError(f"{name}: device tensor expected")
     if t.get_device() != device:
         raise ValueError(f"{name}: on device {t.get_device()}, expected {device}")
-    shp = t.shape
-    if len(shp) != 2 or shp[0] != rows or shp[1] < cols:
-        raise ValueError(f"{name}: [{rows}, {cols}] expected, got {tuple(shp)}")
-    stride = t.stride(0)
-    if shp[0] <= 1 or shp[1] == 0:
-        stride = max(stride, shp[1])  # no second row to step to
-    elif stride < shp[1]:
-        raise ValueError(f"{name}: rows overlap (row stride {stride})")
-    if shp[1] > 1 and t.stride(1) != 1:
+    _is_dtype(t, name, dtypes)
+    if tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{name}: {list(shape)} expected, got {tuple(t.shape)}")
+    rows, cols = shape
+    if cols > 1 and rows > 0 and t.stride(1) != 1:
         raise ValueError(f"{name}: contiguous rows expected")
-    return t.data_ptr(), stride
+    if rows > 1 and t.stride(0) < cols:
+        raise ValueError(f"{name}: rows overlap (row stride {t.stride(0)})")
+    return t.data_ptr(), max(t.stride(0), cols)  # a stride that no step uses may be anything
+
+
+def _scale_rows(t, name: str, rows: int, cols: int, device: int) -> tuple[int, int]:
+    """(pointer, pitch) of a scale tensor in layout ROWS for [rows, cols] elements."""
+    if t.dim() != 2 or t.shape[1] * MX_BLOCK < cols:
+        raise ValueError(f"{name}: {list(mx_scale_shape((rows, cols)))} expected, got "
+                         f"{tuple(t.shape)}")
+    return _rows2(t, name, (rows, t.shape[1]), _dtypes("scales"), device)
 
 
 class NormCall:
@@ -509,54 +529,41 @@ class NormCall:
     (x itself without delta) and may be x or delta; ``y`` the norm in x's dtype; ``y8`` (e4m3 or
     uint8) and ``y8_scale`` (layout ROWS, see ``mx_scale_shape``) the norm in MXFP8."""
 
+    _layout = struct.Struct("=7Qii7qf4x")  # dard_norm_args
+
     def __init__(self, dim: int, dtype, weight=None, eps: float = 1e-6):
-        torch = _torch()
-        if dtype not in (torch.bfloat16, torch.float32):
+        if dtype not in _dtypes("float"):
             raise ValueError(f"unsupported dtype {dtype}")
-        self.dim, self.dtype = dim, dtype
-        a = NormArgs()
-        a.dim, a.eps = dim, eps
-        a.dtype = DARD_BF16 if dtype == torch.bfloat16 else DARD_F32
-        self.device = None if weight is None else weight.get_device()
+        self.dim, self._dt = dim, (dtype,)
         if weight is not None and weight.numel() != dim:
             raise ValueError(f"weight: {dim} elements expected, got {weight.numel()}")
-        a.weight = _dev(weight, "weight", dim, dtype)
+        self.device = None if weight is None else weight.get_device()
+        self._weight_ptr = _dev(weight, "weight", dim, dtype) or 0
         self._weight = weight
-        self._codes, self._scales = _codes_dtypes(), _scale_dtypes()
-        self._args, self._ref = a, ctypes.byref(a)
+        self._eps = eps
+        self._code = DARD_BF16 if dtype == _torch().bfloat16 else DARD_F32
+        self._args = NormArgs()
+        self._ref = ctypes.byref(self._args)
         self._fn = lib().dard_residual_norm
 
     def __call__(self, x, delta=None, residual=None, y=None, y8=None, y8_scale=None, stream=None):
-        a, dim, dt = self._args, self.dim, self.dtype
-        rows, dev = x.shape[0], x.get_device()
-        if x.shape[-1] != dim:
-            raise ValueError(f"x: rows of {dim} elements expected, got {tuple(x.shape)}")
+        dim, dt, dev = self.dim, self._dt, x.get_device()
         if self.device is not None and dev != self.device:
             raise ValueError(f"x: on device {dev}, the weight on {self.device}")
-        a.rows = rows
-        a.x, a.x_stride = _matrix(x, "x", rows, dim, dev)
-        if x.dtype != dt:
-            raise ValueError(f"x: {dt} expected, got {x.dtype}")
-        for name, t in (("delta", delta), ("residual", residual), ("y", y)):
-            if t is None:
-                setattr(a, name, None)
-                continue
-            if t.dtype != dt or t.shape[-1] != dim:
-                raise ValueError(f"{name}: {dt} [{rows}, {dim}] expected, got {t.dtype} "
-                                 f"{tuple(t.shape)}")
-            ptr, stride = _matrix(t, name, rows, dim, dev)
-            setattr(a, name, ptr)
-            setattr(a, name + "_stride", stride)
-        a.y8 = a.y8_scale = None
+        rows = x.shape[0]
+        shape = (rows, dim)
+        xp, xs = _rows2(x, "x", shape, dt, dev)
+        dp, ds = _rows2(delta, "delta", shape, dt, dev) if delta is not None else (0, 0)
+        rp, rs = _rows2(residual, "residual", shape, dt, dev) if residual is not None else (0, 0)
+        yp, ys = _rows2(y, "y", shape, dt, dev) if y is not None else (0, 0)
+        qp = qs = sp = ss = 0
         if y8 is not None:
             if y8_scale is None:
                 raise ValueError("y8 needs y8_scale")
-            _is_dtype(y8, "y8", *self._codes)
-            _is_dtype(y8_scale, "y8_scale", *self._scales)
-            if y8.shape[-1] != dim:
-                raise ValueError(f"y8: [{rows}, {dim}] expected, got {tuple(y8.shape)}")
-            a.y8, a.y8_stride = _matrix(y8, "y8", rows, dim, dev)
-            a.y8_scale, a.y8_scale_stride = _matrix(y8_scale, "y8_scale", rows, dim // MX_BLOCK, dev)
+            qp, qs = _rows2(y8, "y8", shape, _dtypes("codes"), dev)
+            sp, ss = _scale_rows(y8_scale, "y8_scale", rows, dim, dev)
+        self._layout.pack_into(self._args, 0, xp, dp, self._weight_ptr, rp, yp, qp, sp, self._code,
+                               dim, rows, xs, ds, rs, ys, qs, ss, self._eps)
         _check(self._fn(self._ref, _stream_handle(stream, dev)), "dard_residual_norm")
 
 
@@ -566,36 +573,42 @@ def dard_residual_norm(x, delta=None, weight=None, eps: float = 1e-6, residual=N
     NormCall(x.shape[-1], x.dtype, weight, eps)(x, delta, residual, y, y8, y8_scale, stream)
 
 
+_MX_LAYOUT = struct.Struct("=3Qiiiiqqqq")  # dard_mx_args
+
+
+def _flat(t, name: str, dtypes: tuple, device: int) -> int:
+    """Pointer of a contiguous device tensor."""
+    if t.dtype not in dtypes or t.get_device() != device or not t.is_contiguous():
+        _is_dtype(t, name, dtypes)
+        raise ValueError(f"{name}: contiguous tensor on device {device} expected")
+    return t.data_ptr()
+
+
 def dard_mx_quantize(x, codes, scales, layout: int = MX_SCALE_ROWS, stream=None):
     """MXFP8 rounding of x [rows, cols] or [batch, rows, cols] (contiguous rows, any row and batch
     stride) into contiguous ``codes`` of x's shape and ``scales`` of ``mx_scale_shape``."""
     if not x.is_cuda:
         raise ValueError("x: device tensor expected")
-    dev, shp = x.get_device(), x.shape
-    if len(shp) not in (2, 3) or (shp[-1] > 1 and x.stride(-1) != 1):
+    dev, shp, strides = x.get_device(), x.shape, x.stride()
+    if len(shp) not in (2, 3) or (strides[-1] != 1 and shp[-1] > 1):
         raise ValueError("x: [rows, cols] or [batch, rows, cols] with contiguous rows expected")
     if codes.shape != shp:
         raise ValueError(f"codes: {tuple(shp)} expected, got {tuple(codes.shape)}")
-    if layout not in (MX_SCALE_ROWS, MX_SCALE_TILES):
+    by_rows = layout == MX_SCALE_ROWS
+    if not by_rows and layout != MX_SCALE_TILES:
         raise ValueError(f"layout {layout} is neither MX_SCALE_ROWS nor MX_SCALE_TILES")
-    want = mx_scale_shape(shp, layout)
-    if layout == MX_SCALE_TILES and tuple(scales.shape) != want:
-        raise ValueError(f"scales: {want} expected, got {tuple(scales.shape)}")
-    if layout == MX_SCALE_ROWS and (scales.shape[:-1] != shp[:-1] or
-                                    scales.shape[-1] < shp[-1] // MX_BLOCK):
-        raise ValueError(f"scales: {want} expected, got {tuple(scales.shape)}")
-    _is_dtype(codes, "codes", *_codes_dtypes())
-    _is_dtype(scales, "scales", *_scale_dtypes())
+    rows, cols = shp[-2], shp[-1]
+    batch = shp[0] if len(shp) == 3 else 1
+    got = scales.shape
+    if (got[:-1] != shp[:-1] or got[-1] * MX_BLOCK < cols) if by_rows else \
+            got != mx_scale_shape(shp, layout):
+        raise ValueError(f"scales: {mx_scale_shape(shp, layout)} expected, got {tuple(got)}")
     a = MxArgs()
-    a.x, a.dtype, a.layout = x.data_ptr(), _dtype_code(x), layout
-    a.codes = _dev(codes, "codes", 0, codes.dtype, dev)
-    a.scales = _dev(scales, "scales", 0, scales.dtype, dev)
-    a.batch = shp[0] if len(shp) == 3 else 1
-    a.rows, a.cols = shp[-2], shp[-1]
-    # a stride that no step uses may be anything
-    a.x_row_stride = x.stride(-2) if shp[-2] > 1 else shp[-1]
-    a.x_batch_stride = x.stride(0) if a.batch > 1 and len(shp) == 3 else 0
-    a.scale_stride = scales.shape[-1] if layout == MX_SCALE_ROWS else 0
+    # (a stride that no step uses may be anything)
+    _MX_LAYOUT.pack_into(
+        a, 0, x.data_ptr(), _flat(codes, "codes", _dtypes("codes"), dev),
+        _flat(scales, "scales", _dtypes("scales"), dev), _dtype_code(x), layout, batch, cols, rows,
+        strides[-2] if rows > 1 else cols, strides[0] if batch > 1 else 0, got[-1] if by_rows else 0)
     _check(lib().dard_mx_quantize(ctypes.byref(a), _stream_handle(stream, dev)),
            "dard_mx_quantize")
 
@@ -634,11 +647,10 @@ class RouteCall:
     def __call__(self, logits, ids, weights, offsets=None, rows=None, stream=None):
         a, k = self._args, self.top_k
         tokens, dev = logits.shape[0], logits.get_device()
-        if logits.dim() != 2 or logits.shape[1] != self.experts:
-            raise ValueError(f"logits: [tokens, {self.experts}] expected, got {tuple(logits.shape)}")
         if self.device is not None and dev != self.device:
             raise ValueError(f"logits: on device {dev}, expected {self.device}")
-        a.logits, a.logits_stride = _matrix(logits, "logits", tokens, self.experts, dev)
+        a.logits, a.logits_stride = _rows2(logits, "logits", (tokens, self.experts),
+                                           _dtypes("float"), dev)
         a.dtype, a.tokens = _dtype_code(logits), tokens
         if ids.shape != (tokens, k) or weights.shape != (tokens, k):
             raise ValueError(f"ids and weights: [{tokens}, {k}] expected, got {tuple(ids.shape)}, "
@@ -682,12 +694,11 @@ class ExpertsCall:
                              f"got {tuple(w1.shape)}, {tuple(w3.shape)}, {tuple(w2.shape)}")
         self.experts, self.hidden, self.dim = w1.shape
         self.mx = w1.dtype != torch.bfloat16
-        self._codes, self._scales = _codes_dtypes(), _scale_dtypes()
         self._i32, self._f32, self._bf16 = torch.int32, torch.float32, torch.bfloat16
         self.device = dev = w1.get_device()
         a = ExpertsArgs()
         for name, w, s in (("w1", w1, w1_scale), ("w3", w3, w3_scale), ("w2", w2, w2_scale)):
-            _is_dtype(w, name, *(self._codes if self.mx else (self._bf16,)))
+            _is_dtype(w, name, _dtypes("codes" if self.mx else "bf16"))
             setattr(a, name, _dev(w, name, w.numel(), w.dtype, dev))
             if not self.mx:
                 if s is not None:
@@ -696,7 +707,7 @@ class ExpertsCall:
             if s is None:
                 raise ValueError(f"{name}_scale: needed with 8-bit weights")
             want = mx_scale_shape(w.shape, MX_SCALE_TILES)
-            _is_dtype(s, name + "_scale", *self._scales)
+            _is_dtype(s, name + "_scale", _dtypes("scales"))
             if tuple(s.shape) != want:
                 raise ValueError(f"{name}_scale: {want} expected, got {tuple(s.shape)}")
             setattr(a, name + "_scale", _dev(s, name + "_scale", s.numel(), s.dtype, dev))
@@ -714,18 +725,13 @@ class ExpertsCall:
     def __call__(self, x, x_scale, ids, weights, offsets, rows, y, stream=None):
         a, dev, dim = self._args, self.device, self.dim
         tokens, k = ids.shape
-        if x.shape[-1] != dim or y.shape[-1] != dim:
-            raise ValueError(f"x and y: rows of {dim} elements expected, got {tuple(x.shape)}, "
-                             f"{tuple(y.shape)}")
-        _is_dtype(x, "x", *(self._codes if self.mx else (self._bf16,)))
-        a.x, a.x_stride = _matrix(x, "x", tokens, dim, dev)
+        shape = (tokens, dim)
+        a.x, a.x_stride = _rows2(x, "x", shape, _dtypes("codes" if self.mx else "bf16"), dev)
         if self.mx:
             if x_scale is None:
                 raise ValueError("x_scale: needed with 8-bit weights")
-            _is_dtype(x_scale, "x_scale", *self._scales)
-            a.x_scale, a.x_scale_stride = _matrix(x_scale, "x_scale", tokens, dim // MX_BLOCK, dev)
-        _is_dtype(y, "y", self._bf16, self._f32)
-        a.y, a.y_stride = _matrix(y, "y", tokens, dim, dev)
+            a.x_scale, a.x_scale_stride = _scale_rows(x_scale, "x_scale", tokens, dim, dev)
+        a.y, a.y_stride = _rows2(y, "y", shape, _dtypes("float"), dev)
         a.y_dtype = DARD_BF16 if y.dtype == self._bf16 else DARD_F32
         if weights.shape != ids.shape:
             raise ValueError(f"weights: {tuple(ids.shape)} expected, got {tuple(weights.shape)}")

@@ -1,29 +1,42 @@
 // dard_experts.cu - dard_experts: the products of a mixture of experts, grouped over the
 // (token, slot) pairs that dard_route sorted by expert.
 //
+//   gather_rows      many rows: x in the plan's order
 //   product<.., 1>   h = silu(w1 x) * (w3 x) of every pair, rounded (MXFP8 or bf16)
 //   product<.., 2>   o = w2 h of every pair
 //   combine          y_t = sum over the slots of token t of weight * o
 //
-// Both products are one persistent tcgen05 kernel. An output tile is 128 pairs of one expert
-// (the rows of A, M = 128) by kN weight rows (B, N = kN); what a CTA computes follows from
-// `offsets` alone, so no size of an expert ever travels to the host. In phase 1 the weight
-// rows of a tile are kN / 2 of w1 and the same kN / 2 of w3, so that the gate and the value it
-// scales meet in one thread's registers: a thread of the epilogue holds one pair (TMEM lane)
-// and 32 consecutive hidden elements, which is one MX block: its scale needs no exchange.
+// Both products are one persistent tcgen05 kernel. An output tile is the pairs of one expert (the
+// rows of A) by kN weight rows (B, N = kN); what a CTA computes follows from `offsets` alone,
+// so no size of an expert ever travels to the host. In phase 1 half of a tile's weight rows are
+// w1's and half the same rows of w3, so that the gate and the value it scales meet in one
+// thread's registers: a thread of the epilogue holds one pair (TMEM lane) and 32 consecutive
+// hidden elements, which is one MX block: its scale needs no exchange.
+//
+// Two variants:
+//   pair    two CTAs of a cluster (cta_group::2) share one M = 256, N = 256 MMA: each holds 128
+//           rows of A and 128 weight rows, so that a stage moves 32 KB into each SM's shared
+//           memory where one CTA with the same tile would move 48 KB and be bound by it;
+//   single  one CTA, M = 128, N = 128: more and smaller tiles for calls with few rows.
 //
 // Per CTA (one per SM):
 //   warps 0-7   epilogue: TMEM -> registers, then the accumulator is free for the next tile
 //               while SwiGLU, the rounding and the stores run from registers;
-//   warp 8      TMA producer: A rows (phase 1: gathered by token with tile::gather4, only the
-//               groups of four rows that exist; phase 2: boxes of 32 consecutive rows of h),
-//               B tiles, their scales (cp.async.bulk);
-//   warp 9      TMEM allocation; one lane issues the scale copies (tcgen05.cp) and MMAs;
-//   warp 10     phase 1, MXFP8: the scales of the gathered rows. Each lane reads 16 scale
-//               bytes (four stages) of its four rows at once and writes one stage's 4 x 4
-//               bytes into the tile layout.
+//   warp 8      TMA producer: A (consecutive rows) and B tiles, their scales (cp.async.bulk);
+//   warp 9      TMEM allocation; one lane issues the scale copies (tcgen05.cp) and MMAs (pair:
+//               in rank 0; rank 1's lane forwards the landing of its stages to rank 0);
+//   warps 10-11 single, phase 1: gather the rows of x by token (cp.async, 16 bytes per lane,
+//               straight into the swizzled layout) and their scales (16 bytes, four stages, at
+//               a time).
+//
 //   Stage: 128 bytes of K of the A rows and of the B rows (128-byte swizzle), plus scales.
-//   TMEM: accumulator [0, 256), scales of two stages from column 256.
+//   TMEM: accumulator from column 0, scales of two stages from column 256.
+//
+// Pairs read rows of x that an earlier launch (gather_rows) has put in the plan's order. At 4096
+// tokens x 8 of 32 experts of 4096 x 2048 that copy takes 33 us and phase 1 381 us; gathered within
+// phase 1 by two warps it takes 514 us, by TMA's own row gather (tile::gather4, 32 copies per
+// stage) longer still. For few rows the copy's launch costs more than the gather does, so the
+// single variant gathers itself.
 //
 // The work is the weights' bytes for few tokens (HBM) and the tensor pipe for many.
 //
@@ -46,29 +59,41 @@
 namespace dard {
 namespace {
 
-constexpr int kTileM = 128;            // pairs per tile
+constexpr int kTileM = 128;            // rows of A per CTA
+constexpr int kTileB = 128;            // weight rows per CTA
 constexpr int kStageK = 128;           // bytes of K per stage
+constexpr int kStages = 6;
 constexpr int kThreads = 384;
 constexpr int kEpilogueWarps = 8;
-constexpr int kProducerWarp = 8, kIssueWarp = 9, kScaleWarp = 10;
-constexpr uint32_t kBytesA = kTileM * kStageK;
+constexpr int kProducerWarp = 8, kIssueWarp = 9, kGatherWarp = 10;
+constexpr int kGatherWarps = 2;
+constexpr int kGatherLag = 2;          // stages a gather warp has in flight
+constexpr uint32_t kBytesA = kTileM * kStageK, kBytesB = kTileB * kStageK;
+constexpr uint32_t kStageBytes = kBytesA + kBytesB;
+constexpr uint32_t kScaleBytes = 3 * kMxTileBytes;  // of a stage: A's, then two tiles of B's
 constexpr uint32_t kTmemAll = 512;
 constexpr uint32_t kScaleCol = 256;    // first TMEM column of the scales
 constexpr int kGroupM = 16;            // row tiles that share a pass over an expert's columns
+constexpr int kBoxRowsSingle = 32;     // rows of h per copy (single: its tiles hold few rows)
+constexpr uint16_t kBothCtas = 0x3;
 
 struct ExpertsParams {
   const int32_t* offsets;
   const int32_t* rows;
   const int32_t* ids;
   const float* weights;
+  const void* x;
   const uint8_t* x_scale;
   const uint8_t* scale_b[2];  // phase 1: w1, w3; phase 2: w2
+  const uint8_t* a_scale;     // of the rows TMA reads (x in the plan's order, or h), in tiles
+  uint8_t* xg;                // [row tiles * 128][dim]: x in the plan's order
+  uint8_t* xg_scale;          // [row tiles][ceil(dim / 128)][512]
   uint8_t* h;                 // [row tiles * 128][hidden]
   uint8_t* h_scale;           // [row tiles][ceil(hidden / 128)][512]
   float* partial;             // [splits][pairs][dim]
   void* y;
   uint32_t* status;
-  int64_t x_scale_stride, y_stride;
+  int64_t x_stride_bytes, x_scale_stride, y_stride;
   long long wait_cycles;
   int32_t tokens, experts, top_k, dim, hidden, pairs;
   int32_t k_elems, n_elems;     // of this phase: reduced length, weight rows per expert
@@ -90,16 +115,6 @@ __device__ __forceinline__ void tma_load_3d(void* dst, const void* desc, uint64_
       "l"(reinterpret_cast<uint64_t>(desc)), "r"(smem_u32(bar)), "r"(c0), "r"(c1), "r"(c2)
       : "memory");
 }
-// Four rows r0 .. r3 (any order) from column c, one under the other in shared memory.
-__device__ __forceinline__ void tma_gather4(uint32_t dst, const void* desc, uint64_t* bar, int32_t c,
-                                            int32_t r0, int32_t r1, int32_t r2, int32_t r3) {
-  asm volatile(
-      "cp.async.bulk.tensor.2d.shared::cluster.global.tile::gather4.mbarrier::complete_tx::bytes"
-      " [%0], [%1, {%3, %4, %5, %6, %7}], [%2];" ::"r"(dst),
-      "l"(reinterpret_cast<uint64_t>(desc)), "r"(smem_u32(bar)), "r"(c), "r"(r0), "r"(r1), "r"(r2),
-      "r"(r3)
-      : "memory");
-}
 __device__ __forceinline__ void bulk_load(void* dst, const void* src, uint32_t bytes, uint64_t* bar) {
   asm volatile(
       "cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(
@@ -107,19 +122,60 @@ __device__ __forceinline__ void bulk_load(void* dst, const void* src, uint32_t b
       "l"(src), "r"(bytes), "r"(smem_u32(bar))
       : "memory");
 }
-// One 512-byte tile of scales (32 rows of 16 bytes) into four TMEM columns of every lane quarter.
+// One 512-byte tile of scales (32 rows of 16 bytes) into four TMEM columns of every lane quarter;
+// with kPair in both CTAs, each from its own shared memory.
+template <bool kPair>
 __device__ __forceinline__ void copy_scales(uint32_t taddr, uint64_t desc) {
-  asm volatile("tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;" ::"r"(taddr), "l"(desc)
-               : "memory");
+  if constexpr (kPair)
+    asm volatile("tcgen05.cp.cta_group::2.32x128b.warpx4 [%0], %1;" ::"r"(taddr), "l"(desc)
+                 : "memory");
+  else
+    asm volatile("tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;" ::"r"(taddr), "l"(desc)
+                 : "memory");
 }
+template <bool kPair>
 __device__ __forceinline__ void mma_mx(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc,
                                        uint32_t sfa, uint32_t sfb, uint32_t accumulate) {
+  if constexpr (kPair)
+    asm volatile(
+        "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
+        "tcgen05.mma.cta_group::2.kind::mxf8f6f4.block_scale [%0], %1, %2, %3, [%5], [%6], p;\n\t}" ::
+            "r"(d),
+        "l"(a), "l"(b), "r"(idesc), "r"(accumulate), "r"(sfa), "r"(sfb)
+        : "memory");
+  else
+    asm volatile(
+        "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
+        "tcgen05.mma.cta_group::1.kind::mxf8f6f4.block_scale [%0], %1, %2, %3, [%5], [%6], p;\n\t}" ::
+            "r"(d),
+        "l"(a), "l"(b), "r"(idesc), "r"(accumulate), "r"(sfa), "r"(sfb)
+        : "memory");
+}
+__device__ __forceinline__ void mma_ss_pair(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc,
+                                            uint32_t accumulate) {
   asm volatile(
       "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
-      "tcgen05.mma.cta_group::1.kind::mxf8f6f4.block_scale [%0], %1, %2, %3, [%5], [%6], p;\n\t}" ::
-          "r"(d),
-      "l"(a), "l"(b), "r"(idesc), "r"(accumulate), "r"(sfa), "r"(sfb)
+      "tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d),
+      "l"(a), "l"(b), "r"(idesc), "r"(accumulate)
       : "memory");
+}
+// One lane of a converged warp.
+__device__ __forceinline__ bool elect_one() {
+  uint32_t r;
+  asm volatile(
+      "{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}"
+      : "=r"(r));
+  return r != 0;
+}
+template <int kPending>
+__device__ __forceinline__ void cp_async_wait_group() {
+  asm volatile("cp.async.wait_group %0;" ::"n"(kPending) : "memory");
+}
+// 32 bytes to a 32-byte aligned address.
+__device__ __forceinline__ void store32(void* p, const uint32_t (&v)[8]) {
+  asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p), "r"(v[0]),
+               "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7])
+               : "memory");
 }
 // Unswizzled descriptor of a 32 x 16-byte tile of scales: eight-row groups 128 bytes apart.
 __device__ __forceinline__ uint64_t scale_desc(uint32_t saddr) {
@@ -132,64 +188,92 @@ __host__ __device__ constexpr uint32_t idesc_mx(uint32_t M, uint32_t N, uint32_t
   return (ks << 4) | ((N >> 3) << 17) | (1u << 23) | ((M >> 4) << 24) | (ks << 29);
 }
 
-// ---------------------------------------------------------------- shapes of the two variants
-// Wide: 256 weight rows per tile (one N = 256 MMA), 4 stages. Narrow: 128 weight rows, 6
-// stages, twice as many tiles: for calls whose wide tiles would not fill the SMs.
-template <bool kWide>
-struct Shape {
-  static constexpr int kN = kWide ? 256 : 128;
-  static constexpr int kStages = kWide ? 4 : 6;
-  static constexpr uint32_t kBytesB = kN * kStageK;
-  static constexpr uint32_t kScaleA = kMxTileBytes;      // bytes of a stage's A scales
-  static constexpr uint32_t kScaleB = 2 * kMxTileBytes;  // two tiles of weight scales
-  static constexpr uint32_t kStage = kBytesA + kBytesB;
-};
-
-template <int kStages>
 struct __align__(16) Ctl {
   uint64_t full[kStages], empty[kStages];
+  uint64_t peer_full[kStages];  // pair, rank 0: rank 1's stage is full
   uint64_t acc_full, acc_free;
   uint64_t drained;  // every MMA the issuer launched has completed
   uint32_t tmem_base;
   int32_t abort;
   int32_t first_row[DARD_MAX_EXPERTS + 1];   // offsets, clamped to [0, pairs]
-  int32_t first_tile[DARD_MAX_EXPERTS + 1];  // row tiles of the experts before
+  int32_t first_tile[DARD_MAX_EXPERTS + 1];  // row tiles (128 rows) of the experts before
+  int32_t first_unit[DARD_MAX_EXPERTS + 1];  // the same in units of a tile: 1 or 2 row tiles
 };
 
-template <bool kWide>
 constexpr size_t smem_bytes() {
-  using S = Shape<kWide>;
-  return 1024 + static_cast<size_t>(S::kStages) * (S::kStage + S::kScaleA + S::kScaleB) +
-         sizeof(Ctl<S::kStages>);
+  return 1024 + static_cast<size_t>(kStages) * (kStageBytes + kScaleBytes) + sizeof(Ctl);
 }
 
-// One tile: pairs [row, row + count) of expert e, weight columns from n0, reduction split.
+// A CTA's part of one tile: rows [row, row + count) (count <= 0: none) of expert e, in row tile
+// row_tile of h; column tile n, reduction split.
 struct Tile {
   int e, row, count, row_tile, n, split;
 };
 
-// Tile `w` of the call. Within an expert, kGroupM row tiles take each column tile in turn, so
-// that CTAs that run together share weights and rows in L2. `e` walks forward.
-template <class C>
-__device__ __forceinline__ bool get_tile(const ExpertsParams& p, const C& c, int64_t w, int& e,
-                                         Tile& t) {
-  const int per_row = p.n_tiles * p.splits;
-  if (w >= static_cast<int64_t>(c.first_tile[p.experts]) * per_row) return false;
-  while (w >= static_cast<int64_t>(c.first_tile[e + 1]) * per_row) ++e;
-  const int row_tiles = c.first_tile[e + 1] - c.first_tile[e];
-  const int local = static_cast<int>(w - static_cast<int64_t>(c.first_tile[e]) * per_row);
-  const int group = local / (kGroupM * per_row);
-  const int in_group = min(kGroupM, row_tiles - group * kGroupM);
-  const int rest = local - group * kGroupM * per_row;
-  const int m = group * kGroupM + rest % in_group;
+// Tile `w` of the call. Within an expert, a group of row units takes each column tile in turn,
+// so that CTAs that run together share weights and rows in L2. `e` walks forward.
+template <bool kPair>
+__device__ __forceinline__ bool get_tile(const ExpertsParams& p, const Ctl& c, int rank, int64_t w,
+                                         int& e, Tile& t) {
+  constexpr int kUnitTiles = kPair ? 2 : 1, kGroup = kGroupM / kUnitTiles;
+  const int per_unit = p.n_tiles * p.splits;
+  if (w >= static_cast<int64_t>(c.first_unit[p.experts]) * per_unit) return false;
+  while (w >= static_cast<int64_t>(c.first_unit[e + 1]) * per_unit) ++e;
+  const int units = c.first_unit[e + 1] - c.first_unit[e];
+  const int local = static_cast<int>(w - static_cast<int64_t>(c.first_unit[e]) * per_unit);
+  const int group = local / (kGroup * per_unit);
+  const int in_group = min(kGroup, units - group * kGroup);
+  const int rest = local - group * kGroup * per_unit;
+  const int m = (group * kGroup + rest % in_group) * kUnitTiles + rank;
   const int col = rest / in_group;
   t.e = e;
   t.n = col % p.n_tiles;
   t.split = col / p.n_tiles;
   t.row = c.first_row[e] + m * kTileM;
-  t.count = min(kTileM, c.first_row[e + 1] - t.row);
   t.row_tile = c.first_tile[e] + m;
+  // (a plan cut short at the workspace's end may leave a pair's second row tile outside)
+  t.count = t.row_tile < c.first_tile[e + 1] ? min(kTileM, c.first_row[e + 1] - t.row) : 0;
   return true;
+}
+
+// The plan's offsets, clamped to [0, pairs], and by expert the row tiles (128 rows) and the units of
+// kCtas row tiles before it, by the whole CTA. A plan that is none (offsets that fall) never
+// reaches past the workspace. Ends without a barrier.
+template <int kCtas>
+__device__ __forceinline__ void read_plan(const ExpertsParams& p, int32_t* first_row,
+                                          int32_t* first_tile, int32_t* first_unit) {
+  const int lane = threadIdx.x & 31;
+  for (int i = threadIdx.x; i <= p.experts; i += blockDim.x)
+    first_row[i] = min(max(p.offsets[i], 0), p.pairs);
+  __syncthreads();
+  if (threadIdx.x >= 32) return;
+  int carry_t = 0, carry_u = 0;
+  for (int b = 0; b < p.experts; b += 32) {
+    const int i = b + lane;
+    const int n = i < p.experts ? max(first_row[i + 1] - first_row[i], 0) : 0;
+    int tiles = (n + kTileM - 1) / kTileM;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const int y = __shfl_up_sync(0xffffffffu, tiles, o);
+      if (lane >= o) tiles += y;
+    }
+    const int end = min(carry_t + tiles, p.max_row_tiles);
+    const int before = __shfl_up_sync(0xffffffffu, end, 1);
+    const int start = lane == 0 ? carry_t : before;
+    int units = (end - start + kCtas - 1) / kCtas;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const int y = __shfl_up_sync(0xffffffffu, units, o);
+      if (lane >= o) units += y;
+    }
+    if (i < p.experts) {
+      first_tile[i + 1] = end;
+      first_unit[i + 1] = carry_u + units;
+    }
+    carry_t = __shfl_sync(0xffffffffu, end, 31);
+    carry_u += __shfl_sync(0xffffffffu, units, 31);
+  }
+  if (lane == 0) first_tile[0] = first_unit[0] = 0;
 }
 
 __device__ __forceinline__ float silu(float g) { return __fdividef(g, 1.f + __expf(-g)); }
@@ -200,69 +284,60 @@ __device__ __forceinline__ uint32_t pack2(float lo, float hi) {
   return r;
 }
 
-template <bool kMx, bool kWide, int kPhase>
+template <bool kMx, bool kPair, int kPhase>
 __global__ void __launch_bounds__(kThreads, 1)
     product(const __grid_constant__ ExpertsParams p, const __grid_constant__ CUtensorMap map_a,
             const __grid_constant__ CUtensorMap map_b0, const __grid_constant__ CUtensorMap map_b1) {
-  using S = Shape<kWide>;
-  constexpr int kStages = S::kStages, kN = S::kN;
+  constexpr int kCtas = kPair ? 2 : 1;
+  constexpr int kM = kTileM * kCtas, kN = kTileB * kCtas;  // of one MMA
   constexpr int kElems = kMx ? 128 : 64;    // elements of K per stage
   constexpr int kStepElems = kMx ? 32 : 16; // per MMA (32 bytes)
   // weight rows of a tile from one matrix: phase 1 takes half of them from w1, half from w3
   constexpr int kCols = kPhase == 1 ? kN / 2 : kN;
-  constexpr int kBoxRows = kCols < 128 ? kCols : 128;
-  constexpr int kBoxes = kN / kBoxRows;     // B copies per stage
+  constexpr bool kGather = kPhase == 1 && !kPair;  // the A rows come from warps 10-11
+  constexpr int kBoxA = kPair ? kTileM : kBoxRowsSingle;
   grid_dep_launch();
   extern __shared__ uint8_t smem_raw[];
   uint8_t* base = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) &
                                              ~static_cast<uintptr_t>(1023));
-  uint8_t* s_scale = base + kStages * S::kStage;  // per stage: A scales, then B scales
-  Ctl<kStages>& ctl = *reinterpret_cast<Ctl<kStages>*>(
-      s_scale + kStages * (S::kScaleA + S::kScaleB));
+  uint8_t* s_scale = base + kStages * kStageBytes;  // per stage: A scales, then B scales
+  Ctl& ctl = *reinterpret_cast<Ctl*>(s_scale + kStages * kScaleBytes);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int rank = kPair ? static_cast<int>(cluster_ctarank()) : 0;
+  const int64_t first = blockIdx.x / kCtas, step = gridDim.x / kCtas;
   const long long limit = p.wait_cycles > 0 ? p.wait_cycles : kWaitCycles;
+  // rank 0's copy of a barrier (the one the issuer waits on)
+  const auto lead = [](uint64_t* bar) { return map_shared_rank(smem_u32(bar), 0); };
 
   if (warp == kIssueWarp) {
-    tmem_alloc<kTmemAll>(&ctl.tmem_base);
-    tmem_relinquish();
+    if constexpr (kPair) {
+      tmem_alloc_pair<kTmemAll>(&ctl.tmem_base);
+      tmem_relinquish_pair();
+    } else {
+      tmem_alloc<kTmemAll>(&ctl.tmem_base);
+      tmem_relinquish();
+    }
   }
   if (warp == kProducerWarp && lane == 0) {
     for (int b = 0; b < kStages; ++b) {
-      mbar_init(&ctl.full[b], kMx && kPhase == 1 ? 2 : 1);  // the producer (and the scale warp)
+      mbar_init(&ctl.full[b], kGather ? 1 + kGatherWarps : 1);
       mbar_init(&ctl.empty[b], 1);
+      mbar_init(&ctl.peer_full[b], 1);
     }
     mbar_init(&ctl.acc_full, 1);
-    mbar_init(&ctl.acc_free, kEpilogueWarps);
+    mbar_init(&ctl.acc_free, kEpilogueWarps * kCtas);
     mbar_init(&ctl.drained, 1);
     ctl.abort = 0;
     fence_barrier_init();
-    tma_prefetch_desc(&map_a);
+    if (!kGather) tma_prefetch_desc(&map_a);
     tma_prefetch_desc(&map_b0);
     if (kPhase == 1) tma_prefetch_desc(&map_b1);
   }
   // (offsets were complete before this call's first kernel began)
-  for (int i = threadIdx.x; i <= p.experts; i += kThreads)
-    ctl.first_row[i] = min(max(p.offsets[i], 0), p.pairs);
-  __syncthreads();
-  if (warp == 0) {  // row tiles before each expert
-    int carry = 0;
-    for (int b = 0; b < p.experts; b += 32) {
-      const int i = b + lane;
-      const int n = i < p.experts ? max(ctl.first_row[i + 1] - ctl.first_row[i], 0) : 0;
-      int s = (n + kTileM - 1) / kTileM;
-#pragma unroll
-      for (int o = 1; o < 32; o <<= 1) {
-        const int y = __shfl_up_sync(0xffffffffu, s, o);
-        if (lane >= o) s += y;
-      }
-      // a plan that is none (offsets that fall) never reaches past the workspace
-      if (i < p.experts) ctl.first_tile[i + 1] = min(carry + s, p.max_row_tiles);
-      carry = min(carry + __shfl_sync(0xffffffffu, s, 31), p.max_row_tiles);
-    }
-    if (lane == 0) ctl.first_tile[0] = 0;
-  }
+  read_plan<kCtas>(p, ctl.first_row, ctl.first_tile, ctl.first_unit);
   tc_fence_before();
-  __syncthreads();
+  if constexpr (kPair) cluster_sync();  // both CTAs' barriers exist, TMEM is allocated
+  else __syncthreads();
   tc_fence_after();
   const uint32_t tmem = ctl.tmem_base;
   volatile int32_t* abort_flag = &ctl.abort;
@@ -271,75 +346,64 @@ __global__ void __launch_bounds__(kThreads, 1)
     if (p.status) atomicOr(p.status, DARD_STATUS_TIMEOUT);
   };
   const int split_stages = kPhase == 2 ? p.split_stages : p.k_stages;
+  // waits until the MMAs that read stage `b` before its use `use` have completed
+  const auto stage_free = [&](int use, int b) {
+    return !*abort_flag && (use < kStages || mbar_wait(&ctl.empty[b], ((use / kStages) - 1) & 1, limit));
+  };
 
   if (warp == kProducerWarp) {
     // -------------------------------------------------------------- TMA producer
+    // As the issuer: uniform over the warp, one elected lane issues. (Copies issued by several
+    // lanes, or by a lane of a diverged warp, cost the warp about 80 cycles each.)
     int e = 0, use = 0;
     bool ok = true;
     Tile t;
-    if (kPhase == 2) grid_dep_wait();  // h is complete
-    for (int64_t w = blockIdx.x; ok && get_tile(p, ctl, w, e, t); w += gridDim.x) {
-      int r[4];  // phase 1: tokens of this lane's four rows (a row index past the end reads 0)
-      uint32_t bytes_a;
-      if (kPhase == 1) {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const int at = 4 * lane + i;
-          const int pair = at < t.count ? __ldg(p.rows + t.row + at) : -1;
-          r[i] = pair >= 0 && pair < p.pairs ? pair / p.top_k : p.tokens;
-        }
-        bytes_a = (t.count + 3) / 4 * 4 * kStageK;
-      } else {
-        bytes_a = (t.count + 31) / 32 * 32 * kStageK;
-      }
+    const bool issue = elect_one();
+    if (!kGather) grid_dep_wait();  // the rows of A are complete
+    for (int64_t w = first; ok && get_tile<kPair>(p, ctl, rank, w, e, t); w += step) {
+      const int boxes_a = kGather ? 0 : (max(t.count, 0) + kBoxA - 1) / kBoxA;
       const int k0 = t.split * split_stages, k1 = min(p.k_stages, k0 + split_stages);
       const int n0 = t.n * kCols;
-      uint32_t scale_bytes = 0;
-      if (kMx) {
-        // phase 2: a second tile of weight scales where the tile has more than 128 rows
-        scale_bytes = kPhase == 1 ? 2 * kMxTileBytes
-                                  : kMxTileBytes * (kN > 128 && n0 + 128 < p.n_elems ? 3 : 2);
-      }
+      // tiles of weight scales: phase 1 one of w1 and one of w3; phase 2 one per 128 columns
+      const bool second = kPhase == 1 || (kN > 128 && n0 + 128 < p.n_elems);
+      uint32_t bytes = kBytesB + boxes_a * kBoxA * kStageK;
+      if (kMx) bytes += (second ? 2 : 1) * kMxTileBytes + (boxes_a > 0 ? kMxTileBytes : 0);
+      const int64_t step_b = static_cast<int64_t>(p.k_stages) * kMxTileBytes;  // a row of tiles
+      const int64_t at_b = (static_cast<int64_t>(t.e) * ((p.n_elems + 127) / 128) + n0 / 128) * step_b;
+      const uint8_t* sf_b0 = p.scale_b[0] + at_b;
+      const uint8_t* sf_b1 = kPhase == 1 ? p.scale_b[1] + at_b : sf_b0 + step_b;
+      const uint8_t* sf_a = p.a_scale + t.row_tile * step_b;
       for (int k = k0; k < k1; ++k, ++use) {
         const int b = use % kStages;
-        ok = !*abort_flag && (use < kStages ||
-                              mbar_wait(&ctl.empty[b], ((use / kStages) - 1) & 1, limit));
-        ok = __all_sync(0xffffffffu, ok);
+        ok = __all_sync(0xffffffffu, stage_free(use, b));
         if (!ok) break;
-        uint8_t* sa = base + b * S::kStage;
-        uint8_t* sb = sa + kBytesA;
-        uint8_t* ss = s_scale + b * (S::kScaleA + S::kScaleB);
-        if (lane == 0) mbar_arrive_expect_tx(&ctl.full[b], bytes_a + S::kBytesB + scale_bytes);
-        __syncwarp();
-        if (kPhase == 1) {
-          if (4 * lane < t.count)
-            tma_gather4(smem_u32(sa) + lane * 4 * kStageK, &map_a, &ctl.full[b], k * kElems, r[0],
-                        r[1], r[2], r[3]);
-        } else if (32 * lane < t.count) {
-          tma_load_2d(sa + lane * 32 * kStageK, &map_a, &ctl.full[b], k * kElems,
-                      t.row_tile * kTileM + 32 * lane);
-        }
-        if (lane < kBoxes && use != p.test_drop) {
-          const int col = kPhase == 1 ? n0 : n0 + lane * kBoxRows;
-          tma_load_3d(sb + lane * kBoxRows * kStageK, kPhase == 1 && lane == 1 ? &map_b1 : &map_b0,
-                      &ctl.full[b], k * kElems, col, t.e);
-        }
-        if (kMx && lane == 0) {
-          const int row_tiles = (p.n_elems + 127) / 128;
-          const int64_t at = (static_cast<int64_t>(t.e) * row_tiles + n0 / 128) * p.k_stages + k;
-          if (kPhase == 1) {
-            bulk_load(ss + S::kScaleA, p.scale_b[0] + at * kMxTileBytes, kMxTileBytes, &ctl.full[b]);
-            bulk_load(ss + S::kScaleA + kMxTileBytes, p.scale_b[1] + at * kMxTileBytes, kMxTileBytes,
-                      &ctl.full[b]);
-          } else {
-            bulk_load(ss, p.h_scale + (static_cast<int64_t>(t.row_tile) * p.k_stages + k) * kMxTileBytes,
-                      kMxTileBytes, &ctl.full[b]);
-            bulk_load(ss + S::kScaleA, p.scale_b[0] + at * kMxTileBytes, kMxTileBytes, &ctl.full[b]);
-            if (kN > 128 && n0 + 128 < p.n_elems)
-              bulk_load(ss + S::kScaleA + kMxTileBytes,
-                        p.scale_b[0] + (at + p.k_stages) * kMxTileBytes, kMxTileBytes, &ctl.full[b]);
+        if (issue) {
+          uint8_t* sa = base + b * kStageBytes;
+          uint8_t* sb = sa + kBytesA;
+          uint8_t* ss = s_scale + b * kScaleBytes;
+          uint64_t* bar = &ctl.full[b];
+          mbar_arrive_expect_tx(bar, bytes);
+          if (use != p.test_drop) {
+            if constexpr (kPhase == 1 && !kPair) {  // 64 rows of each matrix
+              tma_load_3d(sb, &map_b0, bar, k * kElems, n0, t.e);
+              tma_load_3d(sb + 64 * kStageK, &map_b1, bar, k * kElems, n0, t.e);
+            } else if constexpr (kPhase == 1) {
+              tma_load_3d(sb, rank == 1 ? &map_b1 : &map_b0, bar, k * kElems, n0, t.e);
+            } else {
+              tma_load_3d(sb, &map_b0, bar, k * kElems, n0 + rank * kTileB, t.e);
+            }
+          }
+          for (int i = 0; i < boxes_a; ++i)
+            tma_load_2d(sa + i * kBoxA * kStageK, &map_a, bar, k * kElems,
+                        t.row_tile * kTileM + i * kBoxA);
+          if constexpr (kMx) {
+            const int at = k * kMxTileBytes;
+            if (boxes_a > 0) bulk_load(ss, sf_a + at, kMxTileBytes, bar);
+            bulk_load(ss + kMxTileBytes, sf_b0 + at, kMxTileBytes, bar);
+            if (second) bulk_load(ss + 2 * kMxTileBytes, sf_b1 + at, kMxTileBytes, bar);
           }
         }
+        __syncwarp();
       }
     }
     if (!ok) {
@@ -350,116 +414,184 @@ __global__ void __launch_bounds__(kThreads, 1)
     }
     __syncwarp();
   } else if (warp == kIssueWarp) {
-    // -------------------------------------------------------------- MMA issuer
-    if (lane == 0) {
+    if (rank == 0) {
+      // ------------------------------------------------------------ MMA issuer
+      // The whole warp walks the loop, so that what it computes is uniform over the warp; one
+      // elected lane issues.
       int e = 0, use = 0, tiles = 0;
       bool ok = true;
       Tile t;
-      for (int64_t w = blockIdx.x; ok && get_tile(p, ctl, w, e, t); w += gridDim.x, ++tiles) {
-        ok = tiles == 0 || mbar_wait(&ctl.acc_free, (tiles - 1) & 1, limit);
+      const bool issue = elect_one();
+      const uint32_t s_stage = smem_u32(base), s_sf = smem_u32(s_scale);
+      for (int64_t w = first; ok && get_tile<kPair>(p, ctl, rank, w, e, t); w += step, ++tiles) {
+        ok = __all_sync(0xffffffffu, tiles == 0 || mbar_wait(&ctl.acc_free, (tiles - 1) & 1, limit));
         if (!ok) break;
         tc_fence_after();
         const int k0 = t.split * split_stages, k1 = min(p.k_stages, k0 + split_stages);
-        // narrow phase 1: a tile's 64 weight rows are half of a tile of 128 scales
+        // single, phase 1: a tile's 64 weight rows are half of a tile of 128 scales
         const uint32_t half = kPhase == 1 && kCols == 64 ? (t.n & 1) * 2 : 0;
+        for (int k = k0; k < k1; ++k, ++use) {
+          const int b = use % kStages;
+          ok = !*abort_flag && mbar_wait(&ctl.full[b], (use / kStages) & 1, limit) &&
+               (!kPair || mbar_wait(&ctl.peer_full[b], (use / kStages) & 1, limit));
+          ok = __all_sync(0xffffffffu, ok);
+          if (!ok) break;
+          tc_fence_after();
+          const uint32_t sa = s_stage + b * kStageBytes, sb = sa + kBytesA;
+          const uint32_t sfa = tmem + kScaleCol + (use & 1) * 16, sfb = sfa + 8;
+          const int steps = min(4, (p.k_elems - k * kElems + kStepElems - 1) / kStepElems);
+          if (issue) {
+            if (kMx) {
+              const uint32_t ss = s_sf + b * kScaleBytes;
+              copy_scales<kPair>(sfa, scale_desc(ss));
+              copy_scales<kPair>(sfb, scale_desc(ss + kMxTileBytes));
+              if (kPhase == 1 || kN > 128)
+                copy_scales<kPair>(sfb + 4, scale_desc(ss + 2 * kMxTileBytes));
+            }
+            const uint64_t da = smem_desc_sw128(sa, 16, 1024), db = smem_desc_sw128(sb, 16, 1024);
+#pragma unroll
+            for (int ks = 0; ks < 4; ++ks) {
+              if (ks >= steps) break;
+              const uint32_t acc = (k > k0 || ks > 0) ? 1u : 0u;
+              const uint64_t off = ks * 32 / 16;  // descriptors count 16-byte units
+              if constexpr (!kMx && kPair) {
+                mma_ss_pair(tmem, da + off, db + off, idesc_bf16_f32(kM, kN, 0, 0), acc);
+              } else if constexpr (!kMx) {
+                mma_ss(tmem, da + off, db + off, idesc_bf16_f32(kM, kN, 0, 0), acc);
+              } else if constexpr (kPhase == 1 && kCols == 64) {
+                // w1's and w3's scales lie in different tiles: one MMA for each
+                mma_mx<kPair>(tmem, da + off, db + off, idesc_mx(kM, 64, ks), sfa, sfb + half, acc);
+                mma_mx<kPair>(tmem + 64, da + off, db + off + 64 * kStageK / 16, idesc_mx(kM, 64, ks),
+                              sfa, sfb + 4 + half, acc);
+              } else {
+                mma_mx<kPair>(tmem, da + off, db + off, idesc_mx(kM, kN, ks), sfa, sfb, acc);
+              }
+            }
+            if constexpr (kPair) mma_commit_pair(&ctl.empty[b], kBothCtas);
+            else mma_commit(&ctl.empty[b]);
+            if (k == k1 - 1) {
+              if constexpr (kPair) mma_commit_pair(&ctl.acc_full, kBothCtas);
+              else mma_commit(&ctl.acc_full);
+            }
+          }
+          __syncwarp();
+        }
+      }
+      if (!ok && lane == 0) give_up();
+      if (issue) {
+        if constexpr (kPair) mma_commit_pair(&ctl.drained, kBothCtas);
+        else mma_commit(&ctl.drained);
+      }
+    } else if (lane == 0) {
+      // ------------------------------------------------------------ rank 1: landings to rank 0
+      int e = 0, use = 0;
+      bool ok = true;
+      Tile t;
+      for (int64_t w = first; ok && get_tile<kPair>(p, ctl, rank, w, e, t); w += step) {
+        const int k0 = t.split * split_stages, k1 = min(p.k_stages, k0 + split_stages);
         for (int k = k0; k < k1; ++k, ++use) {
           const int b = use % kStages;
           ok = !*abort_flag && mbar_wait(&ctl.full[b], (use / kStages) & 1, limit);
           if (!ok) break;
-          tc_fence_after();
-          const uint32_t sa = smem_u32(base + b * S::kStage), sb = sa + kBytesA;
-          const uint32_t sfa = tmem + kScaleCol + (use & 1) * 16, sfb = sfa + 8;
-          if (kMx) {
-            const uint32_t ss = smem_u32(s_scale + b * (S::kScaleA + S::kScaleB));
-            copy_scales(sfa, scale_desc(ss));
-            copy_scales(sfb, scale_desc(ss + S::kScaleA));
-            if (kPhase == 1 || kN > 128) copy_scales(sfb + 4, scale_desc(ss + S::kScaleA + kMxTileBytes));
-          }
-          const int steps = min(4, (p.k_elems - k * kElems + kStepElems - 1) / kStepElems);
-#pragma unroll
-          for (int ks = 0; ks < 4; ++ks) {
-            if (ks >= steps) break;
-            const uint32_t acc = (k > k0 || ks > 0) ? 1u : 0u;
-            const uint64_t da = smem_desc_sw128(sa + ks * 32, 16, 1024);
-            const uint64_t db = smem_desc_sw128(sb + ks * 32, 16, 1024);
-            if constexpr (!kMx) {
-              mma_ss(tmem, da, db, idesc_bf16_f32(kTileM, kN, 0, 0), acc);
-            } else if constexpr (kPhase == 1 && kCols == 64) {
-              // w1's and w3's scales lie in different tiles: one MMA for each
-              mma_mx(tmem, da, db, idesc_mx(kTileM, 64, ks), sfa, sfb + half, acc);
-              mma_mx(tmem + 64, da, smem_desc_sw128(sb + 64 * kStageK + ks * 32, 16, 1024),
-                     idesc_mx(kTileM, 64, ks), sfa, sfb + 4 + half, acc);
-            } else {
-              mma_mx(tmem, da, db, idesc_mx(kTileM, kN, ks), sfa, sfb, acc);
-            }
-          }
-          mma_commit(&ctl.empty[b]);
+          mbar_arrive_remote(lead(&ctl.peer_full[b]));
         }
-        if (ok) mma_commit(&ctl.acc_full);
       }
       if (!ok) give_up();
-      mma_commit(&ctl.drained);
     }
     __syncwarp();
-  } else if (warp == kScaleWarp) {
-    // -------------------------------------------------------------- scales of gathered rows
-    if (kMx && kPhase == 1) {
+  } else if (warp >= kGatherWarp) {
+    // -------------------------------------------------------------- rows of x, by token
+    if (kGather) {
+      const int g = warp - kGatherWarp;
+      constexpr int kRows = kTileM / kGatherWarps;  // of this warp: g * kRows ..
+      constexpr int kCopies = kRows / 4;            // a warp copies four rows (8 lanes each) at once
+      const int chunk = lane & 7, sub = lane >> 3;
+      const char* xb = static_cast<const char*>(p.x) + chunk * 16;
+      const int row_bytes = p.k_elems * (kMx ? 1 : 2);
       int e = 0, use = 0;
       bool ok = true;
       Tile t;
-      for (int64_t w = blockIdx.x; ok && get_tile(p, ctl, w, e, t); w += gridDim.x) {
-        // lane l: rows l, 32 + l, 64 + l, 96 + l, whose words lie side by side in the tile
-        const uint4* src[4];
-        uint32_t now[4][4], ahead[4][4];  // [row][stage within a group of four]
+      int done = 0;  // stages announced
+      // tells the issuer of the stages before `upto`, whose copies have landed
+      const auto announce = [&](int upto) {
+        fence_proxy_async_smem();  // before the tensor core reads what was written here
+        __syncwarp();
+        for (; done < upto; ++done)
+          if (lane == 0) mbar_arrive(&ctl.full[done % kStages]);
+      };
+      for (int64_t w = first; ok && get_tile<kPair>(p, ctl, rank, w, e, t); w += step) {
+        int64_t from[kCopies];  // byte offset of the token's row; -1: no row
+        const uint4* src[2] = {nullptr, nullptr};  // scales of rows g * kRows + lane (+ 32)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const int at = 32 * i + lane;
+        for (int h = 0; h < kRows / 32; ++h) {
+          const int at = g * kRows + 32 * h + lane;
           const int pair = at < t.count ? __ldg(p.rows + t.row + at) : -1;
-          src[i] = pair >= 0 && pair < p.pairs
-                       ? reinterpret_cast<const uint4*>(
-                             p.x_scale + static_cast<int64_t>(pair / p.top_k) * p.x_scale_stride)
-                       : nullptr;
-        }
-        const auto fetch = [&](int group, uint32_t (&d)[4][4]) {
+          const int token = pair >= 0 && pair < p.pairs ? pair / p.top_k : -1;
+          if (kMx && token >= 0)
+            src[h] = reinterpret_cast<const uint4*>(p.x_scale + static_cast<int64_t>(token) * p.x_scale_stride);
 #pragma unroll
-          for (int i = 0; i < 4; ++i) {
+          for (int c = 0; c < 8; ++c) {
+            const int tok = __shfl_sync(0xffffffffu, token, 4 * c + sub);
+            from[8 * h + c] = tok >= 0 ? static_cast<int64_t>(tok) * p.x_stride_bytes : -1;
+          }
+        }
+        uint32_t now[2][4] = {}, ahead[2][4] = {};  // [row][stage within a group of four]
+        const auto fetch = [&](int group) {
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
             uint4 v = make_uint4(0, 0, 0, 0);
-            if (src[i] != nullptr && 4 * group < p.k_stages) v = __ldg(src[i] + group);
-            d[i][0] = v.x;
-            d[i][1] = v.y;
-            d[i][2] = v.z;
-            d[i][3] = v.w;
+            if (src[h] != nullptr && 4 * group < p.k_stages) v = __ldg(src[h] + group);
+            ahead[h][0] = v.x;
+            ahead[h][1] = v.y;
+            ahead[h][2] = v.z;
+            ahead[h][3] = v.w;
           }
         };
-        fetch(0, ahead);
+        if (kMx) fetch(0);
         for (int k = 0; ok && k < p.k_stages; k += 4) {
+          if (kMx) {
 #pragma unroll
-          for (int i = 0; i < 4; ++i) {
+            for (int h = 0; h < 2; ++h) {
 #pragma unroll
-            for (int j = 0; j < 4; ++j) now[i][j] = ahead[i][j];
+              for (int j = 0; j < 4; ++j) now[h][j] = ahead[h][j];
+            }
+            fetch(k / 4 + 1);
           }
-          fetch(k / 4 + 1, ahead);
 #pragma unroll
           for (int j = 0; j < 4; ++j) {
             if (k + j >= p.k_stages) break;
             const int b = use % kStages;
-            ok = !*abort_flag && (use < kStages ||
-                                  mbar_wait(&ctl.empty[b], ((use / kStages) - 1) & 1, limit));
-            ok = __all_sync(0xffffffffu, ok);
+            ok = __all_sync(0xffffffffu, stage_free(use, b));
             if (!ok) break;
-            uint8_t* ss = s_scale + b * (S::kScaleA + S::kScaleB);
-            reinterpret_cast<uint4*>(ss)[lane] = make_uint4(now[0][j], now[1][j], now[2][j], now[3][j]);
-            fence_proxy_async_smem();  // before the tensor core's copy reads them
-            __syncwarp();
-            if (lane == 0) mbar_arrive(&ctl.full[b]);
+            uint8_t* sa = base + b * kStageBytes;
+            const int col = (k + j) * kStageK;
+            if (col + chunk * 16 < row_bytes) {
+#pragma unroll
+              for (int c = 0; c < kCopies; ++c) {
+                const int row = g * kRows + 4 * c + sub;
+                if (from[c] >= 0)
+                  cp_async16(sa + row * kStageK + ((chunk ^ (row & 7)) << 4), xb + from[c] + col, 16);
+              }
+            }
+            cp_async_commit();
+            if (kMx) {
+              uint8_t* ss = s_scale + b * kScaleBytes + lane * 16 + g * (kRows / 32) * 4;
+              *reinterpret_cast<uint2*>(ss) = make_uint2(now[0][j], now[1][j]);
+            }
             ++use;
+            if (use - done > kGatherLag) {
+              cp_async_wait_group<kGatherLag>();
+              announce(use - kGatherLag);
+            }
           }
         }
+        cp_async_wait_all();
+        announce(use);
       }
       if (!ok && lane == 0) give_up();
       __syncwarp();
     }
-  } else if (warp < kEpilogueWarps) {
+  } else {
     // -------------------------------------------------------------- epilogue
     const int quarter = warp & 3, half = warp >> 2;
     const int r = quarter * 32 + lane;  // TMEM lane = row of the tile
@@ -475,8 +607,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         constexpr int kRun = 32 * kEpilogueWarps;
         for (int64_t t0 = static_cast<int64_t>(blockIdx.x) * kRun + warp * 32; t0 < p.tokens;
              t0 += static_cast<int64_t>(gridDim.x) * kRun) {
-          uint32_t missing = __ballot_sync(
-              0xffffffffu, t0 + lane < p.tokens && p.ids[t0 + lane] < 0);
+          uint32_t missing = __ballot_sync(0xffffffffu, t0 + lane < p.tokens && p.ids[t0 + lane] < 0);
           for (; missing != 0; missing &= missing - 1) {
             const int64_t at = (t0 + __ffs(missing) - 1) * p.y_stride;
             for (int i = lane; i < p.dim; i += 32) {
@@ -487,7 +618,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         }
       }
     }
-    for (int64_t w = blockIdx.x; ok && get_tile(p, ctl, w, e, t); w += gridDim.x, ++tiles) {
+    for (int64_t w = first; ok && get_tile<kPair>(p, ctl, rank, w, e, t); w += step, ++tiles) {
       const bool in = r < t.count;
       int pair = 0;
       if (kPhase == 2) pair = in ? __ldg(p.rows + t.row + r) : -1;
@@ -507,7 +638,10 @@ __global__ void __launch_bounds__(kThreads, 1)
       tmem_wait_ld();
       tc_fence_before();
       __syncwarp();
-      if (lane == 0) mbar_arrive(&ctl.acc_free);
+      if (lane == 0) {
+        if constexpr (kPair) mbar_arrive_remote(lead(&ctl.acc_free));
+        else mbar_arrive(&ctl.acc_free);
+      }
       if constexpr (kPhase == 1) {
 #pragma unroll
         for (int c = 0; c < kChunks / 2; ++c) {
@@ -528,19 +662,19 @@ __global__ void __launch_bounds__(kThreads, 1)
 #pragma unroll
               for (int i = 0; i < 8; ++i)
                 q[i] = e4m3x4(v[4 * i] * s, v[4 * i + 1] * s, v[4 * i + 2] * s, v[4 * i + 3] * s);
-              uint4* dst = reinterpret_cast<uint4*>(p.h + row * p.hidden + col);
-              dst[0] = make_uint4(q[0], q[1], q[2], q[3]);
-              dst[1] = make_uint4(q[4], q[5], q[6], q[7]);
+              store32(p.h + row * p.hidden + col, q);
               const int tiles_h = (p.hidden + 127) / 128;
               p.h_scale[(static_cast<int64_t>(t.row_tile) * tiles_h + col / 128) * kMxTileBytes +
                         mx_tile_byte(r, col / 32)] = static_cast<uint8_t>(b);
             }
           } else if (in && col < p.hidden) {
-            uint4* dst = reinterpret_cast<uint4*>(p.h + (row * p.hidden + col) * 2);
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
-              dst[i] = make_uint4(pack2(v[8 * i], v[8 * i + 1]), pack2(v[8 * i + 2], v[8 * i + 3]),
-                                  pack2(v[8 * i + 4], v[8 * i + 5]), pack2(v[8 * i + 6], v[8 * i + 7]));
+            for (int i = 0; i < 2; ++i) {
+              uint32_t q[8];
+#pragma unroll
+              for (int j = 0; j < 8; ++j) q[j] = pack2(v[16 * i + 2 * j], v[16 * i + 2 * j + 1]);
+              store32(p.h + (row * p.hidden + col) * 2 + 32 * i, q);
+            }
           }
         }
       } else {
@@ -551,7 +685,16 @@ __global__ void __launch_bounds__(kThreads, 1)
           const int col = t.n * kN + half * (kN / 2) + 32 * c;
           if (!store || col >= p.dim) continue;
           const uint32_t (&a)[32] = acc[c];
-          if (p.direct && !p.y_f32) {
+          if (!p.direct) {
+            float* to = p.partial + (static_cast<int64_t>(t.split) * p.pairs + pair) * p.dim + col;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              uint32_t q[8];
+#pragma unroll
+              for (int j = 0; j < 8; ++j) q[j] = a[8 * i + j];
+              store32(to + 8 * i, q);
+            }
+          } else if (!p.y_f32) {
             uint4* dst = reinterpret_cast<uint4*>(static_cast<__nv_bfloat16*>(p.y) +
                                                   pair * p.y_stride + col);
 #pragma unroll
@@ -564,14 +707,12 @@ __global__ void __launch_bounds__(kThreads, 1)
               dst[i] = make_uint4(q[0], q[1], q[2], q[3]);
             }
           } else {
-            float* to = p.direct ? static_cast<float*>(p.y) + pair * p.y_stride + col
-                                 : p.partial + (static_cast<int64_t>(t.split) * p.pairs + pair) * p.dim + col;
+            float4* dst = reinterpret_cast<float4*>(static_cast<float*>(p.y) + pair * p.y_stride + col);
 #pragma unroll
             for (int i = 0; i < 8; ++i)
-              reinterpret_cast<float4*>(to)[i] =
-                  make_float4(__uint_as_float(a[4 * i]) * weight, __uint_as_float(a[4 * i + 1]) * weight,
-                              __uint_as_float(a[4 * i + 2]) * weight,
-                              __uint_as_float(a[4 * i + 3]) * weight);
+              dst[i] = make_float4(__uint_as_float(a[4 * i]) * weight, __uint_as_float(a[4 * i + 1]) * weight,
+                                   __uint_as_float(a[4 * i + 2]) * weight,
+                                   __uint_as_float(a[4 * i + 3]) * weight);
           }
         }
       }
@@ -581,47 +722,102 @@ __global__ void __launch_bounds__(kThreads, 1)
   }
   // ---------------------------------------------------------------- teardown
   tc_fence_before();
-  __syncthreads();
+  if constexpr (kPair) cluster_sync();  // no CTA leaves while the other may signal its barriers
+  else __syncthreads();
   if (warp == kIssueWarp) {
     if (!mbar_wait(&ctl.drained, 0, limit) && lane == 0) give_up();
     __syncwarp();
     tc_fence_after();
-    tmem_dealloc<kTmemAll>(tmem);
+    if constexpr (kPair) tmem_dealloc_pair<kTmemAll>(tmem);
+    else tmem_dealloc<kTmemAll>(tmem);
   }
 }
 
-// y_t = sum over slots (in order) of weight * (sum over splits of partial). Eight columns per
-// thread.
+// x (and its scales) in the plan's order, every expert's rows from a row tile's start: one warp per
+// pair of the plan.
+template <bool kMx>
+__global__ void __launch_bounds__(256) gather_rows(const __grid_constant__ ExpertsParams p) {
+  grid_dep_launch();
+  __shared__ int32_t first_row[DARD_MAX_EXPERTS + 1], first_tile[DARD_MAX_EXPERTS + 1],
+      first_unit[DARD_MAX_EXPERTS + 1];
+  read_plan<1>(p, first_row, first_tile, first_unit);
+  __syncthreads();
+  const int lane = threadIdx.x & 31;
+  const int64_t row_bytes = static_cast<int64_t>(p.dim) * (kMx ? 1 : 2);
+  const int scale_tiles = (p.dim + 127) / 128;
+  for (int i = blockIdx.x * 8 + (threadIdx.x >> 5); i < p.pairs; i += gridDim.x * 8) {
+    int lo = 0, hi = p.experts;  // first_row[lo] <= i < first_row[hi]
+    while (hi - lo > 1) {
+      const int mid = (lo + hi) >> 1;
+      if (first_row[mid] <= i) lo = mid;
+      else hi = mid;
+    }
+    const int at = i - first_row[lo], tile = first_tile[lo] + at / kTileM;
+    if (at < 0 || i >= first_row[lo + 1] || tile >= first_tile[lo + 1]) continue;
+    const int pair = p.rows[i];
+    if (pair < 0 || pair >= p.pairs) continue;
+    const int64_t token = pair / p.top_k, row = static_cast<int64_t>(tile) * kTileM + at % kTileM;
+    const uint4* src = reinterpret_cast<const uint4*>(static_cast<const char*>(p.x) + token * p.x_stride_bytes);
+    uint4* dst = reinterpret_cast<uint4*>(p.xg + row * row_bytes);
+    const int n = static_cast<int>(row_bytes / 16);
+    for (int c = lane; c < n; c += 128) {
+      uint4 v[4];
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        if (c + 32 * j < n) v[j] = __ldg(src + c + 32 * j);
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        if (c + 32 * j < n) dst[c + 32 * j] = v[j];
+    }
+    if (kMx) {
+      const uint32_t* sc = reinterpret_cast<const uint32_t*>(p.x_scale + token * p.x_scale_stride);
+      for (int c = lane; c < scale_tiles; c += 32)
+        *reinterpret_cast<uint32_t*>(p.xg_scale + (static_cast<int64_t>(tile) * scale_tiles + c) * kMxTileBytes +
+                                     mx_tile_byte(at % kTileM, 0)) = __ldg(sc + c);
+    }
+  }
+}
+
+// y_t = sum over slots (in order) of weight * (sum over splits of the pair's product). Four columns
+// per thread; the products of up to eight slots are in flight at once.
 template <typename Y>
 __global__ void __launch_bounds__(128) combine(const __grid_constant__ ExpertsParams p) {
   grid_dep_wait();
   const int64_t t = blockIdx.x;
-  for (int col = 8 * (blockIdx.y * 128 + threadIdx.x); col < p.dim; col += 8 * 128 * gridDim.y) {
-    float sum[8] = {};
-    for (int s = 0; s < p.top_k; ++s) {
-      const int64_t pair = t * p.top_k + s;
-      if (p.ids[pair] < 0) continue;
-      const float w = p.weights[pair];
-      float o[8] = {};
-      for (int i = 0; i < p.splits; ++i) {
-        const float4* src = reinterpret_cast<const float4*>(
-            p.partial + (static_cast<int64_t>(i) * p.pairs + pair) * p.dim + col);
-        const float4 a = src[0], b = src[1];
-        o[0] += a.x; o[1] += a.y; o[2] += a.z; o[3] += a.w;
-        o[4] += b.x; o[5] += b.y; o[6] += b.z; o[7] += b.w;
-      }
+  const int col = 4 * (blockIdx.y * 128 + threadIdx.x);
+  if (col >= p.dim) return;
+  constexpr int kAhead = 8;
+  float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
+  const int parts = p.top_k * p.splits;  // slot by slot, its splits in order
+  for (int first = 0; first < parts; first += kAhead) {
+    float4 v[kAhead];
+    float w[kAhead];
 #pragma unroll
-      for (int i = 0; i < 8; ++i) sum[i] = fmaf(w, o[i], sum[i]);
+    for (int i = 0; i < kAhead; ++i) {
+      v[i] = make_float4(0.f, 0.f, 0.f, 0.f);
+      w[i] = 0.f;
+      const int s = p.splits == 1 ? first + i : (first + i) / p.splits;
+      const int split = p.splits == 1 ? 0 : (first + i) % p.splits;
+      const int64_t pair = t * p.top_k + s;
+      if (first + i < parts && p.ids[pair] >= 0) {
+        v[i] = __ldcs(reinterpret_cast<const float4*>(
+            p.partial + (static_cast<int64_t>(split) * p.pairs + pair) * p.dim + col));
+        w[i] = p.weights[pair];
+      }
     }
-    Y* y = static_cast<Y*>(p.y) + t * p.y_stride + col;
-    if constexpr (sizeof(Y) == 2) {
-      *reinterpret_cast<uint4*>(y) = make_uint4(pack2(sum[0], sum[1]), pack2(sum[2], sum[3]),
-                                                pack2(sum[4], sum[5]), pack2(sum[6], sum[7]));
-    } else {
-      reinterpret_cast<float4*>(y)[0] = make_float4(sum[0], sum[1], sum[2], sum[3]);
-      reinterpret_cast<float4*>(y)[1] = make_float4(sum[4], sum[5], sum[6], sum[7]);
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) {
+      sum.x = fmaf(w[i], v[i].x, sum.x);
+      sum.y = fmaf(w[i], v[i].y, sum.y);
+      sum.z = fmaf(w[i], v[i].z, sum.z);
+      sum.w = fmaf(w[i], v[i].w, sum.w);
     }
   }
+  Y* y = static_cast<Y*>(p.y) + t * p.y_stride + col;
+  if constexpr (sizeof(Y) == 2)
+    *reinterpret_cast<uint2*>(y) = make_uint2(pack2(sum.x, sum.y), pack2(sum.z, sum.w));
+  else
+    *reinterpret_cast<float4*>(y) = sum;
 }
 
 // ---------------------------------------------------------------- host side
@@ -640,37 +836,71 @@ bool encode(CUtensorMap* m, const void* ptr, bool mx, uint64_t cols, uint64_t ro
             CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-template <bool kMx, bool kWide, int kPhase>
+template <class F>
+cudaLaunchConfig_t pair_config(F*, unsigned ctas, cudaStream_t stream, cudaLaunchAttribute* attr) {
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(ctas);
+  cfg.blockDim = dim3(kThreads);
+  cfg.dynamicSmemBytes = smem_bytes();
+  cfg.stream = stream;
+  attr[0].id = cudaLaunchAttributeClusterDimension;
+  attr[0].val.clusterDim.x = 2;
+  attr[0].val.clusterDim.y = 1;
+  attr[0].val.clusterDim.z = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  return cfg;
+}
+
+// Clusters of two CTAs of this kernel that fit on the device at once, looked up once per device.
+template <class F>
+int max_pairs(F* kernel, std::atomic<int>* cache) {
+  int dev = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return sm_count() / 2;
+  int n = cache[dev].load(std::memory_order_relaxed);
+  if (n > 0) return n;
+  cudaLaunchAttribute attr[1];
+  const cudaLaunchConfig_t cfg = pair_config(kernel, 2 * 64, nullptr, attr);
+  if (cudaOccupancyMaxActiveClusters(&n, kernel, &cfg) != cudaSuccess || n <= 0) {
+    cudaGetLastError();
+    return sm_count() / 2;
+  }
+  cache[dev].store(n, std::memory_order_relaxed);
+  return n;
+}
+
+template <bool kMx, bool kPair, int kPhase>
 cudaError_t launch_product(const ExpertsParams& p, int64_t tiles, const CUtensorMap& a,
                            const CUtensorMap& b0, const CUtensorMap& b1, cudaStream_t stream) {
   static std::atomic<uint64_t> done{0};
-  const size_t smem = smem_bytes<kWide>();
-  const cudaError_t e = ensure_smem_attr(product<kMx, kWide, kPhase>, smem, done);
+  static std::atomic<int> pairs[64];
+  const auto kernel = product<kMx, kPair, kPhase>;
+  const cudaError_t e = ensure_smem_attr(kernel, smem_bytes(), done);
   if (e != cudaSuccess) return e;
-  cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(static_cast<unsigned>(std::min<int64_t>(tiles, sm_count())));
-  cfg.blockDim = dim3(kThreads);
-  cfg.dynamicSmemBytes = smem;
-  cfg.stream = stream;
-  cudaLaunchAttribute attr[1];
-  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  attr[0].val.programmaticStreamSerializationAllowed = 1;
-  cfg.attrs = attr;
-  cfg.numAttrs = kPhase == 2 ? 1 : 0;
-  return cudaLaunchKernelEx(&cfg, product<kMx, kWide, kPhase>, p, a, b0, b1);
+  cudaLaunchAttribute attr[2];
+  const int64_t most = kPair ? max_pairs(kernel, pairs) : sm_count();
+  const unsigned ctas = static_cast<unsigned>(std::min<int64_t>(tiles, most)) * (kPair ? 2 : 1);
+  cudaLaunchConfig_t cfg = pair_config(kernel, ctas, stream, attr);
+  if (!kPair) cfg.numAttrs = 0;
+  if (kPhase == 2 || kPair) {  // after gather_rows or phase 1
+    attr[cfg.numAttrs].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[cfg.numAttrs].val.programmaticStreamSerializationAllowed = 1;
+    ++cfg.numAttrs;
+  }
+  return cudaLaunchKernelEx(&cfg, kernel, p, a, b0, b1);
 }
 
 template <bool kMx, int kPhase>
-cudaError_t launch_phase(const ExpertsParams& p, bool wide, int64_t tiles, const CUtensorMap& a,
+cudaError_t launch_phase(const ExpertsParams& p, bool pair, int64_t tiles, const CUtensorMap& a,
                          const CUtensorMap& b0, const CUtensorMap& b1, cudaStream_t s) {
-  return wide ? launch_product<kMx, true, kPhase>(p, tiles, a, b0, b1, s)
+  return pair ? launch_product<kMx, true, kPhase>(p, tiles, a, b0, b1, s)
               : launch_product<kMx, false, kPhase>(p, tiles, a, b0, b1, s);
 }
 
 template <typename Y>
 cudaError_t launch_combine(const ExpertsParams& p, cudaStream_t stream) {
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(p.tokens, (p.dim / 8 + 127) / 128);
+  cfg.gridDim = dim3(p.tokens, (p.dim / 4 + 127) / 128);
   cfg.blockDim = dim3(128);
   cfg.stream = stream;
   cudaLaunchAttribute attr[1];
@@ -686,37 +916,51 @@ constexpr size_t up256(size_t n) { return (n + 255) / 256 * 256; }
 // Sizes that follow from a call's sizes alone.
 struct Plan {
   int64_t pairs, row_tiles;  // at most so many row tiles of 128 pairs
-  bool wide1, wide2;
+  bool pair1, pair2;
   int64_t tiles1, tiles2;    // at most so many tiles of each phase
   int splits, split_stages;
-  size_t h_bytes, h_scale_bytes, partial_bytes;
+  size_t h_bytes, h_scale_bytes, partial_bytes, xg_bytes, xg_scale_bytes;
+  bool direct;  // phase 2 writes y itself
+  // x in the plan's order is read for the last time in phase 1, the pairs' products are written
+  // in phase 2: they share their bytes
+  size_t bytes() const {
+    return h_bytes + h_scale_bytes + std::max(partial_bytes, xg_bytes + xg_scale_bytes);
+  }
 };
 
-// Wide tiles unless they would leave SMs idle (their count, over the row tiles that the call
-// can have, is below the SM count): a narrow tile reads its rows for half as many weight
-// rows. Where even narrow tiles of phase 2 leave SMs idle (few pairs, a long reduction), the
-// reduction is split, into runs of at least four stages.
+// Pairs of CTAs unless their tiles would leave SMs idle (their count, over the row tiles that
+// the call can have, is below half of the SM count). Where even single tiles of phase 2 leave
+// SMs idle (few pairs, a long reduction), the reduction is split, into runs of at least four
+// stages.
 Plan make_plan(int64_t tokens, int experts, int top_k, int dim, int hidden, bool mx) {
   Plan q = {};
   q.pairs = tokens * top_k;
-  q.row_tiles = q.pairs / kTileM + std::min<int64_t>(experts, q.pairs);
+  const int64_t used = std::min<int64_t>(experts, q.pairs);  // experts with rows, at most
+  q.row_tiles = q.pairs / kTileM + used;
+  const int64_t row_pairs = q.pairs / (2 * kTileM) + used;
   const int64_t sms = sm_count();
-  const auto tiles = [&](int n, int per) { return q.row_tiles * ((n + per - 1) / per); };
-  q.wide1 = tiles(hidden, 128) >= sms;
-  q.wide2 = tiles(dim, 256) >= sms;
-  q.tiles1 = tiles(hidden, q.wide1 ? 128 : 64);
-  q.tiles2 = tiles(dim, q.wide2 ? 256 : 128);
+  const auto columns = [](int n, int per) { return static_cast<int64_t>((n + per - 1) / per); };
+  q.pair1 = row_pairs * columns(hidden, 128) >= sms / 2;
+  q.pair2 = row_pairs * columns(dim, 256) >= sms / 2;
+  q.tiles1 = q.pair1 ? row_pairs * columns(hidden, 128) : q.row_tiles * columns(hidden, 64);
+  q.tiles2 = q.pair2 ? row_pairs * columns(dim, 256) : q.row_tiles * columns(dim, 128);
   const int stages = (hidden + (mx ? 127 : 63)) / (mx ? 128 : 64);
   int64_t splits = 1;
-  if (q.tiles2 * 2 <= sms) splits = std::max<int64_t>(1, std::min<int64_t>(sms / q.tiles2, stages / 4));
+  if (!q.pair2 && q.tiles2 * 2 <= sms)
+    splits = std::max<int64_t>(1, std::min<int64_t>(sms / q.tiles2, stages / 4));
   q.split_stages = static_cast<int>((stages + splits - 1) / splits);
   q.splits = (stages + q.split_stages - 1) / q.split_stages;
   q.tiles2 *= q.splits;
   const size_t rows = static_cast<size_t>(q.row_tiles) * kTileM;
   q.h_bytes = up256(rows * hidden * (mx ? 1 : 2));
   q.h_scale_bytes = mx ? up256(static_cast<size_t>(q.row_tiles) * ((hidden + 127) / 128) * kMxTileBytes) : 0;
-  const bool direct = top_k == 1 && q.splits == 1;
-  q.partial_bytes = direct ? 0 : up256(static_cast<size_t>(q.splits) * q.pairs * dim * 4);
+  if (q.pair1) {
+    q.xg_bytes = up256(rows * dim * (mx ? 1 : 2));
+    q.xg_scale_bytes = mx ? up256(static_cast<size_t>(q.row_tiles) * ((dim + 127) / 128) * kMxTileBytes) : 0;
+  }
+  q.direct = top_k == 1 && q.splits == 1;
+  if (!q.direct)
+    q.partial_bytes = up256(static_cast<size_t>(q.splits) * q.pairs * dim * 4);
   return q;
 }
 
@@ -742,7 +986,7 @@ size_t dard_experts_workspace_size(int32_t tokens, int32_t experts, int32_t top_
   size_t most = 0;
   for (int mx = 0; mx < 2; ++mx) {
     const Plan q = make_plan(tokens, experts, top_k, dim, hidden, mx != 0);
-    most = std::max(most, q.h_bytes + q.h_scale_bytes + q.partial_bytes);
+    most = std::max(most, q.bytes());
   }
   return most;
 }
@@ -781,7 +1025,7 @@ dard_status dard_experts(const dard_experts_args* a, void* stream) {
              !aligned(a->w3_scale, 16) || !aligned(a->w2_scale, 16)))
     return report(DARD_ERR_ALIGN, "the scales and x_scale_stride must be multiples of 16 bytes");
   const Plan q = make_plan(a->tokens, a->experts, a->top_k, a->dim, a->hidden, mx);
-  const size_t need = q.h_bytes + q.h_scale_bytes + q.partial_bytes;
+  const size_t need = q.bytes();
   if (!a->workspace || a->workspace_bytes < need)
     return report(DARD_ERR_WORKSPACE, "workspace of %zu bytes needed", need);
   if (!aligned(a->workspace, 256)) return report(DARD_ERR_ALIGN, "workspace must be 256-byte aligned");
@@ -792,12 +1036,16 @@ dard_status dard_experts(const dard_experts_args* a, void* stream) {
   p.rows = a->rows;
   p.ids = a->ids;
   p.weights = a->weights;
+  p.x = a->x;
+  p.x_stride_bytes = a->x_stride * esz;
   p.x_scale = a->x_scale;
   p.scale_b[0] = a->w1_scale;
   p.scale_b[1] = a->w3_scale;
   p.h = ws;
   p.h_scale = ws + q.h_bytes;
   p.partial = reinterpret_cast<float*>(ws + q.h_bytes + q.h_scale_bytes);
+  p.xg = ws + q.h_bytes + q.h_scale_bytes;
+  p.xg_scale = p.xg + q.xg_bytes;
   p.y = a->y;
   p.status = a->status;
   p.x_scale_stride = a->x_scale_stride;
@@ -810,7 +1058,7 @@ dard_status dard_experts(const dard_experts_args* a, void* stream) {
   p.pairs = static_cast<int32_t>(q.pairs);
   p.max_row_tiles = static_cast<int32_t>(q.row_tiles);
   p.y_f32 = a->y_dtype == DARD_F32;
-  p.direct = q.partial_bytes == 0;
+  p.direct = q.direct;
   p.test_drop = -1;
   // Test hooks (failure-path tests; unset in normal operation): a wait bound, and a stage whose
   // weights never arrive.
@@ -821,40 +1069,49 @@ dard_status dard_experts(const dard_experts_args* a, void* stream) {
   const int stage = mx ? 128 : 64;
   cudaError_t e = std::getenv("DARD_TEST_FAIL_LAUNCH") ? cudaErrorLaunchFailure : cudaSuccess;
   CUtensorMap ma, mb0, mb1;
-  // phase 1: rows of x by token, rows of w1 and w3
+  // phase 1: rows of x (in the plan's order, or gathered by the kernel itself) and of w1 and w3
   const uint64_t drow = static_cast<uint64_t>(a->dim) * esz, hrow = static_cast<uint64_t>(a->hidden) * esz;
-  const uint32_t box1 = q.wide1 ? 128 : 64;
-  if (e == cudaSuccess &&
-      (!encode(&ma, a->x, mx, a->dim, a->tokens, 0, a->x_stride * esz, 1) ||
-       !encode(&mb0, a->w1, mx, a->dim, a->hidden, a->experts, drow, box1) ||
-       !encode(&mb1, a->w3, mx, a->dim, a->hidden, a->experts, drow, box1)))
+  const uint64_t rows = static_cast<uint64_t>(q.row_tiles) * kTileM;
+  const uint32_t box1 = q.pair1 ? 128 : 64;
+  if (e == cudaSuccess && (!encode(&mb0, a->w1, mx, a->dim, a->hidden, a->experts, drow, box1) ||
+                           !encode(&mb1, a->w3, mx, a->dim, a->hidden, a->experts, drow, box1) ||
+                           (q.pair1 && !encode(&ma, p.xg, mx, a->dim, rows, 0, drow, kTileM))))
     e = cudaErrorInvalidValue;
+  if (!q.pair1) ma = mb0;  // not used
+  if (e == cudaSuccess && q.pair1) {
+    const int64_t ctas = std::min<int64_t>((q.pairs + 7) / 8, 8ll * sm_count());
+    if (mx) gather_rows<true><<<static_cast<unsigned>(ctas), 256, 0, s>>>(p);
+    else gather_rows<false><<<static_cast<unsigned>(ctas), 256, 0, s>>>(p);
+    e = cudaGetLastError();
+  }
   if (e == cudaSuccess) {
+    p.a_scale = p.xg_scale;
     p.k_elems = a->dim;
     p.n_elems = a->hidden;
     p.n_tiles = (a->hidden + box1 - 1) / box1;
     p.k_stages = (a->dim + stage - 1) / stage;
     p.splits = 1;
     p.split_stages = p.k_stages;
-    e = mx ? launch_phase<true, 1>(p, q.wide1, q.tiles1, ma, mb0, mb1, s)
-           : launch_phase<false, 1>(p, q.wide1, q.tiles1, ma, mb0, mb1, s);
+    e = mx ? launch_phase<true, 1>(p, q.pair1, q.tiles1, ma, mb0, mb1, s)
+           : launch_phase<false, 1>(p, q.pair1, q.tiles1, ma, mb0, mb1, s);
   }
   // phase 2: rows of h, rows of w2
   if (e == cudaSuccess &&
-      (!encode(&ma, p.h, mx, a->hidden, static_cast<uint64_t>(q.row_tiles) * kTileM, 0, hrow, 32) ||
+      (!encode(&ma, p.h, mx, a->hidden, rows, 0, hrow, q.pair2 ? kTileM : kBoxRowsSingle) ||
        !encode(&mb0, a->w2, mx, a->hidden, a->dim, a->experts, hrow, 128)))
     e = cudaErrorInvalidValue;
   if (e == cudaSuccess) {
-    const int per = q.wide2 ? 256 : 128;
+    const int per = q.pair2 ? 256 : 128;
     p.scale_b[0] = a->w2_scale;
+    p.a_scale = p.h_scale;
     p.k_elems = a->hidden;
     p.n_elems = a->dim;
     p.n_tiles = (a->dim + per - 1) / per;
     p.k_stages = (a->hidden + stage - 1) / stage;
     p.splits = q.splits;
     p.split_stages = q.split_stages;
-    e = mx ? launch_phase<true, 2>(p, q.wide2, q.tiles2, ma, mb0, mb0, s)
-           : launch_phase<false, 2>(p, q.wide2, q.tiles2, ma, mb0, mb0, s);
+    e = mx ? launch_phase<true, 2>(p, q.pair2, q.tiles2, ma, mb0, mb0, s)
+           : launch_phase<false, 2>(p, q.pair2, q.tiles2, ma, mb0, mb0, s);
   }
   if (e == cudaSuccess && !p.direct)
     e = p.y_f32 ? launch_combine<float>(p, s) : launch_combine<__nv_bfloat16>(p, s);

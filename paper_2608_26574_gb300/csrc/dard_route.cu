@@ -1,10 +1,9 @@
 // dard_route.cu - dard_route: each token's experts and weights from its router logits, and the
 // plan (the (token, slot) pairs sorted by expert) that dard_experts reads on the device.
 //
-// route_topk, one warp per token: lane l holds experts l, l + 32, ... in registers as keys
-// whose unsigned order is the order of the choice; a slot is one warp-wide maximum of the keys
-// and one minimum of the indices that reach it (ties to the lowest index). The largest
-// call (38912 x 256 logits, 40 MB) is bound by these dependent rounds, not by HBM.
+// route_topk, one warp per token: lane l holds experts l, l + 32, ... in registers, as keys whose
+// unsigned order is the order of the choice (see choose()). The largest call (38912 x 256 logits,
+// 40 MB) is bound by the instructions of the scores and the choice, not by HBM.
 //
 // The plan is a stable counting sort. A CTA owns a run of consecutive tokens; route_topk
 // counts its pairs per expert, and plan_scatter (chained by programmatic dependent launch)
@@ -25,11 +24,15 @@
 namespace dard {
 namespace {
 
-constexpr int kRouteWarps = 16;                // route_topk
-constexpr int kRouteThreads = 32 * kRouteWarps;
-constexpr int kPlanWarps = 8;                  // plan_scatter
+constexpr int kPlanWarps = 32;                 // plan_scatter
 constexpr int kOneCtaTokens = 64;              // one CTA routes and plans up to this many
-constexpr uint32_t kNone = 0;                  // key of an expert that cannot be chosen
+constexpr uint32_t kNone = 0x007fffffu;        // key of -inf: an expert that cannot be chosen
+
+// Ints of a CTA's counts in the workspace: 16-byte rows.
+__host__ __device__ constexpr int count_row(int experts) { return (experts + 1 + 3) / 4 * 4; }
+
+// Warps of a route_topk CTA with kPer experts per lane (its registers allow no more).
+constexpr int route_warps(int per) { return per <= 8 ? 32 : 16; }
 
 struct RouteParams {
   const void* logits;
@@ -39,7 +42,7 @@ struct RouteParams {
   int32_t* offsets;
   int32_t* rows;
   uint32_t* status;
-  int32_t* counts;        // workspace [ctas][experts + 1]; the last: slots without an expert
+  int32_t* counts;        // workspace [ctas][count_row]: experts, then slots without an expert
   int64_t logits_stride;
   int32_t tokens, experts, top_k, groups, top_groups, group_size;
   int32_t scoring, renormalise;
@@ -48,10 +51,102 @@ struct RouteParams {
   float scale;
 };
 
-// Unsigned order = float order, every finite float above kNone.
+// Unsigned order = float order; -inf gives kNone, every finite float more.
 __device__ __forceinline__ uint32_t order_key(float f) {
-  const uint32_t b = __float_as_uint(f);
-  return b & 0x80000000u ? ~b : b | 0x80000000u;
+  const int32_t b = __float_as_int(f);
+  return static_cast<uint32_t>(b ^ ((b >> 31) | static_cast<int32_t>(0x80000000u)));
+}
+
+// Sorts v falling: Batcher's odd-even merge network.
+template <int kN>
+__device__ __forceinline__ void sort_falling(uint32_t (&v)[kN]) {
+#pragma unroll
+  for (int p = 1; p < kN; p *= 2) {
+#pragma unroll
+    for (int k = p; k >= 1; k /= 2) {
+#pragma unroll
+      for (int j = k % p; j <= kN - 1 - k; j += 2 * k) {
+#pragma unroll
+        for (int i = 0; i < k; ++i) {
+          if (i + j + k < kN && (i + j) / (2 * p) == (i + j + k) / (2 * p)) {
+            const uint32_t a = v[i + j], b = v[i + j + k];
+            v[i + j] = max(a, b);
+            v[i + j + k] = min(a, b);
+          }
+        }
+      }
+    }
+  }
+}
+
+// v[j] for a j that is no constant.
+template <int kN>
+__device__ __forceinline__ uint32_t pick(const uint32_t (&v)[kN], int j) {
+  uint32_t r = v[0];
+#pragma unroll
+  for (int i = 1; i < kN; ++i) r = i == j ? v[i] : r;
+  return r;
+}
+
+// The top_k largest keys (expert j * 32 + lane: key[j]), ties to the lowest expert: the id of slot
+// `lane`, -1 where no key above kNone is left. One slot after the other: the largest key of
+// the warp, and the lowest index that reaches it.
+template <int kPer>
+__device__ int choose_exactly(uint32_t (&key)[kPer], int top_k, int lane) {
+  int my_id = -1;
+  for (int s = 0; s < top_k; ++s) {
+    uint32_t best = key[0];
+#pragma unroll
+    for (int j = 1; j < kPer; ++j) best = max(best, key[j]);
+    const uint32_t most = __reduce_max_sync(0xffffffffu, best);
+    if (most <= kNone) break;
+    int e = INT_MAX;
+#pragma unroll
+    for (int j = kPer - 1; j >= 0; --j)
+      if (key[j] == most) e = j * 32 + lane;
+    const int first = __reduce_min_sync(0xffffffffu, e);
+    if (lane == s) my_id = first;
+#pragma unroll
+    for (int j = 0; j < kPer; ++j)
+      if (first == j * 32 + lane) key[j] = 0;
+  }
+  return my_id;
+}
+
+// The same, mostly for half the instructions. A key's low bits give way to kPer - 1 - j, each lane
+// sorts its keys once, and a slot is the largest head of the lanes' lists (the lowest lane that
+// reaches it) popped. Equal keys come out by rising j, then lane: by rising expert, as they
+// should. Keys that differ in the replaced bits alone could come out in the wrong order; they
+// follow one another then, which is looked at, and the token is done again exactly.
+template <int kPer>
+__device__ __forceinline__ int choose(uint32_t (&key)[kPer], int top_k, int lane) {
+  constexpr uint32_t kLow = kPer - 1;
+  uint32_t list[kPer];
+#pragma unroll
+  for (int j = 0; j < kPer; ++j) list[j] = (key[j] & ~kLow) | (kLow - j);
+  sort_falling(list);
+  int my_id = -1;
+  uint32_t last = 0;  // the slot before: its head and lane
+  int last_lane = 0;
+  for (int s = 0; s <= top_k; ++s) {  // (one more than is kept, for the look)
+    const uint32_t most = __reduce_max_sync(0xffffffffu, list[0]);
+    if (most <= kNone) break;
+    const int from = __ffs(__ballot_sync(0xffffffffu, list[0] == most)) - 1;
+    if (kPer > 1 && s > 0 && (most ^ last) <= kLow) {
+      const uint32_t a = __shfl_sync(0xffffffffu, pick(key, kLow - (last & kLow)), last_lane);
+      const uint32_t b = __shfl_sync(0xffffffffu, pick(key, kLow - (most & kLow)), from);
+      if (a != b) return choose_exactly<kPer>(key, top_k, lane);
+    }
+    if (lane == s) my_id = static_cast<int>(kLow - (most & kLow)) * 32 + from;
+    last = most;
+    last_lane = from;
+    if (lane == from) {
+#pragma unroll
+      for (int j = 0; j < kPer - 1; ++j) list[j] = list[j + 1];
+      list[kPer - 1] = 0;
+    }
+  }
+  return lane < top_k ? my_id : -1;
 }
 
 __device__ __forceinline__ float logit(const __nv_bfloat16* p) { return __bfloat162float(*p); }
@@ -88,24 +183,39 @@ __device__ __forceinline__ uint32_t kept_groups(const RouteParams& p, const floa
   return __ballot_sync(0xffffffffu, lane < p.groups && better < p.top_groups);
 }
 
-// One token by one warp. kPer: experts per lane. Returns the id of slot `lane` (-1: none).
-template <typename T, int kPer>
-__device__ __forceinline__ int route_token(const RouteParams& p, int64_t token, float* choice_smem,
-                                           int lane) {
-  const T* l = static_cast<const T*>(p.logits) + token * p.logits_stride;
-  float score[kPer];
-  uint32_t key[kPer];
-  bool bad = false;
-  float top = -INFINITY;
+// What a lane knows of its experts j * 32 + lane, whatever the token.
+template <int kPer>
+struct LaneExperts {
+  float bias[kPer];      // 0 without a bias
+  uint32_t group[kPer];  // bit of the expert's group; 0: no such expert
+};
+
+template <int kPer>
+__device__ __forceinline__ LaneExperts<kPer> lane_experts(const RouteParams& p, int lane) {
+  LaneExperts<kPer> x;
 #pragma unroll
   for (int j = 0; j < kPer; ++j) {
     const int e = j * 32 + lane;
-    score[j] = e < p.experts ? logit(l + e) : -INFINITY;
-    bad |= !(score[j] < INFINITY);  // +inf or NaN
-    top = fmaxf(top, score[j]);
+    x.bias[j] = p.bias != nullptr && e < p.experts ? p.bias[e] : 0.f;
+    x.group[j] = e < p.experts ? 1u << (e / p.group_size) : 0u;
   }
-  bad = __any_sync(0xffffffffu, bad);
-  if (bad) {
+  return x;
+}
+
+// One token by one warp. kPer: experts per lane. Returns the id of slot `lane` (-1: none).
+template <typename T, int kPer>
+__device__ __forceinline__ int route_token(const RouteParams& p, const LaneExperts<kPer>& mine,
+                                           int64_t token, float* choice_smem, int lane) {
+  const T* l = static_cast<const T*>(p.logits) + token * p.logits_stride;
+  const bool softmax = p.scoring == DARD_ROUTE_SOFTMAX;
+  float choice[kPer];
+  bool bad = false;
+#pragma unroll
+  for (int j = 0; j < kPer; ++j) {
+    choice[j] = mine.group[j] != 0 ? logit(l + j * 32 + lane) : -INFINITY;
+    bad |= !(choice[j] < INFINITY);  // +inf or NaN
+  }
+  if (__any_sync(0xffffffffu, bad)) {
     if (lane == 0 && p.status) atomicOr(p.status, DARD_STATUS_INVALID_ROW);
     if (lane < p.top_k) {
       p.ids[token * p.top_k + lane] = -1;
@@ -113,236 +223,219 @@ __device__ __forceinline__ int route_token(const RouteParams& p, int64_t token, 
     }
     return -1;
   }
-  float total = 0.f;  // SOFTMAX: the sum of the exponentials
-  if (p.scoring == DARD_ROUTE_SOFTMAX) {
+  uint32_t on = 0;  // bit j: this lane's expert j exists and is on
+#pragma unroll
+  for (int j = 0; j < kPer; ++j) on |= choice[j] > -INFINITY ? 1u << j : 0u;
+  float top = 0.f, total = 1.f;  // SOFTMAX: the largest logit, the sum of the exponentials
+  if (softmax) {
+    top = choice[0];
+#pragma unroll
+    for (int j = 1; j < kPer; ++j) top = fmaxf(top, choice[j]);
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
     if (top == -INFINITY) top = 0.f;  // every expert is off
-  }
-  uint32_t off = 0;  // bit j: this lane's expert j is off (or does not exist)
+    total = 0.f;
 #pragma unroll
-  for (int j = 0; j < kPer; ++j) {
-    if (score[j] == -INFINITY) off |= 1u << j;
-    if (p.scoring == DARD_ROUTE_SOFTMAX) {
-      score[j] = expf(score[j] - top);
-      total += score[j];
-    } else {
-      score[j] = 1.f / (1.f + expf(-score[j]));
+    for (int j = 0; j < kPer; ++j) {
+      choice[j] = expf(choice[j] - top);
+      total += choice[j];
     }
-  }
-  if (p.scoring == DARD_ROUTE_SOFTMAX) {
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) total += __shfl_xor_sync(0xffffffffu, total, o);
     // Without a bias the exponentials are in the scores' order already (and the sums of two
-    // in theirs), and the chosen ones are divided at the end.
+    // in theirs), and only the chosen ones are divided, at the end.
     if (p.bias != nullptr) {
 #pragma unroll
-      for (int j = 0; j < kPer; ++j) score[j] /= total;
-      total = 1.f;
+      for (int j = 0; j < kPer; ++j) choice[j] /= total;
     }
   } else {
-    total = 1.f;
+#pragma unroll
+    for (int j = 0; j < kPer; ++j) choice[j] = 1.f / (1.f + expf(-choice[j]));
   }
-  float choice[kPer];
+  uint32_t key[kPer];
 #pragma unroll
   for (int j = 0; j < kPer; ++j) {
-    const int e = j * 32 + lane;
-    choice[j] = score[j];
-    if (p.bias != nullptr && e < p.experts) choice[j] += __ldg(p.bias + e);
-    if (off >> j & 1) choice[j] = -INFINITY;
-    key[j] = choice[j] > -INFINITY ? order_key(choice[j]) : kNone;  // a NaN bias: never chosen
+    choice[j] = on >> j & 1 ? choice[j] + mine.bias[j] : -INFINITY;  // (+ 0 without a bias)
+    key[j] = order_key(choice[j]);
   }
   if (p.top_groups < p.groups) {
     __syncwarp();
 #pragma unroll
-    for (int j = 0; j < kPer; ++j) {
-      const int e = j * 32 + lane;
-      if (e < p.experts) choice_smem[e] = key[j] == kNone ? -INFINITY : choice[j];
-    }
+    for (int j = 0; j < kPer; ++j)
+      if (mine.group[j] != 0) choice_smem[j * 32 + lane] = choice[j];
     __syncwarp();
     const uint32_t keep = kept_groups(p, choice_smem, lane);
 #pragma unroll
-    for (int j = 0; j < kPer; ++j) {
-      const int e = j * 32 + lane;
-      if (e < p.experts && !(keep >> (e / p.group_size) & 1)) key[j] = kNone;
-    }
-  }
-  int my_id = -1;        // slot `lane`
-  float my_weight = 0.f;
-  for (int s = 0; s < p.top_k; ++s) {
-    uint32_t best = key[0];
-#pragma unroll
-    for (int j = 1; j < kPer; ++j) best = max(best, key[j]);
-    const uint32_t most = __reduce_max_sync(0xffffffffu, best);
-    if (most == kNone) break;  // no expert is left
-    int e = INT_MAX;
-    float w = 0.f;
-#pragma unroll
-    for (int j = kPer - 1; j >= 0; --j) {
-      if (key[j] == most) {
-        e = j * 32 + lane;
-        w = score[j];
-      }
-    }
-    const int first = __reduce_min_sync(0xffffffffu, e);
-    w = __shfl_sync(0xffffffffu, w, first & 31);
-    if (lane == s) {
-      my_id = first;
-      my_weight = w;
-    }
-#pragma unroll
     for (int j = 0; j < kPer; ++j)
-      if (first == j * 32 + lane) key[j] = kNone;
+      if ((keep & mine.group[j]) == 0) key[j] = kNone;
   }
-  if (p.renormalise) {  // the softmax's own division cancels
-    float sum = my_weight;
+  const int my_id = choose<kPer>(key, p.top_k, lane);
+  // the chosen experts' scores, from their logits again
+  float weight = 0.f;
+  if (my_id >= 0) {
+    const float x = logit(l + my_id);
+    weight = softmax ? expf(x - top) / total : 1.f / (1.f + expf(-x));
+  }
+  if (p.renormalise) {
+    float sum = weight;
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
-    my_weight = sum > 0.f ? my_weight / sum : 0.f;
-  } else if (my_id >= 0) {
-    my_weight /= total;
+    weight = sum > 0.f ? weight / sum : 0.f;
   }
   if (lane < p.top_k) {
     p.ids[token * p.top_k + lane] = my_id;
-    p.weights[token * p.top_k + lane] = my_weight * p.scale;
+    p.weights[token * p.top_k + lane] = weight * p.scale;
   }
   return my_id;
 }
 
-// Exclusive prefix sums over n <= 1024 values in shared memory, by the whole CTA.
-__device__ void exclusive_scan(int32_t* v, int n, int32_t* warp_sums) {
+// Exclusive prefix sums over v[0 .. n) in shared memory, and their total in v[n], by the whole CTA
+// (n at most its threads).
+__device__ __forceinline__ void exclusive_scan(int32_t* v, int n, int32_t* warp_sums) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
-  int32_t carry = 0;
-  for (int base = 0; base < n; base += blockDim.x) {
-    const int i = base + threadIdx.x;
-    const int32_t x = i < n ? v[i] : 0;
-    int32_t s = x;
+  const int32_t x = static_cast<int>(threadIdx.x) < n ? v[threadIdx.x] : 0;
+  int32_t s = x;
 #pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-      const int32_t y = __shfl_up_sync(0xffffffffu, s, o);
-      if (lane >= o) s += y;
-    }
-    if (lane == 31) warp_sums[warp] = s;
-    __syncthreads();
-    int32_t before = carry;
-    for (int w = 0; w < warps; ++w) {
-      const int32_t ws = warp_sums[w];
-      if (w < warp) before += ws;
-      carry += ws;
-    }
-    if (i < n) v[i] = before + s - x;
-    __syncthreads();
+  for (int o = 1; o < 32; o <<= 1) {
+    const int32_t y = __shfl_up_sync(0xffffffffu, s, o);
+    if (lane >= o) s += y;
   }
+  if (lane == 31) warp_sums[warp] = s;
+  __syncthreads();
+  const int32_t w = lane < warps ? warp_sums[lane] : 0;
+  const int32_t before = __reduce_add_sync(0xffffffffu, lane < warp ? w : 0);
+  if (static_cast<int>(threadIdx.x) < n) v[threadIdx.x] = before + s - x;
+  const int32_t all = __reduce_add_sync(0xffffffffu, w);
+  if (threadIdx.x == 0) v[n] = all;
+  __syncthreads();
 }
 
 // Places of the pairs of tokens [t0, t1): next[b] is the place of the CTA's first pair of
 // bucket b (expert, or `experts` for slots without one). Warp w takes the w-th run of pairs:
 // it counts them (hist), the runs' counts are summed over the warps, then it places them, 32
-// at a time, in order. Every warp of the CTA takes part; `warps` of them have pairs.
-__device__ void place_pairs(const RouteParams& p, int t0, int t1, const int32_t* next,
-                            int32_t* hist, int warps) {
+// at a time, in order.
+template <int kWarps>
+__device__ __forceinline__ void place_pairs(const RouteParams& p, int t0, int t1,
+                                            const int32_t* next, int32_t* hist) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, buckets = p.experts + 1;
-  for (int i = threadIdx.x; i < warps * buckets; i += blockDim.x) hist[i] = 0;
+  for (int i = threadIdx.x; i < kWarps * buckets; i += blockDim.x) hist[i] = 0;
   __syncthreads();
   const int64_t base = static_cast<int64_t>(t0) * p.top_k;
   const int pairs = (t1 - t0) * p.top_k;
-  const int per = ((pairs + warps - 1) / warps + 31) / 32 * 32;
+  const int per = ((pairs + kWarps - 1) / kWarps + 31) / 32 * 32;
   const int i0 = warp * per, i1 = min(pairs, i0 + per);
   int32_t* mine = hist + warp * buckets;
-  if (warp < warps) {
-    for (int i = i0 + lane; i < i1; i += 32) {
-      const int id = p.ids[base + i];
-      atomicAdd(&mine[id < 0 ? p.experts : id], 1);
-    }
+  for (int i = i0 + lane; i < i1; i += 32) {
+    const int id = p.ids[base + i];
+    atomicAdd(&mine[id < 0 ? p.experts : id], 1);
   }
   __syncthreads();
   for (int b = threadIdx.x; b < buckets; b += blockDim.x) {
     int32_t at = next[b];
-    for (int w = 0; w < warps; ++w) {
-      const int32_t n = hist[w * buckets + b];
-      hist[w * buckets + b] = at;
-      at += n;
+#pragma unroll 1
+    for (int w0 = 0; w0 < kWarps; w0 += 8) {
+      int32_t n[8];
+#pragma unroll
+      for (int w = 0; w < 8; ++w) n[w] = hist[(w0 + w) * buckets + b];
+#pragma unroll
+      for (int w = 0; w < 8; ++w) {
+        hist[(w0 + w) * buckets + b] = at;
+        at += n[w];
+      }
     }
   }
   __syncthreads();
-  if (warp < warps) {
-    for (int i = i0; i < i1; i += 32) {
-      const bool in = i + lane < i1;
-      const int id = in ? p.ids[base + i + lane] : -1;
-      const int b = !in ? buckets : id < 0 ? p.experts : id;
-      const uint32_t same = __match_any_sync(0xffffffffu, b);
-      const int rank = __popc(same & ((1u << lane) - 1));
-      if (in) p.rows[mine[b] + rank] = id < 0 ? -1 : static_cast<int32_t>(base) + i + lane;
-      __syncwarp();
-      if (in && rank == 0) mine[b] += __popc(same);
-      __syncwarp();
-    }
+  for (int i = i0; i < i1; i += 32) {
+    const bool in = i + lane < i1;
+    const int id = in ? p.ids[base + i + lane] : -1;
+    const int b = !in ? buckets : id < 0 ? p.experts : id;
+    const uint32_t same = __match_any_sync(0xffffffffu, b);
+    const int rank = __popc(same & ((1u << lane) - 1));
+    if (in) p.rows[mine[b] + rank] = id < 0 ? -1 : static_cast<int32_t>(base) + i + lane;
+    __syncwarp();
+    if (in && rank == 0) mine[b] += __popc(same);
+    __syncwarp();
   }
 }
 
 template <typename T, int kPer>
-__global__ void __launch_bounds__(kRouteThreads) route_topk(const __grid_constant__ RouteParams p) {
+__global__ void __launch_bounds__(32 * route_warps(kPer), 1)
+    route_topk(const __grid_constant__ RouteParams p) {
   grid_dep_launch();  // plan_scatter may be scheduled; it waits for this grid's end
+  constexpr int kWarps = route_warps(kPer);
   extern __shared__ int32_t smem[];
-  // choices of each warp's token (groups only), then the counts, then one_cta's buckets
+  // choices of each warp's token (groups only), then the counts, then one CTA's buckets
   float* choice = reinterpret_cast<float*>(smem);
-  const bool grouped = p.top_groups < p.groups;
-  int32_t* count = smem + (grouped ? kRouteWarps * p.experts : 0);
+  int32_t* count = smem + (p.top_groups < p.groups ? kWarps * p.experts : 0);
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int t0 = blockIdx.x * p.cta_tokens, t1 = min(p.tokens, t0 + p.cta_tokens);
   const bool plan = p.rows != nullptr;
   if (plan) {
-    for (int i = threadIdx.x; i <= p.experts; i += kRouteThreads) count[i] = 0;
+    for (int i = threadIdx.x; i <= p.experts; i += blockDim.x) count[i] = 0;
     __syncthreads();
   }
-  for (int t = t0 + warp; t < t1; t += kRouteWarps) {
-    const int id = route_token<T, kPer>(p, t, choice + warp * p.experts, lane);
+  const LaneExperts<kPer> mine = lane_experts<kPer>(p, lane);
+  for (int t = t0 + warp; t < t1; t += kWarps) {
+    const int id = route_token<T, kPer>(p, mine, t, choice + warp * p.experts, lane);
     if (plan && lane < p.top_k) atomicAdd(&count[id < 0 ? p.experts : id], 1);
   }
   if (!plan) return;
   __syncthreads();
   if (p.ctas > 1) {
-    for (int i = threadIdx.x; i <= p.experts; i += kRouteThreads)
-      p.counts[static_cast<int64_t>(blockIdx.x) * (p.experts + 1) + i] = count[i];
+    const int row = count_row(p.experts);
+    for (int i = threadIdx.x; i < row; i += blockDim.x)
+      p.counts[static_cast<int64_t>(blockIdx.x) * row + i] = i <= p.experts ? count[i] : 0;
     return;
   }
   // one CTA: its counts are the totals
-  __shared__ int32_t warp_sums[kRouteWarps];
-  exclusive_scan(count, p.experts + 1, warp_sums);
-  for (int i = threadIdx.x; i <= p.experts; i += kRouteThreads) p.offsets[i] = count[i];
-  place_pairs(p, t0, t1, count, count + p.experts + 1, kPlanWarps);
+  __shared__ int32_t warp_sums[kWarps];
+  exclusive_scan(count, p.experts, warp_sums);
+  for (int i = threadIdx.x; i <= p.experts; i += blockDim.x) p.offsets[i] = count[i];
+  place_pairs<kWarps>(p, t0, t1, count, count + p.experts + 1);
 }
 
+// Every CTA adds up, per bucket, the counts of all CTAs and of those before it (each thread four
+// buckets of every kRuns-th CTA, its loads in flight together), then places its own pairs.
 __global__ void __launch_bounds__(32 * kPlanWarps)
     plan_scatter(const __grid_constant__ RouteParams p) {
   extern __shared__ int32_t smem[];
   __shared__ int32_t warp_sums[kPlanWarps];
-  const int buckets = p.experts + 1;
-  int32_t* next = smem;             // [buckets] totals, then places
-  int32_t* before = next + buckets; // [buckets] pairs of the CTAs before this one
-  int32_t* hist = before + buckets; // [kPlanWarps][buckets]
+  const int buckets = p.experts + 1, row = count_row(p.experts), quads = row / 4;
+  int32_t* next = smem;          // [row] totals, then places
+  int32_t* before = next + row;  // [row] pairs of the CTAs before this one
+  int32_t* hist = before + row;  // [kPlanWarps][buckets]
+  for (int i = threadIdx.x; i < 2 * row; i += blockDim.x) next[i] = 0;
+  __syncthreads();
+  const int runs = blockDim.x / quads, run = threadIdx.x / quads, quad = threadIdx.x % quads;
   grid_dep_wait();
-  for (int b = threadIdx.x; b < buckets; b += blockDim.x) {
-    int32_t total = 0, prior = 0;
-    const int32_t* c = p.counts + b;
-#pragma unroll 8
-    for (int i = 0; i < p.ctas; ++i) {
-      const int32_t n = c[static_cast<int64_t>(i) * buckets];
-      total += n;
-      if (i < static_cast<int>(blockIdx.x)) prior += n;
+  if (run < runs) {
+    int4 total = make_int4(0, 0, 0, 0), prior = total;
+    const int4* c = reinterpret_cast<const int4*>(p.counts) + quad;
+#pragma unroll 16
+    for (int i = run; i < p.ctas; i += runs) {
+      const int4 n = c[static_cast<int64_t>(i) * quads];
+      const bool b = i < static_cast<int>(blockIdx.x);
+      total.x += n.x; total.y += n.y; total.z += n.z; total.w += n.w;
+      prior.x += b ? n.x : 0; prior.y += b ? n.y : 0; prior.z += b ? n.z : 0; prior.w += b ? n.w : 0;
     }
-    next[b] = total;
-    before[b] = prior;
+    atomicAdd(&next[4 * quad], total.x);
+    atomicAdd(&next[4 * quad + 1], total.y);
+    atomicAdd(&next[4 * quad + 2], total.z);
+    atomicAdd(&next[4 * quad + 3], total.w);
+    atomicAdd(&before[4 * quad], prior.x);
+    atomicAdd(&before[4 * quad + 1], prior.y);
+    atomicAdd(&before[4 * quad + 2], prior.z);
+    atomicAdd(&before[4 * quad + 3], prior.w);
   }
   __syncthreads();
-  exclusive_scan(next, buckets, warp_sums);
-  for (int b = threadIdx.x; b < buckets; b += blockDim.x) {
-    if (blockIdx.x == 0) p.offsets[b] = next[b];
-    next[b] += before[b];
+  exclusive_scan(next, p.experts, warp_sums);
+  if (static_cast<int>(threadIdx.x) < buckets) {
+    if (blockIdx.x == 0) p.offsets[threadIdx.x] = next[threadIdx.x];
+    next[threadIdx.x] += before[threadIdx.x];
   }
   __syncthreads();
   const int t0 = blockIdx.x * p.cta_tokens, t1 = min(p.tokens, t0 + p.cta_tokens);
-  place_pairs(p, t0, t1, next, hist, kPlanWarps);
+  place_pairs<kPlanWarps>(p, t0, t1, next, hist);
 }
 
 // With no token at all every expert's run is empty.
@@ -355,28 +448,36 @@ __global__ void empty_plan(int32_t* offsets, int n) {
 int cta_tokens_for(int tokens) {
   if (tokens <= kOneCtaTokens) return std::max(tokens, 1);
   const int sms = sm_count();
-  return std::max(kRouteWarps, (tokens + sms - 1) / sms);
+  return std::max(32, (tokens + sms - 1) / sms);
 }
 
 template <typename T, int kPer>
 cudaError_t launch_typed(const RouteParams& p, cudaStream_t s) {
   const size_t buckets = static_cast<size_t>(p.experts) + 1;
   const bool plan = p.rows != nullptr;
-  size_t ints = p.top_groups < p.groups ? static_cast<size_t>(kRouteWarps) * p.experts : 0;
+  constexpr int kWarps = route_warps(kPer);
+  constexpr size_t kMost = 100 * 1024;  // 32 warps' choices and buckets of 256 experts: 67 KB
+  size_t ints = p.top_groups < p.groups ? static_cast<size_t>(kWarps) * p.experts : 0;
   if (plan) ints += buckets;
-  if (plan && p.ctas == 1) ints += kPlanWarps * buckets;
+  if (plan && p.ctas == 1) ints += kWarps * buckets;
   if (ints * 4 > 48 * 1024) {
     static std::atomic<uint64_t> done{0};
-    const cudaError_t e = ensure_smem_attr(route_topk<T, kPer>, 64 * 1024, done);
+    const cudaError_t e = ensure_smem_attr(route_topk<T, kPer>, kMost, done);
     if (e != cudaSuccess) return e;
   }
-  route_topk<T, kPer><<<p.ctas, kRouteThreads, ints * 4, s>>>(p);
+  route_topk<T, kPer><<<p.ctas, 32 * kWarps, ints * 4, s>>>(p);
   cudaError_t e = cudaGetLastError();
   if (e != cudaSuccess || !plan || p.ctas == 1) return e;
+  const size_t plan_smem = (2 * static_cast<size_t>(count_row(p.experts)) + kPlanWarps * buckets) * 4;
+  if (plan_smem > 48 * 1024) {
+    static std::atomic<uint64_t> done{0};
+    e = ensure_smem_attr(plan_scatter, kMost, done);
+    if (e != cudaSuccess) return e;
+  }
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(p.ctas);
   cfg.blockDim = dim3(32 * kPlanWarps);
-  cfg.dynamicSmemBytes = (2 + kPlanWarps) * buckets * 4;
+  cfg.dynamicSmemBytes = plan_smem;
   cfg.stream = s;
   cudaLaunchAttribute attr[1];
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
@@ -411,7 +512,7 @@ size_t dard_route_workspace_size(int32_t tokens, int32_t experts, int32_t top_k)
   if (!sizes_ok(tokens, experts, top_k)) return 0;
   const int per = cta_tokens_for(tokens);
   const size_t ctas = (static_cast<size_t>(tokens) + per - 1) / per;
-  return ctas <= 1 ? 0 : ctas * (static_cast<size_t>(experts) + 1) * 4;
+  return ctas <= 1 ? 0 : ctas * count_row(experts) * 4;
 }
 
 dard_status dard_route(const dard_route_args* a, void* stream) {
@@ -458,8 +559,8 @@ dard_status dard_route(const dard_route_args* a, void* stream) {
   const size_t need = a->rows ? dard_route_workspace_size(a->tokens, a->experts, a->top_k) : 0;
   if (need > 0 && (!a->workspace || a->workspace_bytes < need))
     return report(DARD_ERR_WORKSPACE, "workspace of %zu bytes needed", need);
-  if (need > 0 && reinterpret_cast<uintptr_t>(a->workspace) % 4 != 0)
-    return report(DARD_ERR_ALIGN, "workspace must be 4-byte aligned");
+  if (need > 0 && reinterpret_cast<uintptr_t>(a->workspace) % 16 != 0)
+    return report(DARD_ERR_ALIGN, "workspace must be 16-byte aligned");
   RouteParams p = {};
   p.logits = a->logits;
   p.bias = a->bias;
