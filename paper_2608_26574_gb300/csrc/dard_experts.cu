@@ -62,20 +62,29 @@ namespace {
 constexpr int kTileM = 128;            // rows of A per CTA
 constexpr int kTileB = 128;            // weight rows per CTA
 constexpr int kStageK = 128;           // bytes of K per stage
-constexpr int kStages = 6;
-constexpr int kThreads = 384;
-constexpr int kEpilogueWarps = 8;
-constexpr int kProducerWarp = 8, kIssueWarp = 9, kGatherWarp = 10;
+constexpr int kMaxStages = 6;
 constexpr int kGatherWarps = 2;
 constexpr int kGatherLag = 2;          // stages a gather warp has in flight
 constexpr uint32_t kBytesA = kTileM * kStageK, kBytesB = kTileB * kStageK;
 constexpr uint32_t kStageBytes = kBytesA + kBytesB;
 constexpr uint32_t kScaleBytes = 3 * kMxTileBytes;  // of a stage: A's, then two tiles of B's
-constexpr uint32_t kTmemAll = 512;
-constexpr uint32_t kScaleCol = 256;    // first TMEM column of the scales
 constexpr int kGroupM = 16;            // row tiles that share a pass over an expert's columns
 constexpr int kBoxRowsSingle = 32;     // rows of h per copy (single: its tiles hold few rows)
 constexpr uint16_t kBothCtas = 0x3;
+
+// The two variants. A single CTA takes half of an SM's registers, shared memory and TMEM, so that
+// the next launch's CTAs, which do not depend on this one for their weights, can sit next to it.
+template <bool kPair>
+struct Shape {
+  static constexpr int kStages = kPair ? 6 : 3;
+  static constexpr int kEpilogueWarps = kPair ? 8 : 4;
+  static constexpr int kProducerWarp = kEpilogueWarps, kIssueWarp = kProducerWarp + 1,
+                       kGatherWarp = kIssueWarp + 1;
+  static constexpr int kThreads = 32 * (kGatherWarp + kGatherWarps);
+  static constexpr uint32_t kTmem = kPair ? 512 : 256;
+  static constexpr uint32_t kScaleCol = kPair ? 256 : 128;  // first TMEM column of the scales
+  static constexpr int kCtasPerSm = kPair ? 1 : 2;
+};
 
 struct ExpertsParams {
   const int32_t* offsets;
@@ -159,6 +168,18 @@ __device__ __forceinline__ void mma_ss_pair(uint32_t d, uint64_t a, uint64_t b, 
       "l"(a), "l"(b), "r"(idesc), "r"(accumulate)
       : "memory");
 }
+// Whether the phase with this parity has completed, without waiting.
+__device__ __forceinline__ bool mbar_test(uint64_t* bar, uint32_t parity) {
+  uint32_t ok;
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "mbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
+      "selp.u32 %0, 1, 0, p;\n\t}"
+      : "=r"(ok)
+      : "r"(smem_u32(bar)), "r"(parity)
+      : "memory");
+  return ok != 0;
+}
 // One lane of a converged warp.
 __device__ __forceinline__ bool elect_one() {
   uint32_t r;
@@ -189,8 +210,8 @@ __host__ __device__ constexpr uint32_t idesc_mx(uint32_t M, uint32_t N, uint32_t
 }
 
 struct __align__(16) Ctl {
-  uint64_t full[kStages], empty[kStages];
-  uint64_t peer_full[kStages];  // pair, rank 0: rank 1's stage is full
+  uint64_t full[kMaxStages], empty[kMaxStages];
+  uint64_t peer_full[kMaxStages];  // pair, rank 0: rank 1's stage is full
   uint64_t acc_full, acc_free;
   uint64_t drained;  // every MMA the issuer launched has completed
   uint32_t tmem_base;
@@ -200,8 +221,9 @@ struct __align__(16) Ctl {
   int32_t first_unit[DARD_MAX_EXPERTS + 1];  // the same in units of a tile: 1 or 2 row tiles
 };
 
+template <bool kPair>
 constexpr size_t smem_bytes() {
-  return 1024 + static_cast<size_t>(kStages) * (kStageBytes + kScaleBytes) + sizeof(Ctl);
+  return 1024 + static_cast<size_t>(Shape<kPair>::kStages) * (kStageBytes + kScaleBytes) + sizeof(Ctl);
 }
 
 // A CTA's part of one tile: rows [row, row + count) (count <= 0: none) of expert e, in row tile
@@ -285,7 +307,7 @@ __device__ __forceinline__ uint32_t pack2(float lo, float hi) {
 }
 
 template <bool kMx, bool kPair, int kPhase>
-__global__ void __launch_bounds__(kThreads, 1)
+__global__ void __launch_bounds__(Shape<kPair>::kThreads, Shape<kPair>::kCtasPerSm)
     product(const __grid_constant__ ExpertsParams p, const __grid_constant__ CUtensorMap map_a,
             const __grid_constant__ CUtensorMap map_b0, const __grid_constant__ CUtensorMap map_b1) {
   constexpr int kCtas = kPair ? 2 : 1;
@@ -296,7 +318,8 @@ __global__ void __launch_bounds__(kThreads, 1)
   constexpr int kCols = kPhase == 1 ? kN / 2 : kN;
   constexpr bool kGather = kPhase == 1 && !kPair;  // the A rows come from warps 10-11
   constexpr int kBoxA = kPair ? kTileM : kBoxRowsSingle;
-  grid_dep_launch();
+  using S = Shape<kPair>;
+  constexpr int kStages = S::kStages;
   extern __shared__ uint8_t smem_raw[];
   uint8_t* base = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) &
                                              ~static_cast<uintptr_t>(1023));
@@ -309,23 +332,23 @@ __global__ void __launch_bounds__(kThreads, 1)
   // rank 0's copy of a barrier (the one the issuer waits on)
   const auto lead = [](uint64_t* bar) { return map_shared_rank(smem_u32(bar), 0); };
 
-  if (warp == kIssueWarp) {
+  if (warp == S::kIssueWarp) {
     if constexpr (kPair) {
-      tmem_alloc_pair<kTmemAll>(&ctl.tmem_base);
+      tmem_alloc_pair<S::kTmem>(&ctl.tmem_base);
       tmem_relinquish_pair();
     } else {
-      tmem_alloc<kTmemAll>(&ctl.tmem_base);
+      tmem_alloc<S::kTmem>(&ctl.tmem_base);
       tmem_relinquish();
     }
   }
-  if (warp == kProducerWarp && lane == 0) {
+  if (warp == S::kProducerWarp && lane == 0) {
     for (int b = 0; b < kStages; ++b) {
       mbar_init(&ctl.full[b], kGather ? 1 + kGatherWarps : 1);
       mbar_init(&ctl.empty[b], 1);
       mbar_init(&ctl.peer_full[b], 1);
     }
     mbar_init(&ctl.acc_full, 1);
-    mbar_init(&ctl.acc_free, kEpilogueWarps * kCtas);
+    mbar_init(&ctl.acc_free, S::kEpilogueWarps * kCtas);
     mbar_init(&ctl.drained, 1);
     ctl.abort = 0;
     fence_barrier_init();
@@ -333,7 +356,10 @@ __global__ void __launch_bounds__(kThreads, 1)
     tma_prefetch_desc(&map_b0);
     if (kPhase == 1) tma_prefetch_desc(&map_b1);
   }
-  // (offsets were complete before this call's first kernel began)
+  // The call's first launch waits for what is before it on the stream, and only then lets the
+  // next one start: that one may read the plan and the weights at once.
+  if (kGather) grid_dep_wait();
+  grid_dep_launch();
   read_plan<kCtas>(p, ctl.first_row, ctl.first_tile, ctl.first_unit);
   tc_fence_before();
   if constexpr (kPair) cluster_sync();  // both CTAs' barriers exist, TMEM is allocated
@@ -351,7 +377,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     return !*abort_flag && (use < kStages || mbar_wait(&ctl.empty[b], ((use / kStages) - 1) & 1, limit));
   };
 
-  if (warp == kProducerWarp) {
+  if (warp == S::kProducerWarp) {
     // -------------------------------------------------------------- TMA producer
     // As the issuer: uniform over the warp, one elected lane issues. (Copies issued by several
     // lanes, or by a lane of a diverged warp, cost the warp about 80 cycles each.)
@@ -359,7 +385,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     bool ok = true;
     Tile t;
     const bool issue = elect_one();
-    if (!kGather) grid_dep_wait();  // the rows of A are complete
+    bool waited = kGather;  // for the launch before this one, which writes the rows of A
     for (int64_t w = first; ok && get_tile<kPair>(p, ctl, rank, w, e, t); w += step) {
       const int boxes_a = kGather ? 0 : (max(t.count, 0) + kBoxA - 1) / kBoxA;
       const int k0 = t.split * split_stages, k1 = min(p.k_stages, k0 + split_stages);
@@ -373,35 +399,57 @@ __global__ void __launch_bounds__(kThreads, 1)
       const uint8_t* sf_b0 = p.scale_b[0] + at_b;
       const uint8_t* sf_b1 = kPhase == 1 ? p.scale_b[1] + at_b : sf_b0 + step_b;
       const uint8_t* sf_a = p.a_scale + t.row_tile * step_b;
-      for (int k = k0; k < k1; ++k, ++use) {
+      const auto load_b = [&](int k, int b) {
+        uint8_t* sb = base + b * kStageBytes + kBytesA;
+        uint8_t* ss = s_scale + b * kScaleBytes;
+        uint64_t* bar = &ctl.full[b];
+        mbar_arrive_expect_tx(bar, bytes);
+        if (use != p.test_drop) {
+          if constexpr (kPhase == 1 && !kPair) {  // 64 rows of each matrix
+            tma_load_3d(sb, &map_b0, bar, k * kElems, n0, t.e);
+            tma_load_3d(sb + 64 * kStageK, &map_b1, bar, k * kElems, n0, t.e);
+          } else if constexpr (kPhase == 1) {
+            tma_load_3d(sb, rank == 1 ? &map_b1 : &map_b0, bar, k * kElems, n0, t.e);
+          } else {
+            tma_load_3d(sb, &map_b0, bar, k * kElems, n0 + rank * kTileB, t.e);
+          }
+        }
+        if constexpr (kMx) {
+          bulk_load(ss + kMxTileBytes, sf_b0 + k * kMxTileBytes, kMxTileBytes, bar);
+          if (second) bulk_load(ss + 2 * kMxTileBytes, sf_b1 + k * kMxTileBytes, kMxTileBytes, bar);
+        }
+      };
+      const auto load_a = [&](int k, int b) {
+        uint64_t* bar = &ctl.full[b];
+        for (int i = 0; i < boxes_a; ++i)
+          tma_load_2d(base + b * kStageBytes + i * kBoxA * kStageK, &map_a, bar, k * kElems,
+                      t.row_tile * kTileM + i * kBoxA);
+        if (kMx && boxes_a > 0)
+          bulk_load(s_scale + b * kScaleBytes, sf_a + k * kMxTileBytes, kMxTileBytes, bar);
+      };
+      int k = k0;
+      if (!waited) {
+        // the first stages' weights are on their way while the launch before this one finishes
+        const int ahead = min(k1 - k0, kStages);
+        if (issue) {
+          for (int i = 0; i < ahead; ++i, ++use) load_b(k0 + i, i);
+          use -= ahead;
+        }
+        grid_dep_wait();
+        waited = true;
+        if (issue)
+          for (int i = 0; i < ahead; ++i) load_a(k0 + i, i);
+        __syncwarp();
+        use += ahead;
+        k += ahead;
+      }
+      for (; k < k1; ++k, ++use) {
         const int b = use % kStages;
         ok = __all_sync(0xffffffffu, stage_free(use, b));
         if (!ok) break;
         if (issue) {
-          uint8_t* sa = base + b * kStageBytes;
-          uint8_t* sb = sa + kBytesA;
-          uint8_t* ss = s_scale + b * kScaleBytes;
-          uint64_t* bar = &ctl.full[b];
-          mbar_arrive_expect_tx(bar, bytes);
-          if (use != p.test_drop) {
-            if constexpr (kPhase == 1 && !kPair) {  // 64 rows of each matrix
-              tma_load_3d(sb, &map_b0, bar, k * kElems, n0, t.e);
-              tma_load_3d(sb + 64 * kStageK, &map_b1, bar, k * kElems, n0, t.e);
-            } else if constexpr (kPhase == 1) {
-              tma_load_3d(sb, rank == 1 ? &map_b1 : &map_b0, bar, k * kElems, n0, t.e);
-            } else {
-              tma_load_3d(sb, &map_b0, bar, k * kElems, n0 + rank * kTileB, t.e);
-            }
-          }
-          for (int i = 0; i < boxes_a; ++i)
-            tma_load_2d(sa + i * kBoxA * kStageK, &map_a, bar, k * kElems,
-                        t.row_tile * kTileM + i * kBoxA);
-          if constexpr (kMx) {
-            const int at = k * kMxTileBytes;
-            if (boxes_a > 0) bulk_load(ss, sf_a + at, kMxTileBytes, bar);
-            bulk_load(ss + kMxTileBytes, sf_b0 + at, kMxTileBytes, bar);
-            if (second) bulk_load(ss + 2 * kMxTileBytes, sf_b1 + at, kMxTileBytes, bar);
-          }
+          load_b(k, b);
+          load_a(k, b);
         }
         __syncwarp();
       }
@@ -413,7 +461,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         mbar_wait(&ctl.full[u % kStages], (u / kStages) & 1, limit);
     }
     __syncwarp();
-  } else if (warp == kIssueWarp) {
+  } else if (warp == S::kIssueWarp) {
     if (rank == 0) {
       // ------------------------------------------------------------ MMA issuer
       // The whole warp walks the loop, so that what it computes is uniform over the warp; one
@@ -438,7 +486,7 @@ __global__ void __launch_bounds__(kThreads, 1)
           if (!ok) break;
           tc_fence_after();
           const uint32_t sa = s_stage + b * kStageBytes, sb = sa + kBytesA;
-          const uint32_t sfa = tmem + kScaleCol + (use & 1) * 16, sfb = sfa + 8;
+          const uint32_t sfa = tmem + S::kScaleCol + (use & 1) * 16, sfb = sfa + 8;
           const int steps = min(4, (p.k_elems - k * kElems + kStepElems - 1) / kStepElems);
           if (issue) {
             if (kMx) {
@@ -499,10 +547,10 @@ __global__ void __launch_bounds__(kThreads, 1)
       if (!ok) give_up();
     }
     __syncwarp();
-  } else if (warp >= kGatherWarp) {
+  } else if (warp >= S::kGatherWarp) {
     // -------------------------------------------------------------- rows of x, by token
     if (kGather) {
-      const int g = warp - kGatherWarp;
+      const int g = warp - S::kGatherWarp;
       constexpr int kRows = kTileM / kGatherWarps;  // of this warp: g * kRows ..
       constexpr int kCopies = kRows / 4;            // a warp copies four rows (8 lanes each) at once
       const int chunk = lane & 7, sub = lane >> 3;
@@ -561,6 +609,11 @@ __global__ void __launch_bounds__(kThreads, 1)
           for (int j = 0; j < 4; ++j) {
             if (k + j >= p.k_stages) break;
             const int b = use % kStages;
+            if (use >= kStages &&
+                !__all_sync(0xffffffffu, mbar_test(&ctl.empty[b], ((use / kStages) - 1) & 1))) {
+              cp_async_wait_all();  // nothing else to do: tell of every stage so far
+              announce(use);
+            }
             ok = __all_sync(0xffffffffu, stage_free(use, b));
             if (!ok) break;
             uint8_t* sa = base + b * kStageBytes;
@@ -593,10 +646,11 @@ __global__ void __launch_bounds__(kThreads, 1)
     }
   } else {
     // -------------------------------------------------------------- epilogue
-    const int quarter = warp & 3, half = warp >> 2;
+    const int quarter = warp & 3;
     const int r = quarter * 32 + lane;  // TMEM lane = row of the tile
     const uint32_t lanes = static_cast<uint32_t>(quarter * 32) << 16;
-    constexpr int kChunks = kN / 2 / 32;  // 32-column loads of a warp: half of the tile
+    // 32-column loads of half a tile: a pair's warp takes one half, a single CTA's both in turn
+    constexpr int kChunks = kN / 2 / 32;
     int e = 0, tiles = 0;
     bool ok = true;
     Tile t;
@@ -604,7 +658,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       grid_dep_wait();
       if (p.direct) {
         // tokens without an expert: no pair of theirs reaches any tile
-        constexpr int kRun = 32 * kEpilogueWarps;
+        constexpr int kRun = 32 * S::kEpilogueWarps;
         for (int64_t t0 = static_cast<int64_t>(blockIdx.x) * kRun + warp * 32; t0 < p.tokens;
              t0 += static_cast<int64_t>(gridDim.x) * kRun) {
           uint32_t missing = __ballot_sync(0xffffffffu, t0 + lane < p.tokens && p.ids[t0 + lane] < 0);
@@ -626,93 +680,99 @@ __global__ void __launch_bounds__(kThreads, 1)
       ok = __all_sync(0xffffffffu, ok);
       if (!ok) break;
       tc_fence_after();
-      uint32_t acc[kChunks][32];
-#pragma unroll
-      for (int c = 0; c < kChunks; ++c) {
-        // phase 1: chunk c < kChunks / 2 of the gate, then the same columns of the value
-        const int col = kPhase == 1 ? (c < kChunks / 2 ? 0 : kCols) + half * (kCols / 2) +
-                                          32 * (c % (kChunks / 2))
-                                    : half * (kN / 2) + 32 * c;
-        tmem_ld32(tmem + lanes + col, acc[c]);
-      }
-      tmem_wait_ld();
-      tc_fence_before();
-      __syncwarp();
-      if (lane == 0) {
-        if constexpr (kPair) mbar_arrive_remote(lead(&ctl.acc_free));
-        else mbar_arrive(&ctl.acc_free);
-      }
-      if constexpr (kPhase == 1) {
-#pragma unroll
-        for (int c = 0; c < kChunks / 2; ++c) {
-          const int col = t.n * kCols + half * (kCols / 2) + 32 * c;  // hidden element
-          float v[32];
-#pragma unroll
-          for (int i = 0; i < 32; ++i)
-            v[i] = silu(__uint_as_float(acc[c][i])) * __uint_as_float(acc[c + kChunks / 2][i]);
-          const int64_t row = static_cast<int64_t>(t.row_tile) * kTileM + r;
-          if constexpr (kMx) {
-            float m = 0.f;
-#pragma unroll
-            for (int i = 0; i < 32; ++i) m = max_nan(m, fabsf(v[i]));
-            const uint32_t b = mx_scale_byte(m);
-            const float s = mx_inverse(b);
-            if (in && col < p.hidden) {
-              uint32_t q[8];
-#pragma unroll
-              for (int i = 0; i < 8; ++i)
-                q[i] = e4m3x4(v[4 * i] * s, v[4 * i + 1] * s, v[4 * i + 2] * s, v[4 * i + 3] * s);
-              store32(p.h + row * p.hidden + col, q);
-              const int tiles_h = (p.hidden + 127) / 128;
-              p.h_scale[(static_cast<int64_t>(t.row_tile) * tiles_h + col / 128) * kMxTileBytes +
-                        mx_tile_byte(r, col / 32)] = static_cast<uint8_t>(b);
-            }
-          } else if (in && col < p.hidden) {
-#pragma unroll
-            for (int i = 0; i < 2; ++i) {
-              uint32_t q[8];
-#pragma unroll
-              for (int j = 0; j < 8; ++j) q[j] = pack2(v[16 * i + 2 * j], v[16 * i + 2 * j + 1]);
-              store32(p.h + (row * p.hidden + col) * 2 + 32 * i, q);
-            }
-          }
-        }
-      } else {
-        const bool store = pair >= 0 && pair < p.pairs;
-        const float weight = p.direct && store ? p.weights[pair] : 1.f;
+      const int half0 = kPair ? warp >> 2 : 0, half1 = kPair ? half0 + 1 : 2;
+#pragma unroll 1
+      for (int half = half0; half < half1; ++half) {
+        uint32_t acc[kChunks][32];
 #pragma unroll
         for (int c = 0; c < kChunks; ++c) {
-          const int col = t.n * kN + half * (kN / 2) + 32 * c;
-          if (!store || col >= p.dim) continue;
-          const uint32_t (&a)[32] = acc[c];
-          if (!p.direct) {
-            float* to = p.partial + (static_cast<int64_t>(t.split) * p.pairs + pair) * p.dim + col;
+          // phase 1: chunk c < kChunks / 2 of the gate, then the same columns of the value
+          const int col = kPhase == 1 ? (c < kChunks / 2 ? 0 : kCols) + half * (kCols / 2) +
+                                            32 * (c % (kChunks / 2))
+                                      : half * (kN / 2) + 32 * c;
+          tmem_ld32(tmem + lanes + col, acc[c]);
+        }
+        tmem_wait_ld();
+        if (half == half1 - 1) {  // the accumulator is in registers: the next tile's MMAs may start
+          tc_fence_before();
+          __syncwarp();
+          if (lane == 0) {
+            if constexpr (kPair) mbar_arrive_remote(lead(&ctl.acc_free));
+            else mbar_arrive(&ctl.acc_free);
+          }
+        }
+        if constexpr (kPhase == 1) {
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              uint32_t q[8];
+          for (int c = 0; c < kChunks / 2; ++c) {
+            const int col = t.n * kCols + half * (kCols / 2) + 32 * c;  // hidden element
+            float v[32];
 #pragma unroll
-              for (int j = 0; j < 8; ++j) q[j] = a[8 * i + j];
-              store32(to + 8 * i, q);
+            for (int i = 0; i < 32; ++i)
+              v[i] = silu(__uint_as_float(acc[c][i])) * __uint_as_float(acc[c + kChunks / 2][i]);
+            const int64_t row = static_cast<int64_t>(t.row_tile) * kTileM + r;
+            if constexpr (kMx) {
+              float m = 0.f;
+#pragma unroll
+              for (int i = 0; i < 32; ++i) m = max_nan(m, fabsf(v[i]));
+              const uint32_t b = mx_scale_byte(m);
+              const float s = mx_inverse(b);
+              if (in && col < p.hidden) {
+                uint32_t q[8];
+#pragma unroll
+                for (int i = 0; i < 8; ++i)
+                  q[i] = e4m3x4(v[4 * i] * s, v[4 * i + 1] * s, v[4 * i + 2] * s, v[4 * i + 3] * s);
+                store32(p.h + row * p.hidden + col, q);
+                const int tiles_h = (p.hidden + 127) / 128;
+                p.h_scale[(static_cast<int64_t>(t.row_tile) * tiles_h + col / 128) * kMxTileBytes +
+                          mx_tile_byte(r, col / 32)] = static_cast<uint8_t>(b);
+              }
+            } else if (in && col < p.hidden) {
+#pragma unroll
+              for (int i = 0; i < 2; ++i) {
+                uint32_t q[8];
+#pragma unroll
+                for (int j = 0; j < 8; ++j) q[j] = pack2(v[16 * i + 2 * j], v[16 * i + 2 * j + 1]);
+                store32(p.h + (row * p.hidden + col) * 2 + 32 * i, q);
+              }
             }
-          } else if (!p.y_f32) {
-            uint4* dst = reinterpret_cast<uint4*>(static_cast<__nv_bfloat16*>(p.y) +
-                                                  pair * p.y_stride + col);
+          }
+        } else {
+          const bool store = pair >= 0 && pair < p.pairs;
+          const float weight = p.direct && store ? p.weights[pair] : 1.f;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              uint32_t q[4];
+          for (int c = 0; c < kChunks; ++c) {
+            const int col = t.n * kN + half * (kN / 2) + 32 * c;
+            if (!store || col >= p.dim) continue;
+            const uint32_t (&a)[32] = acc[c];
+            if (!p.direct) {
+              float* to = p.partial + (static_cast<int64_t>(t.split) * p.pairs + pair) * p.dim + col;
 #pragma unroll
-              for (int j = 0; j < 4; ++j)
-                q[j] = pack2(__uint_as_float(a[8 * i + 2 * j]) * weight,
-                             __uint_as_float(a[8 * i + 2 * j + 1]) * weight);
-              dst[i] = make_uint4(q[0], q[1], q[2], q[3]);
+              for (int i = 0; i < 4; ++i) {
+                uint32_t q[8];
+#pragma unroll
+                for (int j = 0; j < 8; ++j) q[j] = a[8 * i + j];
+                store32(to + 8 * i, q);
+              }
+            } else if (!p.y_f32) {
+              uint4* dst = reinterpret_cast<uint4*>(static_cast<__nv_bfloat16*>(p.y) +
+                                                    pair * p.y_stride + col);
+#pragma unroll
+              for (int i = 0; i < 4; ++i) {
+                uint32_t q[4];
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                  q[j] = pack2(__uint_as_float(a[8 * i + 2 * j]) * weight,
+                               __uint_as_float(a[8 * i + 2 * j + 1]) * weight);
+                dst[i] = make_uint4(q[0], q[1], q[2], q[3]);
+              }
+            } else {
+              float4* dst = reinterpret_cast<float4*>(static_cast<float*>(p.y) + pair * p.y_stride + col);
+#pragma unroll
+              for (int i = 0; i < 8; ++i)
+                dst[i] = make_float4(__uint_as_float(a[4 * i]) * weight, __uint_as_float(a[4 * i + 1]) * weight,
+                                     __uint_as_float(a[4 * i + 2]) * weight,
+                                     __uint_as_float(a[4 * i + 3]) * weight);
             }
-          } else {
-            float4* dst = reinterpret_cast<float4*>(static_cast<float*>(p.y) + pair * p.y_stride + col);
-#pragma unroll
-            for (int i = 0; i < 8; ++i)
-              dst[i] = make_float4(__uint_as_float(a[4 * i]) * weight, __uint_as_float(a[4 * i + 1]) * weight,
-                                   __uint_as_float(a[4 * i + 2]) * weight,
-                                   __uint_as_float(a[4 * i + 3]) * weight);
           }
         }
       }
@@ -724,12 +784,12 @@ __global__ void __launch_bounds__(kThreads, 1)
   tc_fence_before();
   if constexpr (kPair) cluster_sync();  // no CTA leaves while the other may signal its barriers
   else __syncthreads();
-  if (warp == kIssueWarp) {
+  if (warp == S::kIssueWarp) {
     if (!mbar_wait(&ctl.drained, 0, limit) && lane == 0) give_up();
     __syncwarp();
     tc_fence_after();
-    if constexpr (kPair) tmem_dealloc_pair<kTmemAll>(tmem);
-    else tmem_dealloc<kTmemAll>(tmem);
+    if constexpr (kPair) tmem_dealloc_pair<S::kTmem>(tmem);
+    else tmem_dealloc<S::kTmem>(tmem);
   }
 }
 
@@ -737,6 +797,7 @@ __global__ void __launch_bounds__(kThreads, 1)
 // pair of the plan.
 template <bool kMx>
 __global__ void __launch_bounds__(256) gather_rows(const __grid_constant__ ExpertsParams p) {
+  grid_dep_wait();  // the call's first launch (see product)
   grid_dep_launch();
   __shared__ int32_t first_row[DARD_MAX_EXPERTS + 1], first_tile[DARD_MAX_EXPERTS + 1],
       first_unit[DARD_MAX_EXPERTS + 1];
@@ -782,6 +843,7 @@ __global__ void __launch_bounds__(256) gather_rows(const __grid_constant__ Exper
 // per thread; the products of up to eight slots are in flight at once.
 template <typename Y>
 __global__ void __launch_bounds__(128) combine(const __grid_constant__ ExpertsParams p) {
+  grid_dep_launch();
   grid_dep_wait();
   const int64_t t = blockIdx.x;
   const int col = 4 * (blockIdx.y * 128 + threadIdx.x);
@@ -836,21 +898,28 @@ bool encode(CUtensorMap* m, const void* ptr, bool mx, uint64_t cols, uint64_t ro
             CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-template <class F>
-cudaLaunchConfig_t pair_config(F*, unsigned ctas, cudaStream_t stream, cudaLaunchAttribute* attr) {
+// A launch that may begin (up to its griddepcontrol.wait) while the one before it on the stream
+// still runs, with clusters of `cluster` CTAs. Not copyable: cfg points at attr.
+struct Launch {
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(ctas);
-  cfg.blockDim = dim3(kThreads);
-  cfg.dynamicSmemBytes = smem_bytes();
-  cfg.stream = stream;
-  attr[0].id = cudaLaunchAttributeClusterDimension;
-  attr[0].val.clusterDim.x = 2;
-  attr[0].val.clusterDim.y = 1;
-  attr[0].val.clusterDim.z = 1;
-  cfg.attrs = attr;
-  cfg.numAttrs = 1;
-  return cfg;
-}
+  cudaLaunchAttribute attr[2];
+  Launch(dim3 grid, unsigned block, size_t smem, cudaStream_t stream, unsigned cluster = 1) {
+    cfg.gridDim = grid;
+    cfg.blockDim = dim3(block);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = stream;
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = cluster;
+    attr[1].val.clusterDim.y = 1;
+    attr[1].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = cluster > 1 ? 2 : 1;
+  }
+  Launch(const Launch&) = delete;
+  Launch& operator=(const Launch&) = delete;
+};
 
 // Clusters of two CTAs of this kernel that fit on the device at once, looked up once per device.
 template <class F>
@@ -859,9 +928,8 @@ int max_pairs(F* kernel, std::atomic<int>* cache) {
   if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return sm_count() / 2;
   int n = cache[dev].load(std::memory_order_relaxed);
   if (n > 0) return n;
-  cudaLaunchAttribute attr[1];
-  const cudaLaunchConfig_t cfg = pair_config(kernel, 2 * 64, nullptr, attr);
-  if (cudaOccupancyMaxActiveClusters(&n, kernel, &cfg) != cudaSuccess || n <= 0) {
+  const Launch l(dim3(2 * 64), Shape<true>::kThreads, smem_bytes<true>(), nullptr, 2);
+  if (cudaOccupancyMaxActiveClusters(&n, kernel, &l.cfg) != cudaSuccess || n <= 0) {
     cudaGetLastError();
     return sm_count() / 2;
   }
@@ -875,19 +943,13 @@ cudaError_t launch_product(const ExpertsParams& p, int64_t tiles, const CUtensor
   static std::atomic<uint64_t> done{0};
   static std::atomic<int> pairs[64];
   const auto kernel = product<kMx, kPair, kPhase>;
-  const cudaError_t e = ensure_smem_attr(kernel, smem_bytes(), done);
+  const size_t smem = smem_bytes<kPair>();
+  const cudaError_t e = ensure_smem_attr(kernel, smem, done);
   if (e != cudaSuccess) return e;
-  cudaLaunchAttribute attr[2];
-  const int64_t most = kPair ? max_pairs(kernel, pairs) : sm_count();
+  const int64_t most = kPair ? max_pairs(kernel, pairs) : sm_count() * Shape<false>::kCtasPerSm;
   const unsigned ctas = static_cast<unsigned>(std::min<int64_t>(tiles, most)) * (kPair ? 2 : 1);
-  cudaLaunchConfig_t cfg = pair_config(kernel, ctas, stream, attr);
-  if (!kPair) cfg.numAttrs = 0;
-  if (kPhase == 2 || kPair) {  // after gather_rows or phase 1
-    attr[cfg.numAttrs].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr[cfg.numAttrs].val.programmaticStreamSerializationAllowed = 1;
-    ++cfg.numAttrs;
-  }
-  return cudaLaunchKernelEx(&cfg, kernel, p, a, b0, b1);
+  const Launch l(dim3(ctas), Shape<kPair>::kThreads, smem, stream, kPair ? 2 : 1);
+  return cudaLaunchKernelEx(&l.cfg, kernel, p, a, b0, b1);
 }
 
 template <bool kMx, int kPhase>
@@ -899,16 +961,8 @@ cudaError_t launch_phase(const ExpertsParams& p, bool pair, int64_t tiles, const
 
 template <typename Y>
 cudaError_t launch_combine(const ExpertsParams& p, cudaStream_t stream) {
-  cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(p.tokens, (p.dim / 4 + 127) / 128);
-  cfg.blockDim = dim3(128);
-  cfg.stream = stream;
-  cudaLaunchAttribute attr[1];
-  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  attr[0].val.programmaticStreamSerializationAllowed = 1;
-  cfg.attrs = attr;
-  cfg.numAttrs = 1;
-  return cudaLaunchKernelEx(&cfg, combine<Y>, p);
+  const Launch l(dim3(p.tokens, (p.dim / 4 + 127) / 128), 128, 0, stream);
+  return cudaLaunchKernelEx(&l.cfg, combine<Y>, p);
 }
 
 constexpr size_t up256(size_t n) { return (n + 255) / 256 * 256; }
@@ -1079,10 +1133,10 @@ dard_status dard_experts(const dard_experts_args* a, void* stream) {
     e = cudaErrorInvalidValue;
   if (!q.pair1) ma = mb0;  // not used
   if (e == cudaSuccess && q.pair1) {
-    const int64_t ctas = std::min<int64_t>((q.pairs + 7) / 8, 8ll * sm_count());
-    if (mx) gather_rows<true><<<static_cast<unsigned>(ctas), 256, 0, s>>>(p);
-    else gather_rows<false><<<static_cast<unsigned>(ctas), 256, 0, s>>>(p);
-    e = cudaGetLastError();
+    const Launch l(dim3(static_cast<unsigned>(std::min<int64_t>((q.pairs + 7) / 8, 8ll * sm_count()))),
+                   256, 0, s);
+    e = mx ? cudaLaunchKernelEx(&l.cfg, gather_rows<true>, p)
+           : cudaLaunchKernelEx(&l.cfg, gather_rows<false>, p);
   }
   if (e == cudaSuccess) {
     p.a_scale = p.xg_scale;

@@ -361,7 +361,7 @@ __device__ __forceinline__ void place_pairs(const RouteParams& p, int t0, int t1
 template <typename T, int kPer>
 __global__ void __launch_bounds__(32 * route_warps(kPer), 1)
     route_topk(const __grid_constant__ RouteParams p) {
-  grid_dep_launch();  // plan_scatter may be scheduled; it waits for this grid's end
+  grid_dep_launch();  // what follows may be scheduled; it waits for this grid's end
   constexpr int kWarps = route_warps(kPer);
   extern __shared__ int32_t smem[];
   // choices of each warp's token (groups only), then the counts, then one CTA's buckets
@@ -406,6 +406,7 @@ __global__ void __launch_bounds__(32 * kPlanWarps)
   int32_t* hist = before + row;  // [kPlanWarps][buckets]
   for (int i = threadIdx.x; i < 2 * row; i += blockDim.x) next[i] = 0;
   __syncthreads();
+  grid_dep_launch();  // (what follows waits for this grid's end before it reads the plan)
   const int runs = blockDim.x / quads, run = threadIdx.x / quads, quad = threadIdx.x % quads;
   grid_dep_wait();
   if (run < runs) {
