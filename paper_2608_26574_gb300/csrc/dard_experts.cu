@@ -63,21 +63,29 @@ constexpr int kTileM = 128;            // rows of A per CTA
 constexpr int kTileB = 128;            // weight rows per CTA
 constexpr int kStageK = 128;           // bytes of K per stage
 constexpr int kMaxStages = 6;
-constexpr int kGatherWarps = 2;
 constexpr int kGatherLag = 2;          // stages a gather warp has in flight
-constexpr uint32_t kBytesA = kTileM * kStageK, kBytesB = kTileB * kStageK;
-constexpr uint32_t kStageBytes = kBytesA + kBytesB;
+constexpr uint32_t kBytesB = kTileB * kStageK;
 constexpr uint32_t kScaleBytes = 3 * kMxTileBytes;  // of a stage: A's, then two tiles of B's
 constexpr int kGroupM = 16;            // row tiles that share a pass over an expert's columns
-constexpr int kBoxRowsSingle = 32;     // rows of h per copy (single: its tiles hold few rows)
 constexpr uint16_t kBothCtas = 0x3;
 
-// The two variants. A single CTA takes half of an SM's registers, shared memory and TMEM, so that
-// the next launch's CTAs, which do not depend on this one for their weights, can sit next to it.
-template <bool kPair>
+// The variants (see the top of the file). A CTA of the last two takes half of an SM's registers,
+// shared memory and TMEM, so that the next launch's CTAs, which do not depend on this one for
+// their weights, can sit next to it.
+constexpr int kPairs = 0, kSingle = 1, kFew = 2;
+constexpr int kFewTokens = 32;
+template <int kVariant>
 struct Shape {
-  static constexpr int kStages = kPair ? 6 : 3;
+  static constexpr bool kPair = kVariant == kPairs;
+  static constexpr int kCtas = kPair ? 2 : 1;  // that share an MMA
+  static constexpr int kStages = kPair ? 6 : kVariant == kSingle ? 3 : 5;
+  // Rows of A that a stage holds. The MMA reads 128: what lies behind (this stage's B) gives rows
+  // of the accumulator that nobody reads.
+  static constexpr int kRowsA = kVariant == kFew ? kFewTokens : kTileM;
+  static constexpr int kBoxA = kPair ? kTileM : 32;  // rows per copy
+  static constexpr uint32_t kBytesA = kRowsA * kStageK, kStageBytes = kBytesA + kBytesB;
   static constexpr int kEpilogueWarps = kPair ? 8 : 4;
+  static constexpr int kGatherWarps = kVariant == kFew ? 1 : 2;
   static constexpr int kProducerWarp = kEpilogueWarps, kIssueWarp = kProducerWarp + 1,
                        kGatherWarp = kIssueWarp + 1;
   static constexpr int kThreads = 32 * (kGatherWarp + kGatherWarps);
@@ -99,6 +107,7 @@ struct ExpertsParams {
   uint8_t* xg_scale;          // [row tiles][ceil(dim / 128)][512]
   uint8_t* h;                 // [row tiles * 128][hidden]
   uint8_t* h_scale;           // [row tiles][ceil(hidden / 128)][512]
+  int32_t* arrived;           // few: per column tile of phase 2, the tiles done
   float* partial;             // [splits][pairs][dim]
   void* y;
   uint32_t* status;
@@ -180,6 +189,29 @@ __device__ __forceinline__ bool mbar_test(uint64_t* bar, uint32_t parity) {
       : "memory");
   return ok != 0;
 }
+// mbar_wait that also gives up, once it has to wait, when the CTA's abort flag is set.
+__device__ __noinline__ bool wait_slow(uint64_t* bar, uint32_t parity, long long limit,
+                                       const volatile int32_t* abort_flag) {
+  const long long t0 = clock64();
+  while (!mbar_try_wait(bar, parity)) {
+    if (*abort_flag != 0 || clock64() - t0 > limit) return false;
+  }
+  return true;
+}
+// A place in the ring of stages, and the parity of its barriers' phase there: full[b] completes
+// phase `phase` when stage b's copies have landed, empty[b] when they have been read. (On a new
+// barrier the phase before the first counts as complete.)
+struct Ring {
+  int b = 0;
+  uint32_t phase = 0;
+  template <int kStages>
+  __device__ __forceinline__ void next() {
+    if (++b == kStages) {
+      b = 0;
+      phase ^= 1;
+    }
+  }
+};
 // One lane of a converged warp.
 __device__ __forceinline__ bool elect_one() {
   uint32_t r;
@@ -216,14 +248,17 @@ struct __align__(16) Ctl {
   uint64_t drained;  // every MMA the issuer launched has completed
   uint32_t tmem_base;
   int32_t abort;
+  int32_t last;      // few: this CTA's tile was its columns' last
   int32_t first_row[DARD_MAX_EXPERTS + 1];   // offsets, clamped to [0, pairs]
   int32_t first_tile[DARD_MAX_EXPERTS + 1];  // row tiles (128 rows) of the experts before
-  int32_t first_unit[DARD_MAX_EXPERTS + 1];  // the same in units of a tile: 1 or 2 row tiles
+  // (pairs: after this, the same in units of two row tiles)
 };
 
-template <bool kPair>
+template <int kVariant>
 constexpr size_t smem_bytes() {
-  return 1024 + static_cast<size_t>(Shape<kPair>::kStages) * (kStageBytes + kScaleBytes) + sizeof(Ctl);
+  using S = Shape<kVariant>;
+  return 1024 + static_cast<size_t>(S::kStages) * (S::kStageBytes + kScaleBytes) + sizeof(Ctl) +
+         (S::kPair ? sizeof(int32_t) * (DARD_MAX_EXPERTS + 1) : 0);
 }
 
 // A CTA's part of one tile: rows [row, row + count) (count <= 0: none) of expert e, in row tile
@@ -235,14 +270,15 @@ struct Tile {
 // Tile `w` of the call. Within an expert, a group of row units takes each column tile in turn,
 // so that CTAs that run together share weights and rows in L2. `e` walks forward.
 template <bool kPair>
-__device__ __forceinline__ bool get_tile(const ExpertsParams& p, const Ctl& c, int rank, int64_t w,
-                                         int& e, Tile& t) {
+__device__ __forceinline__ bool get_tile(const ExpertsParams& p, const Ctl& c,
+                                         const int32_t* first_unit, int rank, int64_t w, int& e,
+                                         Tile& t) {
   constexpr int kUnitTiles = kPair ? 2 : 1, kGroup = kGroupM / kUnitTiles;
   const int per_unit = p.n_tiles * p.splits;
-  if (w >= static_cast<int64_t>(c.first_unit[p.experts]) * per_unit) return false;
-  while (w >= static_cast<int64_t>(c.first_unit[e + 1]) * per_unit) ++e;
-  const int units = c.first_unit[e + 1] - c.first_unit[e];
-  const int local = static_cast<int>(w - static_cast<int64_t>(c.first_unit[e]) * per_unit);
+  if (w >= static_cast<int64_t>(first_unit[p.experts]) * per_unit) return false;
+  while (w >= static_cast<int64_t>(first_unit[e + 1]) * per_unit) ++e;
+  const int units = first_unit[e + 1] - first_unit[e];
+  const int local = static_cast<int>(w - static_cast<int64_t>(first_unit[e]) * per_unit);
   const int group = local / (kGroup * per_unit);
   const int in_group = min(kGroup, units - group * kGroup);
   const int rest = local - group * kGroup * per_unit;
@@ -306,25 +342,77 @@ __device__ __forceinline__ uint32_t pack2(float lo, float hi) {
   return r;
 }
 
-template <bool kMx, bool kPair, int kPhase>
-__global__ void __launch_bounds__(Shape<kPair>::kThreads, Shape<kPair>::kCtasPerSm)
+// AND of `ok` over the epilogue's warps, which it also syncs (so that they leave a loop together).
+template <int kWarps>
+__device__ __forceinline__ bool epilogue_and(bool ok) {
+  uint32_t r;
+  asm volatile(
+      "{\n\t.reg .pred p, q;\n\tsetp.ne.u32 p, %1, 0;\n\t"
+      "barrier.red.and.pred q, 1, %2, p;\n\tselp.u32 %0, 1, 0, q;\n\t}"
+      : "=r"(r)
+      : "r"(static_cast<uint32_t>(ok)), "n"(32 * kWarps)
+      : "memory");
+  return r != 0;
+}
+
+// Columns col .. col + 3 of y_t = sum over slots (in order) of weight * (sum over splits of the
+// pair's product). The products of up to eight slots are in flight at once.
+__device__ __forceinline__ void combine_columns(const ExpertsParams& p, int64_t t, int col) {
+  constexpr int kAhead = 8;
+  float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
+  const int parts = p.top_k * p.splits;  // slot by slot, its splits in order
+  for (int first = 0; first < parts; first += kAhead) {
+    float4 v[kAhead];
+    float w[kAhead];
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) {
+      v[i] = make_float4(0.f, 0.f, 0.f, 0.f);
+      w[i] = 0.f;
+      const int s = p.splits == 1 ? first + i : (first + i) / p.splits;
+      const int split = p.splits == 1 ? 0 : (first + i) % p.splits;
+      const int64_t pair = t * p.top_k + s;
+      if (first + i < parts && p.ids[pair] >= 0) {
+        v[i] = __ldcg(reinterpret_cast<const float4*>(
+            p.partial + (static_cast<int64_t>(split) * p.pairs + pair) * p.dim + col));
+        w[i] = p.weights[pair];
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) {
+      sum.x = fmaf(w[i], v[i].x, sum.x);
+      sum.y = fmaf(w[i], v[i].y, sum.y);
+      sum.z = fmaf(w[i], v[i].z, sum.z);
+      sum.w = fmaf(w[i], v[i].w, sum.w);
+    }
+  }
+  if (p.y_f32)
+    *reinterpret_cast<float4*>(static_cast<float*>(p.y) + t * p.y_stride + col) = sum;
+  else
+    *reinterpret_cast<uint2*>(static_cast<__nv_bfloat16*>(p.y) + t * p.y_stride + col) =
+        make_uint2(pack2(sum.x, sum.y), pack2(sum.z, sum.w));
+}
+
+template <bool kMx, int kVariant, int kPhase>
+__global__ void __launch_bounds__(Shape<kVariant>::kThreads, Shape<kVariant>::kCtasPerSm)
     product(const __grid_constant__ ExpertsParams p, const __grid_constant__ CUtensorMap map_a,
             const __grid_constant__ CUtensorMap map_b0, const __grid_constant__ CUtensorMap map_b1) {
-  constexpr int kCtas = kPair ? 2 : 1;
+  using S = Shape<kVariant>;
+  constexpr bool kPair = S::kPair;
+  constexpr int kCtas = S::kCtas, kStages = S::kStages;
+  constexpr uint32_t kStageBytes = S::kStageBytes;
   constexpr int kM = kTileM * kCtas, kN = kTileB * kCtas;  // of one MMA
   constexpr int kElems = kMx ? 128 : 64;    // elements of K per stage
   constexpr int kStepElems = kMx ? 32 : 16; // per MMA (32 bytes)
   // weight rows of a tile from one matrix: phase 1 takes half of them from w1, half from w3
   constexpr int kCols = kPhase == 1 ? kN / 2 : kN;
-  constexpr bool kGather = kPhase == 1 && !kPair;  // the A rows come from warps 10-11
-  constexpr int kBoxA = kPair ? kTileM : kBoxRowsSingle;
-  using S = Shape<kPair>;
-  constexpr int kStages = S::kStages;
+  constexpr bool kGather = kPhase == 1 && !kPair;  // the A rows come from the gather warps
+  constexpr int kBoxA = S::kBoxA;
   extern __shared__ uint8_t smem_raw[];
   uint8_t* base = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) &
                                              ~static_cast<uintptr_t>(1023));
   uint8_t* s_scale = base + kStages * kStageBytes;  // per stage: A scales, then B scales
   Ctl& ctl = *reinterpret_cast<Ctl*>(s_scale + kStages * kScaleBytes);
+  int32_t* first_unit = kPair ? reinterpret_cast<int32_t*>(&ctl + 1) : ctl.first_tile;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int rank = kPair ? static_cast<int>(cluster_ctarank()) : 0;
   const int64_t first = blockIdx.x / kCtas, step = gridDim.x / kCtas;
@@ -343,7 +431,7 @@ __global__ void __launch_bounds__(Shape<kPair>::kThreads, Shape<kPair>::kCtasPer
   }
   if (warp == S::kProducerWarp && lane == 0) {
     for (int b = 0; b < kStages; ++b) {
-      mbar_init(&ctl.full[b], kGather ? 1 + kGatherWarps : 1);
+      mbar_init(&ctl.full[b], kGather ? 1 + S::kGatherWarps : 1);
       mbar_init(&ctl.empty[b], 1);
       mbar_init(&ctl.peer_full[b], 1);
     }
@@ -360,7 +448,9 @@ __global__ void __launch_bounds__(Shape<kPair>::kThreads, Shape<kPair>::kCtasPer
   // next one start: that one may read the plan and the weights at once.
   if (kGather) grid_dep_wait();
   grid_dep_launch();
-  read_plan<kCtas>(p, ctl.first_row, ctl.first_tile, ctl.first_unit);
+  if (kVariant == kFew && kPhase == 1 && blockIdx.x == 0)
+    for (int i = threadIdx.x; i < (p.dim + kTileB - 1) / kTileB; i += S::kThreads) p.arrived[i] = 0;
+  read_plan<kCtas>(p, ctl.first_row, ctl.first_tile, first_unit);
   tc_fence_before();
   if constexpr (kPair) cluster_sync();  // both CTAs' barriers exist, TMEM is allocated
   else __syncthreads();
@@ -372,9 +462,12 @@ __global__ void __launch_bounds__(Shape<kPair>::kThreads, Shape<kPair>::kCtasPer
     if (p.status) atomicOr(p.status, DARD_STATUS_TIMEOUT);
   };
   const int split_stages = kPhase == 2 ? p.split_stages : p.k_stages;
-  // waits until the MMAs that read stage `b` before its use `use` have completed
-  const auto stage_free = [&](int use, int b) {
-    return !*abort_flag && (use < kStages || mbar_wait(&ctl.empty[b], ((use / kStages) - 1) & 1, limit));
+  const auto wait = [&](uint64_t* bar, uint32_t parity) {
+    return mbar_try_wait(bar, parity) || wait_slow(bar, parity, limit, abort_flag);
+  };
+  // the same by every lane of a warp, with one verdict
+  const auto warp_wait = [&](uint64_t* bar, uint32_t parity) {
+    return __all_sync(0xffffffffu, wait(bar, parity)) != 0;
   };
 
   if (warp == S::kProducerWarp) {
@@ -386,7 +479,8 @@ __global__ void __launch_bounds__(Shape<kPair>::kThreads, Shape<kPair>::kCtasPer
     Tile t;
     const bool issue = elect_one();
     bool waited = kGather;  // for the launch before this one, which writes the rows of A
-    for (int64_t w = first; ok && get_tile<kPair>(p, ctl, rank, w, e, t); w += step) {
+    Ring ring;
+    for (int64_t w = first; ok && get_tile<kPair>(p, ctl, first_unit, rank, w, e, t); w += step) {
       const int boxes_a = kGather ? 0 : (max(t.count, 0) + kBoxA - 1) / kBoxA;
       const int k0 = t.split * split_stages, k1 = min(p.k_stages, k0 + split_stages);
       const int n0 = t.n * kCols;
@@ -400,7 +494,7 @@ __global__ void __launch_bounds__(Shape<kPair>::kThreads, Shape<kPair>::kCtasPer
       const uint8_t* sf_b1 = kPhase == 1 ? p.scale_b[1] + at_b : sf_b0 + step_b;
       const uint8_t* sf_a = p.a_scale + t.row_tile * step_b;
       const auto load_b = [&](int k, int b) {
-        uint8_t* sb = base + b * kStageBytes + kBytesA;
+        uint8_t* sb = base + b * kStageBytes + S::kBytesA;
         uint8_t* ss = s_scale + b * kScaleBytes;
         uint64_t* bar = &ctl.full[b];
         mbar_arrive_expect_tx(bar, bytes);
@@ -433,25 +527,26 @@ __global__ void __launch_bounds__(Shape<kPair>::kThreads, Shape<kPair>::kCtasPer
         const int ahead = min(k1 - k0, kStages);
         if (issue) {
           for (int i = 0; i < ahead; ++i, ++use) load_b(k0 + i, i);
-          use -= ahead;
+          use = 0;
         }
         grid_dep_wait();
         waited = true;
         if (issue)
           for (int i = 0; i < ahead; ++i) load_a(k0 + i, i);
         __syncwarp();
-        use += ahead;
+        use = ahead;
         k += ahead;
+        for (int i = 0; i < ahead; ++i) ring.next<kStages>();
       }
       for (; k < k1; ++k, ++use) {
-        const int b = use % kStages;
-        ok = __all_sync(0xffffffffu, stage_free(use, b));
+        ok = warp_wait(&ctl.empty[ring.b], ring.phase ^ 1);
         if (!ok) break;
         if (issue) {
-          load_b(k, b);
-          load_a(k, b);
+          load_b(k, ring.b);
+          load_a(k, ring.b);
         }
         __syncwarp();
+        ring.next<kStages>();
       }
     }
     if (!ok) {
@@ -466,42 +561,42 @@ __global__ void __launch_bounds__(Shape<kPair>::kThreads, Shape<kPair>::kCtasPer
       // ------------------------------------------------------------ MMA issuer
       // The whole warp walks the loop, so that what it computes is uniform over the warp; one
       // elected lane issues.
-      int e = 0, use = 0, tiles = 0;
+      int e = 0, tiles = 0;
       bool ok = true;
       Tile t;
+      Ring ring;
       const bool issue = elect_one();
-      const uint32_t s_stage = smem_u32(base), s_sf = smem_u32(s_scale);
-      for (int64_t w = first; ok && get_tile<kPair>(p, ctl, rank, w, e, t); w += step, ++tiles) {
-        ok = __all_sync(0xffffffffu, tiles == 0 || mbar_wait(&ctl.acc_free, (tiles - 1) & 1, limit));
+      const uint64_t desc_a = smem_desc_sw128(smem_u32(base), 16, 1024);
+      const uint64_t desc_s = scale_desc(smem_u32(s_scale));
+      uint32_t sfa = tmem + S::kScaleCol;  // scales of two stages, 16 columns apart
+      for (int64_t w = first; ok && get_tile<kPair>(p, ctl, first_unit, rank, w, e, t); w += step, ++tiles) {
+        ok = tiles == 0 || warp_wait(&ctl.acc_free, (tiles - 1) & 1);
         if (!ok) break;
         tc_fence_after();
         const int k0 = t.split * split_stages, k1 = min(p.k_stages, k0 + split_stages);
-        // single, phase 1: a tile's 64 weight rows are half of a tile of 128 scales
+        // 64 weight rows of a matrix are half of a tile of 128 scales
         const uint32_t half = kPhase == 1 && kCols == 64 ? (t.n & 1) * 2 : 0;
-        for (int k = k0; k < k1; ++k, ++use) {
-          const int b = use % kStages;
-          ok = !*abort_flag && mbar_wait(&ctl.full[b], (use / kStages) & 1, limit) &&
-               (!kPair || mbar_wait(&ctl.peer_full[b], (use / kStages) & 1, limit));
-          ok = __all_sync(0xffffffffu, ok);
+        for (int k = k0; k < k1; ++k) {
+          ok = warp_wait(&ctl.full[ring.b], ring.phase) &&
+               (!kPair || warp_wait(&ctl.peer_full[ring.b], ring.phase));
           if (!ok) break;
           tc_fence_after();
-          const uint32_t sa = s_stage + b * kStageBytes, sb = sa + kBytesA;
-          const uint32_t sfa = tmem + S::kScaleCol + (use & 1) * 16, sfb = sfa + 8;
-          const int steps = min(4, (p.k_elems - k * kElems + kStepElems - 1) / kStepElems);
           if (issue) {
-            if (kMx) {
-              const uint32_t ss = s_sf + b * kScaleBytes;
-              copy_scales<kPair>(sfa, scale_desc(ss));
-              copy_scales<kPair>(sfb, scale_desc(ss + kMxTileBytes));
-              if (kPhase == 1 || kN > 128)
-                copy_scales<kPair>(sfb + 4, scale_desc(ss + 2 * kMxTileBytes));
+            // descriptors count 16-byte units
+            const uint64_t da = desc_a + ring.b * (kStageBytes / 16), db = da + S::kBytesA / 16;
+            const uint32_t sfb = sfa + 8;
+            if constexpr (kMx) {
+              const uint64_t ds = desc_s + ring.b * (kScaleBytes / 16);
+              copy_scales<kPair>(sfa, ds);
+              copy_scales<kPair>(sfb, ds + kMxTileBytes / 16);
+              if (kPhase == 1 || kN > 128) copy_scales<kPair>(sfb + 4, ds + 2 * kMxTileBytes / 16);
             }
-            const uint64_t da = smem_desc_sw128(sa, 16, 1024), db = smem_desc_sw128(sb, 16, 1024);
+            const int left = p.k_elems - k * kElems;  // the last stage may hold fewer steps
 #pragma unroll
             for (int ks = 0; ks < 4; ++ks) {
-              if (ks >= steps) break;
+              if (ks * kStepElems >= left) break;
               const uint32_t acc = (k > k0 || ks > 0) ? 1u : 0u;
-              const uint64_t off = ks * 32 / 16;  // descriptors count 16-byte units
+              const uint64_t off = ks * 32 / 16;
               if constexpr (!kMx && kPair) {
                 mma_ss_pair(tmem, da + off, db + off, idesc_bf16_f32(kM, kN, 0, 0), acc);
               } else if constexpr (!kMx) {
@@ -515,14 +610,16 @@ __global__ void __launch_bounds__(Shape<kPair>::kThreads, Shape<kPair>::kCtasPer
                 mma_mx<kPair>(tmem, da + off, db + off, idesc_mx(kM, kN, ks), sfa, sfb, acc);
               }
             }
-            if constexpr (kPair) mma_commit_pair(&ctl.empty[b], kBothCtas);
-            else mma_commit(&ctl.empty[b]);
+            if constexpr (kPair) mma_commit_pair(&ctl.empty[ring.b], kBothCtas);
+            else mma_commit(&ctl.empty[ring.b]);
             if (k == k1 - 1) {
               if constexpr (kPair) mma_commit_pair(&ctl.acc_full, kBothCtas);
               else mma_commit(&ctl.acc_full);
             }
           }
           __syncwarp();
+          ring.next<kStages>();
+          sfa ^= 16;
         }
       }
       if (!ok && lane == 0) give_up();
@@ -532,16 +629,17 @@ __global__ void __launch_bounds__(Shape<kPair>::kThreads, Shape<kPair>::kCtasPer
       }
     } else if (lane == 0) {
       // ------------------------------------------------------------ rank 1: landings to rank 0
-      int e = 0, use = 0;
+      int e = 0;
       bool ok = true;
       Tile t;
-      for (int64_t w = first; ok && get_tile<kPair>(p, ctl, rank, w, e, t); w += step) {
+      Ring ring;
+      for (int64_t w = first; ok && get_tile<kPair>(p, ctl, first_unit, rank, w, e, t); w += step) {
         const int k0 = t.split * split_stages, k1 = min(p.k_stages, k0 + split_stages);
-        for (int k = k0; k < k1; ++k, ++use) {
-          const int b = use % kStages;
-          ok = !*abort_flag && mbar_wait(&ctl.full[b], (use / kStages) & 1, limit);
+        for (int k = k0; k < k1; ++k) {
+          ok = wait(&ctl.full[ring.b], ring.phase);
           if (!ok) break;
-          mbar_arrive_remote(lead(&ctl.peer_full[b]));
+          mbar_arrive_remote(lead(&ctl.peer_full[ring.b]));
+          ring.next<kStages>();
         }
       }
       if (!ok) give_up();
@@ -551,23 +649,25 @@ __global__ void __launch_bounds__(Shape<kPair>::kThreads, Shape<kPair>::kCtasPer
     // -------------------------------------------------------------- rows of x, by token
     if (kGather) {
       const int g = warp - S::kGatherWarp;
-      constexpr int kRows = kTileM / kGatherWarps;  // of this warp: g * kRows ..
+      constexpr int kRows = S::kRowsA / S::kGatherWarps;  // of this warp: g * kRows ..
       constexpr int kCopies = kRows / 4;            // a warp copies four rows (8 lanes each) at once
       const int chunk = lane & 7, sub = lane >> 3;
       const char* xb = static_cast<const char*>(p.x) + chunk * 16;
       const int row_bytes = p.k_elems * (kMx ? 1 : 2);
-      int e = 0, use = 0;
+      int e = 0, pending = 0;
       bool ok = true;
       Tile t;
-      int done = 0;  // stages announced
-      // tells the issuer of the stages before `upto`, whose copies have landed
-      const auto announce = [&](int upto) {
+      Ring ring, oldest;  // the next stage; the first of the `pending` that are not announced
+      // tells the issuer of the oldest stages, all but `left`, whose copies have landed
+      const auto announce = [&](int left) {
         fence_proxy_async_smem();  // before the tensor core reads what was written here
         __syncwarp();
-        for (; done < upto; ++done)
-          if (lane == 0) mbar_arrive(&ctl.full[done % kStages]);
+        for (; pending > left; --pending) {
+          if (lane == 0) mbar_arrive(&ctl.full[oldest.b]);
+          oldest.next<kStages>();
+        }
       };
-      for (int64_t w = first; ok && get_tile<kPair>(p, ctl, rank, w, e, t); w += step) {
+      for (int64_t w = first; ok && get_tile<kPair>(p, ctl, first_unit, rank, w, e, t); w += step) {
         int64_t from[kCopies];  // byte offset of the token's row; -1: no row
         const uint4* src[2] = {nullptr, nullptr};  // scales of rows g * kRows + lane (+ 32)
 #pragma unroll
@@ -608,13 +708,12 @@ __global__ void __launch_bounds__(Shape<kPair>::kThreads, Shape<kPair>::kCtasPer
 #pragma unroll
           for (int j = 0; j < 4; ++j) {
             if (k + j >= p.k_stages) break;
-            const int b = use % kStages;
-            if (use >= kStages &&
-                !__all_sync(0xffffffffu, mbar_test(&ctl.empty[b], ((use / kStages) - 1) & 1))) {
+            const int b = ring.b;
+            if (!__all_sync(0xffffffffu, mbar_test(&ctl.empty[b], ring.phase ^ 1))) {
               cp_async_wait_all();  // nothing else to do: tell of every stage so far
-              announce(use);
+              announce(0);
             }
-            ok = __all_sync(0xffffffffu, stage_free(use, b));
+            ok = warp_wait(&ctl.empty[b], ring.phase ^ 1);
             if (!ok) break;
             uint8_t* sa = base + b * kStageBytes;
             const int col = (k + j) * kStageK;
@@ -629,17 +728,18 @@ __global__ void __launch_bounds__(Shape<kPair>::kThreads, Shape<kPair>::kCtasPer
             cp_async_commit();
             if (kMx) {
               uint8_t* ss = s_scale + b * kScaleBytes + lane * 16 + g * (kRows / 32) * 4;
-              *reinterpret_cast<uint2*>(ss) = make_uint2(now[0][j], now[1][j]);
+              if constexpr (kRows > 32) *reinterpret_cast<uint2*>(ss) = make_uint2(now[0][j], now[1][j]);
+              else *reinterpret_cast<uint32_t*>(ss) = now[0][j];
             }
-            ++use;
-            if (use - done > kGatherLag) {
+            ring.next<kStages>();
+            if (++pending > kGatherLag) {
               cp_async_wait_group<kGatherLag>();
-              announce(use - kGatherLag);
+              announce(kGatherLag);
             }
           }
         }
         cp_async_wait_all();
-        announce(use);
+        announce(0);
       }
       if (!ok && lane == 0) give_up();
       __syncwarp();
@@ -672,12 +772,13 @@ __global__ void __launch_bounds__(Shape<kPair>::kThreads, Shape<kPair>::kCtasPer
         }
       }
     }
-    for (int64_t w = first; ok && get_tile<kPair>(p, ctl, rank, w, e, t); w += step, ++tiles) {
+    for (int64_t w = first; ok && get_tile<kPair>(p, ctl, first_unit, rank, w, e, t); w += step, ++tiles) {
       const bool in = r < t.count;
       int pair = 0;
       if (kPhase == 2) pair = in ? __ldg(p.rows + t.row + r) : -1;
-      ok = !*abort_flag && mbar_wait(&ctl.acc_full, tiles & 1, limit);
-      ok = __all_sync(0xffffffffu, ok);
+      ok = wait(&ctl.acc_full, tiles & 1);
+      if constexpr (kVariant == kFew && kPhase == 2) ok = epilogue_and<S::kEpilogueWarps>(ok);
+      else ok = __all_sync(0xffffffffu, ok);
       if (!ok) break;
       tc_fence_after();
       const int half0 = kPair ? warp >> 2 : 0, half1 = kPair ? half0 + 1 : 2;
@@ -776,6 +877,31 @@ __global__ void __launch_bounds__(Shape<kPair>::kThreads, Shape<kPair>::kCtasPer
           }
         }
       }
+      if constexpr (kVariant == kFew && kPhase == 2) {
+        // The last of a column tile's tiles adds them up (in slot order, whichever is last).
+        if (!p.direct) {
+          __threadfence();
+          epilogue_and<S::kEpilogueWarps>(true);
+          if (threadIdx.x == 0) {
+            const int all = ctl.first_tile[p.experts] * p.splits;
+            ctl.last = atomicAdd(p.arrived + t.n, 1) == all - 1;
+          }
+          epilogue_and<S::kEpilogueWarps>(true);
+          if (ctl.last) {
+            __threadfence();
+            for (int i = threadIdx.x; i < p.tokens * 32; i += 32 * S::kEpilogueWarps) {
+              const int col = t.n * kN + 4 * (i % 32);
+              if (col < p.dim) combine_columns(p, i / 32, col);
+            }
+          }
+        }
+      }
+    }
+    if (kVariant == kFew && kPhase == 2 && !p.direct && ctl.first_tile[p.experts] == 0) {
+      // no token has an expert, and no tile says so
+      for (int64_t i = static_cast<int64_t>(blockIdx.x) * 128 + threadIdx.x;
+           i < static_cast<int64_t>(p.tokens) * (p.dim / 4); i += static_cast<int64_t>(gridDim.x) * 128)
+        combine_columns(p, static_cast<int>(i / (p.dim / 4)), 4 * static_cast<int>(i % (p.dim / 4)));
     }
     if (!ok && lane == 0) give_up();
     __syncwarp();
@@ -839,47 +965,12 @@ __global__ void __launch_bounds__(256) gather_rows(const __grid_constant__ Exper
   }
 }
 
-// y_t = sum over slots (in order) of weight * (sum over splits of the pair's product). Four columns
-// per thread; the products of up to eight slots are in flight at once.
-template <typename Y>
+// One thread per four columns of a token.
 __global__ void __launch_bounds__(128) combine(const __grid_constant__ ExpertsParams p) {
   grid_dep_launch();
   grid_dep_wait();
-  const int64_t t = blockIdx.x;
   const int col = 4 * (blockIdx.y * 128 + threadIdx.x);
-  if (col >= p.dim) return;
-  constexpr int kAhead = 8;
-  float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
-  const int parts = p.top_k * p.splits;  // slot by slot, its splits in order
-  for (int first = 0; first < parts; first += kAhead) {
-    float4 v[kAhead];
-    float w[kAhead];
-#pragma unroll
-    for (int i = 0; i < kAhead; ++i) {
-      v[i] = make_float4(0.f, 0.f, 0.f, 0.f);
-      w[i] = 0.f;
-      const int s = p.splits == 1 ? first + i : (first + i) / p.splits;
-      const int split = p.splits == 1 ? 0 : (first + i) % p.splits;
-      const int64_t pair = t * p.top_k + s;
-      if (first + i < parts && p.ids[pair] >= 0) {
-        v[i] = __ldcs(reinterpret_cast<const float4*>(
-            p.partial + (static_cast<int64_t>(split) * p.pairs + pair) * p.dim + col));
-        w[i] = p.weights[pair];
-      }
-    }
-#pragma unroll
-    for (int i = 0; i < kAhead; ++i) {
-      sum.x = fmaf(w[i], v[i].x, sum.x);
-      sum.y = fmaf(w[i], v[i].y, sum.y);
-      sum.z = fmaf(w[i], v[i].z, sum.z);
-      sum.w = fmaf(w[i], v[i].w, sum.w);
-    }
-  }
-  Y* y = static_cast<Y*>(p.y) + t * p.y_stride + col;
-  if constexpr (sizeof(Y) == 2)
-    *reinterpret_cast<uint2*>(y) = make_uint2(pack2(sum.x, sum.y), pack2(sum.z, sum.w));
-  else
-    *reinterpret_cast<float4*>(y) = sum;
+  if (col < p.dim) combine_columns(p, blockIdx.x, col);
 }
 
 // ---------------------------------------------------------------- host side
@@ -928,7 +1019,7 @@ int max_pairs(F* kernel, std::atomic<int>* cache) {
   if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return sm_count() / 2;
   int n = cache[dev].load(std::memory_order_relaxed);
   if (n > 0) return n;
-  const Launch l(dim3(2 * 64), Shape<true>::kThreads, smem_bytes<true>(), nullptr, 2);
+  const Launch l(dim3(2 * 64), Shape<kPairs>::kThreads, smem_bytes<kPairs>(), nullptr, 2);
   if (cudaOccupancyMaxActiveClusters(&n, kernel, &l.cfg) != cudaSuccess || n <= 0) {
     cudaGetLastError();
     return sm_count() / 2;
@@ -937,32 +1028,27 @@ int max_pairs(F* kernel, std::atomic<int>* cache) {
   return n;
 }
 
-template <bool kMx, bool kPair, int kPhase>
+template <bool kMx, int kVariant, int kPhase>
 cudaError_t launch_product(const ExpertsParams& p, int64_t tiles, const CUtensorMap& a,
                            const CUtensorMap& b0, const CUtensorMap& b1, cudaStream_t stream) {
+  using S = Shape<kVariant>;
   static std::atomic<uint64_t> done{0};
   static std::atomic<int> pairs[64];
-  const auto kernel = product<kMx, kPair, kPhase>;
-  const size_t smem = smem_bytes<kPair>();
-  const cudaError_t e = ensure_smem_attr(kernel, smem, done);
+  const auto kernel = product<kMx, kVariant, kPhase>;
+  const cudaError_t e = ensure_smem_attr(kernel, smem_bytes<kVariant>(), done);
   if (e != cudaSuccess) return e;
-  const int64_t most = kPair ? max_pairs(kernel, pairs) : sm_count() * Shape<false>::kCtasPerSm;
-  const unsigned ctas = static_cast<unsigned>(std::min<int64_t>(tiles, most)) * (kPair ? 2 : 1);
-  const Launch l(dim3(ctas), Shape<kPair>::kThreads, smem, stream, kPair ? 2 : 1);
+  const int64_t most = S::kPair ? max_pairs(kernel, pairs) : sm_count() * S::kCtasPerSm;
+  const unsigned ctas = static_cast<unsigned>(std::min<int64_t>(tiles, most)) * S::kCtas;
+  const Launch l(dim3(ctas), S::kThreads, smem_bytes<kVariant>(), stream, S::kCtas);
   return cudaLaunchKernelEx(&l.cfg, kernel, p, a, b0, b1);
 }
 
 template <bool kMx, int kPhase>
-cudaError_t launch_phase(const ExpertsParams& p, bool pair, int64_t tiles, const CUtensorMap& a,
+cudaError_t launch_phase(const ExpertsParams& p, int variant, int64_t tiles, const CUtensorMap& a,
                          const CUtensorMap& b0, const CUtensorMap& b1, cudaStream_t s) {
-  return pair ? launch_product<kMx, true, kPhase>(p, tiles, a, b0, b1, s)
-              : launch_product<kMx, false, kPhase>(p, tiles, a, b0, b1, s);
-}
-
-template <typename Y>
-cudaError_t launch_combine(const ExpertsParams& p, cudaStream_t stream) {
-  const Launch l(dim3(p.tokens, (p.dim / 4 + 127) / 128), 128, 0, stream);
-  return cudaLaunchKernelEx(&l.cfg, combine<Y>, p);
+  return variant == kPairs    ? launch_product<kMx, kPairs, kPhase>(p, tiles, a, b0, b1, s)
+         : variant == kSingle ? launch_product<kMx, kSingle, kPhase>(p, tiles, a, b0, b1, s)
+                              : launch_product<kMx, kFew, kPhase>(p, tiles, a, b0, b1, s);
 }
 
 constexpr size_t up256(size_t n) { return (n + 255) / 256 * 256; }
@@ -970,22 +1056,22 @@ constexpr size_t up256(size_t n) { return (n + 255) / 256 * 256; }
 // Sizes that follow from a call's sizes alone.
 struct Plan {
   int64_t pairs, row_tiles;  // at most so many row tiles of 128 pairs
-  bool pair1, pair2;
+  int variant1, variant2;    // of each phase
   int64_t tiles1, tiles2;    // at most so many tiles of each phase
   int splits, split_stages;
-  size_t h_bytes, h_scale_bytes, partial_bytes, xg_bytes, xg_scale_bytes;
+  size_t arrived_bytes, h_bytes, h_scale_bytes, partial_bytes, xg_bytes, xg_scale_bytes;
   bool direct;  // phase 2 writes y itself
   // x in the plan's order is read for the last time in phase 1, the pairs' products are written
   // in phase 2: they share their bytes
   size_t bytes() const {
-    return h_bytes + h_scale_bytes + std::max(partial_bytes, xg_bytes + xg_scale_bytes);
+    return arrived_bytes + h_bytes + h_scale_bytes + std::max(partial_bytes, xg_bytes + xg_scale_bytes);
   }
 };
 
-// Pairs of CTAs unless their tiles would leave SMs idle (their count, over the row tiles that
-// the call can have, is below half of the SM count). Where even single tiles of phase 2 leave
-// SMs idle (few pairs, a long reduction), the reduction is split, into runs of at least four
-// stages.
+// Few tokens (no expert can have more rows): kFew, in both phases. Else pairs of CTAs, unless their
+// tiles would leave SMs idle (their count, over the row tiles that the call can have, is below
+// half of the SM count), then single ones. Where even those leave SMs idle in phase 2 (few pairs,
+// a long reduction), the reduction is split, into runs of at least four stages.
 Plan make_plan(int64_t tokens, int experts, int top_k, int dim, int hidden, bool mx) {
   Plan q = {};
   q.pairs = tokens * top_k;
@@ -994,13 +1080,14 @@ Plan make_plan(int64_t tokens, int experts, int top_k, int dim, int hidden, bool
   const int64_t row_pairs = q.pairs / (2 * kTileM) + used;
   const int64_t sms = sm_count();
   const auto columns = [](int n, int per) { return static_cast<int64_t>((n + per - 1) / per); };
-  q.pair1 = row_pairs * columns(hidden, 128) >= sms / 2;
-  q.pair2 = row_pairs * columns(dim, 256) >= sms / 2;
-  q.tiles1 = q.pair1 ? row_pairs * columns(hidden, 128) : q.row_tiles * columns(hidden, 64);
-  q.tiles2 = q.pair2 ? row_pairs * columns(dim, 256) : q.row_tiles * columns(dim, 128);
+  const bool few = tokens <= kFewTokens;
+  q.variant1 = few ? kFew : row_pairs * columns(hidden, 128) >= sms / 2 ? kPairs : kSingle;
+  q.variant2 = few ? kFew : row_pairs * columns(dim, 256) >= sms / 2 ? kPairs : kSingle;
+  q.tiles1 = q.variant1 == kPairs ? row_pairs * columns(hidden, 128) : q.row_tiles * columns(hidden, 64);
+  q.tiles2 = q.variant2 == kPairs ? row_pairs * columns(dim, 256) : q.row_tiles * columns(dim, 128);
   const int stages = (hidden + (mx ? 127 : 63)) / (mx ? 128 : 64);
   int64_t splits = 1;
-  if (!q.pair2 && q.tiles2 * 2 <= sms)
+  if (q.variant2 != kPairs && q.tiles2 * 2 <= sms)
     splits = std::max<int64_t>(1, std::min<int64_t>(sms / q.tiles2, stages / 4));
   q.split_stages = static_cast<int>((stages + splits - 1) / splits);
   q.splits = (stages + q.split_stages - 1) / q.split_stages;
@@ -1008,7 +1095,8 @@ Plan make_plan(int64_t tokens, int experts, int top_k, int dim, int hidden, bool
   const size_t rows = static_cast<size_t>(q.row_tiles) * kTileM;
   q.h_bytes = up256(rows * hidden * (mx ? 1 : 2));
   q.h_scale_bytes = mx ? up256(static_cast<size_t>(q.row_tiles) * ((hidden + 127) / 128) * kMxTileBytes) : 0;
-  if (q.pair1) {
+  q.arrived_bytes = few ? up256(static_cast<size_t>(columns(dim, kTileB)) * 4) : 0;
+  if (q.variant1 == kPairs) {
     q.xg_bytes = up256(rows * dim * (mx ? 1 : 2));
     q.xg_scale_bytes = mx ? up256(static_cast<size_t>(q.row_tiles) * ((dim + 127) / 128) * kMxTileBytes) : 0;
   }
@@ -1095,10 +1183,11 @@ dard_status dard_experts(const dard_experts_args* a, void* stream) {
   p.x_scale = a->x_scale;
   p.scale_b[0] = a->w1_scale;
   p.scale_b[1] = a->w3_scale;
-  p.h = ws;
-  p.h_scale = ws + q.h_bytes;
-  p.partial = reinterpret_cast<float*>(ws + q.h_bytes + q.h_scale_bytes);
-  p.xg = ws + q.h_bytes + q.h_scale_bytes;
+  p.arrived = reinterpret_cast<int32_t*>(ws);
+  p.h = ws + q.arrived_bytes;
+  p.h_scale = p.h + q.h_bytes;
+  p.xg = p.h_scale + q.h_scale_bytes;
+  p.partial = reinterpret_cast<float*>(p.xg);
   p.xg_scale = p.xg + q.xg_bytes;
   p.y = a->y;
   p.status = a->status;
@@ -1126,13 +1215,14 @@ dard_status dard_experts(const dard_experts_args* a, void* stream) {
   // phase 1: rows of x (in the plan's order, or gathered by the kernel itself) and of w1 and w3
   const uint64_t drow = static_cast<uint64_t>(a->dim) * esz, hrow = static_cast<uint64_t>(a->hidden) * esz;
   const uint64_t rows = static_cast<uint64_t>(q.row_tiles) * kTileM;
-  const uint32_t box1 = q.pair1 ? 128 : 64;
+  const bool pair1 = q.variant1 == kPairs, pair2 = q.variant2 == kPairs;
+  const uint32_t box1 = pair1 ? 128 : 64;
   if (e == cudaSuccess && (!encode(&mb0, a->w1, mx, a->dim, a->hidden, a->experts, drow, box1) ||
                            !encode(&mb1, a->w3, mx, a->dim, a->hidden, a->experts, drow, box1) ||
-                           (q.pair1 && !encode(&ma, p.xg, mx, a->dim, rows, 0, drow, kTileM))))
+                           (pair1 && !encode(&ma, p.xg, mx, a->dim, rows, 0, drow, kTileM))))
     e = cudaErrorInvalidValue;
-  if (!q.pair1) ma = mb0;  // not used
-  if (e == cudaSuccess && q.pair1) {
+  if (!pair1) ma = mb0;  // not used
+  if (e == cudaSuccess && pair1) {
     const Launch l(dim3(static_cast<unsigned>(std::min<int64_t>((q.pairs + 7) / 8, 8ll * sm_count()))),
                    256, 0, s);
     e = mx ? cudaLaunchKernelEx(&l.cfg, gather_rows<true>, p)
@@ -1146,16 +1236,16 @@ dard_status dard_experts(const dard_experts_args* a, void* stream) {
     p.k_stages = (a->dim + stage - 1) / stage;
     p.splits = 1;
     p.split_stages = p.k_stages;
-    e = mx ? launch_phase<true, 1>(p, q.pair1, q.tiles1, ma, mb0, mb1, s)
-           : launch_phase<false, 1>(p, q.pair1, q.tiles1, ma, mb0, mb1, s);
+    e = mx ? launch_phase<true, 1>(p, q.variant1, q.tiles1, ma, mb0, mb1, s)
+           : launch_phase<false, 1>(p, q.variant1, q.tiles1, ma, mb0, mb1, s);
   }
   // phase 2: rows of h, rows of w2
   if (e == cudaSuccess &&
-      (!encode(&ma, p.h, mx, a->hidden, rows, 0, hrow, q.pair2 ? kTileM : kBoxRowsSingle) ||
+      (!encode(&ma, p.h, mx, a->hidden, rows, 0, hrow, pair2 ? Shape<kPairs>::kBoxA : Shape<kSingle>::kBoxA) ||
        !encode(&mb0, a->w2, mx, a->hidden, a->dim, a->experts, hrow, 128)))
     e = cudaErrorInvalidValue;
   if (e == cudaSuccess) {
-    const int per = q.pair2 ? 256 : 128;
+    const int per = pair2 ? 256 : 128;
     p.scale_b[0] = a->w2_scale;
     p.a_scale = p.h_scale;
     p.k_elems = a->hidden;
@@ -1164,11 +1254,13 @@ dard_status dard_experts(const dard_experts_args* a, void* stream) {
     p.k_stages = (a->hidden + stage - 1) / stage;
     p.splits = q.splits;
     p.split_stages = q.split_stages;
-    e = mx ? launch_phase<true, 2>(p, q.pair2, q.tiles2, ma, mb0, mb0, s)
-           : launch_phase<false, 2>(p, q.pair2, q.tiles2, ma, mb0, mb0, s);
+    e = mx ? launch_phase<true, 2>(p, q.variant2, q.tiles2, ma, mb0, mb0, s)
+           : launch_phase<false, 2>(p, q.variant2, q.tiles2, ma, mb0, mb0, s);
   }
-  if (e == cudaSuccess && !p.direct)
-    e = p.y_f32 ? launch_combine<float>(p, s) : launch_combine<__nv_bfloat16>(p, s);
+  if (e == cudaSuccess && !p.direct && q.variant2 != kFew) {
+    const Launch l(dim3(p.tokens, (p.dim / 4 + 127) / 128), 128, 0, s);
+    e = cudaLaunchKernelEx(&l.cfg, combine, p);
+  }
   if (e != cudaSuccess)
     return report(DARD_ERR_CUDA, "experts launch failed: %s", cudaGetErrorString(e));
   return DARD_OK;
