@@ -242,8 +242,7 @@ __host__ __device__ constexpr uint32_t idesc_mx(uint32_t M, uint32_t N, uint32_t
 }
 
 struct __align__(16) Ctl {
-  uint64_t full[kMaxStages], empty[kMaxStages];
-  uint64_t peer_full[kMaxStages];  // pair, rank 0: rank 1's stage is full
+  uint64_t full[kMaxStages], empty[kMaxStages];  // (pair, rank 0: full in both CTAs)
   uint64_t acc_full, acc_free;
   uint64_t drained;  // every MMA the issuer launched has completed
   uint32_t tmem_base;
@@ -332,6 +331,14 @@ __device__ __forceinline__ void read_plan(const ExpertsParams& p, int32_t* first
     carry_u += __shfl_sync(0xffffffffu, units, 31);
   }
   if (lane == 0) first_tile[0] = first_unit[0] = 0;
+}
+
+// Uses of r stay behind this point.
+__device__ __forceinline__ void pin32(uint32_t (&r)[32]) {
+#pragma unroll
+  for (int i = 0; i < 32; i += 8)
+    asm volatile("" : "+r"(r[i]), "+r"(r[i + 1]), "+r"(r[i + 2]), "+r"(r[i + 3]), "+r"(r[i + 4]),
+                      "+r"(r[i + 5]), "+r"(r[i + 6]), "+r"(r[i + 7]));
 }
 
 __device__ __forceinline__ float silu(float g) { return __fdividef(g, 1.f + __expf(-g)); }
@@ -431,9 +438,9 @@ __global__ void __launch_bounds__(Shape<kVariant>::kThreads, Shape<kVariant>::kC
   }
   if (warp == S::kProducerWarp && lane == 0) {
     for (int b = 0; b < kStages; ++b) {
-      mbar_init(&ctl.full[b], kGather ? 1 + S::kGatherWarps : 1);
+      // the producer, the gather warps, and in rank 0 of a pair rank 1's forwarder
+      mbar_init(&ctl.full[b], 1 + (kGather ? S::kGatherWarps : 0) + (kPair && rank == 0 ? 1 : 0));
       mbar_init(&ctl.empty[b], 1);
-      mbar_init(&ctl.peer_full[b], 1);
     }
     mbar_init(&ctl.acc_full, 1);
     mbar_init(&ctl.acc_free, S::kEpilogueWarps * kCtas);
@@ -569,6 +576,7 @@ __global__ void __launch_bounds__(Shape<kVariant>::kThreads, Shape<kVariant>::kC
       const uint64_t desc_a = smem_desc_sw128(smem_u32(base), 16, 1024);
       const uint64_t desc_s = scale_desc(smem_u32(s_scale));
       uint32_t sfa = tmem + S::kScaleCol;  // scales of two stages, 16 columns apart
+      bool ready = false;                  // the stage at `ring` is known to be full
       for (int64_t w = first; ok && get_tile<kPair>(p, ctl, first_unit, rank, w, e, t); w += step, ++tiles) {
         ok = tiles == 0 || warp_wait(&ctl.acc_free, (tiles - 1) & 1);
         if (!ok) break;
@@ -577,10 +585,14 @@ __global__ void __launch_bounds__(Shape<kVariant>::kThreads, Shape<kVariant>::kC
         // 64 weight rows of a matrix are half of a tile of 128 scales
         const uint32_t half = kPhase == 1 && kCols == 64 ? (t.n & 1) * 2 : 0;
         for (int k = k0; k < k1; ++k) {
-          ok = warp_wait(&ctl.full[ring.b], ring.phase) &&
-               (!kPair || warp_wait(&ctl.peer_full[ring.b], ring.phase));
+          // (a wait, even one that is over, costs some 120 cycles, a fifth of a stage: the next
+          // stage's barrier is looked at while this one's MMAs are issued)
+          if (!ready) ok = warp_wait(&ctl.full[ring.b], ring.phase);
           if (!ok) break;
           tc_fence_after();
+          Ring next = ring;
+          next.next<kStages>();
+          const bool look = mbar_test(&ctl.full[next.b], next.phase);
           if (issue) {
             // descriptors count 16-byte units
             const uint64_t da = desc_a + ring.b * (kStageBytes / 16), db = da + S::kBytesA / 16;
@@ -617,8 +629,8 @@ __global__ void __launch_bounds__(Shape<kVariant>::kThreads, Shape<kVariant>::kC
               else mma_commit(&ctl.acc_full);
             }
           }
-          __syncwarp();
-          ring.next<kStages>();
+          ready = __all_sync(0xffffffffu, look);
+          ring = next;
           sfa ^= 16;
         }
       }
@@ -638,7 +650,7 @@ __global__ void __launch_bounds__(Shape<kVariant>::kThreads, Shape<kVariant>::kC
         for (int k = k0; k < k1; ++k) {
           ok = wait(&ctl.full[ring.b], ring.phase);
           if (!ok) break;
-          mbar_arrive_remote(lead(&ctl.peer_full[ring.b]));
+          mbar_arrive_remote(lead(&ctl.full[ring.b]));
           ring.next<kStages>();
         }
       }
@@ -802,6 +814,9 @@ __global__ void __launch_bounds__(Shape<kVariant>::kThreads, Shape<kVariant>::kC
             else mbar_arrive(&ctl.acc_free);
           }
         }
+        // (what follows may not move ahead of that: it did, and held the MMAs up by 2000 cycles)
+#pragma unroll
+        for (int c = 0; c < kChunks; ++c) pin32(acc[c]);
         if constexpr (kPhase == 1) {
 #pragma unroll
           for (int c = 0; c < kChunks / 2; ++c) {
