@@ -171,13 +171,17 @@ def _torch():
     return torch
 
 
+_current_stream = None
+
+
 def _raw_stream(device_index: int) -> int:
     """cudaStream_t of the device's current torch stream."""
-    torch = _torch()
-    f = getattr(torch._C, "_cuda_getCurrentRawStream", None)
-    if f is not None:
-        return f(device_index)
-    return torch.cuda.current_stream(device_index).cuda_stream
+    global _current_stream
+    if _current_stream is None:
+        torch = _torch()
+        _current_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (
+            lambda i: torch.cuda.current_stream(i).cuda_stream)
+    return _current_stream(device_index)
 
 
 def _stream_handle(stream, device_index: int) -> int:
@@ -495,7 +499,7 @@ def _dtypes(kind: str) -> tuple:
 def _rows2(t, name: str, shape: tuple, dtypes: tuple, device: int) -> tuple[int, int]:
     """(pointer, row stride) of a device tensor of this 2-D shape with contiguous rows. (One
     pass of cheap comparisons; what is wrong is looked for only when one fails.)"""
-    if t.dtype in dtypes and t.get_device() == device and t.shape == shape:
+    if t.dtype in dtypes and t.get_device() == device >= 0 and t.shape == shape:
         s0, s1 = t.stride()
         if s1 == 1 and s0 >= shape[1]:
             return t.data_ptr(), s0
@@ -516,10 +520,10 @@ def _rows2(t, name: str, shape: tuple, dtypes: tuple, device: int) -> tuple[int,
 
 def _scale_rows(t, name: str, rows: int, cols: int, device: int) -> tuple[int, int]:
     """(pointer, pitch) of a scale tensor in layout ROWS for [rows, cols] elements."""
-    if t.dim() != 2 or t.shape[1] * MX_BLOCK < cols:
-        raise ValueError(f"{name}: {list(mx_scale_shape((rows, cols)))} expected, got "
-                         f"{tuple(t.shape)}")
-    return _rows2(t, name, (rows, t.shape[1]), _dtypes("scales"), device)
+    shape = t.shape
+    if len(shape) != 2 or shape[1] * MX_BLOCK < cols:
+        raise ValueError(f"{name}: {list(mx_scale_shape((rows, cols)))} expected, got {tuple(shape)}")
+    return _rows2(t, name, (rows, shape[1]), _dtypes("scales"), device)
 
 
 class NormCall:
@@ -535,6 +539,7 @@ class NormCall:
         if dtype not in _dtypes("float"):
             raise ValueError(f"unsupported dtype {dtype}")
         self.dim, self._dt = dim, (dtype,)
+        self._codes = _dtypes("codes")
         if weight is not None and weight.numel() != dim:
             raise ValueError(f"weight: {dim} elements expected, got {weight.numel()}")
         self.device = None if weight is None else weight.get_device()
@@ -560,7 +565,7 @@ class NormCall:
         if y8 is not None:
             if y8_scale is None:
                 raise ValueError("y8 needs y8_scale")
-            qp, qs = _rows2(y8, "y8", shape, _dtypes("codes"), dev)
+            qp, qs = _rows2(y8, "y8", shape, self._codes, dev)
             sp, ss = _scale_rows(y8_scale, "y8_scale", rows, dim, dev)
         self._layout.pack_into(self._args, 0, xp, dp, self._weight_ptr, rp, yp, qp, sp, self._code,
                                dim, rows, xs, ds, rs, ys, qs, ss, self._eps)
@@ -576,11 +581,13 @@ def dard_residual_norm(x, delta=None, weight=None, eps: float = 1e-6, residual=N
 _MX_LAYOUT = struct.Struct("=3Qiiiiqqqq")  # dard_mx_args
 
 
-def _flat(t, name: str, dtypes: tuple, device: int) -> int:
-    """Pointer of a contiguous device tensor."""
-    if t.dtype not in dtypes or t.get_device() != device or not t.is_contiguous():
+def _flat(t, name: str, dtypes: tuple, device: int, least: int = 0) -> int:
+    """Pointer of a contiguous device tensor of at least ``least`` elements."""
+    if t.dtype not in dtypes or not t.get_device() == device >= 0 or not t.is_contiguous():
         _is_dtype(t, name, dtypes)
         raise ValueError(f"{name}: contiguous tensor on device {device} expected")
+    if t.numel() < least:
+        raise ValueError(f"{name}: at least {least} elements expected, got {t.numel()}")
     return t.data_ptr()
 
 
@@ -630,7 +637,6 @@ class RouteCall:
                  scale: float = 1.0, workspace=None, status=None):
         torch = _torch()
         self.experts, self.top_k = experts, top_k
-        self._i32, self._f32 = torch.int32, torch.float32
         a = RouteArgs()
         self.device = next((t.get_device() for t in (bias, workspace, status) if t is not None), None)
         a.bias = _dev(bias, "bias", experts, torch.float32, self.device)
@@ -655,12 +661,16 @@ class RouteCall:
         if ids.shape != (tokens, k) or weights.shape != (tokens, k):
             raise ValueError(f"ids and weights: [{tokens}, {k}] expected, got {tuple(ids.shape)}, "
                              f"{tuple(weights.shape)}")
-        a.ids = _dev(ids, "ids", tokens * k, self._i32, dev)
-        a.weights = _dev(weights, "weights", tokens * k, self._f32, dev)
+        i32 = _dtypes("i32")
+        a.ids = _flat(ids, "ids", i32, dev)
+        a.weights = _flat(weights, "weights", _dtypes("f32"), dev)
         if (offsets is None) != (rows is None):
             raise ValueError("offsets and rows come together")
-        a.offsets = _dev(offsets, "offsets", self.experts + 1, self._i32, dev)
-        a.rows = _dev(rows, "rows", tokens * k, self._i32, dev)
+        if offsets is not None:
+            a.offsets = _flat(offsets, "offsets", i32, dev, self.experts + 1)
+            a.rows = _flat(rows, "rows", i32, dev, tokens * k)
+        else:
+            a.offsets = a.rows = None
         _check(self._fn(self._ref, _stream_handle(stream, dev)), "dard_route")
 
 
@@ -694,7 +704,7 @@ class ExpertsCall:
                              f"got {tuple(w1.shape)}, {tuple(w3.shape)}, {tuple(w2.shape)}")
         self.experts, self.hidden, self.dim = w1.shape
         self.mx = w1.dtype != torch.bfloat16
-        self._i32, self._f32, self._bf16 = torch.int32, torch.float32, torch.bfloat16
+        self._bf16 = torch.bfloat16
         self.device = dev = w1.get_device()
         a = ExpertsArgs()
         for name, w, s in (("w1", w1, w1_scale), ("w3", w3, w3_scale), ("w2", w2, w2_scale)):
@@ -736,10 +746,11 @@ class ExpertsCall:
         if weights.shape != ids.shape:
             raise ValueError(f"weights: {tuple(ids.shape)} expected, got {tuple(weights.shape)}")
         a.tokens, a.top_k = tokens, k
-        a.ids = _dev(ids, "ids", tokens * k, self._i32, dev)
-        a.weights = _dev(weights, "weights", tokens * k, self._f32, dev)
-        a.offsets = _dev(offsets, "offsets", self.experts + 1, self._i32, dev)
-        a.rows = _dev(rows, "rows", tokens * k, self._i32, dev)
+        i32, f32 = _dtypes("i32"), _dtypes("f32")
+        a.ids = _flat(ids, "ids", i32, dev)
+        a.weights = _flat(weights, "weights", f32, dev)
+        a.offsets = _flat(offsets, "offsets", i32, dev, self.experts + 1)
+        a.rows = _flat(rows, "rows", i32, dev, tokens * k)
         _check(self._fn(self._ref, _stream_handle(stream, dev)), "dard_experts")
 
 

@@ -202,6 +202,16 @@ __global__ void __launch_bounds__(32 * kWarps) norm_rows_any(const __grid_consta
       if (e < p.dim) v[j] = rounded<T>(v[j] + to_f(delta[e]));
     }
   }
+  const T* weight = static_cast<const T*>(p.weight);
+  constexpr bool kEarly = kElems <= 16;  // (more do not fit the registers)
+  T w[kElems];  // on its way during the reduction
+  if (kEarly && weight != nullptr) {
+#pragma unroll
+    for (int j = 0; j < kElems; ++j) {
+      const int e = t + j * kThreads;
+      if (e < p.dim) w[j] = weight[e];
+    }
+  }
   float sum = 0.f;
 #pragma unroll
   for (int j = 0; j < kElems; ++j) sum = fmaf(v[j], v[j], sum);
@@ -216,13 +226,12 @@ __global__ void __launch_bounds__(32 * kWarps) norm_rows_any(const __grid_consta
   sum = row_sum<kWarps>(sum, red);
   const float inv = rsqrtf(sum * p.inv_dim + p.eps);
   T* y = p.y ? static_cast<T*>(p.y) + row * p.y_stride : nullptr;
-  const T* w = static_cast<const T*>(p.weight);
 #pragma unroll
   for (int j = 0; j < kElems; ++j) {
     const int e = t + j * kThreads;
     const bool in = e < p.dim;
     v[j] *= inv;
-    if (w != nullptr && in) v[j] *= to_f(w[e]);
+    if (weight != nullptr && in) v[j] *= to_f(kEarly ? w[j] : weight[e]);
     if (y != nullptr && in) from_f(y[e], v[j]);
     if (p.y8 != nullptr) {
       float m = fabsf(v[j]);
@@ -253,12 +262,14 @@ cudaError_t launch_norm(const NormParams& p, bool vec, cudaStream_t s) {
     else if (d <= 16384) norm_rows<T, 16, 4><<<rows, 512, 0, s>>>(p);
     else norm_rows<T, 32, 4><<<rows, 1024, 0, s>>>(p);
   } else {
-    if (d <= 1024) norm_rows_any<T, 4, 8><<<rows, 128, 0, s>>>(p);
-    else if (d <= 2048) norm_rows_any<T, 8, 8><<<rows, 256, 0, s>>>(p);
-    else if (d <= 4096) norm_rows_any<T, 16, 8><<<rows, 512, 0, s>>>(p);
-    else if (d <= 8192) norm_rows_any<T, 32, 8><<<rows, 1024, 0, s>>>(p);
-    else if (d <= 16384) norm_rows_any<T, 32, 16><<<rows, 1024, 0, s>>>(p);
-    else norm_rows_any<T, 32, 32><<<rows, 1024, 0, s>>>(p);
+    // the fewest warps that hold the row in eight elements per thread
+    if (d <= 4 * 32 * 8) norm_rows_any<T, 4, 8><<<rows, 4 * 32, 0, s>>>(p);
+    else if (d <= 8 * 32 * 8) norm_rows_any<T, 8, 8><<<rows, 8 * 32, 0, s>>>(p);
+    else if (d <= 12 * 32 * 8) norm_rows_any<T, 12, 8><<<rows, 12 * 32, 0, s>>>(p);
+    else if (d <= 16 * 32 * 8) norm_rows_any<T, 16, 8><<<rows, 16 * 32, 0, s>>>(p);
+    else if (d <= 32 * 32 * 8) norm_rows_any<T, 32, 8><<<rows, 32 * 32, 0, s>>>(p);
+    else if (d <= 32 * 32 * 16) norm_rows_any<T, 32, 16><<<rows, 32 * 32, 0, s>>>(p);
+    else norm_rows_any<T, 32, 32><<<rows, 32 * 32, 0, s>>>(p);
   }
   return cudaGetLastError();
 }
