@@ -13,32 +13,37 @@
 // thread's registers: a thread of the epilogue holds one pair (TMEM lane) and 32 consecutive
 // hidden elements, which is one MX block: its scale needs no exchange.
 //
-// Two variants:
-//   pair    two CTAs of a cluster (cta_group::2) share one M = 256, N = 256 MMA: each holds 128
-//           rows of A and 128 weight rows, so that a stage moves 32 KB into each SM's shared
-//           memory where one CTA with the same tile would move 48 KB and be bound by it;
-//   single  one CTA, M = 128, N = 128: more and smaller tiles for calls with few rows.
+// Three variants, chosen by the call's sizes (make_plan):
+//   pairs   two CTAs of a cluster (cta_group::2) share one M = 256, N = 256 MMA: each holds 128
+//           rows of A and 128 weight rows. A stage moves 32 KB into each SM's shared memory; one
+//           CTA with a 128 x 256 tile would move 48 KB, which together with what the MMA reads is
+//           more than shared memory carries (phase 1 at 2.3 against 2.9 PFLOP/s);
+//   single  one CTA, M = 128, N = 128: more and smaller tiles, for calls with few rows;
+//   few     at most 32 tokens: the same with a short A stage and deeper staging of the weights,
+//           and no launch for the sum over the slots: a column tile's last CTA adds them up.
 //
-// Per CTA (one per SM):
-//   warps 0-7   epilogue: TMEM -> registers, then the accumulator is free for the next tile
-//               while SwiGLU, the rounding and the stores run from registers;
-//   warp 8      TMA producer: A (consecutive rows) and B tiles, their scales (cp.async.bulk);
-//   warp 9      TMEM allocation; one lane issues the scale copies (tcgen05.cp) and MMAs (pair:
-//               in rank 0; rank 1's lane forwards the landing of its stages to rank 0);
-//   warps 10-11 single, phase 1: gather the rows of x by token (cp.async, 16 bytes per lane,
-//               straight into the swizzled layout) and their scales (16 bytes, four stages, at
-//               a time).
+// Roles per CTA (warps: pairs 12, single 8, few 7):
+//   epilogue    8 warps (single, few: 4): TMEM -> registers, then the accumulator is free for the
+//               next tile while SwiGLU, the rounding and the stores run from registers;
+//   producer    TMA: rows of A that lie side by side, weights, scales (cp.async.bulk);
+//   issuer      TMEM allocation; scale copies (tcgen05.cp) and MMAs (pairs: in rank 0; in rank 1
+//               it forwards the landing of its stages to rank 0's barriers);
+//   gather      single and few, phase 1: the rows of x by token (cp.async, 16 bytes per lane,
+//               straight into the swizzled layout) and their scales.
+//   Stage: 128 bytes of K of the A rows and of the weight rows (128-byte swizzle), plus scales.
+//   TMEM: the accumulator, then the scales of two stages.
 //
-//   Stage: 128 bytes of K of the A rows and of the B rows (128-byte swizzle), plus scales.
-//   TMEM: accumulator from column 0, scales of two stages from column 256.
+// Pairs read rows of x that an earlier launch (gather_rows) has put in the plan's order. For 4096
+// rows of one expert of 4096 x 12288 the call takes 378 us that way; with the rows gathered in
+// phase 1 by cp.async from four warps 478, by TMA's row gather (tile::gather4) from four warps 448.
+// For few rows the copy's launch costs more than the gather does.
 //
-// Pairs read rows of x that an earlier launch (gather_rows) has put in the plan's order. At 4096
-// tokens x 8 of 32 experts of 4096 x 2048 that copy takes 33 us and phase 1 381 us; gathered within
-// phase 1 by two warps it takes 514 us, by TMA's own row gather (tile::gather4, 32 copies per
-// stage) longer still. For few rows the copy's launch costs more than the gather does, so the
-// single variant gathers itself.
-//
-// The work is the weights' bytes for few tokens (HBM) and the tensor pipe for many.
+// What bounds it, on GB300: pairs, 3.27 PFLOP/s in MXFP8 at 4096 x 4096 x 12288, the tensor pipe
+// and shared memory together (with half of the weights' bytes left out it is 10 % faster, without
+// its stores 7 %); 8192 tokens x 8 of 64 experts of 4096 x 2048 1.46-1.59 ms, of which gather_rows takes
+// 70 us and combine 257 us, both HBM's bytes. Few: the weights' bytes (32 tokens x 8 of 64 of
+// 2048 x 1024: 403 MB in 85 us; with no MMA at all 80) and for one token the chain of latencies
+// (22.7 us; its 52 MB alone would take 7.6).
 //
 // Every wait is bounded; one that gives up sets DARD_STATUS_TIMEOUT and the CTA's abort flag,
 // on which every role leaves its loop. The producer then waits (bounded) for its copies in
@@ -814,7 +819,7 @@ __global__ void __launch_bounds__(Shape<kVariant>::kThreads, Shape<kVariant>::kC
             else mbar_arrive(&ctl.acc_free);
           }
         }
-        // (what follows may not move ahead of that: it did, and held the MMAs up by 2000 cycles)
+        // (the arithmetic that follows may not move ahead of that)
 #pragma unroll
         for (int c = 0; c < kChunks; ++c) pin32(acc[c]);
         if constexpr (kPhase == 1) {
