@@ -310,24 +310,48 @@ __device__ __forceinline__ void exclusive_scan(int32_t* v, int n, int32_t* warp_
   __syncthreads();
 }
 
-// Places of the pairs of tokens [t0, t1): next[b] is the place of the CTA's first pair of
-// bucket b (expert, or `experts` for slots without one). Warp w takes the w-th run of pairs:
-// it counts them (hist), the runs' counts are summed over the warps, then it places them, 32
-// at a time, in order.
+// The pairs of tokens [t0, t1) as warp w of kWarps sees them: the w-th run of `per` pairs (a
+// multiple of 32). The ids of the first kHeld of 32 are held in registers, so that they can be
+// on their way while something else is done.
+constexpr int kHeld = 2;
+struct WarpPairs {
+  int64_t base;  // first pair of the CTA
+  int i0, i1;    // this warp's, from there
+  int id[kHeld];
+};
 template <int kWarps>
-__device__ __forceinline__ void place_pairs(const RouteParams& p, int t0, int t1,
-                                            const int32_t* next, int32_t* hist) {
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, buckets = p.experts + 1;
-  for (int i = threadIdx.x; i < kWarps * buckets; i += blockDim.x) hist[i] = 0;
-  __syncthreads();
-  const int64_t base = static_cast<int64_t>(t0) * p.top_k;
+__device__ __forceinline__ WarpPairs warp_pairs(const RouteParams& p, int t0, int t1) {
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  WarpPairs w;
+  w.base = static_cast<int64_t>(t0) * p.top_k;
   const int pairs = (t1 - t0) * p.top_k;
   const int per = ((pairs + kWarps - 1) / kWarps + 31) / 32 * 32;
-  const int i0 = warp * per, i1 = min(pairs, i0 + per);
+  w.i0 = warp * per;
+  w.i1 = min(pairs, w.i0 + per);
+#pragma unroll
+  for (int j = 0; j < kHeld; ++j) {
+    const int i = w.i0 + 32 * j + lane;
+    w.id[j] = i < w.i1 ? p.ids[w.base + i] : -1;
+  }
+  return w;
+}
+
+// Places of the CTA's pairs: next[b] is the place of its first pair of bucket b (expert, or
+// `experts` for slots without one). Each warp counts its pairs (hist, zeros at the start), the counts
+// are summed over the warps, then each warp places its pairs, 32 at a time, in order.
+template <int kWarps>
+__device__ __forceinline__ void place_pairs(const RouteParams& p, const WarpPairs& w,
+                                            const int32_t* next, int32_t* hist) {
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, buckets = p.experts + 1;
   int32_t* mine = hist + warp * buckets;
-  for (int i = i0 + lane; i < i1; i += 32) {
-    const int id = p.ids[base + i];
-    atomicAdd(&mine[id < 0 ? p.experts : id], 1);
+  const auto id_of = [&](int step) {
+    const int i = w.i0 + 32 * step + lane;
+    return step == 0 ? w.id[0] : step == 1 ? w.id[1] : i < w.i1 ? p.ids[w.base + i] : -1;
+  };
+  const int steps = (w.i1 - w.i0 + 31) / 32;
+  for (int s = 0; s < steps; ++s) {
+    const int id = id_of(s);
+    if (w.i0 + 32 * s + lane < w.i1) atomicAdd(&mine[id < 0 ? p.experts : id], 1);
   }
   __syncthreads();
   for (int b = threadIdx.x; b < buckets; b += blockDim.x) {
@@ -336,22 +360,23 @@ __device__ __forceinline__ void place_pairs(const RouteParams& p, int t0, int t1
     for (int w0 = 0; w0 < kWarps; w0 += 8) {
       int32_t n[8];
 #pragma unroll
-      for (int w = 0; w < 8; ++w) n[w] = hist[(w0 + w) * buckets + b];
+      for (int v = 0; v < 8; ++v) n[v] = hist[(w0 + v) * buckets + b];
 #pragma unroll
-      for (int w = 0; w < 8; ++w) {
-        hist[(w0 + w) * buckets + b] = at;
-        at += n[w];
+      for (int v = 0; v < 8; ++v) {
+        hist[(w0 + v) * buckets + b] = at;
+        at += n[v];
       }
     }
   }
   __syncthreads();
-  for (int i = i0; i < i1; i += 32) {
-    const bool in = i + lane < i1;
-    const int id = in ? p.ids[base + i + lane] : -1;
+  for (int s = 0; s < steps; ++s) {
+    const int i = w.i0 + 32 * s + lane;
+    const bool in = i < w.i1;
+    const int id = id_of(s);
     const int b = !in ? buckets : id < 0 ? p.experts : id;
     const uint32_t same = __match_any_sync(0xffffffffu, b);
     const int rank = __popc(same & ((1u << lane) - 1));
-    if (in) p.rows[mine[b] + rank] = id < 0 ? -1 : static_cast<int32_t>(base) + i + lane;
+    if (in) p.rows[mine[b] + rank] = id < 0 ? -1 : static_cast<int32_t>(w.base) + i;
     __syncwarp();
     if (in && rank == 0) mine[b] += __popc(same);
     __syncwarp();
@@ -389,9 +414,12 @@ __global__ void __launch_bounds__(32 * route_warps(kPer), 1)
   }
   // one CTA: its counts are the totals
   __shared__ int32_t warp_sums[kWarps];
+  int32_t* hist = count + p.experts + 1;
+  for (int i = threadIdx.x; i < kWarps * (p.experts + 1); i += blockDim.x) hist[i] = 0;
+  const WarpPairs pairs = warp_pairs<kWarps>(p, t0, t1);
   exclusive_scan(count, p.experts, warp_sums);
   for (int i = threadIdx.x; i <= p.experts; i += blockDim.x) p.offsets[i] = count[i];
-  place_pairs<kWarps>(p, t0, t1, count, count + p.experts + 1);
+  place_pairs<kWarps>(p, pairs, count, hist);
 }
 
 // Every CTA adds up, per bucket, the counts of all CTAs and of those before it (each thread four
@@ -404,11 +432,13 @@ __global__ void __launch_bounds__(32 * kPlanWarps)
   int32_t* next = smem;          // [row] totals, then places
   int32_t* before = next + row;  // [row] pairs of the CTAs before this one
   int32_t* hist = before + row;  // [kPlanWarps][buckets]
-  for (int i = threadIdx.x; i < 2 * row; i += blockDim.x) next[i] = 0;
+  for (int i = threadIdx.x; i < 2 * row + kPlanWarps * buckets; i += blockDim.x) next[i] = 0;
   __syncthreads();
   grid_dep_launch();  // (what follows waits for this grid's end before it reads the plan)
   const int runs = blockDim.x / quads, run = threadIdx.x / quads, quad = threadIdx.x % quads;
+  const int t0 = blockIdx.x * p.cta_tokens, t1 = min(p.tokens, t0 + p.cta_tokens);
   grid_dep_wait();
+  const WarpPairs pairs = warp_pairs<kPlanWarps>(p, t0, t1);
   if (run < runs) {
     int4 total = make_int4(0, 0, 0, 0), prior = total;
     const int4* c = reinterpret_cast<const int4*>(p.counts) + quad;
@@ -435,8 +465,7 @@ __global__ void __launch_bounds__(32 * kPlanWarps)
     next[threadIdx.x] += before[threadIdx.x];
   }
   __syncthreads();
-  const int t0 = blockIdx.x * p.cta_tokens, t1 = min(p.tokens, t0 + p.cta_tokens);
-  place_pairs<kPlanWarps>(p, t0, t1, next, hist);
+  place_pairs<kPlanWarps>(p, pairs, next, hist);
 }
 
 // With no token at all every expert's run is empty.
