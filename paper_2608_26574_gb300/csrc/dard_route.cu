@@ -2,14 +2,19 @@
 // plan (the (token, slot) pairs sorted by expert) that dard_experts reads on the device.
 //
 // route_topk, one warp per token: lane l holds experts l, l + 32, ... in registers, as keys whose
-// unsigned order is the order of the choice (see choose()). The largest call (38912 x 256 logits,
-// 40 MB) is bound by the instructions of the scores and the choice, not by HBM.
+// unsigned order is the order of the choice (see choose()). It is bound by instructions, not by
+// HBM: 38912 x 256 fp32 logits (40 MB, 6 us of HBM) with a bias, 4 of 8 groups and 8 experts per token
+// take 42 us, of which the scores and their order are 23, the groups 9 and seven more
+// slots 9. So the work per expert is kept short: eight experts per lane, whose scores stay in
+// registers, and no division before the choice where softmax needs none.
 //
 // The plan is a stable counting sort. A CTA owns a run of consecutive tokens; route_topk
 // counts its pairs per expert, and plan_scatter (chained by programmatic dependent launch)
 // adds up the counts of the CTAs before it and gives every pair its place. Counts are integers
-// and places follow from them, so the plan does not depend on the order of execution. Few
-// tokens fit one CTA, which then writes the plan itself, in one launch.
+// and places follow from them, so the plan does not depend on the order of execution. plan_scatter
+// takes 10 us there: the sums of 152 CTAs' counts, 14 loads in flight, then the places in shared
+// memory, each step waiting for the one before. Few tokens fit one CTA, which then writes the plan
+// itself, in one launch.
 #include <cuda_bf16.h>
 
 #include <algorithm>
@@ -25,7 +30,9 @@ namespace dard {
 namespace {
 
 constexpr int kPlanWarps = 32;                 // plan_scatter
-constexpr int kOneCtaTokens = 64;              // one CTA routes and plans up to this many
+// One CTA routes and plans up to this many tokens. Beyond, more CTAs and a second launch
+// are faster (256 experts: 64 tokens 12.5 against 14.5 us in one CTA, 128 tokens 12.6 against 20.8).
+constexpr int kOneCtaTokens = 32;
 constexpr uint32_t kNone = 0x007fffffu;        // key of -inf: an expert that cannot be chosen
 
 // Ints of a CTA's counts in the workspace: 16-byte rows.
@@ -113,7 +120,8 @@ __device__ int choose_exactly(uint32_t (&key)[kPer], int top_k, int lane) {
   return my_id;
 }
 
-// The same, mostly for half the instructions. A key's low bits give way to kPer - 1 - j, each lane
+// The same for fewer instructions where several slots repay the lists (38912 x 256, 8 slots: 42.0
+// us against 47.9; 1 slot 22.8 against 19.8, so up to two are chosen above). A key's low bits give way to kPer - 1 - j, each lane
 // sorts its keys once, and a slot is the largest head of the lanes' lists (the lowest lane that
 // reaches it) popped. Equal keys come out by rising j, then lane: by rising expert, as they
 // should. Keys that differ in the replaced bits alone could come out in the wrong order; they
@@ -121,6 +129,7 @@ __device__ int choose_exactly(uint32_t (&key)[kPer], int top_k, int lane) {
 template <int kPer>
 __device__ __forceinline__ int choose(uint32_t (&key)[kPer], int top_k, int lane) {
   constexpr uint32_t kLow = kPer - 1;
+  if (top_k <= 2) return choose_exactly<kPer>(key, top_k, lane);
   uint32_t list[kPer];
 #pragma unroll
   for (int j = 0; j < kPer; ++j) list[j] = (key[j] & ~kLow) | (kLow - j);
