@@ -121,14 +121,15 @@ __device__ int choose_exactly(uint32_t (&key)[kPer], int top_k, int lane) {
 }
 
 // The same for fewer instructions where several slots repay the lists (38912 x 256, 8 slots: 42.0
-// us against 47.9; 1 slot 22.8 against 19.8, so up to two are chosen above). A key's low bits give way to kPer - 1 - j, each lane
-// sorts its keys once, and a slot is the largest head of the lanes' lists (the lowest lane that
-// reaches it) popped. Equal keys come out by rising j, then lane: by rising expert, as they
-// should. Keys that differ in the replaced bits alone could come out in the wrong order; they
-// follow one another then, which is looked at, and the token is done again exactly.
+// us against 47.9; 1 slot 22.8 against 19.8, so up to two are chosen above). A key's low bits
+// give way to kLow - j, each lane sorts its keys once, and a slot is the largest head of the
+// lanes' lists (the lowest lane that reaches it) popped. Equal keys come out by rising j, then
+// lane: by rising expert, as they should. Keys that differ in the replaced bits alone could
+// come out in the wrong order; they follow one another then, which is looked at, and the token
+// is done again exactly.
 template <int kPer>
 __device__ __forceinline__ int choose(uint32_t (&key)[kPer], int top_k, int lane) {
-  constexpr uint32_t kLow = kPer - 1;
+  constexpr uint32_t kLow = kPer <= 1 ? 0 : kPer <= 2 ? 1 : kPer <= 4 ? 3 : kPer <= 8 ? 7 : 15;
   if (top_k <= 2) return choose_exactly<kPer>(key, top_k, lane);
   uint32_t list[kPer];
 #pragma unroll
@@ -528,11 +529,24 @@ cudaError_t launch_typed(const RouteParams& p, cudaStream_t s) {
 
 template <typename T>
 cudaError_t launch_route(const RouteParams& p, cudaStream_t s) {
-  if (p.experts <= 32) return launch_typed<T, 1>(p, s);
-  if (p.experts <= 64) return launch_typed<T, 2>(p, s);
-  if (p.experts <= 128) return launch_typed<T, 4>(p, s);
-  if (p.experts <= 256) return launch_typed<T, 8>(p, s);
-  return launch_typed<T, 16>(p, s);
+  // Experts per lane: empty ones cost as much as others (38912 tokens, 6 of 160: five per lane
+  // 43.5 us, eight
+  // 51.5; 5121 tokens: 16.6, 18.6; 20000 tokens, 8 of 384: twelve 60.5, sixteen 72.2).
+  switch ((p.experts + 31) / 32) {
+    case 1: return launch_typed<T, 1>(p, s);
+    case 2: return launch_typed<T, 2>(p, s);
+    case 3: return launch_typed<T, 3>(p, s);
+    case 4: return launch_typed<T, 4>(p, s);
+    case 5: return launch_typed<T, 5>(p, s);
+    case 6: return launch_typed<T, 6>(p, s);
+    case 7: return launch_typed<T, 7>(p, s);
+    case 8: return launch_typed<T, 8>(p, s);
+    case 9:
+    case 10:
+    case 11:
+    case 12: return launch_typed<T, 12>(p, s);
+    default: return launch_typed<T, 16>(p, s);
+  }
 }
 
 bool sizes_ok(int64_t tokens, int64_t experts, int64_t top_k) {

@@ -319,6 +319,26 @@ def test_route_groups_and_bias(scoring, n, groups, top_groups, k):
     _check_route(logits, k, _route(logits, "f32", k, bias=bias, **kw), bias=bias, **kw)
 
 
+@pytest.mark.parametrize("n", [31, 40, 90, 128, 150, 190, 200, 256, 270, 380, 400])
+@pytest.mark.parametrize("k", [1, 2, 3, 9])
+def test_route_expert_counts(n, k):
+    """Every number of experts per lane, with ties."""
+    for t in (31, 70):
+        logits = _grid_logits(t, n, t + n + k)
+        _check_route(logits, k, _route(logits, "f32", k))
+
+
+@pytest.mark.parametrize("n", [20, 60, 100, 160, 256, 300, 512])
+def test_route_choices_one_unit_apart(n):
+    """Scores of exactly a half plus a bias of whole units in the last place of fp32: choices that
+    differ in their last bits alone come out in their order, equal ones by expert."""
+    k, t = min(n, 32), 40
+    for spread in (n, n // 4):
+        units = np.random.default_rng(n).integers(0, spread, n)
+        ids, *_ = _route(np.zeros((t, n)), "f32", k, scoring=B.ROUTE_SIGMOID, bias=units * 2.0 ** -24)
+        assert ids.tolist() == [np.argsort(-units, kind="stable")[:k].tolist()] * t
+
+
 @pytest.mark.parametrize("t", [12, 200])
 def test_route_masked_and_invalid_rows(t):
     """Experts switched off, tokens with fewer experts than slots, tokens with none, and tokens
