@@ -940,19 +940,33 @@ __global__ void __launch_bounds__(Shape<kVariant>::kThreads, Shape<kVariant>::kC
 }
 
 // x (and its scales) in the plan's order, every expert's rows from a row tile's start: one warp per
-// pair of the plan.
+// pair of the plan. The first pair's row is on its way while the plan is read.
 template <bool kMx>
 __global__ void __launch_bounds__(256) gather_rows(const __grid_constant__ ExpertsParams p) {
   grid_dep_wait();  // the call's first launch (see product)
   grid_dep_launch();
   __shared__ int32_t first_row[DARD_MAX_EXPERTS + 1], first_tile[DARD_MAX_EXPERTS + 1],
       first_unit[DARD_MAX_EXPERTS + 1];
-  read_plan<1>(p, first_row, first_tile, first_unit);
-  __syncthreads();
   const int lane = threadIdx.x & 31;
   const int64_t row_bytes = static_cast<int64_t>(p.dim) * (kMx ? 1 : 2);
-  const int scale_tiles = (p.dim + 127) / 128;
-  for (int i = blockIdx.x * 8 + (threadIdx.x >> 5); i < p.pairs; i += gridDim.x * 8) {
+  const int n = static_cast<int>(row_bytes / 16), scale_tiles = (p.dim + 127) / 128;
+  const auto token_of = [&](int i) {
+    const int pair = i < p.pairs ? p.rows[i] : -1;
+    return pair >= 0 && pair < p.pairs ? static_cast<int64_t>(pair / p.top_k) : -1;
+  };
+  uint4 v[4];
+  const auto load = [&](int64_t token, int c) {
+    const uint4* src = reinterpret_cast<const uint4*>(static_cast<const char*>(p.x) + token * p.x_stride_bytes);
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+      if (c + 32 * j < n) v[j] = __ldg(src + c + 32 * j);
+  };
+  int i = blockIdx.x * 8 + (threadIdx.x >> 5);
+  int64_t token = token_of(i);
+  if (token >= 0) load(token, lane);
+  read_plan<1>(p, first_row, first_tile, first_unit);
+  __syncthreads();
+  while (i < p.pairs) {
     int lo = 0, hi = p.experts;  // first_row[lo] <= i < first_row[hi]
     while (hi - lo > 1) {
       const int mid = (lo + hi) >> 1;
@@ -960,28 +974,25 @@ __global__ void __launch_bounds__(256) gather_rows(const __grid_constant__ Exper
       else hi = mid;
     }
     const int at = i - first_row[lo], tile = first_tile[lo] + at / kTileM;
-    if (at < 0 || i >= first_row[lo + 1] || tile >= first_tile[lo + 1]) continue;
-    const int pair = p.rows[i];
-    if (pair < 0 || pair >= p.pairs) continue;
-    const int64_t token = pair / p.top_k, row = static_cast<int64_t>(tile) * kTileM + at % kTileM;
-    const uint4* src = reinterpret_cast<const uint4*>(static_cast<const char*>(p.x) + token * p.x_stride_bytes);
-    uint4* dst = reinterpret_cast<uint4*>(p.xg + row * row_bytes);
-    const int n = static_cast<int>(row_bytes / 16);
-    for (int c = lane; c < n; c += 128) {
-      uint4 v[4];
+    if (token >= 0 && at >= 0 && i < first_row[lo + 1] && tile < first_tile[lo + 1]) {
+      const int64_t row = static_cast<int64_t>(tile) * kTileM + at % kTileM;
+      uint4* dst = reinterpret_cast<uint4*>(p.xg + row * row_bytes);
+      for (int c = lane; c < n; c += 128) {
+        if (c != lane) load(token, c);
 #pragma unroll
-      for (int j = 0; j < 4; ++j)
-        if (c + 32 * j < n) v[j] = __ldg(src + c + 32 * j);
-#pragma unroll
-      for (int j = 0; j < 4; ++j)
-        if (c + 32 * j < n) dst[c + 32 * j] = v[j];
+        for (int j = 0; j < 4; ++j)
+          if (c + 32 * j < n) dst[c + 32 * j] = v[j];
+      }
+      if (kMx) {
+        const uint32_t* sc = reinterpret_cast<const uint32_t*>(p.x_scale + token * p.x_scale_stride);
+        for (int c = lane; c < scale_tiles; c += 32)
+          *reinterpret_cast<uint32_t*>(p.xg_scale + (static_cast<int64_t>(tile) * scale_tiles + c) * kMxTileBytes +
+                                       mx_tile_byte(at % kTileM, 0)) = __ldg(sc + c);
+      }
     }
-    if (kMx) {
-      const uint32_t* sc = reinterpret_cast<const uint32_t*>(p.x_scale + token * p.x_scale_stride);
-      for (int c = lane; c < scale_tiles; c += 32)
-        *reinterpret_cast<uint32_t*>(p.xg_scale + (static_cast<int64_t>(tile) * scale_tiles + c) * kMxTileBytes +
-                                     mx_tile_byte(at % kTileM, 0)) = __ldg(sc + c);
-    }
+    i += gridDim.x * 8;
+    token = token_of(i);
+    if (token >= 0) load(token, lane);
   }
 }
 
