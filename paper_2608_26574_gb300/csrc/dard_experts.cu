@@ -124,6 +124,7 @@ struct ExpertsParams {
   int32_t k_stages;             // stages over k_elems
   int32_t splits, split_stages; // phase 2: the reduction in `splits` runs of split_stages
   int32_t max_row_tiles;        // rows of the workspace / 128
+  int32_t gather_shift;         // gather_rows: 1 << gather_shift warps per pair
   int32_t y_f32;
   int32_t direct;               // phase 2 writes y itself (top_k 1, one split)
   int32_t test_drop;            // test hook: the stage use whose B copy is never issued
@@ -228,6 +229,14 @@ __device__ __forceinline__ bool elect_one() {
 template <int kPending>
 __device__ __forceinline__ void cp_async_wait_group() {
   asm volatile("cp.async.wait_group %0;" ::"n"(kPending) : "memory");
+}
+// 16 bytes that no one writes, read here (a plain load may be moved down to where it is used).
+__device__ __forceinline__ uint4 load16_here(const uint4* p) {
+  uint4 v;
+  asm volatile("ld.global.nc.v4.u32 {%0, %1, %2, %3}, [%4];"
+               : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w)
+               : "l"(p));
+  return v;
 }
 // 32 bytes to a 32-byte aligned address.
 __device__ __forceinline__ void store32(void* p, const uint32_t (&v)[8]) {
@@ -939,8 +948,8 @@ __global__ void __launch_bounds__(Shape<kVariant>::kThreads, Shape<kVariant>::kC
   }
 }
 
-// x (and its scales) in the plan's order, every expert's rows from a row tile's start: one warp per
-// pair of the plan. The first pair's row is on its way while the plan is read.
+// x (and its scales) in the plan's order, every expert's rows from a row tile's start: one or
+// a few warps per pair of the plan. The first pair's row is on its way while the plan is read.
 template <bool kMx>
 __global__ void __launch_bounds__(256) gather_rows(const __grid_constant__ ExpertsParams p) {
   grid_dep_wait();  // the call's first launch (see product)
@@ -959,11 +968,13 @@ __global__ void __launch_bounds__(256) gather_rows(const __grid_constant__ Exper
     const uint4* src = reinterpret_cast<const uint4*>(static_cast<const char*>(p.x) + token * p.x_stride_bytes);
 #pragma unroll
     for (int j = 0; j < 4; ++j)
-      if (c + 32 * j < n) v[j] = __ldg(src + c + 32 * j);
+      if (c + 32 * j < n) v[j] = load16_here(src + c + 32 * j);
   };
-  int i = blockIdx.x * 8 + (threadIdx.x >> 5);
+  const int warp = blockIdx.x * 8 + (threadIdx.x >> 5), parts = 1 << p.gather_shift;
+  int i = warp >> p.gather_shift;
+  const int part = warp & (parts - 1), c0 = 128 * part + lane;  // this warp's 16 bytes: c0, c0 + 32, ..
   int64_t token = token_of(i);
-  if (token >= 0) load(token, lane);
+  if (token >= 0) load(token, c0);
   read_plan<1>(p, first_row, first_tile, first_unit);
   __syncthreads();
   while (i < p.pairs) {
@@ -977,22 +988,22 @@ __global__ void __launch_bounds__(256) gather_rows(const __grid_constant__ Exper
     if (token >= 0 && at >= 0 && i < first_row[lo + 1] && tile < first_tile[lo + 1]) {
       const int64_t row = static_cast<int64_t>(tile) * kTileM + at % kTileM;
       uint4* dst = reinterpret_cast<uint4*>(p.xg + row * row_bytes);
-      for (int c = lane; c < n; c += 128) {
-        if (c != lane) load(token, c);
+      for (int c = c0; c < n; c += 128 * parts) {
+        if (c != c0) load(token, c);
 #pragma unroll
         for (int j = 0; j < 4; ++j)
           if (c + 32 * j < n) dst[c + 32 * j] = v[j];
       }
-      if (kMx) {
+      if (kMx && part == 0) {
         const uint32_t* sc = reinterpret_cast<const uint32_t*>(p.x_scale + token * p.x_scale_stride);
         for (int c = lane; c < scale_tiles; c += 32)
           *reinterpret_cast<uint32_t*>(p.xg_scale + (static_cast<int64_t>(tile) * scale_tiles + c) * kMxTileBytes +
                                        mx_tile_byte(at % kTileM, 0)) = __ldg(sc + c);
       }
     }
-    i += gridDim.x * 8;
+    i += gridDim.x * 8 >> p.gather_shift;
     token = token_of(i);
-    if (token >= 0) load(token, lane);
+    if (token >= 0) load(token, c0);
   }
 }
 
@@ -1104,7 +1115,7 @@ struct Plan {
 // experts of 2048 x 1024: 1 token 22.6 / 23.1 us, 8 57 / 66, 32 85 / 87). Else pairs of CTAs, unless their
 // tiles (their count, over the row tiles that the call can have) are fewer than the pairs of SMs,
 // or than half of those where the experts have full row tiles on average: then single ones. (800
-// rows of one expert, phase 2 of 4096 x 12288, 64 tiles: 115 against 121 us for the call; 200 rows
+// rows of one expert, phase 2 of 4096 x 12288, 64 tiles: 109 against 118 us for the call; 200 rows
 // of 8 experts, 1536 x 768, 48 and 48 tiles: 19.0 against 16.5 us.) Where even single tiles leave
 // SMs idle in phase 2 (few rows, a long reduction), the reduction is split, into runs of at least
 // four stages (one expert of 4096 x 12288: 1 row 41.5 us, whole 51.1; 100 rows 57, whole 74).
@@ -1260,8 +1271,14 @@ dard_status dard_experts(const dard_experts_args* a, void* stream) {
     e = cudaErrorInvalidValue;
   if (!pair1) ma = mb0;  // not used
   if (e == cudaSuccess && pair1) {
-    const Launch l(dim3(static_cast<unsigned>(std::min<int64_t>((q.pairs + 7) / 8, 8ll * sm_count()))),
-                   256, 0, s);
+    // Few pairs: several warps share a row of more than 2 KB, so that it is read in one go (800
+    // rows of 4 KB: the call takes 106.4 us, with a warp per row 110.5).
+    const int64_t most = 64ll * sm_count();
+    while (p.gather_shift < 3 && (2048ull << p.gather_shift) < drow &&
+           q.pairs << (p.gather_shift + 1) <= most)
+      ++p.gather_shift;
+    const int64_t warps = std::min(q.pairs << p.gather_shift, most);
+    const Launch l(dim3(static_cast<unsigned>((warps + 7) / 8)), 256, 0, s);
     e = mx ? cudaLaunchKernelEx(&l.cfg, gather_rows<true>, p)
            : cudaLaunchKernelEx(&l.cfg, gather_rows<false>, p);
   }
