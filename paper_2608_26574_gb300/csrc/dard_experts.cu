@@ -40,8 +40,9 @@
 //
 // What bounds it, on GB300: pairs, 3.27 PFLOP/s in MXFP8 at 4096 x 4096 x 12288, the tensor pipe
 // and shared memory together (with half of the weights' bytes left out it is 10 % faster, without
-// its stores 7 %); 8192 tokens x 8 of 64 experts of 4096 x 2048 1.46-1.59 ms, of which gather_rows takes
-// 70 us and combine 257 us, both HBM's bytes. Few: the weights' bytes (32 tokens x 8 of 64 of
+// its stores 7 %); 8192 tokens x 8 of 64 experts of 4096 x 2048 1.46-1.60 ms (the clock
+// falls to 1600-1800 MHz at the power limit), of which gather_rows takes 75 us and combine 255 us, both
+// HBM's bytes. Few: the weights' bytes (32 tokens x 8 of 64 of
 // 2048 x 1024: 403 MB in 85 us; with no MMA at all 80) and for one token the chain of latencies
 // (22.7 us; its 52 MB alone would take 7.6).
 //
@@ -514,11 +515,16 @@ __global__ void __launch_bounds__(Shape<kVariant>::kThreads, Shape<kVariant>::kC
       const uint8_t* sf_b0 = p.scale_b[0] + at_b;
       const uint8_t* sf_b1 = kPhase == 1 ? p.scale_b[1] + at_b : sf_b0 + step_b;
       const uint8_t* sf_a = p.a_scale + t.row_tile * step_b;
+      // A pair's CTA without rows: zeros (a box outside the map) into each stage, once a tile.
+      // Power bounds long runs of the largest calls (the clock falls from 2070 to 1600-1900 MHz),
+      // and zeros take less of it than another tile's rows: 800 rows of 4096 x 12288, call after
+      // call, 115.0 us against 116.8.
+      const auto no_rows = [&](int k) { return kPair && boxes_a == 0 && k - k0 < kStages; };
       const auto load_b = [&](int k, int b) {
         uint8_t* sb = base + b * kStageBytes + S::kBytesA;
         uint8_t* ss = s_scale + b * kScaleBytes;
         uint64_t* bar = &ctl.full[b];
-        mbar_arrive_expect_tx(bar, bytes);
+        mbar_arrive_expect_tx(bar, bytes + (no_rows(k) ? kBoxA * kStageK : 0));
         if (use != p.test_drop) {
           if constexpr (kPhase == 1 && !kPair) {  // 64 rows of each matrix
             tma_load_3d(sb, &map_b0, bar, k * kElems, n0, t.e);
@@ -536,6 +542,8 @@ __global__ void __launch_bounds__(Shape<kVariant>::kThreads, Shape<kVariant>::kC
       };
       const auto load_a = [&](int k, int b) {
         uint64_t* bar = &ctl.full[b];
+        if (no_rows(k))
+          tma_load_2d(base + b * kStageBytes, &map_a, bar, k * kElems, p.max_row_tiles * kTileM);
         for (int i = 0; i < boxes_a; ++i)
           tma_load_2d(base + b * kStageBytes + i * kBoxA * kStageK, &map_a, bar, k * kElems,
                       t.row_tile * kTileM + i * kBoxA);
