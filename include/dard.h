@@ -452,7 +452,8 @@ dard_status dard_route(const dard_route_args* args, void* stream);
  * in tiles) or bf16 (dtype DARD_BF16, the scales unused). Products and sums are fp32 on the
  * tcgen05 tensor cores; the block scales are applied by the matrix instruction. The products of
  * one token's experts are added in slot order, so that equal calls give equal bits.
- * ids, weights, offsets and rows are what dard_route writes. */
+ * ids, weights, offsets and rows are what dard_route writes, or a caller's own of that form (in
+ * which a token may name an expert in several slots). */
 #define DARD_MXFP8 2         /* a dtype of dard_experts_args only                          */
 typedef struct {
   const void* x;             /* device [tokens, dim], row stride x_stride                  */

@@ -85,8 +85,9 @@ struct Shape {
   static constexpr bool kPair = kVariant == kPairs;
   static constexpr int kCtas = kPair ? 2 : 1;  // that share an MMA
   static constexpr int kStages = kPair ? 6 : kVariant == kSingle ? 3 : 5;
-  // Rows of A that a stage holds. The MMA reads 128: what lies behind (this stage's B) gives rows
-  // of the accumulator that nobody reads.
+  // Rows of A that a stage holds, and of a row tile. The MMA reads 128: what lies behind (this
+  // stage's B) gives rows of the accumulator that nobody reads. (An expert has more rows than
+  // there are tokens where tokens name it in several slots: it then has several tiles.)
   static constexpr int kRowsA = kVariant == kFew ? kFewTokens : kTileM;
   static constexpr int kBoxA = kPair ? kTileM : 32;  // rows per copy
   static constexpr uint32_t kBytesA = kRowsA * kStageK, kStageBytes = kBytesA + kBytesB;
@@ -124,7 +125,7 @@ struct ExpertsParams {
   int32_t n_tiles;              // tiles over n_elems
   int32_t k_stages;             // stages over k_elems
   int32_t splits, split_stages; // phase 2: the reduction in `splits` runs of split_stages
-  int32_t max_row_tiles;        // rows of the workspace / 128
+  int32_t max_row_tiles;        // rows of the workspace / kTileM
   int32_t gather_shift;         // gather_rows: 1 << gather_shift warps per pair
   int32_t y_f32;
   int32_t direct;               // phase 2 writes y itself (top_k 1, one split)
@@ -264,7 +265,7 @@ struct __align__(16) Ctl {
   int32_t abort;
   int32_t last;      // few: this CTA's tile was its columns' last
   int32_t first_row[DARD_MAX_EXPERTS + 1];   // offsets, clamped to [0, pairs]
-  int32_t first_tile[DARD_MAX_EXPERTS + 1];  // row tiles (128 rows) of the experts before
+  int32_t first_tile[DARD_MAX_EXPERTS + 1];  // row tiles of the experts before
   // (pairs: after this, the same in units of two row tiles)
 };
 
@@ -276,18 +277,19 @@ constexpr size_t smem_bytes() {
 }
 
 // A CTA's part of one tile: rows [row, row + count) (count <= 0: none) of expert e, in row tile
-// row_tile of h; column tile n, reduction split.
+// row_tile of h (kTileM rows apart, whatever the rows of a tile); column tile n, reduction split.
 struct Tile {
   int e, row, count, row_tile, n, split;
 };
 
 // Tile `w` of the call. Within an expert, a group of row units takes each column tile in turn,
 // so that CTAs that run together share weights and rows in L2. `e` walks forward.
-template <bool kPair>
+template <int kVariant>
 __device__ __forceinline__ bool get_tile(const ExpertsParams& p, const Ctl& c,
                                          const int32_t* first_unit, int rank, int64_t w, int& e,
                                          Tile& t) {
-  constexpr int kUnitTiles = kPair ? 2 : 1, kGroup = kGroupM / kUnitTiles;
+  constexpr int kUnitTiles = Shape<kVariant>::kCtas, kGroup = kGroupM / kUnitTiles;
+  constexpr int kRows = Shape<kVariant>::kRowsA;
   const int per_unit = p.n_tiles * p.splits;
   if (w >= static_cast<int64_t>(first_unit[p.experts]) * per_unit) return false;
   while (w >= static_cast<int64_t>(first_unit[e + 1]) * per_unit) ++e;
@@ -301,17 +303,17 @@ __device__ __forceinline__ bool get_tile(const ExpertsParams& p, const Ctl& c,
   t.e = e;
   t.n = col % p.n_tiles;
   t.split = col / p.n_tiles;
-  t.row = c.first_row[e] + m * kTileM;
+  t.row = c.first_row[e] + m * kRows;
   t.row_tile = c.first_tile[e] + m;
   // (a plan cut short at the workspace's end may leave a pair's second row tile outside)
-  t.count = t.row_tile < c.first_tile[e + 1] ? min(kTileM, c.first_row[e + 1] - t.row) : 0;
+  t.count = t.row_tile < c.first_tile[e + 1] ? min(kRows, c.first_row[e + 1] - t.row) : 0;
   return true;
 }
 
-// The plan's offsets, clamped to [0, pairs], and by expert the row tiles (128 rows) and the units of
+// The plan's offsets, clamped to [0, pairs], and by expert the row tiles (kRows rows) and the units of
 // kCtas row tiles before it, by the whole CTA. A plan that is none (offsets that fall) never
 // reaches past the workspace. Ends without a barrier.
-template <int kCtas>
+template <int kCtas, int kRows>
 __device__ __forceinline__ void read_plan(const ExpertsParams& p, int32_t* first_row,
                                           int32_t* first_tile, int32_t* first_unit) {
   const int lane = threadIdx.x & 31;
@@ -323,7 +325,7 @@ __device__ __forceinline__ void read_plan(const ExpertsParams& p, int32_t* first
   for (int b = 0; b < p.experts; b += 32) {
     const int i = b + lane;
     const int n = i < p.experts ? max(first_row[i + 1] - first_row[i], 0) : 0;
-    int tiles = (n + kTileM - 1) / kTileM;
+    int tiles = (n + kRows - 1) / kRows;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
       const int y = __shfl_up_sync(0xffffffffu, tiles, o);
@@ -472,7 +474,7 @@ __global__ void __launch_bounds__(Shape<kVariant>::kThreads, Shape<kVariant>::kC
   grid_dep_launch();
   if (kVariant == kFew && kPhase == 1 && blockIdx.x == 0)
     for (int i = threadIdx.x; i < (p.dim + kTileB - 1) / kTileB; i += S::kThreads) p.arrived[i] = 0;
-  read_plan<kCtas>(p, ctl.first_row, ctl.first_tile, first_unit);
+  read_plan<kCtas, S::kRowsA>(p, ctl.first_row, ctl.first_tile, first_unit);
   tc_fence_before();
   if constexpr (kPair) cluster_sync();  // both CTAs' barriers exist, TMEM is allocated
   else __syncthreads();
@@ -502,7 +504,7 @@ __global__ void __launch_bounds__(Shape<kVariant>::kThreads, Shape<kVariant>::kC
     const bool issue = elect_one();
     bool waited = kGather;  // for the launch before this one, which writes the rows of A
     Ring ring;
-    for (int64_t w = first; ok && get_tile<kPair>(p, ctl, first_unit, rank, w, e, t); w += step) {
+    for (int64_t w = first; ok && get_tile<kVariant>(p, ctl, first_unit, rank, w, e, t); w += step) {
       const int boxes_a = kGather ? 0 : (max(t.count, 0) + kBoxA - 1) / kBoxA;
       const int k0 = t.split * split_stages, k1 = min(p.k_stages, k0 + split_stages);
       const int n0 = t.n * kCols;
@@ -599,7 +601,7 @@ __global__ void __launch_bounds__(Shape<kVariant>::kThreads, Shape<kVariant>::kC
       const uint64_t desc_s = scale_desc(smem_u32(s_scale));
       uint32_t sfa = tmem + S::kScaleCol;  // scales of two stages, 16 columns apart
       bool ready = false;                  // the stage at `ring` is known to be full
-      for (int64_t w = first; ok && get_tile<kPair>(p, ctl, first_unit, rank, w, e, t); w += step, ++tiles) {
+      for (int64_t w = first; ok && get_tile<kVariant>(p, ctl, first_unit, rank, w, e, t); w += step, ++tiles) {
         ok = tiles == 0 || warp_wait(&ctl.acc_free, (tiles - 1) & 1);
         if (!ok) break;
         tc_fence_after();
@@ -667,7 +669,7 @@ __global__ void __launch_bounds__(Shape<kVariant>::kThreads, Shape<kVariant>::kC
       bool ok = true;
       Tile t;
       Ring ring;
-      for (int64_t w = first; ok && get_tile<kPair>(p, ctl, first_unit, rank, w, e, t); w += step) {
+      for (int64_t w = first; ok && get_tile<kVariant>(p, ctl, first_unit, rank, w, e, t); w += step) {
         const int k0 = t.split * split_stages, k1 = min(p.k_stages, k0 + split_stages);
         for (int k = k0; k < k1; ++k) {
           ok = wait(&ctl.full[ring.b], ring.phase);
@@ -701,7 +703,7 @@ __global__ void __launch_bounds__(Shape<kVariant>::kThreads, Shape<kVariant>::kC
           oldest.next<kStages>();
         }
       };
-      for (int64_t w = first; ok && get_tile<kPair>(p, ctl, first_unit, rank, w, e, t); w += step) {
+      for (int64_t w = first; ok && get_tile<kVariant>(p, ctl, first_unit, rank, w, e, t); w += step) {
         int64_t from[kCopies];  // byte offset of the token's row; -1: no row
         const uint4* src[2] = {nullptr, nullptr};  // scales of rows g * kRows + lane (+ 32)
 #pragma unroll
@@ -806,7 +808,7 @@ __global__ void __launch_bounds__(Shape<kVariant>::kThreads, Shape<kVariant>::kC
         }
       }
     }
-    for (int64_t w = first; ok && get_tile<kPair>(p, ctl, first_unit, rank, w, e, t); w += step, ++tiles) {
+    for (int64_t w = first; ok && get_tile<kVariant>(p, ctl, first_unit, rank, w, e, t); w += step, ++tiles) {
       const bool in = r < t.count;
       int pair = 0;
       if (kPhase == 2) pair = in ? __ldg(p.rows + t.row + r) : -1;
@@ -983,7 +985,7 @@ __global__ void __launch_bounds__(256) gather_rows(const __grid_constant__ Exper
   const int part = warp & (parts - 1), c0 = 128 * part + lane;  // this warp's 16 bytes: c0, c0 + 32, ..
   int64_t token = token_of(i);
   if (token >= 0) load(token, c0);
-  read_plan<1>(p, first_row, first_tile, first_unit);
+  read_plan<1, kTileM>(p, first_row, first_tile, first_unit);
   __syncthreads();
   while (i < p.pairs) {
     int lo = 0, hi = p.experts;  // first_row[lo] <= i < first_row[hi]
@@ -1112,9 +1114,9 @@ constexpr size_t up256(size_t n) { return (n + 255) / 256 * 256; }
 
 // Sizes that follow from a call's sizes alone.
 struct Plan {
-  int64_t pairs, row_tiles;  // at most so many row tiles of 128 pairs
+  int64_t pairs, row_tiles;  // at most so many row tiles, whatever the plan
   int variant1, variant2;    // of each phase
-  int64_t tiles1, tiles2;    // at most so many tiles of each phase
+  int64_t tiles1, tiles2;    // tiles of each phase, at most (few: where a token's experts differ)
   int splits, split_stages;
   size_t arrived_bytes, h_bytes, h_scale_bytes, partial_bytes, xg_bytes, xg_scale_bytes;
   bool direct;  // phase 2 writes y itself
@@ -1125,7 +1127,7 @@ struct Plan {
   }
 };
 
-// Few tokens (no expert can have more rows): kFew, in both phases (against kSingle, 8 of 64
+// Few tokens (few rows per expert): kFew, in both phases (against kSingle, 8 of 64
 // experts of 2048 x 1024: 1 token 22.6 / 23.1 us, 8 57 / 66, 32 85 / 87). Else pairs of CTAs, unless their
 // tiles (their count, over the row tiles that the call can have) are fewer than the pairs of SMs,
 // or than half of those where the experts have full row tiles on average: then single ones. (800
@@ -1137,16 +1139,17 @@ Plan make_plan(int64_t tokens, int experts, int top_k, int dim, int hidden, bool
   Plan q = {};
   q.pairs = tokens * top_k;
   const int64_t used = std::min<int64_t>(experts, q.pairs);  // experts with rows, at most
-  q.row_tiles = q.pairs / kTileM + used;
+  const int64_t row_tiles = q.pairs / kTileM + used;  // where no tile is of kFew
   const int64_t row_pairs = q.pairs / (2 * kTileM) + used;
   const int64_t sms = sm_count();
   const auto columns = [](int n, int per) { return static_cast<int64_t>((n + per - 1) / per); };
   const bool few = tokens <= kFewTokens;
+  q.row_tiles = few ? used + (q.pairs - used) / Shape<kFew>::kRowsA : row_tiles;
   const int64_t enough = q.pairs >= kTileM * used ? sms / 4 : sms / 2;
   q.variant1 = few ? kFew : row_pairs * columns(hidden, 128) >= enough ? kPairs : kSingle;
   q.variant2 = few ? kFew : row_pairs * columns(dim, 256) >= enough ? kPairs : kSingle;
-  q.tiles1 = q.variant1 == kPairs ? row_pairs * columns(hidden, 128) : q.row_tiles * columns(hidden, 64);
-  q.tiles2 = q.variant2 == kPairs ? row_pairs * columns(dim, 256) : q.row_tiles * columns(dim, 128);
+  q.tiles1 = q.variant1 == kPairs ? row_pairs * columns(hidden, 128) : row_tiles * columns(hidden, 64);
+  q.tiles2 = q.variant2 == kPairs ? row_pairs * columns(dim, 256) : row_tiles * columns(dim, 128);
   const int stages = (hidden + (mx ? 127 : 63)) / (mx ? 128 : 64);
   int64_t splits = 1;
   if (q.variant2 != kPairs && q.tiles2 * 2 <= sms)
