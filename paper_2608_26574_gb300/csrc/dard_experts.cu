@@ -580,6 +580,9 @@ __global__ void __launch_bounds__(Shape<kVariant>::kThreads, Shape<kVariant>::kC
         ring.next<kStages>();
       }
     }
+    // Without a tile too: a launch ends after the one before it, which otherwise could still read
+    // the plan or write x's copy when the call seems over to what follows it.
+    if (!waited) grid_dep_wait();
     if (!ok) {
       if (lane == 0) give_up();
       // copies in flight land before shared memory is released: the last use of each stage
