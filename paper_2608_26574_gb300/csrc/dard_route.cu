@@ -320,7 +320,7 @@ __device__ __forceinline__ void exclusive_scan(int32_t* v, int n, int32_t* warp_
   __syncthreads();
 }
 
-// The pairs of tokens [t0, t1) as warp w of kWarps sees them: the w-th run of `per` pairs (a
+// The pairs of `count` tokens from t0 on as warp w of kWarps sees them: the w-th run of `per` pairs (a
 // multiple of 32). The ids of the first kHeld of 32 are held in registers, so that they can be
 // on their way while something else is done.
 constexpr int kHeld = 2;
@@ -330,11 +330,11 @@ struct WarpPairs {
   int id[kHeld];
 };
 template <int kWarps>
-__device__ __forceinline__ WarpPairs warp_pairs(const RouteParams& p, int t0, int t1) {
+__device__ __forceinline__ WarpPairs warp_pairs(const RouteParams& p, int t0, int count) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   WarpPairs w;
   w.base = static_cast<int64_t>(t0) * p.top_k;
-  const int pairs = (t1 - t0) * p.top_k;
+  const int pairs = count * p.top_k;
   const int per = ((pairs + kWarps - 1) / kWarps + 31) / 32 * 32;
   w.i0 = warp * per;
   w.i1 = min(pairs, w.i0 + per);
@@ -403,15 +403,15 @@ __global__ void __launch_bounds__(32 * route_warps(kPer), 1)
   float* choice = reinterpret_cast<float*>(smem);
   int32_t* count = smem + (p.top_groups < p.groups ? kWarps * p.experts : 0);
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  const int t0 = blockIdx.x * p.cta_tokens, t1 = min(p.tokens, t0 + p.cta_tokens);
+  const int t0 = blockIdx.x * p.cta_tokens, count_t = min(p.cta_tokens, p.tokens - t0);
   const bool plan = p.rows != nullptr;
   if (plan) {
     for (int i = threadIdx.x; i <= p.experts; i += blockDim.x) count[i] = 0;
     __syncthreads();
   }
   const LaneExperts<kPer> mine = lane_experts<kPer>(p, lane);
-  for (int t = t0 + warp; t < t1; t += kWarps) {
-    const int id = route_token<T, kPer>(p, mine, t, choice + warp * p.experts, lane);
+  for (int t = warp; t < count_t; t += kWarps) {
+    const int id = route_token<T, kPer>(p, mine, t0 + t, choice + warp * p.experts, lane);
     if (plan && lane < p.top_k) atomicAdd(&count[id < 0 ? p.experts : id], 1);
   }
   if (!plan) return;
@@ -426,7 +426,7 @@ __global__ void __launch_bounds__(32 * route_warps(kPer), 1)
   __shared__ int32_t warp_sums[kWarps];
   int32_t* hist = count + p.experts + 1;
   for (int i = threadIdx.x; i < kWarps * (p.experts + 1); i += blockDim.x) hist[i] = 0;
-  const WarpPairs pairs = warp_pairs<kWarps>(p, t0, t1);
+  const WarpPairs pairs = warp_pairs<kWarps>(p, t0, count_t);
   exclusive_scan(count, p.experts, warp_sums);
   for (int i = threadIdx.x; i <= p.experts; i += blockDim.x) p.offsets[i] = count[i];
   place_pairs<kWarps>(p, pairs, count, hist);
@@ -446,9 +446,9 @@ __global__ void __launch_bounds__(32 * kPlanWarps)
   __syncthreads();
   grid_dep_launch();  // (what follows waits for this grid's end before it reads the plan)
   const int runs = blockDim.x / quads, run = threadIdx.x / quads, quad = threadIdx.x % quads;
-  const int t0 = blockIdx.x * p.cta_tokens, t1 = min(p.tokens, t0 + p.cta_tokens);
+  const int t0 = blockIdx.x * p.cta_tokens, count_t = min(p.cta_tokens, p.tokens - t0);
   grid_dep_wait();
-  const WarpPairs pairs = warp_pairs<kPlanWarps>(p, t0, t1);
+  const WarpPairs pairs = warp_pairs<kPlanWarps>(p, t0, count_t);
   if (run < runs) {
     int4 total = make_int4(0, 0, 0, 0), prior = total;
     const int4* c = reinterpret_cast<const int4*>(p.counts) + quad;
@@ -483,12 +483,14 @@ __global__ void empty_plan(int32_t* offsets, int n) {
   for (int i = threadIdx.x; i < n; i += blockDim.x) offsets[i] = 0;
 }
 
+// (up to 2^31 - 1 tokens: no sum of two counts in 32 bits, here or in the kernels)
+int ceil_div(int64_t n, int d) { return static_cast<int>((n + d - 1) / d); }
+
 // Tokens per CTA: one CTA up to kOneCtaTokens; beyond, runs such that every SM gets one CTA of
 // each kernel, so that plan_scatter's sums over the CTAs before it stay short.
 int cta_tokens_for(int tokens) {
   if (tokens <= kOneCtaTokens) return std::max(tokens, 1);
-  const int sms = sm_count();
-  return std::max(32, (tokens + sms - 1) / sms);
+  return std::max(32, ceil_div(tokens, sm_count()));
 }
 
 template <typename T, int kPer>
@@ -564,7 +566,7 @@ extern "C" {
 size_t dard_route_workspace_size(int32_t tokens, int32_t experts, int32_t top_k) {
   if (!sizes_ok(tokens, experts, top_k)) return 0;
   const int per = cta_tokens_for(tokens);
-  const size_t ctas = (static_cast<size_t>(tokens) + per - 1) / per;
+  const size_t ctas = ceil_div(tokens, per);
   return ctas <= 1 ? 0 : ctas * count_row(experts) * 4;
 }
 
@@ -633,7 +635,7 @@ dard_status dard_route(const dard_route_args* a, void* stream) {
   p.scoring = a->scoring;
   p.renormalise = a->renormalise;
   p.cta_tokens = cta_tokens_for(a->tokens);
-  p.ctas = (a->tokens + p.cta_tokens - 1) / p.cta_tokens;
+  p.ctas = ceil_div(a->tokens, p.cta_tokens);
   p.scale = a->scale;
   if (e == cudaSuccess)
     e = a->dtype == DARD_BF16 ? launch_route<__nv_bfloat16>(p, s) : launch_route<float>(p, s);
