@@ -528,8 +528,8 @@ dard_status dard_mx_quantize(const dard_mx_args* a, void* stream) {
   if (!a) return report(DARD_ERR_NULL, "args is NULL");
   if (a->batch < 0 || a->rows < 0 || a->cols < 1 || a->cols % kMxBlock != 0)
     return report(DARD_ERR_SHAPE, "batch and rows must be >= 0, cols a positive multiple of 32");
-  if (a->rows > (1ll << 40) || a->batch * a->rows > (1ll << 40) ||
-      a->batch * a->rows * a->cols > (1ll << 40))
+  // (by division: the product of sizes such as these does not fit 64 bits)
+  if (a->batch > 0 && a->rows > (1ll << 40) / a->cols / a->batch)
     return report(DARD_ERR_SHAPE, "more than 2^40 elements");
   if (a->dtype != DARD_BF16 && a->dtype != DARD_F32)
     return report(DARD_ERR_VALUE, "dtype %d is neither DARD_F32 nor DARD_BF16", a->dtype);
