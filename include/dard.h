@@ -436,8 +436,8 @@ typedef struct {
   size_t workspace_bytes;
 } dard_route_args;
 
-/* Bytes of workspace a call with these sizes needs (0 where it needs none, or on invalid
- * sizes). */
+/* Bytes of workspace for a call with these sizes or fewer tokens (0 where none is needed, or on
+ * invalid sizes). */
 size_t dard_route_workspace_size(int32_t tokens, int32_t experts, int32_t top_k);
 
 /* One launch for few tokens or without the plan, else two. Errors: DARD_ERR_NULL, _SHAPE,

@@ -630,7 +630,8 @@ class RouteCall:
     Call it with logits [tokens, experts] (bf16 or fp32, contiguous rows), ``ids`` and
     ``weights`` [tokens, top_k], and, for the plan that ``ExpertsCall`` reads, ``offsets``
     [experts + 1] and ``rows`` [tokens * top_k]. The workspace holds
-    ``dard_route_workspace_size`` bytes for the most tokens of a call with a plan."""
+    ``dard_route_workspace_size`` bytes for the most tokens of a call with a plan, which are
+    enough for fewer tokens too."""
 
     def __init__(self, experts: int, top_k: int, scoring: int = ROUTE_SOFTMAX, bias=None,
                  groups: int = 1, top_groups: int = 1, renormalise: bool = True,

@@ -493,6 +493,11 @@ int cta_tokens_for(int tokens) {
   return std::max(32, ceil_div(tokens, sm_count()));
 }
 
+// The workspace of a plan that this many CTAs make.
+size_t counts_bytes(int ctas, int experts) {
+  return ctas <= 1 ? 0 : static_cast<size_t>(ctas) * count_row(experts) * 4;
+}
+
 template <typename T, int kPer>
 cudaError_t launch_typed(const RouteParams& p, cudaStream_t s) {
   const size_t buckets = static_cast<size_t>(p.experts) + 1;
@@ -564,10 +569,10 @@ using namespace dard;
 extern "C" {
 
 size_t dard_route_workspace_size(int32_t tokens, int32_t experts, int32_t top_k) {
-  if (!sizes_ok(tokens, experts, top_k)) return 0;
-  const int per = cta_tokens_for(tokens);
-  const size_t ctas = ceil_div(tokens, per);
-  return ctas <= 1 ? 0 : ctas * count_row(experts) * 4;
+  if (!sizes_ok(tokens, experts, top_k) || tokens <= kOneCtaTokens) return 0;
+  // The most CTAs of any count up to this one: past 32 tokens for each SM a CTA takes more, and
+  // there may be fewer CTAs than for fewer tokens.
+  return counts_bytes(std::min(ceil_div(tokens, 32), sm_count()), experts);
 }
 
 dard_status dard_route(const dard_route_args* a, void* stream) {
@@ -611,7 +616,8 @@ dard_status dard_route(const dard_route_args* a, void* stream) {
     return report(DARD_ERR_NULL, "logits, ids or weights is NULL");
   if (reinterpret_cast<uintptr_t>(a->logits) % (a->dtype == DARD_BF16 ? 2 : 4) != 0)
     return report(DARD_ERR_ALIGN, "logits is not a multiple of the element size");
-  const size_t need = a->rows ? dard_route_workspace_size(a->tokens, a->experts, a->top_k) : 0;
+  const int cta_tokens = cta_tokens_for(a->tokens), ctas = ceil_div(a->tokens, cta_tokens);
+  const size_t need = a->rows ? counts_bytes(ctas, a->experts) : 0;
   if (need > 0 && (!a->workspace || a->workspace_bytes < need))
     return report(DARD_ERR_WORKSPACE, "workspace of %zu bytes needed", need);
   if (need > 0 && reinterpret_cast<uintptr_t>(a->workspace) % 16 != 0)
@@ -634,8 +640,8 @@ dard_status dard_route(const dard_route_args* a, void* stream) {
   p.group_size = a->experts / a->groups;
   p.scoring = a->scoring;
   p.renormalise = a->renormalise;
-  p.cta_tokens = cta_tokens_for(a->tokens);
-  p.ctas = ceil_div(a->tokens, p.cta_tokens);
+  p.cta_tokens = cta_tokens;
+  p.ctas = ctas;
   p.scale = a->scale;
   if (e == cudaSuccess)
     e = a->dtype == DARD_BF16 ? launch_route<__nv_bfloat16>(p, s) : launch_route<float>(p, s);

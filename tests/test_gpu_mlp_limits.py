@@ -1,9 +1,11 @@
 """The experts' MLP operators at the ends of the sizes that include/dard.h accepts."""
 import math
 
+import numpy as np
 import pytest
 import torch
 
+from oracle import mlp_oracle as O
 from paper_2608_26574_gb300 import binding as B
 
 pytestmark = pytest.mark.gpu
@@ -39,3 +41,24 @@ def test_route_the_most_tokens():
         for i in off:
             want += want >= i
         assert torch.equal(rows[a:a + len(want)], want.to(torch.int32))
+
+
+def test_route_one_workspace_for_every_count_below():
+    """One RouteCall with the workspace of its most tokens, over counts on both sides of where a
+    CTA begins to take more than 32 of them."""
+    n, k, sms = 64, 4, torch.cuda.get_device_properties(0).multi_processor_count
+    most = 32 * sms + 1
+    ws = torch.empty(B.dard_route_workspace_size(most, n, k), dtype=torch.uint8, device=DEV)
+    call = B.RouteCall(n, k, workspace=ws)
+    g = torch.Generator(device=DEV).manual_seed(3)
+    logits = torch.rand(most, n, generator=g, device=DEV).argsort(1) / 8.0  # no two alike in a row
+    for t in (most, most - 1, most - 32, 33, 32, 1, 0):
+        ids = torch.empty(t, k, dtype=torch.int32, device=DEV)
+        weights = torch.empty(t, k, device=DEV)
+        offsets = torch.empty(n + 1, dtype=torch.int32, device=DEV)
+        rows = torch.empty(t * k, dtype=torch.int32, device=DEV)
+        call(logits[:t], ids, weights, offsets, rows)
+        assert torch.equal(ids, torch.topk(logits[:t], k).indices.to(torch.int32))
+        want = O.plan(ids.cpu().numpy(), n)
+        assert np.array_equal(offsets.cpu().numpy(), want[0])
+        assert np.array_equal(rows.cpu().numpy(), want[1])

@@ -4,7 +4,9 @@ import ctypes
 
 import pytest
 
-from .test_mlp_abi import SHAPE, _mx, _refuse, lib  # noqa: F401 (lib: a fixture)
+from paper_2608_26574_gb300 import binding as B
+
+from .test_mlp_abi import ALIGN, SHAPE, WORKSPACE, _mx, _refuse, _route, lib  # noqa: F401 (lib: a fixture)
 
 
 @pytest.mark.parametrize("batch,rows,cols", [
@@ -22,3 +24,19 @@ def test_quantize_of_nothing(lib, batch, rows, cols):  # noqa: F811
     a = _mx()
     a.batch, a.rows, a.cols, a.x_row_stride, a.scale_stride, a.x = batch, rows, cols, cols, cols, None
     assert lib.dard_mx_quantize(ctypes.byref(a), None) == 0
+
+
+@pytest.mark.parametrize("experts,top_k", [(1, 1), (64, 8), (256, 8), (512, 32)])
+def test_route_workspace_serves_every_smaller_count(lib, experts, top_k):  # noqa: F811
+    """A workspace for a token count is large enough for each count below it: the size never falls
+    as the count rises, and a call accepts it (it is refused with a byte less than it needs, and
+    with this much gets as far as the next check)."""
+    counts = [*range(0, 6000), *range(6000, 40000, 37), (1 << 31) // top_k - 1]
+    sizes = [B.dard_route_workspace_size(t, experts, top_k) for t in counts]
+    assert all(a <= b for a, b in zip(sizes, sizes[1:]))
+    assert sizes[0] == sizes[32] == 0 and sizes[33] > 0
+    for t, size in list(zip(counts, sizes))[33::101]:
+        a = _route()
+        a.experts, a.top_k, a.tokens, a.logits_stride = experts, top_k, t, experts
+        _refuse(lib, "dard_route", a, dict(workspace_bytes=size, workspace=8), ALIGN)
+        _refuse(lib, "dard_route", a, dict(workspace_bytes=15), WORKSPACE)
