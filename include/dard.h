@@ -484,8 +484,9 @@ typedef struct {
 } dard_experts_args;
 #define DARD_EXPERTS_MAX_DIM 65536
 
-/* Bytes of workspace for these sizes and either dtype (0 on invalid sizes): x in the plan's
- * order, the product in between, and the products of each (token, slot) pair before their sum. */
+/* Bytes of workspace for these sizes or fewer tokens and either dtype (0 on invalid sizes): x in
+ * the plan's order, the product in between, and the products of each (token, slot) pair before
+ * their sum. */
 size_t dard_experts_workspace_size(int32_t tokens, int32_t experts, int32_t top_k, int32_t dim,
                                    int32_t hidden);
 

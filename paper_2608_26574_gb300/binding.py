@@ -695,7 +695,8 @@ class ExpertsCall:
     None), or e4m3 / uint8 codes with uint8 / e8m0 scales in layout TILES (``dard_mx_quantize``).
     Call it with x [tokens, dim] (x_scale in layout ROWS for MXFP8), the outputs of a
     ``RouteCall`` and y [tokens, dim] in bf16 or fp32. The workspace holds
-    ``dard_experts_workspace_size`` bytes for every token count that calls use."""
+    ``dard_experts_workspace_size`` bytes for the most tokens of a call, which are enough for
+    fewer tokens too."""
 
     def __init__(self, w1, w1_scale, w3, w3_scale, w2, w2_scale, workspace, status=None):
         torch = _torch()

@@ -1193,10 +1193,16 @@ extern "C" {
 size_t dard_experts_workspace_size(int32_t tokens, int32_t experts, int32_t top_k, int32_t dim,
                                    int32_t hidden) {
   if (!sizes_ok(tokens, experts, top_k, dim, hidden) || tokens == 0) return 0;
+  // The most that any count up to this one needs. It falls only where fewer tokens have more row
+  // tiles (few) or a reduction that is split (at most half as many tiles as SMs, so at most half
+  // as many row tiles of 128 pairs): those counts are looked at one by one.
   size_t most = 0;
+  const int64_t row_tiles = sm_count() / 2 / ((dim + kTileB - 1) / kTileB);
+  const int64_t alone = std::max<int64_t>(kFewTokens, (row_tiles + 1) * kTileM / top_k);
   for (int mx = 0; mx < 2; ++mx) {
-    const Plan q = make_plan(tokens, experts, top_k, dim, hidden, mx != 0);
-    most = std::max(most, q.bytes());
+    for (int64_t t = 1; t <= std::min<int64_t>(tokens, alone); ++t)
+      most = std::max(most, make_plan(t, experts, top_k, dim, hidden, mx != 0).bytes());
+    most = std::max(most, make_plan(tokens, experts, top_k, dim, hidden, mx != 0).bytes());
   }
   return most;
 }

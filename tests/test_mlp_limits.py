@@ -6,7 +6,8 @@ import pytest
 
 from paper_2608_26574_gb300 import binding as B
 
-from .test_mlp_abi import ALIGN, SHAPE, WORKSPACE, _mx, _refuse, _route, lib  # noqa: F401 (lib: a fixture)
+from .test_mlp_abi import (ALIGN, SHAPE, WORKSPACE, _experts, _mx, _refuse, _route,
+                           lib)  # noqa: F401 (lib: a fixture)
 
 
 @pytest.mark.parametrize("batch,rows,cols", [
@@ -40,3 +41,19 @@ def test_route_workspace_serves_every_smaller_count(lib, experts, top_k):  # noq
         a.experts, a.top_k, a.tokens, a.logits_stride = experts, top_k, t, experts
         _refuse(lib, "dard_route", a, dict(workspace_bytes=size, workspace=8), ALIGN)
         _refuse(lib, "dard_route", a, dict(workspace_bytes=15), WORKSPACE)
+
+
+@pytest.mark.parametrize("experts,top_k,dim,hidden", [
+    (1, 1, 4096, 12288), (1, 1, 32, 65536), (64, 8, 2048, 1024), (8, 2, 96, 32768), (40, 6, 2208, 736),
+    (512, 32, 256, 64), (6, 2, 64, 96), (3, 3, 128, 8192)])
+def test_experts_workspace_serves_every_smaller_count(lib, experts, top_k, dim, hidden):  # noqa: F811
+    """As for routing: the size never falls as the count rises, and calls accept it."""
+    counts = [*range(0, 2600), *range(2600, 20000, 91), (1 << 24) // top_k]
+    sizes = [B.dard_experts_workspace_size(t, experts, top_k, dim, hidden) for t in counts]
+    assert sizes[0] == 0 and all(a <= b for a, b in zip(sizes, sizes[1:]))
+    for dtype in (B.DARD_MXFP8, B.DARD_BF16):
+        for t, size in list(zip(counts, sizes))[1::37]:
+            a = _experts()
+            a.dtype, a.tokens, a.experts, a.top_k, a.dim, a.hidden = dtype, t, experts, top_k, dim, hidden
+            a.x_stride, a.y_stride, a.x_scale_stride = dim, dim, (dim + 511) // 512 * 16
+            _refuse(lib, "dard_experts", a, dict(workspace_bytes=size, workspace=8), ALIGN)
