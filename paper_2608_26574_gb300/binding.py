@@ -27,6 +27,7 @@ MX_SCALE_ROWS, MX_SCALE_TILES = 0, 1
 ROUTE_SOFTMAX, ROUTE_SIGMOID = 0, 1
 MX_BLOCK = 32
 NORM_MAX_DIM, MAX_EXPERTS, MAX_TOP_K, MAX_GROUPS = 32768, 512, 32, 32
+EXPERTS_MAX_PAIRS = 1 << 24  # tokens * top_k of one dard_experts call
 
 _I32P = ctypes.POINTER(ctypes.c_int32)
 

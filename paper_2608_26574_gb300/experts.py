@@ -29,7 +29,14 @@ class ExpertMLP:
     [dim, experts] in the model's dtype (bf16 or fp32). ``mx``: weights and activations of the
     products in MXFP8; without it they stay bf16 (a bf16 model's only). ``route`` holds further
     arguments of ``RouteCall`` (scoring, bias, groups, ...). ``workspaces`` (a dict) may be shared by
-    the layers of a model that run one after another on one stream."""
+    the layers of a model, which run one after another.
+
+    The buffers of a call are kept, one set for each stream and each power of two of tokens from 32
+    on: whatever token counts come, there are few sets, each of about half the size of the next;
+    calls on different streams share none, and a set's addresses stay what a captured graph holds. One thread at a
+    time calls the layers that share a dict on one stream."""
+
+    _MAX_PREPARED = 256  # token counts (and streams) whose views and calls are kept
 
     def __init__(self, w1, w3, w2, router, top_k: int, norm_weight=None, eps: float = 1e-6,
                  mx: bool = True, route: dict | None = None, status=None,
@@ -48,15 +55,15 @@ class ExpertMLP:
         self.norm = B.NormCall(self.dim, router.dtype, norm_weight, eps)
         self._route = dict(route or {})
         self._shared = {} if workspaces is None else workspaces
-        self._calls: dict[int, tuple] = {}  # by token count: buffers, routing, experts
+        # by stream and token count: views of the buffers, routing, experts
+        self._calls: dict[tuple, tuple] = {}
 
-    def _buffers(self, tokens: int) -> dict:
-        """Workspaces and intermediate tensors for ``tokens`` rows, kept for the next call."""
-        key = (tokens, self.experts, self.top_k, self.dim, self.hidden, self.mx, self.dtype)
+    def _buffers(self, stream: int, tokens: int) -> dict:
+        """Workspaces and intermediate tensors for up to ``tokens`` rows on a stream."""
+        dev, dim, k = self.router.device, self.dim, self.top_k
+        key = (dev, stream, tokens, self.experts, k, dim, self.hidden, self.mx, self.dtype)
         b = self._shared.get(key)
         if b is None:
-            dev, dim, k = self.router.device, self.dim, self.top_k
-
             def empty(*shape, dtype):
                 return torch.empty(shape, dtype=dtype, device=dev)
 
@@ -77,14 +84,25 @@ class ExpertMLP:
         return b
 
     def _prepared(self, tokens: int) -> tuple:
-        """(buffers, RouteCall, ExpertsCall) for ``tokens`` rows, marshalled once."""
-        c = self._calls.get(tokens)
+        """(buffers, RouteCall, ExpertsCall) for ``tokens`` rows on the current stream, marshalled
+        once."""
+        stream = B._raw_stream(self.router.get_device())
+        c = self._calls.get((stream, tokens))
         if c is None:
-            b = self._buffers(tokens)
+            # the next power of two from 32 on (an expert's rows take whole tiles, so that sets of
+            # fewer are hardly smaller), as far as the products take so many tokens
+            most = min(1 << max(tokens - 1, 31).bit_length(), B.EXPERTS_MAX_PAIRS // self.top_k)
+            b = dict(self._buffers(stream, max(most, tokens)))
+            for name in ("y", "logits", "ids", "weights", "y8", "y8_scale"):
+                if name in b:
+                    b[name] = b[name][:tokens]
+            b["rows"] = b["rows"][:tokens * self.top_k]
             c = (b, B.RouteCall(self.experts, self.top_k, workspace=b["route_ws"],
                                 status=self.status, **self._route),
                  B.ExpertsCall(*self.weights, workspace=b["experts_ws"], status=self.status))
-            self._calls[tokens] = c
+            if len(self._calls) >= self._MAX_PREPARED:
+                self._calls.clear()
+            self._calls[stream, tokens] = c
         return c
 
     def __call__(self, h: torch.Tensor, delta: torch.Tensor | None = None,
