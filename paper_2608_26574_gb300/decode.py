@@ -251,12 +251,27 @@ def step(model: DLLM, batch: Batch, thr: tuple[float, float], lam: float, p0: fl
     return (lx, ls, state_before) if keep_logits else None
 
 
+def check_status(model: DLLM, batch: Batch) -> None:
+    """Raises when a step left outputs behind that are none: a wait that ran out in the attention,
+    the scoring or the experts, or a row that the experts' router could not place (a NaN or +inf
+    logit). (The scoring's own marks on rows, which have defined outputs, are the caller's to
+    read in ``batch.status``.)"""
+    experts, rest = torch.cat([model.status, batch.status]).tolist()
+    names = [n for n, on in (("TIMEOUT", (experts | rest) & B.STATUS_TIMEOUT),
+                             ("INVALID_ROW", experts & B.STATUS_INVALID_ROW)) if on]
+    if names:
+        raise RuntimeError(f"decoding step failed: status {' and '.join(names)} (experts "
+                           f"{experts:#x}, attention and scoring {rest:#x})")
+
+
 def decode(model: DLLM, prompts: list[np.ndarray], gen_len: int, block_len: int,
            thr=(0.5, 0.8), lam=0.5 ** (1 / 8), p0=0.1, order_mode: int = B.ORDER_CONFIDENCE,
            max_steps: int = 64, min_progress: bool = False, record: bool = False):
     """Algorithm 1 block by block. Returns (generated tokens [n, gen_len], per-block steps,
-    per-step GPU microseconds, step records if ``record``)."""
+    per-step GPU microseconds, step records if ``record``). Raises after a step whose status
+    words report a failure (``check_status``)."""
     dev = model.device
+    model.status.zero_()
     n = len(prompts)
     gen = [np.full(gen_len, model.cfg.mask_token, np.int32) for _ in range(n)]
     nB = n * block_len
@@ -280,6 +295,7 @@ def decode(model: DLLM, prompts: list[np.ndarray], gen_len: int, block_len: int,
                        keep_logits=record)
             e1.record()
             counts = outs["counts"].cpu().numpy()  # synchronises
+            check_status(model, batch)
             step_us.append(e0.elapsed_time(e1) * 1e3)
             if record:
                 lx, ls, _ = res
