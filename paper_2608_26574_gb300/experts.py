@@ -28,7 +28,10 @@ class ExpertMLP:
     w1, w3 [experts, hidden, dim] (gate and value), w2 [experts, dim, hidden] and router
     [dim, experts] in the model's dtype (bf16 or fp32). ``mx``: weights and activations of the
     products in MXFP8; without it they stay bf16 (a bf16 model's only). ``route`` holds further
-    arguments of ``RouteCall`` (scoring, bias, groups, ...). ``workspaces`` (a dict) may be shared by
+    arguments of ``RouteCall`` (scoring, bias, groups, ...). ``status`` (int32, one word; the layer's
+    own one if none is given) collects the kernels' status bits: the caller reads it, for after
+    ``STATUS_TIMEOUT`` outputs are unwritten, and ``STATUS_INVALID_ROW`` marks rows whose router
+    logits were NaN or +inf, which get no expert. ``workspaces`` (a dict) may be shared by
     the layers of a model, which run one after another.
 
     The buffers of a call are kept, one set for each stream and each power of two of tokens from 32
@@ -51,7 +54,8 @@ class ExpertMLP:
             self.weights = [t for w in weights for t in mx_weights(w)]
         else:
             self.weights = [t for w in weights for t in (w, None)]
-        self.status = status
+        self.status = status if status is not None else torch.zeros(
+            1, dtype=torch.int32, device=router.device)
         self.norm = B.NormCall(self.dim, router.dtype, norm_weight, eps)
         self._route = dict(route or {})
         self._shared = {} if workspaces is None else workspaces

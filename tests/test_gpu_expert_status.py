@@ -1,10 +1,13 @@
-"""The decoding driver raises when a kernel reports a failure in a status word: outputs that a
-wait which ran out left unwritten, and rows that the router could not place, become no tokens."""
+"""Status words of the experts' MLP: a layer has one, and the decoding driver raises when a kernel
+reports a failure in it: outputs that a wait which ran out left unwritten, and rows that the router
+could not place, become no tokens."""
 import numpy as np
 import pytest
 import torch
 
+from paper_2608_26574_gb300 import binding as B
 from paper_2608_26574_gb300 import decode as D
+from paper_2608_26574_gb300.experts import ExpertMLP
 
 pytestmark = pytest.mark.gpu
 
@@ -56,3 +59,21 @@ def test_a_row_that_the_router_cannot_place_raises():
     with pytest.raises(RuntimeError, match="INVALID_ROW"):
         _decode(model)
     assert int(model.status.item()) != 0
+
+
+def test_a_layer_without_a_status_word_has_its_own(monkeypatch):
+    n, d, f = 4, 256, 512
+    g = torch.Generator(device="cuda").manual_seed(1)
+    w = [torch.randn(*s, generator=g, device="cuda") / 16 for s in ((n, f, d), (n, f, d), (n, d, f))]
+    layer = ExpertMLP(*w, torch.randn(d, n, generator=g, device="cuda"), 2)
+    h = torch.randn(20, d, generator=g, device="cuda")
+    layer(h)
+    assert int(layer.status.item()) == 0
+    with monkeypatch.context() as m:
+        _short_waits(m)
+        layer(h)
+    assert int(layer.status.item()) == B.STATUS_TIMEOUT
+    layer.status.zero_()
+    h[3, 5] = float("nan")
+    layer(h)
+    assert int(layer.status.item()) == B.STATUS_INVALID_ROW
