@@ -527,14 +527,24 @@ def _scale_rows(t, name: str, rows: int, cols: int, device: int) -> tuple[int, i
     return _rows2(t, name, (rows, shape[1]), _dtypes("scales"), device)
 
 
+def _packed_fn(name: str):
+    """The library's function ``name`` for arguments packed into a bytes object: one per call, so
+    that threads may share a prepared call (the library runs without the interpreter lock)."""
+    f = lib()[name]  # (an object of its own, with its own argument types)
+    f.restype, f.argtypes = ctypes.c_int, [ctypes.c_void_p, ctypes.c_void_p]
+    return f
+
+
 class NormCall:
     """``dard_residual_norm`` with the weight and epsilon of one norm marshalled once.
 
     Call it with ``x`` [rows, dim] and any of the outputs: ``residual`` receives x + ``delta``
     (x itself without delta) and may be x or delta; ``y`` the norm in x's dtype; ``y8`` (e4m3 or
-    uint8) and ``y8_scale`` (layout ROWS, see ``mx_scale_shape``) the norm in MXFP8."""
+    uint8) and ``y8_scale`` (layout ROWS, see ``mx_scale_shape``) the norm in MXFP8. Threads may
+    share this and the MLP's other calls (workspaces are a stream's: calls that overlap on the GPU
+    need their own)."""
 
-    _layout = struct.Struct("=7Qii7qf4x")  # dard_norm_args
+    layout = struct.Struct("=7Qii7qf4x")  # dard_norm_args
 
     def __init__(self, dim: int, dtype, weight=None, eps: float = 1e-6):
         if dtype not in _dtypes("float"):
@@ -548,9 +558,7 @@ class NormCall:
         self._weight = weight
         self._eps = eps
         self._code = DARD_BF16 if dtype == _torch().bfloat16 else DARD_F32
-        self._args = NormArgs()
-        self._ref = ctypes.byref(self._args)
-        self._fn = lib().dard_residual_norm
+        self._fn = _packed_fn("dard_residual_norm")
 
     def __call__(self, x, delta=None, residual=None, y=None, y8=None, y8_scale=None, stream=None):
         dim, dt, dev = self.dim, self._dt, x.get_device()
@@ -568,9 +576,9 @@ class NormCall:
                 raise ValueError("y8 needs y8_scale")
             qp, qs = _rows2(y8, "y8", shape, self._codes, dev)
             sp, ss = _scale_rows(y8_scale, "y8_scale", rows, dim, dev)
-        self._layout.pack_into(self._args, 0, xp, dp, self._weight_ptr, rp, yp, qp, sp, self._code,
-                               dim, rows, xs, ds, rs, ys, qs, ss, self._eps)
-        _check(self._fn(self._ref, _stream_handle(stream, dev)), "dard_residual_norm")
+        args = self.layout.pack(xp, dp, self._weight_ptr, rp, yp, qp, sp, self._code, dim, rows, xs,
+                                ds, rs, ys, qs, ss, self._eps)
+        _check(self._fn(args, _stream_handle(stream, dev)), "dard_residual_norm")
 
 
 def dard_residual_norm(x, delta=None, weight=None, eps: float = 1e-6, residual=None, y=None,
@@ -634,46 +642,45 @@ class RouteCall:
     ``dard_route_workspace_size`` bytes for the most tokens of a call with a plan, which are
     enough for fewer tokens too."""
 
+    layout = struct.Struct("=QqQ8if4x6QQ")  # dard_route_args
+
     def __init__(self, experts: int, top_k: int, scoring: int = ROUTE_SOFTMAX, bias=None,
                  groups: int = 1, top_groups: int = 1, renormalise: bool = True,
                  scale: float = 1.0, workspace=None, status=None):
         torch = _torch()
         self.experts, self.top_k = experts, top_k
-        a = RouteArgs()
         self.device = next((t.get_device() for t in (bias, workspace, status) if t is not None), None)
-        a.bias = _dev(bias, "bias", experts, torch.float32, self.device)
-        a.status = _dev(status, "status", 1, torch.int32, self.device)
-        a.scoring, a.experts, a.top_k, a.groups = scoring, experts, top_k, groups
-        a.top_groups, a.renormalise, a.scale = top_groups, 1 if renormalise else 0, scale
+        self._bias = _dev(bias, "bias", experts, torch.float32, self.device) or 0
+        self._scoring = scoring
+        self._settings = (experts, top_k, groups, top_groups, 1 if renormalise else 0, scale)
+        status_ptr = _dev(status, "status", 1, torch.int32, self.device) or 0
+        self._scratch = (status_ptr, 0, 0)
         if workspace is not None:
-            a.workspace = _dev(workspace, "workspace", 0, workspace.dtype, self.device)
-            a.workspace_bytes = workspace.numel() * workspace.element_size()
+            self._scratch = (status_ptr,
+                             _dev(workspace, "workspace", 0, workspace.dtype, self.device),
+                             workspace.numel() * workspace.element_size())
         self._keep = (bias, workspace, status)
-        self._args, self._ref = a, ctypes.byref(a)
-        self._fn = lib().dard_route
+        self._fn = _packed_fn("dard_route")
 
     def __call__(self, logits, ids, weights, offsets=None, rows=None, stream=None):
-        a, k = self._args, self.top_k
-        tokens, dev = logits.shape[0], logits.get_device()
+        k, tokens, dev = self.top_k, logits.shape[0], logits.get_device()
         if self.device is not None and dev != self.device:
             raise ValueError(f"logits: on device {dev}, expected {self.device}")
-        a.logits, a.logits_stride = _rows2(logits, "logits", (tokens, self.experts),
-                                           _dtypes("float"), dev)
-        a.dtype, a.tokens = _dtype_code(logits), tokens
+        lp, ls = _rows2(logits, "logits", (tokens, self.experts), _dtypes("float"), dev)
         if ids.shape != (tokens, k) or weights.shape != (tokens, k):
             raise ValueError(f"ids and weights: [{tokens}, {k}] expected, got {tuple(ids.shape)}, "
                              f"{tuple(weights.shape)}")
         i32 = _dtypes("i32")
-        a.ids = _flat(ids, "ids", i32, dev)
-        a.weights = _flat(weights, "weights", _dtypes("f32"), dev)
+        ip, wp = _flat(ids, "ids", i32, dev), _flat(weights, "weights", _dtypes("f32"), dev)
         if (offsets is None) != (rows is None):
             raise ValueError("offsets and rows come together")
+        op = rp = 0
         if offsets is not None:
-            a.offsets = _flat(offsets, "offsets", i32, dev, self.experts + 1)
-            a.rows = _flat(rows, "rows", i32, dev, tokens * k)
-        else:
-            a.offsets = a.rows = None
-        _check(self._fn(self._ref, _stream_handle(stream, dev)), "dard_route")
+            op = _flat(offsets, "offsets", i32, dev, self.experts + 1)
+            rp = _flat(rows, "rows", i32, dev, tokens * k)
+        args = self.layout.pack(lp, ls, self._bias, _dtype_code(logits), self._scoring, tokens,
+                                *self._settings, ip, wp, op, rp, *self._scratch)
+        _check(self._fn(args, _stream_handle(stream, dev)), "dard_route")
 
 
 def dard_route(logits, ids, weights, top_k: int, scoring: int = ROUTE_SOFTMAX, bias=None,
@@ -699,6 +706,8 @@ class ExpertsCall:
     ``dard_experts_workspace_size`` bytes for the most tokens of a call, which are enough for
     fewer tokens too."""
 
+    layout = struct.Struct("=13Q3q7i4x3Q")  # dard_experts_args
+
     def __init__(self, w1, w1_scale, w3, w3_scale, w2, w2_scale, workspace, status=None):
         torch = _torch()
         if w1.dim() != 3 or w3.shape != w1.shape or tuple(w2.shape) != (
@@ -709,10 +718,10 @@ class ExpertsCall:
         self.mx = w1.dtype != torch.bfloat16
         self._bf16 = torch.bfloat16
         self.device = dev = w1.get_device()
-        a = ExpertsArgs()
+        codes, scales = [], []  # w1, w3, w2
         for name, w, s in (("w1", w1, w1_scale), ("w3", w3, w3_scale), ("w2", w2, w2_scale)):
             _is_dtype(w, name, _dtypes("codes" if self.mx else "bf16"))
-            setattr(a, name, _dev(w, name, w.numel(), w.dtype, dev))
+            codes.append(_dev(w, name, w.numel(), w.dtype, dev))
             if not self.mx:
                 if s is not None:
                     raise ValueError(f"{name}_scale: bf16 weights have no scales")
@@ -723,38 +732,39 @@ class ExpertsCall:
             _is_dtype(s, name + "_scale", _dtypes("scales"))
             if tuple(s.shape) != want:
                 raise ValueError(f"{name}_scale: {want} expected, got {tuple(s.shape)}")
-            setattr(a, name + "_scale", _dev(s, name + "_scale", s.numel(), s.dtype, dev))
-        a.experts, a.hidden, a.dim = self.experts, self.hidden, self.dim
-        a.dtype = DARD_MXFP8 if self.mx else DARD_BF16
+            scales.append(_dev(s, name + "_scale", s.numel(), s.dtype, dev))
+        self._weights = (*codes, *(scales or (0, 0, 0)))
+        self._code = DARD_MXFP8 if self.mx else DARD_BF16
         if workspace is None:
             raise ValueError("workspace is required (see dard_experts_workspace_size)")
-        a.workspace = _dev(workspace, "workspace", 0, workspace.dtype, dev)
-        a.workspace_bytes = workspace.numel() * workspace.element_size()
-        a.status = _dev(status, "status", 1, torch.int32, dev)
+        self._scratch = (_dev(workspace, "workspace", 0, workspace.dtype, dev),
+                         workspace.numel() * workspace.element_size(),
+                         _dev(status, "status", 1, torch.int32, dev) or 0)
         self._keep = (w1, w1_scale, w3, w3_scale, w2, w2_scale, workspace, status)
-        self._args, self._ref = a, ctypes.byref(a)
-        self._fn = lib().dard_experts
+        self._fn = _packed_fn("dard_experts")
 
     def __call__(self, x, x_scale, ids, weights, offsets, rows, y, stream=None):
-        a, dev, dim = self._args, self.device, self.dim
+        dev, dim = self.device, self.dim
         tokens, k = ids.shape
         shape = (tokens, dim)
-        a.x, a.x_stride = _rows2(x, "x", shape, _dtypes("codes" if self.mx else "bf16"), dev)
+        xp, xs = _rows2(x, "x", shape, _dtypes("codes" if self.mx else "bf16"), dev)
+        sp = ss = 0
         if self.mx:
             if x_scale is None:
                 raise ValueError("x_scale: needed with 8-bit weights")
-            a.x_scale, a.x_scale_stride = _scale_rows(x_scale, "x_scale", tokens, dim, dev)
-        a.y, a.y_stride = _rows2(y, "y", shape, _dtypes("float"), dev)
-        a.y_dtype = DARD_BF16 if y.dtype == self._bf16 else DARD_F32
+            sp, ss = _scale_rows(x_scale, "x_scale", tokens, dim, dev)
+        yp, ys = _rows2(y, "y", shape, _dtypes("float"), dev)
         if weights.shape != ids.shape:
             raise ValueError(f"weights: {tuple(ids.shape)} expected, got {tuple(weights.shape)}")
-        a.tokens, a.top_k = tokens, k
         i32, f32 = _dtypes("i32"), _dtypes("f32")
-        a.ids = _flat(ids, "ids", i32, dev)
-        a.weights = _flat(weights, "weights", f32, dev)
-        a.offsets = _flat(offsets, "offsets", i32, dev, self.experts + 1)
-        a.rows = _flat(rows, "rows", i32, dev, tokens * k)
-        _check(self._fn(self._ref, _stream_handle(stream, dev)), "dard_experts")
+        ip, wp = _flat(ids, "ids", i32, dev), _flat(weights, "weights", f32, dev)
+        op = _flat(offsets, "offsets", i32, dev, self.experts + 1)
+        rp = _flat(rows, "rows", i32, dev, tokens * k)
+        args = self.layout.pack(
+            xp, sp, *self._weights, ip, wp, op, rp, yp, xs, ss, ys, self._code,
+            DARD_BF16 if y.dtype == self._bf16 else DARD_F32, tokens, self.experts, k, dim,
+            self.hidden, *self._scratch)
+        _check(self._fn(args, _stream_handle(stream, dev)), "dard_experts")
 
 
 def dard_experts(x, x_scale, w1, w1_scale, w3, w3_scale, w2, w2_scale, ids, weights, offsets,
