@@ -25,9 +25,12 @@
 // Roles per CTA (warps: pairs 12, single 8, few 7):
 //   epilogue    8 warps (single, few: 4): TMEM -> registers, then the accumulator is free for the
 //               next tile while SwiGLU, the rounding and the stores run from registers;
-//   producer    TMA: rows of A that lie side by side, weights, scales (cp.async.bulk);
-//   issuer      TMEM allocation; scale copies (tcgen05.cp) and MMAs (pairs: in rank 0; in rank 1
-//               it forwards the landing of its stages to rank 0's barriers);
+//   producer    TMA: rows of A that lie side by side, weights, scales (cp.async.bulk). Pairs: each
+//               rank fills its own shared memory, and both ranks' copies report to rank 0's
+//               barriers, where the issuer waits. (A warp of rank 1 that waits for its copies and
+//               tells rank 0 has to do so with release at cluster scope, at some 1500 cycles per
+//               stage: 800 rows of 4096 x 12288 300 us instead of 114.);
+//   issuer      TMEM allocation; scale copies (tcgen05.cp) and MMAs (pairs: in rank 0);
 //   gather      single and few, phase 1: the rows of x by token (cp.async, 16 bytes per lane,
 //               straight into the swizzled layout) and their scales.
 //   Stage: 128 bytes of K of the A rows and of the weight rows (128-byte swizzle), plus scales.
@@ -46,9 +49,10 @@
 // 2048 x 1024: 403 MB in 85 us; with no MMA at all 80) and for one token the chain of latencies
 // (22.7 us; its 52 MB alone would take 7.6).
 //
-// Every wait is bounded; one that gives up sets DARD_STATUS_TIMEOUT and the CTA's abort flag,
-// on which every role leaves its loop. The producer then waits (bounded) for its copies in
-// flight and the issuer for its MMAs before shared memory and TMEM are released.
+// Every wait is bounded; one that gives up sets DARD_STATUS_TIMEOUT and the abort flag of its CTA
+// (of both of a pair), on which every role leaves its loop. The producer (for a pair, rank 0's)
+// then waits (bounded) for copies in flight and the issuer for its MMAs before shared memory and
+// TMEM are released.
 #include <cuda.h>
 #include <cuda_bf16.h>
 #include <cudaTypedefs.h>
@@ -56,6 +60,7 @@
 #include <algorithm>
 #include <cmath>
 #include <cstdlib>
+#include <type_traits>
 
 #include "dard_host.cuh"
 #include "dard_internal.h"
@@ -141,6 +146,24 @@ __device__ __forceinline__ void tma_load_3d(void* dst, const void* desc, uint64_
       "l"(reinterpret_cast<uint64_t>(desc)), "r"(smem_u32(bar)), "r"(c0), "r"(c1), "r"(c2)
       : "memory");
 }
+// CTA pairs: tiled loads into the own shared memory that report to a barrier of either CTA of the
+// pair, given by its shared::cluster address (with release at cluster scope).
+__device__ __forceinline__ void tma_load_2d_pair(void* dst, const void* desc, uint32_t bar, int32_t c0,
+                                                 int32_t c1) {
+  asm volatile(
+      "cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes"
+      " [%0], [%1, {%3, %4}], [%2];" ::"r"(smem_u32(dst)),
+      "l"(reinterpret_cast<uint64_t>(desc)), "r"(bar), "r"(c0), "r"(c1)
+      : "memory");
+}
+__device__ __forceinline__ void tma_load_3d_pair(void* dst, const void* desc, uint32_t bar, int32_t c0,
+                                                 int32_t c1, int32_t c2) {
+  asm volatile(
+      "cp.async.bulk.tensor.3d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes"
+      " [%0], [%1, {%3, %4, %5}], [%2];" ::"r"(smem_u32(dst)),
+      "l"(reinterpret_cast<uint64_t>(desc)), "r"(bar), "r"(c0), "r"(c1), "r"(c2)
+      : "memory");
+}
 __device__ __forceinline__ void bulk_load(void* dst, const void* src, uint32_t bytes, uint64_t* bar) {
   asm volatile(
       "cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(
@@ -185,23 +208,63 @@ __device__ __forceinline__ void mma_ss_pair(uint32_t d, uint64_t a, uint64_t b, 
       "l"(a), "l"(b), "r"(idesc), "r"(accumulate)
       : "memory");
 }
-// Whether the phase with this parity has completed, without waiting.
-__device__ __forceinline__ bool mbar_test(uint64_t* bar, uint32_t parity) {
+// Waits on a barrier, or looks at it, at the scope of what arrives there: the CTA, or (kPair) the
+// cluster, whose other CTA arrives too.
+template <bool kPair>
+__device__ __forceinline__ bool try_wait(uint64_t* bar, uint32_t parity) {
+  if constexpr (!kPair) return mbar_try_wait(bar, parity);
   uint32_t ok;
   asm volatile(
       "{\n\t.reg .pred p;\n\t"
-      "mbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
+      "mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n\t"
       "selp.u32 %0, 1, 0, p;\n\t}"
       : "=r"(ok)
       : "r"(smem_u32(bar)), "r"(parity)
       : "memory");
   return ok != 0;
 }
+// Whether the phase with this parity has completed, without waiting.
+template <bool kPair>
+__device__ __forceinline__ bool mbar_test(uint64_t* bar, uint32_t parity) {
+  uint32_t ok;
+  if constexpr (kPair)
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "mbarrier.test_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n\t"
+        "selp.u32 %0, 1, 0, p;\n\t}"
+        : "=r"(ok)
+        : "r"(smem_u32(bar)), "r"(parity)
+        : "memory");
+  else
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "mbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
+        "selp.u32 %0, 1, 0, p;\n\t}"
+        : "=r"(ok)
+        : "r"(smem_u32(bar)), "r"(parity)
+        : "memory");
+  return ok != 0;
+}
+// CTA pairs: arrivals on a barrier of rank 0, given by its shared::cluster address. Relaxed: what
+// they hand over is ordered by the tcgen05 fences around them (the accumulator), or is the
+// number of bytes that copies will report to the barrier by themselves.
+__device__ __forceinline__ void arrive_cluster(uint32_t bar) {
+  asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
+}
+__device__ __forceinline__ void arrive_expect_tx_cluster(uint32_t bar, uint32_t bytes) {
+  asm volatile("mbarrier.arrive.expect_tx.relaxed.cluster.shared::cluster.b64 _, [%0], %1;" ::"r"(bar),
+               "r"(bytes)
+               : "memory");
+}
+__device__ __forceinline__ void store_cluster(uint32_t addr, int32_t v) {
+  asm volatile("st.shared::cluster.s32 [%0], %1;" ::"r"(addr), "r"(v) : "memory");
+}
 // mbar_wait that also gives up, once it has to wait, when the CTA's abort flag is set.
+template <bool kPair>
 __device__ __noinline__ bool wait_slow(uint64_t* bar, uint32_t parity, long long limit,
                                        const volatile int32_t* abort_flag) {
   const long long t0 = clock64();
-  while (!mbar_try_wait(bar, parity)) {
+  while (!try_wait<kPair>(bar, parity)) {
     if (*abort_flag != 0 || clock64() - t0 > limit) return false;
   }
   return true;
@@ -258,12 +321,13 @@ __host__ __device__ constexpr uint32_t idesc_mx(uint32_t M, uint32_t N, uint32_t
 }
 
 struct __align__(16) Ctl {
-  uint64_t full[kMaxStages], empty[kMaxStages];  // (pair, rank 0: full in both CTAs)
+  uint64_t full[kMaxStages], empty[kMaxStages];  // (pairs: rank 0's full is both CTAs')
   uint64_t acc_full, acc_free;
   uint64_t drained;  // every MMA the issuer launched has completed
   uint32_t tmem_base;
-  int32_t abort;
+  int32_t abort;     // (pairs: set in both CTAs)
   int32_t last;      // few: this CTA's tile was its columns' last
+  int32_t uses[2];   // pairs: stages that each rank has filled (both CTAs hold both)
   int32_t first_row[DARD_MAX_EXPERTS + 1];   // offsets, clamped to [0, pairs]
   int32_t first_tile[DARD_MAX_EXPERTS + 1];  // row tiles of the experts before
   // (pairs: after this, the same in units of two row tiles)
@@ -416,10 +480,20 @@ __device__ __forceinline__ void combine_columns(const ExpertsParams& p, int64_t 
         make_uint2(pack2(sum.x, sum.y), pack2(sum.z, sum.w));
 }
 
+// Pairs: maps of the scales' tiles (rows of 512 bytes), which tiled loads take so that they can
+// report to the other CTA's barrier; the other variants' plain bulk copies need none.
+struct ScaleMaps {
+  CUtensorMap a, b0, b1;
+};
+struct NoScaleMaps {};
+template <int kVariant>
+using ScaleMapsOf = std::conditional_t<kVariant == kPairs, ScaleMaps, NoScaleMaps>;
+
 template <bool kMx, int kVariant, int kPhase>
 __global__ void __launch_bounds__(Shape<kVariant>::kThreads, Shape<kVariant>::kCtasPerSm)
     product(const __grid_constant__ ExpertsParams p, const __grid_constant__ CUtensorMap map_a,
-            const __grid_constant__ CUtensorMap map_b0, const __grid_constant__ CUtensorMap map_b1) {
+            const __grid_constant__ CUtensorMap map_b0, const __grid_constant__ CUtensorMap map_b1,
+            const __grid_constant__ ScaleMapsOf<kVariant> scale_maps) {
   using S = Shape<kVariant>;
   constexpr bool kPair = S::kPair;
   constexpr int kCtas = S::kCtas, kStages = S::kStages;
@@ -455,7 +529,7 @@ __global__ void __launch_bounds__(Shape<kVariant>::kThreads, Shape<kVariant>::kC
   }
   if (warp == S::kProducerWarp && lane == 0) {
     for (int b = 0; b < kStages; ++b) {
-      // the producer, the gather warps, and in rank 0 of a pair rank 1's forwarder
+      // the producer, the gather warps, and in rank 0 of a pair rank 1's producer
       mbar_init(&ctl.full[b], 1 + (kGather ? S::kGatherWarps : 0) + (kPair && rank == 0 ? 1 : 0));
       mbar_init(&ctl.empty[b], 1);
     }
@@ -481,13 +555,19 @@ __global__ void __launch_bounds__(Shape<kVariant>::kThreads, Shape<kVariant>::kC
   tc_fence_after();
   const uint32_t tmem = ctl.tmem_base;
   volatile int32_t* abort_flag = &ctl.abort;
+  // the same shared memory of the pair's other CTA (which stays until the teardown's cluster_sync)
+  const auto peer = [&](const void* at) { return map_shared_rank(smem_u32(at), rank ^ 1); };
+  const auto report_timeout = [&]() {
+    if (p.status) atomicOr(p.status, DARD_STATUS_TIMEOUT);
+  };
   const auto give_up = [&]() {
     *abort_flag = 1;
-    if (p.status) atomicOr(p.status, DARD_STATUS_TIMEOUT);
+    if constexpr (kPair) store_cluster(peer(&ctl.abort), 1);
+    report_timeout();
   };
   const int split_stages = kPhase == 2 ? p.split_stages : p.k_stages;
   const auto wait = [&](uint64_t* bar, uint32_t parity) {
-    return mbar_try_wait(bar, parity) || wait_slow(bar, parity, limit, abort_flag);
+    return try_wait<kPair>(bar, parity) || wait_slow<kPair>(bar, parity, limit, abort_flag);
   };
   // the same by every lane of a warp, with one verdict
   const auto warp_wait = [&](uint64_t* bar, uint32_t parity) {
@@ -512,11 +592,10 @@ __global__ void __launch_bounds__(Shape<kVariant>::kThreads, Shape<kVariant>::kC
       const bool second = kPhase == 1 || (kN > 128 && n0 + 128 < p.n_elems);
       uint32_t bytes = kBytesB + boxes_a * kBoxA * kStageK;
       if (kMx) bytes += (second ? 2 : 1) * kMxTileBytes + (boxes_a > 0 ? kMxTileBytes : 0);
-      const int64_t step_b = static_cast<int64_t>(p.k_stages) * kMxTileBytes;  // a row of tiles
-      const int64_t at_b = (static_cast<int64_t>(t.e) * ((p.n_elems + 127) / 128) + n0 / 128) * step_b;
-      const uint8_t* sf_b0 = p.scale_b[0] + at_b;
-      const uint8_t* sf_b1 = kPhase == 1 ? p.scale_b[1] + at_b : sf_b0 + step_b;
-      const uint8_t* sf_a = p.a_scale + t.row_tile * step_b;
+      // first tiles of scales of this tile's rows: k_stages of them side by side
+      const int64_t at_b = (static_cast<int64_t>(t.e) * ((p.n_elems + 127) / 128) + n0 / 128) * p.k_stages;
+      const int64_t at_b1 = kPhase == 1 ? at_b : at_b + p.k_stages;
+      const int64_t at_a = static_cast<int64_t>(t.row_tile) * p.k_stages;
       // A pair's CTA without rows: zeros (a box outside the map) into each stage, once a tile.
       // Power bounds long runs of the largest calls (the clock falls from 2070 to 1600-1900 MHz),
       // and zeros take less of it than another tile's rows: 800 rows of 4096 x 12288, call after
@@ -525,32 +604,54 @@ __global__ void __launch_bounds__(Shape<kVariant>::kThreads, Shape<kVariant>::kC
       const auto load_b = [&](int k, int b) {
         uint8_t* sb = base + b * kStageBytes + S::kBytesA;
         uint8_t* ss = s_scale + b * kScaleBytes;
-        uint64_t* bar = &ctl.full[b];
-        mbar_arrive_expect_tx(bar, bytes + (no_rows(k) ? kBoxA * kStageK : 0));
-        if (use != p.test_drop) {
-          if constexpr (kPhase == 1 && !kPair) {  // 64 rows of each matrix
-            tma_load_3d(sb, &map_b0, bar, k * kElems, n0, t.e);
-            tma_load_3d(sb + 64 * kStageK, &map_b1, bar, k * kElems, n0, t.e);
-          } else if constexpr (kPhase == 1) {
-            tma_load_3d(sb, rank == 1 ? &map_b1 : &map_b0, bar, k * kElems, n0, t.e);
-          } else {
-            tma_load_3d(sb, &map_b0, bar, k * kElems, n0 + rank * kTileB, t.e);
+        const uint32_t all = bytes + (no_rows(k) ? kBoxA * kStageK : 0);
+        if constexpr (kPair) {
+          const uint32_t bar = lead(&ctl.full[b]);
+          arrive_expect_tx_cluster(bar, all);
+          if (use != p.test_drop) {
+            if constexpr (kPhase == 1)
+              tma_load_3d_pair(sb, rank == 1 ? &map_b1 : &map_b0, bar, k * kElems, n0, t.e);
+            else
+              tma_load_3d_pair(sb, &map_b0, bar, k * kElems, n0 + rank * kTileB, t.e);
           }
-        }
-        if constexpr (kMx) {
-          bulk_load(ss + kMxTileBytes, sf_b0 + k * kMxTileBytes, kMxTileBytes, bar);
-          if (second) bulk_load(ss + 2 * kMxTileBytes, sf_b1 + k * kMxTileBytes, kMxTileBytes, bar);
+          if constexpr (kMx) {
+            tma_load_2d_pair(ss + kMxTileBytes, &scale_maps.b0, bar, 0, static_cast<int32_t>(at_b + k));
+            if (second)
+              tma_load_2d_pair(ss + 2 * kMxTileBytes, &scale_maps.b1, bar, 0, static_cast<int32_t>(at_b1 + k));
+          }
+        } else {
+          uint64_t* bar = &ctl.full[b];
+          mbar_arrive_expect_tx(bar, all);
+          if (use != p.test_drop) {
+            tma_load_3d(sb, &map_b0, bar, k * kElems, n0, t.e);
+            if constexpr (kPhase == 1)  // 64 rows of each matrix
+              tma_load_3d(sb + 64 * kStageK, &map_b1, bar, k * kElems, n0, t.e);
+          }
+          if constexpr (kMx) {
+            bulk_load(ss + kMxTileBytes, p.scale_b[0] + (at_b + k) * kMxTileBytes, kMxTileBytes, bar);
+            if constexpr (kPhase == 1)
+              bulk_load(ss + 2 * kMxTileBytes, p.scale_b[1] + (at_b + k) * kMxTileBytes, kMxTileBytes, bar);
+          }
         }
       };
       const auto load_a = [&](int k, int b) {
-        uint64_t* bar = &ctl.full[b];
-        if (no_rows(k))
-          tma_load_2d(base + b * kStageBytes, &map_a, bar, k * kElems, p.max_row_tiles * kTileM);
-        for (int i = 0; i < boxes_a; ++i)
-          tma_load_2d(base + b * kStageBytes + i * kBoxA * kStageK, &map_a, bar, k * kElems,
-                      t.row_tile * kTileM + i * kBoxA);
-        if (kMx && boxes_a > 0)
-          bulk_load(s_scale + b * kScaleBytes, sf_a + k * kMxTileBytes, kMxTileBytes, bar);
+        uint8_t* sa = base + b * kStageBytes;
+        uint8_t* ss = s_scale + b * kScaleBytes;
+        if constexpr (kPair) {
+          const uint32_t bar = lead(&ctl.full[b]);
+          if (boxes_a > 0 || no_rows(k))
+            tma_load_2d_pair(sa, &map_a, bar, k * kElems,
+                             (boxes_a > 0 ? t.row_tile : p.max_row_tiles) * kTileM);
+          if (kMx && boxes_a > 0)
+            tma_load_2d_pair(ss, &scale_maps.a, bar, 0, static_cast<int32_t>(at_a + k));
+        } else {
+          uint64_t* bar = &ctl.full[b];
+          for (int i = 0; i < boxes_a; ++i)
+            tma_load_2d(sa + i * kBoxA * kStageK, &map_a, bar, k * kElems,
+                        t.row_tile * kTileM + i * kBoxA);
+          if (kMx && boxes_a > 0)
+            bulk_load(ss, p.a_scale + (at_a + k) * kMxTileBytes, kMxTileBytes, bar);
+        }
       };
       int k = k0;
       if (!waited) {
@@ -583,8 +684,13 @@ __global__ void __launch_bounds__(Shape<kVariant>::kThreads, Shape<kVariant>::kC
     // Without a tile too: a launch ends after the one before it, which otherwise could still read
     // the plan or write x's copy when the call seems over to what follows it.
     if (!waited) grid_dep_wait();
-    if (!ok) {
-      if (lane == 0) give_up();
+    if (!ok && lane == 0) give_up();
+    if constexpr (kPair) {  // (the teardown waits for copies in flight)
+      if (lane == 0) {
+        ctl.uses[rank] = use;
+        store_cluster(peer(&ctl.uses[rank]), use);
+      }
+    } else if (!ok) {
       // copies in flight land before shared memory is released: the last use of each stage
       for (int u = max(0, use - kStages); u < use; ++u)
         mbar_wait(&ctl.full[u % kStages], (u / kStages) & 1, limit);
@@ -619,7 +725,7 @@ __global__ void __launch_bounds__(Shape<kVariant>::kThreads, Shape<kVariant>::kC
           tc_fence_after();
           Ring next = ring;
           next.next<kStages>();
-          const bool look = mbar_test(&ctl.full[next.b], next.phase);
+          const bool look = mbar_test<kPair>(&ctl.full[next.b], next.phase);
           if (issue) {
             // descriptors count 16-byte units
             const uint64_t da = desc_a + ring.b * (kStageBytes / 16), db = da + S::kBytesA / 16;
@@ -666,22 +772,6 @@ __global__ void __launch_bounds__(Shape<kVariant>::kThreads, Shape<kVariant>::kC
         if constexpr (kPair) mma_commit_pair(&ctl.drained, kBothCtas);
         else mma_commit(&ctl.drained);
       }
-    } else if (lane == 0) {
-      // ------------------------------------------------------------ rank 1: landings to rank 0
-      int e = 0;
-      bool ok = true;
-      Tile t;
-      Ring ring;
-      for (int64_t w = first; ok && get_tile<kVariant>(p, ctl, first_unit, rank, w, e, t); w += step) {
-        const int k0 = t.split * split_stages, k1 = min(p.k_stages, k0 + split_stages);
-        for (int k = k0; k < k1; ++k) {
-          ok = wait(&ctl.full[ring.b], ring.phase);
-          if (!ok) break;
-          mbar_arrive_remote(lead(&ctl.full[ring.b]));
-          ring.next<kStages>();
-        }
-      }
-      if (!ok) give_up();
     }
     __syncwarp();
   } else if (warp >= S::kGatherWarp) {
@@ -748,7 +838,7 @@ __global__ void __launch_bounds__(Shape<kVariant>::kThreads, Shape<kVariant>::kC
           for (int j = 0; j < 4; ++j) {
             if (k + j >= p.k_stages) break;
             const int b = ring.b;
-            if (!__all_sync(0xffffffffu, mbar_test(&ctl.empty[b], ring.phase ^ 1))) {
+            if (!__all_sync(0xffffffffu, mbar_test<kPair>(&ctl.empty[b], ring.phase ^ 1))) {
               cp_async_wait_all();  // nothing else to do: tell of every stage so far
               announce(0);
             }
@@ -837,7 +927,7 @@ __global__ void __launch_bounds__(Shape<kVariant>::kThreads, Shape<kVariant>::kC
           tc_fence_before();
           __syncwarp();
           if (lane == 0) {
-            if constexpr (kPair) mbar_arrive_remote(lead(&ctl.acc_free));
+            if constexpr (kPair) arrive_cluster(lead(&ctl.acc_free));
             else mbar_arrive(&ctl.acc_free);
           }
         }
@@ -950,10 +1040,28 @@ __global__ void __launch_bounds__(Shape<kVariant>::kThreads, Shape<kVariant>::kC
   }
   // ---------------------------------------------------------------- teardown
   tc_fence_before();
-  if constexpr (kPair) cluster_sync();  // no CTA leaves while the other may signal its barriers
-  else __syncthreads();
+  if constexpr (kPair) {
+    cluster_sync();  // no CTA leaves while the other may signal its barriers
+    if (ctl.abort != 0) {
+      // Both CTAs are here. Copies in flight land before shared memory is released: rank 0's
+      // barriers tell, once the rank that has filled fewer stages (by at most kStages: no stage is
+      // filled again before both ranks' part of it was used) has arrived for the others.
+      if (rank == 0 && warp == S::kProducerWarp) {
+        const int low = min(ctl.uses[0], ctl.uses[1]), high = max(ctl.uses[0], ctl.uses[1]);
+        if (lane == 0)
+          for (int u = low; u < high; ++u) mbar_arrive(&ctl.full[u % kStages]);
+        __syncwarp();
+        for (int u = max(0, high - kStages); u < high; ++u)
+          mbar_wait(&ctl.full[u % kStages], (u / kStages) & 1, limit);
+        __syncwarp();
+      }
+      cluster_sync();
+    }
+  } else {
+    __syncthreads();
+  }
   if (warp == S::kIssueWarp) {
-    if (!mbar_wait(&ctl.drained, 0, limit) && lane == 0) give_up();
+    if (!mbar_wait(&ctl.drained, 0, limit) && lane == 0) report_timeout();
     __syncwarp();
     tc_fence_after();
     if constexpr (kPair) tmem_dealloc_pair<S::kTmem>(tmem);
@@ -1051,6 +1159,18 @@ bool encode(CUtensorMap* m, const void* ptr, bool mx, uint64_t cols, uint64_t ro
             CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
+// Map of tiles of scales, each a row of 128 words.
+bool encode_scales(CUtensorMap* m, const void* ptr, int64_t tiles) {
+  const auto fn = encode_fn();
+  if (!fn) return false;
+  const cuuint64_t dims[2] = {kMxTileBytes / 4, static_cast<cuuint64_t>(tiles)};
+  const cuuint64_t strides[1] = {kMxTileBytes};
+  const cuuint32_t box[2] = {kMxTileBytes / 4, 1}, unit[2] = {1, 1};
+  return fn(m, CU_TENSOR_MAP_DATA_TYPE_UINT32, 2, const_cast<void*>(ptr), dims, strides, box, unit,
+            CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_NONE,
+            CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
 // A launch that may begin (up to its griddepcontrol.wait) while the one before it on the stream
 // still runs, with clusters of `cluster` CTAs. Not copyable: cfg points at attr.
 struct Launch {
@@ -1090,9 +1210,14 @@ int max_pairs(F* kernel, std::atomic<int>* cache) {
   return n;
 }
 
+// The maps of one phase's launch: rows of A, weights, and (pairs, MXFP8) their scales.
+struct Maps {
+  CUtensorMap a, b0, b1;
+  ScaleMaps scales;
+};
+
 template <bool kMx, int kVariant, int kPhase>
-cudaError_t launch_product(const ExpertsParams& p, int64_t tiles, const CUtensorMap& a,
-                           const CUtensorMap& b0, const CUtensorMap& b1, cudaStream_t stream) {
+cudaError_t launch_product(const ExpertsParams& p, int64_t tiles, const Maps& m, cudaStream_t stream) {
   using S = Shape<kVariant>;
   static std::atomic<uint64_t> done{0};
   static std::atomic<int> pairs[64];
@@ -1102,15 +1227,16 @@ cudaError_t launch_product(const ExpertsParams& p, int64_t tiles, const CUtensor
   const int64_t most = S::kPair ? max_pairs(kernel, pairs) : sm_count() * S::kCtasPerSm;
   const unsigned ctas = static_cast<unsigned>(std::min<int64_t>(tiles, most)) * S::kCtas;
   const Launch l(dim3(ctas), S::kThreads, smem_bytes<kVariant>(), stream, S::kCtas);
-  return cudaLaunchKernelEx(&l.cfg, kernel, p, a, b0, b1);
+  if constexpr (S::kPair) return cudaLaunchKernelEx(&l.cfg, kernel, p, m.a, m.b0, m.b1, m.scales);
+  else return cudaLaunchKernelEx(&l.cfg, kernel, p, m.a, m.b0, m.b1, NoScaleMaps{});
 }
 
 template <bool kMx, int kPhase>
-cudaError_t launch_phase(const ExpertsParams& p, int variant, int64_t tiles, const CUtensorMap& a,
-                         const CUtensorMap& b0, const CUtensorMap& b1, cudaStream_t s) {
-  return variant == kPairs    ? launch_product<kMx, kPairs, kPhase>(p, tiles, a, b0, b1, s)
-         : variant == kSingle ? launch_product<kMx, kSingle, kPhase>(p, tiles, a, b0, b1, s)
-                              : launch_product<kMx, kFew, kPhase>(p, tiles, a, b0, b1, s);
+cudaError_t launch_phase(const ExpertsParams& p, int variant, int64_t tiles, const Maps& m,
+                         cudaStream_t s) {
+  return variant == kPairs    ? launch_product<kMx, kPairs, kPhase>(p, tiles, m, s)
+         : variant == kSingle ? launch_product<kMx, kSingle, kPhase>(p, tiles, m, s)
+                              : launch_product<kMx, kFew, kPhase>(p, tiles, m, s);
 }
 
 constexpr size_t up256(size_t n) { return (n + 255) / 256 * 256; }
@@ -1285,17 +1411,23 @@ dard_status dard_experts(const dard_experts_args* a, void* stream) {
   const cudaStream_t s = static_cast<cudaStream_t>(stream);
   const int stage = mx ? 128 : 64;
   cudaError_t e = std::getenv("DARD_TEST_FAIL_LAUNCH") ? cudaErrorLaunchFailure : cudaSuccess;
-  CUtensorMap ma, mb0, mb1;
+  Maps m = {};
   // phase 1: rows of x (in the plan's order, or gathered by the kernel itself) and of w1 and w3
   const uint64_t drow = static_cast<uint64_t>(a->dim) * esz, hrow = static_cast<uint64_t>(a->hidden) * esz;
   const uint64_t rows = static_cast<uint64_t>(q.row_tiles) * kTileM;
   const bool pair1 = q.variant1 == kPairs, pair2 = q.variant2 == kPairs;
   const uint32_t box1 = pair1 ? 128 : 64;
-  if (e == cudaSuccess && (!encode(&mb0, a->w1, mx, a->dim, a->hidden, a->experts, drow, box1) ||
-                           !encode(&mb1, a->w3, mx, a->dim, a->hidden, a->experts, drow, box1) ||
-                           (pair1 && !encode(&ma, p.xg, mx, a->dim, rows, 0, drow, kTileM))))
+  // tiles of scales of all rows of x or h (dtiles, htiles per row tile), and of the weights
+  const int64_t dtiles = (a->dim + 127) / 128, htiles = (a->hidden + 127) / 128;
+  const int64_t weight_tiles = a->experts * dtiles * htiles;
+  if (e == cudaSuccess && (!encode(&m.b0, a->w1, mx, a->dim, a->hidden, a->experts, drow, box1) ||
+                           !encode(&m.b1, a->w3, mx, a->dim, a->hidden, a->experts, drow, box1) ||
+                           (pair1 && !encode(&m.a, p.xg, mx, a->dim, rows, 0, drow, kTileM)) ||
+                           (pair1 && mx && (!encode_scales(&m.scales.a, p.xg_scale, q.row_tiles * dtiles) ||
+                                            !encode_scales(&m.scales.b0, a->w1_scale, weight_tiles) ||
+                                            !encode_scales(&m.scales.b1, a->w3_scale, weight_tiles)))))
     e = cudaErrorInvalidValue;
-  if (!pair1) ma = mb0;  // not used
+  if (!pair1) m.a = m.b0;  // not used
   if (e == cudaSuccess && pair1) {
     // Few pairs: several warps share a row of more than 2 KB, so that it is read in one go (800
     // rows of 4 KB: the call takes 106.4 us, with a warp per row 110.5).
@@ -1316,15 +1448,19 @@ dard_status dard_experts(const dard_experts_args* a, void* stream) {
     p.k_stages = (a->dim + stage - 1) / stage;
     p.splits = 1;
     p.split_stages = p.k_stages;
-    e = mx ? launch_phase<true, 1>(p, q.variant1, q.tiles1, ma, mb0, mb1, s)
-           : launch_phase<false, 1>(p, q.variant1, q.tiles1, ma, mb0, mb1, s);
+    e = mx ? launch_phase<true, 1>(p, q.variant1, q.tiles1, m, s)
+           : launch_phase<false, 1>(p, q.variant1, q.tiles1, m, s);
   }
   // phase 2: rows of h, rows of w2
   if (e == cudaSuccess &&
-      (!encode(&ma, p.h, mx, a->hidden, rows, 0, hrow, pair2 ? Shape<kPairs>::kBoxA : Shape<kSingle>::kBoxA) ||
-       !encode(&mb0, a->w2, mx, a->hidden, a->dim, a->experts, hrow, 128)))
+      (!encode(&m.a, p.h, mx, a->hidden, rows, 0, hrow, pair2 ? Shape<kPairs>::kBoxA : Shape<kSingle>::kBoxA) ||
+       !encode(&m.b0, a->w2, mx, a->hidden, a->dim, a->experts, hrow, 128) ||
+       (pair2 && mx && (!encode_scales(&m.scales.a, p.h_scale, q.row_tiles * htiles) ||
+                        !encode_scales(&m.scales.b0, a->w2_scale, weight_tiles)))))
     e = cudaErrorInvalidValue;
   if (e == cudaSuccess) {
+    m.b1 = m.b0;  // (not used; the scales' map serves both tiles of a pair's 256 columns)
+    m.scales.b1 = m.scales.b0;
     const int per = pair2 ? 256 : 128;
     p.scale_b[0] = a->w2_scale;
     p.a_scale = p.h_scale;
@@ -1334,8 +1470,8 @@ dard_status dard_experts(const dard_experts_args* a, void* stream) {
     p.k_stages = (a->hidden + stage - 1) / stage;
     p.splits = q.splits;
     p.split_stages = q.split_stages;
-    e = mx ? launch_phase<true, 2>(p, q.variant2, q.tiles2, ma, mb0, mb0, s)
-           : launch_phase<false, 2>(p, q.variant2, q.tiles2, ma, mb0, mb0, s);
+    e = mx ? launch_phase<true, 2>(p, q.variant2, q.tiles2, m, s)
+           : launch_phase<false, 2>(p, q.variant2, q.tiles2, m, s);
   }
   if (e == cudaSuccess && !p.direct && q.variant2 != kFew) {
     const Launch l(dim3(p.tokens, (p.dim / 4 + 127) / 128), 128, 0, s);
