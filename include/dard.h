@@ -359,7 +359,7 @@ typedef struct {
   uint8_t* y8_scale;         /* device [rows, y8_scale_stride] out, required with y8       */
   int32_t dtype;             /* dard_dtype of x, delta, weight, residual and y             */
   int32_t dim;               /* 1 .. DARD_NORM_MAX_DIM; a multiple of 32 with y8           */
-  int64_t rows;              /* >= 0                                                       */
+  int64_t rows;              /* 0 .. 2^31 - 1                                              */
   int64_t x_stride, delta_stride, residual_stride, y_stride, y8_stride, y8_scale_stride;
   float eps;                 /* >= 0, finite                                               */
 } dard_norm_args;
@@ -380,7 +380,7 @@ typedef struct {
                                 layout TILES [batch, ceil(rows/128), ceil(cols/128), 512]  */
   int32_t dtype;             /* dard_dtype of x                                            */
   int32_t layout;            /* dard_mx_scale_layout                                       */
-  int32_t batch, cols;       /* batch >= 0; cols a positive multiple of 32                 */
+  int32_t batch, cols;       /* batch >= 0; cols a positive multiple of 32; 2^40 elements  */
   int64_t rows;              /* of each matrix, >= 0                                       */
   int64_t x_row_stride, x_batch_stride;  /* elements                                       */
   int64_t scale_stride;      /* layout ROWS only: a multiple of 16, >= cols / 32           */

@@ -148,9 +148,11 @@ def experts(x, w1, w3, w2, ids, weights, mx, accumulate=2.0 ** -20):
     The tolerance bounds what fp32 arithmetic may change, element by element. A sum of products
     kept in fp32 is off by at most `accumulate` times the sum of the products' magnitudes.
     With g and u off by their bounds, h is off by 1.1 |u| dg + |silu(g)| du (silu's slope is
-    below 1.1) and 2^-20 of itself for the exponential and the division; its rounding then
-    gives a value between the roundings of h's two ends. Through w2, those differences, the sum's
-    own bound, and the routing weights."""
+    below 1.1) and 2^-20 of itself for the exponential and the division (an exponential whose
+    error grows with |g|, as the hardware's does, leaves that below g = -13, where silu is so small
+    that the first term covers it: dg is at least 2^-20 |g|); its rounding then gives a value
+    between the roundings of h's two ends. Through w2, those differences, the sum's own bound, and
+    the routing weights."""
     t, k = ids.shape
     y = np.zeros((t, x.shape[1]))
     tol = np.zeros_like(y)

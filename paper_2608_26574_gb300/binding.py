@@ -636,6 +636,7 @@ def dard_route_workspace_size(tokens: int, experts: int, top_k: int) -> int:
 class RouteCall:
     """``dard_route`` with a router's settings and its bias marshalled once.
 
+    With ``top_groups`` < ``groups`` a group's rank is the sum of its two largest choices.
     Call it with logits [tokens, experts] (bf16 or fp32, contiguous rows), ``ids`` and
     ``weights`` [tokens, top_k], and, for the plan that ``ExpertsCall`` reads, ``offsets``
     [experts + 1] and ``rows`` [tokens * top_k]. The workspace holds

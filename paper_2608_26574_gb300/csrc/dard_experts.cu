@@ -37,17 +37,20 @@
 //   TMEM: the accumulator, then the scales of two stages.
 //
 // Pairs read rows of x that an earlier launch (gather_rows) has put in the plan's order. For 4096
-// rows of one expert of 4096 x 12288 the call takes 378 us that way; with the rows gathered in
+// rows of one expert of 4096 x 12288 the call took 378 us that way (372 now); with the rows gathered in
 // phase 1 by cp.async from four warps 478, by TMA's row gather (tile::gather4) from four warps 448.
 // For few rows the copy's launch costs more than the gather does.
 //
 // What bounds it, on GB300: pairs, 3.27 PFLOP/s in MXFP8 at 4096 x 4096 x 12288, the tensor pipe
 // and shared memory together (with half of the weights' bytes left out it is 10 % faster, without
-// its stores 7 %); 8192 tokens x 8 of 64 experts of 4096 x 2048 1.46-1.60 ms (the clock
-// falls to 1600-1800 MHz at the power limit), of which gather_rows takes 75 us and combine 255 us, both
-// HBM's bytes. Few: the weights' bytes (32 tokens x 8 of 64 of
-// 2048 x 1024: 403 MB in 85 us; with no MMA at all 80) and for one token the chain of latencies
-// (22.7 us; its 52 MB alone would take 7.6).
+// its stores 7 %); 8192 tokens x 8 of 64 experts of 4096 x 2048 1.5-1.65 ms (the clock
+// falls to 1500-1800 MHz at the power limit), of which gather_rows takes 75 us and combine 255 us, both
+// HBM's bytes. Few: the weights' bytes (32 tokens x 8 of 64 of 2048 x 1024, 400 MB: 85 us where the
+// experts have as many rows each, with no MMA at all 80; 90-93 where some have more) and for one
+// token the chain of latencies (21.8 us for the two launches; its 52 MB alone would take 7.6).
+// bf16, with twice the weights' bytes and half the tensor rate: one token 27-32 us, 32 tokens 141
+// (5.6 TB/s), 1111 tokens x 6 of 40 of 2208 x 736 123, 800 rows of 4096 x 12288 184 (1.31 PFLOP/s),
+// 8192 tokens x 8 of 64 of 4096 x 2048 2.46-2.56 ms (1.3 PFLOP/s).
 //
 // Every wait is bounded; one that gives up sets DARD_STATUS_TIMEOUT and the abort flag of its CTA
 // (of both of a pair), on which every role leaves its loop. The producer (for a pair, rank 0's)
@@ -422,6 +425,10 @@ __device__ __forceinline__ void pin32(uint32_t (&r)[32]) {
                       "+r"(r[i + 5]), "+r"(r[i + 6]), "+r"(r[i + 7]));
 }
 
+// g / (1 + exp(-g)) by the hardware's exponential and division: off by about 2 + 1.2 |g| units in
+// fp32's last place, and 0 below g = -87, where it is less than 2^-118. h is rounded to 8 bits (bf16)
+// or 4 right after. With expf one token takes 23.7 us instead of 23.0 and 800 rows of 4096 x 12288
+// 119.3 instead of 117.5; with expf and an IEEE division 43 and 130.
 __device__ __forceinline__ float silu(float g) { return __fdividef(g, 1.f + __expf(-g)); }
 
 __device__ __forceinline__ uint32_t pack2(float lo, float hi) {
@@ -1257,13 +1264,16 @@ struct Plan {
 };
 
 // Few tokens (few rows per expert): kFew, in both phases (against kSingle, 8 of 64
-// experts of 2048 x 1024: 1 token 22.6 / 23.1 us, 8 57 / 66, 32 85 / 87). Else pairs of CTAs, unless their
+// experts of 2048 x 1024: 1 token 22.0 / 22.4 us, 8 51 / 62, 32 85 / 87, or 90 / 88 where some experts
+// have more rows than others; bf16 26.9 / 32.3, 80 / 94, 140 / 146). Else pairs of CTAs, unless their
 // tiles (their count, over the row tiles that the call can have) are fewer than the pairs of SMs,
 // or than half of those where the experts have full row tiles on average: then single ones. (800
-// rows of one expert, phase 2 of 4096 x 12288, 64 tiles: 109 against 118 us for the call; 200 rows
-// of 8 experts, 1536 x 768, 48 and 48 tiles: 19.0 against 16.5 us.) Where even single tiles leave
+// rows of one expert, phase 2 of 4096 x 12288, 64 tiles: 109 against 118 us for the call; both phases
+// 107 against 150, bf16 186 against 263; 200 rows of 8 experts, 1536 x 768, 48 and 48 tiles: 18.2
+// against 16.5 us, bf16 23.4 against 22.1.) Where even single tiles leave
 // SMs idle in phase 2 (few rows, a long reduction), the reduction is split, into runs of at least
-// four stages (one expert of 4096 x 12288: 1 row 41.5 us, whole 51.1; 100 rows 57, whole 74).
+// four stages (one expert of 4096 x 12288: 1 row 39.4 us, whole 50.8, bf16 59.6, 84.8; 100 rows
+// 55.8, whole 72.9, bf16 86, 128).
 Plan make_plan(int64_t tokens, int experts, int top_k, int dim, int hidden, bool mx) {
   Plan q = {};
   q.pairs = tokens * top_k;

@@ -186,7 +186,7 @@ __global__ void __launch_bounds__(kWarps == 1 ? 128 : 32 * kWarps)
 // row per CTA of kWarps warps, element t + j threads of the row with thread t, so that a warp
 // accesses 32 consecutive elements and holds one MX block. 1777 x 2731 fp32 (78 MB)
 // takes 15 us. Where norm_rows can be used it is the faster one: 38912 x 4096 bf16 207 us
-// against 438 here, whose accesses are an eighth as wide.
+// against 438 here, whose accesses are an eighth as wide, so that it is bound by their number.
 template <typename T, int kWarps, int kElems>
 __global__ void __launch_bounds__(32 * kWarps) norm_rows_any(const __grid_constant__ NormParams p) {
   constexpr int kThreads = 32 * kWarps;
@@ -405,8 +405,8 @@ __global__ void __launch_bounds__(256) mx_rows(const __grid_constant__ MxParams 
   }
 }
 
-// Rows that 16-byte accesses cannot take: one block per warp, one element per lane (64 x 2048 x
-// 2048 bf16 would take 1.2 ms this way).
+// Rows that 16-byte accesses cannot take: one block per warp, one element per lane, bound by the
+// instructions around each block (64 x 2048 x 2048 bf16 would take 1.2 ms this way).
 template <typename T>
 __global__ void __launch_bounds__(256) mx_rows_any(const __grid_constant__ MxParams p) {
   const int lane = threadIdx.x & 31, blocks = p.cols / kMxBlock;
