@@ -44,6 +44,8 @@ class ExpertMLP:
     def __init__(self, w1, w3, w2, router, top_k: int, norm_weight=None, eps: float = 1e-6,
                  mx: bool = True, route: dict | None = None, status=None,
                  workspaces: dict | None = None):
+        if not router.is_cuda:
+            raise ValueError("router: device tensor expected")
         self.experts, self.hidden, self.dim = w1.shape
         self.top_k, self.dtype, self.mx = top_k, router.dtype, mx
         if not mx and router.dtype != torch.bfloat16:

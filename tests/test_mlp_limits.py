@@ -3,8 +3,10 @@ pointers are never followed)."""
 import ctypes
 
 import pytest
+import torch
 
 from paper_2608_26574_gb300 import binding as B
+from paper_2608_26574_gb300.experts import ExpertMLP
 
 from .test_mlp_abi import (ALIGN, SHAPE, WORKSPACE, _experts, _mx, _refuse, _route,
                            lib)  # noqa: F401 (lib: a fixture)
@@ -57,3 +59,10 @@ def test_experts_workspace_serves_every_smaller_count(lib, experts, top_k, dim, 
             a.dtype, a.tokens, a.experts, a.top_k, a.dim, a.hidden = dtype, t, experts, top_k, dim, hidden
             a.x_stride, a.y_stride, a.x_scale_stride = dim, dim, (dim + 511) // 512 * 16
             _refuse(lib, "dard_experts", a, dict(workspace_bytes=size, workspace=8), ALIGN)
+
+
+@pytest.mark.parametrize("mx", [True, False])
+def test_a_layer_of_host_tensors_is_refused(mx):
+    w = torch.zeros(2, 96, 64, dtype=torch.bfloat16)
+    with pytest.raises(ValueError, match="device tensor"):
+        ExpertMLP(w, w, w.mT.contiguous(), torch.zeros(64, 2, dtype=torch.bfloat16), 1, mx=mx)
