@@ -496,6 +496,128 @@ size_t dard_experts_workspace_size(int32_t tokens, int32_t experts, int32_t top_
  * Errors: DARD_ERR_NULL, _SHAPE, _VALUE (dtype), _ALIGN, _WORKSPACE, _CUDA. */
 dard_status dard_experts(const dard_experts_args* args, void* stream);
 
+/* ------------------------------------------------------------------------------------- *
+ * Decoding behind a shared prefix. The paper has no counterpart: these are interface additions,
+ * for batches whose sequences all follow one prefix (a system prompt, an image, a document)
+ * whose keys and values are kept in a cache, once for all:
+ *
+ *   dard_prefix_attention  a step's attention over the prefix and each sequence's own rows
+ *   dard_prefix_weights    the attention weight that each key of the prefix has received
+ *   dard_prefix_evict      the keys to keep by that weight, moved together
+ *
+ * The cache of a layer: prefix_k and prefix_v, prefix_len rows of hkv heads of head_dim elements;
+ * row r of head g starts at element r * prefix_row_stride + g * prefix_head_stride (so that
+ * [rows, hkv, head_dim], [hkv, rows, head_dim] and slices of wider buffers all serve). Keys carry
+ * their positions (RoPE applied); after an eviction the heads hold different positions.
+ * Pointers are 16-byte aligned, strides multiples of 16 bytes and positive.
+ * ------------------------------------------------------------------------------------- */
+
+/* For every query row r of sequence i and head h, with c the scale and g = h / (hq / hkv):
+ *     z_j  = c <q[r,h], prefix_k[j,g]>   for every row j of the prefix
+ *     z'_j = c <q[r,h], k[key(r,j),g]>   for every position j of the sequence's own rows, the
+ *                                        copy key(r,j) chosen as in dard_step_attention
+ *     lse[r,h] = log(sum_j exp(z_j) + sum_j exp(z'_j))
+ *     o[r,h]   = sum_j exp(z_j - lse) prefix_v[j,g] + sum_j exp(z'_j - lse) v[key(r,j),g]
+ * The query rows of all sequences, times the heads that share a key/value head, are one run of
+ * queries against the prefix, so that the prefix is read once for many sequences of few rows;
+ * where there are few queries the keys are split over the SMs and the parts joined.
+ * A key that a row does not see (the other copy of a position, another sequence's rows) does not
+ * enter its output, whatever it holds; a NaN or an infinity in a key or value that a row sees does.
+ * Rows that are no query rows (before query_start, and shadow rows with an invalid shadow_src) are
+ * left as they were in o and in lse.
+ * Arithmetic: as dard_step_attention (probabilities rounded to bf16 for the product with the
+ * values when dtype is BF16; the normaliser in lse is that of the unrounded ones). */
+typedef struct {
+  dard_attn_args own;        /* the sequences' own rows, as dard_step_attention takes them;
+                                rope_theta must be 0 (q and k carry their positions)       */
+  const void* prefix_k;      /* device, dtype of own; not read when prefix_len is 0        */
+  const void* prefix_v;
+  int64_t prefix_row_stride, prefix_head_stride;  /* elements, of both                     */
+  int32_t prefix_len;        /* 0 .. DARD_PREFIX_MAX_LEN                                   */
+  float* lse;                /* optional device [total_rows, hq] out                       */
+  void* workspace;           /* optional device scratch of
+                                dard_prefix_attention_workspace_size() bytes, 16-byte aligned;
+                                needs no preparation. Without it the keys are not split.
+                                Calls that overlap on the GPU need separate workspaces.    */
+  size_t workspace_bytes;
+} dard_prefix_attn_args;
+#define DARD_PREFIX_MAX_LEN (1 << 30)
+
+/* Bytes of workspace for these sizes or smaller ones, any dtype and batch (0 on invalid sizes). */
+size_t dard_prefix_attention_workspace_size(int32_t total_rows, int32_t hq, int32_t hkv,
+                                            int32_t head_dim, int32_t prefix_len);
+
+/* One launch, or two where the keys are split. Errors: DARD_ERR_NULL, _SHAPE, _VALUE (as
+ * dard_step_attention; rope_theta not 0), _UNSUPPORTED, _ALIGN, _WORKSPACE (smaller than
+ * needed), _CUDA. */
+dard_status dard_prefix_attention(const dard_prefix_attn_args* args, void* stream);
+
+/* The attention weight that the keys of the prefix have received, per key/value head g and key j:
+ *     weights[g,j] = decay * weights_in[g,j] + sum_{r, h of group g} exp(c <q[r,h], prefix_k[j,g]>
+ *                                                                       - lse[r,h])
+ * over every row r of q (lse as dard_prefix_attention writes it). A row whose lse is +inf adds
+ * nothing, whatever its q holds: fill lse with +inf once, and rows that are no queries stay out.
+ * Without weights_in the first term is 0. Sums are fp32 in a fixed order: equal calls give equal
+ * bits. */
+typedef struct {
+  const void* q;             /* device [rows, hq, head_dim], contiguous                    */
+  const float* lse;          /* device [rows, hq], contiguous                              */
+  const void* prefix_k;      /* device, dtype of q                                         */
+  const float* weights_in;   /* optional device [hkv, prefix_len]; may be weights          */
+  float* weights;            /* device [hkv, prefix_len] out                               */
+  int64_t prefix_row_stride, prefix_head_stride;           /* elements                     */
+  int64_t weights_in_stride, weights_stride;  /* elements between heads, >= prefix_len     */
+  int32_t dtype;             /* dard_dtype of q and prefix_k                               */
+  int32_t rows;              /* >= 0                                                       */
+  int32_t hq, hkv, head_dim; /* as dard_step_attention                                     */
+  int32_t prefix_len;        /* 0 .. DARD_PREFIX_MAX_LEN                                   */
+  float scale;               /* softmax scale; 0 means 1/sqrt(head_dim)                    */
+  float decay;               /* finite                                                     */
+  uint32_t* status;          /* optional device word: DARD_STATUS_TIMEOUT                  */
+  void* workspace;           /* optional device scratch of
+                                dard_prefix_weights_workspace_size() bytes, 16-byte aligned;
+                                needs no preparation. Without it the rows are not split. Calls
+                                that overlap on the GPU need separate workspaces.          */
+  size_t workspace_bytes;
+} dard_prefix_weights_args;
+
+/* Bytes of workspace for these sizes or smaller ones, any dtype (0 on invalid sizes). */
+size_t dard_prefix_weights_workspace_size(int32_t rows, int32_t hq, int32_t hkv, int32_t head_dim,
+                                          int32_t prefix_len);
+
+/* One launch, or two where the rows are split. Errors: DARD_ERR_NULL, _SHAPE, _VALUE,
+ * _UNSUPPORTED, _ALIGN, _WORKSPACE, _CUDA. */
+dard_status dard_prefix_weights(const dard_prefix_weights_args* args, void* stream);
+
+/* Per key/value head g, `keep` of the prefix's keys: the first keep_first, the last keep_last, and
+ * of those in between the keep - keep_first - keep_last with the largest weights (of equal weights
+ * the lowest index; -0 equals 0; a NaN counts as smaller than every number). kept[g] lists them in
+ * rising order, and
+ *     k_out[i,g] = k[kept[g,i],g],   v_out[i,g] = v[kept[g,i],g],   weights_out[g,i] =
+ *     weights[g,kept[g,i]]
+ * The outputs must not overlap the inputs. */
+typedef struct {
+  const float* weights;      /* device [hkv, prefix_len]                                   */
+  const void* prefix_k;      /* device, both optional together                             */
+  const void* prefix_v;
+  int32_t* kept;             /* device [hkv, keep] out, contiguous                         */
+  void* k_out;               /* device out, required with prefix_k                         */
+  void* v_out;
+  float* weights_out;        /* optional device [hkv, keep] out, contiguous                */
+  int64_t weights_stride;    /* elements between heads, >= prefix_len                      */
+  int64_t prefix_row_stride, prefix_head_stride;  /* elements, of prefix_k and prefix_v    */
+  int64_t out_row_stride, out_head_stride;        /* elements, of k_out and v_out          */
+  int32_t dtype;             /* dard_dtype of the keys and values                          */
+  int32_t hkv, head_dim;     /* head_dim 64 or 128                                         */
+  int32_t prefix_len;        /* 0 .. DARD_PREFIX_MAX_LEN                                   */
+  int32_t keep;              /* keep_first + keep_last .. prefix_len                       */
+  int32_t keep_first, keep_last;  /* >= 0                                                  */
+} dard_prefix_evict_args;
+
+/* Two launches, the second a programmatic dependent of the first. Errors: DARD_ERR_NULL, _SHAPE,
+ * _VALUE (dtype; an output that overlaps an input), _UNSUPPORTED, _ALIGN, _CUDA. */
+dard_status dard_prefix_evict(const dard_prefix_evict_args* args, void* stream);
+
 /* Human-readable name of a status code; never NULL. */
 const char* dard_status_string(dard_status s);
 

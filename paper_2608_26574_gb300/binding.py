@@ -28,6 +28,7 @@ ROUTE_SOFTMAX, ROUTE_SIGMOID = 0, 1
 MX_BLOCK = 32
 NORM_MAX_DIM, MAX_EXPERTS, MAX_TOP_K, MAX_GROUPS = 32768, 512, 32, 32
 EXPERTS_MAX_PAIRS = 1 << 24  # tokens * top_k of one dard_experts call
+PREFIX_MAX_LEN = 1 << 30
 
 _I32P = ctypes.POINTER(ctypes.c_int32)
 
@@ -102,6 +103,34 @@ class ExpertsArgs(ctypes.Structure):
                  ("status", ctypes.c_void_p)])
 
 
+class PrefixAttnArgs(ctypes.Structure):
+    _fields_ = [("own", AttnArgs), ("prefix_k", ctypes.c_void_p), ("prefix_v", ctypes.c_void_p),
+                ("prefix_row_stride", ctypes.c_int64), ("prefix_head_stride", ctypes.c_int64),
+                ("prefix_len", ctypes.c_int32), ("lse", ctypes.c_void_p),
+                ("workspace", ctypes.c_void_p), ("workspace_bytes", ctypes.c_size_t)]
+
+
+class PrefixWeightsArgs(ctypes.Structure):
+    _fields_ = ([(n, ctypes.c_void_p) for n in ("q", "lse", "prefix_k", "weights_in", "weights")] +
+                [(n, ctypes.c_int64) for n in ("prefix_row_stride", "prefix_head_stride",
+                                               "weights_in_stride", "weights_stride")] +
+                [(n, ctypes.c_int32) for n in ("dtype", "rows", "hq", "hkv", "head_dim",
+                                               "prefix_len")] +
+                [("scale", ctypes.c_float), ("decay", ctypes.c_float),
+                 ("status", ctypes.c_void_p), ("workspace", ctypes.c_void_p),
+                 ("workspace_bytes", ctypes.c_size_t)])
+
+
+class PrefixEvictArgs(ctypes.Structure):
+    _fields_ = ([(n, ctypes.c_void_p) for n in ("weights", "prefix_k", "prefix_v", "kept", "k_out",
+                                                "v_out", "weights_out")] +
+                [(n, ctypes.c_int64) for n in ("weights_stride", "prefix_row_stride",
+                                               "prefix_head_stride", "out_row_stride",
+                                               "out_head_stride")] +
+                [(n, ctypes.c_int32) for n in ("dtype", "hkv", "head_dim", "prefix_len", "keep",
+                                               "keep_first", "keep_last")])
+
+
 class DardError(RuntimeError):
     def __init__(self, code: int, fn: str, message: str):
         super().__init__(f"{fn} failed: {status_string(code)}: {message}")
@@ -131,6 +160,11 @@ EXPORTS = {
     "dard_route": (ctypes.c_int, [ctypes.POINTER(RouteArgs), ctypes.c_void_p]),
     "dard_experts_workspace_size": (ctypes.c_size_t, [ctypes.c_int32] * 5),
     "dard_experts": (ctypes.c_int, [ctypes.POINTER(ExpertsArgs), ctypes.c_void_p]),
+    "dard_prefix_attention_workspace_size": (ctypes.c_size_t, [ctypes.c_int32] * 5),
+    "dard_prefix_attention": (ctypes.c_int, [ctypes.POINTER(PrefixAttnArgs), ctypes.c_void_p]),
+    "dard_prefix_weights_workspace_size": (ctypes.c_size_t, [ctypes.c_int32] * 5),
+    "dard_prefix_weights": (ctypes.c_int, [ctypes.POINTER(PrefixWeightsArgs), ctypes.c_void_p]),
+    "dard_prefix_evict": (ctypes.c_int, [ctypes.POINTER(PrefixEvictArgs), ctypes.c_void_p]),
     "dard_status_string": (ctypes.c_char_p, [ctypes.c_int]),
     "dard_last_error": (ctypes.c_char_p, []),
     "dard_version": (ctypes.c_int32, []),
@@ -773,3 +807,230 @@ def dard_experts(x, x_scale, w1, w1_scale, w3, w3_scale, w2, w2_scale, ids, weig
     """The experts' products of every token, weighted and added, see ``ExpertsCall``."""
     ExpertsCall(w1, w1_scale, w3, w3_scale, w2, w2_scale, workspace, status)(
         x, x_scale, ids, weights, offsets, rows, y, stream)
+
+
+# ------------------------------------------------------------------ decoding behind a shared prefix
+def _launch(fn, name: str, args, stream, device: int):
+    """Calls the library on ``device``, the current one or another."""
+    torch = _torch()
+    if torch.cuda.current_device() != device:
+        with torch.cuda.device(device):
+            return _check(fn(args, _stream_handle(stream, device)), name)
+    _check(fn(args, _stream_handle(stream, device)), name)
+
+
+def _cache(t, name: str, device: int, dtype, hkv: int, head_dim: int) -> tuple[int, int, int]:
+    """(pointer, row stride, head stride) of one of a layer's cached tensors [rows, hkv, head_dim]
+    with contiguous heads and any row and head strides."""
+    shape = t.shape
+    if t.dtype != dtype or t.get_device() != device or device < 0:
+        _is_dtype(t, name, (dtype,))
+        raise ValueError(f"{name}: tensor on device {device} expected")
+    if len(shape) != 3 or shape[1] != hkv or shape[2] != head_dim:
+        raise ValueError(f"{name}: [rows, {hkv}, {head_dim}] expected, got {tuple(shape)}")
+    rs, hs, es = t.stride()
+    if es != 1:
+        raise ValueError(f"{name}: contiguous heads expected")
+    # (a stride that no step uses may be anything: one that is in order is passed)
+    if shape[0] <= 1:
+        rs = hkv * head_dim
+    if hkv == 1:
+        hs = head_dim
+    if rs < head_dim or hs < head_dim:
+        raise ValueError(f"{name}: heads overlap (strides {t.stride()})")
+    return t.data_ptr(), rs, hs
+
+
+def _caches(k, v, names: tuple, device: int, dtype, hkv: int, head_dim: int):
+    """(k's pointer, v's, row stride, head stride) of a layer's keys and values."""
+    kp, rs, hs = _cache(k, names[0], device, dtype, hkv, head_dim)
+    vp, rv, hv = _cache(v, names[1], device, dtype, hkv, head_dim)
+    if k.shape[0] != v.shape[0] or rs != rv or hs != hv:
+        raise ValueError(f"{names[0]} and {names[1]} need one shape and the same strides")
+    return kp, vp, rs, hs
+
+
+def _workspace(t) -> tuple[int, int, int | None]:
+    """(pointer, bytes, device) of an optional workspace tensor."""
+    if t is None:
+        return 0, 0, None
+    return (_dev(t, "workspace", 0, t.dtype), t.numel() * t.element_size(), t.get_device())
+
+
+def dard_prefix_attention_workspace_size(total_rows: int, hq: int, hkv: int, head_dim: int,
+                                         prefix_len: int) -> int:
+    return int(lib().dard_prefix_attention_workspace_size(total_rows, hq, hkv, head_dim, prefix_len))
+
+
+class PrefixAttentionCall:
+    """``dard_prefix_attention`` with one step's metadata, mask inputs and workspace marshalled once.
+
+    The metadata are those of ``AttentionCall`` and describe the sequences' own rows; the prefix that
+    all of them follow comes with each call. Call it with q and o [rows, hq, d], k and v [rows, hkv,
+    d] (contiguous, positions applied), prefix_k and prefix_v [prefix_len, hkv, d] (contiguous heads,
+    any row and head strides that are multiples of 16 bytes) and, for ``PrefixWeightsCall``, lse
+    [rows, hq] in fp32. Rows that are no query rows are left as they were in o and lse.
+
+    ``workspace`` holds ``dard_prefix_attention_workspace_size`` bytes and needs no preparation; calls
+    that overlap on the GPU need their own. Without one, few query rows behind a long prefix run on
+    few SMs. Threads may share the call where they may share its workspace."""
+
+    # dard_prefix_attn_args
+    layout = struct.Struct("=4Q5i4x7Qf4xQQfiQ" "QQqqi4xQQQ")
+
+    def __init__(self, n_orig, block_start, block_len, shadow_len, state, prev_conf, shadow_src,
+                 scale: float = 0.0, status=None, query_start=None, workspace=None):
+        torch = _torch()
+        self._host = [_host_i32(x) for x in (n_orig, block_start, block_len, shadow_len)]
+        qs = _host_i32(query_start) if query_start is not None else None
+        n, _, bl, sl = self._host
+        ns = len(n)
+        if any(len(x) != ns for x in self._host) or (qs is not None and len(qs) != ns):
+            raise ValueError("per-sequence arrays differ in length")
+        self.rows = int(n.astype(np.int64).sum() + sl.astype(np.int64).sum())
+        blk, sh = int(bl.astype(np.int64).sum()), int(sl.astype(np.int64).sum())
+        self.device = next((t.get_device() for t in (state, prev_conf, shadow_src, status, workspace)
+                            if t is not None), None)
+        ws, ws_bytes, ws_dev = _workspace(workspace)
+        if ws_dev is not None and ws_dev != self.device:
+            raise ValueError(f"workspace: on device {ws_dev}, expected {self.device}")
+        self._mid = (ns, *(x.ctypes.data for x in self._host),
+                     _dev(state, "state", blk, torch.uint8) or 0,
+                     _dev(prev_conf, "prev_conf", blk, torch.float32, self.device) or 0,
+                     _dev(shadow_src, "shadow_src", sh, torch.int32, self.device) or 0, scale,
+                     _dev(status, "status", 1, torch.int32, self.device) or 0,
+                     qs.ctypes.data if qs is not None else 0, 0.0, 0, 0)
+        self._scratch = (ws, ws_bytes)
+        self._keep = (state, prev_conf, shadow_src, status, workspace, qs)
+        self._fn = _packed_fn("dard_prefix_attention")
+
+    def __call__(self, q, k, v, o, prefix_k, prefix_v, lse=None, stream=None):
+        qs, ks, dt, dev = q.shape, k.shape, q.dtype, q.get_device()
+        if not (len(qs) == 3 and len(ks) == 3 and o.shape == qs and v.shape == ks and ks[2] == qs[2]
+                and qs[0] >= self.rows and ks[0] >= self.rows):
+            raise ValueError(f"q/o [>={self.rows}, hq, d] and k/v [>={self.rows}, hkv, d] expected, got "
+                             f"{tuple(qs)}, {tuple(ks)}, {tuple(v.shape)}, {tuple(o.shape)}")
+        if dev < 0 or (self.device is not None and dev != self.device):
+            raise ValueError(f"q: device tensor expected, on the mask inputs' device {self.device}")
+        for name, t in (("q", q), ("k", k), ("v", v), ("o", o)):
+            if t.dtype != dt or t.get_device() != dev or not t.is_contiguous():
+                raise ValueError(f"{name}: contiguous {dt} tensor on device {dev} expected")
+        kp, vp, rs, hs = _caches(prefix_k, prefix_v, ("prefix_k", "prefix_v"), dev, dt, ks[1], ks[2])
+        lp = 0
+        if lse is not None:
+            if lse.dim() != 2 or lse.shape[0] < self.rows or lse.shape[1] != qs[1]:
+                raise ValueError(f"lse: [>={self.rows}, {qs[1]}] expected, got {tuple(lse.shape)}")
+            lp = _flat(lse, "lse", _dtypes("f32"), dev)
+        args = self.layout.pack(q.data_ptr(), k.data_ptr(), v.data_ptr(), o.data_ptr(),
+                                _dtype_code(q), qs[1], ks[1], qs[2], *self._mid, kp, vp, rs, hs,
+                                prefix_k.shape[0], lp, *self._scratch)
+        _launch(self._fn, "dard_prefix_attention", args, stream, dev)
+
+
+def dard_prefix_attention(q, k, v, o, prefix_k, prefix_v, n_orig, block_start, block_len, shadow_len,
+                          state, prev_conf, shadow_src, scale: float = 0.0, status=None,
+                          query_start=None, lse=None, workspace=None, stream=None):
+    """Masked attention of one layer over a shared prefix and each sequence's own rows, see
+    ``PrefixAttentionCall``."""
+    PrefixAttentionCall(n_orig, block_start, block_len, shadow_len, state, prev_conf, shadow_src,
+                        scale, status, query_start, workspace)(q, k, v, o, prefix_k, prefix_v, lse,
+                                                               stream)
+
+
+def dard_prefix_weights_workspace_size(rows: int, hq: int, hkv: int, head_dim: int,
+                                       prefix_len: int) -> int:
+    return int(lib().dard_prefix_weights_workspace_size(rows, hq, hkv, head_dim, prefix_len))
+
+
+class PrefixWeightsCall:
+    """``dard_prefix_weights`` with its settings and workspace marshalled once.
+
+    Call it with q [rows, hq, d] (contiguous), lse [rows, hq] as ``PrefixAttentionCall`` wrote it
+    (+inf: the row adds nothing), prefix_k [prefix_len, hkv, d] and weights [hkv, prefix_len] in
+    fp32 (contiguous rows), which receive the sums, plus ``decay`` times ``weights_in`` (which may be
+    weights) if it is given. The workspace holds ``dard_prefix_weights_workspace_size`` bytes and
+    needs no preparation; without one, many rows over a short prefix run on few SMs."""
+
+    layout = struct.Struct("=5Q4q6iffQQQ")  # dard_prefix_weights_args
+
+    def __init__(self, scale: float = 0.0, decay: float = 1.0, workspace=None, status=None):
+        torch = _torch()
+        self._settings = (scale, decay)
+        ws, ws_bytes, dev = _workspace(workspace)
+        self.device = dev if dev is not None else None if status is None else status.get_device()
+        self._scratch = (_dev(status, "status", 1, torch.int32, self.device) or 0, ws, ws_bytes)
+        self._keep = (workspace, status)
+        self._fn = _packed_fn("dard_prefix_weights")
+
+    def __call__(self, q, lse, prefix_k, weights, weights_in=None, stream=None):
+        shape, dev = q.shape, q.get_device()
+        if len(shape) != 3 or dev < 0 or not q.is_contiguous():
+            raise ValueError("q: contiguous device tensor [rows, hq, d] expected")
+        if self.device is not None and dev != self.device:
+            raise ValueError(f"q: on device {dev}, expected {self.device}")
+        rows, hq, d = shape
+        if lse.shape != (rows, hq):
+            raise ValueError(f"lse: [{rows}, {hq}] expected, got {tuple(lse.shape)}")
+        lp = _flat(lse, "lse", _dtypes("f32"), dev)
+        if prefix_k.dim() != 3:
+            raise ValueError(f"prefix_k: [rows, hkv, {d}] expected, got {tuple(prefix_k.shape)}")
+        hkv, length = prefix_k.shape[1], prefix_k.shape[0]
+        kp, rs, hs = _cache(prefix_k, "prefix_k", dev, q.dtype, hkv, d)
+        wp, wstride = _rows2(weights, "weights", (hkv, length), _dtypes("f32"), dev)
+        ip, istride = (_rows2(weights_in, "weights_in", (hkv, length), _dtypes("f32"), dev)
+                       if weights_in is not None else (0, 0))
+        args = self.layout.pack(q.data_ptr(), lp, kp, ip, wp, rs, hs, istride, wstride,
+                                _dtype_code(q), rows, hq, hkv, d, length, *self._settings,
+                                *self._scratch)
+        _launch(self._fn, "dard_prefix_weights", args, stream, dev)
+
+
+def dard_prefix_weights(q, lse, prefix_k, weights, weights_in=None, scale: float = 0.0,
+                        decay: float = 1.0, workspace=None, status=None, stream=None):
+    """The attention weight that each key of the prefix has received, see ``PrefixWeightsCall``."""
+    PrefixWeightsCall(scale, decay, workspace, status)(q, lse, prefix_k, weights, weights_in, stream)
+
+
+class PrefixEvictCall:
+    """``dard_prefix_evict`` with the fixed ends marshalled once.
+
+    Call it with weights [hkv, prefix_len] in fp32 (contiguous rows), prefix_k and prefix_v
+    [prefix_len, hkv, d], and the outputs ``kept`` [hkv, keep] (int32), ``k_out`` and ``v_out``
+    [keep, hkv, d] (contiguous heads, any row and head strides) and, optionally, ``weights_out``
+    [hkv, keep]. The outputs must not overlap the inputs."""
+
+    layout = struct.Struct("=7Q5q7i4x")  # dard_prefix_evict_args
+
+    def __init__(self, keep_first: int = 0, keep_last: int = 0):
+        self._ends = (keep_first, keep_last)
+        self._fn = _packed_fn("dard_prefix_evict")
+
+    def __call__(self, weights, prefix_k, prefix_v, kept, k_out, v_out, weights_out=None, stream=None):
+        dev = prefix_k.get_device()
+        if dev < 0 or prefix_k.dim() != 3:
+            raise ValueError("prefix_k: device tensor [rows, hkv, d] expected")
+        length, hkv, d = prefix_k.shape
+        dt = prefix_k.dtype
+        code = _dtype_code(prefix_k)
+        wp, wstride = _rows2(weights, "weights", (hkv, length), _dtypes("f32"), dev)
+        kp, vp, rs, hs = _caches(prefix_k, prefix_v, ("prefix_k", "prefix_v"), dev, dt, hkv, d)
+        ko, vo, ors, ohs = _caches(k_out, v_out, ("k_out", "v_out"), dev, dt, hkv, d)
+        keep = k_out.shape[0]
+        if kept.shape != (hkv, keep):
+            raise ValueError(f"kept: [{hkv}, {keep}] expected, got {tuple(kept.shape)}")
+        ip = _flat(kept, "kept", _dtypes("i32"), dev)
+        op = 0
+        if weights_out is not None:
+            if weights_out.shape != (hkv, keep):
+                raise ValueError(f"weights_out: [{hkv}, {keep}] expected, got {tuple(weights_out.shape)}")
+            op = _flat(weights_out, "weights_out", _dtypes("f32"), dev)
+        args = self.layout.pack(wp, kp, vp, ip, ko, vo, op, wstride, rs, hs, ors, ohs, code, hkv, d,
+                                length, keep, *self._ends)
+        _launch(self._fn, "dard_prefix_evict", args, stream, dev)
+
+
+def dard_prefix_evict(weights, prefix_k, prefix_v, kept, k_out, v_out, weights_out=None,
+                      keep_first: int = 0, keep_last: int = 0, stream=None):
+    """The prefix's keys with the largest weights, moved together, see ``PrefixEvictCall``."""
+    PrefixEvictCall(keep_first, keep_last)(weights, prefix_k, prefix_v, kept, k_out, v_out,
+                                           weights_out, stream)

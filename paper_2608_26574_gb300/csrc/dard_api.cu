@@ -52,15 +52,13 @@ const char* dard_status_string(dard_status s) {
 
 const char* dard_last_error(void) { return g_err; }
 
-int32_t dard_version(void) { return 20200; }
+int32_t dard_version(void) { return 20300; }
 
 }  // extern "C"
 
-namespace {
-
 // Host-side validation of an attention call and its launch plan (the per-sequence
 // descriptors, the longest-first work order and the kernel parameters). Touches no device.
-dard_status prepare_attention(const dard_attn_args* a, dard::AttnParams& p) {
+dard_status dard::prepare_attention(const dard_attn_args* a, dard::AttnParams& p) {
   using namespace dard;
   if (!a) return fail(DARD_ERR_NULL, "args is NULL");
   if (!a->q || !a->k || !a->v || !a->o) return fail(DARD_ERR_NULL, "q, k, v or o is NULL");
@@ -177,8 +175,6 @@ dard_status prepare_attention(const dard_attn_args* a, dard::AttnParams& p) {
   }
   return DARD_OK;
 }
-
-}  // namespace
 
 // Host-side validation of a scoring call and its kernel parameters (no device access).
 dard_status dard::prepare_score(const dard_score_args* a, dard::ScoreParams& p) {

@@ -84,6 +84,8 @@ cudaError_t launch_pair_attention(const AttnParams& p, cudaStream_t stream);
 cudaError_t launch_simt_attention(const AttnParams& p, cudaStream_t stream);
 int pair_clusters_for(const AttnParams& p);
 
+// Validates an attention call and fills its kernel parameters; touches no device memory.
+dard_status prepare_attention(const dard_attn_args* a, AttnParams& p);
 dard_status launch_attention(const dard_attn_args& a, AttnParams& p, cudaStream_t stream,
                              char* err, size_t err_len);
 

@@ -1,0 +1,814 @@
+// dard_prefix_attn.cu - attention of a decoding step over a prefix that the batch shares and each
+// sequence's own rows (dard_prefix_attention): validation, the split of the keys, the bf16 kernel
+// on the tensor cores and the kernel that joins the parts of a split.
+//
+// prefix_tc: 128 packed queries (dard_prefix.cuh) of one key/value head against a run of key
+// tiles of 128: first the prefix's, with no mask but the ragged end of the last, then the rows of
+// the sequences that the tile touches, under each row's mask. One pass with a running maximum and
+// sum (the probabilities never leave the chip), fp32 accumulators. 12 warps:
+//   warps 0-7  softmax and epilogue: warps w and w + 4 share TMEM lane quarter w (queries 32w ..
+//              32w + 31), each taking 64 of a tile's 128 keys;
+//   warp 8     TMA producer: K and V through 3 stages each;
+//   warp 9     TMEM allocator and PV issuer: O += P_j V_j, P_j (bf16) read from TMEM;
+//   warp 10    S issuer: S_j = Q K_j^T (Q from TMEM, K from shared memory) into a ring of two
+//              128-column TMEM buffers;
+//   warp 11    own tiles only: looks for NaN and infinities in V (below).
+// TMEM: S ring [0, 256), O [256, 256 + D), P [384, 448), Q [448, 448 + D/2).
+//
+// Values that are not finite: the product with V multiplies every key of a tile by every query's
+// weight, and 0 times NaN is NaN. Keys of the prefix are seen by every query (rows behind its end
+// arrive as zeros), but an own tile holds copies and sequences that a query does not see. Warp 11
+// takes such values out of V before the product and adds them to the queries that do see the key.
+#include <algorithm>
+#include <cstdio>
+#include <cstdlib>
+#include <cstring>
+
+#include "dard_prefix.cuh"
+
+namespace dard {
+namespace {
+
+constexpr int kThreads = 384;
+constexpr int kNS = 2;   // S buffers in TMEM
+constexpr int kNKV = 3;  // TMA stages for K and for V
+constexpr int kSoftmaxWarps = 8;
+constexpr int kWProd = 8, kWPV = 9, kWS = 10, kWCheck = 11;
+
+// Every barrier completes one phase per use of its ring slot; tile j uses slot j % ring and waits
+// for parity (j / ring) & 1. Each wait for use u of a slot is preceded, in the same thread or
+// through a chain of waits, by the completion of use u - 1 (the parity would alias otherwise).
+struct __align__(16) Ctl {
+  uint64_t q_full, o_full, p_full, pv_done;
+  uint64_t k_full[kNKV], k_empty[kNKV], v_full[kNKV], v_empty[kNKV];
+  uint64_t s_full[kNS], s_free[kNS];
+  uint64_t own_go[kNKV];  // an own tile's V copy has been issued (uses of own tiles only)
+  uint64_t v_ok[kNKV];    // an own tile's V holds finite values only (likewise)
+  uint64_t masks;         // row_mask and row_seq are written
+  uint64_t drained;       // every product both issuers launched has completed (two commits)
+  uint32_t tmem_base;
+  int32_t abort;
+  int32_t poison;         // a query sees a value that is not finite
+  float red_max[2][2][kBM];  // per tile parity: the two column halves' row maxima
+  float red_sum[4][kBM];     // the two halves' row sums, rounded and unrounded
+  int64_t out_row[kBM];      // packed query -> row * hq + head, or -1 (not stored)
+  RowMasks row_mask[kBM];
+  int32_t row_seq[kBM];      // -1: no query
+  uint32_t inf_pos[kBM][4], inf_neg[kBM][4];  // elements to become inf, -inf (both: NaN)
+};
+
+template <int D>
+constexpr size_t smem_bytes() {
+  return 1024 + 2 * kNKV * static_cast<size_t>(kTN) * D * 2 + sizeof(Ctl);
+}
+
+__device__ __forceinline__ void flag_timeout(const PrefixParams& p, Ctl& ctl) {
+  ctl.abort = 1;
+  if (p.a.status) atomicOr(p.a.status, DARD_STATUS_TIMEOUT);
+}
+
+__device__ __forceinline__ void tma_load_3d(void* dst, const void* desc, uint64_t* bar, int32_t c0,
+                                            int32_t c1, int32_t c2) {
+  asm volatile(
+      "cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes"
+      " [%0], [%1, {%3, %4, %5}], [%2];" ::"r"(smem_u32(dst)),
+      "l"(reinterpret_cast<uint64_t>(desc)), "r"(smem_u32(bar)), "r"(c0), "r"(c1), "r"(c2)
+      : "memory");
+}
+
+// Warp 11, one own tile in shared memory: values that are not finite become zeros, and the queries
+// that see their keys are marked. `row0` is the tile's first row of k and v.
+template <int D>
+__device__ void check_values(const PrefixParams& p, Ctl& ctl, uint8_t* tile, int row0,
+                             long long wlim) {
+  const int lane = threadIdx.x & 31;
+  bool found = false;
+#pragma unroll 8
+  for (int i = lane; i < kTN * D / 8; i += 32) {
+    const uint4 u = *reinterpret_cast<const uint4*>(tile + 16 * i);
+    const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      found |= (w[e] & 0x7f80u) == 0x7f80u || (w[e] & 0x7f800000u) == 0x7f800000u;
+  }
+  if (!__any_sync(0xffffffffu, found)) return;
+  mbar_wait(&ctl.masks, 0, wlim);
+  if (found) {
+    for (int i = lane; i < kTN * D / 8; i += 32) {
+      uint16_t* v = reinterpret_cast<uint16_t*>(tile + 16 * i);
+      const int key = (i >> 3) % kTN;
+      const int e0 = (i >> 3) / kTN * 64 + (((i & 7) ^ (key & 7)) << 3);
+      uint32_t pos = 0, neg = 0;  // of the chunk's 8 elements
+      for (int e = 0; e < 8; ++e) {
+        const uint32_t b = v[e];
+        if ((b & 0x7f80u) != 0x7f80u) continue;
+        if ((b & 0x7fu) || !(b & 0x8000u)) pos |= 1u << e;
+        if ((b & 0x7fu) || (b & 0x8000u)) neg |= 1u << e;
+        v[e] = 0;
+      }
+      if (!(pos | neg)) continue;
+      for (int t = 0; t < kBM; ++t) {
+        const int s = ctl.row_seq[t];
+        if (s < 0 || !(own_vis64(p.a.seq[s], row0 + key - p.a.seq[s].row_base, ctl.row_mask[t]) & 1))
+          continue;
+        if (pos) atomicOr(&ctl.inf_pos[t][e0 >> 5], pos << (e0 & 31));
+        if (neg) atomicOr(&ctl.inf_neg[t][e0 >> 5], neg << (e0 & 31));
+        ctl.poison = 1;
+      }
+    }
+  }
+  __threadfence_block();
+  fence_proxy_async_smem();  // the zeros, before the product reads the tile
+}
+
+__device__ __forceinline__ float poisoned(const Ctl& ctl, int t, int e, float o) {
+  const bool pos = ctl.inf_pos[t][e >> 5] >> (e & 31) & 1, neg = ctl.inf_neg[t][e >> 5] >> (e & 31) & 1;
+  if (pos) o += INFINITY;
+  if (neg) o -= INFINITY;
+  return o;
+}
+
+// kLse: the normalisers are written too; their sum adds the unrounded probabilities, beside the
+// sum of the rounded ones that divides the output (a convex combination of values then, and a
+// row whose weight is nearly all on one key gets that key's value exactly).
+template <int D, bool kLse>
+__global__ void __launch_bounds__(kThreads, 1)
+    prefix_tc(const __grid_constant__ PrefixParams p, const __grid_constant__ CUtensorMap tpk,
+              const __grid_constant__ CUtensorMap tpv, const __grid_constant__ CUtensorMap tk,
+              const __grid_constant__ CUtensorMap tv) {
+  constexpr int kSub = D / 64;                 // 128-byte (64 x bf16) column blocks
+  constexpr uint32_t kKSub = kTN * 128;        // one 128-row x 128-byte swizzled block
+  constexpr uint32_t kKVBytes = kSub * kKSub;  // one K (or V) tile of 128 keys
+  extern __shared__ uint8_t smem_raw[];
+  uint8_t* base = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) &
+                                             ~static_cast<uintptr_t>(1023));
+  uint8_t* sK = base;                  // kNKV stages
+  uint8_t* sV = sK + kNKV * kKVBytes;  // kNKV stages
+  Ctl& ctl = *reinterpret_cast<Ctl*>(sV + kNKV * kKVBytes);
+
+  grid_dep_launch();  // the launch that joins the parts may be scheduled; it waits for this one
+  const int item = blockIdx.x / p.nsplit, part = blockIdx.x % p.nsplit;
+  const int g = item / p.tiles, m0 = item % p.tiles * kBM;
+  int key0, key_end;
+  own_range(p, m0, kBM, key0, key_end);
+  const int npt = (p.prefix_len + kTN - 1) / kTN;  // the prefix's tiles
+  const int all = npt + (key_end - key0 + kTN - 1) / kTN;
+  const int j0 = static_cast<int>(static_cast<long long>(all) * part / p.nsplit);
+  const int n_kt = static_cast<int>(static_cast<long long>(all) * (part + 1) / p.nsplit) - j0;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const long long wlim = p.a.wait_cycles > 0 ? p.a.wait_cycles : kWaitCycles;
+  const int first_own = max(npt - j0, 0);  // local index of the first own tile (may be >= n_kt)
+
+  auto load_kv = [&](int j, bool k_or_v) {
+    const int b = j % kNKV;
+    uint64_t* bar = k_or_v ? &ctl.k_full[b] : &ctl.v_full[b];
+    uint8_t* dst = (k_or_v ? sK : sV) + b * kKVBytes;
+    const bool own = j >= first_own;
+    const void* map = k_or_v ? (own ? &tk : &tpk) : (own ? &tv : &tpv);
+    const int row = own ? key0 + (j0 + j - npt) * kTN : (j0 + j) * kTN;
+    mbar_arrive_expect_tx(bar, kKVBytes);
+    if (!k_or_v && own) mbar_arrive(&ctl.own_go[b]);
+    if (k_or_v && j == p.a.test_drop_kv) return;  // test hook: this K copy is never issued
+#pragma unroll
+    for (int s = 0; s < kSub; ++s) tma_load_3d(dst + s * kKSub, map, bar, s * 64, row, g);
+  };
+  if (warp == kWProd && lane == 0) {
+    mbar_init(&ctl.q_full, kSoftmaxWarps);
+    mbar_init(&ctl.drained, 2);
+    mbar_init(&ctl.o_full, 1);
+    mbar_init(&ctl.p_full, kSoftmaxWarps);
+    mbar_init(&ctl.pv_done, 1);
+    mbar_init(&ctl.masks, 4);
+    for (int b = 0; b < kNKV; ++b) {
+      mbar_init(&ctl.k_full[b], 1);
+      mbar_init(&ctl.k_empty[b], 1);
+      mbar_init(&ctl.v_full[b], 1);
+      mbar_init(&ctl.v_empty[b], 1);
+      mbar_init(&ctl.own_go[b], 1);
+      mbar_init(&ctl.v_ok[b], 1);
+    }
+    for (int b = 0; b < kNS; ++b) {
+      mbar_init(&ctl.s_full[b], 1);
+      mbar_init(&ctl.s_free[b], kSoftmaxWarps);
+    }
+    ctl.abort = 0;
+    ctl.poison = 0;
+    fence_barrier_init();
+    for (int j = 0; j < kNKV && j < n_kt; ++j) {
+      load_kv(j, true);
+      load_kv(j, false);
+    }
+  }
+  if (warp == kWPV) {
+    tmem_alloc<kTmemCols>(&ctl.tmem_base);
+    tmem_relinquish();
+  }
+  // Softmax warp w: queries 32 (w % 4) .. + 31 (TMEM lane quarter), keys 64 (w / 4) .. of a tile
+  const int quarter = warp & 3, half = warp >> 2;
+  const int t = quarter * 32 + lane;  // this thread's query within the tile
+  uint4 qhalf[D / 16];                // half of its row of q
+  int seq = -1, r = 0;                // its sequence and sequence-relative row
+  int64_t out_row = -1;
+  if (warp < kSoftmaxWarps) {
+    if (m0 + t < p.queries) {
+      const int tq = (m0 + t) / p.group;
+      seq = seq_of_query(p, tq);
+      r = p.a.seq[seq].q_start + tq - p.q_before[seq];
+      out_row = static_cast<int64_t>(p.a.seq[seq].row_base + r) * p.a.hq + g * p.group +
+                (m0 + t) % p.group;
+    }
+    const uint4* src = reinterpret_cast<const uint4*>(
+        static_cast<const __nv_bfloat16*>(p.a.q) + out_row * D + half * (D / 2));
+#pragma unroll
+    for (int c = 0; c < D / 16; ++c) qhalf[c] = seq >= 0 ? __ldg(src + c) : make_uint4(0, 0, 0, 0);
+    if (half == 0) {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) ctl.inf_pos[t][e] = ctl.inf_neg[t][e] = 0;
+    }
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tO = ctl.tmem_base + kNS * kTN;
+  const uint32_t tP = ctl.tmem_base + 384;
+  const uint32_t tQ = ctl.tmem_base + 448;
+  volatile int32_t* abort_flag = &ctl.abort;
+
+  if (warp == kWProd) {
+    // ------------------------------------------------------------ TMA producer
+    if (lane == 0) {
+      int last_k = min(n_kt, kNKV) - 1, last_v = last_k;
+      for (int j = kNKV; j < n_kt && !*abort_flag; ++j) {
+        const int b = j % kNKV, ph = ((j - kNKV) / kNKV) & 1;
+        if (!mbar_wait(&ctl.k_empty[b], ph, wlim)) { flag_timeout(p, ctl); break; }
+        load_kv(j, true);
+        last_k = j;
+        if (!mbar_wait(&ctl.v_empty[b], ph, wlim)) { flag_timeout(p, ctl); break; }
+        load_kv(j, false);
+        last_v = j;
+      }
+      // Every copy issued lands before shared memory is released: the latest use of each stage.
+      for (int b = 0; b < kNKV; ++b) {
+        const int jk = last_k - ((last_k - b) % kNKV + kNKV) % kNKV;
+        const int jv = last_v - ((last_v - b) % kNKV + kNKV) % kNKV;
+        if (last_k >= 0 && jk >= 0 && jk != p.a.test_drop_kv)
+          mbar_wait(&ctl.k_full[b], (jk / kNKV) & 1, wlim);
+        if (last_v >= 0 && jv >= 0) mbar_wait(&ctl.v_full[b], (jv / kNKV) & 1, wlim);
+      }
+    }
+  } else if (warp == kWS) {
+    // ------------------------------------------------------------ S issuer
+    if (lane == 0) {
+      constexpr uint32_t kIdS = idesc_bf16_f32(kBM, kTN, 0, 0);
+      const uint32_t ak = smem_u32(sK);
+      bool ok = mbar_wait(&ctl.q_full, 0, wlim);
+      for (int j = 0; j < n_kt && ok && !*abort_flag; ++j) {
+        const int kb = j % kNKV, sb = j % kNS;
+        if (j >= kNS) ok = mbar_wait(&ctl.s_free[sb], ((j - kNS) / kNS) & 1, wlim);
+        ok = ok && mbar_wait(&ctl.k_full[kb], (j / kNKV) & 1, wlim);
+        if (!ok) break;
+        tc_fence_after();
+        const uint32_t kaddr = ak + kb * kKVBytes;
+        const uint32_t dst = ctl.tmem_base + sb * kTN;
+#pragma unroll
+        for (int ks = 0; ks < D / 16; ++ks) {
+          const uint32_t ko = (ks >> 2) * kKSub + (ks & 3) * 32;
+          mma_ts(dst, tQ + ks * 8, smem_desc_sw128(kaddr + ko, 16, 1024), kIdS, ks > 0);
+        }
+        mma_commit(&ctl.s_full[sb]);
+        mma_commit(&ctl.k_empty[kb]);
+      }
+      if (!ok) flag_timeout(p, ctl);
+      mma_commit(&ctl.drained);
+    }
+  } else if (warp == kWPV) {
+    // ------------------------------------------------------------ PV issuer
+    if (lane == 0) {
+      constexpr uint32_t kIdO = idesc_bf16_f32(kBM, D, 0, 1);
+      const uint32_t av = smem_u32(sV);
+      bool ok = true;
+      for (int j = 0; j < n_kt && ok && !*abort_flag; ++j) {
+        const int vb = j % kNKV, o = j - first_own;
+        ok = mbar_wait(&ctl.p_full, j & 1, wlim) &&
+             (o < 0 ? mbar_wait(&ctl.v_full[vb], (j / kNKV) & 1, wlim)
+                    : mbar_wait(&ctl.v_ok[vb], (o / kNKV) & 1, wlim));
+        if (!ok) break;
+        tc_fence_after();
+        const uint32_t vaddr = av + vb * kKVBytes;
+#pragma unroll
+        for (int ks = 0; ks < kTN / 16; ++ks)
+          mma_ts(tO, tP + ks * 8, smem_desc_sw128(vaddr + ks * 2048, kKSub, 1024), kIdO,
+                 (j > 0 || ks > 0) ? 1u : 0u);
+        mma_commit(&ctl.pv_done);
+        mma_commit(&ctl.v_empty[vb]);
+        if (j == n_kt - 1) mma_commit(&ctl.o_full);
+      }
+      if (!ok) flag_timeout(p, ctl);
+      mma_commit(&ctl.drained);
+    }
+  } else if (warp == kWCheck) {
+    // ------------------------------------------------------------ own tiles' values
+    // (own_go before v_full: the stage's use before this one has completed by then)
+    bool ok = true;
+    for (int j = first_own; j < n_kt && ok && !*abort_flag; ++j) {
+      const int vb = j % kNKV;
+      ok = mbar_wait(&ctl.own_go[vb], ((j - first_own) / kNKV) & 1, wlim) &&
+           mbar_wait(&ctl.v_full[vb], (j / kNKV) & 1, wlim);
+      ok = __all_sync(0xffffffffu, ok);
+      if (!ok) break;
+      check_values<D>(p, ctl, sV + vb * kKVBytes, key0 + (j0 + j - npt) * kTN, wlim);
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&ctl.v_ok[vb]);
+    }
+    if (!ok && lane == 0) flag_timeout(p, ctl);
+  } else {
+    // ------------------------------------------------------------ softmax + epilogue
+    const uint32_t lane_off = static_cast<uint32_t>(quarter * 32) << 16;
+    {  // this warp's half of the query rows into TMEM (bf16 pairs, the A-operand layout)
+#pragma unroll
+      for (int c = 0; c < D / 128; ++c) {
+        uint32_t w[32];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          w[4 * e + 0] = qhalf[8 * c + e].x;
+          w[4 * e + 1] = qhalf[8 * c + e].y;
+          w[4 * e + 2] = qhalf[8 * c + e].z;
+          w[4 * e + 3] = qhalf[8 * c + e].w;
+        }
+        tmem_st32(tQ + lane_off + half * (D / 4) + 32 * c, w);
+      }
+      if (D == 64) {  // 16 columns per half
+        uint32_t w[16];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          w[4 * e + 0] = qhalf[e].x;
+          w[4 * e + 1] = qhalf[e].y;
+          w[4 * e + 2] = qhalf[e].z;
+          w[4 * e + 3] = qhalf[e].w;
+        }
+        tmem_st16(tQ + lane_off + half * 16, w);
+      }
+      tmem_wait_st();
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&ctl.q_full);
+    }
+    // the last part holds the sequences' last rows: it always has own tiles, and it alone decides
+    // which rows are stored
+    RowMasks rm{{0, 0}, {0, 0}};
+    int store = seq >= 0;
+    if (first_own < n_kt) {
+      if (seq >= 0) rm = query_masks(p.a, p.a.seq[seq], r, half == 0 && g == 0, store);
+      if (half == 0) {
+        ctl.row_mask[t] = rm;
+        ctl.row_seq[t] = seq;
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&ctl.masks);
+      }
+    }
+    const int row_base = seq >= 0 ? p.a.seq[seq].row_base : 0;
+    const float sl = p.a.scale_log2;
+    float m_run = -INFINITY, l_run = 0.f, l_all = 0.f;
+    bool ok = true;
+    for (int j = 0; j < n_kt; ++j) {
+      const int b = j % kNS;
+      uint64_t vis = ~0ull;
+      bool masked = false;
+      if (j >= first_own) {
+        masked = true;
+        vis = seq < 0 ? 0ull
+                      : own_vis64(p.a.seq[seq], key0 + (j0 + j - npt) * kTN + 64 * half - row_base, rm);
+      } else if ((j0 + j + 1) * kTN > p.prefix_len) {
+        masked = true;
+        vis = first64(p.prefix_len - (j0 + j) * kTN - 64 * half);
+      }
+      // Both warps of the rows wait for the same S_j with the same bound (no early leave on an
+      // abort flag), so they leave the loop together: a barrier completing between the two warps'
+      // deadlines (a product about a second late) is the only way they could part.
+      ok = mbar_wait(&ctl.s_full[b], (j / kNS) & 1, wlim);
+      if (!__all_sync(0xffffffffu, ok)) { ok = false; break; }
+      tc_fence_after();
+      float s[64];
+      {
+        uint32_t r0[32], r1[32];
+        tmem_ld32(ctl.tmem_base + b * kTN + 64 * half + lane_off, r0);
+        tmem_ld32(ctl.tmem_base + b * kTN + 64 * half + 32 + lane_off, r1);
+        tmem_wait_ld();
+#pragma unroll
+        for (int e = 0; e < 32; ++e) {
+          s[e] = __uint_as_float(r0[e]);
+          s[32 + e] = __uint_as_float(r1[e]);
+        }
+      }
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&ctl.s_free[b]);
+      if (masked) {
+#pragma unroll
+        for (int k = 0; k < 64; ++k) s[k] = ((vis >> k) & 1ull) ? s[k] : -INFINITY;
+      }
+      float mx[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) mx[e] = fmax3(s[e], s[8 + e], s[16 + e]);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) mx[e] = fmax3(mx[e], s[24 + e], s[32 + e]);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) mx[e] = fmax3(mx[e], s[40 + e], s[48 + e]);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) mx[e] = fmaxf(mx[e], s[56 + e]);
+      const float mh = fmaxf(fmax3(mx[0], mx[1], mx[2]),
+                             fmax3(fmax3(mx[3], mx[4], mx[5]), mx[6], mx[7]));
+      ctl.red_max[j & 1][half][t] = mh;
+      pair_bar_sync(quarter);
+      const float mt = fmaxf(mh, ctl.red_max[j & 1][half ^ 1][t]);
+      // The reference maximum rises on the first finite value, or when the tile's exceeds it by
+      // more than 2^kRescaleLog2 in probability; only then is O rescaled. Both warps of a row
+      // take the same decision from the same values.
+      float m_new = m_run;
+      if (m_run == -INFINITY) m_new = mt;
+      else if ((mt - m_run) * sl > kRescaleLog2) m_new = mt;
+      const bool rescale = (m_new != m_run) && (m_run != -INFINITY);
+      const float alpha = rescale ? ex2_approx((m_run - m_new) * sl) : 1.f;
+      const float mL = (m_new == -INFINITY) ? 0.f : m_new * sl;
+      uint32_t pk[32];
+      const uint64_t sl2 = f2_pack(sl, sl), nmL2 = f2_pack(-mL, -mL);
+      float acc[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+      uint64_t acc2[2] = {0, 0};  // bit pattern 0 = +0.0f
+#pragma unroll
+      for (int e = 0; e < 32; ++e) {
+        float x0, x1;
+        f2_unpack(f2_fma(f2_pack(s[2 * e], s[2 * e + 1]), sl2, nmL2), x0, x1);
+        x0 = ex2_approx(x0);
+        x1 = ex2_approx(x1);
+        pk[e] = pack_bf16x2(x0, x1);
+        add_bf16x2_f32(acc[2 * (e & 3)], acc[2 * (e & 3) + 1], pk[e]);
+        if (kLse) acc2[e & 1] = f2_add(acc2[e & 1], f2_pack(x0, x1));
+      }
+      float ls[4];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) ls[k] = acc[k] + acc[4 + k];
+      if (j > 0) {  // P_j replaces P_{j-1}, and O may be rescaled, once PV_{j-1} has completed
+        ok = mbar_wait(&ctl.pv_done, (j - 1) & 1, wlim);
+        if (!__all_sync(0xffffffffu, ok)) { ok = false; break; }
+        tc_fence_after();
+      }
+      if (__any_sync(0xffffffffu, rescale)) {
+#pragma unroll
+        for (int c = 0; c < D / 64; ++c) {  // this warp's half of the O columns
+          uint32_t rr[32];
+          const uint32_t col = tO + lane_off + half * (D / 2) + 32 * c;
+          tmem_ld32(col, rr);
+          tmem_wait_ld();
+#pragma unroll
+          for (int e = 0; e < 32; ++e) rr[e] = __float_as_uint(__uint_as_float(rr[e]) * alpha);
+          tmem_st32(col, rr);
+        }
+      }
+      l_run = l_run * alpha + ((ls[0] + ls[1]) + (ls[2] + ls[3]));
+      if (kLse) {
+        float a0, a1;
+        f2_unpack(f2_add(acc2[0], acc2[1]), a0, a1);
+        l_all = l_all * alpha + (a0 + a1);
+      }
+      m_run = m_new;
+      tmem_st32(tP + lane_off + 32 * half, pk);
+      tmem_wait_st();
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&ctl.p_full);
+    }
+    if (ok) ok = mbar_wait(&ctl.o_full, 0, wlim);
+    const bool wok = __all_sync(0xffffffffu, ok);
+    if (!wok && lane == 0) flag_timeout(p, ctl);
+    ctl.red_sum[half][t] = l_run;
+    ctl.red_sum[2 + half][t] = l_all;
+    if (half == 0) ctl.out_row[t] = wok && store ? out_row : -1;
+    softmax_bar_sync();
+    const float l = ctl.red_sum[0][t] + ctl.red_sum[1][t];
+    const float l_exact = ctl.red_sum[2][t] + ctl.red_sum[3][t];
+    const bool poison = ctl.poison != 0;
+    if (p.nsplit > 1) {
+      // this part of the keys: unnormalised output, reference maximum and sums
+      float* slot = p.part + blockIdx.x * part_slot_floats(kBM, D);
+      if (wok) {  // (whole warps: the loads from TMEM are theirs; padding queries store nothing)
+        tc_fence_after();
+        float* o = slot + t * D + half * (D / 2);
+#pragma unroll
+        for (int c = 0; c < D / 64; ++c) {
+          uint32_t rr[32];
+          tmem_ld32(tO + lane_off + half * (D / 2) + 32 * c, rr);
+          tmem_wait_ld();
+          if (poison)
+            for (int e = 0; e < 32; ++e)
+              rr[e] = __float_as_uint(poisoned(ctl, t, half * (D / 2) + 32 * c + e, __uint_as_float(rr[e])));
+          if (seq >= 0) {
+#pragma unroll
+            for (int v = 0; v < 8; ++v)
+              *reinterpret_cast<uint4*>(o + 32 * c + 4 * v) =
+                  make_uint4(rr[4 * v], rr[4 * v + 1], rr[4 * v + 2], rr[4 * v + 3]);
+          }
+          __syncwarp();
+        }
+      }
+      if (half == 0) {
+        float* stat = slot + kBM * D;
+        stat[t] = m_run == -INFINITY ? -INFINITY : m_run * sl;
+        stat[kBM + t] = l;
+        stat[2 * kBM + t] = wok && store ? l_exact : -1.f;
+      }
+    } else {
+      // O row / row sum -> bf16 into shared memory (the K stages are no longer read once o_full
+      // has completed), 16-byte chunks XOR-swizzled by row; then the 256 softmax threads store
+      // whole rows, coalesced. Every softmax warp reaches the named barriers on every path.
+      constexpr int kChunks = D / 8;  // 16-byte chunks per output row
+      uint4* stage = reinterpret_cast<uint4*>(sK);  // 128 rows x D bf16 <= one K stage
+      if (wok) {
+        tc_fence_after();
+        const float inv_l = 1.0f / l;
+#pragma unroll
+        for (int c = 0; c < D / 64; ++c) {
+          uint32_t rr[32];
+          tmem_ld32(tO + lane_off + half * (D / 2) + 32 * c, rr);
+          tmem_wait_ld();
+          if (poison)
+            for (int e = 0; e < 32; ++e)
+              rr[e] = __float_as_uint(poisoned(ctl, t, half * (D / 2) + 32 * c + e, __uint_as_float(rr[e])));
+#pragma unroll
+          for (int v = 0; v < 4; ++v) {
+            uint4 u;
+            u.x = pack_bf16x2(__uint_as_float(rr[8 * v + 0]) * inv_l, __uint_as_float(rr[8 * v + 1]) * inv_l);
+            u.y = pack_bf16x2(__uint_as_float(rr[8 * v + 2]) * inv_l, __uint_as_float(rr[8 * v + 3]) * inv_l);
+            u.z = pack_bf16x2(__uint_as_float(rr[8 * v + 4]) * inv_l, __uint_as_float(rr[8 * v + 5]) * inv_l);
+            u.w = pack_bf16x2(__uint_as_float(rr[8 * v + 6]) * inv_l, __uint_as_float(rr[8 * v + 7]) * inv_l);
+            const int chunk = half * (kChunks / 2) + c * 4 + v;
+            stage[t * kChunks + (chunk ^ (t & (kChunks - 1)))] = u;
+          }
+        }
+        if (kLse && half == 0 && store)
+          p.lse[out_row] = 0.69314718055994531f * (m_run * sl + log2f(l_exact));
+      }
+      softmax_bar_sync();
+      if (!*abort_flag) {
+        __nv_bfloat16* out = static_cast<__nv_bfloat16*>(p.a.o);
+        const int tid = threadIdx.x;  // 0 .. 255
+#pragma unroll 4
+        for (int idx = tid; idx < kBM * kChunks; idx += 32 * kSoftmaxWarps) {
+          const int row = idx / kChunks, chunk = idx % kChunks;
+          if (ctl.out_row[row] >= 0)
+            reinterpret_cast<uint4*>(out + ctl.out_row[row] * D)[chunk] =
+                stage[row * kChunks + (chunk ^ (row & (kChunks - 1)))];
+        }
+      }
+    }
+  }
+  tc_fence_before();
+  __syncthreads();
+  if (warp == kWPV) {
+    if (lane == 0 && !mbar_wait(&ctl.drained, 0, wlim)) flag_timeout(p, ctl);
+    __syncwarp();
+    tc_fence_after();
+    tmem_dealloc<kTmemCols>(ctl.tmem_base);
+  }
+}
+
+// Joins the parts of a split launch, one warp per packed query: with M the largest reference
+// maximum, o = sum_c 2^(m_c - M) O_c / sum_c 2^(m_c - M) l_c. Reads each part once, coalesced.
+template <typename T, int D>
+__global__ void __launch_bounds__(128) prefix_join(const __grid_constant__ PrefixParams p,
+                                                   int tile_rows) {
+  const int lane = threadIdx.x & 31;
+  const long long w = static_cast<long long>(blockIdx.x) * 4 + (threadIdx.x >> 5);
+  grid_dep_wait();
+  if (w >= static_cast<long long>(p.queries) * p.a.hkv) return;
+  const int g = static_cast<int>(w / p.queries), m = static_cast<int>(w % p.queries);
+  const int t = m % tile_rows;
+  const size_t floats = part_slot_floats(tile_rows, D);
+  const float* slot = p.part + (static_cast<size_t>(g) * p.tiles + m / tile_rows) * p.nsplit * floats;
+  const float* stat = slot + tile_rows * D + t;
+  float top = -INFINITY;
+  bool nan = false;
+  for (int c = lane; c < p.nsplit; c += 32) {
+    const float mc = stat[c * floats];
+    nan |= mc != mc;
+    top = fmaxf(top, mc);
+  }
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+  if (__any_sync(0xffffffffu, nan)) top = NAN;
+  if (stat[(p.nsplit - 1) * floats + 2 * tile_rows] == -1.f) return;  // not stored
+  constexpr int kV = D / 32;  // elements per lane
+  float o[kV];
+#pragma unroll
+  for (int e = 0; e < kV; ++e) o[e] = 0.f;
+  float l = 0.f, l_all = 0.f;
+#pragma unroll 4
+  for (int c = 0; c < p.nsplit; ++c) {
+    const float mc = stat[c * floats];
+    if (mc == -INFINITY && top != -INFINITY) continue;  // a part without a key for this row
+    const float f = mc == top ? 1.f : ex2_approx(mc - top);
+    l = fmaf(f, stat[c * floats + tile_rows], l);
+    l_all = fmaf(f, stat[c * floats + 2 * tile_rows], l_all);
+    const float* src = slot + c * floats + t * D + lane * kV;
+#pragma unroll
+    for (int e = 0; e < kV; ++e) o[e] = fmaf(f, src[e], o[e]);
+  }
+  const int tq = m / p.group, seq = seq_of_query(p, tq);
+  const size_t row = static_cast<size_t>(p.a.seq[seq].row_base + p.a.seq[seq].q_start + tq -
+                                         p.q_before[seq]) * p.a.hq + g * p.group + m % p.group;
+  T* out = static_cast<T*>(p.a.o) + row * D + lane * kV;
+  const float inv = 1.0f / l;
+#pragma unroll
+  for (int e = 0; e < kV; e += 2) {
+    if constexpr (sizeof(T) == 2)
+      *reinterpret_cast<uint32_t*>(out + e) = pack_bf16x2(o[e] * inv, o[e + 1] * inv);
+    else
+      *reinterpret_cast<float2*>(out + e) = make_float2(o[e] * inv, o[e + 1] * inv);
+  }
+  if (p.lse && lane == 0) p.lse[row] = 0.69314718055994531f * (top + log2f(l_all));
+}
+
+// ---------------------------------------------------------------- host side
+constexpr int kSlots = 640;  // parts of a split launch at most
+
+// CTAs per query tile. Costs in SM cycles: a CTA about kFixed plus kStep per key tile, the join
+// about kJoin; a launch with no more CTAs than SMs takes its longest, a larger one total / SMs
+// plus half a CTA.
+int choose_split(long long items, double steps, int most, int sms, double fixed, double step) {
+  constexpr double kJoin = 6000;
+  int best = 1;
+  double best_time = 0;
+  for (int s = 1; s <= most && items * s <= kSlots; ++s) {
+    const double cta = fixed + step * std::ceil(steps / s);
+    const double n = static_cast<double>(items) * s;
+    const double time = (n <= sms ? cta : n * (fixed + step * steps / s) / sms + 0.5 * cta) +
+                        (s > 1 ? kJoin : 0);
+    if (s == 1 || time < best_time) {
+      best = s;
+      best_time = time;
+    }
+  }
+  return best;
+}
+
+bool make_map3(CUtensorMap* m, const void* ptr, int d, long long rows, int heads, int64_t row_stride,
+               int64_t head_stride) {
+  auto fn = encode_fn();
+  if (!fn) return false;
+  const cuuint64_t dims[3] = {static_cast<cuuint64_t>(d), static_cast<cuuint64_t>(rows),
+                              static_cast<cuuint64_t>(heads)};
+  const cuuint64_t strides[2] = {static_cast<cuuint64_t>(row_stride) * 2,
+                                 static_cast<cuuint64_t>(head_stride) * 2};
+  const cuuint32_t box[3] = {64, kTN, 1};
+  const cuuint32_t estr[3] = {1, 1, 1};
+  return fn(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(ptr), dims, strides, box, estr,
+            CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+            CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+template <int D, bool kLse>
+cudaError_t launch_tc(const PrefixParams& p, cudaStream_t stream) {
+  static std::atomic<uint64_t> done{0};
+  CUtensorMap pk, pv, k, v;
+  const AttnParams& a = p.a;
+  if (!make_map3(&k, a.k, D, a.total_rows, a.hkv, static_cast<int64_t>(a.hkv) * D, D) ||
+      !make_map3(&v, a.v, D, a.total_rows, a.hkv, static_cast<int64_t>(a.hkv) * D, D))
+    return cudaErrorInvalidValue;
+  if (p.prefix_len > 0) {
+    if (!make_map3(&pk, p.pk, D, p.prefix_len, a.hkv, p.row_stride, p.head_stride) ||
+        !make_map3(&pv, p.pv, D, p.prefix_len, a.hkv, p.row_stride, p.head_stride))
+      return cudaErrorInvalidValue;
+  } else {
+    pk = k;
+    pv = v;
+  }
+  cudaError_t e = ensure_smem_attr(prefix_tc<D, kLse>, smem_bytes<D>(), done);
+  if (e != cudaSuccess) return e;
+  const AttnLaunch L(static_cast<unsigned>(a.hkv * p.tiles * p.nsplit), kThreads, smem_bytes<D>(),
+                     stream, 1, false);
+  return cudaLaunchKernelEx(&L.cfg, prefix_tc<D, kLse>, p, pk, pv, k, v);
+}
+
+template <typename T>
+cudaError_t launch_join(const PrefixParams& p, int rows, cudaStream_t stream) {
+  const long long warps = static_cast<long long>(p.queries) * p.a.hkv;
+  const AttnLaunch L(static_cast<unsigned>((warps + 3) / 4), 128, 0, stream, 1, true);
+  return p.a.head_dim == 64 ? cudaLaunchKernelEx(&L.cfg, prefix_join<T, 64>, p, rows)
+                            : cudaLaunchKernelEx(&L.cfg, prefix_join<T, 128>, p, rows);
+}
+
+dard_status prepare(const dard_prefix_attn_args* args, PrefixParams& p) {
+  if (!args) return report(DARD_ERR_NULL, "args is NULL");
+  const dard_attn_args& own = args->own;
+  const dard_status st = prepare_attention(&own, p.a);
+  if (st != DARD_OK) return st;
+  if (own.rope_theta != 0.f)
+    return report(DARD_ERR_VALUE, "rope_theta must be 0: q and k carry their positions");
+  if (args->prefix_len < 0 || args->prefix_len > DARD_PREFIX_MAX_LEN)
+    return report(DARD_ERR_SHAPE, "prefix_len %d outside 0..%d", args->prefix_len, DARD_PREFIX_MAX_LEN);
+  const int esz = own.dtype == DARD_BF16 ? 2 : 4;
+  if (args->prefix_len > 0) {
+    if (!args->prefix_k || !args->prefix_v)
+      return report(DARD_ERR_NULL, "prefix_k or prefix_v is NULL");
+    if (args->prefix_row_stride < own.head_dim || args->prefix_head_stride < own.head_dim ||
+        args->prefix_row_stride > (1ll << 36) || args->prefix_head_stride > (1ll << 36))
+      return report(DARD_ERR_SHAPE, "prefix strides outside head_dim..2^36");
+    if (((reinterpret_cast<uintptr_t>(args->prefix_k) | reinterpret_cast<uintptr_t>(args->prefix_v) |
+          static_cast<uintptr_t>(args->prefix_row_stride * esz) |
+          static_cast<uintptr_t>(args->prefix_head_stride * esz)) & 15u) != 0)
+      return report(DARD_ERR_ALIGN, "prefix_k, prefix_v and their strides must be multiples of 16 bytes");
+  }
+  if ((reinterpret_cast<uintptr_t>(args->lse) & 3u) != 0)
+    return report(DARD_ERR_ALIGN, "lse must be 4-byte aligned");
+  p.pk = args->prefix_k;
+  p.pv = args->prefix_v;
+  p.row_stride = args->prefix_row_stride;
+  p.head_stride = args->prefix_head_stride;
+  p.prefix_len = args->prefix_len;
+  p.lse = args->lse;
+  p.group = own.hq / own.hkv;
+  long long rows = 0;
+  for (int s = 0; s < own.num_seqs; ++s) {
+    p.q_before[s] = static_cast<int32_t>(rows);
+    rows += p.a.seq[s].n_orig + p.a.seq[s].slen - p.a.seq[s].q_start;
+  }
+  p.q_before[own.num_seqs] = static_cast<int32_t>(rows);
+  if (rows * p.group > (1ll << 31) - 256)
+    return report(DARD_ERR_SHAPE, "query rows times heads of a group exceed 2^31 - 256");
+  p.queries = static_cast<int32_t>(rows * p.group);
+  const size_t need = dard_prefix_attention_workspace_size(p.a.total_rows, own.hq, own.hkv,
+                                                           own.head_dim, args->prefix_len);
+  if (args->workspace && args->workspace_bytes < need)
+    return report(DARD_ERR_WORKSPACE, "workspace of %zu bytes needed", need);
+  if ((reinterpret_cast<uintptr_t>(args->workspace) & 15u) != 0)
+    return report(DARD_ERR_ALIGN, "workspace must be 16-byte aligned");
+  p.part = static_cast<float*>(args->workspace);
+  return DARD_OK;
+}
+
+}  // namespace
+}  // namespace dard
+
+extern "C" {
+
+size_t dard_prefix_attention_workspace_size(int32_t total_rows, int32_t hq, int32_t hkv,
+                                            int32_t head_dim, int32_t prefix_len) {
+  using namespace dard;
+  if (total_rows < 0 || hq < 1 || hkv < 1 || hq % hkv != 0 || (head_dim != 64 && head_dim != 128) ||
+      prefix_len < 0 || prefix_len > DARD_PREFIX_MAX_LEN)
+    return 0;
+  return kSlots * part_slot_floats(kBM, head_dim) * sizeof(float);
+}
+
+dard_status dard_prefix_attention(const dard_prefix_attn_args* args, void* stream_ptr) {
+  using namespace dard;
+  report(DARD_OK, "%s", "");
+  PrefixParams p;
+  const dard_status st = prepare(args, p);
+  if (st != DARD_OK) return st;
+  if (p.queries == 0) return DARD_OK;
+  const cudaStream_t stream = static_cast<cudaStream_t>(stream_ptr);
+  if (const char* w = std::getenv("DARD_TEST_WAIT_CYCLES")) p.a.wait_cycles = std::atoll(w);
+  if (const char* d = std::getenv("DARD_TEST_DROP_KV")) p.a.test_drop_kv = std::atoi(d);
+  if (std::getenv("DARD_TEST_FAIL_LAUNCH") != nullptr)
+    return report(DARD_ERR_CUDA, "prefix attention launch failed: %s (DARD_TEST_FAIL_LAUNCH)",
+                  cudaGetErrorString(cudaErrorLaunchFailure));
+  const int sms = sm_count();
+  const bool bf16 = args->own.dtype == DARD_BF16;
+  const int rows = bf16 ? kBM : prefix_f32_rows(p, sms);
+  const int key_tile = bf16 ? kTN : 64;
+  p.tiles = (p.queries + rows - 1) / rows;
+  if (static_cast<long long>(p.tiles) * p.a.hkv > (1ll << 31) - 1)
+    return report(DARD_ERR_SHAPE, "too many query tiles");
+  p.nsplit = 1;
+  const long long items = static_cast<long long>(p.tiles) * p.a.hkv;
+  if (p.part != nullptr && items * 2 <= kSlots) {
+    // every tile has the prefix's key tiles and at least one of its own
+    const int least = (p.prefix_len + key_tile - 1) / key_tile + 1;
+    double own = 0;  // own key tiles of a query tile, on average
+    for (int i = 0; i < p.tiles; ++i) {
+      const int t0 = static_cast<int>(static_cast<long long>(i) * rows / p.group);
+      const int t1 = static_cast<int>((std::min<long long>((i + 1ll) * rows, p.queries) - 1) / p.group);
+      const int s0 = static_cast<int>(std::upper_bound(p.q_before, p.q_before + p.a.num_seqs, t0) - p.q_before) - 1;
+      const int s1 = static_cast<int>(std::upper_bound(p.q_before, p.q_before + p.a.num_seqs, t1) - p.q_before) - 1;
+      own += (p.a.seq[s1].row_base + p.a.seq[s1].n_orig + p.a.seq[s1].slen - p.a.seq[s0].row_base +
+              key_tile - 1) / key_tile;
+    }
+    const double steps = least - 1 + own / p.tiles;
+    p.nsplit = bf16 ? choose_split(items, steps, least, sms, 8000, 1500)
+                    : choose_split(items, steps, least, sms, 6000, 100.0 * rows);
+  }
+  cudaError_t e;
+  if (!bf16)
+    e = launch_prefix_f32(p, rows, stream);
+  else if (p.a.head_dim == 64)
+    e = p.lse ? launch_tc<64, true>(p, stream) : launch_tc<64, false>(p, stream);
+  else
+    e = p.lse ? launch_tc<128, true>(p, stream) : launch_tc<128, false>(p, stream);
+  if (e == cudaSuccess && p.nsplit > 1)
+    e = bf16 ? launch_join<__nv_bfloat16>(p, rows, stream) : launch_join<float>(p, rows, stream);
+  if (e != cudaSuccess)
+    return report(DARD_ERR_CUDA, "prefix attention launch failed: %s", cudaGetErrorString(e));
+  return DARD_OK;
+}
+
+}  // extern "C"

@@ -1,0 +1,347 @@
+// dard_prefix_evict.cu - the keys of a shared prefix to keep, by their accumulated attention weight
+// (dard_prefix_evict): per key/value head the largest weights between the fixed ends, in rising
+// order of their index, and the kept rows of K and V moved together.
+//
+// evict_select: one cluster of CTAs per head; each warp owns a run of the candidates. Weights map
+// to unsigned keys in the same order; three rounds of 11, 11 and 10 bits (a radix selection: count
+// each digit's values among the candidates that share the digits so far, take the digit in which
+// the count from the top passes the number wanted) find the smallest kept key and how many of its
+// equals are kept. The counts of a cluster meet in the shared memory of its first CTA. Then each
+// warp counts its kept candidates, a scan over warps and CTAs places them, and ballots place each
+// within its warp. Nothing depends on the order of the atomics: they only count.
+// evict_copy: 16 bytes of K and of V per thread and step, rows in the order of the outputs.
+#include <algorithm>
+#include <cstdio>
+#include <cstdlib>
+#include <cstring>
+
+#include "dard_attn_common.cuh"
+
+namespace dard {
+namespace {
+
+struct EvictParams {
+  const float* w;
+  const uint4* k;
+  const uint4* v;
+  int32_t* kept;
+  uint4* k_out;
+  uint4* v_out;
+  float* w_out;
+  int64_t w_stride;
+  int64_t row, head, out_row, out_head;  // strides in 16-byte units
+  int32_t hkv, prefix_len, keep, first, last;
+  int32_t chunks;  // 16-byte chunks of a row
+};
+
+constexpr int kSelThreads = 1024, kSelWarps = 32;
+constexpr int kBins = 2048;
+constexpr int kMaxCluster = 8;
+
+// Order-preserving: a larger weight has a larger key; -0 as 0, NaN below everything.
+__device__ __forceinline__ uint32_t key_of(float w) {
+  if (w != w) return 0u;
+  const uint32_t b = __float_as_uint(w == 0.f ? 0.f : w);
+  return b & 0x80000000u ? ~b : b | 0x80000000u;  // at least 0x007fffff (-inf)
+}
+
+struct SelShared {
+  uint32_t hist[kBins];
+  uint32_t warp_gt[kSelWarps], warp_eq[kSelWarps];
+  uint32_t cta_gt, cta_eq;        // this CTA's counts
+  uint32_t base_gt, base_eq;      // those of the cluster's earlier CTAs
+  uint32_t digit, above;          // the round's result
+};
+
+__device__ __forceinline__ uint32_t ld_cluster(const uint32_t* p, uint32_t rank) {
+  uint32_t v;
+  asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(v) : "r"(map_shared_rank(smem_u32(p), rank)) : "memory");
+  return v;
+}
+
+// All threads of the cluster; shared memory written before is seen by all of them.
+__device__ __forceinline__ void sync_head(int ctas) {
+  __syncthreads();
+  if (ctas > 1) cluster_sync();
+}
+
+__global__ void __launch_bounds__(kSelThreads, 1) evict_select(const __grid_constant__ EvictParams p,
+                                                               int ctas) {
+  __shared__ SelShared sh;
+  grid_dep_launch();
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const int g = blockIdx.x / ctas, rank = blockIdx.x % ctas;
+  const float* w = p.w + g * p.w_stride;
+  int32_t* kept = p.kept + static_cast<int64_t>(g) * p.keep;
+  float* w_out = p.w_out ? p.w_out + static_cast<int64_t>(g) * p.keep : nullptr;
+  const int lo = p.first, hi = p.prefix_len - p.last;  // candidates
+  const int want = p.keep - p.first - p.last;
+  // the fixed ends
+  for (int i = rank * kSelThreads + tid; i < p.first + p.last; i += ctas * kSelThreads) {
+    const int at = i < p.first ? i : p.prefix_len - p.last + (i - p.first);
+    const int to = i < p.first ? i : p.keep - p.last + (i - p.first);
+    kept[to] = at;
+    if (w_out) w_out[to] = w[at];
+  }
+  if (want == 0) return;  // (the same for the whole cluster)
+  // this warp's run of candidates
+  const long long n = hi - lo, units = static_cast<long long>(ctas) * kSelWarps;
+  const long long unit = static_cast<long long>(rank) * kSelWarps + warp;
+  const int a = lo + static_cast<int>(n * unit / units), b = lo + static_cast<int>(n * (unit + 1) / units);
+
+  uint32_t prefix = 0, need = want;  // digits found so far; how many of their candidates are kept
+  const int shifts[3] = {21, 10, 0}, bits[3] = {11, 11, 10};
+#pragma unroll 1
+  for (int round = 0; round < 3; ++round) {
+    const int shift = shifts[round], bins = 1 << bits[round];
+    for (int i = tid; i < bins; i += kSelThreads) sh.hist[i] = 0;
+    __syncthreads();
+    const uint32_t done = round == 0 ? 0u : ~0u << (shift + bits[round]);
+    for (int i = a + lane; i < b; i += 32) {
+      const uint32_t key = key_of(__ldg(w + i));
+      if ((key & done) == prefix) atomicAdd(&sh.hist[key >> shift & (bins - 1)], 1u);
+    }
+    sync_head(ctas);
+    if (ctas > 1 && rank == 0)
+      for (int i = tid; i < bins; i += kSelThreads) {
+        uint32_t sum = sh.hist[i];
+        for (int c = 1; c < ctas; ++c) sum += ld_cluster(&sh.hist[i], c);
+        sh.hist[i] = sum;
+      }
+    __syncthreads();
+    if (rank == 0 && warp == 0) {
+      // from the largest digit down: the first at which the count reaches `need`
+      uint32_t above = 0;
+      for (int top = bins - 32; top >= 0; top -= 32) {
+        const uint32_t c = sh.hist[top + 31 - lane];  // lane 0: the largest digit
+        uint32_t scan = c;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+          const uint32_t x = __shfl_up_sync(0xffffffffu, scan, o);
+          if (lane >= o) scan += x;
+        }
+        const uint32_t hit = __ballot_sync(0xffffffffu, above + scan >= need);
+        if (hit) {
+          const int at = __ffs(hit) - 1;
+          if (lane == at) {
+            sh.digit = top + 31 - lane;
+            sh.above = above + scan - c;
+          }
+          break;
+        }
+        above += __shfl_sync(0xffffffffu, scan, 31);
+      }
+    }
+    sync_head(ctas);
+    const uint32_t digit = ctas > 1 ? ld_cluster(&sh.digit, 0) : sh.digit;
+    need -= ctas > 1 ? ld_cluster(&sh.above, 0) : sh.above;
+    prefix |= digit << shift;
+    sync_head(ctas);  // read before the next round writes
+  }
+  // `prefix` is the smallest kept key, of which the first `need` are kept
+  uint32_t gt = 0, eq = 0;
+  for (int i = a + lane; i < b; i += 32) {
+    const uint32_t key = key_of(__ldg(w + i));
+    gt += key > prefix;
+    eq += key == prefix;
+  }
+  gt = __reduce_add_sync(0xffffffffu, gt);
+  eq = __reduce_add_sync(0xffffffffu, eq);
+  if (lane == 0) {
+    sh.warp_gt[warp] = gt;
+    sh.warp_eq[warp] = eq;
+  }
+  __syncthreads();
+  if (warp == 0) {
+    const uint32_t x = sh.warp_gt[lane], y = sh.warp_eq[lane];
+    uint32_t sx = x, sy = y;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const uint32_t ux = __shfl_up_sync(0xffffffffu, sx, o), uy = __shfl_up_sync(0xffffffffu, sy, o);
+      if (lane >= o) { sx += ux; sy += uy; }
+    }
+    sh.warp_gt[lane] = sx - x;
+    sh.warp_eq[lane] = sy - y;
+    if (lane == 31) {
+      sh.cta_gt = sx;
+      sh.cta_eq = sy;
+    }
+  }
+  sync_head(ctas);
+  if (tid == 0) {
+    uint32_t bx = 0, by = 0;
+    for (int c = 0; c < rank; ++c) {
+      bx += ld_cluster(&sh.cta_gt, c);
+      by += ld_cluster(&sh.cta_eq, c);
+    }
+    sh.base_gt = bx;
+    sh.base_eq = by;
+  }
+  sync_head(ctas);
+  gt = sh.base_gt + sh.warp_gt[warp];
+  eq = sh.base_eq + sh.warp_eq[warp];
+  const uint32_t below = (1u << lane) - 1;
+  for (int i0 = a; i0 < b; i0 += 32) {
+    const int i = i0 + lane;
+    const float wi = i < b ? __ldg(w + i) : 0.f;
+    const uint32_t key = key_of(wi);
+    const uint32_t is_gt = __ballot_sync(0xffffffffu, i < b && key > prefix);
+    const uint32_t is_eq = __ballot_sync(0xffffffffu, i < b && key == prefix);
+    const uint32_t my_gt = gt + __popc(is_gt & below), my_eq = eq + __popc(is_eq & below);
+    if ((is_gt >> lane & 1u) || ((is_eq >> lane & 1u) && my_eq < need)) {
+      const int to = p.first + static_cast<int>(my_gt + min(my_eq, need));
+      if (to < p.keep - p.last) {  // (always, unless the weights change under the call)
+        kept[to] = i;
+        if (w_out) w_out[to] = wi;
+      }
+    }
+    gt += __popc(is_gt);
+    eq += __popc(is_eq);
+  }
+}
+
+// Each thread moves the same 16-byte chunk of kRowsPer consecutive output rows' K and V: kRowsPer
+// independent loads of each in flight.
+constexpr int kCopyThreads = 256, kRowsPer = 4;
+
+__global__ void __launch_bounds__(kCopyThreads) evict_copy(const __grid_constant__ EvictParams p) {
+  grid_dep_wait();
+  const long long idx = static_cast<long long>(blockIdx.x) * kCopyThreads + threadIdx.x;
+  const int c = static_cast<int>(idx % p.chunks);
+  const long long rest = idx / p.chunks;
+  const int g = static_cast<int>(rest % p.hkv);
+  const long long i0 = rest / p.hkv * kRowsPer;
+  if (i0 >= p.keep) return;
+  const int32_t* kept = p.kept + static_cast<int64_t>(g) * p.keep;
+  uint4 k[kRowsPer], v[kRowsPer];
+#pragma unroll
+  for (int u = 0; u < kRowsPer; ++u) {
+    if (i0 + u >= p.keep) break;
+    const int64_t row = min(max(kept[i0 + u], 0), p.prefix_len - 1);
+    const int64_t at = row * p.row + g * p.head + c;
+    k[u] = __ldcs(p.k + at);
+    v[u] = __ldcs(p.v + at);
+  }
+#pragma unroll
+  for (int u = 0; u < kRowsPer; ++u) {
+    if (i0 + u >= p.keep) break;
+    const int64_t to = (i0 + u) * p.out_row + g * p.out_head + c;
+    p.k_out[to] = k[u];
+    p.v_out[to] = v[u];
+  }
+}
+
+// Bytes from the first to the last element of a strided [rows, heads, d] tensor.
+size_t extent(long long rows, int heads, int d, int64_t row, int64_t head, int esz) {
+  return rows == 0 ? 0 : static_cast<size_t>((rows - 1) * row + (heads - 1) * head + d) * esz;
+}
+bool meet(const void* a, size_t na, const void* b, size_t nb) {
+  const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
+  return na > 0 && nb > 0 && x < y + nb && y < x + na;
+}
+
+dard_status prepare(const dard_prefix_evict_args* a, EvictParams& p) {
+  memset(&p, 0, sizeof(p));
+  if (!a) return report(DARD_ERR_NULL, "args is NULL");
+  if (a->dtype != DARD_BF16 && a->dtype != DARD_F32)
+    return report(DARD_ERR_VALUE, "dtype %d is neither DARD_F32 nor DARD_BF16", a->dtype);
+  if (a->hkv < 1 || a->hkv > 65535) return report(DARD_ERR_SHAPE, "hkv %d outside 1..65535", a->hkv);
+  if (a->head_dim != 64 && a->head_dim != 128)
+    return report(DARD_ERR_UNSUPPORTED, "head_dim %d (supported: 64, 128)", a->head_dim);
+  if (a->prefix_len < 0 || a->prefix_len > DARD_PREFIX_MAX_LEN)
+    return report(DARD_ERR_SHAPE, "prefix_len %d outside 0..%d", a->prefix_len, DARD_PREFIX_MAX_LEN);
+  if (a->keep_first < 0 || a->keep_last < 0 || a->keep > a->prefix_len ||
+      static_cast<long long>(a->keep_first) + a->keep_last > a->keep)
+    return report(DARD_ERR_SHAPE, "need 0 <= keep_first + keep_last <= keep <= prefix_len, got %d + %d, %d, %d",
+                  a->keep_first, a->keep_last, a->keep, a->prefix_len);
+  p.hkv = a->hkv;
+  p.prefix_len = a->prefix_len;
+  p.keep = a->keep;
+  p.first = a->keep_first;
+  p.last = a->keep_last;
+  if (a->keep == 0) return DARD_OK;
+  const int esz = a->dtype == DARD_BF16 ? 2 : 4;
+  if (!a->weights || !a->kept) return report(DARD_ERR_NULL, "weights or kept is NULL");
+  if (a->weights_stride < a->prefix_len) return report(DARD_ERR_SHAPE, "weights_stride is below prefix_len");
+  if (((reinterpret_cast<uintptr_t>(a->weights) | reinterpret_cast<uintptr_t>(a->kept) |
+        reinterpret_cast<uintptr_t>(a->weights_out)) & 3u) != 0)
+    return report(DARD_ERR_ALIGN, "weights, kept and weights_out must be 4-byte aligned");
+  const bool move = a->prefix_k || a->prefix_v || a->k_out || a->v_out;
+  size_t in = 0, out = 0;
+  if (move) {
+    if (!a->prefix_k || !a->prefix_v || !a->k_out || !a->v_out)
+      return report(DARD_ERR_NULL, "prefix_k, prefix_v, k_out and v_out come together");
+    const int64_t most = 1ll << 36;
+    if (a->prefix_row_stride < a->head_dim || a->prefix_head_stride < a->head_dim ||
+        a->out_row_stride < a->head_dim || a->out_head_stride < a->head_dim ||
+        a->prefix_row_stride > most || a->prefix_head_stride > most || a->out_row_stride > most ||
+        a->out_head_stride > most)
+      return report(DARD_ERR_SHAPE, "strides outside head_dim..2^36");
+    if (((reinterpret_cast<uintptr_t>(a->prefix_k) | reinterpret_cast<uintptr_t>(a->prefix_v) |
+          reinterpret_cast<uintptr_t>(a->k_out) | reinterpret_cast<uintptr_t>(a->v_out) |
+          static_cast<uintptr_t>(a->prefix_row_stride * esz) |
+          static_cast<uintptr_t>(a->prefix_head_stride * esz) |
+          static_cast<uintptr_t>(a->out_row_stride * esz) |
+          static_cast<uintptr_t>(a->out_head_stride * esz)) & 15u) != 0)
+      return report(DARD_ERR_ALIGN, "keys, values and their strides must be multiples of 16 bytes");
+    in = extent(a->prefix_len, a->hkv, a->head_dim, a->prefix_row_stride, a->prefix_head_stride, esz);
+    out = extent(a->keep, a->hkv, a->head_dim, a->out_row_stride, a->out_head_stride, esz);
+  }
+  const size_t w_in = static_cast<size_t>((a->hkv - 1) * a->weights_stride + a->prefix_len) * 4;
+  const size_t list = static_cast<size_t>(a->hkv) * a->keep * 4;
+  const void* const ins[3] = {a->weights, a->prefix_k, a->prefix_v};
+  const size_t in_bytes[3] = {w_in, in, in};
+  const void* const outs[4] = {a->kept, a->weights_out, a->k_out, a->v_out};
+  const size_t out_bytes[4] = {list, a->weights_out ? list : 0, out, out};
+  for (int i = 0; i < 3; ++i)
+    for (int o = 0; o < 4; ++o)
+      if (meet(ins[i], in_bytes[i], outs[o], out_bytes[o]))
+        return report(DARD_ERR_VALUE, "an output overlaps an input");
+  p.w = a->weights;
+  p.w_stride = a->weights_stride;
+  p.kept = a->kept;
+  p.w_out = a->weights_out;
+  if (move) {
+    const int per = 16 / esz;
+    p.k = static_cast<const uint4*>(a->prefix_k);
+    p.v = static_cast<const uint4*>(a->prefix_v);
+    p.k_out = static_cast<uint4*>(a->k_out);
+    p.v_out = static_cast<uint4*>(a->v_out);
+    p.row = a->prefix_row_stride / per;
+    p.head = a->prefix_head_stride / per;
+    p.out_row = a->out_row_stride / per;
+    p.out_head = a->out_head_stride / per;
+    p.chunks = a->head_dim / per;
+  }
+  return DARD_OK;
+}
+
+}  // namespace
+}  // namespace dard
+
+extern "C" dard_status dard_prefix_evict(const dard_prefix_evict_args* args, void* stream_ptr) {
+  using namespace dard;
+  report(DARD_OK, "%s", "");
+  EvictParams p;
+  const dard_status st = prepare(args, p);
+  if (st != DARD_OK) return st;
+  if (p.keep == 0) return DARD_OK;
+  if (std::getenv("DARD_TEST_FAIL_LAUNCH") != nullptr)
+    return report(DARD_ERR_CUDA, "prefix eviction launch failed: %s (DARD_TEST_FAIL_LAUNCH)",
+                  cudaGetErrorString(cudaErrorLaunchFailure));
+  const cudaStream_t stream = static_cast<cudaStream_t>(stream_ptr);
+  int ctas = 1;  // of a head: each about 4096 candidates or more
+  while (ctas < kMaxCluster && p.prefix_len / ctas > 8192) ctas *= 2;
+  const AttnLaunch S(static_cast<unsigned>(p.hkv) * ctas, kSelThreads, 0, stream, ctas, false);
+  cudaError_t e = cudaLaunchKernelEx(&S.cfg, evict_select, p, ctas);
+  if (e == cudaSuccess && p.k) {
+    const long long threads = (static_cast<long long>(p.keep) + kRowsPer - 1) / kRowsPer * p.hkv * p.chunks;
+    const long long blocks = (threads + kCopyThreads - 1) / kCopyThreads;
+    if (blocks > 0x7fffffffll) return report(DARD_ERR_SHAPE, "too many rows to move");
+    const AttnLaunch C(static_cast<unsigned>(blocks), kCopyThreads, 0, stream, 1, true);
+    e = cudaLaunchKernelEx(&C.cfg, evict_copy, p);
+  }
+  if (e != cudaSuccess)
+    return report(DARD_ERR_CUDA, "prefix eviction launch failed: %s", cudaGetErrorString(e));
+  return DARD_OK;
+}

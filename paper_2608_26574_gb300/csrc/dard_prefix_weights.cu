@@ -1,0 +1,602 @@
+// dard_prefix_weights.cu - the attention weight that each key of a shared prefix has received
+// (dard_prefix_weights): per key/value head g and key j the sum over the query rows and the heads
+// of the group of exp(c <q, k_j> - lse). Validation, the bf16 kernel on the tensor cores, the fp32
+// kernel on CUDA cores, and the kernel that adds up the parts of a split.
+//
+// weights_tc: 128 keys of one key/value head stay in shared memory as the A operand; tiles of
+// up to 128 (row, head) queries pass by as B, so that an accumulator row is a key and a thread
+// adds up its key's exponentials along the row: no reduction across threads until the end, no
+// atomics, one order of addition. 11 warps:
+//   warps 0-7  exponentials and sums: warps w and w + 4 share TMEM lane quarter w (keys 32w ..
+//              32w + 31), each taking 64 of a tile's 128 queries;
+//   warp 8     TMA producer: the K tile, then Q through 4 stages;
+//   warp 9     TMEM allocator and issuer: S_j = K Q_j^T into a ring of four 128-column buffers;
+//   warp 10    the queries' normalisers through 4 stages.
+// Each tile's sum is formed on its own and then added to the key's total (two levels: the
+// rounding of a long sum grows with the number of tiles, not of queries).
+#include <algorithm>
+#include <cstdio>
+#include <cstdlib>
+#include <cstring>
+
+#include "dard_attn_common.cuh"
+
+namespace dard {
+namespace {
+
+struct WeightsParams {
+  const void* q;
+  const float* lse;
+  const void* pk;
+  const float* w_in;
+  float* w;
+  float* part;               // [nsplit][hkv][prefix_len], nsplit > 1
+  uint32_t* status;
+  int64_t row_stride, head_stride, w_in_stride, w_stride;
+  int32_t rows, hq, hkv, prefix_len, group;
+  int32_t box_heads, box_rows, head_blocks;  // a query tile: box_rows rows x box_heads heads
+  int32_t q_tiles, key_tiles, nsplit;
+  float scale_log2, decay;
+  long long wait_cycles;
+  int32_t test_drop_kv;
+};
+
+constexpr float kLog2e = 1.4426950408889634f;
+
+// Adds what the earlier sum contributes.
+__device__ __forceinline__ float with_earlier(const WeightsParams& p, int g, int key, float sum) {
+  return p.w_in ? fmaf(p.decay, p.w_in[g * p.w_in_stride + key], sum) : sum;
+}
+
+// ---------------------------------------------------------------- bf16, tensor cores
+constexpr int kThreads = 352;
+constexpr int kQStages = 4, kSBufs = 4;
+constexpr int kWorkers = 8;
+constexpr int kWProd = 8, kWMma = 9, kWLse = 10;
+
+struct __align__(16) Ctl {
+  uint64_t k_full;
+  uint64_t q_full[kQStages], q_empty[kQStages];
+  uint64_t l_full[kQStages], l_empty[kQStages];
+  uint64_t s_full[kSBufs], s_free[kSBufs];
+  uint64_t drained;
+  uint32_t tmem_base;
+  int32_t abort;
+  __align__(16) float lse[kQStages][kBM];  // times log2 e (read four at a time)
+  uint32_t off[kQStages][4];      // queries that add nothing (bit per column)
+  float red[kBM];
+};
+
+template <int D>
+constexpr size_t smem_bytes() {
+  return 1024 + (1 + kQStages) * static_cast<size_t>(kTN) * D * 2 + sizeof(Ctl);
+}
+
+__device__ __forceinline__ void flag_timeout(const WeightsParams& p, Ctl& ctl) {
+  ctl.abort = 1;
+  if (p.status) atomicOr(p.status, DARD_STATUS_TIMEOUT);
+}
+
+__device__ __forceinline__ void tma_load_3d(void* dst, const void* desc, uint64_t* bar, int32_t c0,
+                                            int32_t c1, int32_t c2) {
+  asm volatile(
+      "cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes"
+      " [%0], [%1, {%3, %4, %5}], [%2];" ::"r"(smem_u32(dst)),
+      "l"(reinterpret_cast<uint64_t>(desc)), "r"(smem_u32(bar)), "r"(c0), "r"(c1), "r"(c2)
+      : "memory");
+}
+
+// Sum over 32 columns of 2^(s sl - lse) for one key.
+template <bool kOff>
+__device__ __forceinline__ float sum32(const uint32_t (&s)[32], const float* lse, uint32_t off,
+                                       uint64_t sl2) {
+  uint64_t acc[4] = {0, 0, 0, 0};
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    const float4 n = *reinterpret_cast<const float4*>(lse + 4 * e);
+    float x[4];
+    f2_unpack(f2_fma(f2_pack(__uint_as_float(s[4 * e]), __uint_as_float(s[4 * e + 1])), sl2,
+                     f2_pack(-n.x, -n.y)), x[0], x[1]);
+    f2_unpack(f2_fma(f2_pack(__uint_as_float(s[4 * e + 2]), __uint_as_float(s[4 * e + 3])), sl2,
+                     f2_pack(-n.z, -n.w)), x[2], x[3]);
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      x[k] = ex2_approx(x[k]);
+      if (kOff && (off >> (4 * e + k) & 1u)) x[k] = 0.f;
+    }
+    acc[(2 * e) & 3] = f2_add(acc[(2 * e) & 3], f2_pack(x[0], x[1]));
+    acc[(2 * e + 1) & 3] = f2_add(acc[(2 * e + 1) & 3], f2_pack(x[2], x[3]));
+  }
+  float a, b;
+  f2_unpack(f2_add(f2_add(acc[0], acc[1]), f2_add(acc[2], acc[3])), a, b);
+  return a + b;
+}
+
+template <int D>
+__global__ void __launch_bounds__(kThreads, 1)
+    weights_tc(const __grid_constant__ WeightsParams p, const __grid_constant__ CUtensorMap tk,
+               const __grid_constant__ CUtensorMap tq) {
+  constexpr int kSub = D / 64;
+  constexpr uint32_t kKSub = kTN * 128;
+  constexpr uint32_t kTile = kSub * kKSub;
+  extern __shared__ uint8_t smem_raw[];
+  uint8_t* base = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) &
+                                             ~static_cast<uintptr_t>(1023));
+  uint8_t* sK = base;
+  uint8_t* sQ = sK + kTile;
+  Ctl& ctl = *reinterpret_cast<Ctl*>(sQ + kQStages * kTile);
+  grid_dep_launch();
+  const int item = blockIdx.x / p.nsplit, part = blockIdx.x % p.nsplit;
+  const int g = item / p.key_tiles, key0 = item % p.key_tiles * kTN;
+  const int j0 = static_cast<int>(static_cast<long long>(p.q_tiles) * part / p.nsplit);
+  const int n = static_cast<int>(static_cast<long long>(p.q_tiles) * (part + 1) / p.nsplit) - j0;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const long long wlim = p.wait_cycles > 0 ? p.wait_cycles : kWaitCycles;
+  const int columns = p.box_heads * p.box_rows;  // queries of a tile, at most 128
+
+  if (warp == kWProd && lane == 0) {
+    mbar_init(&ctl.k_full, 1);
+    mbar_init(&ctl.drained, 1);
+    for (int b = 0; b < kQStages; ++b) {
+      mbar_init(&ctl.q_full[b], 1);
+      mbar_init(&ctl.q_empty[b], 1);
+      mbar_init(&ctl.l_full[b], 1);
+      mbar_init(&ctl.l_empty[b], kWorkers);
+    }
+    for (int b = 0; b < kSBufs; ++b) {
+      mbar_init(&ctl.s_full[b], 1);
+      mbar_init(&ctl.s_free[b], kWorkers);
+    }
+    ctl.abort = 0;
+    fence_barrier_init();
+  }
+  if (warp == kWMma) {
+    tmem_alloc<kTmemCols>(&ctl.tmem_base);
+    tmem_relinquish();
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  volatile int32_t* abort_flag = &ctl.abort;
+
+  if (warp == kWProd) {
+    // ------------------------------------------------------------ TMA producer
+    if (lane == 0) {
+      mbar_arrive_expect_tx(&ctl.k_full, kTile);
+      const bool drop = p.test_drop_kv == 0;  // test hook: the K copy is never issued
+      if (!drop)
+        for (int s = 0; s < kSub; ++s) tma_load_3d(sK + s * kKSub, &tk, &ctl.k_full, s * 64, key0, g);
+      int last = -1;
+      for (int j = 0; j < n && !*abort_flag; ++j) {
+        const int b = j % kQStages;
+        if (j >= kQStages && !mbar_wait(&ctl.q_empty[b], ((j - kQStages) / kQStages) & 1, wlim)) {
+          flag_timeout(p, ctl);
+          break;
+        }
+        const int tile = j0 + j;
+        const int head = g * p.group + tile % p.head_blocks * p.box_heads;
+        const int row = tile / p.head_blocks * p.box_rows;
+        mbar_arrive_expect_tx(&ctl.q_full[b], kSub * columns * 128);
+        for (int s = 0; s < kSub; ++s)
+          tma_load_3d(sQ + b * kTile + s * kKSub, &tq, &ctl.q_full[b], s * 64, head, row);
+        last = j;
+      }
+      // every copy issued lands before shared memory is released: the latest use of each stage
+      for (int b = 0; b < kQStages; ++b) {
+        const int jb = last - ((last - b) % kQStages + kQStages) % kQStages;
+        if (last >= 0 && jb >= 0) mbar_wait(&ctl.q_full[b], (jb / kQStages) & 1, wlim);
+      }
+      if (!drop) mbar_wait(&ctl.k_full, 0, wlim);
+    }
+  } else if (warp == kWMma) {
+    // ------------------------------------------------------------ issuer
+    if (lane == 0) {
+      constexpr uint32_t kId = idesc_bf16_f32(kBM, kTN, 0, 0);
+      const uint32_t ak = smem_u32(sK), aq = smem_u32(sQ);
+      bool ok = mbar_wait(&ctl.k_full, 0, wlim);
+      for (int j = 0; j < n && ok && !*abort_flag; ++j) {
+        const int b = j % kQStages, sb = j % kSBufs;
+        if (j >= kSBufs) ok = mbar_wait(&ctl.s_free[sb], ((j - kSBufs) / kSBufs) & 1, wlim);
+        ok = ok && mbar_wait(&ctl.q_full[b], (j / kQStages) & 1, wlim);
+        if (!ok) break;
+        tc_fence_after();
+#pragma unroll
+        for (int ks = 0; ks < D / 16; ++ks) {
+          const uint32_t off = (ks >> 2) * kKSub + (ks & 3) * 32;
+          mma_ss(ctl.tmem_base + sb * kTN, smem_desc_sw128(ak + off, 16, 1024),
+                 smem_desc_sw128(aq + b * kTile + off, 16, 1024), kId, ks > 0);
+        }
+        mma_commit(&ctl.s_full[sb]);
+        mma_commit(&ctl.q_empty[b]);
+      }
+      if (!ok) flag_timeout(p, ctl);
+      mma_commit(&ctl.drained);
+    }
+  } else if (warp == kWLse) {
+    // ------------------------------------------------------------ normalisers
+    bool ok = true;
+    for (int j = 0; j < n && ok && !*abort_flag; ++j) {
+      const int b = j % kQStages, tile = j0 + j;
+      float v[4];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {  // column 32 e + lane
+        const int c = 32 * e + lane;
+        const int h = tile % p.head_blocks * p.box_heads + c % p.box_heads;
+        const int64_t row = static_cast<int64_t>(tile / p.head_blocks) * p.box_rows + c / p.box_heads;
+        v[e] = c < columns && h < p.group && row < p.rows
+                   ? __ldg(p.lse + row * p.hq + g * p.group + h) : INFINITY;
+      }
+      if (j >= kQStages) ok = mbar_wait(&ctl.l_empty[b], ((j - kQStages) / kQStages) & 1, wlim);
+      ok = __all_sync(0xffffffffu, ok);
+      if (!ok) break;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const uint32_t off = __ballot_sync(0xffffffffu, v[e] == INFINITY);
+        ctl.lse[b][32 * e + lane] = v[e] * kLog2e;
+        if (lane == 0) ctl.off[b][e] = off;
+      }
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&ctl.l_full[b]);
+    }
+    if (!ok && lane == 0) flag_timeout(p, ctl);
+  } else {
+    // ------------------------------------------------------------ exponentials and sums
+    const int quarter = warp & 3, half = warp >> 2;
+    const uint32_t lane_off = static_cast<uint32_t>(quarter * 32) << 16;
+    const uint64_t sl2 = f2_pack(p.scale_log2, p.scale_log2);
+    float total = 0.f;
+    bool ok = true;
+    for (int j = 0; j < n && ok; ++j) {
+      const int b = j % kQStages, sb = j % kSBufs;
+      ok = !*abort_flag && mbar_wait(&ctl.l_full[b], (j / kQStages) & 1, wlim) &&
+           mbar_wait(&ctl.s_full[sb], (j / kSBufs) & 1, wlim);
+      if (!__all_sync(0xffffffffu, ok)) { ok = false; break; }
+      tc_fence_after();
+      uint32_t r0[32], r1[32];
+      tmem_ld32(ctl.tmem_base + sb * kTN + 64 * half + lane_off, r0);
+      tmem_ld32(ctl.tmem_base + sb * kTN + 64 * half + 32 + lane_off, r1);
+      tmem_wait_ld();
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&ctl.s_free[sb]);
+      const float* lse = ctl.lse[b] + 64 * half;
+      const uint32_t off0 = ctl.off[b][2 * half], off1 = ctl.off[b][2 * half + 1];
+      float sum = 0.f;
+      if ((off0 | off1) == 0) {
+        sum = sum32<false>(r0, lse, 0, sl2) + sum32<false>(r1, lse + 32, 0, sl2);
+      } else {
+        if (off0 != 0xffffffffu) sum = sum32<true>(r0, lse, off0, sl2);
+        if (off1 != 0xffffffffu) sum += sum32<true>(r1, lse + 32, off1, sl2);
+      }
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&ctl.l_empty[b]);
+      total += sum;
+    }
+    const bool wok = __all_sync(0xffffffffu, ok);
+    if (!wok && lane == 0) flag_timeout(p, ctl);
+    const int t = quarter * 32 + lane;
+    if (half == 1) ctl.red[t] = total;
+    softmax_bar_sync();
+    const int key = key0 + t;
+    if (half == 0 && wok && key < p.prefix_len) {
+      total += ctl.red[t];
+      if (p.nsplit > 1)
+        p.part[(static_cast<size_t>(part) * p.hkv + g) * p.prefix_len + key] = total;
+      else
+        p.w[g * p.w_stride + key] = with_earlier(p, g, key, total);
+    }
+  }
+  tc_fence_before();
+  __syncthreads();
+  if (warp == kWMma) {
+    if (lane == 0 && !mbar_wait(&ctl.drained, 0, wlim)) flag_timeout(p, ctl);
+    __syncwarp();
+    tc_fence_after();
+    tmem_dealloc<kTmemCols>(ctl.tmem_base);
+  }
+}
+
+// ---------------------------------------------------------------- fp32, CUDA cores
+// 256 threads (16 x 16) hold 128 keys and take 64 queries at a time through shared memory: thread
+// (ty, tx) computes the scores of keys ty + 16 u and queries tx + 16 i (a 16-byte shared-memory
+// load serves 4 or 8 dot products), and adds up its keys' exponentials.
+constexpr int kFThreads = 256, kFKeys = 128, kFQueries = 64;
+
+__device__ __forceinline__ int swz(int row, int c) { return c ^ (row & 7); }
+
+template <int D>
+constexpr size_t f32_smem() {
+  return sizeof(float) * ((kFKeys + 2 * kFQueries) * D + 2 * kFQueries);
+}
+
+template <int D>
+__global__ void __launch_bounds__(kFThreads) weights_f32(const __grid_constant__ WeightsParams p) {
+  constexpr int kC = D / 4, kU = kFKeys / 16, kI = kFQueries / 16;
+  extern __shared__ __align__(16) uint8_t smem_raw[];
+  float4* sK = reinterpret_cast<float4*>(smem_raw);
+  float4* sQ = sK + kFKeys * kC;  // two tiles
+  float* sL = reinterpret_cast<float*>(sQ + 2 * kFQueries * kC);
+  grid_dep_launch();
+  const int item = blockIdx.x / p.nsplit, part = blockIdx.x % p.nsplit;
+  const int g = item / p.key_tiles, key0 = item % p.key_tiles * kFKeys;
+  const int j0 = static_cast<int>(static_cast<long long>(p.q_tiles) * part / p.nsplit);
+  const int j1 = static_cast<int>(static_cast<long long>(p.q_tiles) * (part + 1) / p.nsplit);
+  const int tid = threadIdx.x, tx = tid & 15, ty = tid >> 4;
+  const int64_t queries = static_cast<int64_t>(p.rows) * p.group;
+  for (int i = tid; i < kFKeys * kC; i += kFThreads) {
+    const int r = i / kC, c = i % kC;
+    const bool in = key0 + r < p.prefix_len;
+    cp_async16(sK + r * kC + swz(r, c),
+               static_cast<const float*>(p.pk) +
+                   (in ? (key0 + r) * p.row_stride + g * p.head_stride + 4 * c : 0), in ? 16 : 0);
+  }
+  auto load = [&](int j, int b) {
+    for (int i = tid; i < kFQueries * kC; i += kFThreads) {
+      const int t = i / kC, c = i % kC;
+      const int64_t m = static_cast<int64_t>(j) * kFQueries + t;
+      const bool in = m < queries;
+      const int64_t at = in ? m / p.group * p.hq + g * p.group + m % p.group : 0;
+      cp_async16(sQ + (b * kFQueries + t) * kC + swz(t, c), static_cast<const float*>(p.q) + at * D + 4 * c,
+                 in ? 16 : 0);
+    }
+    cp_async_commit();
+    if (tid < kFQueries) {
+      const int64_t m = static_cast<int64_t>(j) * kFQueries + tid;
+      sL[b * kFQueries + tid] =
+          m < queries ? __ldg(p.lse + m / p.group * p.hq + g * p.group + m % p.group) * kLog2e : INFINITY;
+    }
+  };
+  load(j0, 0);
+  float total[kU];
+#pragma unroll
+  for (int u = 0; u < kU; ++u) total[u] = 0.f;
+  for (int j = j0; j < j1; ++j) {
+    const int b = (j - j0) & 1;
+    cp_async_wait_all();
+    __syncthreads();  // tile j is there, and tile j - 1 has been read
+    if (j + 1 < j1) load(j + 1, b ^ 1);
+    const float4* q = sQ + b * kFQueries * kC;
+    float s[kU][kI];
+#pragma unroll
+    for (int u = 0; u < kU; ++u)
+#pragma unroll
+      for (int i = 0; i < kI; ++i) s[u][i] = 0.f;
+#pragma unroll 4
+    for (int c = 0; c < kC; ++c) {
+      float4 qf[kI];
+#pragma unroll
+      for (int i = 0; i < kI; ++i) qf[i] = q[(tx + 16 * i) * kC + swz(tx, c)];
+#pragma unroll
+      for (int u = 0; u < kU; ++u) {
+        const float4 kf = sK[(ty + 16 * u) * kC + swz(ty, c)];
+#pragma unroll
+        for (int i = 0; i < kI; ++i) {
+          s[u][i] = fmaf(qf[i].x, kf.x, s[u][i]);
+          s[u][i] = fmaf(qf[i].y, kf.y, s[u][i]);
+          s[u][i] = fmaf(qf[i].z, kf.z, s[u][i]);
+          s[u][i] = fmaf(qf[i].w, kf.w, s[u][i]);
+        }
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < kI; ++i) {
+      const float lse = sL[b * kFQueries + tx + 16 * i];
+      if (lse == INFINITY) continue;  // adds nothing, whatever q holds
+#pragma unroll
+      for (int u = 0; u < kU; ++u) total[u] += exp2f(fmaf(s[u][i], p.scale_log2, -lse));
+    }
+  }
+#pragma unroll
+  for (int u = 0; u < kU; ++u) {
+    float sum = total[u];
+#pragma unroll
+    for (int x = 8; x > 0; x >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, x);
+    const int key = key0 + ty + 16 * u;
+    if (tx != 0 || key >= p.prefix_len) continue;
+    if (p.nsplit > 1)
+      p.part[(static_cast<size_t>(part) * p.hkv + g) * p.prefix_len + key] = sum;
+    else
+      p.w[g * p.w_stride + key] = with_earlier(p, g, key, sum);
+  }
+}
+
+// The parts of a split launch, added in order; without parts (no rows) what is left of the earlier
+// sum.
+__global__ void __launch_bounds__(256) weights_join(const __grid_constant__ WeightsParams p) {
+  grid_dep_wait();
+  const int key = static_cast<int>(blockIdx.x * 256u + threadIdx.x);
+  const int g = blockIdx.y;
+  if (key >= p.prefix_len) return;
+  float sum = 0.f;
+#pragma unroll 8
+  for (int c = 0; c < p.nsplit; ++c)
+    sum += p.part[(static_cast<size_t>(c) * p.hkv + g) * p.prefix_len + key];
+  p.w[g * p.w_stride + key] = with_earlier(p, g, key, sum);
+}
+
+// ---------------------------------------------------------------- host side
+constexpr int kParts = 64;               // parts of a split launch at most
+constexpr long long kSplitCtas = 1024;   // CTAs of a split launch at most
+
+bool make_map3(CUtensorMap* m, const void* ptr, int d, long long n1, long long n2, int64_t stride1,
+               int64_t stride2, int box1, int box2) {
+  auto fn = encode_fn();
+  if (!fn) return false;
+  const cuuint64_t dims[3] = {static_cast<cuuint64_t>(d), static_cast<cuuint64_t>(n1),
+                              static_cast<cuuint64_t>(n2)};
+  const cuuint64_t strides[2] = {static_cast<cuuint64_t>(stride1) * 2, static_cast<cuuint64_t>(stride2) * 2};
+  const cuuint32_t box[3] = {64, static_cast<cuuint32_t>(box1), static_cast<cuuint32_t>(box2)};
+  const cuuint32_t estr[3] = {1, 1, 1};
+  return fn(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(ptr), dims, strides, box, estr,
+            CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+            CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+template <int D>
+cudaError_t launch_tc(const WeightsParams& p, cudaStream_t stream) {
+  static std::atomic<uint64_t> done{0};
+  CUtensorMap k, q;
+  if (!make_map3(&k, p.pk, D, p.prefix_len, p.hkv, p.row_stride, p.head_stride, kTN, 1) ||
+      !make_map3(&q, p.q, D, p.hq, p.rows, D, static_cast<int64_t>(p.hq) * D, p.box_heads, p.box_rows))
+    return cudaErrorInvalidValue;
+  const cudaError_t e = ensure_smem_attr(weights_tc<D>, smem_bytes<D>(), done);
+  if (e != cudaSuccess) return e;
+  const AttnLaunch L(static_cast<unsigned>(p.hkv) * p.key_tiles * p.nsplit, kThreads, smem_bytes<D>(),
+                     stream, 1, false);
+  return cudaLaunchKernelEx(&L.cfg, weights_tc<D>, p, k, q);
+}
+
+template <int D>
+cudaError_t launch_f32(const WeightsParams& p, cudaStream_t stream) {
+  static std::atomic<uint64_t> done{0};
+  const cudaError_t e = ensure_smem_attr(weights_f32<D>, f32_smem<D>(), done);
+  if (e != cudaSuccess) return e;
+  const AttnLaunch L(static_cast<unsigned>(p.hkv) * p.key_tiles * p.nsplit, kFThreads, f32_smem<D>(),
+                     stream, 1, false);
+  return cudaLaunchKernelEx(&L.cfg, weights_f32<D>, p);
+}
+
+dard_status prepare(const dard_prefix_weights_args* a, WeightsParams& p) {
+  memset(&p, 0, sizeof(p));
+  if (!a) return report(DARD_ERR_NULL, "args is NULL");
+  if (a->dtype != DARD_BF16 && a->dtype != DARD_F32)
+    return report(DARD_ERR_VALUE, "dtype %d is neither DARD_F32 nor DARD_BF16", a->dtype);
+  if (a->rows < 0) return report(DARD_ERR_SHAPE, "rows %d < 0", a->rows);
+  if (a->hq < 1 || a->hkv < 1 || a->hq % a->hkv != 0)
+    return report(DARD_ERR_SHAPE, "hq %d / hkv %d: need hq %% hkv == 0", a->hq, a->hkv);
+  if (a->hkv > 65535) return report(DARD_ERR_SHAPE, "hkv %d above 65535", a->hkv);
+  if (a->head_dim != 64 && a->head_dim != 128)
+    return report(DARD_ERR_UNSUPPORTED, "head_dim %d (supported: 64, 128)", a->head_dim);
+  if (a->prefix_len < 0 || a->prefix_len > DARD_PREFIX_MAX_LEN)
+    return report(DARD_ERR_SHAPE, "prefix_len %d outside 0..%d", a->prefix_len, DARD_PREFIX_MAX_LEN);
+  if (!(a->scale >= 0.f) || !std::isfinite(a->scale))
+    return report(DARD_ERR_VALUE, "scale must be finite and >= 0");
+  if (!std::isfinite(a->decay)) return report(DARD_ERR_VALUE, "decay must be finite");
+  if (a->prefix_len == 0) return DARD_OK;
+  if (!a->weights) return report(DARD_ERR_NULL, "weights is NULL");
+  if (a->weights_stride < a->prefix_len || (a->weights_in && a->weights_in_stride < a->prefix_len))
+    return report(DARD_ERR_SHAPE, "a weights stride is below prefix_len");
+  if (a->weights_in == a->weights && a->weights_in_stride != a->weights_stride)
+    return report(DARD_ERR_VALUE, "weights_in may be weights with the same stride only");
+  if (((reinterpret_cast<uintptr_t>(a->weights) | reinterpret_cast<uintptr_t>(a->weights_in) |
+        reinterpret_cast<uintptr_t>(a->lse)) & 3u) != 0)
+    return report(DARD_ERR_ALIGN, "weights, weights_in and lse must be 4-byte aligned");
+  const int esz = a->dtype == DARD_BF16 ? 2 : 4;
+  if (a->rows > 0) {
+    if (!a->q || !a->lse || !a->prefix_k) return report(DARD_ERR_NULL, "q, lse or prefix_k is NULL");
+    if (static_cast<long long>(a->rows) * a->hq > (1ll << 31) - 256)
+      return report(DARD_ERR_SHAPE, "rows times hq exceed 2^31 - 256");
+    if (a->prefix_row_stride < a->head_dim || a->prefix_head_stride < a->head_dim ||
+        a->prefix_row_stride > (1ll << 36) || a->prefix_head_stride > (1ll << 36))
+      return report(DARD_ERR_SHAPE, "prefix strides outside head_dim..2^36");
+    if (((reinterpret_cast<uintptr_t>(a->q) | reinterpret_cast<uintptr_t>(a->prefix_k) |
+          static_cast<uintptr_t>(a->prefix_row_stride * esz) |
+          static_cast<uintptr_t>(a->prefix_head_stride * esz)) & 15u) != 0)
+      return report(DARD_ERR_ALIGN, "q, prefix_k and its strides must be multiples of 16 bytes");
+  }
+  const size_t need = dard_prefix_weights_workspace_size(a->rows, a->hq, a->hkv, a->head_dim,
+                                                         a->prefix_len);
+  if (a->workspace && a->workspace_bytes < need)
+    return report(DARD_ERR_WORKSPACE, "workspace of %zu bytes needed", need);
+  if ((reinterpret_cast<uintptr_t>(a->workspace) & 15u) != 0)
+    return report(DARD_ERR_ALIGN, "workspace must be 16-byte aligned");
+  p.q = a->q;
+  p.lse = a->lse;
+  p.pk = a->prefix_k;
+  p.w_in = a->weights_in;
+  p.w = a->weights;
+  p.part = static_cast<float*>(a->workspace);
+  p.status = a->status;
+  p.row_stride = a->prefix_row_stride;
+  p.head_stride = a->prefix_head_stride;
+  p.w_in_stride = a->weights_in_stride;
+  p.w_stride = a->weights_stride;
+  p.rows = a->rows;
+  p.hq = a->hq;
+  p.hkv = a->hkv;
+  p.prefix_len = a->prefix_len;
+  p.group = a->hq / a->hkv;
+  p.decay = a->decay;
+  p.scale_log2 = (a->scale > 0.f ? a->scale : 1.0f / std::sqrt(static_cast<float>(a->head_dim))) * kLog2e;
+  p.test_drop_kv = -1;
+  return DARD_OK;
+}
+
+// Parts of the split: as few as give every SM a CTA or two, each with query tiles enough to pay for
+// its start (bounded by what the workspace holds).
+int choose_parts(long long items, int q_tiles, int sms) {
+  if (items >= 4ll * sms) return 1;
+  long long best = 1;
+  double best_time = 0;
+  for (long long s = 1; s <= std::min<long long>(kParts, q_tiles) && (s == 1 || items * s <= kSplitCtas); ++s) {
+    const double cta = 6.0 + std::ceil(static_cast<double>(q_tiles) / s);
+    const double n = static_cast<double>(items) * s;
+    const double time = (n <= sms ? cta : n * (6.0 + static_cast<double>(q_tiles) / s) / sms + 0.5 * cta) +
+                        (s > 1 ? 4.0 : 0.0);
+    if (s == 1 || time < best_time) {
+      best = s;
+      best_time = time;
+    }
+  }
+  return static_cast<int>(best);
+}
+
+}  // namespace
+}  // namespace dard
+
+extern "C" {
+
+size_t dard_prefix_weights_workspace_size(int32_t rows, int32_t hq, int32_t hkv, int32_t head_dim,
+                                          int32_t prefix_len) {
+  using namespace dard;
+  if (rows < 0 || hq < 1 || hkv < 1 || hq % hkv != 0 || (head_dim != 64 && head_dim != 128) ||
+      prefix_len < 0 || prefix_len > DARD_PREFIX_MAX_LEN)
+    return 0;
+  // at most kSplitCtas CTAs of 128 keys, so that many parts of 128 sums each
+  return kSplitCtas * 128 * sizeof(float);
+}
+
+dard_status dard_prefix_weights(const dard_prefix_weights_args* args, void* stream_ptr) {
+  using namespace dard;
+  report(DARD_OK, "%s", "");
+  WeightsParams p;
+  const dard_status st = prepare(args, p);
+  if (st != DARD_OK) return st;
+  if (args->prefix_len == 0) return DARD_OK;
+  const cudaStream_t stream = static_cast<cudaStream_t>(stream_ptr);
+  if (const char* w = std::getenv("DARD_TEST_WAIT_CYCLES")) p.wait_cycles = std::atoll(w);
+  if (const char* d = std::getenv("DARD_TEST_DROP_KV")) p.test_drop_kv = std::atoi(d);
+  if (std::getenv("DARD_TEST_FAIL_LAUNCH") != nullptr)
+    return report(DARD_ERR_CUDA, "prefix weights launch failed: %s (DARD_TEST_FAIL_LAUNCH)",
+                  cudaGetErrorString(cudaErrorLaunchFailure));
+  const bool bf16 = args->dtype == DARD_BF16;
+  cudaError_t e = cudaSuccess;
+  if (p.rows > 0) {
+    p.key_tiles = (p.prefix_len + 127) / 128;
+    if (bf16) {
+      p.box_heads = std::min(p.group, 128);
+      p.box_rows = std::min(128 / p.box_heads, p.rows);
+      p.head_blocks = (p.group + p.box_heads - 1) / p.box_heads;
+      p.q_tiles = (p.rows + p.box_rows - 1) / p.box_rows * p.head_blocks;
+    } else {
+      p.q_tiles = static_cast<int32_t>((static_cast<long long>(p.rows) * p.group + kFQueries - 1) / kFQueries);
+    }
+    const long long items = static_cast<long long>(p.key_tiles) * p.hkv;
+    if (items > (1ll << 31) - 1) return report(DARD_ERR_SHAPE, "too many key tiles");
+    p.nsplit = p.part ? choose_parts(items, p.q_tiles, sm_count()) : 1;
+    if (!bf16)
+      e = args->head_dim == 64 ? launch_f32<64>(p, stream) : launch_f32<128>(p, stream);
+    else
+      e = args->head_dim == 64 ? launch_tc<64>(p, stream) : launch_tc<128>(p, stream);
+  }
+  if (e == cudaSuccess && p.nsplit != 1) {
+    AttnLaunch L((p.prefix_len + 255) / 256, 256, 0, stream, 1, p.nsplit > 1);
+    L.cfg.gridDim.y = p.hkv;
+    e = cudaLaunchKernelEx(&L.cfg, weights_join, p);
+  }
+  if (e != cudaSuccess)
+    return report(DARD_ERR_CUDA, "prefix weights launch failed: %s", cudaGetErrorString(e));
+  return DARD_OK;
+}
+
+}  // extern "C"
