@@ -27,11 +27,11 @@ struct PrefixParams {
   int32_t q_before[DARD_MAX_SEQS + 1];  // query rows of the sequences before each
 };
 
-// Parts of a split launch: one slot per (tile, part), rows x (D + 3) floats: the unnormalised
-// output rows, then per row the reference maximum (times scale log2 e; -inf: no key), the sum of
-// the weights as the product uses them, and their sum unrounded (-1: a row that is not stored).
+// Parts of a split launch: one slot per (tile, part), rows x (D + 2) floats: the unnormalised
+// output rows, then per row the reference maximum (times scale log2 e; -inf: no key) and the sum of
+// the weights (-1 in a tile's last part: a row that is not stored).
 __host__ __device__ inline size_t part_slot_floats(int rows, int d) {
-  return static_cast<size_t>(rows) * (d + 3);
+  return static_cast<size_t>(rows) * (d + 2);
 }
 
 // The fp32 kernel on CUDA cores.
@@ -59,81 +59,143 @@ __device__ __forceinline__ void own_range(const PrefixParams& p, int m0, int row
   key_end = s.row_base + s.n_orig + s.slen;
 }
 
-// The masks of sequence-relative row r over its sequence's block, read from global memory by one
-// thread: what publish_block_info(), row_info() and row_masks() derive for a CTA whose rows are
-// all of one sequence. store = 0 for a shadow row whose shadow_src is invalid.
-__device__ RowMasks query_masks(const AttnParams& p, const SeqDesc& sd, int r, bool report,
-                                int& store) {
-  Bits128 mb{0, 0}, cb{0, 0}, hs{0, 0}, valid{0, 0};
-  uint32_t flags = 0;
-  const uint8_t* st = p.state + sd.blk_off;
-  for (int j0 = 0; j0 < sd.blen; j0 += 8) {
-    int s[8];
+// The masks of the rows of one warp over their sequences' blocks, read from global memory: what
+// publish_block_info(), row_info() and row_masks() derive for a CTA whose rows are all of one
+// sequence. Lane by lane: `seq` (-1: no row) and the sequence-relative row r; store = 0 for a
+// shadow row whose shadow_src is invalid. Called by whole warps. The lanes fetch a sequence's block
+// together, 32 positions each time, and every lane derives its row's masks from ballots of it.
+__device__ RowMasks warp_query_masks(const AttnParams& p, int seq, int r, bool report, int& store) {
+  constexpr uint32_t kAll = 0xffffffffu;
+  const int lane = threadIdx.x & 31;
+  RowMasks out{{0, 0}, {0, 0}};
+  store = seq >= 0;
+  uint32_t todo = __ballot_sync(kAll, seq >= 0);
+  while (todo) {
+    const int s = __shfl_sync(kAll, seq, __ffs(todo) - 1);
+    const bool mine = seq == s;
+    todo &= ~__ballot_sync(kAll, mine);
+    const SeqDesc& sd = p.seq[s];
+    const int blen = sd.blen, slen = sd.slen;
+    if (blen == 0) continue;  // no block, no shadow rows: nothing is hidden
+    int st[4], pos[4];
+    float cf[4];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) s[e] = j0 + e < sd.blen ? __ldg(st + j0 + e) : kStateU;
-    uint64_t m8 = 0, c8 = 0;
-#pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      if (s[e] > 2) flags |= DARD_STATUS_BAD_STATE;
-      m8 |= static_cast<uint64_t>(s[e] == kStateM || s[e] > 2) << e;
-      c8 |= static_cast<uint64_t>(s[e] == kStateC) << e;
+    for (int i = 0; i < 4; ++i) {
+      const int j = 32 * i + lane;
+      st[i] = j < blen ? __ldg(p.state + sd.blk_off + j) : kStateU;
+      cf[i] = j < blen ? __ldg(p.prev_conf + sd.blk_off + j) : 0.f;
+      pos[i] = j < slen ? __ldg(p.shadow_src + sd.sh_off + j) - sd.b0 : -1;
+      if (pos[i] >= blen) pos[i] = -1;
     }
-    if (j0 < 64) { mb.lo |= m8 << j0; cb.lo |= c8 << j0; }
-    else { mb.hi |= m8 << (j0 - 64); cb.hi |= c8 << (j0 - 64); }
-  }
-  // shadow rows: a repeated position keeps its lowest row
-  RowInfo q{0, kStateU, 0.f, -1, 1};
-  const int32_t* src = p.shadow_src + sd.sh_off;
-  const int kq = r - sd.n_orig;  // the row's shadow index, if it is one
-  if (kq >= 0) q.store = 0;
-  for (int k0 = 0; k0 < sd.slen; k0 += 8) {
-    int pos[8];
+    // bit words over block positions (m, c: states; hs: a shadow copy exists) and over shadow rows
+    // (valid: the position's lowest shadow row)
+    uint32_t m[4], c[4], hs[4] = {0, 0, 0, 0}, valid[4];
+    int rows = 0, positions = 0;
+    bool bad_state = false, identity = true;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) pos[e] = k0 + e < sd.slen ? __ldg(src + k0 + e) - sd.b0 : INT_MIN;
+    for (int i = 0; i < 4; ++i) {
+      m[i] = __ballot_sync(kAll, st[i] == kStateM || st[i] > 2);
+      c[i] = __ballot_sync(kAll, st[i] == kStateC);
+      valid[i] = __ballot_sync(kAll, pos[i] >= 0);
+      bad_state |= st[i] > 2;
+      identity &= 32 * i + lane >= slen || pos[i] == 32 * i + lane;
+      rows += __popc(valid[i]);
+      if (32 * i < slen) {
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      if (k0 + e >= sd.slen) break;
-      const bool ok = pos[e] >= 0 && pos[e] < sd.blen && !get_bit(hs, pos[e]);
-      if (!ok) { flags |= DARD_STATUS_BAD_SHADOW; continue; }
-      set_bit(hs, pos[e]);
-      set_bit(valid, k0 + e);
-      if (k0 + e == kq) { q.qs = 1; q.i = pos[e]; q.store = 1; }
+        for (int w = 0; w < 4; ++w)
+          if (32 * w < blen)
+            hs[w] |= __reduce_or_sync(kAll, pos[i] >= 0 && pos[i] >> 5 == w ? 1u << (pos[i] & 31) : 0u);
+      }
+    }
+#pragma unroll
+    for (int w = 0; w < 4; ++w) positions += __popc(hs[w]);
+    if (positions != rows) {  // a repeated position: its lowest row alone is valid
+      uint32_t seen[4] = {0, 0, 0, 0};
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        for (int l = 0; l < 32 && 32 * i + l < slen; ++l) {
+          const int x = __shfl_sync(kAll, pos[i], l);
+          if (x < 0) continue;
+          bool again = false;
+#pragma unroll
+          for (int w = 0; w < 4; ++w) {
+            const uint32_t bit = x >> 5 == w ? 1u << (x & 31) : 0u;
+            again |= (seen[w] & bit) != 0;
+            seen[w] |= bit;
+          }
+          if (again) valid[i] &= ~(1u << l);
+        }
+      }
+    }
+    identity = __all_sync(kAll, identity);
+    if (report && p.status) {
+      const uint32_t flags = (__any_sync(kAll, bad_state) ? DARD_STATUS_BAD_STATE : 0u) |
+                             (positions != slen ? DARD_STATUS_BAD_SHADOW : 0u);
+      if (lane == 0 && flags) atomicOr(p.status, flags);
+    }
+    // this lane's row
+    RowInfo q{0, kStateU, 0.f, -1, 1};
+    const int kq = r - sd.n_orig, j = r - sd.b0;  // its shadow index, its block position
+    if (kq < 0) {
+      if (j >= 0 && j < blen) q.i = j;
+      else q.si = j < 0 ? kStateU : kStateM;  // decoded context / still masked
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int x = __shfl_sync(kAll, pos[i], kq & 31);
+      if (kq >= 0 && kq >> 5 == i) {
+        q.qs = valid[i] >> (kq & 31) & 1u;
+        if (q.qs) q.i = x;
+        q.store = q.qs;
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const float x = __shfl_sync(kAll, cf[i], q.i & 31);
+      if (q.i >= 0 && q.i >> 5 == i) {
+        q.si = m[i] >> (q.i & 31) & 1u ? kStateM : c[i] >> (q.i & 31) & 1u ? kStateC : kStateU;
+        q.ci = x;
+      }
+    }
+    // positions taken from their shadow copy, as in row_masks()
+    uint32_t ts[4];
+    const bool is_c = q.si == kStateC;
+    const bool all_mc = q.si == kStateU || (q.si == kStateM && q.qs);
+    const bool any_c = __any_sync(kAll, mine && is_c);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      uint32_t lower = 0;  // C keys with !(c_i <= c_j) (Eq. 3)
+      if (any_c && 32 * i < blen) {
+#pragma unroll 8
+        for (int l = 0; l < 32; ++l)
+          lower |= static_cast<uint32_t>(!(q.ci <= __shfl_sync(kAll, cf[i], l))) << l;
+      }
+      ts[i] = all_mc ? m[i] | c[i] : is_c ? m[i] | (c[i] & lower) : 0u;
+      if (q.qs && q.i >> 5 == i) ts[i] |= 1u << (q.i & 31);
+    }
+    uint32_t see[4] = {0, 0, 0, 0};
+    if (identity) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) see[i] = ts[i] & valid[i];
+    } else {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        for (int l = 0; l < 32 && 32 * i + l < slen; ++l) {
+          const int x = __shfl_sync(kAll, pos[i], l);
+          const uint32_t word = x < 64 ? (x < 32 ? ts[0] : ts[1]) : (x < 96 ? ts[2] : ts[3]);
+          see[i] |= (word >> (x & 31) & 1u) << l;
+        }
+        see[i] &= valid[i];
+      }
+    }
+    if (mine) {
+      store = q.store;
+      const uint32_t hide[4] = {ts[0] & hs[0], ts[1] & hs[1], ts[2] & hs[2], ts[3] & hs[3]};
+      out.hide_x = words128(hide);
+      out.see_s = words128(see);
     }
   }
-  if (report && flags && p.status) atomicOr(p.status, flags);
-  if (kq < 0) {
-    const int j = r - sd.b0;
-    if (j >= 0 && j < sd.blen) q.i = j;
-    else q.si = j < 0 ? kStateU : kStateM;  // decoded context / still masked
-  }
-  if (q.i >= 0) {
-    q.si = get_bit(mb, q.i) ? kStateM : get_bit(cb, q.i) ? kStateC : kStateU;
-    q.ci = __ldg(p.prev_conf + sd.blk_off + q.i);
-  }
-  store = q.store;
-  // positions taken from their shadow copy, as in row_masks()
-  Bits128 ts{0, 0};
-  if (q.si == kStateU || (q.si == kStateM && q.qs)) {
-    ts = {mb.lo | cb.lo, mb.hi | cb.hi};
-  } else if (q.si == kStateC) {
-    Bits128 lower{0, 0};
-    const float* cf = p.prev_conf + sd.blk_off;
-    for (int j0 = 0; j0 < sd.blen; j0 += 8) {
-      uint64_t l8 = 0;
-#pragma unroll
-      for (int e = 0; e < 8; ++e)
-        l8 |= static_cast<uint64_t>(j0 + e < sd.blen && !(q.ci <= __ldg(cf + j0 + e))) << e;
-      if (j0 < 64) lower.lo |= l8 << j0; else lower.hi |= l8 << (j0 - 64);
-    }
-    ts = {mb.lo | (cb.lo & lower.lo), mb.hi | (cb.hi & lower.hi)};
-  }
-  if (q.qs && q.i >= 0) set_bit(ts, q.i);
-  RowMasks m;
-  m.hide_x = {ts.lo & hs.lo, ts.hi & hs.hi};
-  m.see_s = {0, 0};
-  for (int k = 0; k < sd.slen; ++k)
-    if (get_bit(valid, k) && get_bit(ts, __ldg(src + k) - sd.b0)) set_bit(m.see_s, k);
-  return m;
+  return out;
 }
 
 // Visibility of the 64 keys from sequence-relative row kt0 on (bit t = key kt0 + t); kt0 may lie

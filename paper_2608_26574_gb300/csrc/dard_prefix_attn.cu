@@ -5,19 +5,19 @@
 // prefix_tc: 128 packed queries (dard_prefix.cuh) of one key/value head against a run of key
 // tiles of 128: first the prefix's, with no mask but the ragged end of the last, then the rows of
 // the sequences that the tile touches, under each row's mask. One pass with a running maximum and
-// sum (the probabilities never leave the chip), fp32 accumulators. 12 warps:
-//   warps 0-7  softmax and epilogue: warps w and w + 4 share TMEM lane quarter w (queries 32w ..
-//              32w + 31), each taking 64 of a tile's 128 keys;
-//   warp 8     TMA producer: K and V through 3 stages each;
-//   warp 9     TMEM allocator and PV issuer: O += P_j V_j, P_j (bf16) read from TMEM;
-//   warp 10    S issuer: S_j = Q K_j^T (Q from TMEM, K from shared memory) into a ring of two
+// sum (the probabilities never leave the chip), fp32 accumulators. 20 warps:
+//   warps 0-15 softmax and epilogue: warps q, q + 4, q + 8 and q + 12 share TMEM lane quarter q
+//              (queries 32q .. 32q + 31), each taking 32 of a tile's 128 keys;
+//   warp 16    TMA producer: K and V through 3 stages each;
+//   warp 17    TMEM allocator and PV issuer: O += P_j V_j, P_j (bf16) read from TMEM;
+//   warp 18    S issuer: S_j = Q K_j^T (Q from TMEM, K from shared memory) into a ring of two
 //              128-column TMEM buffers;
-//   warp 11    own tiles only: looks for NaN and infinities in V (below).
+//   warp 19    own tiles only: looks for NaN and infinities in V (below).
 // TMEM: S ring [0, 256), O [256, 256 + D), P [384, 448), Q [448, 448 + D/2).
 //
 // Values that are not finite: the product with V multiplies every key of a tile by every query's
 // weight, and 0 times NaN is NaN. Keys of the prefix are seen by every query (rows behind its end
-// arrive as zeros), but an own tile holds copies and sequences that a query does not see. Warp 11
+// arrive as zeros), but an own tile holds copies and sequences that a query does not see. Warp 19
 // takes such values out of V before the product and adds them to the queries that do see the key.
 #include <algorithm>
 #include <cstdio>
@@ -29,11 +29,13 @@
 namespace dard {
 namespace {
 
-constexpr int kThreads = 384;
+constexpr int kThreads = 640;
 constexpr int kNS = 2;   // S buffers in TMEM
 constexpr int kNKV = 3;  // TMA stages for K and for V
-constexpr int kSoftmaxWarps = 8;
-constexpr int kWProd = 8, kWPV = 9, kWS = 10, kWCheck = 11;
+constexpr int kSoftmaxWarps = 16;
+constexpr int kParts = 4;              // warps that share a query's keys
+constexpr int kCols = kTN / kParts;    // keys of a tile per thread
+constexpr int kWProd = 16, kWPV = 17, kWS = 18, kWCheck = 19;
 
 // Every barrier completes one phase per use of its ring slot; tile j uses slot j % ring and waits
 // for parity (j / ring) & 1. Each wait for use u of a slot is preceded, in the same thread or
@@ -49,8 +51,8 @@ struct __align__(16) Ctl {
   uint32_t tmem_base;
   int32_t abort;
   int32_t poison;         // a query sees a value that is not finite
-  float red_max[2][2][kBM];  // per tile parity: the two column halves' row maxima
-  float red_sum[4][kBM];     // the two halves' row sums, rounded and unrounded
+  float red_max[2][kParts][kBM];  // per tile parity: the column parts' row maxima
+  float red_sum[kParts][kBM];     // their row sums
   int64_t out_row[kBM];      // packed query -> row * hq + head, or -1 (not stored)
   RowMasks row_mask[kBM];
   int32_t row_seq[kBM];      // -1: no query
@@ -76,7 +78,7 @@ __device__ __forceinline__ void tma_load_3d(void* dst, const void* desc, uint64_
       : "memory");
 }
 
-// Warp 11, one own tile in shared memory: values that are not finite become zeros, and the queries
+// Warp 19, one own tile in shared memory: values that are not finite become zeros, and the queries
 // that see their keys are marked. `row0` is the tile's first row of k and v.
 template <int D>
 __device__ void check_values(const PrefixParams& p, Ctl& ctl, uint8_t* tile, int row0,
@@ -128,10 +130,26 @@ __device__ __forceinline__ float poisoned(const Ctl& ctl, int t, int e, float o)
   return o;
 }
 
-// kLse: the normalisers are written too; their sum adds the unrounded probabilities, beside the
-// sum of the rounded ones that divides the output (a convex combination of values then, and a
-// row whose weight is nearly all on one key gets that key's value exactly).
-template <int D, bool kLse>
+// All softmax threads, and those of the four warps of TMEM lane quarter q.
+__device__ __forceinline__ void all_bar_sync() {
+  asm volatile("bar.sync 2, 512;" ::: "memory");
+}
+__device__ __forceinline__ void quarter_bar_sync(int q) {
+  asm volatile("bar.sync %0, 128;" ::"r"(3 + q) : "memory");
+}
+__device__ __forceinline__ void tmem_st8(uint32_t taddr, const uint32_t (&r)[8]) {
+  asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"r"(taddr),
+               "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7])
+               : "memory");
+}
+// 32 or 16 columns of this warp's lanes.
+__device__ __forceinline__ void tmem_load(uint32_t addr, uint32_t (&r)[32]) { tmem_ld32(addr, r); }
+__device__ __forceinline__ void tmem_load(uint32_t addr, uint32_t (&r)[16]) { tmem_ld16(addr, r); }
+__device__ __forceinline__ void tmem_store(uint32_t addr, const uint32_t (&r)[32]) { tmem_st32(addr, r); }
+__device__ __forceinline__ void tmem_store(uint32_t addr, const uint32_t (&r)[16]) { tmem_st16(addr, r); }
+__device__ __forceinline__ void tmem_store(uint32_t addr, const uint32_t (&r)[8]) { tmem_st8(addr, r); }
+
+template <int D>
 __global__ void __launch_bounds__(kThreads, 1)
     prefix_tc(const __grid_constant__ PrefixParams p, const __grid_constant__ CUtensorMap tpk,
               const __grid_constant__ CUtensorMap tpv, const __grid_constant__ CUtensorMap tk,
@@ -203,10 +221,11 @@ __global__ void __launch_bounds__(kThreads, 1)
     tmem_alloc<kTmemCols>(&ctl.tmem_base);
     tmem_relinquish();
   }
-  // Softmax warp w: queries 32 (w % 4) .. + 31 (TMEM lane quarter), keys 64 (w / 4) .. of a tile
-  const int quarter = warp & 3, half = warp >> 2;
+  // Softmax warp w: queries 32 (w % 4) .. + 31 (TMEM lane quarter), keys 32 (w / 4) .. of a tile
+  const int quarter = warp & 3, part4 = warp >> 2;
   const int t = quarter * 32 + lane;  // this thread's query within the tile
-  uint4 qhalf[D / 16];                // half of its row of q
+  constexpr int kOC = D / kParts;     // its share of the output's columns
+  uint32_t qreg[D / 8];               // a quarter of its row of q
   int seq = -1, r = 0;                // its sequence and sequence-relative row
   int64_t out_row = -1;
   if (warp < kSoftmaxWarps) {
@@ -218,10 +237,16 @@ __global__ void __launch_bounds__(kThreads, 1)
                 (m0 + t) % p.group;
     }
     const uint4* src = reinterpret_cast<const uint4*>(
-        static_cast<const __nv_bfloat16*>(p.a.q) + out_row * D + half * (D / 2));
+        static_cast<const __nv_bfloat16*>(p.a.q) + out_row * D + part4 * kOC);
 #pragma unroll
-    for (int c = 0; c < D / 16; ++c) qhalf[c] = seq >= 0 ? __ldg(src + c) : make_uint4(0, 0, 0, 0);
-    if (half == 0) {
+    for (int c = 0; c < D / 32; ++c) {
+      const uint4 u = seq >= 0 ? __ldg(src + c) : make_uint4(0, 0, 0, 0);
+      qreg[4 * c] = u.x;
+      qreg[4 * c + 1] = u.y;
+      qreg[4 * c + 2] = u.z;
+      qreg[4 * c + 3] = u.w;
+    }
+    if (part4 == 0) {
 #pragma unroll
       for (int e = 0; e < 4; ++e) ctl.inf_pos[t][e] = ctl.inf_neg[t][e] = 0;
     }
@@ -324,233 +349,165 @@ __global__ void __launch_bounds__(kThreads, 1)
   } else {
     // ------------------------------------------------------------ softmax + epilogue
     const uint32_t lane_off = static_cast<uint32_t>(quarter * 32) << 16;
-    {  // this warp's half of the query rows into TMEM (bf16 pairs, the A-operand layout)
-#pragma unroll
-      for (int c = 0; c < D / 128; ++c) {
-        uint32_t w[32];
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          w[4 * e + 0] = qhalf[8 * c + e].x;
-          w[4 * e + 1] = qhalf[8 * c + e].y;
-          w[4 * e + 2] = qhalf[8 * c + e].z;
-          w[4 * e + 3] = qhalf[8 * c + e].w;
-        }
-        tmem_st32(tQ + lane_off + half * (D / 4) + 32 * c, w);
-      }
-      if (D == 64) {  // 16 columns per half
-        uint32_t w[16];
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          w[4 * e + 0] = qhalf[e].x;
-          w[4 * e + 1] = qhalf[e].y;
-          w[4 * e + 2] = qhalf[e].z;
-          w[4 * e + 3] = qhalf[e].w;
-        }
-        tmem_st16(tQ + lane_off + half * 16, w);
-      }
-      tmem_wait_st();
-      tc_fence_before();
-      __syncwarp();
-      if (lane == 0) mbar_arrive(&ctl.q_full);
-    }
+    // this warp's quarter of the query rows into TMEM (bf16 pairs, the A-operand layout)
+    tmem_store(tQ + lane_off + part4 * (D / 8), qreg);
+    tmem_wait_st();
+    tc_fence_before();
+    __syncwarp();
+    if (lane == 0) mbar_arrive(&ctl.q_full);
     // the last part holds the sequences' last rows: it always has own tiles, and it alone decides
     // which rows are stored
-    RowMasks rm{{0, 0}, {0, 0}};
     int store = seq >= 0;
     if (first_own < n_kt) {
-      if (seq >= 0) rm = query_masks(p.a, p.a.seq[seq], r, half == 0 && g == 0, store);
-      if (half == 0) {
-        ctl.row_mask[t] = rm;
+      if (part4 == 0) {
+        ctl.row_mask[t] = warp_query_masks(p.a, seq, r, g == 0, store);
         ctl.row_seq[t] = seq;
+        ctl.out_row[t] = store ? out_row : -1;
         __syncwarp();
         if (lane == 0) mbar_arrive(&ctl.masks);
       }
+      quarter_bar_sync(quarter);
+    } else if (part4 == 0) {
+      ctl.out_row[t] = out_row;
     }
-    const int row_base = seq >= 0 ? p.a.seq[seq].row_base : 0;
     const float sl = p.a.scale_log2;
-    float m_run = -INFINITY, l_run = 0.f, l_all = 0.f;
+    float m_run = -INFINITY, l_run = 0.f;
     bool ok = true;
     for (int j = 0; j < n_kt; ++j) {
       const int b = j % kNS;
-      uint64_t vis = ~0ull;
-      bool masked = false;
-      if (j >= first_own) {
-        masked = true;
-        vis = seq < 0 ? 0ull
-                      : own_vis64(p.a.seq[seq], key0 + (j0 + j - npt) * kTN + 64 * half - row_base, rm);
-      } else if ((j0 + j + 1) * kTN > p.prefix_len) {
-        masked = true;
-        vis = first64(p.prefix_len - (j0 + j) * kTN - 64 * half);
-      }
-      // Both warps of the rows wait for the same S_j with the same bound (no early leave on an
-      // abort flag), so they leave the loop together: a barrier completing between the two warps'
+      uint32_t vis = ~0u;
+      if (j >= first_own)
+        vis = seq < 0 ? 0u
+                      : static_cast<uint32_t>(own_vis64(
+                            p.a.seq[seq], key0 + (j0 + j - npt) * kTN + kCols * part4 - p.a.seq[seq].row_base,
+                            ctl.row_mask[t]));
+      else if ((j0 + j + 1) * kTN > p.prefix_len)
+        vis = static_cast<uint32_t>(first64(p.prefix_len - (j0 + j) * kTN - kCols * part4));
+      // The four warps of the rows wait for the same S_j with the same bound (no early leave on an
+      // abort flag), so they leave the loop together: a barrier completing between the warps'
       // deadlines (a product about a second late) is the only way they could part.
       ok = mbar_wait(&ctl.s_full[b], (j / kNS) & 1, wlim);
       if (!__all_sync(0xffffffffu, ok)) { ok = false; break; }
       tc_fence_after();
-      float s[64];
-      {
-        uint32_t r0[32], r1[32];
-        tmem_ld32(ctl.tmem_base + b * kTN + 64 * half + lane_off, r0);
-        tmem_ld32(ctl.tmem_base + b * kTN + 64 * half + 32 + lane_off, r1);
-        tmem_wait_ld();
-#pragma unroll
-        for (int e = 0; e < 32; ++e) {
-          s[e] = __uint_as_float(r0[e]);
-          s[32 + e] = __uint_as_float(r1[e]);
-        }
-      }
+      uint32_t s[kCols];
+      tmem_load(ctl.tmem_base + b * kTN + kCols * part4 + lane_off, s);
+      tmem_wait_ld();
       tc_fence_before();
       __syncwarp();
       if (lane == 0) mbar_arrive(&ctl.s_free[b]);
-      if (masked) {
+      if (__any_sync(0xffffffffu, vis != ~0u)) {
 #pragma unroll
-        for (int k = 0; k < 64; ++k) s[k] = ((vis >> k) & 1ull) ? s[k] : -INFINITY;
+        for (int k = 0; k < kCols; ++k) s[k] = (vis >> k) & 1u ? s[k] : 0xff800000u;  // -inf
       }
       float mx[8];
 #pragma unroll
-      for (int e = 0; e < 8; ++e) mx[e] = fmax3(s[e], s[8 + e], s[16 + e]);
+      for (int e = 0; e < 8; ++e)
+        mx[e] = fmax3(__uint_as_float(s[e]), __uint_as_float(s[8 + e]), __uint_as_float(s[16 + e]));
 #pragma unroll
-      for (int e = 0; e < 8; ++e) mx[e] = fmax3(mx[e], s[24 + e], s[32 + e]);
-#pragma unroll
-      for (int e = 0; e < 8; ++e) mx[e] = fmax3(mx[e], s[40 + e], s[48 + e]);
-#pragma unroll
-      for (int e = 0; e < 8; ++e) mx[e] = fmaxf(mx[e], s[56 + e]);
-      const float mh = fmaxf(fmax3(mx[0], mx[1], mx[2]),
-                             fmax3(fmax3(mx[3], mx[4], mx[5]), mx[6], mx[7]));
-      ctl.red_max[j & 1][half][t] = mh;
-      pair_bar_sync(quarter);
-      const float mt = fmaxf(mh, ctl.red_max[j & 1][half ^ 1][t]);
+      for (int e = 0; e < 4; ++e)
+        mx[e] = fmax3(mx[e], __uint_as_float(s[24 + e]), fmaxf(mx[4 + e], __uint_as_float(s[28 + e])));
+      ctl.red_max[j & 1][part4][t] = fmaxf(fmax3(mx[0], mx[1], mx[2]), mx[3]);
+      quarter_bar_sync(quarter);
+      const float* red = &ctl.red_max[j & 1][0][t];
+      const float mt = fmaxf(fmax3(red[0], red[kBM], red[2 * kBM]), red[3 * kBM]);
       // The reference maximum rises on the first finite value, or when the tile's exceeds it by
-      // more than 2^kRescaleLog2 in probability; only then is O rescaled. Both warps of a row
-      // take the same decision from the same values.
+      // more than 2^kRescaleLog2 in probability; only then is O rescaled. The warps of a row take
+      // the same decision from the same values.
       float m_new = m_run;
       if (m_run == -INFINITY) m_new = mt;
       else if ((mt - m_run) * sl > kRescaleLog2) m_new = mt;
       const bool rescale = (m_new != m_run) && (m_run != -INFINITY);
       const float alpha = rescale ? ex2_approx((m_run - m_new) * sl) : 1.f;
       const float mL = (m_new == -INFINITY) ? 0.f : m_new * sl;
-      uint32_t pk[32];
+      uint32_t pk[kCols / 2];
       const uint64_t sl2 = f2_pack(sl, sl), nmL2 = f2_pack(-mL, -mL);
-      float acc[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-      uint64_t acc2[2] = {0, 0};  // bit pattern 0 = +0.0f
+      uint64_t acc[2] = {0, 0};  // bit pattern 0 = +0.0f
 #pragma unroll
-      for (int e = 0; e < 32; ++e) {
+      for (int e = 0; e < kCols / 2; ++e) {
         float x0, x1;
-        f2_unpack(f2_fma(f2_pack(s[2 * e], s[2 * e + 1]), sl2, nmL2), x0, x1);
+        f2_unpack(f2_fma(f2_pack(__uint_as_float(s[2 * e]), __uint_as_float(s[2 * e + 1])), sl2, nmL2), x0, x1);
         x0 = ex2_approx(x0);
         x1 = ex2_approx(x1);
         pk[e] = pack_bf16x2(x0, x1);
-        add_bf16x2_f32(acc[2 * (e & 3)], acc[2 * (e & 3) + 1], pk[e]);
-        if (kLse) acc2[e & 1] = f2_add(acc2[e & 1], f2_pack(x0, x1));
+        acc[e & 1] = f2_add(acc[e & 1], f2_pack(x0, x1));
       }
-      float ls[4];
-#pragma unroll
-      for (int k = 0; k < 4; ++k) ls[k] = acc[k] + acc[4 + k];
       if (j > 0) {  // P_j replaces P_{j-1}, and O may be rescaled, once PV_{j-1} has completed
         ok = mbar_wait(&ctl.pv_done, (j - 1) & 1, wlim);
         if (!__all_sync(0xffffffffu, ok)) { ok = false; break; }
         tc_fence_after();
       }
-      if (__any_sync(0xffffffffu, rescale)) {
+      if (__any_sync(0xffffffffu, rescale)) {  // this warp's share of the O columns
+        uint32_t rr[kOC];
+        tmem_load(tO + lane_off + part4 * kOC, rr);
+        tmem_wait_ld();
 #pragma unroll
-        for (int c = 0; c < D / 64; ++c) {  // this warp's half of the O columns
-          uint32_t rr[32];
-          const uint32_t col = tO + lane_off + half * (D / 2) + 32 * c;
-          tmem_ld32(col, rr);
-          tmem_wait_ld();
-#pragma unroll
-          for (int e = 0; e < 32; ++e) rr[e] = __float_as_uint(__uint_as_float(rr[e]) * alpha);
-          tmem_st32(col, rr);
-        }
+        for (int e = 0; e < kOC; ++e) rr[e] = __float_as_uint(__uint_as_float(rr[e]) * alpha);
+        tmem_store(tO + lane_off + part4 * kOC, rr);
       }
-      l_run = l_run * alpha + ((ls[0] + ls[1]) + (ls[2] + ls[3]));
-      if (kLse) {
-        float a0, a1;
-        f2_unpack(f2_add(acc2[0], acc2[1]), a0, a1);
-        l_all = l_all * alpha + (a0 + a1);
-      }
-      m_run = m_new;
-      tmem_st32(tP + lane_off + 32 * half, pk);
+      tmem_store(tP + lane_off + part4 * (kCols / 2), pk);
       tmem_wait_st();
       tc_fence_before();
       __syncwarp();
       if (lane == 0) mbar_arrive(&ctl.p_full);
+      float a0, a1;
+      f2_unpack(f2_add(acc[0], acc[1]), a0, a1);
+      l_run = l_run * alpha + (a0 + a1);
+      m_run = m_new;
     }
     if (ok) ok = mbar_wait(&ctl.o_full, 0, wlim);
     const bool wok = __all_sync(0xffffffffu, ok);
     if (!wok && lane == 0) flag_timeout(p, ctl);
-    ctl.red_sum[half][t] = l_run;
-    ctl.red_sum[2 + half][t] = l_all;
-    if (half == 0) ctl.out_row[t] = wok && store ? out_row : -1;
-    softmax_bar_sync();
-    const float l = ctl.red_sum[0][t] + ctl.red_sum[1][t];
-    const float l_exact = ctl.red_sum[2][t] + ctl.red_sum[3][t];
-    const bool poison = ctl.poison != 0;
+    ctl.red_sum[part4][t] = l_run;
+    all_bar_sync();
+    const float l = (ctl.red_sum[0][t] + ctl.red_sum[1][t]) + (ctl.red_sum[2][t] + ctl.red_sum[3][t]);
+    uint32_t rr[kOC];
+    if (wok) {  // (whole warps: the loads from TMEM are theirs)
+      tc_fence_after();
+      tmem_load(tO + lane_off + part4 * kOC, rr);
+      tmem_wait_ld();
+      if (ctl.poison)
+#pragma unroll
+        for (int e = 0; e < kOC; ++e)
+          rr[e] = __float_as_uint(poisoned(ctl, t, part4 * kOC + e, __uint_as_float(rr[e])));
+    }
     if (p.nsplit > 1) {
-      // this part of the keys: unnormalised output, reference maximum and sums
+      // this part of the keys: unnormalised output, reference maximum and sum
       float* slot = p.part + blockIdx.x * part_slot_floats(kBM, D);
-      if (wok) {  // (whole warps: the loads from TMEM are theirs; padding queries store nothing)
-        tc_fence_after();
-        float* o = slot + t * D + half * (D / 2);
+      if (wok && seq >= 0) {
+        uint4* o = reinterpret_cast<uint4*>(slot + t * D + part4 * kOC);
 #pragma unroll
-        for (int c = 0; c < D / 64; ++c) {
-          uint32_t rr[32];
-          tmem_ld32(tO + lane_off + half * (D / 2) + 32 * c, rr);
-          tmem_wait_ld();
-          if (poison)
-            for (int e = 0; e < 32; ++e)
-              rr[e] = __float_as_uint(poisoned(ctl, t, half * (D / 2) + 32 * c + e, __uint_as_float(rr[e])));
-          if (seq >= 0) {
-#pragma unroll
-            for (int v = 0; v < 8; ++v)
-              *reinterpret_cast<uint4*>(o + 32 * c + 4 * v) =
-                  make_uint4(rr[4 * v], rr[4 * v + 1], rr[4 * v + 2], rr[4 * v + 3]);
-          }
-          __syncwarp();
-        }
+        for (int v = 0; v < kOC / 4; ++v) o[v] = make_uint4(rr[4 * v], rr[4 * v + 1], rr[4 * v + 2], rr[4 * v + 3]);
       }
-      if (half == 0) {
+      if (part4 == 0) {
         float* stat = slot + kBM * D;
         stat[t] = m_run == -INFINITY ? -INFINITY : m_run * sl;
-        stat[kBM + t] = l;
-        stat[2 * kBM + t] = wok && store ? l_exact : -1.f;
+        stat[kBM + t] = wok && ctl.out_row[t] >= 0 ? l : -1.f;
       }
     } else {
       // O row / row sum -> bf16 into shared memory (the K stages are no longer read once o_full
-      // has completed), 16-byte chunks XOR-swizzled by row; then the 256 softmax threads store
-      // whole rows, coalesced. Every softmax warp reaches the named barriers on every path.
+      // has completed), 16-byte chunks XOR-swizzled by row; then the softmax threads store whole
+      // rows, coalesced. Every softmax warp reaches the named barriers on every path.
       constexpr int kChunks = D / 8;  // 16-byte chunks per output row
       uint4* stage = reinterpret_cast<uint4*>(sK);  // 128 rows x D bf16 <= one K stage
       if (wok) {
-        tc_fence_after();
         const float inv_l = 1.0f / l;
 #pragma unroll
-        for (int c = 0; c < D / 64; ++c) {
-          uint32_t rr[32];
-          tmem_ld32(tO + lane_off + half * (D / 2) + 32 * c, rr);
-          tmem_wait_ld();
-          if (poison)
-            for (int e = 0; e < 32; ++e)
-              rr[e] = __float_as_uint(poisoned(ctl, t, half * (D / 2) + 32 * c + e, __uint_as_float(rr[e])));
-#pragma unroll
-          for (int v = 0; v < 4; ++v) {
-            uint4 u;
-            u.x = pack_bf16x2(__uint_as_float(rr[8 * v + 0]) * inv_l, __uint_as_float(rr[8 * v + 1]) * inv_l);
-            u.y = pack_bf16x2(__uint_as_float(rr[8 * v + 2]) * inv_l, __uint_as_float(rr[8 * v + 3]) * inv_l);
-            u.z = pack_bf16x2(__uint_as_float(rr[8 * v + 4]) * inv_l, __uint_as_float(rr[8 * v + 5]) * inv_l);
-            u.w = pack_bf16x2(__uint_as_float(rr[8 * v + 6]) * inv_l, __uint_as_float(rr[8 * v + 7]) * inv_l);
-            const int chunk = half * (kChunks / 2) + c * 4 + v;
-            stage[t * kChunks + (chunk ^ (t & (kChunks - 1)))] = u;
-          }
+        for (int v = 0; v < kOC / 8; ++v) {
+          uint4 u;
+          u.x = pack_bf16x2(__uint_as_float(rr[8 * v + 0]) * inv_l, __uint_as_float(rr[8 * v + 1]) * inv_l);
+          u.y = pack_bf16x2(__uint_as_float(rr[8 * v + 2]) * inv_l, __uint_as_float(rr[8 * v + 3]) * inv_l);
+          u.z = pack_bf16x2(__uint_as_float(rr[8 * v + 4]) * inv_l, __uint_as_float(rr[8 * v + 5]) * inv_l);
+          u.w = pack_bf16x2(__uint_as_float(rr[8 * v + 6]) * inv_l, __uint_as_float(rr[8 * v + 7]) * inv_l);
+          const int chunk = part4 * (kChunks / kParts) + v;
+          stage[t * kChunks + (chunk ^ (t & (kChunks - 1)))] = u;
         }
-        if (kLse && half == 0 && store)
-          p.lse[out_row] = 0.69314718055994531f * (m_run * sl + log2f(l_exact));
+        if (p.lse && part4 == 0 && ctl.out_row[t] >= 0)
+          p.lse[ctl.out_row[t]] = 0.69314718055994531f * (m_run * sl + log2f(l));
       }
-      softmax_bar_sync();
+      all_bar_sync();
       if (!*abort_flag) {
         __nv_bfloat16* out = static_cast<__nv_bfloat16*>(p.a.o);
-        const int tid = threadIdx.x;  // 0 .. 255
+        const int tid = threadIdx.x;  // 0 .. 511
 #pragma unroll 4
         for (int idx = tid; idx < kBM * kChunks; idx += 32 * kSoftmaxWarps) {
           const int row = idx / kChunks, chunk = idx % kChunks;
@@ -571,50 +528,91 @@ __global__ void __launch_bounds__(kThreads, 1)
   }
 }
 
-// Joins the parts of a split launch, one warp per packed query: with M the largest reference
-// maximum, o = sum_c 2^(m_c - M) O_c / sum_c 2^(m_c - M) l_c. Reads each part once, coalesced.
-template <typename T, int D>
-__global__ void __launch_bounds__(128) prefix_join(const __grid_constant__ PrefixParams p,
+// Joins the parts of a split launch: with M the largest reference maximum of a packed query,
+// o = sum_c 2^(m_c - M) O_c / sum_c 2^(m_c - M) l_c. kWarps warps share a query's parts, 32 at a time:
+// a lane takes a part's factor and sum, then all take the parts' rows, coalesced.
+template <typename T, int D, int kWarps>
+__global__ void __launch_bounds__(128, 6) prefix_join(const __grid_constant__ PrefixParams p,
                                                    int tile_rows) {
-  const int lane = threadIdx.x & 31;
-  const long long w = static_cast<long long>(blockIdx.x) * 4 + (threadIdx.x >> 5);
-  grid_dep_wait();
-  if (w >= static_cast<long long>(p.queries) * p.a.hkv) return;
-  const int g = static_cast<int>(w / p.queries), m = static_cast<int>(w % p.queries);
+  constexpr int kV = D / 32;  // elements per lane
+  __shared__ float s_o[4][D], s_top[4], s_l[4];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, sub = warp % kWarps;
+  const long long w = (static_cast<long long>(blockIdx.x) * 4 + warp) / kWarps;
+  const bool in = w < static_cast<long long>(p.queries) * p.a.hkv;
+  const int g = in ? static_cast<int>(w / p.queries) : 0, m = in ? static_cast<int>(w % p.queries) : 0;
   const int t = m % tile_rows;
   const size_t floats = part_slot_floats(tile_rows, D);
   const float* slot = p.part + (static_cast<size_t>(g) * p.tiles + m / tile_rows) * p.nsplit * floats;
   const float* stat = slot + tile_rows * D + t;
-  float top = -INFINITY;
-  bool nan = false;
-  for (int c = lane; c < p.nsplit; c += 32) {
-    const float mc = stat[c * floats];
-    nan |= mc != mc;
-    top = fmaxf(top, mc);
-  }
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
-  if (__any_sync(0xffffffffu, nan)) top = NAN;
-  if (stat[(p.nsplit - 1) * floats + 2 * tile_rows] == -1.f) return;  // not stored
-  constexpr int kV = D / 32;  // elements per lane
-  float o[kV];
-#pragma unroll
-  for (int e = 0; e < kV; ++e) o[e] = 0.f;
-  float l = 0.f, l_all = 0.f;
-#pragma unroll 4
-  for (int c = 0; c < p.nsplit; ++c) {
-    const float mc = stat[c * floats];
-    if (mc == -INFINITY && top != -INFINITY) continue;  // a part without a key for this row
-    const float f = mc == top ? 1.f : ex2_approx(mc - top);
-    l = fmaf(f, stat[c * floats + tile_rows], l);
-    l_all = fmaf(f, stat[c * floats + 2 * tile_rows], l_all);
-    const float* src = slot + c * floats + t * D + lane * kV;
-#pragma unroll
-    for (int e = 0; e < kV; ++e) o[e] = fmaf(f, src[e], o[e]);
-  }
   const int tq = m / p.group, seq = seq_of_query(p, tq);
   const size_t row = static_cast<size_t>(p.a.seq[seq].row_base + p.a.seq[seq].q_start + tq -
                                          p.q_before[seq]) * p.a.hq + g * p.group + m % p.group;
+  grid_dep_wait();
+  const bool stored = stat[(p.nsplit - 1) * floats + tile_rows] != -1.f;  // (its last part decides)
+  float top = -INFINITY, l = 0.f, o[kV];
+#pragma unroll
+  for (int e = 0; e < kV; ++e) o[e] = 0.f;
+  const int c0 = p.nsplit * sub / kWarps, c1 = p.nsplit * (sub + 1) / kWarps;
+  for (int c = c0; c < c1; c += 32) {
+    const int n = min(32, c1 - c);
+    const float mc = lane < n ? stat[(c + lane) * floats] : -INFINITY;
+    const float lc = lane < n ? stat[(c + lane) * floats + tile_rows] : 0.f;
+    float most = fmaxf(top, mc);
+#pragma unroll
+    for (int x = 16; x > 0; x >>= 1) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, x));
+    // (a part without a key has no weight; a maximum that is NaN makes its part NaN)
+    const float f = mc == -INFINITY ? 0.f : mc == most ? 1.f : ex2_approx(mc - most);
+    const float back = top == -INFINITY ? 0.f : top == most ? 1.f : ex2_approx(top - most);
+    float lf = mc == -INFINITY ? 0.f : f * lc;
+#pragma unroll
+    for (int x = 16; x > 0; x >>= 1) lf += __shfl_xor_sync(0xffffffffu, lf, x);
+    l = l * back + lf;
+#pragma unroll
+    for (int e = 0; e < kV; ++e) o[e] *= back;
+    top = most;
+#pragma unroll 8
+    for (int u = 0; u < n; ++u) {
+      const float fu = __shfl_sync(0xffffffffu, f, u);
+      const float* src = slot + (c + u) * floats + t * D + lane * kV;
+      if constexpr (kV == 4) {
+        const float4 x = *reinterpret_cast<const float4*>(src);
+        o[0] = fmaf(fu, x.x, o[0]);
+        o[1] = fmaf(fu, x.y, o[1]);
+        o[2] = fmaf(fu, x.z, o[2]);
+        o[3] = fmaf(fu, x.w, o[3]);
+      } else {
+        const float2 x = *reinterpret_cast<const float2*>(src);
+        o[0] = fmaf(fu, x.x, o[0]);
+        o[1] = fmaf(fu, x.y, o[1]);
+      }
+    }
+  }
+  if (kWarps > 1) {
+#pragma unroll
+    for (int e = 0; e < kV; ++e) s_o[warp][lane * kV + e] = o[e];
+    if (lane == 0) {
+      s_top[warp] = top;
+      s_l[warp] = l;
+    }
+    __syncthreads();
+    if (sub != 0) return;
+    float most = s_top[0];
+#pragma unroll
+    for (int k = 1; k < kWarps; ++k) most = fmaxf(most, s_top[k]);
+    l = 0.f;
+#pragma unroll
+    for (int e = 0; e < kV; ++e) o[e] = 0.f;
+#pragma unroll
+    for (int k = 0; k < kWarps; ++k) {
+      const float f = s_top[k] == -INFINITY ? 0.f : s_top[k] == most ? 1.f : ex2_approx(s_top[k] - most);
+      if (s_top[k] == -INFINITY && s_l[k] == s_l[k]) continue;
+      l = fmaf(f, s_l[k], l);
+#pragma unroll
+      for (int e = 0; e < kV; ++e) o[e] = fmaf(f, s_o[k][lane * kV + e], o[e]);
+    }
+    top = most;
+  }
+  if (!in || !stored) return;
   T* out = static_cast<T*>(p.a.o) + row * D + lane * kV;
   const float inv = 1.0f / l;
 #pragma unroll
@@ -624,7 +622,7 @@ __global__ void __launch_bounds__(128) prefix_join(const __grid_constant__ Prefi
     else
       *reinterpret_cast<float2*>(out + e) = make_float2(o[e] * inv, o[e + 1] * inv);
   }
-  if (p.lse && lane == 0) p.lse[row] = 0.69314718055994531f * (top + log2f(l_all));
+  if (p.lse && lane == 0) p.lse[row] = 0.69314718055994531f * (top + log2f(l));
 }
 
 // ---------------------------------------------------------------- host side
@@ -665,7 +663,7 @@ bool make_map3(CUtensorMap* m, const void* ptr, int d, long long rows, int heads
             CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-template <int D, bool kLse>
+template <int D>
 cudaError_t launch_tc(const PrefixParams& p, cudaStream_t stream) {
   static std::atomic<uint64_t> done{0};
   CUtensorMap pk, pv, k, v;
@@ -681,19 +679,26 @@ cudaError_t launch_tc(const PrefixParams& p, cudaStream_t stream) {
     pk = k;
     pv = v;
   }
-  cudaError_t e = ensure_smem_attr(prefix_tc<D, kLse>, smem_bytes<D>(), done);
+  cudaError_t e = ensure_smem_attr(prefix_tc<D>, smem_bytes<D>(), done);
   if (e != cudaSuccess) return e;
   const AttnLaunch L(static_cast<unsigned>(a.hkv * p.tiles * p.nsplit), kThreads, smem_bytes<D>(),
                      stream, 1, false);
-  return cudaLaunchKernelEx(&L.cfg, prefix_tc<D, kLse>, p, pk, pv, k, v);
+  return cudaLaunchKernelEx(&L.cfg, prefix_tc<D>, p, pk, pv, k, v);
 }
 
+template <typename T, int D>
+cudaError_t launch_join_d(const PrefixParams& p, int rows, cudaStream_t stream) {
+  const long long queries = static_cast<long long>(p.queries) * p.a.hkv;
+  if (p.nsplit > 8) {  // four warps to a query: its parts' rows are in flight together
+    const AttnLaunch L(static_cast<unsigned>(queries), 128, 0, stream, 1, true);
+    return cudaLaunchKernelEx(&L.cfg, prefix_join<T, D, 4>, p, rows);
+  }
+  const AttnLaunch L(static_cast<unsigned>((queries + 3) / 4), 128, 0, stream, 1, true);
+  return cudaLaunchKernelEx(&L.cfg, prefix_join<T, D, 1>, p, rows);
+}
 template <typename T>
 cudaError_t launch_join(const PrefixParams& p, int rows, cudaStream_t stream) {
-  const long long warps = static_cast<long long>(p.queries) * p.a.hkv;
-  const AttnLaunch L(static_cast<unsigned>((warps + 3) / 4), 128, 0, stream, 1, true);
-  return p.a.head_dim == 64 ? cudaLaunchKernelEx(&L.cfg, prefix_join<T, 64>, p, rows)
-                            : cudaLaunchKernelEx(&L.cfg, prefix_join<T, 128>, p, rows);
+  return p.a.head_dim == 64 ? launch_join_d<T, 64>(p, rows, stream) : launch_join_d<T, 128>(p, rows, stream);
 }
 
 dard_status prepare(const dard_prefix_attn_args* args, PrefixParams& p) {
@@ -801,9 +806,9 @@ dard_status dard_prefix_attention(const dard_prefix_attn_args* args, void* strea
   if (!bf16)
     e = launch_prefix_f32(p, rows, stream);
   else if (p.a.head_dim == 64)
-    e = p.lse ? launch_tc<64, true>(p, stream) : launch_tc<64, false>(p, stream);
+    e = launch_tc<64>(p, stream);
   else
-    e = p.lse ? launch_tc<128, true>(p, stream) : launch_tc<128, false>(p, stream);
+    e = launch_tc<128>(p, stream);
   if (e == cudaSuccess && p.nsplit > 1)
     e = bf16 ? launch_join<__nv_bfloat16>(p, rows, stream) : launch_join<float>(p, rows, stream);
   if (e != cudaSuccess)

@@ -6,9 +6,11 @@
 // to unsigned keys in the same order; three rounds of 11, 11 and 10 bits (a radix selection: count
 // each digit's values among the candidates that share the digits so far, take the digit in which
 // the count from the top passes the number wanted) find the smallest kept key and how many of its
-// equals are kept. The counts of a cluster meet in the shared memory of its first CTA. Then each
-// warp counts its kept candidates, a scan over warps and CTAs places them, and ballots place each
-// within its warp. Nothing depends on the order of the atomics: they only count.
+// equals are kept. The CTAs of a cluster add their counts up in the shared memory of the first, which
+// finds the digit with one scan over its threads. Then each warp counts its kept candidates, a scan
+// over warps and CTAs places them, and ballots place each within its warp. Nothing depends on the
+// order of the atomics: they only count. Bound by the barriers of the rounds (two of the cluster
+// each), not by the weights' bytes.
 // evict_copy: 16 bytes of K and of V per thread and step, rows in the order of the outputs.
 #include <algorithm>
 #include <cstdio>
@@ -46,13 +48,20 @@ __device__ __forceinline__ uint32_t key_of(float w) {
 }
 
 struct SelShared {
-  uint32_t hist[kBins];
+  uint32_t hist[2][kBins];        // one for every other round
+  uint32_t warp_sum[kSelWarps];
   uint32_t warp_gt[kSelWarps], warp_eq[kSelWarps];
   uint32_t cta_gt, cta_eq;        // this CTA's counts
   uint32_t base_gt, base_eq;      // those of the cluster's earlier CTAs
   uint32_t digit, above;          // the round's result
 };
 
+__device__ __forceinline__ void add_cluster(uint32_t* p, uint32_t rank, uint32_t v) {
+  asm volatile("red.relaxed.cluster.shared::cluster.add.u32 [%0], %1;" ::"r"(map_shared_rank(smem_u32(p), rank)), "r"(v) : "memory");
+}
+__device__ __forceinline__ void st_cluster(uint32_t* p, uint32_t rank, uint32_t v) {
+  asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(map_shared_rank(smem_u32(p), rank)), "r"(v) : "memory");
+}
 __device__ __forceinline__ uint32_t ld_cluster(const uint32_t* p, uint32_t rank) {
   uint32_t v;
   asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(v) : "r"(map_shared_rank(smem_u32(p), rank)) : "memory");
@@ -90,53 +99,55 @@ __global__ void __launch_bounds__(kSelThreads, 1) evict_select(const __grid_cons
   const int a = lo + static_cast<int>(n * unit / units), b = lo + static_cast<int>(n * (unit + 1) / units);
 
   uint32_t prefix = 0, need = want;  // digits found so far; how many of their candidates are kept
-  const int shifts[3] = {21, 10, 0}, bits[3] = {11, 11, 10};
+  for (int i = tid; i < 2 * kBins; i += kSelThreads) sh.hist[0][i] = 0;
+  sync_head(ctas);
 #pragma unroll 1
   for (int round = 0; round < 3; ++round) {
-    const int shift = shifts[round], bins = 1 << bits[round];
-    for (int i = tid; i < bins; i += kSelThreads) sh.hist[i] = 0;
-    __syncthreads();
-    const uint32_t done = round == 0 ? 0u : ~0u << (shift + bits[round]);
+    const int shift = round == 0 ? 21 : round == 1 ? 10 : 0, bins = round == 2 ? 1024 : 2048;
+    const uint32_t done = round == 0 ? 0u : round == 1 ? 0xffe00000u : 0xfffffc00u;
+    uint32_t* hist = sh.hist[round & 1];
+#pragma unroll 4
     for (int i = a + lane; i < b; i += 32) {
       const uint32_t key = key_of(__ldg(w + i));
-      if ((key & done) == prefix) atomicAdd(&sh.hist[key >> shift & (bins - 1)], 1u);
+      if ((key & done) == prefix) atomicAdd(&hist[key >> shift & (bins - 1)], 1u);
+    }
+    if (ctas > 1) {
+      __syncthreads();
+      if (rank != 0)
+        for (int i = tid; i < bins; i += kSelThreads) {
+          const uint32_t c = hist[i];
+          if (c) add_cluster(&hist[i], 0, c);
+        }
     }
     sync_head(ctas);
-    if (ctas > 1 && rank == 0)
-      for (int i = tid; i < bins; i += kSelThreads) {
-        uint32_t sum = sh.hist[i];
-        for (int c = 1; c < ctas; ++c) sum += ld_cluster(&sh.hist[i], c);
-        sh.hist[i] = sum;
-      }
-    __syncthreads();
-    if (rank == 0 && warp == 0) {
-      // from the largest digit down: the first at which the count reaches `need`
-      uint32_t above = 0;
-      for (int top = bins - 32; top >= 0; top -= 32) {
-        const uint32_t c = sh.hist[top + 31 - lane];  // lane 0: the largest digit
-        uint32_t scan = c;
+    if (rank == 0) {
+      // thread t takes the two digits bins - 1 - 2t and bins - 2 - 2t: the first digit, from the
+      // largest down, at which the count reaches `need`
+      const int top = bins - 1 - 2 * tid;
+      const uint32_t c0 = top > 0 ? hist[top] : 0u, c1 = top > 0 ? hist[top - 1] : 0u;
+      uint32_t scan = c0 + c1;
 #pragma unroll
-        for (int o = 1; o < 32; o <<= 1) {
-          const uint32_t x = __shfl_up_sync(0xffffffffu, scan, o);
-          if (lane >= o) scan += x;
+      for (int o = 1; o < 32; o <<= 1) {
+        const uint32_t x = __shfl_up_sync(0xffffffffu, scan, o);
+        if (lane >= o) scan += x;
+      }
+      if (lane == 31) sh.warp_sum[warp] = scan;
+      __syncthreads();
+      uint32_t before = lane < warp ? sh.warp_sum[lane] : 0u;
+      before = __reduce_add_sync(0xffffffffu, before) + scan - c0 - c1;
+      if (before < need && before + c0 + c1 >= need) {  // one thread
+        const bool second = before + c0 < need;
+        for (int c = 0; c < ctas; ++c) {
+          st_cluster(&sh.digit, c, static_cast<uint32_t>(second ? top - 1 : top));
+          st_cluster(&sh.above, c, second ? before + c0 : before);
         }
-        const uint32_t hit = __ballot_sync(0xffffffffu, above + scan >= need);
-        if (hit) {
-          const int at = __ffs(hit) - 1;
-          if (lane == at) {
-            sh.digit = top + 31 - lane;
-            sh.above = above + scan - c;
-          }
-          break;
-        }
-        above += __shfl_sync(0xffffffffu, scan, 31);
       }
     }
+    // (the counts have been read or added up) room for the next round but one
+    for (int i = tid; i < bins; i += kSelThreads) hist[i] = 0;
     sync_head(ctas);
-    const uint32_t digit = ctas > 1 ? ld_cluster(&sh.digit, 0) : sh.digit;
-    need -= ctas > 1 ? ld_cluster(&sh.above, 0) : sh.above;
-    prefix |= digit << shift;
-    sync_head(ctas);  // read before the next round writes
+    need -= sh.above;
+    prefix |= sh.digit << shift;
   }
   // `prefix` is the smallest kept key, of which the first `need` are kept
   uint32_t gt = 0, eq = 0;

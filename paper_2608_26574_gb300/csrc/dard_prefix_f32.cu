@@ -83,14 +83,18 @@ __global__ void __launch_bounds__(kF32Threads) prefix_f32(const __grid_constant_
     }
     sQ[t * kC + swz(t, c)] = v;
   }
-  // thread t < kRows: query t's masks (kept while own tiles are to come)
+  // thread t < kRows: query t's masks (while own tiles are to come)
   RowMasks rm{{0, 0}, {0, 0}};
   int seq = -1, store = 1;
-  if (tid < kRows && m0 + tid < p.queries && j1 > npt) {
-    const int tq = (m0 + tid) / p.group;
-    seq = seq_of_query(p, tq);
-    const SeqDesc& sd = p.a.seq[seq];
-    rm = query_masks(p.a, sd, sd.q_start + tq - p.q_before[seq], g == 0, store);
+  if (tid < (kRows + 31) / 32 * 32 && j1 > npt) {
+    int r = 0;
+    if (tid < kRows && m0 + tid < p.queries) {
+      const int tq = (m0 + tid) / p.group;
+      seq = seq_of_query(p, tq);
+      r = p.a.seq[seq].q_start + tq - p.q_before[seq];
+    }
+    __syncwarp();
+    rm = warp_query_masks(p.a, seq, r, g == 0, store);
   }
 
   float m[TR], l[TR];
@@ -233,8 +237,7 @@ __global__ void __launch_bounds__(kF32Threads) prefix_f32(const __grid_constant_
       if (tx == 0) {
         float* stat = slot + kRows * D + t;
         stat[0] = m[u];
-        stat[kRows] = sum;
-        stat[2 * kRows] = st ? sum : -1.f;
+        stat[kRows] = st ? sum : -1.f;
       }
     } else if (st) {
       const int tq = (m0 + t) / p.group, s = seq_of_query(p, tq);

@@ -6,12 +6,12 @@
 // weights_tc: 128 keys of one key/value head stay in shared memory as the A operand; tiles of
 // up to 128 (row, head) queries pass by as B, so that an accumulator row is a key and a thread
 // adds up its key's exponentials along the row: no reduction across threads until the end, no
-// atomics, one order of addition. 11 warps:
-//   warps 0-7  exponentials and sums: warps w and w + 4 share TMEM lane quarter w (keys 32w ..
-//              32w + 31), each taking 64 of a tile's 128 queries;
-//   warp 8     TMA producer: the K tile, then Q through 4 stages;
-//   warp 9     TMEM allocator and issuer: S_j = K Q_j^T into a ring of four 128-column buffers;
-//   warp 10    the queries' normalisers through 4 stages.
+// atomics, one order of addition. 19 warps:
+//   warps 0-15 exponentials and sums: warps q, q + 4, q + 8 and q + 12 share TMEM lane quarter q
+//              (keys 32q .. 32q + 31), each taking 32 of a tile's 128 queries;
+//   warp 16    TMA producer: the K tile, then Q through 4 stages;
+//   warp 17    TMEM allocator and issuer: S_j = K Q_j^T into a ring of four 128-column buffers;
+//   warp 18    the queries' normalisers through 4 stages.
 // Each tile's sum is formed on its own and then added to the key's total (two levels: the
 // rounding of a long sum grows with the number of tiles, not of queries).
 #include <algorithm>
@@ -49,10 +49,10 @@ __device__ __forceinline__ float with_earlier(const WeightsParams& p, int g, int
 }
 
 // ---------------------------------------------------------------- bf16, tensor cores
-constexpr int kThreads = 352;
+constexpr int kThreads = 608;
 constexpr int kQStages = 4, kSBufs = 4;
-constexpr int kWorkers = 8;
-constexpr int kWProd = 8, kWMma = 9, kWLse = 10;
+constexpr int kWorkers = 16;
+constexpr int kWProd = 16, kWMma = 17, kWLse = 18;
 
 struct __align__(16) Ctl {
   uint64_t k_full;
@@ -62,9 +62,9 @@ struct __align__(16) Ctl {
   uint64_t drained;
   uint32_t tmem_base;
   int32_t abort;
-  __align__(16) float lse[kQStages][kBM];  // times log2 e (read four at a time)
+  __align__(16) float lse[kQStages][kBM];  // times -log2 e (read four at a time)
   uint32_t off[kQStages][4];      // queries that add nothing (bit per column)
-  float red[kBM];
+  float red[4][kBM];
 };
 
 template <int D>
@@ -86,19 +86,18 @@ __device__ __forceinline__ void tma_load_3d(void* dst, const void* desc, uint64_
       : "memory");
 }
 
-// Sum over 32 columns of 2^(s sl - lse) for one key.
+// Sum over 32 columns of 2^(s sl - lse) for one key. kOff: columns with a bit of `off` count for
+// nothing, whatever their scores are.
 template <bool kOff>
 __device__ __forceinline__ float sum32(const uint32_t (&s)[32], const float* lse, uint32_t off,
                                        uint64_t sl2) {
   uint64_t acc[4] = {0, 0, 0, 0};
 #pragma unroll
   for (int e = 0; e < 8; ++e) {
-    const float4 n = *reinterpret_cast<const float4*>(lse + 4 * e);
+    const ulonglong2 n = *reinterpret_cast<const ulonglong2*>(lse + 4 * e);
     float x[4];
-    f2_unpack(f2_fma(f2_pack(__uint_as_float(s[4 * e]), __uint_as_float(s[4 * e + 1])), sl2,
-                     f2_pack(-n.x, -n.y)), x[0], x[1]);
-    f2_unpack(f2_fma(f2_pack(__uint_as_float(s[4 * e + 2]), __uint_as_float(s[4 * e + 3])), sl2,
-                     f2_pack(-n.z, -n.w)), x[2], x[3]);
+    f2_unpack(f2_fma(f2_pack(__uint_as_float(s[4 * e]), __uint_as_float(s[4 * e + 1])), sl2, n.x), x[0], x[1]);
+    f2_unpack(f2_fma(f2_pack(__uint_as_float(s[4 * e + 2]), __uint_as_float(s[4 * e + 3])), sl2, n.y), x[2], x[3]);
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
       x[k] = ex2_approx(x[k]);
@@ -154,6 +153,11 @@ __global__ void __launch_bounds__(kThreads, 1)
     tmem_alloc<kTmemCols>(&ctl.tmem_base);
     tmem_relinquish();
   }
+  // rows of the stages that no copy writes: zeros, whose scores (0) count for nothing with lse = +inf
+  for (int i = columns * 8 + threadIdx.x; i < kTN * 8; i += kThreads)
+    for (int b = 0; b < kQStages * kSub; ++b)
+      *reinterpret_cast<uint4*>(sQ + b * kKSub + 16 * i) = make_uint4(0, 0, 0, 0);
+  fence_proxy_async_smem();
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
@@ -218,22 +222,24 @@ __global__ void __launch_bounds__(kThreads, 1)
     for (int j = 0; j < n && ok && !*abort_flag; ++j) {
       const int b = j % kQStages, tile = j0 + j;
       float v[4];
+      bool off[4];  // a query with lse = +inf (columns without a query have scores of 0)
 #pragma unroll
       for (int e = 0; e < 4; ++e) {  // column 32 e + lane
         const int c = 32 * e + lane;
         const int h = tile % p.head_blocks * p.box_heads + c % p.box_heads;
         const int64_t row = static_cast<int64_t>(tile / p.head_blocks) * p.box_rows + c / p.box_heads;
-        v[e] = c < columns && h < p.group && row < p.rows
-                   ? __ldg(p.lse + row * p.hq + g * p.group + h) : INFINITY;
+        const bool in = c < columns && h < p.group && row < p.rows;
+        v[e] = in ? __ldg(p.lse + row * p.hq + g * p.group + h) : INFINITY;
+        off[e] = v[e] == INFINITY && c < columns && row < p.rows;
       }
       if (j >= kQStages) ok = mbar_wait(&ctl.l_empty[b], ((j - kQStages) / kQStages) & 1, wlim);
       ok = __all_sync(0xffffffffu, ok);
       if (!ok) break;
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        const uint32_t off = __ballot_sync(0xffffffffu, v[e] == INFINITY);
-        ctl.lse[b][32 * e + lane] = v[e] * kLog2e;
-        if (lane == 0) ctl.off[b][e] = off;
+        const uint32_t bits = __ballot_sync(0xffffffffu, off[e]);
+        ctl.lse[b][32 * e + lane] = v[e] * -kLog2e;
+        if (lane == 0) ctl.off[b][e] = bits;
       }
       __syncwarp();
       if (lane == 0) mbar_arrive(&ctl.l_full[b]);
@@ -241,7 +247,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     if (!ok && lane == 0) flag_timeout(p, ctl);
   } else {
     // ------------------------------------------------------------ exponentials and sums
-    const int quarter = warp & 3, half = warp >> 2;
+    const int quarter = warp & 3, col = warp >> 2;  // keys 32 quarter .., queries 32 col ..
     const uint32_t lane_off = static_cast<uint32_t>(quarter * 32) << 16;
     const uint64_t sl2 = f2_pack(p.scale_log2, p.scale_log2);
     float total = 0.f;
@@ -252,34 +258,27 @@ __global__ void __launch_bounds__(kThreads, 1)
            mbar_wait(&ctl.s_full[sb], (j / kSBufs) & 1, wlim);
       if (!__all_sync(0xffffffffu, ok)) { ok = false; break; }
       tc_fence_after();
-      uint32_t r0[32], r1[32];
-      tmem_ld32(ctl.tmem_base + sb * kTN + 64 * half + lane_off, r0);
-      tmem_ld32(ctl.tmem_base + sb * kTN + 64 * half + 32 + lane_off, r1);
+      uint32_t r[32];
+      tmem_ld32(ctl.tmem_base + sb * kTN + 32 * col + lane_off, r);
       tmem_wait_ld();
       tc_fence_before();
       __syncwarp();
       if (lane == 0) mbar_arrive(&ctl.s_free[sb]);
-      const float* lse = ctl.lse[b] + 64 * half;
-      const uint32_t off0 = ctl.off[b][2 * half], off1 = ctl.off[b][2 * half + 1];
-      float sum = 0.f;
-      if ((off0 | off1) == 0) {
-        sum = sum32<false>(r0, lse, 0, sl2) + sum32<false>(r1, lse + 32, 0, sl2);
-      } else {
-        if (off0 != 0xffffffffu) sum = sum32<true>(r0, lse, off0, sl2);
-        if (off1 != 0xffffffffu) sum += sum32<true>(r1, lse + 32, off1, sl2);
-      }
+      const float* lse = ctl.lse[b] + 32 * col;
+      const uint32_t off = ctl.off[b][col];
+      if (32 * col < columns)  // (else no query)
+        total += off == 0 ? sum32<false>(r, lse, 0, sl2) : sum32<true>(r, lse, off, sl2);
       __syncwarp();
       if (lane == 0) mbar_arrive(&ctl.l_empty[b]);
-      total += sum;
     }
     const bool wok = __all_sync(0xffffffffu, ok);
     if (!wok && lane == 0) flag_timeout(p, ctl);
     const int t = quarter * 32 + lane;
-    if (half == 1) ctl.red[t] = total;
-    softmax_bar_sync();
+    ctl.red[col][t] = total;
+    asm volatile("bar.sync 2, 512;" ::: "memory");  // the sixteen warps
     const int key = key0 + t;
-    if (half == 0 && wok && key < p.prefix_len) {
-      total += ctl.red[t];
+    if (col == 0 && wok && key < p.prefix_len) {
+      total = (ctl.red[0][t] + ctl.red[1][t]) + (ctl.red[2][t] + ctl.red[3][t]);
       if (p.nsplit > 1)
         p.part[(static_cast<size_t>(part) * p.hkv + g) * p.prefix_len + key] = total;
       else
@@ -416,7 +415,7 @@ __global__ void __launch_bounds__(256) weights_join(const __grid_constant__ Weig
 
 // ---------------------------------------------------------------- host side
 constexpr int kParts = 64;               // parts of a split launch at most
-constexpr long long kSplitCtas = 1024;   // CTAs of a split launch at most
+constexpr long long kSplitCtas = 2048;   // CTAs of a split launch at most
 
 bool make_map3(CUtensorMap* m, const void* ptr, int d, long long n1, long long n2, int64_t stride1,
                int64_t stride2, int box1, int box2) {
@@ -522,17 +521,17 @@ dard_status prepare(const dard_prefix_weights_args* a, WeightsParams& p) {
   return DARD_OK;
 }
 
-// Parts of the split: as few as give every SM a CTA or two, each with query tiles enough to pay for
-// its start (bounded by what the workspace holds).
-int choose_parts(long long items, int q_tiles, int sms) {
-  if (items >= 4ll * sms) return 1;
+// Parts of the split, by the time of a launch in query tiles: a CTA costs `start` beside its tiles, the
+// join `join`; a launch with no more CTAs than SMs takes its longest, a larger one total / SMs plus half
+// a CTA. Bounded by what the workspace holds.
+int choose_parts(long long items, int q_tiles, int sms, double start, double join) {
   long long best = 1;
   double best_time = 0;
   for (long long s = 1; s <= std::min<long long>(kParts, q_tiles) && (s == 1 || items * s <= kSplitCtas); ++s) {
-    const double cta = 6.0 + std::ceil(static_cast<double>(q_tiles) / s);
+    const double cta = start + std::ceil(static_cast<double>(q_tiles) / s);
     const double n = static_cast<double>(items) * s;
-    const double time = (n <= sms ? cta : n * (6.0 + static_cast<double>(q_tiles) / s) / sms + 0.5 * cta) +
-                        (s > 1 ? 4.0 : 0.0);
+    const double time = (n <= sms ? cta : n * (start + static_cast<double>(q_tiles) / s) / sms + 0.5 * cta) +
+                        (s > 1 ? join : 0.0);
     if (s == 1 || time < best_time) {
       best = s;
       best_time = time;
@@ -583,7 +582,8 @@ dard_status dard_prefix_weights(const dard_prefix_weights_args* args, void* stre
     }
     const long long items = static_cast<long long>(p.key_tiles) * p.hkv;
     if (items > (1ll << 31) - 1) return report(DARD_ERR_SHAPE, "too many key tiles");
-    p.nsplit = p.part ? choose_parts(items, p.q_tiles, sm_count()) : 1;
+    p.nsplit = !p.part ? 1 : bf16 ? choose_parts(items, p.q_tiles, sm_count(), 10.0, 8.0)
+                                  : choose_parts(items, p.q_tiles, sm_count(), 1.5, 1.0);
     if (!bf16)
       e = args->head_dim == 64 ? launch_f32<64>(p, stream) : launch_f32<128>(p, stream);
     else
