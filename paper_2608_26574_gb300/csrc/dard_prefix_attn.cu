@@ -8,17 +8,19 @@
 // sum (the probabilities never leave the chip), fp32 accumulators. 20 warps:
 //   warps 0-15 softmax and epilogue: warps q, q + 4, q + 8 and q + 12 share TMEM lane quarter q
 //              (queries 32q .. 32q + 31), each taking 32 of a tile's 128 keys;
-//   warp 16    TMA producer: K and V through 3 stages each;
+//   warp 16    TMA producer of K, through 3 stages;
 //   warp 17    TMEM allocator and PV issuer: O += P_j V_j, P_j (bf16) read from TMEM;
 //   warp 18    S issuer: S_j = Q K_j^T (Q from TMEM, K from shared memory) into a ring of two
 //              128-column TMEM buffers;
-//   warp 19    own tiles only: looks for NaN and infinities in V (below).
+//   warp 19    TMA producer of V, through 3 stages (K runs ahead of V by two tiles: one producer of
+//              both would hold K up for V's stages).
 // TMEM: S ring [0, 256), O [256, 256 + D), P [384, 448), Q [448, 448 + D/2).
 //
 // Values that are not finite: the product with V multiplies every key of a tile by every query's
 // weight, and 0 times NaN is NaN. Keys of the prefix are seen by every query (rows behind its end
-// arrive as zeros), but an own tile holds copies and sequences that a query does not see. Warp 19
-// takes such values out of V before the product and adds them to the queries that do see the key.
+// arrive as zeros), but an own tile holds copies and sequences that a query does not see. The
+// softmax warps look through an own tile's V, a sixteenth each, before they hand their weights over:
+// such values are taken out of V before the product and added to the queries that do see the key.
 #include <algorithm>
 #include <cstdio>
 #include <cstdlib>
@@ -35,7 +37,7 @@ constexpr int kNKV = 3;  // TMA stages for K and for V
 constexpr int kSoftmaxWarps = 16;
 constexpr int kParts = 4;              // warps that share a query's keys
 constexpr int kCols = kTN / kParts;    // keys of a tile per thread
-constexpr int kWProd = 16, kWPV = 17, kWS = 18, kWCheck = 19;
+constexpr int kWK = 16, kWPV = 17, kWS = 18, kWV = 19;
 
 // Every barrier completes one phase per use of its ring slot; tile j uses slot j % ring and waits
 // for parity (j / ring) & 1. Each wait for use u of a slot is preceded, in the same thread or
@@ -44,9 +46,6 @@ struct __align__(16) Ctl {
   uint64_t q_full, o_full, p_full, pv_done;
   uint64_t k_full[kNKV], k_empty[kNKV], v_full[kNKV], v_empty[kNKV];
   uint64_t s_full[kNS], s_free[kNS];
-  uint64_t own_go[kNKV];  // an own tile's V copy has been issued (uses of own tiles only)
-  uint64_t v_ok[kNKV];    // an own tile's V holds finite values only (likewise)
-  uint64_t masks;         // row_mask and row_seq are written
   uint64_t drained;       // every product both issuers launched has completed (two commits)
   uint32_t tmem_base;
   int32_t abort;
@@ -69,58 +68,47 @@ __device__ __forceinline__ void flag_timeout(const PrefixParams& p, Ctl& ctl) {
   if (p.a.status) atomicOr(p.a.status, DARD_STATUS_TIMEOUT);
 }
 
-__device__ __forceinline__ void tma_load_3d(void* dst, const void* desc, uint64_t* bar, int32_t c0,
-                                            int32_t c1, int32_t c2) {
-  asm volatile(
-      "cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes"
-      " [%0], [%1, {%3, %4, %5}], [%2];" ::"r"(smem_u32(dst)),
-      "l"(reinterpret_cast<uint64_t>(desc)), "r"(smem_u32(bar)), "r"(c0), "r"(c1), "r"(c2)
-      : "memory");
-}
-
-// Warp 19, one own tile in shared memory: values that are not finite become zeros, and the queries
-// that see their keys are marked. `row0` is the tile's first row of k and v.
+// A sixteenth (`share`) of an own tile of V in shared memory: values that are not finite become
+// zeros, and the queries that see their keys are marked. `row0` is the tile's first row of k and v.
+// Called by whole warps, after row_mask and row_seq are written.
 template <int D>
-__device__ void check_values(const PrefixParams& p, Ctl& ctl, uint8_t* tile, int row0,
-                             long long wlim) {
+__device__ __forceinline__ void check_values(const PrefixParams& p, Ctl& ctl, uint8_t* tile, int row0,
+                                             int share) {
+  constexpr int kChunks = kTN * D / 8 / kSoftmaxWarps;  // 16-byte chunks of the warp
   const int lane = threadIdx.x & 31;
-  bool found = false;
-#pragma unroll 8
-  for (int i = lane; i < kTN * D / 8; i += 32) {
-    const uint4 u = *reinterpret_cast<const uint4*>(tile + 16 * i);
-    const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+  uint32_t bits = 0;  // bit 15 or 31: an exponent of all ones
 #pragma unroll
-    for (int e = 0; e < 4; ++e)
-      found |= (w[e] & 0x7f80u) == 0x7f80u || (w[e] & 0x7f800000u) == 0x7f800000u;
+  for (int u = 0; u < kChunks / 32; ++u) {
+    const uint4 x = *reinterpret_cast<const uint4*>(tile + 16 * (share * kChunks + 32 * u + lane));
+    bits |= ((x.x & 0x7fff7fffu) + 0x00800080u) | ((x.y & 0x7fff7fffu) + 0x00800080u) |
+            ((x.z & 0x7fff7fffu) + 0x00800080u) | ((x.w & 0x7fff7fffu) + 0x00800080u);
   }
-  if (!__any_sync(0xffffffffu, found)) return;
-  mbar_wait(&ctl.masks, 0, wlim);
-  if (found) {
-    for (int i = lane; i < kTN * D / 8; i += 32) {
-      uint16_t* v = reinterpret_cast<uint16_t*>(tile + 16 * i);
-      const int key = (i >> 3) % kTN;
-      const int e0 = (i >> 3) / kTN * 64 + (((i & 7) ^ (key & 7)) << 3);
-      uint32_t pos = 0, neg = 0;  // of the chunk's 8 elements
-      for (int e = 0; e < 8; ++e) {
-        const uint32_t b = v[e];
-        if ((b & 0x7f80u) != 0x7f80u) continue;
-        if ((b & 0x7fu) || !(b & 0x8000u)) pos |= 1u << e;
-        if ((b & 0x7fu) || (b & 0x8000u)) neg |= 1u << e;
-        v[e] = 0;
-      }
-      if (!(pos | neg)) continue;
-      for (int t = 0; t < kBM; ++t) {
-        const int s = ctl.row_seq[t];
-        if (s < 0 || !(own_vis64(p.a.seq[s], row0 + key - p.a.seq[s].row_base, ctl.row_mask[t]) & 1))
-          continue;
-        if (pos) atomicOr(&ctl.inf_pos[t][e0 >> 5], pos << (e0 & 31));
-        if (neg) atomicOr(&ctl.inf_neg[t][e0 >> 5], neg << (e0 & 31));
-        ctl.poison = 1;
-      }
+  if (!__any_sync(0xffffffffu, bits & 0x80008000u)) return;
+  for (int u = 0; u < kChunks / 32; ++u) {
+    const int i = share * kChunks + 32 * u + lane;
+    uint16_t* v = reinterpret_cast<uint16_t*>(tile + 16 * i);
+    const int key = (i >> 3) % kTN;
+    const int e0 = (i >> 3) / kTN * 64 + (((i & 7) ^ (key & 7)) << 3);
+    uint32_t pos = 0, neg = 0;  // of the chunk's 8 elements
+    for (int e = 0; e < 8; ++e) {
+      const uint32_t b = v[e];
+      if ((b & 0x7f80u) != 0x7f80u) continue;
+      if ((b & 0x7fu) || !(b & 0x8000u)) pos |= 1u << e;
+      if ((b & 0x7fu) || (b & 0x8000u)) neg |= 1u << e;
+      v[e] = 0;
+    }
+    if (!(pos | neg)) continue;
+    for (int t = 0; t < kBM; ++t) {
+      const int s = ctl.row_seq[t];
+      if (s < 0 || !(own_vis64(p.a.seq[s], row0 + key - p.a.seq[s].row_base, ctl.row_mask[t]) & 1))
+        continue;
+      if (pos) atomicOr(&ctl.inf_pos[t][e0 >> 5], pos << (e0 & 31));
+      if (neg) atomicOr(&ctl.inf_neg[t][e0 >> 5], neg << (e0 & 31));
+      ctl.poison = 1;
     }
   }
-  __threadfence_block();
   fence_proxy_async_smem();  // the zeros, before the product reads the tile
+  __syncwarp();
 }
 
 __device__ __forceinline__ float poisoned(const Ctl& ctl, int t, int e, float o) {
@@ -185,25 +173,21 @@ __global__ void __launch_bounds__(kThreads, 1)
     const void* map = k_or_v ? (own ? &tk : &tpk) : (own ? &tv : &tpv);
     const int row = own ? key0 + (j0 + j - npt) * kTN : (j0 + j) * kTN;
     mbar_arrive_expect_tx(bar, kKVBytes);
-    if (!k_or_v && own) mbar_arrive(&ctl.own_go[b]);
     if (k_or_v && j == p.a.test_drop_kv) return;  // test hook: this K copy is never issued
 #pragma unroll
     for (int s = 0; s < kSub; ++s) tma_load_3d(dst + s * kKSub, map, bar, s * 64, row, g);
   };
-  if (warp == kWProd && lane == 0) {
+  if (warp == kWK && lane == 0) {
     mbar_init(&ctl.q_full, kSoftmaxWarps);
     mbar_init(&ctl.drained, 2);
     mbar_init(&ctl.o_full, 1);
     mbar_init(&ctl.p_full, kSoftmaxWarps);
     mbar_init(&ctl.pv_done, 1);
-    mbar_init(&ctl.masks, 4);
     for (int b = 0; b < kNKV; ++b) {
       mbar_init(&ctl.k_full[b], 1);
       mbar_init(&ctl.k_empty[b], 1);
       mbar_init(&ctl.v_full[b], 1);
       mbar_init(&ctl.v_empty[b], 1);
-      mbar_init(&ctl.own_go[b], 1);
-      mbar_init(&ctl.v_ok[b], 1);
     }
     for (int b = 0; b < kNS; ++b) {
       mbar_init(&ctl.s_full[b], 1);
@@ -259,93 +243,74 @@ __global__ void __launch_bounds__(kThreads, 1)
   const uint32_t tQ = ctl.tmem_base + 448;
   volatile int32_t* abort_flag = &ctl.abort;
 
-  if (warp == kWProd) {
-    // ------------------------------------------------------------ TMA producer
+  if (warp == kWK || warp == kWV) {
+    // ------------------------------------------------------------ TMA producers
     if (lane == 0) {
-      int last_k = min(n_kt, kNKV) - 1, last_v = last_k;
+      const bool is_k = warp == kWK;
+      uint64_t* full = is_k ? ctl.k_full : ctl.v_full;
+      uint64_t* empty = is_k ? ctl.k_empty : ctl.v_empty;
+      int last = min(n_kt, kNKV) - 1;
       for (int j = kNKV; j < n_kt && !*abort_flag; ++j) {
-        const int b = j % kNKV, ph = ((j - kNKV) / kNKV) & 1;
-        if (!mbar_wait(&ctl.k_empty[b], ph, wlim)) { flag_timeout(p, ctl); break; }
-        load_kv(j, true);
-        last_k = j;
-        if (!mbar_wait(&ctl.v_empty[b], ph, wlim)) { flag_timeout(p, ctl); break; }
-        load_kv(j, false);
-        last_v = j;
+        if (!mbar_wait(&empty[j % kNKV], ((j - kNKV) / kNKV) & 1, wlim)) { flag_timeout(p, ctl); break; }
+        load_kv(j, is_k);
+        last = j;
       }
       // Every copy issued lands before shared memory is released: the latest use of each stage.
       for (int b = 0; b < kNKV; ++b) {
-        const int jk = last_k - ((last_k - b) % kNKV + kNKV) % kNKV;
-        const int jv = last_v - ((last_v - b) % kNKV + kNKV) % kNKV;
-        if (last_k >= 0 && jk >= 0 && jk != p.a.test_drop_kv)
-          mbar_wait(&ctl.k_full[b], (jk / kNKV) & 1, wlim);
-        if (last_v >= 0 && jv >= 0) mbar_wait(&ctl.v_full[b], (jv / kNKV) & 1, wlim);
+        const int jb = last - ((last - b) % kNKV + kNKV) % kNKV;
+        if (jb >= 0 && !(is_k && jb == p.a.test_drop_kv)) mbar_wait(&full[b], (jb / kNKV) & 1, wlim);
       }
     }
   } else if (warp == kWS) {
     // ------------------------------------------------------------ S issuer
-    if (lane == 0) {
-      constexpr uint32_t kIdS = idesc_bf16_f32(kBM, kTN, 0, 0);
-      const uint32_t ak = smem_u32(sK);
-      bool ok = mbar_wait(&ctl.q_full, 0, wlim);
-      for (int j = 0; j < n_kt && ok && !*abort_flag; ++j) {
-        const int kb = j % kNKV, sb = j % kNS;
-        if (j >= kNS) ok = mbar_wait(&ctl.s_free[sb], ((j - kNS) / kNS) & 1, wlim);
-        ok = ok && mbar_wait(&ctl.k_full[kb], (j / kNKV) & 1, wlim);
-        if (!ok) break;
-        tc_fence_after();
-        const uint32_t kaddr = ak + kb * kKVBytes;
-        const uint32_t dst = ctl.tmem_base + sb * kTN;
+    // (both issuers: the whole warp walks the loop, so that what it computes is uniform over the
+    // warp and stays in uniform registers; one elected lane issues)
+    constexpr uint32_t kIdS = idesc_bf16_f32(kBM, kTN, 0, 0);
+    const bool issue = elect_one();
+    const uint64_t desc = smem_desc_sw128(smem_u32(sK), 16, 1024);
+    bool ok = warp_wait(&ctl.q_full, 0, wlim);
+    for (int j = 0; j < n_kt && ok; ++j) {
+      const int kb = j % kNKV, sb = j % kNS;
+      if (j >= kNS) ok = warp_wait(&ctl.s_free[sb], ((j - kNS) / kNS) & 1, wlim);
+      ok = ok && warp_wait(&ctl.k_full[kb], (j / kNKV) & 1, wlim);
+      if (!ok) break;
+      tc_fence_after();
+      if (issue) {
+        const uint64_t dk = desc + kb * (kKVBytes / 16);
 #pragma unroll
-        for (int ks = 0; ks < D / 16; ++ks) {
-          const uint32_t ko = (ks >> 2) * kKSub + (ks & 3) * 32;
-          mma_ts(dst, tQ + ks * 8, smem_desc_sw128(kaddr + ko, 16, 1024), kIdS, ks > 0);
-        }
+        for (int ks = 0; ks < D / 16; ++ks)
+          mma_ts(ctl.tmem_base + sb * kTN, tQ + ks * 8, dk + (ks >> 2) * (kKSub / 16) + (ks & 3) * 2, kIdS, ks > 0);
         mma_commit(&ctl.s_full[sb]);
         mma_commit(&ctl.k_empty[kb]);
       }
-      if (!ok) flag_timeout(p, ctl);
-      mma_commit(&ctl.drained);
     }
+    if (!ok && lane == 0) flag_timeout(p, ctl);
+    if (issue) mma_commit(&ctl.drained);
+    __syncwarp();
   } else if (warp == kWPV) {
     // ------------------------------------------------------------ PV issuer
-    if (lane == 0) {
-      constexpr uint32_t kIdO = idesc_bf16_f32(kBM, D, 0, 1);
-      const uint32_t av = smem_u32(sV);
-      bool ok = true;
-      for (int j = 0; j < n_kt && ok && !*abort_flag; ++j) {
-        const int vb = j % kNKV, o = j - first_own;
-        ok = mbar_wait(&ctl.p_full, j & 1, wlim) &&
-             (o < 0 ? mbar_wait(&ctl.v_full[vb], (j / kNKV) & 1, wlim)
-                    : mbar_wait(&ctl.v_ok[vb], (o / kNKV) & 1, wlim));
-        if (!ok) break;
-        tc_fence_after();
-        const uint32_t vaddr = av + vb * kKVBytes;
+    constexpr uint32_t kIdO = idesc_bf16_f32(kBM, D, 0, 1);
+    const bool issue = elect_one();
+    const uint64_t desc = smem_desc_sw128(smem_u32(sV), kKSub, 1024);
+    bool ok = true;
+    for (int j = 0; j < n_kt && ok; ++j) {
+      const int vb = j % kNKV;
+      ok = warp_wait(&ctl.v_full[vb], (j / kNKV) & 1, wlim) && warp_wait(&ctl.p_full, j & 1, wlim);
+      if (!ok) break;
+      tc_fence_after();
+      if (issue) {
+        const uint64_t dv = desc + vb * (kKVBytes / 16);
 #pragma unroll
         for (int ks = 0; ks < kTN / 16; ++ks)
-          mma_ts(tO, tP + ks * 8, smem_desc_sw128(vaddr + ks * 2048, kKSub, 1024), kIdO,
-                 (j > 0 || ks > 0) ? 1u : 0u);
+          mma_ts(tO, tP + ks * 8, dv + ks * (2048 / 16), kIdO, (j > 0 || ks > 0) ? 1u : 0u);
         mma_commit(&ctl.pv_done);
         mma_commit(&ctl.v_empty[vb]);
         if (j == n_kt - 1) mma_commit(&ctl.o_full);
       }
-      if (!ok) flag_timeout(p, ctl);
-      mma_commit(&ctl.drained);
-    }
-  } else if (warp == kWCheck) {
-    // ------------------------------------------------------------ own tiles' values
-    // (own_go before v_full: the stage's use before this one has completed by then)
-    bool ok = true;
-    for (int j = first_own; j < n_kt && ok && !*abort_flag; ++j) {
-      const int vb = j % kNKV;
-      ok = mbar_wait(&ctl.own_go[vb], ((j - first_own) / kNKV) & 1, wlim) &&
-           mbar_wait(&ctl.v_full[vb], (j / kNKV) & 1, wlim);
-      ok = __all_sync(0xffffffffu, ok);
-      if (!ok) break;
-      check_values<D>(p, ctl, sV + vb * kKVBytes, key0 + (j0 + j - npt) * kTN, wlim);
-      __syncwarp();
-      if (lane == 0) mbar_arrive(&ctl.v_ok[vb]);
     }
     if (!ok && lane == 0) flag_timeout(p, ctl);
+    if (issue) mma_commit(&ctl.drained);
+    __syncwarp();
   } else {
     // ------------------------------------------------------------ softmax + epilogue
     const uint32_t lane_off = static_cast<uint32_t>(quarter * 32) << 16;
@@ -363,10 +328,8 @@ __global__ void __launch_bounds__(kThreads, 1)
         ctl.row_mask[t] = warp_query_masks(p.a, seq, r, g == 0, store);
         ctl.row_seq[t] = seq;
         ctl.out_row[t] = store ? out_row : -1;
-        __syncwarp();
-        if (lane == 0) mbar_arrive(&ctl.masks);
       }
-      quarter_bar_sync(quarter);
+      all_bar_sync();  // (check_values() reads every row's mask)
     } else if (part4 == 0) {
       ctl.out_row[t] = out_row;
     }
@@ -445,6 +408,13 @@ __global__ void __launch_bounds__(kThreads, 1)
         tmem_store(tO + lane_off + part4 * kOC, rr);
       }
       tmem_store(tP + lane_off + part4 * (kCols / 2), pk);
+      if (j >= first_own) {
+        // (the stage's use before this one has landed: PV_{j-1} has completed, and this use ends
+        // only after this warp's weights)
+        ok = mbar_wait(&ctl.v_full[j % kNKV], (j / kNKV) & 1, wlim);
+        if (!__all_sync(0xffffffffu, ok)) { ok = false; break; }
+        check_values<D>(p, ctl, sV + j % kNKV * kKVBytes, key0 + (j0 + j - npt) * kTN, warp);
+      }
       tmem_wait_st();
       tc_fence_before();
       __syncwarp();
@@ -648,32 +618,17 @@ int choose_split(long long items, double steps, int most, int sms, double fixed,
   return best;
 }
 
-bool make_map3(CUtensorMap* m, const void* ptr, int d, long long rows, int heads, int64_t row_stride,
-               int64_t head_stride) {
-  auto fn = encode_fn();
-  if (!fn) return false;
-  const cuuint64_t dims[3] = {static_cast<cuuint64_t>(d), static_cast<cuuint64_t>(rows),
-                              static_cast<cuuint64_t>(heads)};
-  const cuuint64_t strides[2] = {static_cast<cuuint64_t>(row_stride) * 2,
-                                 static_cast<cuuint64_t>(head_stride) * 2};
-  const cuuint32_t box[3] = {64, kTN, 1};
-  const cuuint32_t estr[3] = {1, 1, 1};
-  return fn(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(ptr), dims, strides, box, estr,
-            CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
-            CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
-}
-
 template <int D>
 cudaError_t launch_tc(const PrefixParams& p, cudaStream_t stream) {
   static std::atomic<uint64_t> done{0};
   CUtensorMap pk, pv, k, v;
   const AttnParams& a = p.a;
-  if (!make_map3(&k, a.k, D, a.total_rows, a.hkv, static_cast<int64_t>(a.hkv) * D, D) ||
-      !make_map3(&v, a.v, D, a.total_rows, a.hkv, static_cast<int64_t>(a.hkv) * D, D))
+  if (!make_map3(&k, a.k, D, a.total_rows, a.hkv, static_cast<int64_t>(a.hkv) * D, D, kTN, 1) ||
+      !make_map3(&v, a.v, D, a.total_rows, a.hkv, static_cast<int64_t>(a.hkv) * D, D, kTN, 1))
     return cudaErrorInvalidValue;
   if (p.prefix_len > 0) {
-    if (!make_map3(&pk, p.pk, D, p.prefix_len, a.hkv, p.row_stride, p.head_stride) ||
-        !make_map3(&pv, p.pv, D, p.prefix_len, a.hkv, p.row_stride, p.head_stride))
+    if (!make_map3(&pk, p.pk, D, p.prefix_len, a.hkv, p.row_stride, p.head_stride, kTN, 1) ||
+        !make_map3(&pv, p.pv, D, p.prefix_len, a.hkv, p.row_stride, p.head_stride, kTN, 1))
       return cudaErrorInvalidValue;
   } else {
     pk = k;

@@ -19,7 +19,7 @@
 #include <cstdlib>
 #include <cstring>
 
-#include "dard_attn_common.cuh"
+#include "dard_prefix.cuh"
 
 namespace dard {
 namespace {
@@ -75,15 +75,6 @@ constexpr size_t smem_bytes() {
 __device__ __forceinline__ void flag_timeout(const WeightsParams& p, Ctl& ctl) {
   ctl.abort = 1;
   if (p.status) atomicOr(p.status, DARD_STATUS_TIMEOUT);
-}
-
-__device__ __forceinline__ void tma_load_3d(void* dst, const void* desc, uint64_t* bar, int32_t c0,
-                                            int32_t c1, int32_t c2) {
-  asm volatile(
-      "cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes"
-      " [%0], [%1, {%3, %4, %5}], [%2];" ::"r"(smem_u32(dst)),
-      "l"(reinterpret_cast<uint64_t>(desc)), "r"(smem_u32(bar)), "r"(c0), "r"(c1), "r"(c2)
-      : "memory");
 }
 
 // Sum over 32 columns of 2^(s sl - lse) for one key. kOff: columns with a bit of `off` count for
@@ -194,55 +185,77 @@ __global__ void __launch_bounds__(kThreads, 1)
     }
   } else if (warp == kWMma) {
     // ------------------------------------------------------------ issuer
-    if (lane == 0) {
-      constexpr uint32_t kId = idesc_bf16_f32(kBM, kTN, 0, 0);
-      const uint32_t ak = smem_u32(sK), aq = smem_u32(sQ);
-      bool ok = mbar_wait(&ctl.k_full, 0, wlim);
-      for (int j = 0; j < n && ok && !*abort_flag; ++j) {
-        const int b = j % kQStages, sb = j % kSBufs;
-        if (j >= kSBufs) ok = mbar_wait(&ctl.s_free[sb], ((j - kSBufs) / kSBufs) & 1, wlim);
-        ok = ok && mbar_wait(&ctl.q_full[b], (j / kQStages) & 1, wlim);
-        if (!ok) break;
-        tc_fence_after();
+    // (the whole warp walks the loop, so that what it computes is uniform over the warp and stays in
+    // uniform registers; one elected lane issues: with one lane walking alone a tile took 1600
+    // cycles, most of them the issue of its products)
+    constexpr uint32_t kId = idesc_bf16_f32(kBM, kTN, 0, 0);
+    const bool issue = elect_one();
+    const uint64_t da = smem_desc_sw128(smem_u32(sK), 16, 1024), dq = smem_desc_sw128(smem_u32(sQ), 16, 1024);
+    bool ok = warp_wait(&ctl.k_full, 0, wlim);
+    for (int j = 0; j < n && ok; ++j) {
+      const int b = j % kQStages, sb = j % kSBufs;
+      if (j >= kSBufs) ok = warp_wait(&ctl.s_free[sb], ((j - kSBufs) / kSBufs) & 1, wlim);
+      ok = ok && warp_wait(&ctl.q_full[b], (j / kQStages) & 1, wlim);
+      if (!ok) break;
+      tc_fence_after();
+      if (issue) {
+        const uint64_t db = dq + b * (kTile / 16);
 #pragma unroll
         for (int ks = 0; ks < D / 16; ++ks) {
-          const uint32_t off = (ks >> 2) * kKSub + (ks & 3) * 32;
-          mma_ss(ctl.tmem_base + sb * kTN, smem_desc_sw128(ak + off, 16, 1024),
-                 smem_desc_sw128(aq + b * kTile + off, 16, 1024), kId, ks > 0);
+          const uint64_t off = (ks >> 2) * (kKSub / 16) + (ks & 3) * 2;
+          mma_ss(ctl.tmem_base + sb * kTN, da + off, db + off, kId, ks > 0);
         }
         mma_commit(&ctl.s_full[sb]);
         mma_commit(&ctl.q_empty[b]);
       }
-      if (!ok) flag_timeout(p, ctl);
-      mma_commit(&ctl.drained);
     }
+    if (!ok && lane == 0) flag_timeout(p, ctl);
+    if (issue) mma_commit(&ctl.drained);
+    __syncwarp();
   } else if (warp == kWLse) {
     // ------------------------------------------------------------ normalisers
+    // (three tiles' loads in flight; column 32 e + lane of a tile is row rr[e], head hh[e] of it)
+    constexpr int kAhead = 3;
+    int rr[4], hh[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      rr[e] = (32 * e + lane) / p.box_heads;
+      hh[e] = (32 * e + lane) % p.box_heads;
+    }
+    auto fetch = [&](int j, float (&v)[4]) {
+      const int tile = j0 + j;
+      const int h0 = p.head_blocks > 1 ? tile % p.head_blocks * p.box_heads : 0;
+      const int64_t row0 = static_cast<int64_t>(p.head_blocks > 1 ? tile / p.head_blocks : tile) * p.box_rows;
+      const float* src = p.lse + row0 * p.hq + g * p.group + h0;
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        v[e] = j < n && 32 * e + lane < columns && h0 + hh[e] < p.group && row0 + rr[e] < p.rows
+                   ? __ldg(src + static_cast<int64_t>(rr[e]) * p.hq + hh[e]) : INFINITY;
+    };
+    float v[kAhead][4];
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u) fetch(u, v[u]);
     bool ok = true;
     for (int j = 0; j < n && ok && !*abort_flag; ++j) {
-      const int b = j % kQStages, tile = j0 + j;
-      float v[4];
-      bool off[4];  // a query with lse = +inf (columns without a query have scores of 0)
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {  // column 32 e + lane
-        const int c = 32 * e + lane;
-        const int h = tile % p.head_blocks * p.box_heads + c % p.box_heads;
-        const int64_t row = static_cast<int64_t>(tile / p.head_blocks) * p.box_rows + c / p.box_heads;
-        const bool in = c < columns && h < p.group && row < p.rows;
-        v[e] = in ? __ldg(p.lse + row * p.hq + g * p.group + h) : INFINITY;
-        off[e] = v[e] == INFINITY && c < columns && row < p.rows;
-      }
+      const int b = j % kQStages;
       if (j >= kQStages) ok = mbar_wait(&ctl.l_empty[b], ((j - kQStages) / kQStages) & 1, wlim);
       ok = __all_sync(0xffffffffu, ok);
       if (!ok) break;
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        const uint32_t bits = __ballot_sync(0xffffffffu, off[e]);
-        ctl.lse[b][32 * e + lane] = v[e] * -kLog2e;
+        // a query whose lse is +inf adds nothing (columns without a query or behind the last row
+        // need no bit: their scores are 0)
+        const uint32_t bits = __ballot_sync(0xffffffffu, v[0][e] == INFINITY && 32 * e + lane < columns);
+        ctl.lse[b][32 * e + lane] = v[0][e] * -kLog2e;
         if (lane == 0) ctl.off[b][e] = bits;
       }
       __syncwarp();
       if (lane == 0) mbar_arrive(&ctl.l_full[b]);
+#pragma unroll
+      for (int u = 0; u + 1 < kAhead; ++u)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[u][e] = v[u + 1][e];
+      fetch(j + kAhead, v[kAhead - 1]);
     }
     if (!ok && lane == 0) flag_timeout(p, ctl);
   } else {
@@ -416,20 +429,6 @@ __global__ void __launch_bounds__(256) weights_join(const __grid_constant__ Weig
 // ---------------------------------------------------------------- host side
 constexpr int kParts = 64;               // parts of a split launch at most
 constexpr long long kSplitCtas = 2048;   // CTAs of a split launch at most
-
-bool make_map3(CUtensorMap* m, const void* ptr, int d, long long n1, long long n2, int64_t stride1,
-               int64_t stride2, int box1, int box2) {
-  auto fn = encode_fn();
-  if (!fn) return false;
-  const cuuint64_t dims[3] = {static_cast<cuuint64_t>(d), static_cast<cuuint64_t>(n1),
-                              static_cast<cuuint64_t>(n2)};
-  const cuuint64_t strides[2] = {static_cast<cuuint64_t>(stride1) * 2, static_cast<cuuint64_t>(stride2) * 2};
-  const cuuint32_t box[3] = {64, static_cast<cuuint32_t>(box1), static_cast<cuuint32_t>(box2)};
-  const cuuint32_t estr[3] = {1, 1, 1};
-  return fn(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(ptr), dims, strides, box, estr,
-            CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
-            CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
-}
 
 template <int D>
 cudaError_t launch_tc(const WeightsParams& p, cudaStream_t stream) {
