@@ -46,6 +46,18 @@ __device__ __forceinline__ bool elect_one() {
   asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(r));
   return r != 0;
 }
+// Whether a phase has completed, without waiting: its answer takes some 120 cycles, which a wait at
+// the same place would too; asked ahead of the work before that place, it costs nothing.
+__device__ __forceinline__ bool mbar_test(uint64_t* bar, uint32_t parity) {
+  uint32_t ok;
+  asm volatile(
+      "{\n\t.reg .pred p;\n\tmbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
+      "selp.u32 %0, 1, 0, p;\n\t}"
+      : "=r"(ok)
+      : "r"(smem_u32(bar)), "r"(parity)
+      : "memory");
+  return ok != 0;
+}
 // Bounded wait of a whole warp.
 __device__ __forceinline__ bool warp_wait(uint64_t* bar, uint32_t parity, long long limit) {
   return __all_sync(0xffffffffu, mbar_wait(bar, parity, limit));

@@ -335,22 +335,18 @@ __global__ void __launch_bounds__(kThreads, 1)
     }
     const float sl = p.a.scale_log2;
     float m_run = -INFINITY, l_run = 0.f;
-    bool ok = true;
+    // from here on tiles have keys that some query does not see
+    const int first_masked = min(first_own, p.prefix_len / kTN - j0);
+    bool ok = true, ready = false;
     for (int j = 0; j < n_kt; ++j) {
-      const int b = j % kNS;
-      uint32_t vis = ~0u;
-      if (j >= first_own)
-        vis = seq < 0 ? 0u
-                      : static_cast<uint32_t>(own_vis64(
-                            p.a.seq[seq], key0 + (j0 + j - npt) * kTN + kCols * part4 - p.a.seq[seq].row_base,
-                            ctl.row_mask[t]));
-      else if ((j0 + j + 1) * kTN > p.prefix_len)
-        vis = static_cast<uint32_t>(first64(p.prefix_len - (j0 + j) * kTN - kCols * part4));
+      const int b = j & (kNS - 1);
       // The four warps of the rows wait for the same S_j with the same bound (no early leave on an
       // abort flag), so they leave the loop together: a barrier completing between the warps'
       // deadlines (a product about a second late) is the only way they could part.
-      ok = mbar_wait(&ctl.s_full[b], (j / kNS) & 1, wlim);
-      if (!__all_sync(0xffffffffu, ok)) { ok = false; break; }
+      if (!__all_sync(0xffffffffu, ready)) {
+        ok = warp_wait(&ctl.s_full[b], (j / kNS) & 1, wlim);
+        if (!ok) break;
+      }
       tc_fence_after();
       uint32_t s[kCols];
       tmem_load(ctl.tmem_base + b * kTN + kCols * part4 + lane_off, s);
@@ -358,7 +354,14 @@ __global__ void __launch_bounds__(kThreads, 1)
       tc_fence_before();
       __syncwarp();
       if (lane == 0) mbar_arrive(&ctl.s_free[b]);
-      if (__any_sync(0xffffffffu, vis != ~0u)) {
+      if (j >= first_masked) {
+        uint32_t vis = 0;
+        if (j < first_own)
+          vis = static_cast<uint32_t>(first64(p.prefix_len - (j0 + j) * kTN - kCols * part4));
+        else if (seq >= 0)
+          vis = static_cast<uint32_t>(own_vis64(
+              p.a.seq[seq], key0 + (j0 + j - npt) * kTN + kCols * part4 - p.a.seq[seq].row_base,
+              ctl.row_mask[t]));
 #pragma unroll
         for (int k = 0; k < kCols; ++k) s[k] = (vis >> k) & 1u ? s[k] : 0xff800000u;  // -inf
       }
@@ -382,6 +385,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       const bool rescale = (m_new != m_run) && (m_run != -INFINITY);
       const float alpha = rescale ? ex2_approx((m_run - m_new) * sl) : 1.f;
       const float mL = (m_new == -INFINITY) ? 0.f : m_new * sl;
+      const bool pv_done = j == 0 || mbar_test(&ctl.pv_done, (j - 1) & 1);  // (asked ahead)
       uint32_t pk[kCols / 2];
       const uint64_t sl2 = f2_pack(sl, sl), nmL2 = f2_pack(-mL, -mL);
       uint64_t acc[2] = {0, 0};  // bit pattern 0 = +0.0f
@@ -394,11 +398,12 @@ __global__ void __launch_bounds__(kThreads, 1)
         pk[e] = pack_bf16x2(x0, x1);
         acc[e & 1] = f2_add(acc[e & 1], f2_pack(x0, x1));
       }
-      if (j > 0) {  // P_j replaces P_{j-1}, and O may be rescaled, once PV_{j-1} has completed
-        ok = mbar_wait(&ctl.pv_done, (j - 1) & 1, wlim);
-        if (!__all_sync(0xffffffffu, ok)) { ok = false; break; }
-        tc_fence_after();
+      // P_j replaces P_{j-1}, and O may be rescaled, once PV_{j-1} has completed
+      if (!__all_sync(0xffffffffu, pv_done)) {
+        ok = warp_wait(&ctl.pv_done, (j - 1) & 1, wlim);
+        if (!ok) break;
       }
+      tc_fence_after();
       if (__any_sync(0xffffffffu, rescale)) {  // this warp's share of the O columns
         uint32_t rr[kOC];
         tmem_load(tO + lane_off + part4 * kOC, rr);
@@ -415,6 +420,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         if (!__all_sync(0xffffffffu, ok)) { ok = false; break; }
         check_values<D>(p, ctl, sV + j % kNKV * kKVBytes, key0 + (j0 + j - npt) * kTN, warp);
       }
+      ready = j + 1 < n_kt && mbar_test(&ctl.s_full[(j + 1) & (kNS - 1)], ((j + 1) / kNS) & 1);  // (asked ahead)
       tmem_wait_st();
       tc_fence_before();
       __syncwarp();
