@@ -12,6 +12,9 @@
 
 namespace dard {
 
+constexpr int kTileTable = 1024;
+static_assert(DARD_MAX_SEQS <= 256, "sequences fit in a byte");
+
 struct PrefixParams {
   AttnParams a;               // the own rows (a.q, a.k, a.v, a.o and the sequences)
   const void* pk;
@@ -25,6 +28,7 @@ struct PrefixParams {
   int32_t tiles;              // query tiles of a key/value head
   int32_t nsplit;             // CTAs that share a tile's keys
   int32_t q_before[DARD_MAX_SEQS + 1];  // query rows of the sequences before each
+  uint8_t tile_seq[kTileTable][2];      // first and last sequence of a query tile, if all fit in
 };
 
 // Parts of a split launch: one slot per (tile, part), rows x (D + 2) floats: the unnormalised
@@ -70,6 +74,18 @@ __device__ __forceinline__ void tma_load_3d(void* dst, const void* desc, uint64_
       "l"(reinterpret_cast<uint64_t>(desc)), "r"(smem_u32(bar)), "r"(c0), "r"(c1), "r"(c2)
       : "memory");
 }
+__device__ __forceinline__ void tmem_st8(uint32_t taddr, const uint32_t (&r)[8]) {
+  asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"r"(taddr),
+               "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7])
+               : "memory");
+}
+// 32 or 16 columns of this warp's lanes.
+__device__ __forceinline__ void tmem_load(uint32_t addr, uint32_t (&r)[32]) { tmem_ld32(addr, r); }
+__device__ __forceinline__ void tmem_load(uint32_t addr, uint32_t (&r)[16]) { tmem_ld16(addr, r); }
+__device__ __forceinline__ void tmem_store(uint32_t addr, const uint32_t (&r)[32]) { tmem_st32(addr, r); }
+__device__ __forceinline__ void tmem_store(uint32_t addr, const uint32_t (&r)[16]) { tmem_st16(addr, r); }
+__device__ __forceinline__ void tmem_store(uint32_t addr, const uint32_t (&r)[8]) { tmem_st8(addr, r); }
+
 // Tensor map of bf16 elements [n2, n1, d], strides in elements, boxes of 64 x box1 x box2 with the
 // 128-byte swizzle; elements outside read as zeros.
 inline bool make_map3(CUtensorMap* m, const void* ptr, int d, long long n1, long long n2, int64_t stride1,
@@ -86,23 +102,34 @@ inline bool make_map3(CUtensorMap* m, const void* ptr, int d, long long n1, long
             CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-// Sequence of query row t.
-__device__ __forceinline__ int seq_of_query(const PrefixParams& p, int t) {
-  int lo = 0, hi = p.a.num_seqs;  // q_before[lo] <= t < q_before[hi]
-  while (hi - lo > 1) {
+// Sequence of query row t, one of [lo, hi) (the last that starts at t or before: sequences without
+// queries are passed over).
+__device__ __forceinline__ int seq_of_query(const PrefixParams& p, int t, int lo, int hi) {
+  while (hi - lo > 1) {  // q_before[lo] <= t < q_before[hi]
     const int mid = (lo + hi) >> 1;
     if (p.q_before[mid] <= t) lo = mid; else hi = mid;
   }
   return lo;
 }
+__device__ __forceinline__ int seq_of_query(const PrefixParams& p, int t) {
+  return seq_of_query(p, t, 0, p.a.num_seqs);
+}
 
-// A tile's keys behind the prefix: rows [key0, key_end) of k and v.
-__device__ __forceinline__ void own_range(const PrefixParams& p, int m0, int rows, int& key0,
-                                          int& key_end) {
-  const int last = min(m0 + rows, p.queries) - 1;
-  key0 = p.a.seq[seq_of_query(p, m0 / p.group)].row_base;
-  const SeqDesc& s = p.a.seq[seq_of_query(p, last / p.group)];
-  key_end = s.row_base + s.n_orig + s.slen;
+// A tile's sequences [s0, s1] and its keys behind the prefix: rows [key0, key_end) of k and v. The
+// same for every thread of a CTA, in a form that the compiler sees to be (results of ballots or
+// selects would make the loop bounds that depend on it a thread's own: 5 % of a long call); from the
+// launch's table where the tiles fit in (a search waits some 200 cycles for each of its reads).
+__device__ __forceinline__ void own_range(const PrefixParams& p, int tile, int rows, int& s0, int& s1,
+                                          int& key0, int& key_end) {
+  if (p.tiles <= kTileTable) {
+    s0 = p.tile_seq[tile][0];
+    s1 = p.tile_seq[tile][1];
+  } else {
+    s0 = seq_of_query(p, tile * rows / p.group);
+    s1 = seq_of_query(p, (min((tile + 1) * rows, p.queries) - 1) / p.group);
+  }
+  key0 = p.a.seq[s0].row_base;
+  key_end = p.a.seq[s1].row_base + p.a.seq[s1].n_orig + p.a.seq[s1].slen;
 }
 
 // The masks of the rows of one warp over their sequences' blocks, read from global memory: what

@@ -125,18 +125,6 @@ __device__ __forceinline__ void all_bar_sync() {
 __device__ __forceinline__ void quarter_bar_sync(int q) {
   asm volatile("bar.sync %0, 128;" ::"r"(3 + q) : "memory");
 }
-__device__ __forceinline__ void tmem_st8(uint32_t taddr, const uint32_t (&r)[8]) {
-  asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"r"(taddr),
-               "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7])
-               : "memory");
-}
-// 32 or 16 columns of this warp's lanes.
-__device__ __forceinline__ void tmem_load(uint32_t addr, uint32_t (&r)[32]) { tmem_ld32(addr, r); }
-__device__ __forceinline__ void tmem_load(uint32_t addr, uint32_t (&r)[16]) { tmem_ld16(addr, r); }
-__device__ __forceinline__ void tmem_store(uint32_t addr, const uint32_t (&r)[32]) { tmem_st32(addr, r); }
-__device__ __forceinline__ void tmem_store(uint32_t addr, const uint32_t (&r)[16]) { tmem_st16(addr, r); }
-__device__ __forceinline__ void tmem_store(uint32_t addr, const uint32_t (&r)[8]) { tmem_st8(addr, r); }
-
 template <int D>
 __global__ void __launch_bounds__(kThreads, 1)
     prefix_tc(const __grid_constant__ PrefixParams p, const __grid_constant__ CUtensorMap tpk,
@@ -153,10 +141,12 @@ __global__ void __launch_bounds__(kThreads, 1)
   Ctl& ctl = *reinterpret_cast<Ctl*>(sV + kNKV * kKVBytes);
 
   grid_dep_launch();  // the launch that joins the parts may be scheduled; it waits for this one
+  // (The work's bounds come before any branch on the warp: behind one the compiler holds them per
+  // thread, and the loops below run 6 % slower.)
   const int item = blockIdx.x / p.nsplit, part = blockIdx.x % p.nsplit;
   const int g = item / p.tiles, m0 = item % p.tiles * kBM;
-  int key0, key_end;
-  own_range(p, m0, kBM, key0, key_end);
+  int s0, s1, key0, key_end;
+  own_range(p, item % p.tiles, kBM, s0, s1, key0, key_end);
   const int npt = (p.prefix_len + kTN - 1) / kTN;  // the prefix's tiles
   const int all = npt + (key_end - key0 + kTN - 1) / kTN;
   const int j0 = static_cast<int>(static_cast<long long>(all) * part / p.nsplit);
@@ -196,10 +186,8 @@ __global__ void __launch_bounds__(kThreads, 1)
     ctl.abort = 0;
     ctl.poison = 0;
     fence_barrier_init();
-    for (int j = 0; j < kNKV && j < n_kt; ++j) {
-      load_kv(j, true);
-      load_kv(j, false);
-    }
+    load_kv(0, true);  // (the rest follows behind the block's barrier)
+    load_kv(0, false);
   }
   if (warp == kWPV) {
     tmem_alloc<kTmemCols>(&ctl.tmem_base);
@@ -215,7 +203,7 @@ __global__ void __launch_bounds__(kThreads, 1)
   if (warp < kSoftmaxWarps) {
     if (m0 + t < p.queries) {
       const int tq = (m0 + t) / p.group;
-      seq = seq_of_query(p, tq);
+      seq = seq_of_query(p, tq, s0, s1 + 1);
       r = p.a.seq[seq].q_start + tq - p.q_before[seq];
       out_row = static_cast<int64_t>(p.a.seq[seq].row_base + r) * p.a.hq + g * p.group +
                 (m0 + t) % p.group;
@@ -249,9 +237,12 @@ __global__ void __launch_bounds__(kThreads, 1)
       const bool is_k = warp == kWK;
       uint64_t* full = is_k ? ctl.k_full : ctl.v_full;
       uint64_t* empty = is_k ? ctl.k_empty : ctl.v_empty;
-      int last = min(n_kt, kNKV) - 1;
-      for (int j = kNKV; j < n_kt && !*abort_flag; ++j) {
-        if (!mbar_wait(&empty[j % kNKV], ((j - kNKV) / kNKV) & 1, wlim)) { flag_timeout(p, ctl); break; }
+      int last = 0;
+      for (int j = 1; j < n_kt && !*abort_flag; ++j) {
+        if (j >= kNKV && !mbar_wait(&empty[j % kNKV], ((j - kNKV) / kNKV) & 1, wlim)) {
+          flag_timeout(p, ctl);
+          break;
+        }
         load_kv(j, is_k);
         last = j;
       }
@@ -747,21 +738,25 @@ dard_status dard_prefix_attention(const dard_prefix_attn_args* args, void* strea
     return report(DARD_ERR_SHAPE, "too many query tiles");
   p.nsplit = 1;
   const long long items = static_cast<long long>(p.tiles) * p.a.hkv;
-  if (p.part != nullptr && items * 2 <= kSlots) {
-    // every tile has the prefix's key tiles and at least one of its own
-    const int least = (p.prefix_len + key_tile - 1) / key_tile + 1;
-    double own = 0;  // own key tiles of a query tile, on average
+  // every tile has the prefix's key tiles and at least one of its own
+  const int least = (p.prefix_len + key_tile - 1) / key_tile + 1;
+  double own = 0;  // own key tiles of a query tile, on average
+  if (p.tiles <= kTileTable) {
+    int s0 = 0, s1 = 0;
     for (int i = 0; i < p.tiles; ++i) {
       const int t0 = static_cast<int>(static_cast<long long>(i) * rows / p.group);
       const int t1 = static_cast<int>((std::min<long long>((i + 1ll) * rows, p.queries) - 1) / p.group);
-      const int s0 = static_cast<int>(std::upper_bound(p.q_before, p.q_before + p.a.num_seqs, t0) - p.q_before) - 1;
-      const int s1 = static_cast<int>(std::upper_bound(p.q_before, p.q_before + p.a.num_seqs, t1) - p.q_before) - 1;
+      while (p.q_before[s0 + 1] <= t0) ++s0;
+      while (p.q_before[s1 + 1] <= t1) ++s1;
+      p.tile_seq[i][0] = static_cast<uint8_t>(s0);
+      p.tile_seq[i][1] = static_cast<uint8_t>(s1);
       own += (p.a.seq[s1].row_base + p.a.seq[s1].n_orig + p.a.seq[s1].slen - p.a.seq[s0].row_base +
               key_tile - 1) / key_tile;
     }
     const double steps = least - 1 + own / p.tiles;
-    p.nsplit = bf16 ? choose_split(items, steps, least, sms, 8000, 1500)
-                    : choose_split(items, steps, least, sms, 6000, 100.0 * rows);
+    if (p.part != nullptr)
+      p.nsplit = bf16 ? choose_split(items, steps, least, sms, 8000, 1500)
+                      : choose_split(items, steps, least, sms, 6000, 100.0 * rows);
   }
   cudaError_t e;
   if (!bf16)

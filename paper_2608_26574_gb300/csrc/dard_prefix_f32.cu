@@ -45,8 +45,8 @@ __global__ void __launch_bounds__(kF32Threads) prefix_f32(const __grid_constant_
   grid_dep_launch();
   const int item = blockIdx.x / p.nsplit, part = blockIdx.x % p.nsplit;
   const int g = item / p.tiles, m0 = item % p.tiles * kRows;
-  int key0, key_end;
-  own_range(p, m0, kRows, key0, key_end);
+  int s0, s1, key0, key_end;
+  own_range(p, item % p.tiles, kRows, s0, s1, key0, key_end);
   const int npt = (p.prefix_len + kF32Keys - 1) / kF32Keys;
   const int all = npt + (key_end - key0 + kF32Keys - 1) / kF32Keys;
   const int j0 = static_cast<int>(static_cast<long long>(all) * part / p.nsplit);
@@ -76,7 +76,7 @@ __global__ void __launch_bounds__(kF32Threads) prefix_f32(const __grid_constant_
     const int t = i / kC, c = i % kC;
     float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
     if (m0 + t < p.queries) {
-      const int tq = (m0 + t) / p.group, s = seq_of_query(p, tq);
+      const int tq = (m0 + t) / p.group, s = seq_of_query(p, tq, s0, s1 + 1);
       const int64_t row = p.a.seq[s].row_base + p.a.seq[s].q_start + tq - p.q_before[s];
       v = __ldg(reinterpret_cast<const float4*>(p.a.q) +
                 (row * p.a.hq + g * p.group + (m0 + t) % p.group) * kC + c);
@@ -90,7 +90,7 @@ __global__ void __launch_bounds__(kF32Threads) prefix_f32(const __grid_constant_
     int r = 0;
     if (tid < kRows && m0 + tid < p.queries) {
       const int tq = (m0 + tid) / p.group;
-      seq = seq_of_query(p, tq);
+      seq = seq_of_query(p, tq, s0, s1 + 1);
       r = p.a.seq[seq].q_start + tq - p.q_before[seq];
     }
     __syncwarp();
@@ -240,7 +240,7 @@ __global__ void __launch_bounds__(kF32Threads) prefix_f32(const __grid_constant_
         stat[kRows] = st ? sum : -1.f;
       }
     } else if (st) {
-      const int tq = (m0 + t) / p.group, s = seq_of_query(p, tq);
+      const int tq = (m0 + t) / p.group, s = seq_of_query(p, tq, s0, s1 + 1);
       const int64_t row = (static_cast<int64_t>(p.a.seq[s].row_base) + p.a.seq[s].q_start + tq -
                            p.q_before[s]) * p.a.hq + g * p.group + (m0 + t) % p.group;
       float4* out = reinterpret_cast<float4*>(p.a.o) + row * kC;

@@ -3,15 +3,17 @@
 // of the group of exp(c <q, k_j> - lse). Validation, the bf16 kernel on the tensor cores, the fp32
 // kernel on CUDA cores, and the kernel that adds up the parts of a split.
 //
-// weights_tc: 128 keys of one key/value head stay in shared memory as the A operand; tiles of
-// up to 128 (row, head) queries pass by as B, so that an accumulator row is a key and a thread
-// adds up its key's exponentials along the row: no reduction across threads until the end, no
-// atomics, one order of addition. 19 warps:
-//   warps 0-15 exponentials and sums: warps q, q + 4, q + 8 and q + 12 share TMEM lane quarter q
-//              (keys 32q .. 32q + 31), each taking 32 of a tile's 128 queries;
-//   warp 16    TMA producer: the K tile, then Q through 4 stages;
-//   warp 17    TMEM allocator and issuer: S_j = K Q_j^T into a ring of four 128-column buffers;
-//   warp 18    the queries' normalisers through 4 stages.
+// weights_tc: 128 keys of one key/value head stay in TMEM as the A operand (their rows read straight
+// from global memory); tiles of up to 128 (row, head) queries pass by as B, so that an accumulator row
+// is a key and a thread adds up its key's exponentials along the row: no reduction across threads
+// until the end, no atomics, one order of addition. 19 warps:
+//   warps 0-15 exponentials and sums: eight warps take every other tile; of those, warps q and q + 4
+//              share TMEM lane quarter q (keys 32q .. 32q + 31), each taking 64 of the 128 queries;
+//   warp 16    TMA producer: Q through 6 stages (128-element heads: 192 KB);
+//   warp 17    TMEM allocator and issuer: S_j = K Q_j^T into a ring of three 128-column buffers;
+//   warp 18    the queries' normalisers through 6 stages.
+// TMEM: S ring [0, 384), K [448, 448 + D/2). Bound by the exponentials, one to each product of D
+// elements (for D = 128 the tensor cores need about as long).
 // Each tile's sum is formed on its own and then added to the key's total (two levels: the
 // rounding of a long sum grows with the number of tiles, not of queries).
 #include <algorithm>
@@ -50,12 +52,13 @@ __device__ __forceinline__ float with_earlier(const WeightsParams& p, int g, int
 
 // ---------------------------------------------------------------- bf16, tensor cores
 constexpr int kThreads = 608;
-constexpr int kQStages = 4, kSBufs = 4;
-constexpr int kWorkers = 16;
+constexpr int kQStages = 6, kSBufs = 3;
+constexpr int kWorkers = 8;  // warps of a tile
 constexpr int kWProd = 16, kWMma = 17, kWLse = 18;
+constexpr uint32_t kKCol = 448;  // TMEM columns of K
 
 struct __align__(16) Ctl {
-  uint64_t k_full;
+  uint64_t k_full;  // K is in TMEM
   uint64_t q_full[kQStages], q_empty[kQStages];
   uint64_t l_full[kQStages], l_empty[kQStages];
   uint64_t s_full[kSBufs], s_free[kSBufs];
@@ -69,7 +72,7 @@ struct __align__(16) Ctl {
 
 template <int D>
 constexpr size_t smem_bytes() {
-  return 1024 + (1 + kQStages) * static_cast<size_t>(kTN) * D * 2 + sizeof(Ctl);
+  return 1024 + kQStages * static_cast<size_t>(kTN) * D * 2 + sizeof(Ctl);
 }
 
 __device__ __forceinline__ void flag_timeout(const WeightsParams& p, Ctl& ctl) {
@@ -104,16 +107,14 @@ __device__ __forceinline__ float sum32(const uint32_t (&s)[32], const float* lse
 
 template <int D>
 __global__ void __launch_bounds__(kThreads, 1)
-    weights_tc(const __grid_constant__ WeightsParams p, const __grid_constant__ CUtensorMap tk,
-               const __grid_constant__ CUtensorMap tq) {
+    weights_tc(const __grid_constant__ WeightsParams p, const __grid_constant__ CUtensorMap tq) {
   constexpr int kSub = D / 64;
   constexpr uint32_t kKSub = kTN * 128;
   constexpr uint32_t kTile = kSub * kKSub;
   extern __shared__ uint8_t smem_raw[];
   uint8_t* base = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) &
                                              ~static_cast<uintptr_t>(1023));
-  uint8_t* sK = base;
-  uint8_t* sQ = sK + kTile;
+  uint8_t* sQ = base;
   Ctl& ctl = *reinterpret_cast<Ctl*>(sQ + kQStages * kTile);
   grid_dep_launch();
   const int item = blockIdx.x / p.nsplit, part = blockIdx.x % p.nsplit;
@@ -125,7 +126,7 @@ __global__ void __launch_bounds__(kThreads, 1)
   const int columns = p.box_heads * p.box_rows;  // queries of a tile, at most 128
 
   if (warp == kWProd && lane == 0) {
-    mbar_init(&ctl.k_full, 1);
+    mbar_init(&ctl.k_full, 16);
     mbar_init(&ctl.drained, 1);
     for (int b = 0; b < kQStages; ++b) {
       mbar_init(&ctl.q_full[b], 1);
@@ -144,6 +145,21 @@ __global__ void __launch_bounds__(kThreads, 1)
     tmem_alloc<kTmemCols>(&ctl.tmem_base);
     tmem_relinquish();
   }
+  uint32_t kreg[D / 8];  // workers: a quarter of key 32 (warp % 4) + lane's row
+  if (warp < 16) {
+    const int key = key0 + (warp & 3) * 32 + lane;
+    const uint4* src = reinterpret_cast<const uint4*>(
+        static_cast<const __nv_bfloat16*>(p.pk) + (key < p.prefix_len ? key * p.row_stride + g * p.head_stride : 0) +
+        (warp >> 2) * (D / 4));
+#pragma unroll
+    for (int c = 0; c < D / 32; ++c) {
+      const uint4 u = key < p.prefix_len ? __ldg(src + c) : make_uint4(0, 0, 0, 0);
+      kreg[4 * c] = u.x;
+      kreg[4 * c + 1] = u.y;
+      kreg[4 * c + 2] = u.z;
+      kreg[4 * c + 3] = u.w;
+    }
+  }
   // rows of the stages that no copy writes: zeros, whose scores (0) count for nothing with lse = +inf
   for (int i = columns * 8 + threadIdx.x; i < kTN * 8; i += kThreads)
     for (int b = 0; b < kQStages * kSub; ++b)
@@ -157,10 +173,6 @@ __global__ void __launch_bounds__(kThreads, 1)
   if (warp == kWProd) {
     // ------------------------------------------------------------ TMA producer
     if (lane == 0) {
-      mbar_arrive_expect_tx(&ctl.k_full, kTile);
-      const bool drop = p.test_drop_kv == 0;  // test hook: the K copy is never issued
-      if (!drop)
-        for (int s = 0; s < kSub; ++s) tma_load_3d(sK + s * kKSub, &tk, &ctl.k_full, s * 64, key0, g);
       int last = -1;
       for (int j = 0; j < n && !*abort_flag; ++j) {
         const int b = j % kQStages;
@@ -172,16 +184,17 @@ __global__ void __launch_bounds__(kThreads, 1)
         const int head = g * p.group + tile % p.head_blocks * p.box_heads;
         const int row = tile / p.head_blocks * p.box_rows;
         mbar_arrive_expect_tx(&ctl.q_full[b], kSub * columns * 128);
-        for (int s = 0; s < kSub; ++s)
-          tma_load_3d(sQ + b * kTile + s * kKSub, &tq, &ctl.q_full[b], s * 64, head, row);
+        if (j != p.test_drop_kv)  // (test hook: this copy is never issued)
+          for (int s = 0; s < kSub; ++s)
+            tma_load_3d(sQ + b * kTile + s * kKSub, &tq, &ctl.q_full[b], s * 64, head, row);
         last = j;
       }
       // every copy issued lands before shared memory is released: the latest use of each stage
       for (int b = 0; b < kQStages; ++b) {
         const int jb = last - ((last - b) % kQStages + kQStages) % kQStages;
-        if (last >= 0 && jb >= 0) mbar_wait(&ctl.q_full[b], (jb / kQStages) & 1, wlim);
+        if (last >= 0 && jb >= 0 && jb != p.test_drop_kv)
+          mbar_wait(&ctl.q_full[b], (jb / kQStages) & 1, wlim);
       }
-      if (!drop) mbar_wait(&ctl.k_full, 0, wlim);
     }
   } else if (warp == kWMma) {
     // ------------------------------------------------------------ issuer
@@ -190,7 +203,8 @@ __global__ void __launch_bounds__(kThreads, 1)
     // cycles, most of them the issue of its products)
     constexpr uint32_t kId = idesc_bf16_f32(kBM, kTN, 0, 0);
     const bool issue = elect_one();
-    const uint64_t da = smem_desc_sw128(smem_u32(sK), 16, 1024), dq = smem_desc_sw128(smem_u32(sQ), 16, 1024);
+    const uint64_t dq = smem_desc_sw128(smem_u32(sQ), 16, 1024);
+    const uint32_t tK = ctl.tmem_base + kKCol;
     bool ok = warp_wait(&ctl.k_full, 0, wlim);
     for (int j = 0; j < n && ok; ++j) {
       const int b = j % kQStages, sb = j % kSBufs;
@@ -201,10 +215,8 @@ __global__ void __launch_bounds__(kThreads, 1)
       if (issue) {
         const uint64_t db = dq + b * (kTile / 16);
 #pragma unroll
-        for (int ks = 0; ks < D / 16; ++ks) {
-          const uint64_t off = (ks >> 2) * (kKSub / 16) + (ks & 3) * 2;
-          mma_ss(ctl.tmem_base + sb * kTN, da + off, db + off, kId, ks > 0);
-        }
+        for (int ks = 0; ks < D / 16; ++ks)
+          mma_ts(ctl.tmem_base + sb * kTN, tK + ks * 8, db + (ks >> 2) * (kKSub / 16) + (ks & 3) * 2, kId, ks > 0);
         mma_commit(&ctl.s_full[sb]);
         mma_commit(&ctl.q_empty[b]);
       }
@@ -260,37 +272,57 @@ __global__ void __launch_bounds__(kThreads, 1)
     if (!ok && lane == 0) flag_timeout(p, ctl);
   } else {
     // ------------------------------------------------------------ exponentials and sums
-    const int quarter = warp & 3, col = warp >> 2;  // keys 32 quarter .., queries 32 col ..
+    const int quarter = warp & 3;
+    const int t = quarter * 32 + lane, key = key0 + t;
     const uint32_t lane_off = static_cast<uint32_t>(quarter * 32) << 16;
+    // a quarter of key t's row into TMEM (bf16 pairs, the A-operand layout)
+    const int part4 = warp >> 2;
+    tmem_store(ctl.tmem_base + kKCol + lane_off + part4 * (D / 8), kreg);
+    tmem_wait_st();
+    tc_fence_before();
+    __syncwarp();
+    if (lane == 0) mbar_arrive(&ctl.k_full);
+    const int turn = warp >> 3, half = (warp >> 2) & 1;  // tiles turn, turn + 2 ..; queries 64 half ..
     const uint64_t sl2 = f2_pack(p.scale_log2, p.scale_log2);
     float total = 0.f;
-    bool ok = true;
-    for (int j = 0; j < n && ok; ++j) {
-      const int b = j % kQStages, sb = j % kSBufs;
-      ok = !*abort_flag && mbar_wait(&ctl.l_full[b], (j / kQStages) & 1, wlim) &&
-           mbar_wait(&ctl.s_full[sb], (j / kSBufs) & 1, wlim);
-      if (!__all_sync(0xffffffffu, ok)) { ok = false; break; }
+    bool ok = true, ready = false;
+    int sb = turn;  // j % kSBufs, and the parity of its use
+    uint32_t sp = 0;
+    int b = turn;
+    uint32_t bp = 0;
+    for (int j = turn; j < n; j += 2) {
+      if (!__all_sync(0xffffffffu, ready)) {
+        ok = warp_wait(&ctl.l_full[b], bp, wlim) && warp_wait(&ctl.s_full[sb], sp, wlim);
+        if (!ok) break;
+      }
       tc_fence_after();
-      uint32_t r[32];
-      tmem_ld32(ctl.tmem_base + sb * kTN + 32 * col + lane_off, r);
+      uint32_t r0[32], r1[32];
+      tmem_ld32(ctl.tmem_base + sb * kTN + 64 * half + lane_off, r0);
+      tmem_ld32(ctl.tmem_base + sb * kTN + 64 * half + 32 + lane_off, r1);
       tmem_wait_ld();
       tc_fence_before();
       __syncwarp();
       if (lane == 0) mbar_arrive(&ctl.s_free[sb]);
-      const float* lse = ctl.lse[b] + 32 * col;
-      const uint32_t off = ctl.off[b][col];
-      if (32 * col < columns)  // (else no query)
-        total += off == 0 ? sum32<false>(r, lse, 0, sl2) : sum32<true>(r, lse, off, sl2);
+      const float* lse = ctl.lse[b] + 64 * half;
+      const uint32_t off0 = ctl.off[b][2 * half], off1 = ctl.off[b][2 * half + 1];
+      // the next tile's place in the rings, and whether it is there (asked ahead)
+      const int b_now = b;
+      if ((sb += 2) >= kSBufs) { sb -= kSBufs; sp ^= 1; }
+      if ((b += 2) >= kQStages) { b -= kQStages; bp ^= 1; }
+      ready = j + 2 < n && mbar_test(&ctl.l_full[b], bp) && mbar_test(&ctl.s_full[sb], sp);
+      float sum = 0.f;
+      if (64 * half < columns) sum = off0 == 0 ? sum32<false>(r0, lse, 0, sl2) : sum32<true>(r0, lse, off0, sl2);
+      if (64 * half + 32 < columns)
+        sum += off1 == 0 ? sum32<false>(r1, lse + 32, 0, sl2) : sum32<true>(r1, lse + 32, off1, sl2);
+      total += sum;
       __syncwarp();
-      if (lane == 0) mbar_arrive(&ctl.l_empty[b]);
+      if (lane == 0) mbar_arrive(&ctl.l_empty[b_now]);
     }
     const bool wok = __all_sync(0xffffffffu, ok);
     if (!wok && lane == 0) flag_timeout(p, ctl);
-    const int t = quarter * 32 + lane;
-    ctl.red[col][t] = total;
+    ctl.red[part4][t] = total;
     asm volatile("bar.sync 2, 512;" ::: "memory");  // the sixteen warps
-    const int key = key0 + t;
-    if (col == 0 && wok && key < p.prefix_len) {
+    if (part4 == 0 && wok && key < p.prefix_len) {
       total = (ctl.red[0][t] + ctl.red[1][t]) + (ctl.red[2][t] + ctl.red[3][t]);
       if (p.nsplit > 1)
         p.part[(static_cast<size_t>(part) * p.hkv + g) * p.prefix_len + key] = total;
@@ -433,15 +465,14 @@ constexpr long long kSplitCtas = 2048;   // CTAs of a split launch at most
 template <int D>
 cudaError_t launch_tc(const WeightsParams& p, cudaStream_t stream) {
   static std::atomic<uint64_t> done{0};
-  CUtensorMap k, q;
-  if (!make_map3(&k, p.pk, D, p.prefix_len, p.hkv, p.row_stride, p.head_stride, kTN, 1) ||
-      !make_map3(&q, p.q, D, p.hq, p.rows, D, static_cast<int64_t>(p.hq) * D, p.box_heads, p.box_rows))
+  CUtensorMap q;
+  if (!make_map3(&q, p.q, D, p.hq, p.rows, D, static_cast<int64_t>(p.hq) * D, p.box_heads, p.box_rows))
     return cudaErrorInvalidValue;
   const cudaError_t e = ensure_smem_attr(weights_tc<D>, smem_bytes<D>(), done);
   if (e != cudaSuccess) return e;
   const AttnLaunch L(static_cast<unsigned>(p.hkv) * p.key_tiles * p.nsplit, kThreads, smem_bytes<D>(),
                      stream, 1, false);
-  return cudaLaunchKernelEx(&L.cfg, weights_tc<D>, p, k, q);
+  return cudaLaunchKernelEx(&L.cfg, weights_tc<D>, p, q);
 }
 
 template <int D>
