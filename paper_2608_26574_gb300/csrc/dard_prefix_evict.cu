@@ -341,8 +341,8 @@ extern "C" dard_status dard_prefix_evict(const dard_prefix_evict_args* args, voi
     return report(DARD_ERR_CUDA, "prefix eviction launch failed: %s (DARD_TEST_FAIL_LAUNCH)",
                   cudaGetErrorString(cudaErrorLaunchFailure));
   const cudaStream_t stream = static_cast<cudaStream_t>(stream_ptr);
-  int ctas = 1;  // of a head: each about 4096 candidates or more
-  while (ctas < kMaxCluster && p.prefix_len / ctas > 8192) ctas *= 2;
+  int ctas = 1;  // of a head
+  while (ctas < kMaxCluster && p.prefix_len / ctas > 8192 && 2ll * ctas * p.hkv <= sm_count()) ctas *= 2;
   const AttnLaunch S(static_cast<unsigned>(p.hkv) * ctas, kSelThreads, 0, stream, ctas, false);
   cudaError_t e = cudaLaunchKernelEx(&S.cfg, evict_select, p, ctas);
   if (e == cudaSuccess && p.k) {

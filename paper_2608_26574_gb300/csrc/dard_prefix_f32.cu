@@ -9,6 +9,8 @@
 // share its maximum by shuffles, exchange the probabilities through shared memory within their
 // half-warp, and add up columns 4 tx .. (and 64 + 4 tx ..) of its output.
 // Bound: the fp32 FMA rate where the queries fill the tile; TR is chosen by their number.
+#include <cfloat>
+
 #include "dard_prefix.cuh"
 
 namespace dard {
@@ -172,8 +174,16 @@ __global__ void __launch_bounds__(kF32Threads) prefix_f32(const __grid_constant_
       }
     }
     cp_async_wait_group<1>();  // V_j
-    __syncthreads();
-    if (!own) {
+    bool bad = false;  // an own tile with values that are not finite
+    if (own) {
+#pragma unroll
+      for (int u = 0; u < kF32Keys * kC / kF32Threads; ++u) {  // (what this thread copied)
+        const float4 x = sV[tid + u * kF32Threads];
+        bad |= !(fabsf(x.x) <= FLT_MAX && fabsf(x.y) <= FLT_MAX && fabsf(x.z) <= FLT_MAX && fabsf(x.w) <= FLT_MAX);
+      }
+    }
+    if (own) bad = __syncthreads_or(bad); else __syncthreads();
+    if (!bad) {
 #pragma unroll 1
       for (int k = 0; k < kF32Keys; k += 4) {
         float4 vf[4][kV];
@@ -196,7 +206,7 @@ __global__ void __launch_bounds__(kF32Threads) prefix_f32(const __grid_constant_
             }
         }
       }
-    } else {  // a key that a query does not see is left out, whatever its value holds
+    } else {  // a key that a query does not see is left out (its weight is 0, its value may be NaN)
 #pragma unroll
       for (int u = 0; u < TR; ++u) {
         const uint64_t vis = sVis[ty + 16 * u];
