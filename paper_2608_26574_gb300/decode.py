@@ -19,6 +19,13 @@ This drives the library's two entry points the way a diffusion LLM would, step a
   optional one (``min_progress``) moves the most confident non-U position to U whenever a
   step adds no U position.
 
+* With ``shared`` (the tokens of a prefix that every prompt follows: a system prompt, a document)
+  ``decode`` runs the model over the prefix once, keeps its keys and values (``prefix.PrefixCache``),
+  and the steps run on the sequences' own rows only: ``dard_prefix_attention`` in every layer. The
+  prefix's rows do not see the sequences then. With ``keep`` the cache is cut down to that many keys
+  of each head after every block, by the attention weight they have received (``dard_prefix_weights``,
+  ``dard_prefix_evict``).
+
 Nothing here is on the measured hot path of ``bench.py``; it exists to run the path in its
 setting and to time whole steps (``python -m paper_2608_26574_gb300.decode``).
 """
@@ -35,6 +42,7 @@ import torch
 
 from . import binding as B
 from .experts import ExpertMLP
+from .prefix import PrefixCache
 
 
 @dataclass
@@ -74,7 +82,7 @@ class DLLM:
         d, hd = cfg.d_model, cfg.head_dim
         self.emb = w(cfg.vocab, d, fan_in=1)
         self.layers = []
-        # experts only: the layers' shared buffers and their status word
+        # the layers' shared buffers (experts only) and the status word of all but the batch's calls
         workspaces: dict = {}
         self.status = torch.zeros(1, dtype=torch.int32, device=self.device)
         self.norm = B.NormCall(d, self.dt) if cfg.experts > 0 else None
@@ -99,8 +107,37 @@ class DLLM:
         xf = x.float()
         return (xf * torch.rsqrt(xf.pow(2).mean(-1, keepdim=True) + 1e-6)).to(x.dtype)
 
-    def forward(self, batch: "Batch", need_attn_out: bool = False):
-        """Logits of the block rows: (logits_x [sum B_i, V], logits_s [sum B_i, V])."""
+    def rotate(self, x, pos):
+        """RoPE of x [rows, heads, head_dim] at positions pos [rows]: pairs (2i, 2i + 1), base
+        rope_base (what the attention does in its call where it rotates by itself)."""
+        half = x.shape[-1] // 2
+        f = self.cfg.rope_base ** (-torch.arange(half, device=x.device, dtype=torch.float64) / half)
+        angle = (pos.double()[:, None] * f).unsqueeze(1)
+        c, s = torch.cos(angle).float(), torch.sin(angle).float()
+        a, b = x.float().unflatten(-1, (half, 2)).unbind(-1)
+        return torch.stack([a * c - b * s, a * s + b * c], -1).flatten(-2).to(x.dtype)
+
+    def cache_prefix(self, tokens: np.ndarray, capacity: int = 0) -> PrefixCache:
+        """Runs the model over a prefix by itself and keeps its keys and values of every layer."""
+        cfg = self.cfg
+        cache = PrefixCache(cfg.n_layers, cfg.hq, cfg.hkv, cfg.head_dim, max(capacity, len(tokens)),
+                            self.dt, self.device, status=self.status)
+        n, zero = np.array([len(tokens)], np.int32), np.zeros(1, np.int32)
+        none = torch.zeros(1, dtype=torch.int32, device=self.device)
+        batch = Batch(tokens=torch.from_numpy(tokens.astype(np.int32)).to(self.device),
+                      pos=torch.arange(len(tokens), dtype=torch.int32, device=self.device), n_orig=n,
+                      block_start=zero, block_len=zero, shadow_len=zero, state=none.to(torch.uint8),
+                      prev_conf=none.float(), shadow_src=none, x_rows=none[:0].long(),
+                      s_rows=none[:0].long(), block_tok=none[:0], status=none)
+        self.forward(batch, fill=cache)
+        check_status(self, batch)
+        return cache
+
+    def forward(self, batch: "Batch", need_attn_out: bool = False, prefix: PrefixCache | None = None,
+                weigh: bool = False, fill: PrefixCache | None = None):
+        """Logits of the block rows: (logits_x [sum B_i, V], logits_s [sum B_i, V]). With ``prefix`` the
+        batch's rows follow the cached prefix (``weigh``: their attention weights are added to its
+        keys'); with ``fill`` the layers' keys and values are stored there."""
         cfg = self.cfg
         rows = batch.tokens.numel()
         h = self.emb[batch.tokens.long()]
@@ -108,13 +145,17 @@ class DLLM:
         # one step's mask metadata serves every layer: marshalled once. RoPE runs inside the
         # call (pairs (2i, 2i+1), base rope_base): q and k go in before RoPE, each row at its
         # position and each shadow row at the position it copies; k_rope receives the keys.
-        attention = B.AttentionCall(batch.n_orig, batch.block_start, batch.block_len,
-                                    batch.shadow_len, batch.state, batch.prev_conf,
-                                    batch.shadow_src, status=batch.status,
-                                    rope_theta=cfg.rope_base,
-                                    rope_style=B.DARD_ROPE_INTERLEAVED)
+        step = (batch.n_orig, batch.block_start, batch.block_len, batch.shadow_len, batch.state,
+                batch.prev_conf, batch.shadow_src)
+        if prefix is None:
+            attention = B.AttentionCall(*step, status=batch.status, rope_theta=cfg.rope_base,
+                                        rope_style=B.DARD_ROPE_INTERLEAVED)
+        else:
+            attention = prefix.attention(*step)
+            pos = batch.pos + prefix.start
+            lse = torch.empty(rows, cfg.hq, device=self.device) if weigh else None
         delta = None  # experts only: the last MLP's output, not yet added to h
-        for L in self.layers:
+        for i, L in enumerate(self.layers):
             if cfg.experts > 0:
                 a = torch.empty_like(h)
                 self.norm(h, delta, residual=h if delta is not None else None, y=a)
@@ -124,8 +165,16 @@ class DLLM:
             k = (a @ L["wk"]).view(rows, cfg.hkv, cfg.head_dim).contiguous()
             v = (a @ L["wv"]).view(rows, cfg.hkv, cfg.head_dim).contiguous()
             o = torch.empty_like(q)
-            k_rope = torch.empty_like(k)
-            attention(q, k, v, o, k_rope=k_rope)
+            if prefix is None:
+                k_rope = torch.empty_like(k)
+                attention(q, k, v, o, k_rope=k_rope)
+            else:
+                q, k = self.rotate(q, pos), self.rotate(k, pos)
+                prefix.attend(attention, i, q, k, v, o, lse=lse)
+                if weigh:
+                    prefix.accumulate(i, q, lse)
+            if fill is not None:
+                fill.store(i, k_rope, v)
             if need_attn_out:
                 attn_outs.append((q, k, v, o))
             if cfg.experts > 0:
@@ -222,11 +271,12 @@ class StepRecord:
 
 
 def step(model: DLLM, batch: Batch, thr: tuple[float, float], lam: float, p0: float,
-         order_mode: int, workspace, outs: dict, min_progress: bool, keep_logits=False):
+         order_mode: int, workspace, outs: dict, min_progress: bool, keep_logits=False,
+         prefix: PrefixCache | None = None, weigh: bool = False):
     """One step of Algorithm 1 for the current block of every sequence, on the device."""
     cfg = model.cfg
     batch.block_tok.copy_(batch.tokens[batch.x_rows])
-    lx, ls = model.forward(batch)
+    lx, ls = model.forward(batch, prefix=prefix, weigh=weigh)
     state_before = batch.state.clone() if keep_logits else None
     n, blen = len(batch.n_orig), int(batch.block_len[0])
     u_before = (batch.state.view(n, blen) == 2).sum(1) if min_progress else None
@@ -253,7 +303,7 @@ def step(model: DLLM, batch: Batch, thr: tuple[float, float], lam: float, p0: fl
 
 def check_status(model: DLLM, batch: Batch) -> None:
     """Raises when a step left outputs behind that are none: a wait that ran out in the attention,
-    the scoring or the experts, or a row that the experts' router could not place (a NaN or +inf
+    the scoring, the experts or the prefix cache's calls, or a row that the experts' router could not place (a NaN or +inf
     logit). (The scoring's own marks on rows, which have defined outputs, are the caller's to
     read in ``batch.status``.)"""
     experts, rest = torch.cat([model.status, batch.status]).tolist()
@@ -266,12 +316,20 @@ def check_status(model: DLLM, batch: Batch) -> None:
 
 def decode(model: DLLM, prompts: list[np.ndarray], gen_len: int, block_len: int,
            thr=(0.5, 0.8), lam=0.5 ** (1 / 8), p0=0.1, order_mode: int = B.ORDER_CONFIDENCE,
-           max_steps: int = 64, min_progress: bool = False, record: bool = False):
-    """Algorithm 1 block by block. Returns (generated tokens [n, gen_len], per-block steps,
+           max_steps: int = 64, min_progress: bool = False, record: bool = False,
+           shared: np.ndarray | None = None, keep: int = 0, keep_ends: tuple[int, int] = (4, 32)):
+    """Algorithm 1 block by block. ``shared``: tokens that every prompt follows, cached once;
+    ``keep``: the cache's keys per head after each block (0: all), ``keep_ends`` of them the first and
+    the last ones. Returns (generated tokens [n, gen_len], per-block steps,
     per-step GPU microseconds, step records if ``record``). Raises after a step whose status
     words report a failure (``check_status``)."""
     dev = model.device
     model.status.zero_()
+    if keep and shared is None:
+        raise ValueError("keep needs a shared prefix")
+    if keep and sum(keep_ends) > keep:
+        raise ValueError(f"keep {keep} with ends {keep_ends}")
+    prefix = model.cache_prefix(np.asarray(shared)) if shared is not None and len(shared) else None
     n = len(prompts)
     gen = [np.full(gen_len, model.cfg.mask_token, np.int32) for _ in range(n)]
     nB = n * block_len
@@ -292,7 +350,7 @@ def decode(model: DLLM, prompts: list[np.ndarray], gen_len: int, block_len: int,
                           batch.tokens[batch.x_rows].cpu().numpy())
             e0.record()
             res = step(model, batch, thr, lam, p0, order_mode, ws, outs, min_progress,
-                       keep_logits=record)
+                       keep_logits=record, prefix=prefix, weigh=keep > 0)
             e1.record()
             counts = outs["counts"].cpu().numpy()  # synchronises
             check_status(model, batch)
@@ -310,6 +368,8 @@ def decode(model: DLLM, prompts: list[np.ndarray], gen_len: int, block_len: int,
             if (st == 2).all():
                 break
         steps_per_block.append(done)
+        if prefix is not None and keep:
+            prefix.evict(keep, *keep_ends)
         blk_tok = batch.tokens[batch.x_rows].cpu().numpy().reshape(n, block_len)
         for i in range(n):
             gen[i][blk * block_len:(blk + 1) * block_len] = blk_tok[i]
@@ -320,6 +380,10 @@ def main():
     ap = argparse.ArgumentParser(description="DARD multi-step decoding on a random-weight model")
     ap.add_argument("--seqs", type=int, default=4)
     ap.add_argument("--prompt", type=int, default=512)
+    ap.add_argument("--shared", type=int, default=0,
+                    help="tokens of a prefix that every prompt follows, cached once")
+    ap.add_argument("--keep", type=int, default=0,
+                    help="keys of the cached prefix kept per head after each block (0: all)")
     ap.add_argument("--gen", type=int, default=128)
     ap.add_argument("--block", type=int, default=32)
     ap.add_argument("--layers", type=int, default=4)
@@ -349,10 +413,11 @@ def main():
     rng = np.random.default_rng(args.seed)
     prompts = [rng.integers(0, cfg.vocab - 1, size=args.prompt).astype(np.int32)
                for _ in range(args.seqs)]
+    shared = rng.integers(0, cfg.vocab - 1, size=args.shared).astype(np.int32) if args.shared else None
     t0 = time.perf_counter()
     _, steps, us, _ = decode(model, prompts, args.gen, args.block, thr=tuple(args.tau),
                              order_mode=args.order, max_steps=args.max_steps,
-                             min_progress=args.min_progress)
+                             min_progress=args.min_progress, shared=shared, keep=args.keep)
     wall = time.perf_counter() - t0
     warm = us[1:] if len(us) > 1 else us
     print(json.dumps({"steps_per_block": steps, "steps": len(us),
