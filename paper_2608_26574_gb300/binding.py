@@ -810,13 +810,21 @@ def dard_experts(x, x_scale, w1, w1_scale, w3, w3_scale, w2, w2_scale, ids, weig
 
 
 # ------------------------------------------------------------------ decoding behind a shared prefix
+_current_device = None
+
+
 def _launch(fn, name: str, args, stream, device: int):
     """Calls the library on ``device``, the current one or another."""
-    torch = _torch()
-    if torch.cuda.current_device() != device:
-        with torch.cuda.device(device):
-            return _check(fn(args, _stream_handle(stream, device)), name)
-    _check(fn(args, _stream_handle(stream, device)), name)
+    global _current_device
+    if _current_device is None:
+        _current_device = _torch().cuda.current_device
+    if _current_device() != device:
+        with _torch().cuda.device(device):
+            code = fn(args, _stream_handle(stream, device))
+    else:
+        code = fn(args, _raw_stream(device) if stream is None else _stream_handle(stream, device))
+    if code:
+        _check(code, name)
 
 
 def _cache(t, name: str, device: int, dtype, hkv: int, head_dim: int) -> tuple[int, int, int]:
@@ -842,7 +850,15 @@ def _cache(t, name: str, device: int, dtype, hkv: int, head_dim: int) -> tuple[i
 
 
 def _caches(k, v, names: tuple, device: int, dtype, hkv: int, head_dim: int):
-    """(k's pointer, v's, row stride, head stride) of a layer's keys and values."""
+    """(k's pointer, v's, row stride, head stride) of a layer's keys and values. (One pass of cheap
+    comparisons; what is unusual or wrong is looked at only when one fails.)"""
+    shape, strides = k.shape, k.stride()
+    if (len(shape) == 3 and v.shape == shape and v.stride() == strides and k.dtype == dtype == v.dtype
+            and k.get_device() == device == v.get_device() and device >= 0):
+        n, heads, d = shape
+        rs, hs, es = strides
+        if heads == hkv and d == head_dim and es == 1 and rs >= d and hs >= d and n > 1 and heads > 1:
+            return k.data_ptr(), v.data_ptr(), rs, hs
     kp, rs, hs = _cache(k, names[0], device, dtype, hkv, head_dim)
     vp, rv, hv = _cache(v, names[1], device, dtype, hkv, head_dim)
     if k.shape[0] != v.shape[0] or rs != rv or hs != hv:
@@ -905,8 +921,30 @@ class PrefixAttentionCall:
         self._fn = _packed_fn("dard_prefix_attention")
 
     def __call__(self, q, k, v, o, prefix_k, prefix_v, lse=None, stream=None):
+        qs, ks, dt, dev, rows = q.shape, k.shape, q.dtype, q.get_device(), self.rows
+        if not (len(qs) == 3 == len(ks) and o.shape == qs and v.shape == ks and ks[2] == qs[2]
+                and qs[0] >= rows and ks[0] >= rows and dev >= 0
+                and (dev == self.device or self.device is None)
+                and k.dtype == dt and v.dtype == dt and o.dtype == dt and k.get_device() == dev
+                and v.get_device() == dev and o.get_device() == dev and q.is_contiguous()
+                and k.is_contiguous() and v.is_contiguous() and o.is_contiguous()):
+            self._refuse(q, k, v, o)
+        hq, d = qs[1], qs[2]
+        kp, vp, rs, hs = _caches(prefix_k, prefix_v, ("prefix_k", "prefix_v"), dev, dt, ks[1], d)
+        lp = 0
+        if lse is not None:
+            if lse.dim() != 2 or lse.shape[0] < rows or lse.shape[1] != hq:
+                raise ValueError(f"lse: [>={rows}, {hq}] expected, got {tuple(lse.shape)}")
+            lp = _flat(lse, "lse", _dtypes("f32"), dev)
+        args = self.layout.pack(q.data_ptr(), k.data_ptr(), v.data_ptr(), o.data_ptr(),
+                                _dtype_code(q), hq, ks[1], d, *self._mid, kp, vp, rs, hs,
+                                prefix_k.shape[0], lp, *self._scratch)
+        _launch(self._fn, "dard_prefix_attention", args, stream, dev)
+
+    def _refuse(self, q, k, v, o):
+        """What is wrong with a call's own rows."""
         qs, ks, dt, dev = q.shape, k.shape, q.dtype, q.get_device()
-        if not (len(qs) == 3 and len(ks) == 3 and o.shape == qs and v.shape == ks and ks[2] == qs[2]
+        if not (len(qs) == 3 == len(ks) and o.shape == qs and v.shape == ks and ks[2] == qs[2]
                 and qs[0] >= self.rows and ks[0] >= self.rows):
             raise ValueError(f"q/o [>={self.rows}, hq, d] and k/v [>={self.rows}, hkv, d] expected, got "
                              f"{tuple(qs)}, {tuple(ks)}, {tuple(v.shape)}, {tuple(o.shape)}")
@@ -915,16 +953,7 @@ class PrefixAttentionCall:
         for name, t in (("q", q), ("k", k), ("v", v), ("o", o)):
             if t.dtype != dt or t.get_device() != dev or not t.is_contiguous():
                 raise ValueError(f"{name}: contiguous {dt} tensor on device {dev} expected")
-        kp, vp, rs, hs = _caches(prefix_k, prefix_v, ("prefix_k", "prefix_v"), dev, dt, ks[1], ks[2])
-        lp = 0
-        if lse is not None:
-            if lse.dim() != 2 or lse.shape[0] < self.rows or lse.shape[1] != qs[1]:
-                raise ValueError(f"lse: [>={self.rows}, {qs[1]}] expected, got {tuple(lse.shape)}")
-            lp = _flat(lse, "lse", _dtypes("f32"), dev)
-        args = self.layout.pack(q.data_ptr(), k.data_ptr(), v.data_ptr(), o.data_ptr(),
-                                _dtype_code(q), qs[1], ks[1], qs[2], *self._mid, kp, vp, rs, hs,
-                                prefix_k.shape[0], lp, *self._scratch)
-        _launch(self._fn, "dard_prefix_attention", args, stream, dev)
+        raise ValueError("q, k, v and o do not fit")
 
 
 def dard_prefix_attention(q, k, v, o, prefix_k, prefix_v, n_orig, block_start, block_len, shadow_len,
@@ -972,9 +1001,10 @@ class PrefixWeightsCall:
         if lse.shape != (rows, hq):
             raise ValueError(f"lse: [{rows}, {hq}] expected, got {tuple(lse.shape)}")
         lp = _flat(lse, "lse", _dtypes("f32"), dev)
-        if prefix_k.dim() != 3:
-            raise ValueError(f"prefix_k: [rows, hkv, {d}] expected, got {tuple(prefix_k.shape)}")
-        hkv, length = prefix_k.shape[1], prefix_k.shape[0]
+        ps = prefix_k.shape
+        if len(ps) != 3:
+            raise ValueError(f"prefix_k: [rows, hkv, {d}] expected, got {tuple(ps)}")
+        length, hkv = ps[0], ps[1]
         kp, rs, hs = _cache(prefix_k, "prefix_k", dev, q.dtype, hkv, d)
         wp, wstride = _rows2(weights, "weights", (hkv, length), _dtypes("f32"), dev)
         ip, istride = (_rows2(weights_in, "weights_in", (hkv, length), _dtypes("f32"), dev)

@@ -31,12 +31,20 @@ struct PrefixParams {
   uint8_t tile_seq[kTileTable][2];      // first and last sequence of a query tile, if all fit in
 };
 
-// Parts of a split launch: one slot per (tile, part), rows x (D + 2) floats: the unnormalised
-// output rows, then per row the reference maximum (times scale log2 e; -inf: no key) and the sum of
-// the weights (-1 in a tile's last part: a row that is not stored).
+// Parts of a split launch: one slot per (tile, part), rows x (D + 4) floats: the unnormalised
+// output rows, then per row the reference maximum (times scale log2 e; -inf: no key), the sum of
+// the weights, and (8 bytes; the tile's last part counts) the output row, -1 for none.
 __host__ __device__ inline size_t part_slot_floats(int rows, int d) {
-  return static_cast<size_t>(rows) * (d + 2);
+  return static_cast<size_t>(rows) * (d + 4);
 }
+
+struct JoinParams {
+  const float* part;
+  void* o;
+  float* lse;
+  int64_t rows;               // packed queries of all key/value heads
+  int32_t queries, tiles, nsplit, tile_rows;
+};
 
 // The fp32 kernel on CUDA cores.
 int prefix_f32_rows(const PrefixParams& p, int sms);  // packed queries per CTA

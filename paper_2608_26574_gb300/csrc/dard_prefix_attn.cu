@@ -448,7 +448,8 @@ __global__ void __launch_bounds__(kThreads, 1)
       if (part4 == 0) {
         float* stat = slot + kBM * D;
         stat[t] = m_run == -INFINITY ? -INFINITY : m_run * sl;
-        stat[kBM + t] = wok && ctl.out_row[t] >= 0 ? l : -1.f;
+        stat[kBM + t] = l;
+        reinterpret_cast<int64_t*>(stat + 2 * kBM)[t] = wok ? ctl.out_row[t] : -1;
       }
     } else {
       // O row / row sum -> bf16 into shared memory (the K stages are no longer read once o_full
@@ -499,23 +500,20 @@ __global__ void __launch_bounds__(kThreads, 1)
 // o = sum_c 2^(m_c - M) O_c / sum_c 2^(m_c - M) l_c. kWarps warps share a query's parts, 32 at a time:
 // a lane takes a part's factor and sum, then all take the parts' rows, coalesced.
 template <typename T, int D, int kWarps>
-__global__ void __launch_bounds__(128, 6) prefix_join(const __grid_constant__ PrefixParams p,
-                                                   int tile_rows) {
+__global__ void __launch_bounds__(128, 6) prefix_join(const __grid_constant__ JoinParams p) {
   constexpr int kV = D / 32;  // elements per lane
   __shared__ float s_o[4][D], s_top[4], s_l[4];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, sub = warp % kWarps;
   const long long w = (static_cast<long long>(blockIdx.x) * 4 + warp) / kWarps;
-  const bool in = w < static_cast<long long>(p.queries) * p.a.hkv;
+  const bool in = w < p.rows;
   const int g = in ? static_cast<int>(w / p.queries) : 0, m = in ? static_cast<int>(w % p.queries) : 0;
-  const int t = m % tile_rows;
-  const size_t floats = part_slot_floats(tile_rows, D);
-  const float* slot = p.part + (static_cast<size_t>(g) * p.tiles + m / tile_rows) * p.nsplit * floats;
-  const float* stat = slot + tile_rows * D + t;
-  const int tq = m / p.group, seq = seq_of_query(p, tq);
-  const size_t row = static_cast<size_t>(p.a.seq[seq].row_base + p.a.seq[seq].q_start + tq -
-                                         p.q_before[seq]) * p.a.hq + g * p.group + m % p.group;
+  const int t = m % p.tile_rows;
+  const size_t floats = part_slot_floats(p.tile_rows, D);
+  const float* slot = p.part + (static_cast<size_t>(g) * p.tiles + m / p.tile_rows) * p.nsplit * floats;
+  const float* stat = slot + p.tile_rows * D + t;
   grid_dep_wait();
-  const bool stored = stat[(p.nsplit - 1) * floats + tile_rows] != -1.f;  // (its last part decides)
+  const int64_t row = reinterpret_cast<const int64_t*>(slot + (p.nsplit - 1) * floats +
+                                                       p.tile_rows * (D + 2))[t];
   float top = -INFINITY, l = 0.f, o[kV];
 #pragma unroll
   for (int e = 0; e < kV; ++e) o[e] = 0.f;
@@ -523,7 +521,7 @@ __global__ void __launch_bounds__(128, 6) prefix_join(const __grid_constant__ Pr
   for (int c = c0; c < c1; c += 32) {
     const int n = min(32, c1 - c);
     const float mc = lane < n ? stat[(c + lane) * floats] : -INFINITY;
-    const float lc = lane < n ? stat[(c + lane) * floats + tile_rows] : 0.f;
+    const float lc = lane < n ? stat[(c + lane) * floats + p.tile_rows] : 0.f;
     float most = fmaxf(top, mc);
 #pragma unroll
     for (int x = 16; x > 0; x >>= 1) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, x));
@@ -579,8 +577,8 @@ __global__ void __launch_bounds__(128, 6) prefix_join(const __grid_constant__ Pr
     }
     top = most;
   }
-  if (!in || !stored) return;
-  T* out = static_cast<T*>(p.a.o) + row * D + lane * kV;
+  if (!in || row < 0) return;
+  T* out = static_cast<T*>(p.o) + row * D + lane * kV;
   const float inv = 1.0f / l;
 #pragma unroll
   for (int e = 0; e < kV; e += 2) {
@@ -639,18 +637,19 @@ cudaError_t launch_tc(const PrefixParams& p, cudaStream_t stream) {
 }
 
 template <typename T, int D>
-cudaError_t launch_join_d(const PrefixParams& p, int rows, cudaStream_t stream) {
-  const long long queries = static_cast<long long>(p.queries) * p.a.hkv;
-  if (p.nsplit > 8) {  // four warps to a query: its parts' rows are in flight together
-    const AttnLaunch L(static_cast<unsigned>(queries), 128, 0, stream, 1, true);
-    return cudaLaunchKernelEx(&L.cfg, prefix_join<T, D, 4>, p, rows);
+cudaError_t launch_join_d(const JoinParams& j, cudaStream_t stream) {
+  if (j.nsplit > 8) {  // four warps to a query: its parts' rows are in flight together
+    const AttnLaunch L(static_cast<unsigned>(j.rows), 128, 0, stream, 1, true);
+    return cudaLaunchKernelEx(&L.cfg, prefix_join<T, D, 4>, j);
   }
-  const AttnLaunch L(static_cast<unsigned>((queries + 3) / 4), 128, 0, stream, 1, true);
-  return cudaLaunchKernelEx(&L.cfg, prefix_join<T, D, 1>, p, rows);
+  const AttnLaunch L(static_cast<unsigned>((j.rows + 3) / 4), 128, 0, stream, 1, true);
+  return cudaLaunchKernelEx(&L.cfg, prefix_join<T, D, 1>, j);
 }
 template <typename T>
 cudaError_t launch_join(const PrefixParams& p, int rows, cudaStream_t stream) {
-  return p.a.head_dim == 64 ? launch_join_d<T, 64>(p, rows, stream) : launch_join_d<T, 128>(p, rows, stream);
+  const JoinParams j{p.part, p.a.o, p.lse, static_cast<int64_t>(p.queries) * p.a.hkv,
+                     p.queries, p.tiles, p.nsplit, rows};
+  return p.a.head_dim == 64 ? launch_join_d<T, 64>(j, stream) : launch_join_d<T, 128>(j, stream);
 }
 
 dard_status prepare(const dard_prefix_attn_args* args, PrefixParams& p) {

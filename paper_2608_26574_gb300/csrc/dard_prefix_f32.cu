@@ -238,7 +238,10 @@ __global__ void __launch_bounds__(kF32Threads) prefix_f32(const __grid_constant_
 #pragma unroll
     for (int x = 8; x > 0; x >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, x);
     if (m0 + t >= p.queries) continue;
-    const bool st = sVis[t] != 0;
+    const int tq = (m0 + t) / p.group, s = seq_of_query(p, tq, s0, s1 + 1);
+    const int64_t row = sVis[t] == 0 ? -1
+                            : (static_cast<int64_t>(p.a.seq[s].row_base) + p.a.seq[s].q_start + tq -
+                               p.q_before[s]) * p.a.hq + g * p.group + (m0 + t) % p.group;
     if (p.nsplit > 1) {
       float* slot = p.part + blockIdx.x * part_slot_floats(kRows, D);
 #pragma unroll
@@ -247,12 +250,10 @@ __global__ void __launch_bounds__(kF32Threads) prefix_f32(const __grid_constant_
       if (tx == 0) {
         float* stat = slot + kRows * D + t;
         stat[0] = m[u];
-        stat[kRows] = st ? sum : -1.f;
+        stat[kRows] = sum;
+        reinterpret_cast<int64_t*>(slot + kRows * (D + 2))[t] = row;
       }
-    } else if (st) {
-      const int tq = (m0 + t) / p.group, s = seq_of_query(p, tq, s0, s1 + 1);
-      const int64_t row = (static_cast<int64_t>(p.a.seq[s].row_base) + p.a.seq[s].q_start + tq -
-                           p.q_before[s]) * p.a.hq + g * p.group + (m0 + t) % p.group;
+    } else if (row >= 0) {
       float4* out = reinterpret_cast<float4*>(p.a.o) + row * kC;
       const float inv = 1.0f / sum;
 #pragma unroll

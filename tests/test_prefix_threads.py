@@ -42,7 +42,7 @@ def _evict():
 def test_calls_shared_by_threads(make, monkeypatch):
     BUILD.build()
     B.lib()
-    monkeypatch.setattr(torch.cuda, "current_device", lambda: 0)
+    monkeypatch.setattr(B, "_current_device", lambda: 0)
     monkeypatch.setattr(B, "_raw_stream", lambda i: 0)
     call, struct, args, fields = make()
     seen, wrong = [], []
@@ -91,7 +91,7 @@ def test_launch_on_another_device(monkeypatch):
 
     BUILD.build()
     B.lib()
-    monkeypatch.setattr(torch.cuda, "current_device", lambda: 1)
+    monkeypatch.setattr(B, "_current_device", lambda: 1)
     monkeypatch.setattr(torch.cuda, "device", Guard)
     monkeypatch.setattr(B, "_raw_stream", lambda i: 100 + i)
     calls = []
