@@ -6,12 +6,13 @@
 // weights_tc: 128 keys of one key/value head stay in TMEM as the A operand (their rows read straight
 // from global memory); tiles of up to 128 (row, head) queries pass by as B, so that an accumulator row
 // is a key and a thread adds up its key's exponentials along the row: no reduction across threads
-// until the end, no atomics, one order of addition. 19 warps:
-//   warps 0-15 exponentials and sums: eight warps take every other tile; of those, warps q and q + 4
-//              share TMEM lane quarter q (keys 32q .. 32q + 31), each taking 64 of the 128 queries;
-//   warp 16    TMA producer: Q through 6 stages (128-element heads: 192 KB);
-//   warp 17    TMEM allocator and issuer: S_j = K Q_j^T into a ring of three 128-column buffers;
-//   warp 18    the queries' normalisers through 6 stages.
+// until the end, no atomics, one order of addition. 27 warps:
+//   warps 0-23 exponentials and sums: groups of eight warps take every third tile; of a group, warps q
+//              and q + 4 share TMEM lane quarter q (keys 32q .. 32q + 31), each taking 64 of the 128
+//              queries;
+//   warp 24    TMA producer: Q through 6 stages (128-element heads: 192 KB);
+//   warp 25    TMEM allocator and issuer: S_j = K Q_j^T into a buffer of 128 columns for each group;
+//   warp 26    the queries' normalisers through 6 stages.
 // TMEM: S ring [0, 384), K [448, 448 + D/2). Bound by the exponentials, one to each product of D
 // elements (for D = 128 the tensor cores need about as long).
 // Each tile's sum is formed on its own and then added to the key's total (two levels: the
@@ -51,10 +52,12 @@ __device__ __forceinline__ float with_earlier(const WeightsParams& p, int g, int
 }
 
 // ---------------------------------------------------------------- bf16, tensor cores
-constexpr int kThreads = 608;
-constexpr int kQStages = 6, kSBufs = 3;
+constexpr int kThreads = 864;
+constexpr int kGroups = 3;
+constexpr int kQStages = 6, kSBufs = kGroups;
+static_assert(kQStages % kGroups == 0, "a group's tiles come back to the stages that it used");
 constexpr int kWorkers = 8;  // warps of a tile
-constexpr int kWProd = 16, kWMma = 17, kWLse = 18;
+constexpr int kWProd = 24, kWMma = 25, kWLse = 26;
 constexpr uint32_t kKCol = 448;  // TMEM columns of K
 
 struct __align__(16) Ctl {
@@ -67,7 +70,7 @@ struct __align__(16) Ctl {
   int32_t abort;
   __align__(16) float lse[kQStages][kBM];  // times -log2 e (read four at a time)
   uint32_t off[kQStages][4];      // queries that add nothing (bit per column)
-  float red[4][kBM];
+  float red[2 * kGroups][kBM];
 };
 
 template <int D>
@@ -162,7 +165,7 @@ __global__ void __launch_bounds__(kThreads, 1)
   }
   // rows of the stages that no copy writes: zeros, whose scores (0) count for nothing with lse = +inf
   for (int i = columns * 8 + threadIdx.x; i < kTN * 8; i += kThreads)
-    for (int b = 0; b < kQStages * kSub; ++b)
+    for (int b = 0; b < min(n, kQStages) * kSub; ++b)
       *reinterpret_cast<uint4*>(sQ + b * kKSub + 16 * i) = make_uint4(0, 0, 0, 0);
   fence_proxy_async_smem();
   tc_fence_before();
@@ -275,57 +278,64 @@ __global__ void __launch_bounds__(kThreads, 1)
     const int quarter = warp & 3;
     const int t = quarter * 32 + lane, key = key0 + t;
     const uint32_t lane_off = static_cast<uint32_t>(quarter * 32) << 16;
-    // a quarter of key t's row into TMEM (bf16 pairs, the A-operand layout)
-    const int part4 = warp >> 2;
-    tmem_store(ctl.tmem_base + kKCol + lane_off + part4 * (D / 8), kreg);
-    tmem_wait_st();
-    tc_fence_before();
-    __syncwarp();
-    if (lane == 0) mbar_arrive(&ctl.k_full);
-    const int turn = warp >> 3, half = (warp >> 2) & 1;  // tiles turn, turn + 2 ..; queries 64 half ..
+    // the first sixteen warps: a quarter of key t's row into TMEM (bf16 pairs, the A-operand layout)
+    const int part = warp >> 2;
+    if (warp < 16) {
+      tmem_store(ctl.tmem_base + kKCol + lane_off + part * (D / 8), kreg);
+      tmem_wait_st();
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&ctl.k_full);
+    }
+    const int turn = warp >> 3, half = part & 1;  // tiles turn, turn + 3 ..; queries 64 half ..
+    const uint32_t tS = ctl.tmem_base + turn * kTN + 64 * half + lane_off;
     const uint64_t sl2 = f2_pack(p.scale_log2, p.scale_log2);
     float total = 0.f;
     bool ok = true, ready = false;
-    int sb = turn;  // j % kSBufs, and the parity of its use
-    uint32_t sp = 0;
-    int b = turn;
-    uint32_t bp = 0;
-    for (int j = turn; j < n; j += 2) {
+    int b = turn;  // stage of the tile, and the parity of its use
+    uint32_t bp = 0, sp = 0;
+    for (int j = turn; j < n; j += kGroups) {
       if (!__all_sync(0xffffffffu, ready)) {
-        ok = warp_wait(&ctl.l_full[b], bp, wlim) && warp_wait(&ctl.s_full[sb], sp, wlim);
+        ok = warp_wait(&ctl.l_full[b], bp, wlim) && warp_wait(&ctl.s_full[turn], sp, wlim);
         if (!ok) break;
       }
       tc_fence_after();
-      uint32_t r0[32], r1[32];
-      tmem_ld32(ctl.tmem_base + sb * kTN + 64 * half + lane_off, r0);
-      tmem_ld32(ctl.tmem_base + sb * kTN + 64 * half + 32 + lane_off, r1);
+      const float* lse = ctl.lse[b] + 64 * half;
+      const uint32_t off0 = ctl.off[b][2 * half], off1 = ctl.off[b][2 * half + 1];
+      uint32_t r[32];
+      tmem_ld32(tS, r);
+      tmem_wait_ld();
+      float sum = 0.f;
+      if (64 * half < columns) sum = off0 == 0 ? sum32<false>(r, lse, 0, sl2) : sum32<true>(r, lse, off0, sl2);
+      tmem_ld32(tS + 32, r);
       tmem_wait_ld();
       tc_fence_before();
       __syncwarp();
-      if (lane == 0) mbar_arrive(&ctl.s_free[sb]);
-      const float* lse = ctl.lse[b] + 64 * half;
-      const uint32_t off0 = ctl.off[b][2 * half], off1 = ctl.off[b][2 * half + 1];
-      // the next tile's place in the rings, and whether it is there (asked ahead)
-      const int b_now = b;
-      if ((sb += 2) >= kSBufs) { sb -= kSBufs; sp ^= 1; }
-      if ((b += 2) >= kQStages) { b -= kQStages; bp ^= 1; }
-      ready = j + 2 < n && mbar_test(&ctl.l_full[b], bp) && mbar_test(&ctl.s_full[sb], sp);
-      float sum = 0.f;
-      if (64 * half < columns) sum = off0 == 0 ? sum32<false>(r0, lse, 0, sl2) : sum32<true>(r0, lse, off0, sl2);
+      if (lane == 0) mbar_arrive(&ctl.s_free[turn]);
       if (64 * half + 32 < columns)
-        sum += off1 == 0 ? sum32<false>(r1, lse + 32, 0, sl2) : sum32<true>(r1, lse + 32, off1, sl2);
+        sum += off1 == 0 ? sum32<false>(r, lse + 32, 0, sl2) : sum32<true>(r, lse + 32, off1, sl2);
+      // the next tile's stage, and whether it is there (asked ahead)
+      const int b_now = b;
+      if ((b += kGroups) >= kQStages) {
+        b -= kQStages;
+        bp ^= 1;
+      }
+      sp ^= 1;
+      ready = j + kGroups < n && mbar_test(&ctl.l_full[b], bp) && mbar_test(&ctl.s_full[turn], sp);
       total += sum;
       __syncwarp();
       if (lane == 0) mbar_arrive(&ctl.l_empty[b_now]);
     }
     const bool wok = __all_sync(0xffffffffu, ok);
     if (!wok && lane == 0) flag_timeout(p, ctl);
-    ctl.red[part4][t] = total;
-    asm volatile("bar.sync 2, 512;" ::: "memory");  // the sixteen warps
-    if (part4 == 0 && wok && key < p.prefix_len) {
-      total = (ctl.red[0][t] + ctl.red[1][t]) + (ctl.red[2][t] + ctl.red[3][t]);
+    ctl.red[part][t] = total;
+    asm volatile("bar.sync 2, %0;" ::"n"(256 * kGroups) : "memory");  // the groups
+    if (part == 0 && wok && key < p.prefix_len) {
+      total = 0.f;
+#pragma unroll
+      for (int k = 0; k < 2 * kGroups; ++k) total += ctl.red[k][t];
       if (p.nsplit > 1)
-        p.part[(static_cast<size_t>(part) * p.hkv + g) * p.prefix_len + key] = total;
+        p.part[(static_cast<size_t>(blockIdx.x % p.nsplit) * p.hkv + g) * p.prefix_len + key] = total;
       else
         p.w[g * p.w_stride + key] = with_earlier(p, g, key, total);
     }
