@@ -6,13 +6,14 @@
 // weights_tc: 128 keys of one key/value head stay in TMEM as the A operand (their rows read straight
 // from global memory); tiles of up to 128 (row, head) queries pass by as B, so that an accumulator row
 // is a key and a thread adds up its key's exponentials along the row: no reduction across threads
-// until the end, no atomics, one order of addition. 27 warps:
+// until the end, no atomics, one order of addition. 28 warps:
 //   warps 0-23 exponentials and sums: groups of eight warps take every third tile; of a group, warps q
 //              and q + 4 share TMEM lane quarter q (keys 32q .. 32q + 31), each taking 64 of the 128
 //              queries;
 //   warp 24    TMA producer: Q through 6 stages (128-element heads: 192 KB);
 //   warp 25    TMEM allocator and issuer: S_j = K Q_j^T into a buffer of 128 columns for each group;
-//   warp 26    the queries' normalisers through 6 stages.
+//   warps 26, 27 the queries' normalisers through 6 stages, every other tile each (one warp took 800
+//              cycles a tile, more than the products do).
 // TMEM: S ring [0, 384), K [448, 448 + D/2). Bound by the exponentials, one to each product of D
 // elements (for D = 128 the tensor cores need about as long).
 // Each tile's sum is formed on its own and then added to the key's total (two levels: the
@@ -52,7 +53,7 @@ __device__ __forceinline__ float with_earlier(const WeightsParams& p, int g, int
 }
 
 // ---------------------------------------------------------------- bf16, tensor cores
-constexpr int kThreads = 864;
+constexpr int kThreads = 896;
 constexpr int kGroups = 3;
 constexpr int kQStages = 6, kSBufs = kGroups;
 static_assert(kQStages % kGroups == 0, "a group's tiles come back to the stages that it used");
@@ -227,34 +228,38 @@ __global__ void __launch_bounds__(kThreads, 1)
     if (!ok && lane == 0) flag_timeout(p, ctl);
     if (issue) mma_commit(&ctl.drained);
     __syncwarp();
-  } else if (warp == kWLse) {
+  } else if (warp >= kWLse) {
     // ------------------------------------------------------------ normalisers
-    // (three tiles' loads in flight; column 32 e + lane of a tile is row rr[e], head hh[e] of it)
-    constexpr int kAhead = 3;
-    int rr[4], hh[4];
+    // (two tiles' loads in flight; column 32 e + lane of a tile is row rr[e] of it, `at[e]` elements on)
+    int rr[4], at[4];
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
-      rr[e] = (32 * e + lane) / p.box_heads;
-      hh[e] = (32 * e + lane) % p.box_heads;
+      const int c = 32 * e + lane, h = c % p.box_heads;
+      rr[e] = c < columns ? c / p.box_heads : INT_MAX;  // (no column: behind the last row)
+      at[e] = c / p.box_heads * p.hq + h;
     }
     auto fetch = [&](int j, float (&v)[4]) {
       const int tile = j0 + j;
-      const int h0 = p.head_blocks > 1 ? tile % p.head_blocks * p.box_heads : 0;
-      const int64_t row0 = static_cast<int64_t>(p.head_blocks > 1 ? tile / p.head_blocks : tile) * p.box_rows;
-      const float* src = p.lse + row0 * p.hq + g * p.group + h0;
+      int row0 = tile * p.box_rows, h0 = 0;
+      if (p.head_blocks > 1) {
+        h0 = tile % p.head_blocks * p.box_heads;
+        row0 = tile / p.head_blocks * p.box_rows;
+      }
+      const int left = j < n ? p.rows - row0 : 0;
+      const float* src = p.lse + static_cast<int64_t>(row0) * p.hq + g * p.group + h0;
 #pragma unroll
       for (int e = 0; e < 4; ++e)
-        v[e] = j < n && 32 * e + lane < columns && h0 + hh[e] < p.group && row0 + rr[e] < p.rows
-                   ? __ldg(src + static_cast<int64_t>(rr[e]) * p.hq + hh[e]) : INFINITY;
+        v[e] = rr[e] < left && (p.head_blocks == 1 || h0 + (32 * e + lane) % p.box_heads < p.group)
+                   ? __ldg(src + at[e]) : INFINITY;
     };
-    float v[kAhead][4];
-#pragma unroll
-    for (int u = 0; u < kAhead; ++u) fetch(u, v[u]);
+    float v[2][4];
+    int b = warp - kWLse;
+    uint32_t parity = 1;  // of the stage's use before this one (the first round does not wait)
+    fetch(b, v[0]);
+    fetch(b + 2, v[1]);
     bool ok = true;
-    for (int j = 0; j < n && ok && !*abort_flag; ++j) {
-      const int b = j % kQStages;
-      if (j >= kQStages) ok = mbar_wait(&ctl.l_empty[b], ((j - kQStages) / kQStages) & 1, wlim);
-      ok = __all_sync(0xffffffffu, ok);
+    for (int j = b; j < n && ok && !*abort_flag; j += 2) {
+      if (j >= kQStages) ok = warp_wait(&ctl.l_empty[b], parity, wlim);
       if (!ok) break;
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
@@ -266,11 +271,13 @@ __global__ void __launch_bounds__(kThreads, 1)
       }
       __syncwarp();
       if (lane == 0) mbar_arrive(&ctl.l_full[b]);
+      if ((b += 2) >= kQStages) {
+        b -= kQStages;
+        parity ^= 1;
+      }
 #pragma unroll
-      for (int u = 0; u + 1 < kAhead; ++u)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) v[u][e] = v[u + 1][e];
-      fetch(j + kAhead, v[kAhead - 1]);
+      for (int e = 0; e < 4; ++e) v[0][e] = v[1][e];
+      fetch(j + 4, v[1]);
     }
     if (!ok && lane == 0) flag_timeout(p, ctl);
   } else {
