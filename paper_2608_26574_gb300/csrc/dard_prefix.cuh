@@ -46,8 +46,7 @@ struct JoinParams {
   int32_t queries, tiles, nsplit, tile_rows;
 };
 
-// The fp32 kernel on CUDA cores.
-int prefix_f32_rows(const PrefixParams& p, int sms);  // packed queries per CTA
+// The fp32 kernel on CUDA cores, with 16, 32 or 128 packed queries per CTA.
 cudaError_t launch_prefix_f32(const PrefixParams& p, int rows, cudaStream_t stream);
 
 namespace {

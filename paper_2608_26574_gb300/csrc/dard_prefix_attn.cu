@@ -593,21 +593,44 @@ __global__ void __launch_bounds__(128, 6) prefix_join(const __grid_constant__ Jo
 // ---------------------------------------------------------------- host side
 constexpr int kSlots = 640;  // parts of a split launch at most
 
-// CTAs per query tile. Costs in SM cycles: a CTA about kFixed plus kStep per key tile, the join
-// about kJoin; a launch with no more CTAs than SMs takes its longest, a larger one total / SMs
-// plus half a CTA.
+// CTAs per query tile. Costs in SM cycles: a CTA about `fixed` plus `step` per key tile; CTAs are alike,
+// so that a launch takes as many rounds of them as the SMs need (measured: 112 tiles of 514 steps in 1,
+// 2, 3, 4 and 5 parts take 399, 421, 428, 342 and 368 us); the join 5000 and 25 per part.
 int choose_split(long long items, double steps, int most, int sms, double fixed, double step) {
-  constexpr double kJoin = 6000;
   int best = 1;
   double best_time = 0;
   for (int s = 1; s <= most && items * s <= kSlots; ++s) {
-    const double cta = fixed + step * std::ceil(steps / s);
-    const double n = static_cast<double>(items) * s;
-    const double time = (n <= sms ? cta : n * (fixed + step * steps / s) / sms + 0.5 * cta) +
-                        (s > 1 ? kJoin : 0);
+    const long long n = items * s;
+    const double time = static_cast<double>((n + sms - 1) / sms) * (fixed + step * std::ceil(steps / s)) +
+                        (s > 1 ? 5000.0 + 25.0 * static_cast<double>(n) : 0.0);
     if (s == 1 || time < best_time) {
       best = s;
       best_time = time;
+    }
+  }
+  return best;
+}
+
+// The fp32 kernel: queries per CTA (16, 32 or 128) and CTAs per query tile. Costs in SM cycles per tile
+// of 64 keys of 128 elements, measured: 4600, 5100 and 15000 on SMs full of CTAs, 10000, 10000 and
+// 15000 for a CTA that has its SM to itself.
+int choose_f32(long long queries, int heads, int d, int steps, int sms, bool may_split, int& split) {
+  constexpr int kRows[3] = {16, 32, 128};
+  constexpr double kFull[3] = {4600, 5100, 15000}, kAlone[3] = {10000, 10000, 15000};
+  int best = 128;
+  double best_time = 0;
+  split = 1;
+  for (int i = 0; i < 3; ++i) {
+    const long long items = (queries + kRows[i] - 1) / kRows[i] * heads;
+    for (int s = 1; s <= (may_split ? steps : 1) && (s == 1 || items * s <= kSlots); ++s) {
+      const double n = static_cast<double>(items) * s, part = std::ceil(static_cast<double>(steps) / s);
+      const double work = std::max(part * kAlone[i], items * static_cast<double>(steps) * kFull[i] / sms);
+      const double time = work * d / 128 + 6000 * std::max(1.0, n / sms) + (s > 1 ? 5000 + 10 * n : 0);
+      if (best_time == 0 || time < best_time) {
+        best = kRows[i];
+        split = s;
+        best_time = time;
+      }
     }
   }
   return best;
@@ -730,18 +753,18 @@ dard_status dard_prefix_attention(const dard_prefix_attn_args* args, void* strea
                   cudaGetErrorString(cudaErrorLaunchFailure));
   const int sms = sm_count();
   const bool bf16 = args->own.dtype == DARD_BF16;
-  const int rows = bf16 ? kBM : prefix_f32_rows(p, sms);
   const int key_tile = bf16 ? kTN : 64;
-  p.tiles = (p.queries + rows - 1) / rows;
-  if (static_cast<long long>(p.tiles) * p.a.hkv > (1ll << 31) - 1)
-    return report(DARD_ERR_SHAPE, "too many query tiles");
-  p.nsplit = 1;
-  const long long items = static_cast<long long>(p.tiles) * p.a.hkv;
   // every tile has the prefix's key tiles and at least one of its own
   const int least = (p.prefix_len + key_tile - 1) / key_tile + 1;
-  double own = 0;  // own key tiles of a query tile, on average
+  p.nsplit = 1;
+  const int rows = bf16 ? kBM : choose_f32(p.queries, p.a.hkv, p.a.head_dim, least, sms,
+                                           p.part != nullptr, p.nsplit);
+  p.tiles = (p.queries + rows - 1) / rows;
+  const long long items = static_cast<long long>(p.tiles) * p.a.hkv;
+  if (items > (1ll << 31) - 1) return report(DARD_ERR_SHAPE, "too many query tiles");
   if (p.tiles <= kTileTable) {
     int s0 = 0, s1 = 0;
+    double own = 0;  // own key tiles of a query tile, on average
     for (int i = 0; i < p.tiles; ++i) {
       const int t0 = static_cast<int>(static_cast<long long>(i) * rows / p.group);
       const int t1 = static_cast<int>((std::min<long long>((i + 1ll) * rows, p.queries) - 1) / p.group);
@@ -752,10 +775,8 @@ dard_status dard_prefix_attention(const dard_prefix_attn_args* args, void* strea
       own += (p.a.seq[s1].row_base + p.a.seq[s1].n_orig + p.a.seq[s1].slen - p.a.seq[s0].row_base +
               key_tile - 1) / key_tile;
     }
-    const double steps = least - 1 + own / p.tiles;
-    if (p.part != nullptr)
-      p.nsplit = bf16 ? choose_split(items, steps, least, sms, 8000, 1500)
-                      : choose_split(items, steps, least, sms, 6000, 100.0 * rows);
+    if (bf16 && p.part != nullptr)
+      p.nsplit = choose_split(items, least - 1 + own / p.tiles, least, sms, 12000, 1500);
   }
   cudaError_t e;
   if (!bf16)

@@ -8,7 +8,8 @@
 // shared-memory load of a query or a key serves 4 or TR dot products; the 16 threads of a query
 // share its maximum by shuffles, exchange the probabilities through shared memory within their
 // half-warp, and add up columns 4 tx .. (and 64 + 4 tx ..) of its output.
-// Bound: the fp32 FMA rate where the queries fill the tile; TR is chosen by their number.
+// Bound by the fp32 FMA rate with TR = 8 (2048 rows x 28 heads over 4096 keys: 80 TFLOP/s); fewer queries
+// take smaller tiles, which wait for shared memory (dard_prefix_attn.cu chooses).
 #include <cfloat>
 
 #include "dard_prefix.cuh"
@@ -280,13 +281,6 @@ cudaError_t launch_rows(const PrefixParams& p, int rows, cudaStream_t stream) {
 }
 
 }  // namespace
-
-// Queries per CTA: 128 where they give every SM a CTA, else 32, or 16 for very few.
-int prefix_f32_rows(const PrefixParams& p, int sms) {
-  const long long all = static_cast<long long>(p.queries) * p.a.hkv;
-  if (p.queries <= 16) return 16;
-  return all < 128ll * sms ? 32 : 128;
-}
 
 cudaError_t launch_prefix_f32(const PrefixParams& p, int rows, cudaStream_t stream) {
   return p.a.head_dim == 64 ? launch_rows<64>(p, rows, stream) : launch_rows<128>(p, rows, stream);
