@@ -595,14 +595,17 @@ constexpr int kSlots = 640;  // parts of a split launch at most
 
 // CTAs per query tile. Costs in SM cycles: a CTA about `fixed` plus `step` per key tile; CTAs are alike,
 // so that a launch takes as many rounds of them as the SMs need (measured: 112 tiles of 514 steps in 1,
-// 2, 3, 4 and 5 parts take 399, 421, 428, 342 and 368 us); the join 5000 and 25 per part.
-int choose_split(long long items, double steps, int most, int sms, double fixed, double step) {
+// 2, 3, 4 and 5 parts take 399, 421, 428, 342 and 368 us); the join 5000 and 25 per part of a full
+// tile.
+int choose_split(long long items, int queries, double steps, int most, int sms) {
+  constexpr double fixed = 12000, step = 1500;
+  const double part = 25.0 * std::min(1.0, queries / static_cast<double>(kBM));
   int best = 1;
   double best_time = 0;
   for (int s = 1; s <= most && items * s <= kSlots; ++s) {
     const long long n = items * s;
     const double time = static_cast<double>((n + sms - 1) / sms) * (fixed + step * std::ceil(steps / s)) +
-                        (s > 1 ? 5000.0 + 25.0 * static_cast<double>(n) : 0.0);
+                        (s > 1 ? 5000.0 + part * static_cast<double>(n) : 0.0);
     if (s == 1 || time < best_time) {
       best = s;
       best_time = time;
@@ -776,7 +779,7 @@ dard_status dard_prefix_attention(const dard_prefix_attn_args* args, void* strea
               key_tile - 1) / key_tile;
     }
     if (bf16 && p.part != nullptr)
-      p.nsplit = choose_split(items, least - 1 + own / p.tiles, least, sms, 12000, 1500);
+      p.nsplit = choose_split(items, p.queries, least - 1 + own / p.tiles, least, sms);
   }
   cudaError_t e;
   if (!bf16)
