@@ -12,6 +12,9 @@
  *                              (Eq. 7) and the three-state transition (Eq. 8), in the order
  *                              of Algorithm 1.
  *
+ * Beside them: the MLP half of a layer with experts (dard_residual_norm .. dard_experts) and
+ * decoding behind a shared prefix (dard_prefix_attention, _weights, _evict).
+ *
  * Conventions shared by every entry point
  *   - Pointers named "device" are CUDA device memory owned by the caller; pointers named
  *     "host" are ordinary host memory owned by the caller and read during the call only.
@@ -563,7 +566,8 @@ typedef struct {
   const void* q;             /* device [rows, hq, head_dim], contiguous                    */
   const float* lse;          /* device [rows, hq], contiguous                              */
   const void* prefix_k;      /* device, dtype of q                                         */
-  const float* weights_in;   /* optional device [hkv, prefix_len]; may be weights          */
+  const float* weights_in;   /* optional device [hkv, prefix_len]; weights itself, or apart
+                                from it                                                    */
   float* weights;            /* device [hkv, prefix_len] out                               */
   int64_t prefix_row_stride, prefix_head_stride;           /* elements                     */
   int64_t weights_in_stride, weights_stride;  /* elements between heads, >= prefix_len     */

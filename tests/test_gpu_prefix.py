@@ -126,6 +126,9 @@ CASES = [
     # a group of more heads than a tile has rows
     ("bf16", 150, 1, 64, 200, [(3, 4, 0, 4), (1, 0, 0, 0)]),
     ("f32", 150, 1, 64, 70, [(3, 4, 0, 4), (1, 0, 0, 0)]),
+    # more query tiles than the launch's table of sequences holds
+    ("bf16", 64, 1, 64, 10, [(14, 9, 3, 9), (1, 0, 0, 0)] * 60),
+    ("f32", 64, 1, 64, 10, [(14, 9, 3, 9), (1, 0, 0, 0)] * 60),
     # enough queries for the fp32 kernel's large tiles
     ("f32", 16, 16, 64, 100, [(0, 64, 500, 64)] * 2),
     ("f32", 40, 8, 128, 40, [(0, 32, 300, 32)] * 2),
