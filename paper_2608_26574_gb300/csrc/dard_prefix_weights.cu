@@ -127,7 +127,8 @@ __global__ void __launch_bounds__(kThreads, 1)
   const int g = item / p.key_tiles, key0 = item % p.key_tiles * kTN;
   const int j0 = static_cast<int>(static_cast<long long>(p.q_tiles) * part / p.nsplit);
   const int n = static_cast<int>(static_cast<long long>(p.q_tiles) * (part + 1) / p.nsplit) - j0;
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  // (a shuffle's result is the warp's, as the compiler knows, and so are the branches on it: 866 -> 842 us)
+  const int warp = __shfl_sync(0xffffffffu, static_cast<int>(threadIdx.x >> 5), 0), lane = threadIdx.x & 31;
   const long long wlim = p.wait_cycles > 0 ? p.wait_cycles : kWaitCycles;
   const int columns = p.box_heads * p.box_rows;  // queries of a tile, at most 128
 
