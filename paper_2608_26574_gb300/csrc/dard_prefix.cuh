@@ -143,10 +143,18 @@ __device__ __forceinline__ void own_range(const PrefixParams& p, int tile, int r
 // publish_block_info(), row_info() and row_masks() derive for a CTA whose rows are all of one
 // sequence. Lane by lane: `seq` (-1: no row) and the sequence-relative row r; store = 0 for a
 // shadow row whose shadow_src is invalid. Called by whole warps. The lanes fetch a sequence's block
-// together, 32 positions each time, and every lane derives its row's masks from ballots of it.
-__device__ RowMasks warp_query_masks(const AttnParams& p, int seq, int r, bool report, int& store) {
+// together, 32 positions each time; ballots make bit words of it, and the warp's scratch lets every
+// lane read any position's confidence and any shadow row's position.
+struct BlockScratch {
+  float4 cf[DARD_MAX_BLOCK / 4];
+  int4 pos[DARD_MAX_BLOCK / 4];  // block positions of the shadow rows (-1: none)
+};
+__device__ __forceinline__ RowMasks warp_query_masks(const AttnParams& p, BlockScratch& scratch, int seq,
+                                                     int r, bool report, int& store) {
   constexpr uint32_t kAll = 0xffffffffu;
   const int lane = threadIdx.x & 31;
+  float* cf = reinterpret_cast<float*>(scratch.cf);
+  int* pos = reinterpret_cast<int*>(scratch.pos);
   RowMasks out{{0, 0}, {0, 0}};
   store = seq >= 0;
   uint32_t todo = __ballot_sync(kAll, seq >= 0);
@@ -157,44 +165,41 @@ __device__ RowMasks warp_query_masks(const AttnParams& p, int seq, int r, bool r
     const SeqDesc& sd = p.seq[s];
     const int blen = sd.blen, slen = sd.slen;
     if (blen == 0) continue;  // no block, no shadow rows: nothing is hidden
-    int st[4], pos[4];
-    float cf[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const int j = 32 * i + lane;
-      st[i] = j < blen ? __ldg(p.state + sd.blk_off + j) : kStateU;
-      cf[i] = j < blen ? __ldg(p.prev_conf + sd.blk_off + j) : 0.f;
-      pos[i] = j < slen ? __ldg(p.shadow_src + sd.sh_off + j) - sd.b0 : -1;
-      if (pos[i] >= blen) pos[i] = -1;
-    }
     // bit words over block positions (m, c: states; hs: a shadow copy exists) and over shadow rows
     // (valid: the position's lowest shadow row)
-    uint32_t m[4], c[4], hs[4] = {0, 0, 0, 0}, valid[4];
+    uint32_t m[4] = {0, 0, 0, 0}, c[4] = {0, 0, 0, 0}, hs[4] = {0, 0, 0, 0}, valid[4] = {0, 0, 0, 0};
     int rows = 0, positions = 0;
     bool bad_state = false, identity = true;
+    __syncwarp();
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      m[i] = __ballot_sync(kAll, st[i] == kStateM || st[i] > 2);
-      c[i] = __ballot_sync(kAll, st[i] == kStateC);
-      valid[i] = __ballot_sync(kAll, pos[i] >= 0);
-      bad_state |= st[i] > 2;
-      identity &= 32 * i + lane >= slen || pos[i] == 32 * i + lane;
+      if (32 * i >= blen) break;
+      const int j = 32 * i + lane;
+      const int st = j < blen ? __ldg(p.state + sd.blk_off + j) : kStateU;
+      const float x = j < blen ? __ldg(p.prev_conf + sd.blk_off + j) : 0.f;
+      int at = j < slen ? __ldg(p.shadow_src + sd.sh_off + j) - sd.b0 : -1;
+      if (at >= blen) at = -1;
+      cf[j] = x;
+      pos[j] = at;
+      m[i] = __ballot_sync(kAll, st == kStateM || st > 2);
+      c[i] = __ballot_sync(kAll, st == kStateC);
+      valid[i] = __ballot_sync(kAll, at >= 0);
+      bad_state |= st > 2;
+      identity &= j >= slen || at == j;
       rows += __popc(valid[i]);
-      if (32 * i < slen) {
 #pragma unroll
-        for (int w = 0; w < 4; ++w)
-          if (32 * w < blen)
-            hs[w] |= __reduce_or_sync(kAll, pos[i] >= 0 && pos[i] >> 5 == w ? 1u << (pos[i] & 31) : 0u);
-      }
+      for (int w = 0; w < 4; ++w)
+        if (32 * w < blen) hs[w] |= __reduce_or_sync(kAll, at >= 0 && at >> 5 == w ? 1u << (at & 31) : 0u);
     }
 #pragma unroll
     for (int w = 0; w < 4; ++w) positions += __popc(hs[w]);
+    __syncwarp();
     if (positions != rows) {  // a repeated position: its lowest row alone is valid
       uint32_t seen[4] = {0, 0, 0, 0};
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         for (int l = 0; l < 32 && 32 * i + l < slen; ++l) {
-          const int x = __shfl_sync(kAll, pos[i], l);
+          const int x = pos[32 * i + l];
           if (x < 0) continue;
           bool again = false;
 #pragma unroll
@@ -213,67 +218,63 @@ __device__ RowMasks warp_query_masks(const AttnParams& p, int seq, int r, bool r
                              (positions != slen ? DARD_STATUS_BAD_SHADOW : 0u);
       if (lane == 0 && flags) atomicOr(p.status, flags);
     }
-    // this lane's row
-    RowInfo q{0, kStateU, 0.f, -1, 1};
-    const int kq = r - sd.n_orig, j = r - sd.b0;  // its shadow index, its block position
-    if (kq < 0) {
-      if (j >= 0 && j < blen) q.i = j;
-      else q.si = j < 0 ? kStateU : kStateM;  // decoded context / still masked
-    }
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const int x = __shfl_sync(kAll, pos[i], kq & 31);
-      if (kq >= 0 && kq >> 5 == i) {
-        q.qs = valid[i] >> (kq & 31) & 1u;
-        if (q.qs) q.i = x;
-        q.store = q.qs;
+    if (mine) {  // this lane's row
+      RowInfo q{0, kStateU, 0.f, -1, 1};
+      const int kq = r - sd.n_orig, j = r - sd.b0;  // its shadow index, its block position
+      if (kq >= 0) {
+        const uint32_t word = kq < 64 ? (kq < 32 ? valid[0] : valid[1]) : (kq < 96 ? valid[2] : valid[3]);
+        q.qs = q.store = word >> (kq & 31) & 1u;
+        if (q.qs) q.i = pos[kq];
+      } else if (j >= 0 && j < blen) {
+        q.i = j;
+      } else {
+        q.si = j < 0 ? kStateU : kStateM;  // decoded context / still masked
       }
-    }
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const float x = __shfl_sync(kAll, cf[i], q.i & 31);
-      if (q.i >= 0 && q.i >> 5 == i) {
-        q.si = m[i] >> (q.i & 31) & 1u ? kStateM : c[i] >> (q.i & 31) & 1u ? kStateC : kStateU;
-        q.ci = x;
+      if (q.i >= 0) {
+        const int w = q.i >> 5;
+        const uint32_t mw = w < 2 ? (w == 0 ? m[0] : m[1]) : (w == 2 ? m[2] : m[3]);
+        const uint32_t cw = w < 2 ? (w == 0 ? c[0] : c[1]) : (w == 2 ? c[2] : c[3]);
+        q.si = mw >> (q.i & 31) & 1u ? kStateM : cw >> (q.i & 31) & 1u ? kStateC : kStateU;
+        q.ci = cf[q.i];
       }
-    }
-    // positions taken from their shadow copy, as in row_masks()
-    uint32_t ts[4];
-    const bool is_c = q.si == kStateC;
-    const bool all_mc = q.si == kStateU || (q.si == kStateM && q.qs);
-    const bool any_c = __any_sync(kAll, mine && is_c);
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      uint32_t lower = 0;  // C keys with !(c_i <= c_j) (Eq. 3)
-      if (any_c && 32 * i < blen) {
-#pragma unroll 8
-        for (int l = 0; l < 32; ++l)
-          lower |= static_cast<uint32_t>(!(q.ci <= __shfl_sync(kAll, cf[i], l))) << l;
-      }
-      ts[i] = all_mc ? m[i] | c[i] : is_c ? m[i] | (c[i] & lower) : 0u;
-      if (q.qs && q.i >> 5 == i) ts[i] |= 1u << (q.i & 31);
-    }
-    uint32_t see[4] = {0, 0, 0, 0};
-    if (identity) {
-#pragma unroll
-      for (int i = 0; i < 4; ++i) see[i] = ts[i] & valid[i];
-    } else {
+      // positions taken from their shadow copy, as in row_masks()
+      uint32_t ts[4], see[4] = {0, 0, 0, 0};
+      const bool all_mc = q.si == kStateU || (q.si == kStateM && q.qs);
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        for (int l = 0; l < 32 && 32 * i + l < slen; ++l) {
-          const int x = __shfl_sync(kAll, pos[i], l);
-          const uint32_t word = x < 64 ? (x < 32 ? ts[0] : ts[1]) : (x < 96 ? ts[2] : ts[3]);
-          see[i] |= (word >> (x & 31) & 1u) << l;
+        ts[i] = all_mc ? m[i] | c[i] : 0u;
+        if (q.si == kStateC && 32 * i < blen) {
+          uint32_t lower = 0;  // C keys with !(c_i <= c_j) (Eq. 3)
+#pragma unroll
+          for (int l = 0; l < 8; ++l) {
+            const float4 x = scratch.cf[8 * i + l];
+            lower |= (static_cast<uint32_t>(!(q.ci <= x.x)) | static_cast<uint32_t>(!(q.ci <= x.y)) << 1 |
+                      static_cast<uint32_t>(!(q.ci <= x.z)) << 2 | static_cast<uint32_t>(!(q.ci <= x.w)) << 3)
+                     << (4 * l);
+          }
+          ts[i] = m[i] | (c[i] & lower);
+        }
+        if (q.qs && q.i >> 5 == i) ts[i] |= 1u << (q.i & 31);  // a shadow query takes its own copy
+      }
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        if (identity) {
+          see[i] = ts[i];
+        } else {
+          for (int l = 0; l < 32 && 32 * i + l < slen; ++l) {
+            const int x = pos[32 * i + l];
+            const uint32_t word = x < 64 ? (x < 32 ? ts[0] : ts[1]) : (x < 96 ? ts[2] : ts[3]);
+            see[i] |= (word >> (x & 31) & 1u) << l;
+          }
         }
         see[i] &= valid[i];
       }
-    }
-    if (mine) {
       store = q.store;
       const uint32_t hide[4] = {ts[0] & hs[0], ts[1] & hs[1], ts[2] & hs[2], ts[3] & hs[3]};
       out.hide_x = words128(hide);
       out.see_s = words128(see);
     }
+    __syncwarp();
   }
   return out;
 }

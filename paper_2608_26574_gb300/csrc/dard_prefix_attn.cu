@@ -58,6 +58,7 @@ struct __align__(16) Ctl {
   float red_sum[kParts][kBM];     // their row sums
   int64_t out_row[kBM];      // packed query -> row * hq + head, or -1 (not stored)
   RowMasks row_mask[kBM];
+  BlockScratch scratch[4];
   int32_t row_seq[kBM];      // -1: no query
   uint32_t inf_pos[kBM][4], inf_neg[kBM][4];  // elements to become inf, -inf (both: NaN)
 };
@@ -320,7 +321,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     int store = seq >= 0;
     if (first_own < n_kt) {
       if (part4 == 0) {
-        ctl.row_mask[t] = warp_query_masks(p.a, seq, r, g == 0, store);
+        ctl.row_mask[t] = warp_query_masks(p.a, ctl.scratch[quarter], seq, r, g == 0, store);
         ctl.row_seq[t] = seq;
         ctl.out_row[t] = store ? out_row : -1;
       }

@@ -89,7 +89,9 @@ __global__ void __launch_bounds__(kF32Threads) prefix_f32(const __grid_constant_
   // thread t < kRows: query t's masks (while own tiles are to come)
   RowMasks rm{{0, 0}, {0, 0}};
   int seq = -1, store = 1;
+  __shared__ BlockScratch scratch[(kRows + 31) / 32];
   if (tid < (kRows + 31) / 32 * 32 && j1 > npt) {
+    const int warp_of_rows = tid / 32;
     int r = 0;
     if (tid < kRows && m0 + tid < p.queries) {
       const int tq = (m0 + tid) / p.group;
@@ -97,7 +99,7 @@ __global__ void __launch_bounds__(kF32Threads) prefix_f32(const __grid_constant_
       r = p.a.seq[seq].q_start + tq - p.q_before[seq];
     }
     __syncwarp();
-    rm = warp_query_masks(p.a, seq, r, g == 0, store);
+    rm = warp_query_masks(p.a, scratch[warp_of_rows], seq, r, g == 0, store);
   }
 
   float m[TR], l[TR];
