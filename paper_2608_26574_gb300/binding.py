@@ -842,7 +842,7 @@ def _cache(t, name: str, device: int, dtype, hkv: int, head_dim: int) -> tuple[i
     # (a stride that no step uses may be anything: one that is in order is passed)
     if shape[0] <= 1:
         rs = hkv * head_dim
-    if hkv == 1:
+    if hkv == 1 or shape[0] == 0:
         hs = head_dim
     if rs < head_dim or hs < head_dim:
         raise ValueError(f"{name}: heads overlap (strides {t.stride()})")

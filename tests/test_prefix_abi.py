@@ -202,6 +202,34 @@ def test_binding_refuses_before_the_library(lib):
         B._cache(kv.to(f32), "prefix_k", -1, bf, 2, 64)
 
 
+def test_strides_that_no_step_uses(lib):
+    """Rows of an empty or one-row cache, heads of a one-head cache: any stride will do."""
+    class Fake:
+        dtype = torch.bfloat16
+
+        def __init__(self, shape, strides):
+            self.shape, self.strides = torch.Size(shape), strides
+
+        def get_device(self):
+            return 0
+
+        def stride(self):
+            return self.strides
+
+        def data_ptr(self):
+            return PTR
+
+    def strides(shape, s):
+        return B._cache(Fake(shape, s), "k", 0, torch.bfloat16, shape[1], 64)[1:]
+
+    assert strides((0, 2, 64), (1, 3, 1)) == (128, 64)
+    assert strides((1, 2, 64), (1, 72, 1)) == (128, 72)
+    assert strides((9, 1, 64), (80, 0, 1)) == (80, 64)
+    for shape, s in (((9, 2, 64), (128, 8, 1)), ((9, 2, 64), (32, 64, 1)), ((9, 2, 64), (128, 64, 2))):
+        with pytest.raises(ValueError):
+            strides(shape, s)
+
+
 def test_prefix_cache_refusals(lib):
     from paper_2608_26574_gb300.prefix import PrefixCache
     with pytest.raises(ValueError, match="CUDA device"):
