@@ -46,7 +46,8 @@ struct JoinParams {
   int32_t queries, tiles, nsplit, tile_rows;
 };
 
-// The fp32 kernel on CUDA cores, with 16, 32 or 128 packed queries per CTA.
+// The fp32 kernels on CUDA cores, with kF32FewRows or 128 packed queries per CTA.
+constexpr int kF32FewRows = 8;
 cudaError_t launch_prefix_f32(const PrefixParams& p, int rows, cudaStream_t stream);
 
 namespace {

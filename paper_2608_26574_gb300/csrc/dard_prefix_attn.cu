@@ -620,26 +620,34 @@ int choose_split(long long items, int queries, double steps, int most, int sms) 
   return best;
 }
 
-// The fp32 kernel: queries per CTA (16, 32 or 128) and CTAs per query tile. Costs in SM cycles per tile
-// of 64 keys of 128 elements, measured: 4600, 5100 and 15000 on SMs full of CTAs, 10000, 10000 and
-// 15000 for a CTA that has its SM to itself.
+// The fp32 kernels: queries per CTA (8, two CTAs to an SM, or 128, one) and CTAs per query tile. Costs in
+// SM cycles, fitted to 24 shapes (1 to 7168 packed queries, 3 to 1025 key tiles) with 1 to 152 parts, 8 % off
+// on average: a CTA `fixed`, and per tile of 64 keys of 128 elements `tile`, a pair of the small ones
+// together `pair`; the join 6000 and 9 per part. The choice is 0.3 % behind the best of all measured, 5 % at
+// most. Measured with 4 kv heads, as 8 and as 128 queries: 7 queries over 4096 keys 10.8 and 37.7 us, 448 over
+// 2048 83 and 86 us, 1792 over 2048 274 and 234 us.
 int choose_f32(long long queries, int heads, int d, int steps, int sms, bool may_split, int& split) {
-  constexpr int kRows[3] = {16, 32, 128};
-  constexpr double kFull[3] = {4600, 5100, 15000}, kAlone[3] = {10000, 10000, 15000};
-  int best = 128;
+  int best = 0;
   double best_time = 0;
-  split = 1;
-  for (int i = 0; i < 3; ++i) {
-    const long long items = (queries + kRows[i] - 1) / kRows[i] * heads;
-    for (int s = 1; s <= (may_split ? steps : 1) && (s == 1 || items * s <= kSlots); ++s) {
-      const double n = static_cast<double>(items) * s, part = std::ceil(static_cast<double>(steps) / s);
-      const double work = std::max(part * kAlone[i], items * static_cast<double>(steps) * kFull[i] / sms);
-      const double time = work * d / 128 + 6000 * std::max(1.0, n / sms) + (s > 1 ? 5000 + 10 * n : 0);
-      if (best_time == 0 || time < best_time) {
-        best = kRows[i];
+  for (const int rows : {kF32FewRows, kBM}) {
+    const bool few = rows == kF32FewRows;
+    const double width = d == 64 ? 0.64 : 1.0;
+    const double tile = width * (few ? 3300 : 27000), pair = width * 5200, fixed = few ? 5500 : 25000;
+    const long long items = (queries + rows - 1) / rows * heads;
+    for (int s = 1;;) {
+      const long long n = items * s, each = (n + sms - 1) / sms;
+      const int part = (steps + s - 1) / s;
+      const double single = fixed + part * tile;
+      const double time = (few ? (each / 2) * (fixed + part * pair) + (each % 2) * single : each * single) +
+                          (s > 1 ? 6000.0 + 9.0 * n : 0.0);
+      if (best == 0 || time < best_time) {
+        best = rows;
         split = s;
         best_time = time;
       }
+      if (!may_split || part == 1) break;
+      s = (steps + part - 2) / (part - 1);  // the fewest parts that are shorter
+      if (items * s > kSlots) break;
     }
   }
   return best;

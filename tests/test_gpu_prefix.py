@@ -241,6 +241,38 @@ def test_attention_hidden_values(dtype, ws):
     assert np.isnan(want).any() and np.isfinite(want[:base[1]]).all()
 
 
+@pytest.mark.parametrize("ws", [True, False])
+@pytest.mark.parametrize("hq,hkv,d,prefix,seqs", [
+    (28, 4, 64, 1900, [(0, 64, 0, 64)] * 3),  # with a workspace in parts
+    (28, 4, 64, 1900, [(0, 64, 0, 64)] * 5),
+    (48, 2, 128, 700, [(9, 40, 5, 33), (0, 64, 0, 64), (100, 30, 7, 30)]),
+    (28, 4, 128, 4097, [(1, 0, 0, 0)]), (1, 1, 64, 20000, [(1, 0, 0, 0)]),  # few queries, many parts
+    (28, 4, 128, 1000, [(1, 0, 0, 0)] * 33), (9, 1, 64, 640, [(0, 3, 2, 3)])])
+def test_attention_f32_tiles(hq, hkv, d, prefix, seqs, ws):
+    """Both fp32 kernels, unsplit and in parts."""
+    lays, t = make("f32", hq, hkv, d, prefix, seqs, seed=prefix)
+    o, ls = attend(lays, t, ws=ws)
+    check_attention(lays, t, o, ls)
+
+
+def test_attention_hidden_values_f32_tiles():
+    """NaN and infinite values of hidden keys in the fp32 kernel for many queries."""
+    lays, t = make("f32", 96, 2, 128, 140, [(6, 9, 4, 9), (0, 12, 3, 12), (2, 0, 0, 0), (50, 20, 9, 14)] * 3, 21)
+    base = np.cumsum([0] + [x.rows for x in lays])
+    t["v"][base[0] + 7, 0, 5] = math.nan
+    t["v"][base[1] + 3, 0, 64] = -math.inf
+    t["v"][base[1] + 5, 0, 64] = math.inf
+    t["v"][base[7] + 55, 1, 0] = math.nan
+    o, _ = attend(lays, t)
+    want = O.prefix_attention(*(_np(t[x]) for x in ("q", "k", "v", "pk", "pv")), lays)[0]
+    got = _np(o)
+    assert np.array_equal(np.isnan(got), np.isnan(want))
+    assert np.array_equal(np.isinf(got), np.isinf(want))
+    fin = np.isfinite(want)
+    assert 0 < (~fin).sum() < fin.sum()
+    assert np.abs(got[fin] - want[fin]).max() <= 2e-5 * np.abs(_np(t["pv"])).max() * 1.2
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_attention_extreme_scores(dtype):
     """Scores far apart: one key takes all the weight, and its value comes back exactly."""
