@@ -505,6 +505,15 @@ cudaError_t launch_f32(const WeightsParams& p, cudaStream_t stream) {
   return cudaLaunchKernelEx(&L.cfg, weights_f32<D>, p);
 }
 
+// Whether [hkv, len] elements at a and at b, rows sa and sb apart, may have one in common: with one
+// stride exactly, otherwise by the first and the last.
+bool share(const float* a, int64_t sa, const float* b, int64_t sb, int64_t len, int hkv) {
+  const int64_t at = (reinterpret_cast<intptr_t>(b) - reinterpret_cast<intptr_t>(a)) / 4;
+  if (at >= (hkv - 1) * sa + len || -at >= (hkv - 1) * sb + len) return false;
+  const int64_t off = sa == sb ? (at % sa + sa) % sa : 0;  // of b's rows behind a's
+  return off < len || off > sa - len;
+}
+
 dard_status prepare(const dard_prefix_weights_args* a, WeightsParams& p) {
   memset(&p, 0, sizeof(p));
   if (!a) return report(DARD_ERR_NULL, "args is NULL");
@@ -527,6 +536,9 @@ dard_status prepare(const dard_prefix_weights_args* a, WeightsParams& p) {
     return report(DARD_ERR_SHAPE, "a weights stride is below prefix_len");
   if (a->weights_in == a->weights && a->weights_in_stride != a->weights_stride)
     return report(DARD_ERR_VALUE, "weights_in may be weights with the same stride only");
+  if (a->weights_in && a->weights_in != a->weights &&
+      share(a->weights, a->weights_stride, a->weights_in, a->weights_in_stride, a->prefix_len, a->hkv))
+    return report(DARD_ERR_VALUE, "weights_in must be weights or lie apart from it");
   if (((reinterpret_cast<uintptr_t>(a->weights) | reinterpret_cast<uintptr_t>(a->weights_in) |
         reinterpret_cast<uintptr_t>(a->lse)) & 3u) != 0)
     return report(DARD_ERR_ALIGN, "weights, weights_in and lse must be 4-byte aligned");

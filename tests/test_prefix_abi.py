@@ -110,6 +110,21 @@ def test_weights_refusals(lib, change, code):
     _refuse(lib, "dard_prefix_weights", _weights(), change, code)
 
 
+@pytest.mark.parametrize("at,stride,in_stride,hkv,refused", [
+    # weights [2, 100] at 4 PTR, 100 or 250 elements between heads; the earlier sums `at` elements on
+    (1, 100, 100, 2, True), (199, 100, 100, 2, True), (200, 100, 100, 2, False), (-199, 100, 100, 2, True),
+    (-200, 100, 100, 2, False), (100, 250, 250, 2, False), (150, 250, 250, 2, False), (99, 250, 250, 2, True),
+    (151, 250, 250, 2, True), (-100, 250, 250, 2, False), (-99, 250, 250, 2, True), (400, 250, 250, 2, False),
+    (300, 250, 120, 2, True), (350, 250, 120, 2, False), (50, 100, 100, 1, True), (100, 100, 100, 1, False)])
+def test_weights_beside_their_earlier_sums(lib, at, stride, in_stride, hkv, refused):
+    """weights_in is weights itself or has no element in common with it. (The calls that are not refused
+    for that end with a launch that fails, as there is no device here, or with the workspace's size.)"""
+    a = _weights()
+    a.hkv, a.weights_stride, a.weights_in_stride, a.weights_in = hkv, stride, in_stride, 4 * PTR + 4 * at
+    _refuse(lib, "dard_prefix_weights", a, {"workspace": 9 * PTR, "workspace_bytes": 16},
+            VALUE if refused else WORKSPACE)
+
+
 def _evict():
     a = B.PrefixEvictArgs()
     a.weights, a.prefix_k, a.prefix_v, a.kept, a.k_out, a.v_out = (i * PTR for i in range(1, 7))
