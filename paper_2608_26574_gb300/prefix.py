@@ -18,8 +18,10 @@ class PrefixCache:
     ``store`` fills a layer (the same number of rows in each), ``attention`` prepares a step's calls,
     ``attend`` runs a layer's attention, ``accumulate`` adds the weights of its queries to the layer's,
     and ``evict`` keeps the ``keep`` keys of each head with the largest weights. ``status``: optional
-    int32 word that the calls report in. Calls on several streams have workspaces of their own; what
-    they read and write of the cache itself is the caller's to order."""
+    int32 word that the calls report in. Every prepared attention and every ``accumulate`` has a
+    workspace of its own, so that they may overlap, as may graphs that hold them; what they read and
+    write of the cache itself is the caller's to order. ``store`` and ``evict`` change lengths and,
+    the latter, buffers: a graph captured before one of them holds the cache as it was then."""
 
     def __init__(self, layers: int, hq: int, hkv: int, head_dim: int, capacity: int,
                  dtype=torch.bfloat16, device="cuda", status=None):
@@ -38,7 +40,6 @@ class PrefixCache:
         self._length = [0] * layers
         self._layers = layers
         self.start = 0  # positions that the prefix takes: rows behind it start there
-        self._workspace: dict[tuple, torch.Tensor] = {}  # by use and stream
         self._kept = torch.empty(hkv * capacity, dtype=torch.int32, device=self.device)
 
     @property
@@ -72,23 +73,18 @@ class PrefixCache:
         self.values(layer).copy_(v)
         self.weights(layer).zero_()
 
-    def _scratch(self, name: str, need: int):
-        if need == 0:
-            return None
-        key = (name, torch.cuda.current_stream(self.device).cuda_stream)
-        w = self._workspace.get(key)
-        if w is None or w.numel() < need:
-            w = self._workspace[key] = torch.empty(need, dtype=torch.uint8, device=self.device)
-        return w
+    def _scratch(self, need: int):
+        return torch.empty(need, dtype=torch.uint8, device=self.device) if need else None
 
     def attention(self, n_orig, block_start, block_len, shadow_len, state, prev_conf, shadow_src,
                   scale: float = 0.0, query_start=None) -> B.PrefixAttentionCall:
-        """One step's prepared attention, for ``attend``: see ``PrefixAttentionCall``."""
+        """One step's prepared attention, for ``attend``: see ``PrefixAttentionCall``. (Calls of it share
+        its workspace: prepare one for each of those that overlap on the GPU.)"""
         rows = sum(int(x) for x in n_orig) + sum(int(x) for x in shadow_len)
         need = B.dard_prefix_attention_workspace_size(rows, self.hq, self.hkv, self.head_dim, self.capacity)
         return B.PrefixAttentionCall(n_orig, block_start, block_len, shadow_len, state, prev_conf,
                                      shadow_src, scale, self.status, query_start,
-                                     self._scratch("attention", need))
+                                     self._scratch(need))
 
     def attend(self, call: B.PrefixAttentionCall, layer: int, q, k, v, o, lse=None):
         """A layer's attention over the cache and the sequences' own rows."""
@@ -103,7 +99,7 @@ class PrefixCache:
                                                     self.capacity)
         w = self.weights(layer)
         B.dard_prefix_weights(q, lse, self.keys(layer), w, weights_in=w, scale=scale, decay=decay,
-                              workspace=self._scratch("weights", need), status=self.status)
+                              workspace=self._scratch(need), status=self.status)
 
     def evict(self, keep: int, keep_first: int = 0, keep_last: int = 0):
         """Every layer down to ``keep`` keys per head: the first and last few, and of the others those

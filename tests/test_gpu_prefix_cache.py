@@ -73,6 +73,42 @@ def test_cache_attention_after_eviction():
             assert np.abs(_np(lse) - wl).max() < 1e-4
 
 
+def test_cache_graphs_side_by_side():
+    """Two captured steps, in parts, replayed on two streams at once: each has its own workspaces."""
+    c, g = _filled(layers=2, hq=8, hkv=2, n=3000, capacity=3000)
+    steps = []
+    for i in range(2):
+        q = torch.randn(3, 8, 64, generator=g, device=DEV).to(torch.bfloat16)
+        k, v = (torch.randn(3, 2, 64, generator=g, device=DEV).to(torch.bfloat16) for _ in range(2))
+        steps.append((q, k, v, torch.empty_like(q), torch.empty(3, 8, device=DEV)))
+
+    def step(i):
+        q, k, v, o, lse = steps[i]
+        call = c.attention([3], [0], [0], [0], None, None, None)
+        c.attend(call, i, q, k, v, o, lse)
+        c.accumulate(i, q, lse, decay=0.0)
+        return call
+
+    want, graphs, calls = [], [], []
+    for i in range(2):
+        step(i)
+        want.append([x.clone() for x in (*steps[i][3:], c.weights(i))])
+    torch.cuda.synchronize()
+    for i in range(2):
+        graphs.append(torch.cuda.CUDAGraph())
+        with torch.cuda.graph(graphs[-1]):
+            calls.append(step(i))
+    assert calls[0]._scratch[0] != calls[1]._scratch[0]
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    for _ in range(50):
+        for graph, stream in zip(graphs, streams):
+            with torch.cuda.stream(stream):
+                graph.replay()
+    torch.cuda.synchronize()
+    for i in range(2):
+        assert all(torch.equal(a, b) for a, b in zip(want[i], (*steps[i][3:], c.weights(i))))
+
+
 def test_cache_refusals():
     c, _ = _filled()
     z = torch.zeros(5, 2, 64, device=DEV, dtype=torch.bfloat16)
