@@ -153,7 +153,8 @@ class DLLM:
         else:
             attention = prefix.attention(*step)
             pos = batch.pos + prefix.start
-            lse = torch.empty(rows, cfg.hq, device=self.device) if weigh else None
+            # (+inf: a row that the attention does not write adds no weight)
+            lse = torch.full((rows, cfg.hq), torch.inf, device=self.device) if weigh else None
         delta = None  # experts only: the last MLP's output, not yet added to h
         for i, L in enumerate(self.layers):
             if cfg.experts > 0:

@@ -151,6 +151,24 @@ def test_forward_behind_a_prefix(experts):
     assert ((total > 0) & (total < rows)).all()
 
 
+def test_forward_rows_without_output_add_no_weight():
+    """Shadow rows with a repeated source are not stored, and add nothing to the keys' weights."""
+    cfg = D.ModelConfig(vocab=128, d_model=128, n_layers=1, hq=4, hkv=2, head_dim=64, mlp=128)
+    model = D.DLLM(cfg, seed=2)
+    rng = np.random.default_rng(0)
+    prefix = model.cache_prefix(rng.integers(0, 127, 150).astype(np.int32))
+    batch = D.make_batch([rng.integers(0, 127, 5).astype(np.int32)], 16, 8, 0, None, cfg, DEV)
+    batch.shadow_src[2:] = batch.shadow_src[1]
+    rows = batch.tokens.numel()
+    for _ in range(8):  # what the allocator hands out next is no number
+        torch.full((rows, cfg.hq), torch.nan, device=DEV)
+    model.forward(batch, prefix=prefix, weigh=True)
+    w = prefix.weights(0)
+    assert torch.isfinite(w).all() and (w >= 0).all()
+    # every stored row (all but six) spends at most a weight of 1 per head
+    assert float(w.sum()) <= (rows - 6) * cfg.hq * (1 + 1e-3)
+
+
 @pytest.mark.parametrize("keep", [0, 40])
 def test_decode_behind_a_prefix(keep):
     cfg = D.ModelConfig(vocab=128, d_model=128, n_layers=2, hq=4, hkv=2, head_dim=64, mlp=128,
