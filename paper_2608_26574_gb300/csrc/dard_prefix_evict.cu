@@ -10,7 +10,8 @@
 // finds the digit with one scan over its threads. Then each warp counts its kept candidates, a scan
 // over warps and CTAs places them, and ballots place each within its warp. Nothing depends on the
 // order of the atomics: they only count. Bound by the barriers of the rounds (two of the cluster
-// each), not by the weights' bytes: 29 us for 32 heads of 65537 weights (8 MB), 5 for 704.
+// each) and, of long rows, by the passes over them (five; four loads of a lane in flight: 29 -> 26 us for
+// 32 heads of 65537 weights, 8 MB), not by their bytes; 5 us for 704.
 // evict_copy: 16 bytes of K and of V per thread and step, rows in the order of the outputs.
 #include <algorithm>
 #include <cstdio>
@@ -39,6 +40,7 @@ struct EvictParams {
 constexpr int kSelThreads = 1024, kSelWarps = 32;
 constexpr int kBins = 2048;
 constexpr int kMaxCluster = 8;
+constexpr int kAhead = 4;  // a lane's weights in flight
 
 // Order-preserving: a larger weight has a larger key; -0 as 0, NaN below everything.
 __device__ __forceinline__ uint32_t key_of(float w) {
@@ -98,6 +100,24 @@ __global__ void __launch_bounds__(kSelThreads, 1) evict_select(const __grid_cons
   const long long unit = static_cast<long long>(rank) * kSelWarps + warp;
   const int a = lo + static_cast<int>(n * unit / units), b = lo + static_cast<int>(n * (unit + 1) / units);
 
+  // f(index, weight, whether there is one) for the run, 32 at a time in order; kAhead loads in flight
+  auto each = [&](auto f) {
+    for (int i0 = a; i0 < b; i0 += 32 * kAhead) {
+      float x[kAhead];
+#pragma unroll
+      for (int u = 0; u < kAhead; ++u) {
+        const int i = i0 + 32 * u + lane;
+        x[u] = i < b ? __ldg(w + i) : 0.f;
+      }
+#pragma unroll
+      for (int u = 0; u < kAhead; ++u) {
+        if (i0 + 32 * u >= b) break;
+        const int i = i0 + 32 * u + lane;
+        f(i, x[u], i < b);
+      }
+    }
+  };
+
   uint32_t prefix = 0, need = want;  // digits found so far; how many of their candidates are kept
   for (int i = tid; i < 2 * kBins; i += kSelThreads) sh.hist[0][i] = 0;
   sync_head(ctas);
@@ -106,11 +126,10 @@ __global__ void __launch_bounds__(kSelThreads, 1) evict_select(const __grid_cons
     const int shift = round == 0 ? 21 : round == 1 ? 10 : 0, bins = round == 2 ? 1024 : 2048;
     const uint32_t done = round == 0 ? 0u : round == 1 ? 0xffe00000u : 0xfffffc00u;
     uint32_t* hist = sh.hist[round & 1];
-#pragma unroll 4
-    for (int i = a + lane; i < b; i += 32) {
-      const uint32_t key = key_of(__ldg(w + i));
-      if ((key & done) == prefix) atomicAdd(&hist[key >> shift & (bins - 1)], 1u);
-    }
+    each([&](int, float x, bool in) {
+      const uint32_t key = key_of(x);
+      if (in && (key & done) == prefix) atomicAdd(&hist[key >> shift & (bins - 1)], 1u);
+    });
     if (ctas > 1) {
       __syncthreads();
       if (rank != 0)
@@ -151,11 +170,11 @@ __global__ void __launch_bounds__(kSelThreads, 1) evict_select(const __grid_cons
   }
   // `prefix` is the smallest kept key, of which the first `need` are kept
   uint32_t gt = 0, eq = 0;
-  for (int i = a + lane; i < b; i += 32) {
-    const uint32_t key = key_of(__ldg(w + i));
-    gt += key > prefix;
-    eq += key == prefix;
-  }
+  each([&](int, float x, bool in) {
+    const uint32_t key = key_of(x);
+    gt += in && key > prefix;
+    eq += in && key == prefix;
+  });
   gt = __reduce_add_sync(0xffffffffu, gt);
   eq = __reduce_add_sync(0xffffffffu, eq);
   if (lane == 0) {
@@ -189,26 +208,25 @@ __global__ void __launch_bounds__(kSelThreads, 1) evict_select(const __grid_cons
     sh.base_eq = by;
   }
   sync_head(ctas);
-  gt = sh.base_gt + sh.warp_gt[warp];
   eq = sh.base_eq + sh.warp_eq[warp];
+  int at = p.first + static_cast<int>(sh.base_gt + sh.warp_gt[warp] + min(eq, need));  // the next kept key's place
   const uint32_t below = (1u << lane) - 1;
-  for (int i0 = a; i0 < b; i0 += 32) {
-    const int i = i0 + lane;
-    const float wi = i < b ? __ldg(w + i) : 0.f;
-    const uint32_t key = key_of(wi);
-    const uint32_t is_gt = __ballot_sync(0xffffffffu, i < b && key > prefix);
-    const uint32_t is_eq = __ballot_sync(0xffffffffu, i < b && key == prefix);
-    const uint32_t my_gt = gt + __popc(is_gt & below), my_eq = eq + __popc(is_eq & below);
-    if ((is_gt >> lane & 1u) || ((is_eq >> lane & 1u) && my_eq < need)) {
-      const int to = p.first + static_cast<int>(my_gt + min(my_eq, need));
-      if (to < p.keep - p.last) {  // (always, unless the weights change under the call)
-        kept[to] = i;
-        if (w_out) w_out[to] = wi;
-      }
+  each([&](int i, float x, bool in) {
+    const uint32_t key = key_of(x);
+    bool take = in && key > prefix;
+    const uint32_t equal = __ballot_sync(0xffffffffu, in && key == prefix);
+    if (equal != 0) {
+      take |= (equal >> lane & 1u) && eq + __popc(equal & below) < need;
+      eq += __popc(equal);
     }
-    gt += __popc(is_gt);
-    eq += __popc(is_eq);
-  }
+    const uint32_t taken = __ballot_sync(0xffffffffu, take);
+    const int to = at + __popc(taken & below);
+    if (take && to < p.keep - p.last) {  // (always, unless the weights change under the call)
+      kept[to] = i;
+      if (w_out) w_out[to] = x;
+    }
+    at += __popc(taken);
+  });
 }
 
 // Each thread moves the same 16-byte chunk of kRowsPer consecutive output rows' K and V: kRowsPer
@@ -341,8 +359,11 @@ extern "C" dard_status dard_prefix_evict(const dard_prefix_evict_args* args, voi
     return report(DARD_ERR_CUDA, "prefix eviction launch failed: %s (DARD_TEST_FAIL_LAUNCH)",
                   cudaGetErrorString(cudaErrorLaunchFailure));
   const cudaStream_t stream = static_cast<cudaStream_t>(stream_ptr);
-  int ctas = 1;  // of a head
-  while (ctas < kMaxCluster && p.prefix_len / ctas > 8192 && 2ll * ctas * p.hkv <= sm_count()) ctas *= 2;
+  // CTAs of a head: one up to 8192 keys, as the cluster's barriers cost 3.5 us (8 heads of 4099 keys: 9.7 us
+  // with one CTA, 13.3 with two), then one per 4096 (8 heads of 16384: 19.9 us with two, 17.6 with four)
+  int ctas = 1;
+  while (ctas < kMaxCluster && p.prefix_len > std::max(8192, 4096 * ctas) && 2ll * ctas * p.hkv <= sm_count())
+    ctas *= 2;
   const AttnLaunch S(static_cast<unsigned>(p.hkv) * ctas, kSelThreads, 0, stream, ctas, false);
   cudaError_t e = cudaLaunchKernelEx(&S.cfg, evict_select, p, ctas);
   if (e == cudaSuccess && p.k) {

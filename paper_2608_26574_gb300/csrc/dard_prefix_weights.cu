@@ -15,9 +15,9 @@
 //   warps 26, 27 the queries' normalisers through 6 stages, every other tile each (one warp took 800
 //              cycles a tile, more than the products do).
 // TMEM: S ring [0, 384), K [448, 448 + D/2). Bound by the issue slots of the exponentials and by TMEM,
-// which the products' A operand and the workers' reads share: about 940 cycles per 128 x 128 scores, of
-// which the tensor cores work 512. Measured: 4608 rows of 28 heads on 4 of 128 over 32768 keys 864-920 us
-// (1180-1250 TFLOP/s; 688 without the exponentials); with K in shared memory 960.
+// which the products' A operand and the workers' reads share: about 915 cycles per 128 x 128 scores, of
+// which the tensor cores work 512. Measured: 4608 rows of 28 heads on 4 of 128 over 32768 keys 842-900 us
+// (1200-1285 TFLOP/s; 688 without the exponentials); with K in shared memory 960.
 // Each tile's sum is formed on its own and then added to the key's total (two levels: the
 // rounding of a long sum grows with the number of tiles, not of queries).
 #include <algorithm>
