@@ -292,9 +292,12 @@ __global__ void __launch_bounds__(kF32Threads) prefix_f32(const __grid_constant_
 // its 512 bytes' time even where it is a broadcast. Scores: a half-warp takes a key, a thread every 16th
 // chunk of it and of four queries, which stay in registers; 16 sums (four keys' with four queries) are
 // added up over the half-warp by 15 shuffles that leave one to each thread (its registers hold them in an
-// order of its own, the one that ends up in it first, so that no step has to select). Then warp r takes query r's
-// online softmax step, its weights in place of the scores; products with V: thread (key group, column) adds
-// eight queries' columns over its keys, and the groups are added up at the end.
+// order of its own, the one that ends up in it first, so that no step has to select). Then warp r takes query
+// r's online softmax step, its weights in place of the scores; products with V: thread (key group, column)
+// adds eight queries' columns over its keys, and the groups are added up at the end.
+// Two CTAs to an SM hide each other's waits; bound by the issue of instructions (a third of them FMAs) beside
+// HBM: one token of 28 heads on 4 of 128 over 65536 keys (268 MB) 52 us, 40 at the copy's rate; with three
+// CTAs of 80 registers 84, with bounds checked at every copy and selects in the shuffles' steps 73.
 constexpr int kFewRows = kF32FewRows;
 constexpr int kFewStride = kF32Keys + 4;  // of a row of scores
 

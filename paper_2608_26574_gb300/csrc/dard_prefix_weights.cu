@@ -16,8 +16,9 @@
 //              cycles a tile, more than the products do).
 // TMEM: S ring [0, 384), K [448, 448 + D/2). Bound by the issue slots of the exponentials and by TMEM,
 // which the products' A operand and the workers' reads share: about 915 cycles per 128 x 128 scores, of
-// which the tensor cores work 512. Measured: 4608 rows of 28 heads on 4 of 128 over 32768 keys 842-900 us
-// (1200-1285 TFLOP/s; 688 without the exponentials); with K in shared memory 960.
+// which the tensor cores work 512. Measured: 4608 rows of 28 heads on 4 of 128 over 32768 keys 845-980 us
+// (1100-1280 TFLOP/s; the more, the more sums exact_sum32 forms again; 688 without the exponentials); with K
+// in shared memory 960 instead of 870.
 // Each tile's sum is formed on its own and then added to the key's total (two levels: the
 // rounding of a long sum grows with the number of tiles, not of queries).
 #include <algorithm>
@@ -43,11 +44,18 @@ struct WeightsParams {
   int32_t box_heads, box_rows, head_blocks;  // a query tile: box_rows rows x box_heads heads
   int32_t q_tiles, key_tiles, nsplit;
   float scale_log2, decay;
+  float lse_hi, lse_lo;      // what lse is multiplied with, in two parts
+  double scale;              // of the scores, times log2 e: scale_log2 before its rounding
   long long wait_cycles;
   int32_t test_drop_kv;
 };
 
 constexpr float kLog2e = 1.4426950408889634f;
+
+// -lse in the unit in which scale_log2 takes the scores.
+__device__ __forceinline__ float lse_unit(const WeightsParams& p, float lse) {
+  return fabsf(lse) == INFINITY ? -lse : fmaf(lse, p.lse_hi, lse * p.lse_lo);
+}
 
 // Adds what the earlier sum contributes.
 __device__ __forceinline__ float with_earlier(const WeightsParams& p, int g, int key, float sum) {
@@ -109,6 +117,59 @@ __device__ __forceinline__ float sum32(const uint32_t (&s)[32], const float* lse
   float a, b;
   f2_unpack(f2_add(f2_add(acc[0], acc[1]), f2_add(acc[2], acc[3])), a, b);
   return a + b;
+}
+
+// Sums above `large` (some lane's of the warp) once more, with exact scores: the tensor cores cut the bits that
+// a running sum has no room for, which takes up to two units in the last place off a large score, 3.4e-6 of
+// its exponential at a score of 35 and more where small products follow large ones. `large` is a quarter of
+// the columns, which is the most that so many queries' weights add up to where their lse is over these keys: a
+// few keys reach it, and where lse is over others (a part of them, a cache that has changed since) single terms
+// may be as large as they like, and are a key's whole sum. Key by key for those that need it, a lane for each
+// of the 32 columns from `first` on; eight products at a time, their sums added up with what the roundings cut
+// off. 4608 rows of 28 heads over 32768 keys: 842 us without it, 845-850 while no sum is that large, 887-983 with
+// lse over 256 of the keys, where the largest error against 64 bits goes from 3.8e-6 to 0.6e-6 (above all of the
+// columns 868-931, an eighth 901-1018); one row over 4096 keys 7.7 instead of 5.7 us. Not inlined: the loop that
+// calls it has no register to spare (inlined 1630 us).
+__device__ __forceinline__ float dot2(uint32_t a, uint32_t b, float c) {  // bf16 pairs
+  c = fmaf(__uint_as_float(a << 16), __uint_as_float(b << 16), c);
+  return fmaf(__uint_as_float(a & 0xffff0000u), __uint_as_float(b & 0xffff0000u), c);
+}
+template <int D>
+__device__ __noinline__ float exact_sum32(const WeightsParams& p, float sum, float large, int g, int key, int tile,
+                                           int first) {
+  const int lane = threadIdx.x & 31, c = first + lane;
+  const int row = tile / p.head_blocks * p.box_rows + c / p.box_heads;
+  const int head = tile % p.head_blocks * p.box_heads + c % p.box_heads;  // of the group
+  const bool in = c < p.box_rows * p.box_heads && row < p.rows && head < p.group;
+  const int64_t query = static_cast<int64_t>(row) * p.hq + g * p.group + head;  // this lane's, if it is one
+  const float lse = in ? __ldg(p.lse + query) : INFINITY;
+  for (uint32_t lanes = __ballot_sync(0xffffffffu, sum > large && key < p.prefix_len); lanes; lanes &= lanes - 1) {
+    const int of = __ffs(lanes) - 1;
+    const int at = __shfl_sync(0xffffffffu, key, of);
+    float x = 0.f;
+    if (in) {
+      const uint4* k = reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(p.pk) + at * p.row_stride +
+                                                      g * p.head_stride);
+      const uint4* q = reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(p.q) + query * D);
+      float z = 0.f, left = 0.f;  // the sum, and what its roundings have left out
+#pragma unroll 4
+      for (int i = 0; i < D / 8; ++i) {
+        const uint4 u = __ldg(k + i), v = __ldg(q + i);
+        const float dot = dot2(u.x, v.x, dot2(u.y, v.y, dot2(u.z, v.z, dot2(u.w, v.w, 0.f))));
+        const float to = z + dot, added = to - z;
+        left += (z - (to - added)) + (dot - added);
+        z = to;
+      }
+      if (left != left) left = 0.f;  // (z is infinite)
+      // (with lse = +inf q may hold anything)
+      if (lse != INFINITY)
+        x = ex2_approx(static_cast<float>((static_cast<double>(z) + left) * p.scale - lse * 1.4426950408889634));
+    }
+#pragma unroll
+    for (int i = 16; i > 0; i >>= 1) x += __shfl_xor_sync(0xffffffffu, x, i);
+    if (lane == of) sum = x;
+  }
+  return sum;
 }
 
 template <int D>
@@ -269,7 +330,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         // a query whose lse is +inf adds nothing (columns without a query or behind the last row
         // need no bit: their scores are 0)
         const uint32_t bits = __ballot_sync(0xffffffffu, v[0][e] == INFINITY && 32 * e + lane < columns);
-        ctl.lse[b][32 * e + lane] = v[0][e] * -kLog2e;
+        ctl.lse[b][32 * e + lane] = lse_unit(p, v[0][e]);
         if (lane == 0) ctl.off[b][e] = bits;
       }
       __syncwarp();
@@ -300,6 +361,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     const int turn = warp >> 3, half = part & 1;  // tiles turn, turn + 3 ..; queries 64 half ..
     const uint32_t tS = ctl.tmem_base + turn * kTN + 64 * half + lane_off;
     const uint64_t sl2 = f2_pack(p.scale_log2, p.scale_log2);
+    const float large = 0.25f * min(columns, 32);  // sums above it are formed again
     float total = 0.f;
     bool ok = true, ready = false;
     int b = turn;  // stage of the tile, and the parity of its use
@@ -316,14 +378,20 @@ __global__ void __launch_bounds__(kThreads, 1)
       tmem_ld32(tS, r);
       tmem_wait_ld();
       float sum = 0.f;
-      if (64 * half < columns) sum = off0 == 0 ? sum32<false>(r, lse, 0, sl2) : sum32<true>(r, lse, off0, sl2);
+      if (64 * half < columns) {
+        sum = off0 == 0 ? sum32<false>(r, lse, 0, sl2) : sum32<true>(r, lse, off0, sl2);
+        if (__any_sync(0xffffffffu, sum > large)) sum = exact_sum32<D>(p, sum, large, g, key, j0 + j, 64 * half);
+      }
       tmem_ld32(tS + 32, r);
       tmem_wait_ld();
       tc_fence_before();
       __syncwarp();
       if (lane == 0) mbar_arrive(&ctl.s_free[turn]);
-      if (64 * half + 32 < columns)
-        sum += off1 == 0 ? sum32<false>(r, lse + 32, 0, sl2) : sum32<true>(r, lse + 32, off1, sl2);
+      if (64 * half + 32 < columns) {
+        float more = off1 == 0 ? sum32<false>(r, lse + 32, 0, sl2) : sum32<true>(r, lse + 32, off1, sl2);
+        if (__any_sync(0xffffffffu, more > large)) more = exact_sum32<D>(p, more, large, g, key, j0 + j, 64 * half + 32);
+        sum += more;
+      }
       // the next tile's stage, and whether it is there (asked ahead)
       const int b_now = b;
       if ((b += kGroups) >= kQStages) {
@@ -406,8 +474,8 @@ __global__ void __launch_bounds__(kFThreads) weights_f32(const __grid_constant__
     cp_async_commit();
     if (tid < kFQueries) {
       const int64_t m = static_cast<int64_t>(j) * kFQueries + tid;
-      sL[b * kFQueries + tid] =
-          m < queries ? __ldg(p.lse + m / p.group * p.hq + g * p.group + m % p.group) * kLog2e : INFINITY;
+      sL[b * kFQueries + tid] = lse_unit(
+          p, m < queries ? __ldg(p.lse + m / p.group * p.hq + g * p.group + m % p.group) : INFINITY);
     }
   };
   load(j0, 0);
@@ -445,9 +513,9 @@ __global__ void __launch_bounds__(kFThreads) weights_f32(const __grid_constant__
 #pragma unroll
     for (int i = 0; i < kI; ++i) {
       const float lse = sL[b * kFQueries + tx + 16 * i];
-      if (lse == INFINITY) continue;  // adds nothing, whatever q holds
+      if (lse == -INFINITY) continue;  // adds nothing, whatever q holds
 #pragma unroll
-      for (int u = 0; u < kU; ++u) total[u] += exp2f(fmaf(s[u][i], p.scale_log2, -lse));
+      for (int u = 0; u < kU; ++u) total[u] += exp2f(fmaf(s[u][i], p.scale_log2, lse));
     }
   }
 #pragma unroll
@@ -579,6 +647,15 @@ dard_status prepare(const dard_prefix_weights_args* a, WeightsParams& p) {
   p.group = a->hq / a->hkv;
   p.decay = a->decay;
   p.scale_log2 = (a->scale > 0.f ? a->scale : 1.0f / std::sqrt(static_cast<float>(a->head_dim))) * kLog2e;
+  p.scale = (a->scale > 0.f ? static_cast<double>(a->scale) : 1.0 / std::sqrt(static_cast<double>(a->head_dim))) *
+            1.4426950408889634;
+  // lse in the unit in which scale_log2, rounded to 32 bits, takes the scores: its rounding then counts for their
+  // difference only. From the tensor cores scores come short by 3e-10 per element of a head on average, as a
+  // running sum is cut (with this keys' weights of random q and k are off by 1e-7 on average, without by 4e-7).
+  const double unit = p.scale_log2 / p.scale * 1.4426950408889634 /
+                      (a->dtype == DARD_BF16 ? 1.0 + 3e-10 * a->head_dim : 1.0);
+  p.lse_hi = static_cast<float>(-unit);
+  p.lse_lo = static_cast<float>(-unit - p.lse_hi);
   p.test_drop_kv = -1;
   return DARD_OK;
 }

@@ -449,6 +449,30 @@ def test_weights_all_rows_off_and_no_rows():
     assert (weigh(t["q"][:0], lse[:0], t["pk"]) == 0).all()
 
 
+@pytest.mark.parametrize("ws", [True, False])
+@pytest.mark.parametrize("d,hq,hkv,rows,prefix", [(64, 4, 2, 40, 200), (128, 6, 2, 77, 300), (128, 1, 1, 1, 1),
+                                                  (128, 130, 1, 3, 129), (64, 3, 3, 200, 64)])
+def test_weights_of_large_scores(d, hq, hkv, rows, prefix, ws):
+    """Scores of 512 beside 1e-4 per element, far above their lse: an fp32 sum of them that is cut or
+    rounded element by element is off by up to a unit of 6e-5 each time, times 1 / sqrt(d) the relative
+    error of the weight (6e-5 to 9e-5 here without exact scores). They leave the rounding of the exponent (below 32 in base 2:
+    32 * 2^-24 * ln 2 = 1.4e-6), of the exponential (2^-22) and of the sums (16 * 2^-24)."""
+    g = torch.Generator(device=DEV).manual_seed(d + rows)
+
+    def make_rows(n, h):
+        x = 1 + torch.randint(0, 128, (n, h, d), generator=g, device=DEV) / 128  # 8 bits
+        x *= 2.0 ** -7
+        x[..., :8] = 8.0
+        return x.to(torch.bfloat16)
+    q, pk = make_rows(rows, hq), make_rows(prefix, hkv)
+    lse = 512 / d ** 0.5 - 10 - torch.rand(rows, hq, generator=g, device=DEV)
+    got = weigh(q, lse, pk, None, 0.5, ws)
+    want = O.prefix_weights(_np(q), _np(lse), _np(pk))[0]
+    assert want.min() > 2e4
+    rel = np.abs(_np(got) - want) / want
+    assert rel.max() <= 32 * U * math.log(2) + 2.0 ** -22 + 16 * U, rel.max()
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_weights_strides(dtype):
     _, t = make(dtype, 6, 3, 64, 201, [(30, 0, 0, 0)], 11)
