@@ -59,7 +59,9 @@ struct SelShared {
 };
 
 __device__ __forceinline__ void add_cluster(uint32_t* p, uint32_t rank, uint32_t v) {
-  asm volatile("red.relaxed.cluster.shared::cluster.add.u32 [%0], %1;" ::"r"(map_shared_rank(smem_u32(p), rank)), "r"(v) : "memory");
+  asm volatile("red.relaxed.cluster.shared::cluster.add.u32 [%0], %1;" ::"r"(map_shared_rank(smem_u32(p), rank)),
+               "r"(v)
+               : "memory");
 }
 __device__ __forceinline__ void st_cluster(uint32_t* p, uint32_t rank, uint32_t v) {
   asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(map_shared_rank(smem_u32(p), rank)), "r"(v) : "memory");

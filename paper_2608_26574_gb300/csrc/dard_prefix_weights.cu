@@ -44,6 +44,7 @@ struct WeightsParams {
   int32_t box_heads, box_rows, head_blocks;  // a query tile: box_rows rows x box_heads heads
   int32_t q_tiles, key_tiles, nsplit;
   float scale_log2, decay;
+  float large;               // bf16: sums of 32 columns above it are formed again (exact_sum32)
   float lse_hi, lse_lo;      // what lse is multiplied with, in two parts
   double scale;              // of the scores, times log2 e: scale_log2 before its rounding
   long long wait_cycles;
@@ -119,31 +120,31 @@ __device__ __forceinline__ float sum32(const uint32_t (&s)[32], const float* lse
   return a + b;
 }
 
-// Sums above `large` (some lane's of the warp) once more, with exact scores: the tensor cores cut the bits that
+// Sums above p.large (some lane's of the warp) once more, with exact scores: the tensor cores cut the bits that
 // a running sum has no room for, which takes up to two units in the last place off a large score, 3.4e-6 of
-// its exponential at a score of 35 and more where small products follow large ones. `large` is a quarter of
-// the columns, which is the most that so many queries' weights add up to where their lse is over these keys: a
-// few keys reach it, and where lse is over others (a part of them, a cache that has changed since) single terms
-// may be as large as they like, and are a key's whole sum. Key by key for those that need it, a lane for each
-// of the 32 columns from `first` on; eight products at a time, their sums added up with what the roundings cut
-// off. 4608 rows of 28 heads over 32768 keys: 842 us without it, 845-850 while no sum is that large, 887-983 with
-// lse over 256 of the keys, where the largest error against 64 bits goes from 3.8e-6 to 0.6e-6 (above all of the
-// columns 868-931, an eighth 901-1018); one row over 4096 keys 7.7 instead of 5.7 us. Not inlined: the loop that
-// calls it has no register to spare (inlined 1630 us).
+// its exponential at a score of 35 and more where small products follow large ones. p.large is a quarter of
+// the columns and twice a key's share of them, but not more than all, which is the most that so many queries'
+// weights add up to where their lse is over these keys: a few keys reach it, and where lse is over others (a
+// part of them, a cache that has changed since) single terms may be as large as they like, and are a key's
+// whole sum. (1111 rows of 32 heads over two keys: 13.7 us, 48 without the share.) Key by key for those that
+// need it, a lane for each of the 32 columns from `first` on; eight products at a time, their sums added up
+// with what the roundings cut off. 4608 rows of 28 heads over 32768 keys: 842 us without it, 845-850 while no
+// sum is that large, 887-983 with lse over 256 of the keys, where the largest error against 64 bits goes from
+// 3.8e-6 to 0.6e-6 (above all of the columns 868-931, an eighth 901-1018); one row over 4096 keys 7.7 instead
+// of 5.7 us. Not inlined: the loop that calls it has no register to spare (inlined 1630 us).
 __device__ __forceinline__ float dot2(uint32_t a, uint32_t b, float c) {  // bf16 pairs
   c = fmaf(__uint_as_float(a << 16), __uint_as_float(b << 16), c);
   return fmaf(__uint_as_float(a & 0xffff0000u), __uint_as_float(b & 0xffff0000u), c);
 }
 template <int D>
-__device__ __noinline__ float exact_sum32(const WeightsParams& p, float sum, float large, int g, int key, int tile,
-                                           int first) {
+__device__ __noinline__ float exact_sum32(const WeightsParams& p, float sum, int g, int key, int tile, int first) {
   const int lane = threadIdx.x & 31, c = first + lane;
   const int row = tile / p.head_blocks * p.box_rows + c / p.box_heads;
   const int head = tile % p.head_blocks * p.box_heads + c % p.box_heads;  // of the group
   const bool in = c < p.box_rows * p.box_heads && row < p.rows && head < p.group;
   const int64_t query = static_cast<int64_t>(row) * p.hq + g * p.group + head;  // this lane's, if it is one
   const float lse = in ? __ldg(p.lse + query) : INFINITY;
-  for (uint32_t lanes = __ballot_sync(0xffffffffu, sum > large && key < p.prefix_len); lanes; lanes &= lanes - 1) {
+  for (uint32_t lanes = __ballot_sync(0xffffffffu, sum > p.large && key < p.prefix_len); lanes; lanes &= lanes - 1) {
     const int of = __ffs(lanes) - 1;
     const int at = __shfl_sync(0xffffffffu, key, of);
     float x = 0.f;
@@ -361,7 +362,6 @@ __global__ void __launch_bounds__(kThreads, 1)
     const int turn = warp >> 3, half = part & 1;  // tiles turn, turn + 3 ..; queries 64 half ..
     const uint32_t tS = ctl.tmem_base + turn * kTN + 64 * half + lane_off;
     const uint64_t sl2 = f2_pack(p.scale_log2, p.scale_log2);
-    const float large = 0.25f * min(columns, 32);  // sums above it are formed again
     float total = 0.f;
     bool ok = true, ready = false;
     int b = turn;  // stage of the tile, and the parity of its use
@@ -380,7 +380,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       float sum = 0.f;
       if (64 * half < columns) {
         sum = off0 == 0 ? sum32<false>(r, lse, 0, sl2) : sum32<true>(r, lse, off0, sl2);
-        if (__any_sync(0xffffffffu, sum > large)) sum = exact_sum32<D>(p, sum, large, g, key, j0 + j, 64 * half);
+        if (__any_sync(0xffffffffu, sum > p.large)) sum = exact_sum32<D>(p, sum, g, key, j0 + j, 64 * half);
       }
       tmem_ld32(tS + 32, r);
       tmem_wait_ld();
@@ -389,7 +389,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       if (lane == 0) mbar_arrive(&ctl.s_free[turn]);
       if (64 * half + 32 < columns) {
         float more = off1 == 0 ? sum32<false>(r, lse + 32, 0, sl2) : sum32<true>(r, lse + 32, off1, sl2);
-        if (__any_sync(0xffffffffu, more > large)) more = exact_sum32<D>(p, more, large, g, key, j0 + j, 64 * half + 32);
+        if (__any_sync(0xffffffffu, more > p.large)) more = exact_sum32<D>(p, more, g, key, j0 + j, 64 * half + 32);
         sum += more;
       }
       // the next tile's stage, and whether it is there (asked ahead)
@@ -716,6 +716,7 @@ dard_status dard_prefix_weights(const dard_prefix_weights_args* args, void* stre
       p.box_rows = std::min(128 / p.box_heads, p.rows);
       p.head_blocks = (p.group + p.box_heads - 1) / p.box_heads;
       p.q_tiles = (p.rows + p.box_rows - 1) / p.box_rows * p.head_blocks;
+      p.large = std::min(32, p.box_rows * p.box_heads) * std::min(1.0f, 0.25f + 2.0f / p.prefix_len);
     } else {
       p.q_tiles = static_cast<int32_t>((static_cast<long long>(p.rows) * p.group + kFQueries - 1) / kFQueries);
     }
