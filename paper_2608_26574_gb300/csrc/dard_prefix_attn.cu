@@ -531,10 +531,11 @@ __global__ void __launch_bounds__(128, 6) prefix_join(const __grid_constant__ Jo
     float most = fmaxf(top, mc);
 #pragma unroll
     for (int x = 16; x > 0; x >>= 1) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, x));
-    // (a part without a key has no weight; a maximum that is NaN makes its part NaN)
+    // (A maximum of -inf: no key, or none with a weight, and a sum of 0; or, as maxima pass NaN over, scores
+    // that are all NaN beside such keys, and a sum of NaN, which 0 times it lets through.)
     const float f = mc == -INFINITY ? 0.f : mc == most ? 1.f : ex2_approx(mc - most);
     const float back = top == -INFINITY ? 0.f : top == most ? 1.f : ex2_approx(top - most);
-    float lf = mc == -INFINITY ? 0.f : f * lc;
+    float lf = f * lc;
 #pragma unroll
     for (int x = 16; x > 0; x >>= 1) lf += __shfl_xor_sync(0xffffffffu, lf, x);
     l = l * back + lf;
@@ -576,7 +577,6 @@ __global__ void __launch_bounds__(128, 6) prefix_join(const __grid_constant__ Jo
 #pragma unroll
     for (int k = 0; k < kWarps; ++k) {
       const float f = s_top[k] == -INFINITY ? 0.f : s_top[k] == most ? 1.f : ex2_approx(s_top[k] - most);
-      if (s_top[k] == -INFINITY && s_l[k] == s_l[k]) continue;
       l = fmaf(f, s_l[k], l);
 #pragma unroll
       for (int e = 0; e < kV; ++e) o[e] = fmaf(f, s_o[k][lane * kV + e], o[e]);

@@ -1,0 +1,65 @@
+"""The shared prefix's operators where sums of many parts, values that are not finite and roundings
+meet, against the float64 oracle (helpers and tolerances as in test_gpu_prefix.py)."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+from oracle import prefix_oracle as O
+
+from . import test_gpu_prefix as T
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda"
+U = T.U
+
+
+def _same_nan(lays, t, ws):
+    o, ls = T.attend(lays, t, ws=ws)
+    want, wl = O.prefix_attention(*(T._np(t[x]) for x in ("q", "k", "v", "pk", "pv")), lays)[:2]
+    assert np.array_equal(np.isnan(T._np(o)), np.isnan(want))
+    assert np.array_equal(np.isnan(T._np(ls)), np.isnan(wl))
+    fin = np.isfinite(wl)
+    assert np.abs(T._np(ls)[fin] - wl[fin]).max(initial=0.0) <= 1e-4
+    return want
+
+
+PART_CASES = [("bf16", 28, 4, 128, 4096, [(1, 0, 0, 0)]), ("f32", 28, 4, 128, 4096, [(1, 0, 0, 0)]),
+              ("bf16", 28, 4, 64, 2000, [(0, 5, 0, 5)] * 2), ("f32", 28, 4, 64, 1900, [(0, 64, 0, 64)] * 3)]
+
+
+@pytest.mark.parametrize("ws", [True, False])
+@pytest.mark.parametrize("dtype,hq,hkv,d,prefix,seqs", PART_CASES)
+@pytest.mark.parametrize("first,n", [(0, 128), (0, 1024), (256, 64), (1024, 512), (1800, 2200), (0, 5000)])
+def test_attention_nan_throughout_a_part(dtype, hq, hkv, d, prefix, seqs, first, n, ws):
+    """Runs of NaN keys that fill whole parts of a split (one, a quarter of them, all): every row sees
+    them, so that its output and its normaliser are NaN, in parts or not."""
+    lays, t = T.make(dtype, hq, hkv, d, prefix, seqs, 5)
+    t["pk"][first:first + n, 1, 3] = math.nan
+    want = _same_nan(lays, t, ws)
+    assert np.isnan(want[:, hq // hkv:2 * hq // hkv]).all() and np.isfinite(want[:, :hq // hkv]).all()
+
+
+@pytest.mark.parametrize("ws", [True, False])
+@pytest.mark.parametrize("dtype,hq,hkv,d,prefix,seqs", PART_CASES)
+def test_attention_nan_in_the_last_part(dtype, hq, hkv, d, prefix, seqs, ws):
+    """A row whose own keys alone are NaN (the last part of a split may hold nothing else)."""
+    lays, t = T.make(dtype, hq, hkv, d, prefix, seqs, 5)
+    t["k"][:lays[0].rows, 2] = math.nan
+    want = _same_nan(lays, t, ws)
+    assert np.isnan(want).any() and np.isfinite(want).any()
+
+
+@pytest.mark.parametrize("ws", [True, False])
+@pytest.mark.parametrize("dtype,hq,hkv,d,prefix,seqs", PART_CASES)
+def test_attention_nan_query_and_parts_without_weight(dtype, hq, hkv, d, prefix, seqs, ws):
+    """A NaN query head: NaN, its normaliser too. Keys whose scores are -inf over whole parts have no
+    weight, and the other keys' sum is left as it is; a NaN value behind one of them is seen all the same."""
+    lays, t = T.make(dtype, hq, hkv, d, prefix, seqs, 5)
+    t["q"][..., 3] = t["q"][..., 3].abs() + 0.5
+    t["pk"][:1200, :, 3] = -math.inf
+    t["pv"][100, 3, 5] = math.nan
+    t["q"][0, 2, 7] = math.nan
+    want = _same_nan(lays, t, ws)
+    assert np.isnan(want[0, 2]).all() and np.isfinite(want[0, 3]).all() and np.isnan(want[:, -1, 5]).all()
