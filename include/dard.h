@@ -529,7 +529,8 @@ dard_status dard_experts(const dard_experts_args* args, void* stream);
  * Rows that are no query rows (before query_start, and shadow rows with an invalid shadow_src) are
  * left as they were in o and in lse.
  * Arithmetic: as dard_step_attention (probabilities rounded to bf16 for the product with the
- * values when dtype is BF16; the normaliser in lse is that of the unrounded ones). */
+ * values when dtype is BF16, and divided by the sum of the rounded ones; the normaliser in lse is
+ * that of the unrounded ones). */
 typedef struct {
   dard_attn_args own;        /* the sequences' own rows, as dard_step_attention takes them;
                                 rope_theta must be 0 (q and k carry their positions)       */

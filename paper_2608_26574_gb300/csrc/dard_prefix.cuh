@@ -31,11 +31,12 @@ struct PrefixParams {
   uint8_t tile_seq[kTileTable][2];      // first and last sequence of a query tile, if all fit in
 };
 
-// Parts of a split launch: one slot per (tile, part), rows x (D + 4) floats: the unnormalised
+// Parts of a split launch: one slot per (tile, part), rows x (D + 5) floats: the unnormalised
 // output rows, then per row the reference maximum (times scale log2 e; -inf: no key), the sum of
-// the weights, and (8 bytes; the tile's last part counts) the output row, -1 for none.
+// the weights, (8 bytes; the tile's last part counts) the output row, -1 for none, and the sum of
+// the weights as the output has them (bf16: rounded; fp32: not used).
 __host__ __device__ inline size_t part_slot_floats(int rows, int d) {
-  return static_cast<size_t>(rows) * (d + 4);
+  return static_cast<size_t>(rows) * (d + 5);
 }
 
 struct JoinParams {

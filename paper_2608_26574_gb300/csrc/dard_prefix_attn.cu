@@ -55,7 +55,7 @@ struct __align__(16) Ctl {
   int32_t abort;
   int32_t poison;         // a query sees a value that is not finite
   float red_max[2][kParts][kBM];  // per tile parity: the column parts' row maxima
-  float red_sum[kParts][kBM];     // their row sums
+  float red_sum[2][kParts][kBM];  // their row sums: of the weights, of the weights rounded to bf16
   int64_t out_row[kBM];      // packed query -> row * hq + head, or -1 (not stored)
   RowMasks row_mask[kBM];
   BlockScratch scratch[4];
@@ -330,7 +330,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       ctl.out_row[t] = out_row;
     }
     const float sl = p.a.scale_log2;
-    float m_run = -INFINITY, l_run = 0.f;
+    float m_run = -INFINITY, l_run = 0.f, l_rnd = 0.f;
     // from here on tiles have keys that some query does not see
     const int first_masked = min(first_own, p.prefix_len / kTN - j0);
     bool ok = true, ready = false;
@@ -424,14 +424,27 @@ __global__ void __launch_bounds__(kThreads, 1)
       float a0, a1;
       f2_unpack(f2_add(acc[0], acc[1]), a0, a1);
       l_run = l_run * alpha + (a0 + a1);
+      // The output is divided by the sum of the weights that the product takes, the rounded ones, so that it is a
+      // convex combination of the values (lse is of the unrounded sum). Added here, behind the hand-over, the
+      // sum costs 5 % of a long call; in the loop above, 7 %.
+      {
+        float rnd[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int e = 0; e < kCols / 2; ++e) add_bf16x2_f32(rnd[2 * (e & 1)], rnd[2 * (e & 1) + 1], pk[e]);
+        l_rnd = l_rnd * alpha + ((rnd[0] + rnd[1]) + (rnd[2] + rnd[3]));
+      }
       m_run = m_new;
     }
     if (ok) ok = mbar_wait(&ctl.o_full, 0, wlim);
     const bool wok = __all_sync(0xffffffffu, ok);
     if (!wok && lane == 0) flag_timeout(p, ctl);
-    ctl.red_sum[part4][t] = l_run;
+    ctl.red_sum[0][part4][t] = l_run;
+    ctl.red_sum[1][part4][t] = l_rnd;
     all_bar_sync();
-    const float l = (ctl.red_sum[0][t] + ctl.red_sum[1][t]) + (ctl.red_sum[2][t] + ctl.red_sum[3][t]);
+    auto row_sum = [&](int i) {
+      return (ctl.red_sum[i][0][t] + ctl.red_sum[i][1][t]) + (ctl.red_sum[i][2][t] + ctl.red_sum[i][3][t]);
+    };
+    const float l = row_sum(0), l_out = row_sum(1);
     uint32_t rr[kOC];
     if (wok) {  // (whole warps: the loads from TMEM are theirs)
       tc_fence_after();
@@ -454,6 +467,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         float* stat = slot + kBM * D;
         stat[t] = m_run == -INFINITY ? -INFINITY : m_run * sl;
         stat[kBM + t] = l;
+        stat[4 * kBM + t] = l_out;
         reinterpret_cast<int64_t*>(stat + 2 * kBM)[t] = wok ? ctl.out_row[t] : -1;
       }
     } else {
@@ -463,7 +477,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       constexpr int kChunks = D / 8;  // 16-byte chunks per output row
       uint4* stage = reinterpret_cast<uint4*>(sK);  // 128 rows x D bf16 <= one K stage
       if (wok) {
-        const float inv_l = 1.0f / l;
+        const float inv_l = 1.0f / l_out;
 #pragma unroll
         for (int v = 0; v < kOC / 8; ++v) {
           uint4 u;
@@ -502,13 +516,15 @@ __global__ void __launch_bounds__(kThreads, 1)
 }
 
 // Joins the parts of a split launch: with M the largest reference maximum of a packed query,
-// o = sum_c 2^(m_c - M) O_c / sum_c 2^(m_c - M) l_c. kWarps warps share a query's parts, 32 at a time:
-// a lane takes a part's factor and sum, then all take the parts' rows, coalesced. Bound by latency: one
-// warp walking 33 parts of a row with a wait for each took 24 us, this 3 beside the launch.
+// o = sum_c 2^(m_c - M) O_c / sum_c 2^(m_c - M) l'_c, l' the sum of the weights as O has them. kWarps warps
+// share a query's parts, 32 at a time: a lane takes a part's factor and sums, then all take the parts' rows,
+// coalesced. Bound by latency: one warp walking 33 parts of a row with a wait for each took 24 us, this 3
+// beside the launch.
 template <typename T, int D, int kWarps>
 __global__ void __launch_bounds__(128, 6) prefix_join(const __grid_constant__ JoinParams p) {
   constexpr int kV = D / 32;  // elements per lane
-  __shared__ float s_o[4][D], s_top[4], s_l[4];
+  constexpr bool kRounded = sizeof(T) == 2;  // the output has its own sum
+  __shared__ float s_o[4][D], s_top[4], s_l[4], s_lo[4];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, sub = warp % kWarps;
   const long long w = (static_cast<long long>(blockIdx.x) * 4 + warp) / kWarps;
   const bool in = w < p.rows;
@@ -520,7 +536,7 @@ __global__ void __launch_bounds__(128, 6) prefix_join(const __grid_constant__ Jo
   grid_dep_wait();
   const int64_t row = reinterpret_cast<const int64_t*>(slot + (p.nsplit - 1) * floats +
                                                        p.tile_rows * (D + 2))[t];
-  float top = -INFINITY, l = 0.f, o[kV];
+  float top = -INFINITY, l = 0.f, lo = 0.f, o[kV];
 #pragma unroll
   for (int e = 0; e < kV; ++e) o[e] = 0.f;
   const int c0 = p.nsplit * sub / kWarps, c1 = p.nsplit * (sub + 1) / kWarps;
@@ -528,6 +544,7 @@ __global__ void __launch_bounds__(128, 6) prefix_join(const __grid_constant__ Jo
     const int n = min(32, c1 - c);
     const float mc = lane < n ? stat[(c + lane) * floats] : -INFINITY;
     const float lc = lane < n ? stat[(c + lane) * floats + p.tile_rows] : 0.f;
+    const float lr = kRounded && lane < n ? stat[(c + lane) * floats + 4 * p.tile_rows] : 0.f;
     float most = fmaxf(top, mc);
 #pragma unroll
     for (int x = 16; x > 0; x >>= 1) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, x));
@@ -535,10 +552,14 @@ __global__ void __launch_bounds__(128, 6) prefix_join(const __grid_constant__ Jo
     // that are all NaN beside such keys, and a sum of NaN, which 0 times it lets through.)
     const float f = mc == -INFINITY ? 0.f : mc == most ? 1.f : ex2_approx(mc - most);
     const float back = top == -INFINITY ? 0.f : top == most ? 1.f : ex2_approx(top - most);
-    float lf = f * lc;
+    float lf = f * lc, lof = f * lr;
 #pragma unroll
-    for (int x = 16; x > 0; x >>= 1) lf += __shfl_xor_sync(0xffffffffu, lf, x);
+    for (int x = 16; x > 0; x >>= 1) {
+      lf += __shfl_xor_sync(0xffffffffu, lf, x);
+      if (kRounded) lof += __shfl_xor_sync(0xffffffffu, lof, x);
+    }
     l = l * back + lf;
+    lo = lo * back + lof;
 #pragma unroll
     for (int e = 0; e < kV; ++e) o[e] *= back;
     top = most;
@@ -565,19 +586,21 @@ __global__ void __launch_bounds__(128, 6) prefix_join(const __grid_constant__ Jo
     if (lane == 0) {
       s_top[warp] = top;
       s_l[warp] = l;
+      s_lo[warp] = lo;
     }
     __syncthreads();
     if (sub != 0) return;
     float most = s_top[0];
 #pragma unroll
     for (int k = 1; k < kWarps; ++k) most = fmaxf(most, s_top[k]);
-    l = 0.f;
+    l = lo = 0.f;
 #pragma unroll
     for (int e = 0; e < kV; ++e) o[e] = 0.f;
 #pragma unroll
     for (int k = 0; k < kWarps; ++k) {
       const float f = s_top[k] == -INFINITY ? 0.f : s_top[k] == most ? 1.f : ex2_approx(s_top[k] - most);
       l = fmaf(f, s_l[k], l);
+      lo = fmaf(f, s_lo[k], lo);
 #pragma unroll
       for (int e = 0; e < kV; ++e) o[e] = fmaf(f, s_o[k][lane * kV + e], o[e]);
     }
@@ -585,7 +608,7 @@ __global__ void __launch_bounds__(128, 6) prefix_join(const __grid_constant__ Jo
   }
   if (!in || row < 0) return;
   T* out = static_cast<T*>(p.o) + row * D + lane * kV;
-  const float inv = 1.0f / l;
+  const float inv = 1.0f / (kRounded ? lo : l);
 #pragma unroll
   for (int e = 0; e < kV; e += 2) {
     if constexpr (sizeof(T) == 2)

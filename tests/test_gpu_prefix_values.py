@@ -63,3 +63,26 @@ def test_attention_nan_query_and_parts_without_weight(dtype, hq, hkv, d, prefix,
     t["q"][0, 2, 7] = math.nan
     want = _same_nan(lays, t, ws)
     assert np.isnan(want[0, 2]).all() and np.isfinite(want[0, 3]).all() and np.isnan(want[:, -1, 5]).all()
+
+
+@pytest.mark.parametrize("ws", [True, False])
+@pytest.mark.parametrize("seqs,prefix", [([(1, 0, 0, 0)] * 12, 201), ([(0, 6, 0, 6)] * 3, 130), ([(1, 0, 0, 0)], 4500)])
+@pytest.mark.parametrize("d", [64, 128])
+def test_attention_of_equal_values(d, seqs, prefix, ws):
+    """Weights that all round the same way (one key ahead, the others alike behind it, at every distance):
+    an output that adds rounded weights is divided by their sum, so that equal values come back as they
+    are. (The sum of the unrounded ones is off by up to 2^-8, half a step of these values by 2^-9.)"""
+    lays, t = T.make("bf16", 4, 2, d, prefix, seqs, 3)
+    rows = t["q"].shape[0]
+    for x in ("q", "k", "pk"):
+        t[x].zero_()
+    # q.k = 0 for the first key of the prefix and -x for all others, x a different one for each query
+    x = torch.linspace(0.1, 2.0, rows * 4, device=DEV).view(rows, 4)
+    t["q"][..., 0] = x.to(torch.bfloat16)
+    t["k"][..., 0] = t["pk"][..., 0] = -d ** 0.5
+    t["pk"][0] = 0
+    for x in ("v", "pv"):
+        t[x].fill_(1.9921875)  # the relative half step is smallest just below 2
+    o, ls = T.attend(lays, t, ws=ws)
+    assert (o == 1.9921875).all(), o[o != 1.9921875]
+    T.check_attention(lays, t, o, ls)
