@@ -80,6 +80,7 @@ struct __align__(16) Ctl {
   uint64_t drained;
   uint32_t tmem_base;
   int32_t abort;
+  int32_t odd_keys;               // an element of K is not finite (before k_full)
   __align__(16) float lse[kQStages][kBM];  // times -log2 e (read four at a time)
   uint32_t off[kQStages][4];      // queries that add nothing (bit per column)
   float red[2 * kGroups][kBM];
@@ -208,6 +209,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       mbar_init(&ctl.s_free[b], kWorkers);
     }
     ctl.abort = 0;
+    ctl.odd_keys = 0;
     fence_barrier_init();
   }
   if (warp == kWMma) {
@@ -229,7 +231,8 @@ __global__ void __launch_bounds__(kThreads, 1)
       kreg[4 * c + 3] = u.w;
     }
   }
-  // rows of the stages that no copy writes: zeros, whose scores (0) count for nothing with lse = +inf
+  // rows of the stages that no copy writes: zeros, whose scores (0; NaN with a key that is not finite) count for
+  // nothing with lse = +inf
   for (int i = columns * 8 + threadIdx.x; i < kTN * 8; i += kThreads)
     for (int b = 0; b < min(n, kQStages) * kSub; ++b)
       *reinterpret_cast<uint4*>(sQ + b * kKSub + 16 * i) = make_uint4(0, 0, 0, 0);
@@ -322,15 +325,16 @@ __global__ void __launch_bounds__(kThreads, 1)
     uint32_t parity = 1;  // of the stage's use before this one (the first round does not wait)
     fetch(b, v[0]);
     fetch(b + 2, v[1]);
-    bool ok = true;
+    bool ok = warp_wait(&ctl.k_full, 0, wlim);
+    const bool odd_keys = ctl.odd_keys != 0;
     for (int j = b; j < n && ok && !*abort_flag; j += 2) {
       if (j >= kQStages) ok = warp_wait(&ctl.l_empty[b], parity, wlim);
       if (!ok) break;
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        // a query whose lse is +inf adds nothing (columns without a query or behind the last row
-        // need no bit: their scores are 0)
-        const uint32_t bits = __ballot_sync(0xffffffffu, v[0][e] == INFINITY && 32 * e + lane < columns);
+        // a query whose lse is +inf adds nothing; nor does a column without a query, which needs the bit
+        // only where a key makes NaN of its zeros (sums that look at bits take longer)
+        const uint32_t bits = __ballot_sync(0xffffffffu, v[0][e] == INFINITY && (odd_keys || 32 * e + lane < columns));
         ctl.lse[b][32 * e + lane] = lse_unit(p, v[0][e]);
         if (lane == 0) ctl.off[b][e] = bits;
       }
@@ -354,6 +358,10 @@ __global__ void __launch_bounds__(kThreads, 1)
     const int part = warp >> 2;
     if (warp < 16) {
       tmem_store(ctl.tmem_base + kKCol + lane_off + part * (D / 8), kreg);
+      uint32_t bits = 0;  // bit 15 or 31: an exponent of all ones
+#pragma unroll
+      for (int c = 0; c < D / 8; ++c) bits |= (kreg[c] & 0x7fff7fffu) + 0x00800080u;
+      if (bits & 0x80008000u) ctl.odd_keys = 1;
       tmem_wait_st();
       tc_fence_before();
       __syncwarp();

@@ -86,3 +86,37 @@ def test_attention_of_equal_values(d, seqs, prefix, ws):
     o, ls = T.attend(lays, t, ws=ws)
     assert (o == 1.9921875).all(), o[o != 1.9921875]
     T.check_attention(lays, t, o, ls)
+
+
+@pytest.mark.parametrize("hq,hkv,rows", [(7, 1, 40), (8, 1, 40), (14, 2, 1), (16, 2, 3), (150, 1, 9), (3, 3, 130),
+                                         (9, 3, 43)])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("ws", [True, False])
+def test_weights_of_keys_that_are_not_finite(dtype, hq, hkv, rows, ws):
+    """Infinite elements make a key's scores +inf or -inf: its weight is +inf or what the other rows give
+    it. A NaN makes it NaN, but where no row counts (lse = +inf) everything is 0. Whatever number of query
+    heads a tile has room for."""
+    _, t = T.make(dtype, hq, hkv, 64, 300, [(rows, 0, 0, 0)], 5)
+    q, pk = t["q"], t["pk"]
+    q[..., 3] = q[..., 3].abs() + 0.25
+    lse = torch.rand(rows, hq, device=DEV, generator=torch.Generator(DEV).manual_seed(2)) + 7
+    lse[rows // 2, hq // 2] = math.inf
+    clean = pk.clone()
+    pk[5, :, 3] = math.inf
+    pk[6, :, 3] = -math.inf
+    pk[200, 0, 3] = -math.inf
+    pk[7, hkv - 1, 9] = math.nan
+    got = T.weigh(q, lse, pk, ws=ws)
+    inf = torch.zeros(hkv, 300, dtype=torch.bool, device=DEV)
+    inf[:, 5] = True
+    none, nan = torch.zeros_like(inf), torch.zeros_like(inf)
+    none[:, 6] = none[0, 200] = nan[hkv - 1, 7] = True
+    if (rows, hq // hkv) == (1, 1):
+        inf[:, 5] = lse[0, 0] != math.inf
+    assert torch.equal(got == math.inf, inf)
+    assert torch.equal(torch.isnan(got), nan)
+    assert (got[none] == 0).all()
+    odd = inf | none | nan
+    want = T.weigh(q, lse, clean, ws=ws)
+    assert torch.equal(got[~odd], want[~odd])
+    assert (T.weigh(q, torch.full_like(lse, math.inf), pk, ws=ws) == 0).all()
