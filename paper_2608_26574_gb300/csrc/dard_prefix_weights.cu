@@ -658,10 +658,9 @@ dard_status prepare(const dard_prefix_weights_args* a, WeightsParams& p) {
   p.scale = (a->scale > 0.f ? static_cast<double>(a->scale) : 1.0 / std::sqrt(static_cast<double>(a->head_dim))) *
             1.4426950408889634;
   // lse in the unit in which scale_log2, rounded to 32 bits, takes the scores: its rounding then counts for their
-  // difference only. From the tensor cores scores come short by 3e-10 per element of a head on average, as a
-  // running sum is cut (with this keys' weights of random q and k are off by 1e-7 on average, without by 4e-7).
-  const double unit = p.scale_log2 / p.scale * 1.4426950408889634 /
-                      (a->dtype == DARD_BF16 ? 1.0 + 3e-10 * a->head_dim : 1.0);
+  // difference only. (Scores from the tensor cores come short, as a running sum is cut: weights of random q and k
+  // of 128 elements by some 1e-7 of themselves. Nothing makes up for that: how much it is depends on the keys.)
+  const double unit = p.scale_log2 / p.scale * 1.4426950408889634;
   p.lse_hi = static_cast<float>(-unit);
   p.lse_lo = static_cast<float>(-unit - p.lse_hi);
   p.test_drop_kv = -1;

@@ -120,3 +120,30 @@ def test_weights_of_keys_that_are_not_finite(dtype, hq, hkv, rows, ws):
     want = T.weigh(q, lse, clean, ws=ws)
     assert torch.equal(got[~odd], want[~odd])
     assert (T.weigh(q, torch.full_like(lse, math.inf), pk, ws=ws) == 0).all()
+
+
+@pytest.mark.parametrize("ws", [True, False])
+@pytest.mark.parametrize("scale", [0.25, 0.0])
+def test_weights_of_exact_scores(scale, ws):
+    """Scores of a few large products, which no sum cuts or rounds, next to their normalisers: z = 512 scale,
+    up to 128. The normaliser enters as a 32-bit number in base 2, which is taken into account here (values
+    whose product lies halfway between two of them are left out); what remains is the exponent itself (below 8
+    in base 2: 4 u ln 2), the exponential (2^-22), 16 additions and the scale's rounding, which counts for the
+    difference of at most 5. (A normaliser off by 4e-8 of itself is 5e-6 of the weight.)"""
+    d, hq, rows, prefix = 128, 8, 64, 300
+    q, pk = (torch.zeros(n, h, d, dtype=torch.bfloat16, device=DEV) for n, h in ((rows, hq), (prefix, 1)))
+    q[..., 16:24] = pk[..., 16:24] = 8.0
+    c = scale or d ** -0.5
+    z = 512 * c
+    unit = float(np.float32(np.float32(c) * np.float32(math.log2(math.e)))) / c
+    cand = (z + 2 + np.random.default_rng(1).random(4000) * 3).astype(np.float32)
+    prod = cand.astype(np.float64) * unit
+    near = prod.astype(np.float32).astype(np.float64)
+    use = np.abs(prod - near) < 0.48 * np.spacing(near.astype(np.float32))
+    cand, near = cand[use][:rows * hq], near[use][:rows * hq]
+    got = T.weigh(q, torch.from_numpy(cand).to(DEV).view(rows, hq), pk, ws=ws, scale=scale)
+    want = np.exp2(z * unit - near).sum()
+    assert want / (rows * hq) * 32 < 4  # far from the sums that are formed another way
+    tol = 4 * U * math.log(2) + 2.0 ** -22 + 16 * U
+    rel = np.abs(T._np(got) / want - 1).max()
+    assert rel <= tol, (rel, tol)
