@@ -124,10 +124,9 @@ __device__ __forceinline__ float sum32(const uint32_t (&s)[32], const float* lse
 // Sums above p.large (some lane's of the warp) once more, with exact scores: the tensor cores cut the bits that
 // a running sum has no room for, which takes up to two units in the last place off a large score, 3.4e-6 of
 // its exponential at a score of 35 and more where small products follow large ones. p.large is a quarter of
-// the columns and twice a key's share of them, but not more than all, which is the most that so many queries'
-// weights add up to where their lse is over these keys: a few keys reach it, and where lse is over others (a
-// part of them, a cache that has changed since) single terms may be as large as they like, and are a key's
-// whole sum. (1111 rows of 32 heads over two keys: 13.7 us, 48 without the share.) Key by key for those that
+// the columns, whatever the prefix: keys that draw that much of their queries' weight reach it, and where lse is
+// over other keys (a part of them, a cache that has changed since) single terms may be as large as they like, and
+// are a key's whole sum. Such a key costs its CTA some 2 us for every 32 queries. Key by key for those that
 // need it, a lane for each of the 32 columns from `first` on; eight products at a time, their sums added up
 // with what the roundings cut off. 4608 rows of 28 heads over 32768 keys: 842 us without it, 845-850 while no
 // sum is that large, 887-983 with lse over 256 of the keys, where the largest error against 64 bits goes from
@@ -723,7 +722,7 @@ dard_status dard_prefix_weights(const dard_prefix_weights_args* args, void* stre
       p.box_rows = std::min(128 / p.box_heads, p.rows);
       p.head_blocks = (p.group + p.box_heads - 1) / p.box_heads;
       p.q_tiles = (p.rows + p.box_rows - 1) / p.box_rows * p.head_blocks;
-      p.large = std::min(32, p.box_rows * p.box_heads) * std::min(1.0f, 0.25f + 2.0f / p.prefix_len);
+      p.large = 0.25f * std::min(32, p.box_rows * p.box_heads);
     } else {
       p.q_tiles = static_cast<int32_t>((static_cast<long long>(p.rows) * p.group + kFQueries - 1) / kFQueries);
     }

@@ -147,3 +147,33 @@ def test_weights_of_exact_scores(scale, ws):
     tol = 4 * U * math.log(2) + 2.0 ** -22 + 16 * U
     rel = np.abs(T._np(got) / want - 1).max()
     assert rel <= tol, (rel, tol)
+
+
+@pytest.mark.parametrize("ws", [True, False])
+@pytest.mark.parametrize("prefix", [1, 2, 5])
+@pytest.mark.parametrize("d,hq,hkv,rows", [(128, 8, 2, 128), (64, 6, 2, 77)])
+def test_weights_of_large_scores_behind_few_keys(d, hq, hkv, rows, prefix, ws):
+    """The scores of test_weights_of_large_scores behind a prefix of a few keys, each with its share of
+    every query's weight: their sums are exact too (6e-5 off if they are formed on the tensor cores, each
+    element a unit of a running sum of 512). Left are the exponent's rounding (below 4 in base 2: 4 u ln 2), the
+    exponential's (2^-22) and at most 24 additions; and 32 columns of a tile that hold so few queries that
+    their sum stays below 8, whose terms keep the cut: at most a unit of 512 (2^-14) for each of d - 8 elements."""
+    g = torch.Generator(device=DEV).manual_seed(d + rows)
+
+    def make_rows(n, h):
+        x = 1 + torch.randint(0, 128, (n, h, d), generator=g, device=DEV) / 128  # 8 bits
+        x *= 2.0 ** -7
+        x[..., :8] = 8.0
+        return x.to(torch.bfloat16)
+    q, pk = make_rows(rows, hq), make_rows(prefix, hkv)
+    z = torch.einsum("rhgd,khd->rhgk", q.double().view(rows, hkv, -1, d), pk.double()) / d ** 0.5
+    share = min(prefix, 3)  # a key's part: above a quarter
+    lse = (z.mean(-1) + math.log(share)).float().view(rows, hq)
+    got = T.weigh(q, lse, pk, ws=ws)
+    want = O.prefix_weights(T._np(q), T._np(lse), T._np(pk))[0]
+    rel = np.abs(T._np(got) - want) / want
+    group, per_tile = hq // hkv, 128 // (hq // hkv)
+    tiles = [min(per_tile, rows - r) * group for r in range(0, rows, per_tile)]
+    words = [min(32, n - c) for n in tiles for c in range(0, n, 32)]
+    cut = sum(n for n in words if n / share <= 8) / (rows * group) * (d - 8) * 2.0 ** -14 / d ** 0.5
+    assert rel.max() <= 4 * U * math.log(2) + 2.0 ** -22 + 24 * U + cut, (rel.max(), cut)
