@@ -438,7 +438,9 @@ __global__ void __launch_bounds__(kThreads, 1)
 // ---------------------------------------------------------------- fp32, CUDA cores
 // 256 threads (16 x 16) hold 128 keys and take 64 queries at a time through shared memory: thread
 // (ty, tx) computes the scores of keys ty + 16 u and queries tx + 16 i (a 16-byte shared-memory
-// load serves 4 or 8 dot products), and adds up its keys' exponentials.
+// load serves 4 or 8 dot products), and adds up its keys' exponentials, a tile's four first. What the
+// roundings of the sum over the tiles cut off is kept beside it and taken up by the next tile: equal terms, which
+// all round the same way, would put a long plain sum off by 7e-5 (73728 terms of a key).
 constexpr int kFThreads = 256, kFKeys = 128, kFQueries = 64;
 
 __device__ __forceinline__ int swz(int row, int c) { return c ^ (row & 7); }
@@ -448,8 +450,9 @@ constexpr size_t f32_smem() {
   return sizeof(float) * ((kFKeys + 2 * kFQueries) * D + 2 * kFQueries);
 }
 
+// (Its registers: with 128 elements one CTA fits on an SM anyway; without the hint a long call takes 7 % more.)
 template <int D>
-__global__ void __launch_bounds__(kFThreads) weights_f32(const __grid_constant__ WeightsParams p) {
+__global__ void __launch_bounds__(kFThreads, D == 128 ? 1 : 0) weights_f32(const __grid_constant__ WeightsParams p) {
   constexpr int kC = D / 4, kU = kFKeys / 16, kI = kFQueries / 16;
   extern __shared__ __align__(16) uint8_t smem_raw[];
   float4* sK = reinterpret_cast<float4*>(smem_raw);
@@ -486,9 +489,9 @@ __global__ void __launch_bounds__(kFThreads) weights_f32(const __grid_constant__
     }
   };
   load(j0, 0);
-  float total[kU];
+  float total[kU], over[kU];  // the sum, and what its last rounding added to it
 #pragma unroll
-  for (int u = 0; u < kU; ++u) total[u] = 0.f;
+  for (int u = 0; u < kU; ++u) total[u] = over[u] = 0.f;
   for (int j = j0; j < j1; ++j) {
     const int b = (j - j0) & 1;
     cp_async_wait_all();
@@ -517,12 +520,22 @@ __global__ void __launch_bounds__(kFThreads) weights_f32(const __grid_constant__
         }
       }
     }
+    float sum[kU];
+#pragma unroll
+    for (int u = 0; u < kU; ++u) sum[u] = -over[u];
 #pragma unroll
     for (int i = 0; i < kI; ++i) {
       const float lse = sL[b * kFQueries + tx + 16 * i];
       if (lse == -INFINITY) continue;  // adds nothing, whatever q holds
 #pragma unroll
-      for (int u = 0; u < kU; ++u) total[u] += exp2f(fmaf(s[u][i], p.scale_log2, lse));
+      for (int u = 0; u < kU; ++u) sum[u] += exp2f(fmaf(s[u][i], p.scale_log2, lse));
+    }
+#pragma unroll
+    for (int u = 0; u < kU; ++u) {
+      const float to = total[u] + sum[u];
+      over[u] = (to - total[u]) - sum[u];
+      if (!(fabsf(over[u]) < INFINITY)) over[u] = 0.f;  // (an infinite sum stays one)
+      total[u] = to;
     }
   }
 #pragma unroll

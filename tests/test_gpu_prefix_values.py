@@ -177,3 +177,22 @@ def test_weights_of_large_scores_behind_few_keys(d, hq, hkv, rows, prefix, ws):
     words = [min(32, n - c) for n in tiles for c in range(0, n, 32)]
     cut = sum(n for n in words if n / share <= 8) / (rows * group) * (d - 8) * 2.0 ** -14 / d ** 0.5
     assert rel.max() <= 4 * U * math.log(2) + 2.0 ** -22 + 24 * U + cut, (rel.max(), cut)
+
+
+@pytest.mark.parametrize("x", [0.7, 1.1, 2.3])
+def test_weights_f32_of_many_equal_terms(x):
+    """73728 equal terms for each key, in one run (no workspace): every addition to a running sum would round the
+    same way (up to 2^-24 of the sum each time, 6e-5 in all). The kernel keeps what the roundings of its
+    long sums cut off, which leaves a tile's 4 terms of a thread, the 16 threads' sums and the last
+    roundings (12 u), the term's own error (the exponential 2^-22, its exponent 8 u ln 2)."""
+    rows, hq, d, prefix = 9216, 8, 64, 130
+    g = torch.Generator(device=DEV).manual_seed(1)
+    q = torch.randn(1, 1, d, device=DEV, generator=g).expand(rows, hq, d).contiguous()
+    pk = torch.randn(prefix, 1, d, device=DEV, generator=g) * 0.1
+    lse = torch.full((rows, hq), x, device=DEV)
+    got = T.weigh(q, lse, pk, ws=False)
+    want, _, dot = O.prefix_weights(T._np(q[:1, :1]), T._np(lse[:1, :1]), T._np(pk))
+    want = want * (rows * hq)
+    rel = np.abs(T._np(got) - want) / want
+    tol = 2 * (d + 4) * U * dot + 2.0 ** -22 + 8 * U * math.log(2) + 4 * U * x + 12 * U
+    assert (rel <= tol).all(), (rel.max(), (rel - tol).max())
