@@ -334,14 +334,17 @@ __global__ void __launch_bounds__(kThreads, 1)
     // from here on tiles have keys that some query does not see
     const int first_masked = min(first_own, p.prefix_len / kTN - j0);
     bool ok = true, ready = false;
+    int missed = 0;  // tiles whose barrier this warp has not come to
     for (int j = 0; j < n_kt; ++j) {
       const int b = j & (kNS - 1);
-      // The four warps of the rows wait for the same S_j with the same bound (no early leave on an
-      // abort flag), so they leave the loop together: a barrier completing between the warps'
-      // deadlines (a product about a second late) is the only way they could part.
+      // (A warp whose wait runs out leaves, hands nothing over any more and catches up on the barriers behind the
+      // loop.)
       if (!__all_sync(0xffffffffu, ready)) {
         ok = warp_wait(&ctl.s_full[b], (j / kNS) & 1, wlim);
-        if (!ok) break;
+        if (!ok) {
+          missed = n_kt - j;
+          break;
+        }
       }
       tc_fence_after();
       uint32_t s[kCols];
@@ -397,7 +400,10 @@ __global__ void __launch_bounds__(kThreads, 1)
       // P_j replaces P_{j-1}, and O may be rescaled, once PV_{j-1} has completed
       if (!__all_sync(0xffffffffu, pv_done)) {
         ok = warp_wait(&ctl.pv_done, (j - 1) & 1, wlim);
-        if (!ok) break;
+        if (!ok) {
+          missed = n_kt - j - 1;
+          break;
+        }
       }
       tc_fence_after();
       if (__any_sync(0xffffffffu, rescale)) {  // this warp's share of the O columns
@@ -413,7 +419,11 @@ __global__ void __launch_bounds__(kThreads, 1)
         // (the stage's use before this one has landed: PV_{j-1} has completed, and this use ends
         // only after this warp's weights)
         ok = mbar_wait(&ctl.v_full[j % kNKV], (j / kNKV) & 1, wlim);
-        if (!__all_sync(0xffffffffu, ok)) { ok = false; break; }
+        if (!__all_sync(0xffffffffu, ok)) {
+          ok = false;
+          missed = n_kt - j - 1;
+          break;
+        }
         check_values<D>(p, ctl, sV + j % kNKV * kKVBytes, key0 + (j0 + j - npt) * kTN, warp);
       }
       ready = j + 1 < n_kt && mbar_test(&ctl.s_full[(j + 1) & (kNS - 1)], ((j + 1) / kNS) & 1);  // (asked ahead)
@@ -435,6 +445,10 @@ __global__ void __launch_bounds__(kThreads, 1)
       }
       m_run = m_new;
     }
+    // The barrier of the rows' four warps has no limit of its own: whoever left early still comes to it for every
+    // tile, or the others would wait there for ever. (They find out by their own waits. Agreeing at the barrier
+    // to leave, by a reduction or a flag, takes 9 to 10 % of a long call.)
+    for (; missed > 0; --missed) quarter_bar_sync(quarter);
     if (ok) ok = mbar_wait(&ctl.o_full, 0, wlim);
     const bool wok = __all_sync(0xffffffffu, ok);
     if (!wok && lane == 0) flag_timeout(p, ctl);
@@ -468,7 +482,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         stat[t] = m_run == -INFINITY ? -INFINITY : m_run * sl;
         stat[kBM + t] = l;
         stat[4 * kBM + t] = l_out;
-        reinterpret_cast<int64_t*>(stat + 2 * kBM)[t] = wok ? ctl.out_row[t] : -1;
+        reinterpret_cast<int64_t*>(stat + 2 * kBM)[t] = *abort_flag ? -1 : ctl.out_row[t];
       }
     } else {
       // O row / row sum -> bf16 into shared memory (the K stages are no longer read once o_full
