@@ -327,16 +327,20 @@ __global__ void __launch_bounds__(kTc1Threads, 1)
     const float sl = p.scale_log2;
     float m_run = -INFINITY, l_run = 0.f;
     bool ok = true;
+    int missed = 0;  // tiles whose barrier this warp has not come to
     for (int j = 0; j < n_kt; ++j) {
       const int b = j % kNS;
       const int kt0 = j * kTN + half * 64;  // this warp's 64 keys
       const bool masked = tile_needs_mask(sd, j * kTN);
       const uint64_t vis = masked ? vis64(sd, kt0, rm) : ~0ull;
-      // Both warps of the rows wait for the same S_j with the same bound (no early leave on
-      // an abort flag), so they leave the loop together: a barrier completing between the two
-      // warps' deadlines (a product about a second late) is the only way they could part.
+      // (A warp whose wait runs out leaves, hands nothing over any more and catches up on the barriers behind the
+      // loop.)
       ok = mbar_wait(&ctl.s_full[b], (j / kNS) & 1, wlim);
-      if (!__all_sync(0xffffffffu, ok)) { ok = false; break; }
+      if (!__all_sync(0xffffffffu, ok)) {
+        ok = false;
+        missed = n_kt - j;
+        break;
+      }
       tc_fence_after();
       float s[64];
       {
@@ -398,8 +402,12 @@ __global__ void __launch_bounds__(kTc1Threads, 1)
       for (int k = 0; k < 4; ++k) ls[k] = acc[k] + acc[4 + k];
       // P_j replaces P_{j-1}, and O may be rescaled, once PV_{j-1} has completed
       if (j > 0) {
-        ok = mbar_wait(&ctl.pv_done, (j - 1) & 1, wlim);  // the same barrier for both warps
-        if (!__all_sync(0xffffffffu, ok)) { ok = false; break; }
+        ok = mbar_wait(&ctl.pv_done, (j - 1) & 1, wlim);
+        if (!__all_sync(0xffffffffu, ok)) {
+          ok = false;
+          missed = n_kt - j - 1;
+          break;
+        }
         tc_fence_after();
       }
       if (__any_sync(0xffffffffu, rescale)) {
@@ -422,6 +430,9 @@ __global__ void __launch_bounds__(kTc1Threads, 1)
       __syncwarp();
       if (lane == 0) mbar_arrive(&ctl.p_full);
     }
+    // The barrier of the rows' two warps has no limit of its own: a warp that left early still comes to it for
+    // every tile, or the other would wait there for ever. (It finds out by its own waits.)
+    for (; missed > 0; --missed) pair_bar_sync(quarter);
     if (ok) ok = mbar_wait(&ctl.o_full, 0, wlim);
     const bool wok = __all_sync(0xffffffffu, ok);
     if (!wok && lane == 0) flag_timeout(p, ctl);

@@ -32,7 +32,7 @@ def _loop(file, kernel):
     raise AssertionError("no such loop")
 
 
-@pytest.mark.parametrize("file,kernel", [("dard_prefix_attn.cu", "prefix_tc")])
+@pytest.mark.parametrize("file,kernel", [("dard_prefix_attn.cu", "prefix_tc"), ("dard_attention.cu", "attn_tc1")])
 def test_softmax_warps_miss_no_barrier(file, kernel):
     loop, behind = _loop(file, kernel)
     barrier, = re.findall(r"\w+_bar_sync\(quarter\);", loop)
