@@ -600,7 +600,8 @@ dard_status dard_prefix_weights(const dard_prefix_weights_args* args, void* stre
  * rising order, and
  *     k_out[i,g] = k[kept[g,i],g],   v_out[i,g] = v[kept[g,i],g],   weights_out[g,i] =
  *     weights[g,kept[g,i]]
- * The outputs must not overlap the inputs. */
+ * The outputs must not overlap the inputs or one another, nor rows of an output by its strides
+ * (k_out and v_out may lie row by row beside each other in one buffer). */
 typedef struct {
   const float* weights;      /* device [hkv, prefix_len]                                   */
   const void* prefix_k;      /* device, both optional together                             */
@@ -620,7 +621,8 @@ typedef struct {
 } dard_prefix_evict_args;
 
 /* Two launches, the second a programmatic dependent of the first. Errors: DARD_ERR_NULL, _SHAPE,
- * _VALUE (dtype; an output that overlaps an input), _UNSUPPORTED, _ALIGN, _CUDA. */
+ * _VALUE (dtype; an output that overlaps an input, another output or itself), _UNSUPPORTED, _ALIGN,
+ * _CUDA. */
 dard_status dard_prefix_evict(const dard_prefix_evict_args* args, void* stream);
 
 /* Human-readable name of a status code; never NULL. */

@@ -1027,7 +1027,8 @@ class PrefixEvictCall:
     Call it with weights [hkv, prefix_len] in fp32 (contiguous rows), prefix_k and prefix_v
     [prefix_len, hkv, d], and the outputs ``kept`` [hkv, keep] (int32), ``k_out`` and ``v_out``
     [keep, hkv, d] (contiguous heads, any row and head strides) and, optionally, ``weights_out``
-    [hkv, keep]. The outputs must not overlap the inputs."""
+    [hkv, keep]. The outputs must not overlap the inputs or one another, nor rows of them by their
+    strides."""
 
     layout = struct.Struct("=7Q5q7i4x")  # dard_prefix_evict_args
 

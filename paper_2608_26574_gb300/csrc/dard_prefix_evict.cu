@@ -262,13 +262,46 @@ __global__ void __launch_bounds__(kCopyThreads) evict_copy(const __grid_constant
   }
 }
 
-// Bytes from the first to the last element of a strided [rows, heads, d] tensor.
-size_t extent(long long rows, int heads, int d, int64_t row, int64_t head, int esz) {
-  return rows == 0 ? 0 : static_cast<size_t>((rows - 1) * row + (heads - 1) * head + d) * esz;
-}
+// A tensor [rows, heads, d] in bytes: runs of `run` bytes, r * row + g * head from its start. (Rows times a
+// stride may pass 64 bits: wide, and cut to more than any address.)
+using wide = __int128;
+struct Strided {
+  long long rows, heads;
+  int64_t row, head, run;
+  size_t bytes() const {  // from the first to the last
+    if (rows == 0) return 0;
+    const wide n = static_cast<wide>(rows - 1) * row + static_cast<wide>(heads - 1) * head + run;
+    return static_cast<size_t>(std::min(n, static_cast<wide>(1) << 62));
+  }
+};
 bool meet(const void* a, size_t na, const void* b, size_t nb) {
   const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
   return na > 0 && nb > 0 && x < y + nb && y < x + na;
+}
+wide floor_div(wide a, wide b) { return a / b - (a % b < 0); }  // b > 0
+
+// Whether a byte range [lo, hi) from the start of `t` meets one of its runs.
+bool meets_run(const Strided& t, wide lo, wide hi) {
+  for (long long g = 0; g < t.heads; ++g) {
+    // rows r with lo - run < r * row + g * head < hi
+    const wide at = static_cast<wide>(g) * t.head;
+    const wide first = floor_div(lo - t.run - at, t.row) + 1, last = floor_div(hi - 1 - at, t.row);
+    if (std::max(first, static_cast<wide>(0)) <= std::min(last, static_cast<wide>(t.rows - 1))) return true;
+  }
+  return false;
+}
+// Whether a run of `t` meets another one, or, with `at` bytes to a second tensor of the same form, one of that.
+bool runs_meet(const Strided& t, int64_t at) {
+  for (long long g = 1 - t.heads; g < t.heads; ++g) {
+    // row differences r with |at + r * row + g * head| < run
+    const wide off = static_cast<wide>(at) + static_cast<wide>(g) * t.head;
+    wide first = floor_div(-t.run - off, t.row) + 1, last = floor_div(t.run - 1 - off, t.row);
+    first = std::max(first, static_cast<wide>(1 - t.rows));
+    last = std::min(last, static_cast<wide>(t.rows - 1));
+    if (at == 0 && g == 0 && first == 0 && last == 0) continue;  // a run and itself
+    if (first <= last) return true;
+  }
+  return false;
 }
 
 dard_status prepare(const dard_prefix_evict_args* a, EvictParams& p) {
@@ -298,7 +331,7 @@ dard_status prepare(const dard_prefix_evict_args* a, EvictParams& p) {
         reinterpret_cast<uintptr_t>(a->weights_out)) & 3u) != 0)
     return report(DARD_ERR_ALIGN, "weights, kept and weights_out must be 4-byte aligned");
   const bool move = a->prefix_k || a->prefix_v || a->k_out || a->v_out;
-  size_t in = 0, out = 0;
+  Strided in{0, 0, 0, 0, 0}, out{0, 0, 0, 0, 0};
   if (move) {
     if (!a->prefix_k || !a->prefix_v || !a->k_out || !a->v_out)
       return report(DARD_ERR_NULL, "prefix_k, prefix_v, k_out and v_out come together");
@@ -315,19 +348,39 @@ dard_status prepare(const dard_prefix_evict_args* a, EvictParams& p) {
           static_cast<uintptr_t>(a->out_row_stride * esz) |
           static_cast<uintptr_t>(a->out_head_stride * esz)) & 15u) != 0)
       return report(DARD_ERR_ALIGN, "keys, values and their strides must be multiples of 16 bytes");
-    in = extent(a->prefix_len, a->hkv, a->head_dim, a->prefix_row_stride, a->prefix_head_stride, esz);
-    out = extent(a->keep, a->hkv, a->head_dim, a->out_row_stride, a->out_head_stride, esz);
+    const int64_t run = static_cast<int64_t>(a->head_dim) * esz;
+    in = {a->prefix_len, a->hkv, a->prefix_row_stride * esz, a->prefix_head_stride * esz, run};
+    out = {a->keep, a->hkv, a->out_row_stride * esz, a->out_head_stride * esz, run};
   }
   const size_t w_in = static_cast<size_t>((a->hkv - 1) * a->weights_stride + a->prefix_len) * 4;
   const size_t list = static_cast<size_t>(a->hkv) * a->keep * 4;
   const void* const ins[3] = {a->weights, a->prefix_k, a->prefix_v};
-  const size_t in_bytes[3] = {w_in, in, in};
+  const size_t in_bytes[3] = {w_in, in.bytes(), in.bytes()};
   const void* const outs[4] = {a->kept, a->weights_out, a->k_out, a->v_out};
-  const size_t out_bytes[4] = {list, a->weights_out ? list : 0, out, out};
+  const size_t out_bytes[4] = {list, a->weights_out ? list : 0, out.bytes(), out.bytes()};
   for (int i = 0; i < 3; ++i)
     for (int o = 0; o < 4; ++o)
       if (meet(ins[i], in_bytes[i], outs[o], out_bytes[o]))
         return report(DARD_ERR_VALUE, "an output overlaps an input");
+  // outputs and one another: by extent first; k_out and v_out may lie row by row beside each other
+  if (meet(a->kept, list, a->weights_out, out_bytes[1]))
+    return report(DARD_ERR_VALUE, "kept overlaps weights_out");
+  for (int i = 0; i < 2; ++i)
+    for (int o = 2; o < 4; ++o) {
+      const wide lo = static_cast<wide>(reinterpret_cast<uintptr_t>(outs[i])) -
+                      static_cast<wide>(reinterpret_cast<uintptr_t>(outs[o]));
+      if (meet(outs[i], out_bytes[i], outs[o], out_bytes[o]) && meets_run(out, lo, lo + static_cast<wide>(out_bytes[i])))
+        return report(DARD_ERR_VALUE, "kept or weights_out overlaps k_out or v_out");
+    }
+  if (move) {
+    if (out.row < (out.heads - 1) * out.head + out.run && out.head < static_cast<wide>(out.rows - 1) * out.row + out.run &&
+        runs_meet(out, 0))
+      return report(DARD_ERR_VALUE, "rows of k_out and v_out overlap: strides %lld and %lld",
+                    static_cast<long long>(a->out_row_stride), static_cast<long long>(a->out_head_stride));
+    const int64_t at = static_cast<int64_t>(reinterpret_cast<intptr_t>(a->v_out) - reinterpret_cast<intptr_t>(a->k_out));
+    if (at == 0 || (meet(a->k_out, out.bytes(), a->v_out, out.bytes()) && runs_meet(out, at)))
+      return report(DARD_ERR_VALUE, "k_out overlaps v_out");
+  }
   p.w = a->weights;
   p.w_stride = a->weights_stride;
   p.kept = a->kept;
