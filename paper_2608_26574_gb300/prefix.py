@@ -30,6 +30,8 @@ class PrefixCache:
         self.device = torch.device(device)
         if self.device.type != "cuda":
             raise ValueError("a CUDA device is needed")
+        if self.device.index is None:  # (the current device may be another one at a later call)
+            self.device = torch.device("cuda", torch.cuda.current_device())
         self.hq, self.hkv, self.head_dim, self.capacity, self.dtype = hq, hkv, head_dim, capacity, dtype
         self.status = status
         # a layer more than the model has: an eviction writes into the spare one, which then takes
