@@ -44,6 +44,7 @@ struct JoinParams {
   void* o;
   float* lse;
   int64_t rows;               // packed queries of all key/value heads
+  int64_t out_rows;           // rows times heads of o
   int32_t queries, tiles, nsplit, tile_rows;
 };
 

@@ -620,7 +620,8 @@ __global__ void __launch_bounds__(128, 6) prefix_join(const __grid_constant__ Jo
     }
     top = most;
   }
-  if (!in || row < 0) return;
+  // (a row outside o: the workspace was changed under the call)
+  if (!in || row < 0 || row >= p.out_rows) return;
   T* out = static_cast<T*>(p.o) + row * D + lane * kV;
   const float inv = 1.0f / (kRounded ? lo : l);
 #pragma unroll
@@ -725,7 +726,7 @@ cudaError_t launch_join_d(const JoinParams& j, cudaStream_t stream) {
 template <typename T>
 cudaError_t launch_join(const PrefixParams& p, int rows, cudaStream_t stream) {
   const JoinParams j{p.part, p.a.o, p.lse, static_cast<int64_t>(p.queries) * p.a.hkv,
-                     p.queries, p.tiles, p.nsplit, rows};
+                     static_cast<int64_t>(p.a.total_rows) * p.a.hq, p.queries, p.tiles, p.nsplit, rows};
   return p.a.head_dim == 64 ? launch_join_d<T, 64>(j, stream) : launch_join_d<T, 128>(j, stream);
 }
 

@@ -81,16 +81,22 @@ class PrefixCache:
     def attention(self, n_orig, block_start, block_len, shadow_len, state, prev_conf, shadow_src,
                   scale: float = 0.0, query_start=None) -> B.PrefixAttentionCall:
         """One step's prepared attention, for ``attend``: see ``PrefixAttentionCall``. (Calls of it share
-        its workspace: prepare one for each of those that overlap on the GPU.)"""
+        its workspace: prepare one for each of those that overlap on the GPU. A graph that captured it
+        needs it kept, like every tensor that it was given.)"""
         rows = sum(int(x) for x in n_orig) + sum(int(x) for x in shadow_len)
         need = B.dard_prefix_attention_workspace_size(rows, self.hq, self.hkv, self.head_dim, self.capacity)
-        return B.PrefixAttentionCall(n_orig, block_start, block_len, shadow_len, state, prev_conf,
-                                     shadow_src, scale, self.status, query_start,
-                                     self._scratch(need))
+        call = B.PrefixAttentionCall(n_orig, block_start, block_len, shadow_len, state, prev_conf,
+                                     shadow_src, scale, self.status, query_start, scratch := self._scratch(need))
+        call.scratch, call.prepared_on = scratch, B._raw_stream(self.device.index)
+        return call
 
     def attend(self, call: B.PrefixAttentionCall, layer: int, q, k, v, o, lse=None):
         """A layer's attention over the cache and the sequences' own rows."""
         call(q, k, v, o, self.keys(layer), self.values(layer), lse=lse)
+        # the workspace belongs to the stream of the preparation: on another one it must outlive the launch,
+        # though the call may be dropped right away
+        if call.scratch is not None and B._raw_stream(self.device.index) != call.prepared_on:
+            call.scratch.record_stream(torch.cuda.current_stream(self.device))
 
     def accumulate(self, layer: int, q, lse, scale: float = 0.0, decay: float = 1.0):
         """Adds the weights that q's rows spent on the layer's keys to ``decay`` times the earlier ones
