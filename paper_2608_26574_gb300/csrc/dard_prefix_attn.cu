@@ -16,9 +16,10 @@
 //              both would hold K up for V's stages).
 // TMEM: S ring [0, 256), O [256, 256 + D), P [384, 448), Q [448, 448 + D/2).
 // Bound by the chain of one tile's softmax (load, maximum over four warps, exponentials, hand-over):
-// about 1480 cycles per 128 x 128 scores, of which the tensor cores work 1024. Measured: 4608 rows of 28
-// heads on 4 of 128 over 32768 keys 1.44-1.57 ms (1390-1510 TFLOP/s); one token over 4096 keys 8.5 us with
-// its join. Sixteen softmax warps instead of eight: 1732 -> 1571 us when they came in.
+// about 1570 cycles per 128 x 128 scores, of which the tensor cores work 1024 and the special-function units
+// 500. Measured: 4608 rows of 28 heads on 4 of 128 over 32768 keys 1.54-1.63 ms (1340-1420 TFLOP/s); one token
+// over 4096 keys 8.8-9.8 us with its join. Sixteen softmax warps instead of eight: 1732 -> 1571 us when they
+// came in.
 //
 // Values that are not finite: the product with V multiplies every key of a tile by every query's
 // weight, and 0 times NaN is NaN. Keys of the prefix are seen by every query (rows behind its end

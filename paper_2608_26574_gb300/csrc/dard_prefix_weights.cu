@@ -16,8 +16,8 @@
 //              cycles a tile, more than the products do).
 // TMEM: S ring [0, 384), K [448, 448 + D/2). Bound by the issue slots of the exponentials and by TMEM,
 // which the products' A operand and the workers' reads share: about 915 cycles per 128 x 128 scores, of
-// which the tensor cores work 512. Measured: 4608 rows of 28 heads on 4 of 128 over 32768 keys 845-980 us
-// (1100-1280 TFLOP/s; the more, the more sums exact_sum32 forms again; 688 without the exponentials); with K
+// which the tensor cores work 512. Measured: 4608 rows of 28 heads on 4 of 128 over 32768 keys 850-990 us
+// (1090-1270 TFLOP/s; the more, the more sums exact_sum32 forms again; 688 without the exponentials); with K
 // in shared memory 960 instead of 870.
 // Each tile's sum is formed on its own and then added to the key's total (two levels: the
 // rounding of a long sum grows with the number of tiles, not of queries).
@@ -126,12 +126,14 @@ __device__ __forceinline__ float sum32(const uint32_t (&s)[32], const float* lse
 // its exponential at a score of 35 and more where small products follow large ones. p.large is a quarter of
 // the columns, whatever the prefix: keys that draw that much of their queries' weight reach it, and where lse is
 // over other keys (a part of them, a cache that has changed since) single terms may be as large as they like, and
-// are a key's whole sum. Such a key costs its CTA some 2 us for every 32 queries. Key by key for those that
-// need it, a lane for each of the 32 columns from `first` on; eight products at a time, their sums added up
+// are a key's whole sum. Such a key costs one of its CTA's warps 2 to 3 us for every 32 queries. Key by key for
+// those that need it, a lane for each of the 32 columns from `first` on; eight products at a time, their sums added up
 // with what the roundings cut off. 4608 rows of 28 heads over 32768 keys: 842 us without it, 845-850 while no
 // sum is that large, 887-983 with lse over 256 of the keys, where the largest error against 64 bits goes from
-// 3.8e-6 to 0.6e-6 (above all of the columns 868-931, an eighth 901-1018); one row over 4096 keys 7.7 instead
-// of 5.7 us. Not inlined: the loop that calls it has no register to spare (inlined 1630 us).
+// 3.8e-6 to 0.6e-6 (above all of the columns 868-931, an eighth 901-1018); one row over 4096 keys 8 instead
+// of 6 us. A key that takes half of every query's weight makes its CTA form nearly every sum again: 4608 rows over
+// 4096 keys 123 -> 690 us, over 32768 keys 851 -> 1283, 64 rows over 4096 8 -> 19. Not inlined: the loop that calls it has no
+// register to spare (inlined 1630 us).
 __device__ __forceinline__ float dot2(uint32_t a, uint32_t b, float c) {  // bf16 pairs
   c = fmaf(__uint_as_float(a << 16), __uint_as_float(b << 16), c);
   return fmaf(__uint_as_float(a & 0xffff0000u), __uint_as_float(b & 0xffff0000u), c);

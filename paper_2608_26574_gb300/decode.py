@@ -22,9 +22,9 @@ This drives the library's two entry points the way a diffusion LLM would, step a
 * With ``shared`` (the tokens of a prefix that every prompt follows: a system prompt, a document)
   ``decode`` runs the model over the prefix once, keeps its keys and values (``prefix.PrefixCache``),
   and the steps run on the sequences' own rows only: ``dard_prefix_attention`` in every layer. The
-  prefix's rows do not see the sequences then. With ``keep`` the cache is cut down to that many keys
-  of each head after every block, by the attention weight they have received (``dard_prefix_weights``,
-  ``dard_prefix_evict``).
+  prefix's rows do not see the sequences then. With ``keep`` a cache of more keys is cut down to that
+  many of each head after the first block, by the attention weight they have received
+  (``dard_prefix_weights``, ``dard_prefix_evict``); it does not grow again.
 
 Nothing here is on the measured hot path of ``bench.py``; it exists to run the path in its
 setting and to time whole steps (``python -m paper_2608_26574_gb300.decode``).
@@ -304,9 +304,9 @@ def step(model: DLLM, batch: Batch, thr: tuple[float, float], lam: float, p0: fl
 
 def check_status(model: DLLM, batch: Batch) -> None:
     """Raises when a step left outputs behind that are none: a wait that ran out in the attention,
-    the scoring, the experts or the prefix cache's calls, or a row that the experts' router could not place (a NaN or +inf
-    logit). (The scoring's own marks on rows, which have defined outputs, are the caller's to
-    read in ``batch.status``.)"""
+    the scoring, the experts or the prefix cache's calls, or a row that the experts' router could
+    not place (a NaN or +inf logit). (The scoring's own marks on rows, which have defined outputs,
+    are the caller's to read in ``batch.status``.)"""
     experts, rest = torch.cat([model.status, batch.status]).tolist()
     names = [n for n, on in (("TIMEOUT", (experts | rest) & B.STATUS_TIMEOUT),
                              ("INVALID_ROW", experts & B.STATUS_INVALID_ROW)) if on]
@@ -320,8 +320,8 @@ def decode(model: DLLM, prompts: list[np.ndarray], gen_len: int, block_len: int,
            max_steps: int = 64, min_progress: bool = False, record: bool = False,
            shared: np.ndarray | None = None, keep: int = 0, keep_ends: tuple[int, int] = (4, 32)):
     """Algorithm 1 block by block. ``shared``: tokens that every prompt follows, cached once;
-    ``keep``: the cache's keys per head after each block (0: all), ``keep_ends`` of them the first and
-    the last ones. Returns (generated tokens [n, gen_len], per-block steps,
+    ``keep``: the cache's keys per head after the first block (0: all), ``keep_ends`` of them the first
+    and the last ones. Returns (generated tokens [n, gen_len], per-block steps,
     per-step GPU microseconds, step records if ``record``). Raises after a step whose status
     words report a failure (``check_status``)."""
     dev = model.device
@@ -384,7 +384,7 @@ def main():
     ap.add_argument("--shared", type=int, default=0,
                     help="tokens of a prefix that every prompt follows, cached once")
     ap.add_argument("--keep", type=int, default=0,
-                    help="keys of the cached prefix kept per head after each block (0: all)")
+                    help="keys of the cached prefix kept per head after the first block (0: all)")
     ap.add_argument("--gen", type=int, default=128)
     ap.add_argument("--block", type=int, default=32)
     ap.add_argument("--layers", type=int, default=4)
