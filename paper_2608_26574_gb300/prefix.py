@@ -95,8 +95,9 @@ class PrefixCache:
         call(q, k, v, o, self.keys(layer), self.values(layer), lse=lse)
         # the workspace belongs to the stream of the preparation: on another one it must outlive the launch,
         # though the call may be dropped right away
-        if call.scratch is not None and B._raw_stream(self.device.index) != call.prepared_on:
-            call.scratch.record_stream(torch.cuda.current_stream(self.device))
+        scratch = getattr(call, "scratch", None)  # (a call that was made otherwise has its maker's)
+        if scratch is not None and B._raw_stream(self.device.index) != call.prepared_on:
+            scratch.record_stream(torch.cuda.current_stream(self.device))
 
     def accumulate(self, layer: int, q, lse, scale: float = 0.0, decay: float = 1.0):
         """Adds the weights that q's rows spent on the layer's keys to ``decay`` times the earlier ones

@@ -2,6 +2,7 @@
 import pytest
 import torch
 
+from paper_2608_26574_gb300 import binding as B
 from paper_2608_26574_gb300.prefix import PrefixCache
 
 from . import test_gpu_prefix_cache as C
@@ -37,4 +38,28 @@ def test_workspace_of_a_call_on_another_stream():
     busy = not side.query()
     assert busy and all(x.data_ptr() != at for x in others)
     side.synchronize()
+    assert torch.equal(o, want)
+
+
+def test_calls_that_the_cache_did_not_prepare():
+    """``attend`` takes any ``PrefixAttentionCall``, with its own workspace or none, and a graph may capture one
+    that was prepared on another stream."""
+    c, g = C._filled(layers=1, n=3000, capacity=3000)
+    q = torch.randn(3, 8, 64, generator=g, device=DEV).to(torch.bfloat16)
+    k, v = (torch.randn(3, 2, 64, generator=g, device=DEV).to(torch.bfloat16) for _ in range(2))
+    want, o, plain = (torch.empty_like(q) for _ in range(3))
+    call = c.attention([3], [0], [0], [0], None, None, None)
+    c.attend(call, 0, q, k, v, want)
+    ws = torch.empty(call._scratch[1], dtype=torch.uint8, device=DEV)
+    c.attend(B.PrefixAttentionCall([3], [0], [0], [0], None, None, None, workspace=ws), 0, q, k, v, o)
+    assert torch.equal(o, want)
+    c.attend(B.PrefixAttentionCall([3], [0], [0], [0], None, None, None), 0, q, k, v, plain)
+    assert (plain.float() - want.float()).abs().max() <= 2 ** -6 * want.float().abs().max()
+    o.zero_()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        c.attend(call, 0, q, k, v, o)
+    for _ in range(3):
+        graph.replay()
+    torch.cuda.synchronize()
     assert torch.equal(o, want)
