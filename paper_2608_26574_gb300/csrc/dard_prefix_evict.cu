@@ -262,42 +262,38 @@ __global__ void __launch_bounds__(kCopyThreads) evict_copy(const __grid_constant
   }
 }
 
-// A tensor [rows, heads, d] in bytes: runs of `run` bytes, r * row + g * head from its start. (Rows times a
-// stride may pass 64 bits: wide, and cut to more than any address.)
-using wide = __int128;
+// A tensor [rows, heads, d] in bytes: runs of `run` bytes, r * row + g * head from its start.
+constexpr int64_t kMostBytes = 1ll << 60;  // more than any tensor has
 struct Strided {
-  long long rows, heads;
-  int64_t row, head, run;
-  size_t bytes() const {  // from the first to the last
-    if (rows == 0) return 0;
-    const wide n = static_cast<wide>(rows - 1) * row + static_cast<wide>(heads - 1) * head + run;
-    return static_cast<size_t>(std::min(n, static_cast<wide>(1) << 62));
+  int64_t rows, heads, row, head, run;
+  bool fits() const {  // (rows times a stride may pass 64 bits)
+    return rows == 0 || static_cast<double>(rows - 1) * row + static_cast<double>(heads - 1) * head < kMostBytes;
   }
+  int64_t bytes() const { return rows == 0 ? 0 : (rows - 1) * row + (heads - 1) * head + run; }  // first to last
 };
 bool meet(const void* a, size_t na, const void* b, size_t nb) {
   const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
   return na > 0 && nb > 0 && x < y + nb && y < x + na;
 }
-wide floor_div(wide a, wide b) { return a / b - (a % b < 0); }  // b > 0
+int64_t floor_div(int64_t a, int64_t b) { return a / b - (a % b < 0); }  // b > 0
 
 // Whether a byte range [lo, hi) from the start of `t` meets one of its runs.
-bool meets_run(const Strided& t, wide lo, wide hi) {
-  for (long long g = 0; g < t.heads; ++g) {
+bool meets_run(const Strided& t, int64_t lo, int64_t hi) {
+  for (int64_t g = 0; g < t.heads; ++g) {
     // rows r with lo - run < r * row + g * head < hi
-    const wide at = static_cast<wide>(g) * t.head;
-    const wide first = floor_div(lo - t.run - at, t.row) + 1, last = floor_div(hi - 1 - at, t.row);
-    if (std::max(first, static_cast<wide>(0)) <= std::min(last, static_cast<wide>(t.rows - 1))) return true;
+    const int64_t at = g * t.head;
+    const int64_t first = floor_div(lo - t.run - at, t.row) + 1, last = floor_div(hi - 1 - at, t.row);
+    if (std::max<int64_t>(first, 0) <= std::min(last, t.rows - 1)) return true;
   }
   return false;
 }
 // Whether a run of `t` meets another one, or, with `at` bytes to a second tensor of the same form, one of that.
 bool runs_meet(const Strided& t, int64_t at) {
-  for (long long g = 1 - t.heads; g < t.heads; ++g) {
+  for (int64_t g = 1 - t.heads; g < t.heads; ++g) {
     // row differences r with |at + r * row + g * head| < run
-    const wide off = static_cast<wide>(at) + static_cast<wide>(g) * t.head;
-    wide first = floor_div(-t.run - off, t.row) + 1, last = floor_div(t.run - 1 - off, t.row);
-    first = std::max(first, static_cast<wide>(1 - t.rows));
-    last = std::min(last, static_cast<wide>(t.rows - 1));
+    const int64_t off = at + g * t.head;
+    const int64_t first = std::max(floor_div(-t.run - off, t.row) + 1, 1 - t.rows);
+    const int64_t last = std::min(floor_div(t.run - 1 - off, t.row), t.rows - 1);
     if (at == 0 && g == 0 && first == 0 && last == 0) continue;  // a run and itself
     if (first <= last) return true;
   }
@@ -327,6 +323,8 @@ dard_status prepare(const dard_prefix_evict_args* a, EvictParams& p) {
   const int esz = a->dtype == DARD_BF16 ? 2 : 4;
   if (!a->weights || !a->kept) return report(DARD_ERR_NULL, "weights or kept is NULL");
   if (a->weights_stride < a->prefix_len) return report(DARD_ERR_SHAPE, "weights_stride is below prefix_len");
+  if (static_cast<double>(a->hkv - 1) * a->weights_stride * 4 >= kMostBytes)
+    return report(DARD_ERR_SHAPE, "rows times weights_stride exceed 2^60 bytes");
   if (((reinterpret_cast<uintptr_t>(a->weights) | reinterpret_cast<uintptr_t>(a->kept) |
         reinterpret_cast<uintptr_t>(a->weights_out)) & 3u) != 0)
     return report(DARD_ERR_ALIGN, "weights, kept and weights_out must be 4-byte aligned");
@@ -351,13 +349,15 @@ dard_status prepare(const dard_prefix_evict_args* a, EvictParams& p) {
     const int64_t run = static_cast<int64_t>(a->head_dim) * esz;
     in = {a->prefix_len, a->hkv, a->prefix_row_stride * esz, a->prefix_head_stride * esz, run};
     out = {a->keep, a->hkv, a->out_row_stride * esz, a->out_head_stride * esz, run};
+    if (!in.fits() || !out.fits()) return report(DARD_ERR_SHAPE, "rows times strides exceed 2^60 bytes");
   }
   const size_t w_in = static_cast<size_t>((a->hkv - 1) * a->weights_stride + a->prefix_len) * 4;
   const size_t list = static_cast<size_t>(a->hkv) * a->keep * 4;
   const void* const ins[3] = {a->weights, a->prefix_k, a->prefix_v};
-  const size_t in_bytes[3] = {w_in, in.bytes(), in.bytes()};
+  const size_t in_bytes[3] = {w_in, static_cast<size_t>(in.bytes()), static_cast<size_t>(in.bytes())};
   const void* const outs[4] = {a->kept, a->weights_out, a->k_out, a->v_out};
-  const size_t out_bytes[4] = {list, a->weights_out ? list : 0, out.bytes(), out.bytes()};
+  const size_t out_bytes[4] = {list, a->weights_out ? list : 0, static_cast<size_t>(out.bytes()),
+                               static_cast<size_t>(out.bytes())};
   for (int i = 0; i < 3; ++i)
     for (int o = 0; o < 4; ++o)
       if (meet(ins[i], in_bytes[i], outs[o], out_bytes[o]))
@@ -367,13 +367,13 @@ dard_status prepare(const dard_prefix_evict_args* a, EvictParams& p) {
     return report(DARD_ERR_VALUE, "kept overlaps weights_out");
   for (int i = 0; i < 2; ++i)
     for (int o = 2; o < 4; ++o) {
-      const wide lo = static_cast<wide>(reinterpret_cast<uintptr_t>(outs[i])) -
-                      static_cast<wide>(reinterpret_cast<uintptr_t>(outs[o]));
-      if (meet(outs[i], out_bytes[i], outs[o], out_bytes[o]) && meets_run(out, lo, lo + static_cast<wide>(out_bytes[i])))
+      const int64_t lo = reinterpret_cast<intptr_t>(outs[i]) - reinterpret_cast<intptr_t>(outs[o]);
+      if (meet(outs[i], out_bytes[i], outs[o], out_bytes[o]) &&
+          meets_run(out, lo, lo + static_cast<int64_t>(out_bytes[i])))
         return report(DARD_ERR_VALUE, "kept or weights_out overlaps k_out or v_out");
     }
   if (move) {
-    if (out.row < (out.heads - 1) * out.head + out.run && out.head < static_cast<wide>(out.rows - 1) * out.row + out.run &&
+    if (out.row < (out.heads - 1) * out.head + out.run && out.head < (out.rows - 1) * out.row + out.run &&
         runs_meet(out, 0))
       return report(DARD_ERR_VALUE, "rows of k_out and v_out overlap: strides %lld and %lld",
                     static_cast<long long>(a->out_row_stride), static_cast<long long>(a->out_head_stride));

@@ -94,3 +94,16 @@ def test_outputs_against_brute_force(lib, monkeypatch):
         assert _refused(lib, a, monkeypatch) == want, (keep, hkv, esz, row, head, v - k, kept - k, w - k)
         seen.add(want)
     assert seen == {True, False}
+
+
+def test_tensors_beyond_any_address(lib, monkeypatch):
+    """Rows times strides that pass 64 bits would meet nothing, or anything."""
+    for change in ({"keep": 1 << 30, "out_row_stride": 1 << 36}, {"prefix_row_stride": 1 << 36},
+                   {"weights_stride": 1 << 62}):
+        a = _args(40, 2, 128, B.DARD_BF16, 256, 128, BASE, 1 << 55, 1 << 33, 1 << 34)
+        a.prefix_len = a.weights_stride = 1 << 30
+        for k, v in change.items():
+            setattr(a, k, v)
+        monkeypatch.setenv("DARD_TEST_FAIL_LAUNCH", "1")
+        assert lib.dard_prefix_evict(ctypes.byref(a), None) == 2
+        assert b"2^60" in lib.dard_last_error()
